@@ -74,7 +74,7 @@ def draw(rng):
     if op in ("ln_fwd", "ln_bwd"):
         cols = spread(rng, 32, 8192)
         workers = spread(rng, 1, 64)
-        rows = spread(rng, 1, max(1, min(4096, 50_000_000 // (cols * workers))))
+        rows = spread(rng, 1, max(1, min(4096, 25_000_000 // (cols * workers))))
         case = dict(op=op, workers=workers, rows=rows, cols=cols, dtype=rng.choice(("f32", "bf16")))
         if op == "ln_bwd":
             case["grads"] = rng.choice(("f32", "bf16"))
@@ -85,6 +85,8 @@ def draw(rng):
         wide = min(spread(rng, small, 8 * small), 21_000_000 // (batch * small))
         wide = max(wide, small) + rng.choice((0, 0, 1, 5))
         rows, cols = rng.choice(((small, wide), (wide, small)))
+        cost = STEPS * small * small * (3 * wide + small)
+        batch = max(1, min(batch, 270_000_000_000 // cost))
         return dict(op=op, batch=batch, rows=rows, cols=cols, dtype=rng.choice(("f32", "bf16")))
     head_dim = rng.choice((16, 32, 40, 64, 64, 80, 96, 128))
     kv_heads = rng.choice((1, 2, 4, 6))
@@ -92,8 +94,9 @@ def draw(rng):
     # with a single key the probability is one whatever the score, and dq and dk are zero but for rounding:
     # the backward pass is drawn from two keys on
     least = 2 if op == "attn_bwd" else 1
-    len_q = spread(rng, least, 4096)
-    len_kv = rng.choice((len_q, len_q, spread(rng, max(least, len_q // 2), min(4096, 2 * len_q))))
+    most = min(4096, math.isqrt(130_000_000 // heads))
+    len_q = spread(rng, least, most)
+    len_kv = rng.choice((len_q, len_q, spread(rng, max(least, len_q // 2), min(most, 2 * len_q))))
     batch = spread(rng, 1, max(1, min(32, 100_000_000 // (len_q * len_kv * heads))))
     return dict(op=op, batch=batch, len_q=len_q, len_kv=len_kv, heads=heads, kv_heads=kv_heads, head_dim=head_dim,
                 causal=rng.random() < 0.6, ragged=rng.random() < 0.3, packed=len_q == len_kv and rng.random() < 0.5)
