@@ -394,6 +394,119 @@ int cdgrab_step_noalloc(int m, long long d, int dtype, const void *grads_dev, fl
  * Not to be called while a stream capture is open (it synchronises). */
 int cdgrab_noalloc_status(void);
 
+/* ------------------------------------------------------------------------------------------------
+ * Training operators beside the order server.  They make the stale gradients that are balanced
+ * (layer norm and attention, forward and backward) and use the averaged gradient that
+ * cdgrab_step_mean returns (the orthogonalised update).  None of them needs a handle.
+ *
+ * All pointers are DEVICE pointers on the current device unless said otherwise; tensors are
+ * CDGRAB_F32 or CDGRAB_BF16.  Strides are in elements.  Every call only enqueues work on
+ * `stream`; none allocates, and the caller owns the workspace (contents undefined before and
+ * after; it may be reused by a later call on the same stream).  Sums, statistics and
+ * accumulators are held in 32 bits; results do not depend on the order in which blocks run.
+ * CDGRAB_ERR_INVALID (nothing enqueued): a NULL pointer that is not allowed, a size, stride or
+ * alignment outside the stated range, a workspace that is too small.  CDGRAB_ERR_DEVICE: the
+ * current device is no sm_100.  CDGRAB_ERR_CUDA: a launch was refused.
+ */
+
+/*
+ * Layer normalisation over the last axis:  y = (x - mean) * rstd * weight + bias,
+ * mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps).
+ *   rows, cols   rows >= 0 (0: nothing to do), cols >= 1
+ *   dtype        type of x and y
+ *   x, y         [rows] rows of cols values, row starts x_stride / y_stride (>= cols) apart; y may be x
+ *   weight, bias float [cols]; NULL: 1 and 0
+ *   eps          >= 0
+ *   mean, rstd   float [rows], the statistics that the backward pass reads; both may be NULL
+ */
+int cdgrab_layer_norm_forward(long long rows, int cols, int dtype, const void *x_dev, long long x_stride,
+                              const float *weight_dev, const float *bias_dev, float eps, void *y_dev,
+                              long long y_stride, float *mean_dev, float *rstd_dev, void *stream);
+
+/*
+ * Its backward pass for the rows of m workers, rows_per_worker consecutive rows each:
+ *   n = (x - mean) * rstd,  g = dy * weight,
+ *   dx = rstd * (g - sum_c g / cols - n * (sum_c g n) / cols)            every row
+ *   dweight[i] = sum over worker i's rows of dy * n,   dbias[i] = the sum of dy
+ * so that a worker's gradient of the two parameters lands in its row of the gather buffer.
+ *   dy, x, dx    of `dtype`, row strides >= cols; dx may be dy or x, or NULL (not computed)
+ *   mean, rstd   float [m * rows_per_worker] from the forward pass
+ *   dweight, dbias  of grad_dtype, worker i's cols values start at i * worker_stride; either may be
+ *                NULL (not computed).  With rows_per_worker = 0 they are set to zero.
+ *                worker_stride >= cols where m > 1.  The two may lie side by side in one row.
+ *   workspace    16-byte aligned, cdgrab_layer_norm_workspace_bytes(m, rows_per_worker, cols) bytes
+ *                (-1 for invalid sizes)
+ */
+long long cdgrab_layer_norm_workspace_bytes(int m, long long rows_per_worker, int cols);
+int cdgrab_layer_norm_backward(int m, long long rows_per_worker, int cols, int dtype, const void *dy_dev,
+                               long long dy_stride, const void *x_dev, long long x_stride,
+                               const float *weight_dev, const float *mean_dev, const float *rstd_dev,
+                               void *dx_dev, long long dx_stride, int grad_dtype, void *dweight_dev,
+                               void *dbias_dev, long long worker_stride, void *workspace_dev,
+                               long long workspace_bytes, void *stream);
+
+/*
+ * Softmax attention, bf16 with 32-bit sums:  o = softmax(scale * q k^T) v.
+ * Query head h reads key head h / (heads / kv_heads).  Sequence b uses its first q_lens[b] queries
+ * and kv_lens[b] keys (NULL: all).  The causal rule aligns the ends of the two: query i sees key j
+ * iff j <= i + (kv_len - q_len).  Rows that see no key, and rows past q_lens[b], have o = 0,
+ * lse = -infinity and zero gradients; what lies in masked places (NaN included) is never used.
+ *
+ * Shape (HOST struct): strides of q, k, v, o and of the gradients, in elements, for batch, token
+ * and head; the head's values are contiguous.
+ *   batch, len_q, len_kv   >= 0;  heads >= 1 a multiple of kv_heads >= 1
+ *   head_dim     a multiple of 8 from 8 to 128
+ *   strides      multiples of 8 and every base address a multiple of 16 bytes, as the bulk copies need;
+ *                token and head strides at least head_dim where that axis is longer than 1
+ */
+typedef struct {
+  int batch, len_q, len_kv, heads, kv_heads, head_dim;
+  int causal;                /* 0 or 1 */
+  float scale;               /* finite */
+  long long q_stride[3], k_stride[3], v_stride[3], o_stride[3];      /* batch, token, head */
+  long long do_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];  /* backward pass only */
+} cdgrab_attention_shape;
+
+/*   lse   float [batch][heads][len_q]: natural log of the row's sum of exp(scale q k^T)  */
+int cdgrab_attention_forward(const cdgrab_attention_shape *shape, const void *q_dev, const void *k_dev,
+                             const void *v_dev, const int32_t *q_lens_dev, const int32_t *kv_lens_dev,
+                             void *o_dev, float *lse_dev, void *stream);
+
+/*
+ * Its backward pass.  The probabilities are recomputed from lse, never stored:
+ *   p = exp(scale q k^T - lse),  delta = sum_d do * o,  ds = p * (do v^T - delta),
+ *   dq = scale ds k,  dk = scale sum over the key head's queries of ds^T q,  dv = likewise p^T do.
+ *   o, lse     from the forward pass;  do: the gradient of o;  dq, dk, dv: outputs, every element written
+ *   workspace  16-byte aligned, cdgrab_attention_workspace_bytes(shape) bytes (-1 for an invalid shape)
+ */
+long long cdgrab_attention_workspace_bytes(const cdgrab_attention_shape *shape);
+int cdgrab_attention_backward(const cdgrab_attention_shape *shape, const void *do_dev, const void *q_dev,
+                              const void *k_dev, const void *v_dev, const void *o_dev, const float *lse_dev,
+                              const int32_t *q_lens_dev, const int32_t *kv_lens_dev, void *dq_dev, void *dk_dev,
+                              void *dv_dev, void *workspace_dev, long long workspace_bytes, void *stream);
+
+/*
+ * The orthogonalised update of a batch of matrices by Newton-Schulz products:
+ *   X = G / (|G|_F + eps), then `steps` times   X <- a X + (b A + c A A) X,   A = X X^T
+ * (of the transposed matrix where rows > cols), which drives the singular values towards one.
+ *   batch, rows, cols   >= 0 (nothing to do where any is 0);  steps 1 to 64
+ *   dtype    of G: [batch] matrices g_batch_stride apart, rows of cols contiguous values g_stride apart
+ *   coeffs   HOST float [3]: a, b, c
+ *   o        bf16 output, strides likewise; o may not overlap G
+ *   workspace  16-byte aligned, cdgrab_orthogonalise_workspace_bytes(batch, rows, cols) bytes (-1: invalid)
+ */
+long long cdgrab_orthogonalise_workspace_bytes(int batch, int rows, int cols);
+int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, const void *g_dev, long long g_batch_stride,
+                         long long g_stride, int steps, const float *coeffs, float eps, void *o_dev,
+                         long long o_batch_stride, long long o_stride, void *workspace_dev,
+                         long long workspace_bytes, void *stream);
+
+/* What the training operators' kernels reported on the current device since the last call of this
+ * function: CDGRAB_OK, or CDGRAB_ERR_TIMEOUT when a bounded device-side wait expired (the outputs of
+ * the calls since then are not valid).  Synchronises the device and clears the word; not to be called
+ * while a stream capture is open. */
+int cdgrab_operators_status(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,14 @@ PATH_AUTO, PATH_FUSED, PATH_FMA, PATH_UMMA = 0, 1, 2, 3
 KERNEL_KINDS = ("gram", "combine", "scan", "update", "fused", "logreg")
 PATH_NAMES = {PATH_FUSED: "fused", PATH_FMA: "fma", PATH_UMMA: "umma", 4: "independent", 5: "literal"}
 
+
+class AttentionShape(C.Structure):
+    """cdgrab_attention_shape: sizes, and strides in elements for (batch, token, head)."""
+    _fields_ = [(n, C.c_int) for n in ("batch", "len_q", "len_kv", "heads", "kv_heads", "head_dim", "causal")] + \
+               [("scale", C.c_float)] + \
+               [(n + "_stride", C.c_longlong * 3) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")]
+
+
 # name -> (restype, argtypes); the single list of what include/cdgrab.h declares
 SIGNATURES = {
     "cdgrab_create": (C.c_int, [C.c_int, C.c_int, C.c_longlong, C.c_int, C.POINTER(C.c_void_p)]),
@@ -67,6 +75,22 @@ SIGNATURES = {
     "cdgrab_step_noalloc": (C.c_int, [C.c_int, C.c_longlong, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                       C.c_void_p]),
     "cdgrab_noalloc_status": (C.c_int, []),
+    "cdgrab_layer_norm_forward": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p,
+                                            C.c_void_p, C.c_float, C.c_void_p, C.c_longlong, C.c_void_p, C.c_void_p,
+                                            C.c_void_p]),
+    "cdgrab_layer_norm_workspace_bytes": (C.c_longlong, [C.c_int, C.c_longlong, C.c_int]),
+    "cdgrab_layer_norm_backward": (C.c_int, [C.c_int, C.c_longlong, C.c_int, C.c_int, C.c_void_p, C.c_longlong,
+                                             C.c_void_p, C.c_longlong, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_longlong, C.c_int, C.c_void_p, C.c_void_p, C.c_longlong, C.c_void_p,
+                                             C.c_longlong, C.c_void_p]),
+    "cdgrab_attention_forward": (C.c_int, [C.POINTER(AttentionShape)] + [C.c_void_p] * 8),
+    "cdgrab_attention_workspace_bytes": (C.c_longlong, [C.POINTER(AttentionShape)]),
+    "cdgrab_attention_backward": (C.c_int, [C.POINTER(AttentionShape)] + [C.c_void_p] * 12 + [C.c_longlong, C.c_void_p]),
+    "cdgrab_orthogonalise_workspace_bytes": (C.c_longlong, [C.c_int, C.c_int, C.c_int]),
+    "cdgrab_orthogonalise": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_longlong, C.c_longlong,
+                                       C.c_int, C.POINTER(C.c_float), C.c_float, C.c_void_p, C.c_longlong,
+                                       C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p]),
+    "cdgrab_operators_status": (C.c_int, []),
 }
 
 _lib = None
@@ -321,6 +345,216 @@ def herding_objective(z, perms, stream=None) -> float:
     _check(lib().cdgrab_herding_objective(_ptr(z), _ptr(perms), m, n, d, _ptr(ws), nbytes, _ptr(out),
                                           _stream_ptr(stream)), "cdgrab_herding_objective")
     return float(out.item())
+
+
+# ---- training operators --------------------------------------------------------------------------
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _code(t, name: str) -> int:
+    import torch
+    _want(t.dtype in (torch.float32, torch.bfloat16), f"{name}: float32 or bfloat16, not {t.dtype}")
+    return F32 if t.dtype == torch.float32 else BF16
+
+
+class _OnStream:
+    """Where an operator runs: the handle its launches go to, and allocation of its outputs and
+    scratch from that stream's pool (so that freeing them is ordered after the launches)."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+        dev = torch.cuda.current_device()
+        for t in tensors:
+            _want(t is None or (t.is_cuda and t.device.index == dev), "tensors have to be on the current CUDA device")
+        self.torch, self.other = torch, None
+        if stream is None:
+            self.handle = torch.cuda.current_stream().cuda_stream
+        else:
+            self.handle = stream.cuda_stream
+            if self.handle != torch.cuda.current_stream().cuda_stream:
+                self.other = stream
+        self.device = torch.device("cuda", dev)
+
+    def empty(self, shape, dtype):
+        if self.other is None:
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+        with self.torch.cuda.stream(self.other):
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+
+    def scratch(self, nbytes: int):
+        return self.empty((max(16, nbytes),), self.torch.uint8)
+
+
+def _rows_of(t, name: str, rows=None, cols=None):
+    """Row stride of a [rows][cols] tensor with contiguous rows."""
+    _want(t.dim() == 2 and (rows is None or tuple(t.shape) == (rows, cols)), f"{name}: shape {tuple(t.shape)}")
+    _want(t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: the values of a row have to be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t, name: str, n: int):
+    import torch
+    if t is None:
+        return None
+    _want(t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous(),
+          f"{name}: a contiguous float32 tensor [{n}]")
+    return t.data_ptr()
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None):
+    """Layer normalisation of the rows of x [rows][cols] (float32 or bfloat16; rows may be strided) with
+    float32 weight and bias [cols] or None.  Returns (y, mean, rstd)."""
+    import torch
+    on = _OnStream(stream, x, weight, bias, out)
+    xs = _rows_of(x, "x")
+    rows, cols = x.shape
+    code = _code(x, "x")
+    w, b = _vector(weight, "weight", cols), _vector(bias, "bias", cols)
+    y = on.empty((rows, cols), x.dtype) if out is None else out
+    _want(y.dtype == x.dtype, "out: the type of x")
+    stats = on.empty((2, rows), torch.float32)
+    base = stats.data_ptr()
+    _check(lib().cdgrab_layer_norm_forward(rows, cols, code, x.data_ptr(), xs, w, b, eps, y.data_ptr(),
+                                           _rows_of(y, "out", rows, cols), base, base + 4 * rows, on.handle),
+           "cdgrab_layer_norm_forward")
+    return y, stats[0], stats[1]
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=None, dx=None, stream=None):
+    """Backward pass of layer_norm_forward for m workers' rows: dy, x [m * rows][cols]; dweight and dbias
+    [m][cols] (float32 or bfloat16, equal row strides, views into the gather buffer as a rule) receive each
+    worker's own sums, either may be None.  Returns dx."""
+    on = _OnStream(stream, dy, x, weight, mean, rstd, dweight, dbias, dx)
+    rows, cols = x.shape
+    _want(dy.dtype == x.dtype, "dy: the type of x")
+    code = _code(x, "x")
+    g = dweight if dweight is not None else dbias
+    m = 1 if g is None else g.shape[0]
+    _want(m >= 1 and rows % m == 0, f"{rows} rows are not {m} workers' equal shares")
+    gcode, ws = F32, cols
+    if g is not None:
+        gcode, ws = _code(g, "dweight, dbias"), _rows_of(g, "dweight, dbias", m, cols)
+        for t in (dweight, dbias):
+            _want(t is None or (t.dtype == g.dtype and _rows_of(t, "dweight, dbias", m, cols) == ws),
+                  "dweight and dbias: one type and one row stride")
+    if dx is None:
+        dx = on.empty((rows, cols), x.dtype)
+    _want(dx.dtype == x.dtype, "dx: the type of x")
+    L = lib()
+    nbytes = L.cdgrab_layer_norm_workspace_bytes(m, rows // m, cols)
+    scratch = on.scratch(nbytes)
+    _check(L.cdgrab_layer_norm_backward(
+        m, rows // m, cols, code, dy.data_ptr(), _rows_of(dy, "dy", rows, cols), x.data_ptr(), _rows_of(x, "x"),
+        _vector(weight, "weight", cols), _vector(mean, "mean", rows), _vector(rstd, "rstd", rows), dx.data_ptr(),
+        _rows_of(dx, "dx", rows, cols), gcode, None if dweight is None else dweight.data_ptr(),
+        None if dbias is None else dbias.data_ptr(), ws, scratch.data_ptr(), scratch.numel(), on.handle),
+        "cdgrab_layer_norm_backward")
+    return dx
+
+
+def _attention_shape(q, k, v, causal, scale):
+    import torch
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        _want(t.dtype == torch.bfloat16 and t.dim() == 4, f"{name}: a bfloat16 tensor [batch][token][head][head_dim]")
+    b, tq, h, d = q.shape
+    _, tk, hk, _ = k.shape
+    _want(tuple(k.shape) == (b, tk, hk, d) and tuple(v.shape) == (b, tk, hk, d), "q, k and v do not go together")
+    sh = AttentionShape(b, tq, tk, h, hk, d, int(bool(causal)), d ** -0.5 if scale is None else scale)
+    _strides(sh.q_stride, q, "q")
+    _strides(sh.k_stride, k, "k")
+    _strides(sh.v_stride, v, "v")
+    return sh
+
+
+def _strides(field, t, name: str, like=None):
+    _want(like is None or (t.shape == like.shape and t.dtype == like.dtype), f"{name}: shape {tuple(t.shape)}, {t.dtype}")
+    s = t.stride()
+    _want(s[3] == 1 or t.shape[3] <= 1, f"{name}: the values of a head have to be contiguous")
+    field[0], field[1], field[2] = s[:3]
+    # an axis of length one has no stride of its own
+    for i in range(3):
+        if t.shape[i] <= 1:
+            field[i] = (field[i] + 7) & ~7
+
+
+def _lens(t, name: str, batch: int):
+    import torch
+    if t is None:
+        return None
+    _want(t.dtype == torch.int32 and tuple(t.shape) == (batch,) and t.is_contiguous(), f"{name}: an int32 tensor [{batch}]")
+    return t.data_ptr()
+
+
+def attention_forward(q, k, v, causal: bool = False, scale: float | None = None, q_lens=None, kv_lens=None, out=None,
+                      stream=None):
+    """Softmax attention of q [b][t_q][h][d] with k, v [b][t_kv][h_kv][d], bfloat16, any strides that are
+    multiples of 8 (slices of one projection's output).  scale: d**-0.5 by default.  q_lens, kv_lens: int32
+    [b], the tokens in use.  Returns (o, lse): o like q, lse float32 [b][h][t_q]."""
+    import torch
+    on = _OnStream(stream, q, k, v, q_lens, kv_lens, out)
+    sh = _attention_shape(q, k, v, causal, scale)
+    o = on.empty(q.shape, q.dtype) if out is None else out
+    _strides(sh.o_stride, o, "out", q)
+    lse = on.empty((sh.batch, sh.heads, sh.len_q), torch.float32)
+    _check(lib().cdgrab_attention_forward(C.byref(sh), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                          _lens(q_lens, "q_lens", sh.batch), _lens(kv_lens, "kv_lens", sh.batch),
+                                          o.data_ptr(), lse.data_ptr(), on.handle), "cdgrab_attention_forward")
+    return o, lse
+
+
+def attention_backward(do, q, k, v, o, lse, causal: bool = False, scale: float | None = None, q_lens=None,
+                       kv_lens=None, dq=None, dk=None, dv=None, stream=None):
+    """Backward pass of attention_forward from its outputs o and lse and the gradient do of o.
+    Returns (dq, dk, dv); destinations may be given (views of one buffer as a rule)."""
+    import torch
+    on = _OnStream(stream, do, q, k, v, o, lse, q_lens, kv_lens, dq, dk, dv)
+    sh = _attention_shape(q, k, v, causal, scale)
+    _want(lse.dtype == torch.float32 and tuple(lse.shape) == (sh.batch, sh.heads, sh.len_q) and lse.is_contiguous(),
+          "lse: a contiguous float32 tensor [batch][heads][len_q]")
+    dq = on.empty(q.shape, q.dtype) if dq is None else dq
+    dk = on.empty(k.shape, k.dtype) if dk is None else dk
+    dv = on.empty(v.shape, v.dtype) if dv is None else dv
+    for field, t, name, like in ((sh.o_stride, o, "o", q), (sh.do_stride, do, "do", q), (sh.dq_stride, dq, "dq", q),
+                                 (sh.dk_stride, dk, "dk", k), (sh.dv_stride, dv, "dv", v)):
+        _strides(field, t, name, like)
+    L = lib()
+    nbytes = L.cdgrab_attention_workspace_bytes(C.byref(sh))
+    scratch = on.scratch(nbytes)
+    _check(L.cdgrab_attention_backward(
+        C.byref(sh), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+        _lens(q_lens, "q_lens", sh.batch), _lens(kv_lens, "kv_lens", sh.batch), dq.data_ptr(), dk.data_ptr(),
+        dv.data_ptr(), scratch.data_ptr(), scratch.numel(), on.handle), "cdgrab_attention_backward")
+    return dq, dk, dv
+
+
+def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, stream=None):
+    """The orthogonalised update of a gradient g [rows][cols] or [batch][rows][cols] (float32 or bfloat16):
+    `steps` Newton-Schulz products on g / (|g| + eps).  Returns a bfloat16 tensor of g's shape."""
+    import torch
+    on = _OnStream(stream, g, out)
+    _want(g.dim() in (2, 3), "g: [rows][cols] or [batch][rows][cols]")
+    o = on.empty(g.shape, torch.bfloat16) if out is None else out
+    _want(o.dtype == torch.bfloat16 and o.shape == g.shape, "out: a bfloat16 tensor of g's shape")
+    g3, o3 = (t if t.dim() == 3 else t.unsqueeze(0) for t in (g, o))
+    batch, rows, cols = g3.shape
+    _want(len(coeffs) == 3, "coeffs: three numbers")
+    for t, name in ((g3, "g"), (o3, "out")):
+        _want(cols <= 1 or t.stride(2) == 1, f"{name}: the values of a row have to be contiguous")
+    row = [t.stride(1) if rows > 1 else max(cols, t.stride(1)) for t in (g3, o3)]
+    L = lib()
+    nbytes = L.cdgrab_orthogonalise_workspace_bytes(batch, rows, cols)
+    scratch = on.scratch(nbytes)
+    _check(L.cdgrab_orthogonalise(batch, rows, cols, _code(g, "g"), g.data_ptr(), g3.stride(0), row[0], steps,
+                                  (C.c_float * 3)(*coeffs), eps, o.data_ptr(), o3.stride(0), row[1],
+                                  scratch.data_ptr(), scratch.numel(), on.handle), "cdgrab_orthogonalise")
+    return o
+
+
+def operators_status() -> int:
+    """cdgrab_operators_status: what the training operators' kernels reported so far (read and cleared)."""
+    return int(lib().cdgrab_operators_status())
 
 
 class ShardedCdGrab:

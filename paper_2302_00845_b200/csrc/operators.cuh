@@ -1,0 +1,32 @@
+// Shared by the training operators (layer norm, attention, orthogonalised update): the device they
+// run on, their status word, and small device helpers.
+#pragma once
+
+#include "common.cuh"
+
+struct CdgOpsDevice {
+  int sms;        // multiprocessors
+  int *status;    // the operators' device status word (CDG_ST_* bits)
+};
+// the current device, looked up once per device; CDGRAB_ERR_DEVICE when it is no sm_100
+int cdg_ops_device(const CdgOpsDevice **out);
+
+inline bool cdg_aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// the error of the launches since the last check, as a CDGRAB_* code
+inline int cdg_launch_rc(cudaError_t e = cudaSuccess) {
+  const cudaError_t l = cudaGetLastError();
+  return e == cudaSuccess && l == cudaSuccess ? CDGRAB_OK : CDGRAB_ERR_CUDA;
+}
+
+#ifdef __CUDACC__
+template <typename T> __device__ __forceinline__ T cdg_cast(float v);
+template <> __device__ __forceinline__ float cdg_cast<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 cdg_cast<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ float cdg_warp_sum(float v) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
+#endif
