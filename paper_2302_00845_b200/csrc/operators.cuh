@@ -29,4 +29,19 @@ __device__ __forceinline__ float cdg_warp_sum(float v) {
   for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
   return v;
 }
+
+// Launch that may be scheduled while its predecessor in the stream still runs; every thread of the
+// kernel has to call cdg_grid_dep_wait() before it reads or writes global memory.
+template <typename... KArgs, typename... Args>
+inline cudaError_t cdg_ops_launch(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t st,
+                                  Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
 #endif
