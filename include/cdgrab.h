@@ -450,11 +450,12 @@ int cdgrab_layer_norm_backward(int m, long long rows_per_worker, int cols, int d
  * Query head h reads key head h / (heads / kv_heads).  Sequence b uses its first q_lens[b] queries
  * and kv_lens[b] keys (NULL: all).  The causal rule aligns the ends of the two: query i sees key j
  * iff j <= i + (kv_len - q_len).  Rows that see no key, and rows past q_lens[b], have o = 0,
- * lse = -infinity and zero gradients; what lies in masked places (NaN included) is never used.
+ * lse = -infinity and zero gradients.  What lies past a length (NaN included) is never used; a NaN or an
+ * infinity in a row in use spoils the rows that see it and may spoil others.
  *
  * Shape (HOST struct): strides of q, k, v, o and of the gradients, in elements, for batch, token
  * and head; the head's values are contiguous.
- *   batch, len_q, len_kv   >= 0;  heads >= 1 a multiple of kv_heads >= 1
+ *   batch, len_q, len_kv   >= 0, lengths up to 4,194,304;  heads >= 1 a multiple of kv_heads >= 1
  *   head_dim     a multiple of 8 from 8 to 128
  *   strides      multiples of 8 and every base address a multiple of 16 bytes, as the bulk copies need;
  *                token and head strides at least head_dim where that axis is longer than 1

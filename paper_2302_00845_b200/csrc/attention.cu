@@ -1,111 +1,841 @@
-// Softmax attention, forward and backward, bf16 operands with 32-bit sums.
+// Softmax attention, forward and backward, on the 5th-generation tensor cores: bf16 operands, 32-bit sums.
 //
 // Forward:   s = scale q k^T,  lse = log sum_j exp(s_j),  o = sum_j exp(s_j - lse) v_j.
 // Backward:  p = exp(s - lse),  delta = sum_d do o,  ds = p (do v^T - delta),
 //            dq = scale ds k,  dk = scale ds^T q,  dv = p^T do  (dk, dv summed over the query heads of a key head).
+//
+// Common to the three kernels: tiles of 128 x 128 scores.  A bulk-copy warp fills rings of shared-memory
+// tiles (panels of 64 head dimensions, 128-byte swizzle, zeros past the tensor's ends), a matrix warp
+// issues the products, and the other warps read scores from tensor memory, one row per thread, and write
+// probabilities (or their gradients) back to it as the bf16 operand of the next product.  Nothing of the
+// size of the score matrix ever leaves the SM.  Rounding a probability to bf16 changes it by at most
+// 2^-8 relative, as much as the output's own rounding; running maxima, sums and accumulators are fp32.
+//
+// Masking: a score outside the visible set is replaced, not added to, so whatever lies there (NaN
+// included) is never used; rows of a tile past a sequence's length are zeroed in shared memory where they
+// are the summed index of a product, because 0 x NaN would not be 0.
 #include <math.h>
 
-#include "operators.cuh"
+#include "tensor_core.cuh"
 
 namespace {
 
 typedef __nv_bfloat16 bf16;
 
+constexpr int kT = 128;                       // edge of a score tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
 struct Sizes {
   int batch, tq, tk, heads, group, dim, causal;
-  float scale;
+  float scale;               // as given
+  float a;                   // |scale| log2 e, at least 1e-30: a scale of 0 still leaves masked scores at -infinity
+  int negative;              // scale < 0
+  int shared;                // bits q, k, v, do: one for the whole batch (a batch stride of 0)
   const int *q_lens, *kv_lens;
+  int *status;
+};
+struct View { bf16 *p; long long b, t, h; };
+
+enum { kQ = 1, kK = 2, kV = 4, kDo = 8 };
+__device__ __forceinline__ int batch_of(const Sizes &z, int which, int b) { return z.shared & which ? 0 : b; }
+__device__ __forceinline__ int used(const int *lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// one tile of 128 tokens of one head: NP panels of 64 head dimensions
+template <int NP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int token, int head, int batch, uint32_t bar) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) tma_load_4d(dst + p * kT * 128, map, p * 64, token, head, batch, bar);
+}
+// zeroes rows from..127 of a tile (a whole warp)
+template <int NP>
+__device__ __forceinline__ void zero_rows(uint8_t *tile, int from) {
+  const int lane = threadIdx.x & 31;
+  for (int r = from + (lane >> 3); r < kT; r += 4)
+#pragma unroll
+    for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4 *>(tile + p * kT * 128 + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+  tc_proxy_fence();
+  __syncwarp();
+}
+
+// products of one tile, issued by one thread.  128-row operands, DP = 64 NP head dimensions.
+// scores: D[128][128] = A B^T over the head dimension
+template <int NP>
+__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
+  constexpr uint32_t idesc = tc_idesc(true, kT, kT, false, false);
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      tc_mma(d, tc_desc_k(a + p * kT * 128 + k * 32), tc_desc_k(b + p * kT * 128 + k * 32), idesc, p > 0 || k > 0);
+}
+// weighted rows: D[128][DP] (+)= W B, W a 128 x 128 bf16 operand in tensor memory whose columns 64..127
+// start `half` 32-bit columns after the first, B 128 rows of DP values
+template <int NP>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, uint32_t half, uint32_t b, bool add) {
+  constexpr uint32_t idesc = tc_idesc(true, kT, 64 * NP, false, true);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    tc_mma_ta(d, w + (k >> 2) * half + (k & 3) * 8, tc_desc_mn(b + k * 2048, kT * 128), idesc, add || k > 0);
+}
+
+// 32 rows of DP bf16 values from registers to memory through this warp's part of a tile: each lane
+// brings its row, the warp writes whole rows
+template <int NP>
+__device__ __forceinline__ void stage_row(uint8_t *tile, int row, int c0, const uint32_t (&w)[16]) {   // 32 values from column c0
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int chunk = (c0 >> 3) + i;
+    *reinterpret_cast<uint4 *>(tile + (chunk >> 3) * kT * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) =
+        make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+template <int NP>
+__device__ __forceinline__ void write_rows(const uint8_t *tile, int row0, int token0, int tokens, const Sizes &z, bf16 *dst, long long stride) {
+  const int lane = threadIdx.x & 31, per = NP * 8;
+  for (int i = lane; i < 32 * per; i += 32) {
+    const int r = row0 + i / per, chunk = i % per;
+    if (token0 + r < tokens && chunk * 8 < z.dim)
+      *reinterpret_cast<uint4 *>(dst + (long long)(token0 + r) * stride + chunk * 8) =
+          *reinterpret_cast<const uint4 *>(tile + (chunk >> 3) * kT * 128 + r * 128 + (((chunk & 7) ^ (r & 7)) << 4));
+  }
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+// One CTA per 256 queries of a head: two tiles of 128 that share every key and value tile, so that while
+// one tile's four warps are at their exponentials the other's products run.
+//   warps 0-3, 4-7   softmax of query tile 0, 1        warp 8  bulk copies        warp 9  products
+// Tensor memory: scores S_t at 128 t; head dimensions up to 64: O_t at 256 + 64 t and P_t apart at
+// 384 + 64 t, so that S of the next key tile is computed while P of this one is formed; above 64: O_t at
+// 256 + 128 t and P_t over S_t.
+// The maximum that the exponents refer to is only raised when it has grown by more than 2^8 (P then
+// stays below 256, and the sum and O below that times the length): rescaling O is rare.
+constexpr int kFwdThreads = 384;       // three warpgroups: 168 registers a thread at launch, 64,512 in all
+template <int NP> struct Fwd {
+  static constexpr uint32_t tile = kT * 128 * NP;
+  static constexpr int ring = NP == 1 ? 3 : 2;              // stages of K and of V
+  static constexpr size_t smem = 2 * tile + 2 * ring * tile + 1024;
+  static constexpr uint32_t o = 256, p = NP == 1 ? 384 : 0, o_step = NP == 1 ? 64 : 128, p_step = NP == 1 ? 64 : 128;
 };
 
-__device__ __forceinline__ int q_len(const Sizes &z, int b) { return z.q_lens ? min(max(z.q_lens[b], 0), z.tq) : z.tq; }
-__device__ __forceinline__ int kv_len(const Sizes &z, int b) { return z.kv_lens ? min(max(z.kv_lens[b], 0), z.tk) : z.tk; }
+template <int NP>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+             const __grid_constant__ CUtensorMap mv, const Sizes z, const View o, float *__restrict__ lse) {
+  typedef Fwd<NP> F;
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t q_full, k_full[F::ring], k_empty[F::ring], v_full[F::ring], v_empty[F::ring], s_full[2],
+      s_free[2], p_ready[2], pv_done[2];
+  __shared__ uint32_t tmem_slot;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  const uint32_t sq = smem_u32(base), sk = sq + 2 * F::tile, sv = sk + F::ring * F::tile;
+  const int h = blockIdx.x % z.heads, b = blockIdx.x / z.heads, hk = h / z.group;
+  // the longest query blocks of a causal batch start first
+  const int i0 = (z.causal ? (int)gridDim.y - 1 - (int)blockIdx.y : (int)blockIdx.y) * 2 * kT;
 
-// one warp per row; a lane holds elements lane, lane + 32, ... of the head
-struct Row { float v[4]; };
-__device__ __forceinline__ Row load_row(const bf16 *p, int dim) {
-  Row r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const int c = (threadIdx.x & 31) + 32 * i; r.v[i] = c < dim ? __bfloat162float(p[c]) : 0.0f; }
-  return r;
-}
-__device__ __forceinline__ void store_row(bf16 *p, int dim, const Row &r, float f) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const int c = (threadIdx.x & 31) + 32 * i; if (c < dim) p[c] = __float2bfloat16_rn(r.v[i] * f); }
-}
-__device__ __forceinline__ float dot(const Row &a, const Row &b) {
-  return cdg_warp_sum(a.v[0] * b.v[0] + a.v[1] * b.v[1] + a.v[2] * b.v[2] + a.v[3] * b.v[3]);
-}
-__device__ __forceinline__ void axpy(Row &a, float f, const Row &b) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) a.v[i] += f * b.v[i];
-}
-
-struct View { const bf16 *p; long long b, t, h; __device__ const bf16 *row(int bb, long long tt, int hh) const { return p + bb * b + tt * t + hh * h; } };
-struct OutView { bf16 *p; long long b, t, h; __device__ bf16 *row(int bb, long long tt, int hh) const { return p + bb * b + tt * t + hh * h; } };
-
-__global__ void __launch_bounds__(128) attn_forward_rows(Sizes z, View q, View k, View v, OutView o, float *lse) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-  if (i >= z.tq) return;
-  const int lq = q_len(z, b), lk = kv_len(z, b);
-  int n = i < lq ? (z.causal ? min(lk, i + lk - lq + 1) : lk) : 0;
-  Row acc = {}, qr = load_row(q.row(b, i, h), z.dim);
-  float top = -INFINITY, sum = 0.0f;
-  for (int j = 0; j < n; ++j) {
-    const float s = z.scale * dot(qr, load_row(k.row(b, j, h / z.group), z.dim));
-    const float nt = fmaxf(top, s), f = __expf(top - nt), p = __expf(s - nt);
-    sum = sum * f + p;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc.v[c] *= f;
-    axpy(acc, p, load_row(v.row(b, j, h / z.group), z.dim));
-    top = nt;
-  }
-  store_row(o.row(b, i, h), z.dim, acc, n > 0 ? 1.0f / sum : 0.0f);
-  if ((threadIdx.x & 31) == 0) lse[((long long)b * z.heads + h) * z.tq + i] = n > 0 ? top + logf(sum) : -INFINITY;
-}
-
-__global__ void __launch_bounds__(128) attn_delta(Sizes z, View d_o, View o, float *delta) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-  if (i >= z.tq) return;
-  const float d = i < q_len(z, b) ? dot(load_row(d_o.row(b, i, h), z.dim), load_row(o.row(b, i, h), z.dim)) : 0.0f;
-  if ((threadIdx.x & 31) == 0) delta[((long long)b * z.heads + h) * z.tq + i] = d;
-}
-
-__global__ void __launch_bounds__(128) attn_dq_rows(Sizes z, View q, View k, View v, View d_o, const float *lse,
-                                                    const float *delta, OutView dq) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-  if (i >= z.tq) return;
-  const int lq = q_len(z, b), lk = kv_len(z, b);
-  const int n = i < lq ? (z.causal ? min(lk, i + lk - lq + 1) : lk) : 0;
-  Row acc = {}, qr = load_row(q.row(b, i, h), z.dim), dor = load_row(d_o.row(b, i, h), z.dim);
-  const long long at = ((long long)b * z.heads + h) * z.tq + i;
-  for (int j = 0; j < n; ++j) {
-    const Row kr = load_row(k.row(b, j, h / z.group), z.dim);
-    const float p = __expf(z.scale * dot(qr, kr) - lse[at]);
-    const float dp = dot(dor, load_row(v.row(b, j, h / z.group), z.dim));
-    axpy(acc, p * (dp - delta[at]), kr);
-  }
-  store_row(dq.row(b, i, h), z.dim, acc, z.scale);
-}
-
-__global__ void __launch_bounds__(128) attn_dkv_rows(Sizes z, View q, View k, View v, View d_o, const float *lse,
-                                                     const float *delta, OutView dk, OutView dv) {
-  const int j = blockIdx.x * 4 + (threadIdx.x >> 5), hk = blockIdx.y, b = blockIdx.z;
-  if (j >= z.tk) return;
-  const int lq = q_len(z, b), lk = kv_len(z, b);
-  Row ak = {}, av = {}, kr = load_row(k.row(b, j, hk), z.dim), vr = load_row(v.row(b, j, hk), z.dim);
-  const int first = j < lk ? (z.causal ? max(0, j - (lk - lq)) : 0) : lq;
-  for (int h = hk * z.group; h < (hk + 1) * z.group; ++h)
-    for (int i = first; i < lq; ++i) {
-      const long long at = ((long long)b * z.heads + h) * z.tq + i;
-      const Row qr = load_row(q.row(b, i, h), z.dim), dor = load_row(d_o.row(b, i, h), z.dim);
-      const float p = __expf(z.scale * dot(qr, kr) - lse[at]);
-      axpy(av, p, dor);
-      axpy(ak, p * (dot(dor, vr) - delta[at]), qr);
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&q_full), 1);
+    for (int i = 0; i < F::ring; ++i) {
+      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1);
+      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
     }
-  store_row(dk.row(b, j, hk), z.dim, ak, z.scale);
-  store_row(dv.row(b, j, hk), z.dim, av, 1.0f);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&s_free[t]), 4);
+      mbar_init(smem_u32(&p_ready[t]), 4); mbar_init(smem_u32(&pv_done[t]), 1);
+    }
+    mbar_init_fence();
+  }
+  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = tmem_slot;
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const long long deadline = clock64() + kCdgWaitCycles;
+
+  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
+  int n[2];                      // key tiles that query tile t sees
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int first = i0 + t * kT, last = min(first + kT, lq) - 1;
+    const int keys = first >= lq ? 0 : z.causal ? min(lk, last + lk - lq + 1) : lk;
+    n[t] = keys > 0 ? (keys + kT - 1) / kT : 0;
+  }
+  const int tiles = max(n[0], n[1]);
+
+  if (warp >= 8) {
+  tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+  if (warp == 8) {
+    if (tc_elect() && tiles > 0) {
+      bool ok = true;
+      int kn = 0, vn = 0;        // tiles issued
+      mbar_expect_tx(smem_u32(&q_full), 2 * F::tile);
+      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full));
+      load_tile<NP>(sq + F::tile, &mq, i0 + kT, h, batch_of(z, kQ, b), smem_u32(&q_full));
+      for (int j = 0; j <= tiles && ok; ++j) {         // K runs one tile ahead of V
+        if (j < tiles) {
+          const int s = j % F::ring;
+          if (j >= F::ring) ok = mbar_wait(smem_u32(&k_empty[s]), (j / F::ring - 1) & 1, deadline);
+          if (!ok) break;
+          mbar_expect_tx(smem_u32(&k_full[s]), F::tile);
+          load_tile<NP>(sk + s * F::tile, &mk, j * kT, hk, batch_of(z, kK, b), smem_u32(&k_full[s]));
+          ++kn;
+        }
+        if (j > 0) {
+          const int i = j - 1, s = i % F::ring;
+          if (i >= F::ring) ok = mbar_wait(smem_u32(&v_empty[s]), (i / F::ring - 1) & 1, deadline);
+          if (!ok) break;
+          mbar_expect_tx(smem_u32(&v_full[s]), F::tile);
+          load_tile<NP>(sv + s * F::tile, &mv, i * kT, hk, batch_of(z, kV, b), smem_u32(&v_full[s]));
+          ++vn;
+        }
+      }
+      if (!ok) {                 // let the copies in flight land before the CTA gives up its shared memory
+        atomicOr(z.status, CDG_ST_TIMEOUT);
+        mbar_wait(smem_u32(&q_full), 0, clock64() + kCdgWaitCycles);
+        for (int i = max(0, kn - F::ring); i < kn; ++i) mbar_wait(smem_u32(&k_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, vn - F::ring); i < vn; ++i) mbar_wait(smem_u32(&v_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+      }
+    }
+  } else if (warp == 9) {
+    bool ok = tiles == 0 || tc_wait(&q_full, 0, deadline);
+    if (ok && tiles > 0) ok = tc_wait(&k_full[0], 0, deadline);
+    tc_fence_after();
+    if (ok && tiles > 0 && tc_elect()) {
+      for (int t = 0; t < 2; ++t)
+        if (n[t] > 0) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(smem_u32(&s_full[t])); }
+      tc_commit(smem_u32(&k_empty[0]));
+    }
+    __syncwarp();
+    for (int j = 0; j < tiles && ok; ++j) {
+      const int vs = j % F::ring, ks = (j + 1) % F::ring;
+      const uint32_t k_next = sk + ks * F::tile, v_this = sv + vs * F::tile;
+      if (!(ok = tc_wait(&v_full[vs], (j / F::ring) & 1, deadline))) break;
+      if (z.kv_lens && (j + 1) * kT > lk) zero_rows<NP>(base + 2 * F::tile + F::ring * F::tile + vs * F::tile, lk - j * kT);
+      if (j + 1 < tiles && !(ok = tc_wait(&k_full[ks], ((j + 1) / F::ring) & 1, deadline))) break;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (NP == 1 && j + 1 < n[t]) {               // S_t(j) is in registers: the next one may overwrite it
+          if (!(ok = tc_wait(&s_free[t], j & 1, deadline))) break;
+          tc_fence_after();
+          if (tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(smem_u32(&s_full[t])); }
+          __syncwarp();
+        }
+        if (j < n[t]) {
+          if (!(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
+          tc_fence_after();
+          if (tc_elect()) {
+            mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
+            tc_commit(smem_u32(&pv_done[t]));
+          }
+          __syncwarp();
+        }
+        if (NP == 2 && j + 1 < n[t]) {               // P_t lies over S_t: its product has to be over
+          if (!(ok = tc_wait(&pv_done[t], j & 1, deadline))) break;
+          tc_fence_after();
+          if (tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(smem_u32(&s_full[t])); }
+          __syncwarp();
+        }
+      }
+      if (!ok) break;
+      if (tc_elect()) {
+        tc_commit(smem_u32(&v_empty[vs]));
+        if (j + 1 < tiles) tc_commit(smem_u32(&k_empty[ks]));
+      }
+      __syncwarp();
+    }
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+  }
+  } else {
+    tc_regs_up<224>();
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + t * kT + row;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tm + lanes + t * kT, tp = tm + lanes + F::p + t * F::p_step, to = tm + lanes + F::o + t * F::o_step;
+    const int keys = i >= lq ? 0 : z.causal ? min(lk, i + lk - lq + 1) : lk;     // this row sees keys 0 .. keys - 1
+    const float a = z.a;
+    float ref = -INFINITY, sum = 0.0f;
+    bool ok = true;
+    for (int j = 0; j < n[t]; ++j) {
+      if (!(ok = tc_wait(&s_full[t], j & 1, deadline))) break;
+      tc_fence_after();
+      uint32_t v[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_load32(ts + c * 32, v[c]);
+      tc_wait_ld();
+      if (NP == 1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_free[t]));
+      }
+      if (z.negative) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[c][e] ^= 0x80000000u;
+      }
+      const int left = keys - j * kT;
+      if (__any_sync(0xffffffffu, left < kT)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e >= left) v[c][e] = 0xff800000u;
+      }
+      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(v[c][e]));
+      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      // raise the reference where the maximum has outgrown it by 2^8, or where there was none
+      const bool raise = mx > ref && (ref == -INFINITY || (mx - ref) * a > 8.0f);
+      const float factor = raise ? exp2_fast((ref - mx) * a) : 1.0f;
+      if (raise) { ref = mx; sum *= factor; }
+      const float shift = ref == -INFINITY ? 0.0f : -ref * a;
+      if (j > 0 && !(ok = tc_wait(&pv_done[t], (j - 1) & 1, deadline))) break;
+      if (j > 0 && __any_sync(0xffffffffu, raise)) {
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < 2 * NP; ++c) {
+          uint32_t w[32];
+          tc_load32(to + c * 32, w);
+          tc_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * factor);
+          tc_store32(to + c * 32, w);
+        }
+      }
+      float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < 4; c += 2) {
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float p0 = exp2_fast(fmaf(__uint_as_float(v[c + (e >> 5)][e & 31]), a, shift));
+          const float p1 = exp2_fast(fmaf(__uint_as_float(v[c + (e >> 5)][(e & 31) + 1]), a, shift));
+          part[(e >> 1) & 3] += p0 + p1;
+          w[e >> 1] = pack(p0, p1);
+        }
+        tc_store32(tp + c * 16, w);
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&p_ready[t]));
+    }
+    if (ok && n[t] > 0) ok = tc_wait(&pv_done[t], (n[t] - 1) & 1, deadline);
+    if (ok && n[t] == 0 && tiles > 0) ok = tc_wait(&q_full, 0, deadline);     // its copy of Q has landed
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+    tc_fence_after();
+    // the tile of Q is no longer read: it takes O on its way out
+    uint8_t *tile = base + t * F::tile;
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int c = 0; c < 2 * NP; ++c) {
+      uint32_t w[32], u[16];
+      if (n[t] > 0) {
+        tc_load32(to + c * 32, w);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * inv, __uint_as_float(w[2 * e + 1]) * inv) : 0u;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = 0u;
+      }
+      stage_row<NP>(tile, row, c * 32, u);
+    }
+    __syncwarp();
+    write_rows<NP>(tile, (warp & 3) * 32, i0 + t * kT, z.tq, z, o.p + (long long)b * o.b + (long long)h * o.h, o.t);
+    if (i < z.tq)
+      lse[((long long)b * z.heads + h) * z.tq + i] = keys > 0 ? fmaf(ref, a * kLn2, logf(sum)) : -INFINITY;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
 }
 
+// ---- backward -----------------------------------------------------------------------------------
+// For every query row: delta = sum_d do o, and lse in base 2 (+infinity where the row sees nothing, so that
+// its recomputed probabilities are 0).  Rows are padded to whole tiles: [batch][heads][2][rows], first lse.
+// Eight lanes to a row and head, 16 bytes a lane.
+__global__ void __launch_bounds__(256) attn_delta(const Sizes z, const View d_o, const View o, const float *__restrict__ lse,
+                                                  float *__restrict__ out, int padded) {
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const long long group = ((long long)blockIdx.x * 256 + threadIdx.x) >> 3;
+  const int l = threadIdx.x & 7;
+  const int h = (int)(group % z.heads), i = (int)(group / z.heads % padded), b = (int)(group / z.heads / padded);
+  if (b >= z.batch) return;
+  float s = 0.0f, l2 = INFINITY;
+  if (i < used(z.q_lens, b, z.tq)) {
+    const bf16 *x = d_o.p + b * d_o.b + i * d_o.t + h * d_o.h, *y = o.p + b * o.b + i * o.t + h * o.h;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      if (c * 64 + l * 8 >= z.dim) continue;
+      const uint4 u = *reinterpret_cast<const uint4 *>(x + c * 64 + l * 8), w = *reinterpret_cast<const uint4 *>(y + c * 64 + l * 8);
+      const uint32_t ua[4] = {u.x, u.y, u.z, u.w}, wa[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&ua[e]));
+        const float2 g = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&wa[e]));
+        s = fmaf(f.x, g.x, fmaf(f.y, g.y, s));
+      }
+    }
+    l2 = lse[((long long)b * z.heads + h) * z.tq + i] * kLog2e;
+    if (l2 == -INFINITY) l2 = INFINITY;
+  }
+#pragma unroll
+  for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off, 8);
+  if (l == 0) {
+    float *row = out + ((long long)b * z.heads + h) * 2 * padded + i;
+    row[0] = l2;
+    row[padded] = l2 == INFINITY ? 0.0f : s;
+  }
+}
+
+// 512 bytes of a row of `out` above; both addresses are multiples of 16 bytes
+__device__ __forceinline__ void load_line(uint32_t dst, const float *src, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(kT * 4), "r"(bar) : "memory");
+}
+
+// Both backward kernels: eight warps work on a tile of scores, four on its columns 0..63 and four on
+// 64..127, one row per thread.  Columns of tensor memory: S (then P, as bf16, over each half's own
+// scores) and dP (then dS likewise), then the accumulators.
+//   warps 0-7  P and dS        warp 8  bulk copies        warp 9  products
+constexpr int kBwdThreads = 320;
+
+// dk and dv of 128 keys: the loop runs over the query tiles of every query head that reads this key head.
+// Scores are transposed (a row is a key), so that P^T and dS^T are the row operands of
+//   dv += P^T dO,  dk += dS^T Q,    with  S^T = K Q^T,  dP^T = V dO^T.
+// Summing over query tiles and heads inside one CTA makes the result the same bits every time.
+template <int NP> struct Dkv {
+  static constexpr uint32_t tile = kT * 128 * NP;
+  static constexpr int ring = 2;
+  static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
+  static constexpr size_t smem = 2 * tile + ring * (2 * tile + line) + 1024;
+  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
+};
+
+template <int NP>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
+                 const float *__restrict__ lines, int padded, const View dk, const View dv) {
+  typedef Dkv<NP> F;
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t kv_full, q_full[F::ring], q_empty[F::ring], do_full[F::ring], do_empty[F::ring], s_full,
+      dp_full, p_ready, ds_ready, dv_done, dk_done;
+  __shared__ uint32_t tmem_slot;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  const uint32_t sk = smem_u32(base), sv = sk + F::tile, sq = sv + F::tile, sdo = sq + F::ring * F::tile;
+  float *sline = reinterpret_cast<float *>(base + 2 * F::tile + 2 * F::ring * F::tile);      // [ring][2][128]
+  const int kv_heads = z.heads / z.group;
+  const int hk = blockIdx.x % kv_heads, b = blockIdx.x / kv_heads;
+  const int j0 = blockIdx.y * kT;            // the first keys, which most queries see, start first
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&kv_full), 1);
+    for (int i = 0; i < F::ring; ++i) {
+      mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_empty[i]), 1);
+      mbar_init(smem_u32(&do_full[i]), 1); mbar_init(smem_u32(&do_empty[i]), 1);
+    }
+    mbar_init(smem_u32(&s_full), 1); mbar_init(smem_u32(&dp_full), 1);
+    mbar_init(smem_u32(&p_ready), 8); mbar_init(smem_u32(&ds_ready), 8);
+    mbar_init(smem_u32(&dv_done), 1); mbar_init(smem_u32(&dk_done), 1);
+    mbar_init_fence();
+  }
+  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = tmem_slot;
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const long long deadline = clock64() + kCdgWaitCycles;
+
+  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
+  // query tiles first .. last - 1 see key j0 or a later one of this tile
+  const int first = j0 >= lk ? 0 : z.causal ? max(0, j0 - (lk - lq)) / kT : 0;
+  const int last = j0 >= lk ? 0 : (lq + kT - 1) / kT;
+  const int per = max(0, last - first), total = per * z.group;
+
+  if (warp == 8) {
+    if (tc_elect() && total > 0) {
+      bool ok = true;
+      int qn = 0, dn = 0;
+      mbar_expect_tx(smem_u32(&kv_full), 2 * F::tile);
+      load_tile<NP>(sk, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&kv_full));
+      load_tile<NP>(sv, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&kv_full));
+      for (int it = 0; it < total; ++it) {
+        const int s = it % F::ring, h = hk * z.group + it / per, i0 = (first + it % per) * kT;
+        const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i0;
+        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&q_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&q_full[s]), F::tile + F::line);
+        load_tile<NP>(sq + s * F::tile, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full[s]));
+        load_line(smem_u32(sline + s * 2 * kT), line, smem_u32(&q_full[s]));
+        load_line(smem_u32(sline + s * 2 * kT + kT), line + padded, smem_u32(&q_full[s]));
+        ++qn;
+        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&do_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&do_full[s]), F::tile);
+        load_tile<NP>(sdo + s * F::tile, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&do_full[s]));
+        ++dn;
+      }
+      if (!ok) {
+        atomicOr(z.status, CDG_ST_TIMEOUT);
+        mbar_wait(smem_u32(&kv_full), 0, clock64() + kCdgWaitCycles);
+        for (int i = max(0, qn - F::ring); i < qn; ++i) mbar_wait(smem_u32(&q_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, dn - F::ring); i < dn; ++i) mbar_wait(smem_u32(&do_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+      }
+    }
+  } else if (warp == 9) {
+    // A tile's rows past the sequence's queries are zeroed before any product reads them
+    auto arrived = [&](uint64_t *bars, uint32_t tiles, int it) {
+      const int s = it % F::ring;
+      if (!tc_wait(&bars[s], (it / F::ring) & 1, deadline)) return false;
+      const int left = lq - (first + it % per) * kT;
+      if (z.q_lens && left < kT) zero_rows<NP>(base + (tiles - sk) + s * F::tile, left);
+      return true;
+    };
+    bool ok = true;
+    if (total > 0) {
+      ok = tc_wait(&kv_full, 0, deadline) && arrived(q_full, sq, 0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm, sk, sq); tc_commit(smem_u32(&s_full)); }
+      __syncwarp();
+      ok = ok && arrived(do_full, sdo, 0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(smem_u32(&dp_full)); }
+      __syncwarp();
+    }
+    for (int it = 0; it < total && ok; ++it) {
+      const int s = it % F::ring, sn = (it + 1) % F::ring;
+      const bool next = it + 1 < total;
+      if (!(ok = tc_wait(&p_ready, it & 1, deadline))) break;
+      tc_fence_after();
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dv, tm, 64, sdo + s * F::tile, it > 0);
+        tc_commit(smem_u32(&dv_done));
+        tc_commit(smem_u32(&do_empty[s]));
+      }
+      __syncwarp();
+      if (next) {              // S lies under P: its product has to be over
+        if (!(ok = arrived(q_full, sq, it + 1) && tc_wait(&dv_done, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) { mma_scores<NP>(tm, sk, sq + sn * F::tile); tc_commit(smem_u32(&s_full)); }
+        __syncwarp();
+      }
+      if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
+      tc_fence_after();
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dk, tm + kT, 64, sq + s * F::tile, it > 0);
+        tc_commit(smem_u32(&dk_done));
+        tc_commit(smem_u32(&q_empty[s]));
+      }
+      __syncwarp();
+      if (next) {
+        if (!(ok = arrived(do_full, sdo, it + 1) && tc_wait(&dk_done, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo + sn * F::tile); tc_commit(smem_u32(&dp_full)); }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+  } else {
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane, j = j0 + row;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
+    const float a = z.negative ? -z.a : z.a;
+    const int off = lk - lq;
+    bool ok = true;
+    for (int it = 0; it < total; ++it) {
+      const int s = it % F::ring, i0 = (first + it % per) * kT + half * 64;
+      const float *l2 = sline + s * 2 * kT + half * 64, *delta = l2 + kT;
+      // the lines came with Q, whose stage is released when dS of this tile has been used
+      if (!(ok = tc_wait(&q_full[s], (it / F::ring) & 1, deadline) && tc_wait(&s_full, it & 1, deadline))) break;
+      tc_fence_after();
+      float p[64];
+      // under the causal rule key j is seen by queries from j - off on
+      const int from = z.causal ? j - off - i0 : 0;
+      const bool some_hidden = __any_sync(0xffffffffu, from > 0);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32], w[16];
+        tc_load32(ts + c * 32, v);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const float4 l = *reinterpret_cast<const float4 *>(l2 + c * 32 + e);
+          p[c * 32 + e] = exp2_fast(fmaf(__uint_as_float(v[e]), a, -l.x));
+          p[c * 32 + e + 1] = exp2_fast(fmaf(__uint_as_float(v[e + 1]), a, -l.y));
+          p[c * 32 + e + 2] = exp2_fast(fmaf(__uint_as_float(v[e + 2]), a, -l.z));
+          p[c * 32 + e + 3] = exp2_fast(fmaf(__uint_as_float(v[e + 3]), a, -l.w));
+        }
+        if (some_hidden) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e < from) p[c * 32 + e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack(p[c * 32 + 2 * e], p[c * 32 + 2 * e + 1]);
+        tc_store16(ts + c * 16, w);
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&p_ready));
+      if (!(ok = tc_wait(&dp_full, it & 1, deadline))) break;
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32], w[16];
+        tc_load32(tdp + c * 32, v);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const float4 d = *reinterpret_cast<const float4 *>(delta + c * 32 + e);
+          w[e / 2] = pack(p[c * 32 + e] * (__uint_as_float(v[e]) - d.x), p[c * 32 + e + 1] * (__uint_as_float(v[e + 1]) - d.y));
+          w[e / 2 + 1] = pack(p[c * 32 + e + 2] * (__uint_as_float(v[e + 2]) - d.z), p[c * 32 + e + 3] * (__uint_as_float(v[e + 3]) - d.w));
+        }
+        tc_store16(tdp + c * 16, w);
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ds_ready));
+    }
+    // warps 0-3 bring dv out, 4-7 dk, through the tiles of K and V, which no product reads any more
+    if (ok && total > 0) ok = tc_wait(&dv_done, (total - 1) & 1, deadline) && tc_wait(&dk_done, (total - 1) & 1, deadline);
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+    tc_fence_after();
+    uint8_t *tile = base + half * F::tile;
+    const uint32_t from = tm + lanes + (half ? F::dk : F::dv);
+    const float f = half ? z.scale : 1.0f;
+#pragma unroll
+    for (int c = 0; c < 2 * NP; ++c) {
+      uint32_t w[32], u[16];
+      if (total > 0) {
+        tc_load32(from + c * 32, w);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = j < lk ? pack(__uint_as_float(w[2 * e]) * f, __uint_as_float(w[2 * e + 1]) * f) : 0u;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = 0u;
+      }
+      stage_row<NP>(tile, row, c * 32, u);
+    }
+    __syncwarp();
+    const View &out = half ? dk : dv;
+    write_rows<NP>(tile, (warp & 3) * 32, j0, z.tk, z, out.p + (long long)b * out.b + (long long)hk * out.h, out.t);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
+}
+
+// dq of 128 queries of a head: dq += dS K over the key tiles it sees, S = Q K^T, dP = dO V^T.  A pass of its
+// own: adding dq's parts up from the kernel above would need additions to memory in no fixed order.
+template <int NP> struct Dq {
+  static constexpr uint32_t tile = kT * 128 * NP;
+  static constexpr int ring = 2;
+  static constexpr size_t smem = 2 * tile + ring * 2 * tile + 1024;
+  static constexpr uint32_t dq = 256;
+};
+
+template <int NP>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
+                const float *__restrict__ lines, int padded, const View dq) {
+  typedef Dq<NP> F;
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t q_full, k_full[F::ring], k_empty[F::ring], v_full[F::ring], v_empty[F::ring], s_full, dp_full,
+      s_free, ds_ready, dq_done;
+  __shared__ uint32_t tmem_slot;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  const uint32_t sq = smem_u32(base), sdo = sq + F::tile, sk = sdo + F::tile, sv = sk + F::ring * F::tile;
+  const int h = blockIdx.x % z.heads, b = blockIdx.x / z.heads, hk = h / z.group;
+  const int i0 = (z.causal ? (int)gridDim.y - 1 - (int)blockIdx.y : (int)blockIdx.y) * kT;
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&q_full), 1);
+    for (int i = 0; i < F::ring; ++i) {
+      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1);
+      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
+    }
+    mbar_init(smem_u32(&s_full), 1); mbar_init(smem_u32(&dp_full), 1);
+    mbar_init(smem_u32(&s_free), 8); mbar_init(smem_u32(&ds_ready), 8);
+    mbar_init(smem_u32(&dq_done), 1);
+    mbar_init_fence();
+  }
+  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = tmem_slot;
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const long long deadline = clock64() + kCdgWaitCycles;
+
+  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
+  const int seen = i0 >= lq ? 0 : z.causal ? min(lk, min(i0 + kT, lq) + lk - lq) : lk;
+  const int total = seen > 0 ? (seen + kT - 1) / kT : 0;
+
+  if (warp == 8) {
+    if (tc_elect() && total > 0) {
+      bool ok = true;
+      int kn = 0, vn = 0;
+      mbar_expect_tx(smem_u32(&q_full), 2 * F::tile);
+      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full));
+      load_tile<NP>(sdo, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&q_full));
+      for (int it = 0; it < total; ++it) {
+        const int s = it % F::ring;
+        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&k_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&k_full[s]), F::tile);
+        load_tile<NP>(sk + s * F::tile, &mk, it * kT, hk, batch_of(z, kK, b), smem_u32(&k_full[s]));
+        ++kn;
+        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&v_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&v_full[s]), F::tile);
+        load_tile<NP>(sv + s * F::tile, &mv, it * kT, hk, batch_of(z, kV, b), smem_u32(&v_full[s]));
+        ++vn;
+      }
+      if (!ok) {
+        atomicOr(z.status, CDG_ST_TIMEOUT);
+        mbar_wait(smem_u32(&q_full), 0, clock64() + kCdgWaitCycles);
+        for (int i = max(0, kn - F::ring); i < kn; ++i) mbar_wait(smem_u32(&k_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, vn - F::ring); i < vn; ++i) mbar_wait(smem_u32(&v_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+      }
+    }
+  } else if (warp == 9) {
+    auto arrived = [&](int it) {         // K of tile it, its rows past the sequence zeroed
+      const int s = it % F::ring;
+      if (!tc_wait(&k_full[s], (it / F::ring) & 1, deadline)) return false;
+      if (z.kv_lens && (it + 1) * kT > lk) zero_rows<NP>(base + (sk - sq) + s * F::tile, lk - it * kT);
+      return true;
+    };
+    bool ok = true;
+    if (total > 0) {
+      ok = tc_wait(&q_full, 0, deadline) && arrived(0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm, sq, sk); tc_commit(smem_u32(&s_full)); }
+      __syncwarp();
+      ok = ok && tc_wait(&v_full[0], 0, deadline);
+      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(smem_u32(&dp_full)); tc_commit(smem_u32(&v_empty[0])); }
+      __syncwarp();
+    }
+    for (int it = 0; it < total && ok; ++it) {
+      const int s = it % F::ring, sn = (it + 1) % F::ring;
+      const bool next = it + 1 < total;
+      if (next) {              // S is in registers: the next one may overwrite it
+        if (!(ok = arrived(it + 1) && tc_wait(&s_free, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) { mma_scores<NP>(tm, sq, sk + sn * F::tile); tc_commit(smem_u32(&s_full)); }
+        __syncwarp();
+      }
+      if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
+      tc_fence_after();
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dq, tm + kT, 64, sk + s * F::tile, it > 0);
+        tc_commit(smem_u32(&dq_done));
+        tc_commit(smem_u32(&k_empty[s]));
+      }
+      __syncwarp();
+      if (next) {              // dP lies under dS: its product has to be over
+        if (!(ok = tc_wait(&v_full[sn], ((it + 1) / F::ring) & 1, deadline) && tc_wait(&dq_done, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv + sn * F::tile); tc_commit(smem_u32(&dp_full)); tc_commit(smem_u32(&v_empty[sn])); }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+  } else {
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + row;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
+    const float a = z.negative ? -z.a : z.a;
+    const int keys = i >= lq ? 0 : z.causal ? min(lk, i + lk - lq + 1) : lk;
+    float l2 = INFINITY, delta = 0.0f;
+    if (i < padded) {
+      const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i;
+      l2 = line[0];
+      delta = line[padded];
+    }
+    bool ok = true;
+    for (int it = 0; it < total; ++it) {
+      if (!(ok = tc_wait(&s_full, it & 1, deadline))) break;
+      tc_fence_after();
+      uint32_t v[2][32];
+      tc_load32(ts, v[0]);
+      tc_load32(ts + 32, v[1]);
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_free));
+      const int left = keys - it * kT - half * 64;
+      float p[64];
+#pragma unroll
+      for (int e = 0; e < 64; ++e) p[e] = exp2_fast(fmaf(__uint_as_float(v[e >> 5][e & 31]), a, -l2));
+      const bool some_hidden = __any_sync(0xffffffffu, left < 64);
+      if (!(ok = tc_wait(&dp_full, it & 1, deadline))) break;
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t u[32], w[16];
+        tc_load32(tdp + c * 32, u);
+        tc_wait_ld();
+        float ds[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) ds[e] = p[c * 32 + e] * (__uint_as_float(u[e]) - delta);
+        if (some_hidden) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (c * 32 + e >= left) ds[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack(ds[2 * e], ds[2 * e + 1]);
+        tc_store16(tdp + c * 16, w);
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ds_ready));
+    }
+    if (ok && total > 0) ok = tc_wait(&dq_done, (total - 1) & 1, deadline);
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+    tc_fence_after();
+    // the two groups of warps bring out half of the head dimensions each, through the tile of Q
+    const uint32_t from = tm + lanes + F::dq;
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+      const int col = (half * NP + c) * 32;
+      uint32_t w[32], u[16];
+      if (total > 0) {
+        tc_load32(from + col, w);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * z.scale, __uint_as_float(w[2 * e + 1]) * z.scale) : 0u;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = 0u;
+      }
+      stage_row<NP>(base, row, col, u);
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (half == 0)
+      write_rows<NP>(base, (warp & 3) * 32, i0, z.tq, z, dq.p + (long long)b * dq.b + (long long)h * dq.h, dq.t);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
 constexpr long long kMaxStride = 1ll << 38;   // elements; a tensor map holds byte strides below 2^40
 
 // strides of a tensor that is read: multiples of 16 bytes, tokens and heads apart from each other
@@ -130,19 +860,62 @@ bool out_ok(const long long s[3], int batch, int tokens, int heads, int dim) {
   return true;
 }
 
+constexpr int kMaxTokens = 1 << 22;
+
 bool shape_ok(const cdgrab_attention_shape *s) {
   if (!s || s->batch < 0 || s->batch > 65535 || s->len_q < 0 || s->len_kv < 0 || s->heads < 1 || s->kv_heads < 1 ||
       s->heads > 65535 || s->heads % s->kv_heads != 0)
     return false;
   if (s->head_dim < 8 || s->head_dim > 128 || s->head_dim % 8 != 0 || (s->causal != 0 && s->causal != 1)) return false;
+  // the grid's axes: batch x heads, and tiles of tokens
+  if ((long long)s->batch * s->heads > 0x7fffffffll || s->len_q > kMaxTokens || s->len_kv > kMaxTokens) return false;
   return isfinite(s->scale);
 }
 
-Sizes sizes_of(const cdgrab_attention_shape *s, const int32_t *q_lens, const int32_t *kv_lens) {
-  return Sizes{s->batch, s->len_q, s->len_kv, s->heads, s->heads / s->kv_heads, s->head_dim, s->causal, s->scale, q_lens, kv_lens};
+Sizes sizes_of(const cdgrab_attention_shape *s, const int32_t *q_lens, const int32_t *kv_lens, int *status) {
+  const int shared = (s->q_stride[0] > 0 ? 0 : kQ) | (s->k_stride[0] > 0 ? 0 : kK) | (s->v_stride[0] > 0 ? 0 : kV) |
+                     (s->do_stride[0] > 0 ? 0 : kDo);
+  return Sizes{s->batch, s->len_q, s->len_kv, s->heads, s->heads / s->kv_heads, s->head_dim, s->causal, s->scale,
+               fmaxf(fabsf(s->scale) * kLog2e, 1e-30f), s->scale < 0.0f, shared, q_lens, kv_lens, status};
 }
-View view(const void *p, const long long s[3]) { return View{(const bf16 *)p, s[0], s[1], s[2]}; }
-OutView out_view(void *p, const long long s[3]) { return OutView{(bf16 *)p, s[0], s[1], s[2]}; }
+View view(const void *p, const long long s[3]) { return View{(bf16 *)const_cast<void *>(p), s[0], s[1], s[2]}; }
+
+// [batch][head][token][dim] as the copies see it, boxes of 64 dimensions by 128 tokens
+bool map_of(CUtensorMap *m, const void *p, const long long s[3], int batch, int tokens, int heads, int dim) {
+  const long long dims[4] = {dim, tokens, heads, s[0] > 0 ? batch : 1};
+  // an axis of length one (or shared by the batch, read at 0) still needs a stride the copy engine takes
+  const long long strides[4] = {1, s[1] > 0 ? s[1] : 64, s[2] > 0 ? s[2] : 64, s[0] > 0 ? s[0] : 64};
+  return tc_encode(m, true, p, 4, dims, strides, kT);
+}
+template <typename K>
+bool raise_limit(CdgPerDevice &flags, K *kernel, size_t bytes) {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cdg_raise_smem_limit(flags, dev, kernel, bytes) == cudaSuccess;
+}
+
+template <int NP>
+int forward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const Sizes &z,
+            const View &o, float *lse, cudaStream_t st) {
+  static CdgPerDevice flags;
+  if (!raise_limit(flags, attn_forward<NP>, Fwd<NP>::smem)) return CDGRAB_ERR_CUDA;
+  return cdg_launch_rc(cdg_ops_launch(attn_forward<NP>, dim3(s->heads * s->batch, (s->len_q + 2 * kT - 1) / (2 * kT)), kFwdThreads,
+                                      Fwd<NP>::smem, st, mq, mk, mv, z, o, lse));
+}
+
+template <int NP>
+int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mdo,
+             const Sizes &z, const float *lines, int padded, const View &dq, const View &dk, const View &dv, cudaStream_t st) {
+  static CdgPerDevice kf, qf;
+  if (!raise_limit(kf, attn_backward_kv<NP>, Dkv<NP>::smem) || !raise_limit(qf, attn_backward_q<NP>, Dq<NP>::smem)) return CDGRAB_ERR_CUDA;
+  int rc = CDGRAB_OK;
+  if (s->len_kv > 0)
+    rc = cdg_launch_rc(cdg_ops_launch(attn_backward_kv<NP>, dim3(s->kv_heads * s->batch, (s->len_kv + kT - 1) / kT), kBwdThreads,
+                                      Dkv<NP>::smem, st, mq, mk, mv, mdo, z, lines, padded, dk, dv));
+  if (rc == CDGRAB_OK && s->len_q > 0)
+    rc = cdg_launch_rc(cdg_ops_launch(attn_backward_q<NP>, dim3(s->heads * s->batch, (s->len_q + kT - 1) / kT), kBwdThreads,
+                                      Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines, padded, dq));
+  return rc;
+}
 
 }  // namespace
 
@@ -161,15 +934,23 @@ extern "C" int cdgrab_attention_forward(const cdgrab_attention_shape *s, const v
     return CDGRAB_ERR_INVALID;
   const CdgOpsDevice *dev;
   if (const int rc = cdg_ops_device(&dev)) return rc;
-  attn_forward_rows<<<dim3((s->len_q + 3) / 4, s->heads, s->batch), 128, 0, (cudaStream_t)stream>>>(
-      sizes_of(s, q_lens, kv_lens), view(q, s->q_stride), view(k, s->k_stride), view(v, s->v_stride),
-      out_view(o, s->o_stride), lse);
-  return cdg_launch_rc();
+  const Sizes z = sizes_of(s, q_lens, kv_lens, dev->status);
+  // with no keys at all the maps of k and v are never used; they describe q
+  const int tk = s->len_kv > 0 ? s->len_kv : 1;
+  CUtensorMap mq, mk, mv;
+  if (!map_of(&mq, q, s->q_stride, s->batch, s->len_q, s->heads, s->head_dim) ||
+      !map_of(&mk, s->len_kv > 0 ? k : q, s->k_stride, s->batch, tk, s->kv_heads, s->head_dim) ||
+      !map_of(&mv, s->len_kv > 0 ? v : q, s->v_stride, s->batch, tk, s->kv_heads, s->head_dim))
+    return CDGRAB_ERR_CUDA;
+  const View ov = view(o, s->o_stride);
+  return s->head_dim <= 64 ? forward<1>(s, mq, mk, mv, z, ov, lse, (cudaStream_t)stream)
+                           : forward<2>(s, mq, mk, mv, z, ov, lse, (cudaStream_t)stream);
 }
 
 extern "C" long long cdgrab_attention_workspace_bytes(const cdgrab_attention_shape *s) {
   if (!shape_ok(s)) return -1;
-  return ((long long)s->batch * s->heads * s->len_q * 4 + 31) & ~15ll;
+  const long long rows = ((long long)s->len_q + kT - 1) / kT * kT;        // lse and delta, padded to whole tiles
+  return (long long)s->batch * s->heads * rows * 2 * 4 + 16;
 }
 
 extern "C" int cdgrab_attention_backward(const cdgrab_attention_shape *s, const void *d_o, const void *q, const void *k,
@@ -197,15 +978,26 @@ extern "C" int cdgrab_attention_backward(const cdgrab_attention_shape *s, const 
   const CdgOpsDevice *dev;
   if (const int rc = cdg_ops_device(&dev)) return rc;
   cudaStream_t st = (cudaStream_t)stream;
-  const Sizes z = sizes_of(s, q_lens, kv_lens);
-  float *delta = (float *)workspace;
-  const View vq = view(q, s->q_stride), vk = view(k, s->k_stride), vv = view(v, s->v_stride), vdo = view(d_o, s->do_stride);
-  const dim3 gq((s->len_q + 3) / 4, s->heads, s->batch), gk((s->len_kv + 3) / 4, s->kv_heads, s->batch);
+  const Sizes z = sizes_of(s, q_lens, kv_lens, dev->status);
+  float *lines = (float *)workspace;
+  const long long padded = ((long long)s->len_q + kT - 1) / kT * kT;
   if (s->len_q > 0) {
-    attn_delta<<<gq, 128, 0, st>>>(z, vdo, view(o, s->o_stride), delta);
-    attn_dq_rows<<<gq, 128, 0, st>>>(z, vq, vk, vv, vdo, lse, delta, out_view(dq, s->dq_stride));
+    const long long blocks = (s->batch * padded * s->heads * 8 + 255) / 256;
+    if (blocks > 0x7fffffffll) return CDGRAB_ERR_INVALID;
+    const int rc = cdg_launch_rc(cdg_ops_launch(attn_delta, dim3((unsigned)blocks), 256, 0, st, z, view(d_o, s->do_stride),
+                                                view(o, s->o_stride), lse, lines, (int)padded));
+    if (rc != CDGRAB_OK) return rc;
   }
-  if (s->len_kv > 0)
-    attn_dkv_rows<<<gk, 128, 0, st>>>(z, vq, vk, vv, vdo, lse, delta, out_view(dk, s->dk_stride), out_view(dv, s->dv_stride));
-  return cdg_launch_rc();
+  // a tensor without tokens is never read; its map describes one that is there
+  const bool has_q = s->len_q > 0, has_k = s->len_kv > 0;
+  const int tq = has_q ? s->len_q : 1, tk = has_k ? s->len_kv : 1;
+  CUtensorMap mq, mk, mv, mdo;
+  if (!map_of(&mq, has_q ? q : k, s->q_stride, s->batch, tq, s->heads, s->head_dim) ||
+      !map_of(&mk, has_k ? k : q, s->k_stride, s->batch, tk, s->kv_heads, s->head_dim) ||
+      !map_of(&mv, has_k ? v : q, s->v_stride, s->batch, tk, s->kv_heads, s->head_dim) ||
+      !map_of(&mdo, has_q ? d_o : k, s->do_stride, s->batch, tq, s->heads, s->head_dim))
+    return CDGRAB_ERR_CUDA;
+  const View vdq = view(dq, s->dq_stride), vdk = view(dk, s->dk_stride), vdv = view(dv, s->dv_stride);
+  return s->head_dim <= 64 ? backward<1>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, st)
+                           : backward<2>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, st);
 }

@@ -53,6 +53,15 @@ __device__ __forceinline__ bool tc_elect() {
   return pred != 0;
 }
 
+// bounded wait of a whole warp; false in all its lanes when it expired in one
+__device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity, long long deadline) {
+  return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, deadline));
+}
+// moves registers between warpgroups: all four warps of one execute it.  The shares have to add up to
+// no more than the block was launched with.
+template <int N> __device__ __forceinline__ void tc_regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void tc_regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // ---- tensor memory ----------------------------------------------------------------------------
 // one whole warp; `columns` a power of two from 32
 __device__ __forceinline__ void tc_alloc(uint32_t *slot, uint32_t columns) {
