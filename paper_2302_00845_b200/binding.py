@@ -9,6 +9,9 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+
+import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 # CDGRAB_LIB: file name (inside the package) of a diagnostic build to load instead
@@ -348,142 +351,155 @@ def herding_objective(z, perms, stream=None) -> float:
 
 
 # ---- training operators --------------------------------------------------------------------------
-def _want(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+# A call costs a few microseconds of host time, as much as a small operator takes on the device: checks
+# build their messages only when they fail, and shapes cross the boundary as one packed struct.
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+_SHAPE = struct.Struct("7if24q")          # cdgrab_attention_shape
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _place(stream, *tensors):
+    """Where an operator runs: the raw stream, and the torch stream whose pool its outputs and scratch come
+    from when that is not the current one (so that freeing them is ordered after the launches)."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors have to be on the current CUDA device")
+    current = _raw_stream(dev)
+    if stream is None or stream.cuda_stream == current:
+        return current, None
+    return stream.cuda_stream, stream
+
+
+def _empty(like, shape, dtype, other):
+    if other is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(other):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _code(t, name: str) -> int:
-    import torch
-    _want(t.dtype in (torch.float32, torch.bfloat16), f"{name}: float32 or bfloat16, not {t.dtype}")
-    return F32 if t.dtype == torch.float32 else BF16
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: float32 or bfloat16, not {t.dtype}")
+    return code
 
 
-class _OnStream:
-    """Where an operator runs: the handle its launches go to, and allocation of its outputs and
-    scratch from that stream's pool (so that freeing them is ordered after the launches)."""
-
-    def __init__(self, stream, *tensors):
-        import torch
-        dev = torch.cuda.current_device()
-        for t in tensors:
-            _want(t is None or (t.is_cuda and t.device.index == dev), "tensors have to be on the current CUDA device")
-        self.torch, self.other = torch, None
-        if stream is None:
-            self.handle = torch.cuda.current_stream().cuda_stream
-        else:
-            self.handle = stream.cuda_stream
-            if self.handle != torch.cuda.current_stream().cuda_stream:
-                self.other = stream
-        self.device = torch.device("cuda", dev)
-
-    def empty(self, shape, dtype):
-        if self.other is None:
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
-        with self.torch.cuda.stream(self.other):
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
-
-    def scratch(self, nbytes: int):
-        return self.empty((max(16, nbytes),), self.torch.uint8)
-
-
-def _rows_of(t, name: str, rows=None, cols=None):
+def _row_stride(t, name: str, rows: int, cols: int) -> int:
     """Row stride of a [rows][cols] tensor with contiguous rows."""
-    _want(t.dim() == 2 and (rows is None or tuple(t.shape) == (rows, cols)), f"{name}: shape {tuple(t.shape)}")
-    _want(t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: the values of a row have to be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} where ({rows}, {cols}) is wanted")
+    stride, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{name}: the values of a row have to be contiguous")
+    return stride if rows > 1 else max(stride, cols)
 
 
 def _vector(t, name: str, n: int):
-    import torch
     if t is None:
         return None
-    _want(t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous(),
-          f"{name}: a contiguous float32 tensor [{n}]")
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous float32 tensor [{n}]")
     return t.data_ptr()
 
 
 def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None):
     """Layer normalisation of the rows of x [rows][cols] (float32 or bfloat16; rows may be strided) with
     float32 weight and bias [cols] or None.  Returns (y, mean, rstd)."""
-    import torch
-    on = _OnStream(stream, x, weight, bias, out)
-    xs = _rows_of(x, "x")
+    handle, other = _place(stream, x, weight, bias, out)
+    if x.dim() != 2:
+        raise ValueError(f"x: [rows][cols], not {tuple(x.shape)}")
     rows, cols = x.shape
     code = _code(x, "x")
+    xs = _row_stride(x, "x", rows, cols)
     w, b = _vector(weight, "weight", cols), _vector(bias, "bias", cols)
-    y = on.empty((rows, cols), x.dtype) if out is None else out
-    _want(y.dtype == x.dtype, "out: the type of x")
-    stats = on.empty((2, rows), torch.float32)
-    base = stats.data_ptr()
-    _check(lib().cdgrab_layer_norm_forward(rows, cols, code, x.data_ptr(), xs, w, b, eps, y.data_ptr(),
-                                           _rows_of(y, "out", rows, cols), base, base + 4 * rows, on.handle),
-           "cdgrab_layer_norm_forward")
-    return y, stats[0], stats[1]
+    if out is None:
+        y, ys = _empty(x, (rows, cols), x.dtype, other), cols
+    else:
+        y, ys = out, _row_stride(out, "out", rows, cols)
+        if out.dtype != x.dtype:
+            raise ValueError("out: the type of x")
+    mean, rstd = _empty(x, (rows,), torch.float32, other), _empty(x, (rows,), torch.float32, other)
+    rc = lib().cdgrab_layer_norm_forward(rows, cols, code, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys, mean.data_ptr(),
+                                         rstd.data_ptr(), handle)
+    if rc:
+        _check(rc, "cdgrab_layer_norm_forward")
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=None, dx=None, stream=None):
     """Backward pass of layer_norm_forward for m workers' rows: dy, x [m * rows][cols]; dweight and dbias
     [m][cols] (float32 or bfloat16, equal row strides, views into the gather buffer as a rule) receive each
     worker's own sums, either may be None.  Returns dx."""
-    on = _OnStream(stream, dy, x, weight, mean, rstd, dweight, dbias, dx)
+    handle, other = _place(stream, dy, x, weight, mean, rstd, dweight, dbias, dx)
+    if x.dim() != 2:
+        raise ValueError(f"x: [rows][cols], not {tuple(x.shape)}")
     rows, cols = x.shape
-    _want(dy.dtype == x.dtype, "dy: the type of x")
     code = _code(x, "x")
+    if dy.dtype != x.dtype:
+        raise ValueError("dy: the type of x")
     g = dweight if dweight is not None else dbias
-    m = 1 if g is None else g.shape[0]
-    _want(m >= 1 and rows % m == 0, f"{rows} rows are not {m} workers' equal shares")
-    gcode, ws = F32, cols
+    m, gcode, ws, pw, pb = 1, F32, cols, None, None
     if g is not None:
-        gcode, ws = _code(g, "dweight, dbias"), _rows_of(g, "dweight, dbias", m, cols)
-        for t in (dweight, dbias):
-            _want(t is None or (t.dtype == g.dtype and _rows_of(t, "dweight, dbias", m, cols) == ws),
-                  "dweight and dbias: one type and one row stride")
+        m = g.shape[0]
+        if m < 1 or rows % m:
+            raise ValueError(f"{rows} rows are not {m} workers' equal shares")
+        gcode, ws = _code(g, "dweight, dbias"), _row_stride(g, "dweight, dbias", m, cols)
+        if dweight is not None:
+            pw = dweight.data_ptr()
+        if dbias is not None:
+            pb = dbias.data_ptr()
+            if dbias is not g and (dbias.dtype != g.dtype or _row_stride(dbias, "dbias", m, cols) != ws):
+                raise ValueError("dweight and dbias: one type and one row stride")
     if dx is None:
-        dx = on.empty((rows, cols), x.dtype)
-    _want(dx.dtype == x.dtype, "dx: the type of x")
+        dx, dxs = _empty(x, (rows, cols), x.dtype, other), cols
+    else:
+        dxs = _row_stride(dx, "dx", rows, cols)
+        if dx.dtype != x.dtype:
+            raise ValueError("dx: the type of x")
     L = lib()
     nbytes = L.cdgrab_layer_norm_workspace_bytes(m, rows // m, cols)
-    scratch = on.scratch(nbytes)
-    _check(L.cdgrab_layer_norm_backward(
-        m, rows // m, cols, code, dy.data_ptr(), _rows_of(dy, "dy", rows, cols), x.data_ptr(), _rows_of(x, "x"),
-        _vector(weight, "weight", cols), _vector(mean, "mean", rows), _vector(rstd, "rstd", rows), dx.data_ptr(),
-        _rows_of(dx, "dx", rows, cols), gcode, None if dweight is None else dweight.data_ptr(),
-        None if dbias is None else dbias.data_ptr(), ws, scratch.data_ptr(), scratch.numel(), on.handle),
-        "cdgrab_layer_norm_backward")
+    scratch = _empty(x, (max(16, nbytes),), torch.uint8, other)
+    rc = L.cdgrab_layer_norm_backward(
+        m, rows // m, cols, code, dy.data_ptr(), _row_stride(dy, "dy", rows, cols), x.data_ptr(),
+        _row_stride(x, "x", rows, cols), _vector(weight, "weight", cols), _vector(mean, "mean", rows),
+        _vector(rstd, "rstd", rows), dx.data_ptr(), dxs, gcode, pw, pb, ws, scratch.data_ptr(), max(16, nbytes), handle)
+    if rc:
+        _check(rc, "cdgrab_layer_norm_backward")
     return dx
 
 
-def _attention_shape(q, k, v, causal, scale):
-    import torch
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _want(t.dtype == torch.bfloat16 and t.dim() == 4, f"{name}: a bfloat16 tensor [batch][token][head][head_dim]")
+def _head_strides(t, name: str, shape):
+    """(batch, token, head) strides of a [batch][token][head][head_dim] tensor."""
+    if t.dtype != torch.bfloat16 or t.shape != shape:
+        raise ValueError(f"{name}: a bfloat16 tensor of shape {tuple(shape)}, not {tuple(t.shape)} {t.dtype}")
+    a, b, c, inner = t.stride()
+    if inner != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: the values of a head have to be contiguous")
+    if (a | b | c) & 7:         # an axis of length one has no stride of its own
+        a, b, c = ((v + 7) & ~7 if n <= 1 else v for v, n in zip((a, b, c), shape))
+    return a, b, c
+
+
+_NONE = (0, 0, 0)
+
+
+def _attention_sizes(q, k, v, causal, scale):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k, v: [batch][token][head][head_dim]")
     b, tq, h, d = q.shape
-    _, tk, hk, _ = k.shape
-    _want(tuple(k.shape) == (b, tk, hk, d) and tuple(v.shape) == (b, tk, hk, d), "q, k and v do not go together")
-    sh = AttentionShape(b, tq, tk, h, hk, d, int(bool(causal)), d ** -0.5 if scale is None else scale)
-    _strides(sh.q_stride, q, "q")
-    _strides(sh.k_stride, k, "k")
-    _strides(sh.v_stride, v, "v")
-    return sh
-
-
-def _strides(field, t, name: str, like=None):
-    _want(like is None or (t.shape == like.shape and t.dtype == like.dtype), f"{name}: shape {tuple(t.shape)}, {t.dtype}")
-    s = t.stride()
-    _want(s[3] == 1 or t.shape[3] <= 1, f"{name}: the values of a head have to be contiguous")
-    field[0], field[1], field[2] = s[:3]
-    # an axis of length one has no stride of its own
-    for i in range(3):
-        if t.shape[i] <= 1:
-            field[i] = (field[i] + 7) & ~7
+    kb, tk, hk, kd = k.shape
+    if kb != b or kd != d:
+        raise ValueError("q, k and v do not go together")
+    sizes = (b, tq, tk, h, hk, d, 1 if causal else 0, d ** -0.5 if scale is None else scale)
+    return sizes, _head_strides(q, "q", q.shape) + _head_strides(k, "k", k.shape) + _head_strides(v, "v", k.shape)
 
 
 def _lens(t, name: str, batch: int):
-    import torch
     if t is None:
         return None
-    _want(t.dtype == torch.int32 and tuple(t.shape) == (batch,) and t.is_contiguous(), f"{name}: an int32 tensor [{batch}]")
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != batch or not t.is_contiguous():
+        raise ValueError(f"{name}: an int32 tensor [{batch}]")
     return t.data_ptr()
 
 
@@ -492,15 +508,17 @@ def attention_forward(q, k, v, causal: bool = False, scale: float | None = None,
     """Softmax attention of q [b][t_q][h][d] with k, v [b][t_kv][h_kv][d], bfloat16, any strides that are
     multiples of 8 (slices of one projection's output).  scale: d**-0.5 by default.  q_lens, kv_lens: int32
     [b], the tokens in use.  Returns (o, lse): o like q, lse float32 [b][h][t_q]."""
-    import torch
-    on = _OnStream(stream, q, k, v, q_lens, kv_lens, out)
-    sh = _attention_shape(q, k, v, causal, scale)
-    o = on.empty(q.shape, q.dtype) if out is None else out
-    _strides(sh.o_stride, o, "out", q)
-    lse = on.empty((sh.batch, sh.heads, sh.len_q), torch.float32)
-    _check(lib().cdgrab_attention_forward(C.byref(sh), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                          _lens(q_lens, "q_lens", sh.batch), _lens(kv_lens, "kv_lens", sh.batch),
-                                          o.data_ptr(), lse.data_ptr(), on.handle), "cdgrab_attention_forward")
+    handle, other = _place(stream, q, k, v, q_lens, kv_lens, out)
+    sizes, strides = _attention_sizes(q, k, v, causal, scale)
+    b, tq, h = sizes[0], sizes[1], sizes[3]
+    o = _empty(q, q.shape, q.dtype, other) if out is None else out
+    sh = AttentionShape.from_buffer_copy(_SHAPE.pack(*sizes, *strides, *_head_strides(o, "out", q.shape), *_NONE, *_NONE,
+                                                     *_NONE, *_NONE))
+    lse = _empty(q, (b, h, tq), torch.float32, other)
+    rc = lib().cdgrab_attention_forward(sh, q.data_ptr(), k.data_ptr(), v.data_ptr(), _lens(q_lens, "q_lens", b),
+                                        _lens(kv_lens, "kv_lens", b), o.data_ptr(), lse.data_ptr(), handle)
+    if rc:
+        _check(rc, "cdgrab_attention_forward")
     return o, lse
 
 
@@ -508,47 +526,58 @@ def attention_backward(do, q, k, v, o, lse, causal: bool = False, scale: float |
                        kv_lens=None, dq=None, dk=None, dv=None, stream=None):
     """Backward pass of attention_forward from its outputs o and lse and the gradient do of o.
     Returns (dq, dk, dv); destinations may be given (views of one buffer as a rule)."""
-    import torch
-    on = _OnStream(stream, do, q, k, v, o, lse, q_lens, kv_lens, dq, dk, dv)
-    sh = _attention_shape(q, k, v, causal, scale)
-    _want(lse.dtype == torch.float32 and tuple(lse.shape) == (sh.batch, sh.heads, sh.len_q) and lse.is_contiguous(),
-          "lse: a contiguous float32 tensor [batch][heads][len_q]")
-    dq = on.empty(q.shape, q.dtype) if dq is None else dq
-    dk = on.empty(k.shape, k.dtype) if dk is None else dk
-    dv = on.empty(v.shape, v.dtype) if dv is None else dv
-    for field, t, name, like in ((sh.o_stride, o, "o", q), (sh.do_stride, do, "do", q), (sh.dq_stride, dq, "dq", q),
-                                 (sh.dk_stride, dk, "dk", k), (sh.dv_stride, dv, "dv", v)):
-        _strides(field, t, name, like)
+    handle, other = _place(stream, do, q, k, v, o, lse, q_lens, kv_lens, dq, dk, dv)
+    sizes, strides = _attention_sizes(q, k, v, causal, scale)
+    b, tq, h = sizes[0], sizes[1], sizes[3]
+    if lse.dtype != torch.float32 or lse.shape != (b, h, tq) or not lse.is_contiguous():
+        raise ValueError("lse: a contiguous float32 tensor [batch][heads][len_q]")
+    dq = _empty(q, q.shape, q.dtype, other) if dq is None else dq
+    dk = _empty(k, k.shape, k.dtype, other) if dk is None else dk
+    dv = _empty(v, v.shape, v.dtype, other) if dv is None else dv
+    qs, ks = q.shape, k.shape
+    sh = AttentionShape.from_buffer_copy(_SHAPE.pack(
+        *sizes, *strides, *_head_strides(o, "o", qs), *_head_strides(do, "do", qs), *_head_strides(dq, "dq", qs),
+        *_head_strides(dk, "dk", ks), *_head_strides(dv, "dv", ks)))
     L = lib()
-    nbytes = L.cdgrab_attention_workspace_bytes(C.byref(sh))
-    scratch = on.scratch(nbytes)
-    _check(L.cdgrab_attention_backward(
-        C.byref(sh), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-        _lens(q_lens, "q_lens", sh.batch), _lens(kv_lens, "kv_lens", sh.batch), dq.data_ptr(), dk.data_ptr(),
-        dv.data_ptr(), scratch.data_ptr(), scratch.numel(), on.handle), "cdgrab_attention_backward")
+    nbytes = L.cdgrab_attention_workspace_bytes(sh)
+    scratch = _empty(q, (max(16, nbytes),), torch.uint8, other)
+    rc = L.cdgrab_attention_backward(
+        sh, do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+        _lens(q_lens, "q_lens", b), _lens(kv_lens, "kv_lens", b), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        scratch.data_ptr(), max(16, nbytes), handle)
+    if rc:
+        _check(rc, "cdgrab_attention_backward")
     return dq, dk, dv
 
 
 def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, stream=None):
     """The orthogonalised update of a gradient g [rows][cols] or [batch][rows][cols] (float32 or bfloat16):
     `steps` Newton-Schulz products on g / (|g| + eps).  Returns a bfloat16 tensor of g's shape."""
-    import torch
-    on = _OnStream(stream, g, out)
-    _want(g.dim() in (2, 3), "g: [rows][cols] or [batch][rows][cols]")
-    o = on.empty(g.shape, torch.bfloat16) if out is None else out
-    _want(o.dtype == torch.bfloat16 and o.shape == g.shape, "out: a bfloat16 tensor of g's shape")
-    g3, o3 = (t if t.dim() == 3 else t.unsqueeze(0) for t in (g, o))
-    batch, rows, cols = g3.shape
-    _want(len(coeffs) == 3, "coeffs: three numbers")
-    for t, name in ((g3, "g"), (o3, "out")):
-        _want(cols <= 1 or t.stride(2) == 1, f"{name}: the values of a row have to be contiguous")
-    row = [t.stride(1) if rows > 1 else max(cols, t.stride(1)) for t in (g3, o3)]
+    handle, other = _place(stream, g, out)
+    o = _empty(g, g.shape, torch.bfloat16, other) if out is None else out
+    if g.dim() not in (2, 3):
+        raise ValueError("g: [rows][cols] or [batch][rows][cols]")
+    if o.dtype != torch.bfloat16 or o.shape != g.shape:
+        raise ValueError("out: a bfloat16 tensor of g's shape")
+    if len(coeffs) != 3:
+        raise ValueError("coeffs: three numbers")
+    rows, cols = g.shape[-2:]
+    batch = g.shape[0] if g.dim() == 3 else 1
+    strides = []
+    for t, name in ((g, "g"), (o, "out")):
+        s = t.stride()
+        if s[-1] != 1 and cols > 1:
+            raise ValueError(f"{name}: the values of a row have to be contiguous")
+        strides += [s[0] if len(s) == 3 else 0, s[-2] if rows > 1 else max(cols, s[-2])]
+    code = _code(g, "g")
     L = lib()
     nbytes = L.cdgrab_orthogonalise_workspace_bytes(batch, rows, cols)
-    scratch = on.scratch(nbytes)
-    _check(L.cdgrab_orthogonalise(batch, rows, cols, _code(g, "g"), g.data_ptr(), g3.stride(0), row[0], steps,
-                                  (C.c_float * 3)(*coeffs), eps, o.data_ptr(), o3.stride(0), row[1],
-                                  scratch.data_ptr(), scratch.numel(), on.handle), "cdgrab_orthogonalise")
+    scratch = _empty(g, (max(16, nbytes),), torch.uint8, other)
+    rc = L.cdgrab_orthogonalise(batch, rows, cols, code, g.data_ptr(), strides[0], strides[1], steps,
+                                (C.c_float * 3)(*coeffs), eps, o.data_ptr(), strides[2], strides[3], scratch.data_ptr(),
+                                max(16, nbytes), handle)
+    if rc:
+        _check(rc, "cdgrab_orthogonalise")
     return o
 
 
