@@ -24,6 +24,7 @@ int cdg_ops_device(const CdgOpsDevice **out) {
       return CDGRAB_ERR_DEVICE;
     }
     // two threads that arrive together write the same values
+    g_ops[dev].index = dev;
     g_ops[dev].sms = sms;
     g_ops[dev].status = static_cast<int *>(p);
     g_ready[dev].store(1, std::memory_order_release);

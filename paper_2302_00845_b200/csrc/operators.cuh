@@ -5,6 +5,7 @@
 #include "common.cuh"
 
 struct CdgOpsDevice {
+  int index;      // the device
   int sms;        // multiprocessors
   int *status;    // the operators' device status word (CDG_ST_* bits)
 };
