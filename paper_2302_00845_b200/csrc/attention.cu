@@ -62,7 +62,7 @@ __device__ __forceinline__ void zero_rows(uint8_t *tile, int from) {
   __syncwarp();
 }
 
-// products of one tile, issued by one thread.  128-row operands, DP = 64 NP head dimensions.
+// products of one tile, called by a whole warp.  128-row operands, DP = 64 NP head dimensions.
 // scores: D[128][128] = A B^T over the head dimension
 template <int NP>
 __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
@@ -207,12 +207,11 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     bool ok = tiles == 0 || tc_wait(&q_full, 0, deadline);
     if (ok && tiles > 0) ok = tc_wait(&k_full[0], 0, deadline);
     tc_fence_after();
-    if (ok && tiles > 0 && tc_elect()) {
+    if (ok && tiles > 0) {
       for (int t = 0; t < 2; ++t)
-        if (n[t] > 0) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(smem_u32(&s_full[t])); }
-      tc_commit(smem_u32(&k_empty[0]));
+        if (n[t] > 0) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(&s_full[t]); }
+      tc_commit(&k_empty[0]);
     }
-    __syncwarp();
     for (int j = 0; j < tiles && ok; ++j) {
       const int vs = j % F::ring, ks = (j + 1) % F::ring;
       const uint32_t k_next = sk + ks * F::tile, v_this = sv + vs * F::tile;
@@ -224,31 +223,23 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         if (NP == 1 && j + 1 < n[t]) {               // S_t(j) is in registers: the next one may overwrite it
           if (!(ok = tc_wait(&s_free[t], j & 1, deadline))) break;
           tc_fence_after();
-          if (tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(smem_u32(&s_full[t])); }
-          __syncwarp();
+          mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]); 
         }
         if (j < n[t]) {
           if (!(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
           tc_fence_after();
-          if (tc_elect()) {
-            mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
-            tc_commit(smem_u32(&pv_done[t]));
-          }
-          __syncwarp();
+                      mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
+            tc_commit(&pv_done[t]);
         }
         if (NP == 2 && j + 1 < n[t]) {               // P_t lies over S_t: its product has to be over
           if (!(ok = tc_wait(&pv_done[t], j & 1, deadline))) break;
           tc_fence_after();
-          if (tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(smem_u32(&s_full[t])); }
-          __syncwarp();
+          mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]); 
         }
       }
       if (!ok) break;
-      if (tc_elect()) {
-        tc_commit(smem_u32(&v_empty[vs]));
-        if (j + 1 < tiles) tc_commit(smem_u32(&k_empty[ks]));
-      }
-      __syncwarp();
+              tc_commit(&v_empty[vs]);
+        if (j + 1 < tiles) tc_commit(&k_empty[ks]);
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
@@ -509,42 +500,32 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     bool ok = true;
     if (total > 0) {
       ok = tc_wait(&kv_full, 0, deadline) && arrived(q_full, sq, 0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm, sk, sq); tc_commit(smem_u32(&s_full)); }
-      __syncwarp();
+      if (ok) { mma_scores<NP>(tm, sk, sq); tc_commit(&s_full); }
       ok = ok && arrived(do_full, sdo, 0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(smem_u32(&dp_full)); }
-      __syncwarp();
+      if (ok) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(&dp_full); }
     }
     for (int it = 0; it < total && ok; ++it) {
       const int s = it % F::ring, sn = (it + 1) % F::ring;
       const bool next = it + 1 < total;
       if (!(ok = tc_wait(&p_ready, it & 1, deadline))) break;
       tc_fence_after();
-      if (tc_elect()) {
-        mma_rows<NP>(tm + F::dv, tm, 64, sdo + s * F::tile, it > 0);
-        tc_commit(smem_u32(&dv_done));
-        tc_commit(smem_u32(&do_empty[s]));
-      }
-      __syncwarp();
+              mma_rows<NP>(tm + F::dv, tm, 64, sdo + s * F::tile, it > 0);
+        tc_commit(&dv_done);
+        tc_commit(&do_empty[s]);
       if (next) {              // S lies under P: its product has to be over
         if (!(ok = arrived(q_full, sq, it + 1) && tc_wait(&dv_done, it & 1, deadline))) break;
         tc_fence_after();
-        if (tc_elect()) { mma_scores<NP>(tm, sk, sq + sn * F::tile); tc_commit(smem_u32(&s_full)); }
-        __syncwarp();
+        mma_scores<NP>(tm, sk, sq + sn * F::tile); tc_commit(&s_full); 
       }
       if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
       tc_fence_after();
-      if (tc_elect()) {
-        mma_rows<NP>(tm + F::dk, tm + kT, 64, sq + s * F::tile, it > 0);
-        tc_commit(smem_u32(&dk_done));
-        tc_commit(smem_u32(&q_empty[s]));
-      }
-      __syncwarp();
+              mma_rows<NP>(tm + F::dk, tm + kT, 64, sq + s * F::tile, it > 0);
+        tc_commit(&dk_done);
+        tc_commit(&q_empty[s]);
       if (next) {
         if (!(ok = arrived(do_full, sdo, it + 1) && tc_wait(&dk_done, it & 1, deadline))) break;
         tc_fence_after();
-        if (tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo + sn * F::tile); tc_commit(smem_u32(&dp_full)); }
-        __syncwarp();
+        mma_scores<NP>(tm + kT, sv, sdo + sn * F::tile); tc_commit(&dp_full); 
       }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
@@ -724,11 +705,9 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     bool ok = true;
     if (total > 0) {
       ok = tc_wait(&q_full, 0, deadline) && arrived(0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm, sq, sk); tc_commit(smem_u32(&s_full)); }
-      __syncwarp();
+      if (ok) { mma_scores<NP>(tm, sq, sk); tc_commit(&s_full); }
       ok = ok && tc_wait(&v_full[0], 0, deadline);
-      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(smem_u32(&dp_full)); tc_commit(smem_u32(&v_empty[0])); }
-      __syncwarp();
+      if (ok) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(&dp_full); tc_commit(&v_empty[0]); }
     }
     for (int it = 0; it < total && ok; ++it) {
       const int s = it % F::ring, sn = (it + 1) % F::ring;
@@ -736,22 +715,17 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       if (next) {              // S is in registers: the next one may overwrite it
         if (!(ok = arrived(it + 1) && tc_wait(&s_free, it & 1, deadline))) break;
         tc_fence_after();
-        if (tc_elect()) { mma_scores<NP>(tm, sq, sk + sn * F::tile); tc_commit(smem_u32(&s_full)); }
-        __syncwarp();
+        mma_scores<NP>(tm, sq, sk + sn * F::tile); tc_commit(&s_full); 
       }
       if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
       tc_fence_after();
-      if (tc_elect()) {
-        mma_rows<NP>(tm + F::dq, tm + kT, 64, sk + s * F::tile, it > 0);
-        tc_commit(smem_u32(&dq_done));
-        tc_commit(smem_u32(&k_empty[s]));
-      }
-      __syncwarp();
+              mma_rows<NP>(tm + F::dq, tm + kT, 64, sk + s * F::tile, it > 0);
+        tc_commit(&dq_done);
+        tc_commit(&k_empty[s]);
       if (next) {              // dP lies under dS: its product has to be over
         if (!(ok = tc_wait(&v_full[sn], ((it + 1) / F::ring) & 1, deadline) && tc_wait(&dq_done, it & 1, deadline))) break;
         tc_fence_after();
-        if (tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv + sn * F::tile); tc_commit(smem_u32(&dp_full)); tc_commit(smem_u32(&v_empty[sn])); }
-        __syncwarp();
+        mma_scores<NP>(tm + kT, sdo, sv + sn * F::tile); tc_commit(&dp_full); tc_commit(&v_empty[sn]); 
       }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);

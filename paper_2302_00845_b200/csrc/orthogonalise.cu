@@ -160,23 +160,21 @@ __global__ void __launch_bounds__(128) orth_product(const __grid_constant__ CUte
       }
     }
   } else if (warp == 1) {
-    if (tc_elect()) {
-      constexpr uint32_t idesc = tc_idesc(false, kTile, kTile, false, !symmetric);
-      bool ok = true;
-      for (int it = 0; it < nk; ++it) {
-        const int s = it % kStages;
-        if (!(ok = mbar_wait(smem_u32(&full[s]), (it / kStages) & 1, deadline))) break;
-        tc_fence_after();
-        const uint32_t a = ring + s * kStageBytes, b = a + kOperandBytes;
+    constexpr uint32_t idesc = tc_idesc(false, kTile, kTile, false, !symmetric);
+    bool ok = true;
+    for (int it = 0; it < nk; ++it) {
+      const int s = it % kStages;
+      if (!(ok = tc_wait(&full[s], (it / kStages) & 1, deadline))) break;
+      tc_fence_after();
+      const uint32_t a = ring + s * kStageBytes, b = a + kOperandBytes;
 #pragma unroll
-        for (int kk = 0; kk < kK / 16; ++kk)
-          tc_mma(acc, tc_desc_k(a + kk * 32), symmetric ? tc_desc_k(b + kk * 32) : tc_desc_mn(b + kk * 2048, kOperandBytes / 2),
-                 idesc, it > 0 || kk > 0);
-        tc_commit(smem_u32(&empty[s]));
-      }
-      if (!ok) atomicOr(p.status, CDG_ST_TIMEOUT);
-      tc_commit(smem_u32(&done));
+      for (int kk = 0; kk < kK / 16; ++kk)
+        tc_mma(acc, tc_desc_k(a + kk * 32), symmetric ? tc_desc_k(b + kk * 32) : tc_desc_mn(b + kk * 2048, kOperandBytes / 2),
+               idesc, it > 0 || kk > 0);
+      tc_commit(&empty[s]);
     }
+    if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
+    tc_commit(&done);
   }
   __syncwarp();
 
