@@ -40,6 +40,26 @@ enum { kQ = 1, kK = 2, kV = 4, kDo = 8 };
 __device__ __forceinline__ int batch_of(const Sizes &z, int which, int b) { return z.shared & which ? 0 : b; }
 __device__ __forceinline__ int used(const int *lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// two fp32 operations to an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\n"
+      "fma.rn.f32x2 z, x, y, z;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&h);
@@ -62,25 +82,25 @@ __device__ __forceinline__ void zero_rows(uint8_t *tile, int from) {
   __syncwarp();
 }
 
-// products of one tile, called by a whole warp.  128-row operands, DP = 64 NP head dimensions.
+// products of one tile, issued by one thread.  128-row operands, DP = 64 NP head dimensions.
 // scores: D[128][128] = A B^T over the head dimension
 template <int NP>
 __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
   constexpr uint32_t idesc = tc_idesc(true, kT, kT, false, false);
+  const uint64_t da = tc_desc_k(a), db = tc_desc_k(b);          // addresses in units of 16 bytes
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      tc_mma(d, tc_desc_k(a + p * kT * 128 + k * 32), tc_desc_k(b + p * kT * 128 + k * 32), idesc, p > 0 || k > 0);
+    for (int k = 0; k < 4; ++k) tc_mma(d, da + (p * kT * 8 + k * 2), db + (p * kT * 8 + k * 2), idesc, p > 0 || k > 0);
 }
 // weighted rows: D[128][DP] (+)= W B, W a 128 x 128 bf16 operand in tensor memory whose columns 64..127
 // start `half` 32-bit columns after the first, B 128 rows of DP values
 template <int NP>
 __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, uint32_t half, uint32_t b, bool add) {
   constexpr uint32_t idesc = tc_idesc(true, kT, 64 * NP, false, true);
+  const uint64_t db = tc_desc_mn(b, kT * 128);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    tc_mma_ta(d, w + (k >> 2) * half + (k & 3) * 8, tc_desc_mn(b + k * 2048, kT * 128), idesc, add || k > 0);
+  for (int k = 0; k < 8; ++k) tc_mma_ta(d, w + (k >> 2) * half + (k & 3) * 8, db + k * 128, idesc, add || k > 0);
 }
 
 // 32 rows of DP bf16 values from registers to memory through this warp's part of a tile: each lane
@@ -209,8 +229,11 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     tc_fence_after();
     if (ok && tiles > 0) {
       for (int t = 0; t < 2; ++t)
-        if (n[t] > 0) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(&s_full[t]); }
-      tc_commit(&k_empty[0]);
+        if (n[t] > 0 && tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(&s_full[t]); }
+      if (tc_elect()) {
+        tc_commit(&k_empty[0]);
+      }
+      __syncwarp();
     }
     for (int j = 0; j < tiles && ok; ++j) {
       const int vs = j % F::ring, ks = (j + 1) % F::ring;
@@ -223,23 +246,35 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         if (NP == 1 && j + 1 < n[t]) {               // S_t(j) is in registers: the next one may overwrite it
           if (!(ok = tc_wait(&s_free[t], j & 1, deadline))) break;
           tc_fence_after();
-          mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]); 
+          if (tc_elect()) {
+            mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]);
+          }
+          __syncwarp();
         }
         if (j < n[t]) {
           if (!(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
           tc_fence_after();
-                      mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
-            tc_commit(&pv_done[t]);
+                      if (tc_elect()) {
+                        mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
+                        tc_commit(&pv_done[t]);
+                      }
+                      __syncwarp();
         }
         if (NP == 2 && j + 1 < n[t]) {               // P_t lies over S_t: its product has to be over
           if (!(ok = tc_wait(&pv_done[t], j & 1, deadline))) break;
           tc_fence_after();
-          mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]); 
+          if (tc_elect()) {
+            mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]);
+          }
+          __syncwarp();
         }
       }
       if (!ok) break;
-              tc_commit(&v_empty[vs]);
-        if (j + 1 < tiles) tc_commit(&k_empty[ks]);
+              if (tc_elect()) {
+                tc_commit(&v_empty[vs]);
+                if (j + 1 < tiles) tc_commit(&k_empty[ks]);
+              }
+              __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
@@ -354,8 +389,8 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
 }
 
 // ---- backward -----------------------------------------------------------------------------------
-// For every query row: delta = sum_d do o, and lse in base 2 (+infinity where the row sees nothing, so that
-// its recomputed probabilities are 0).  Rows are padded to whole tiles: [batch][heads][2][rows], first lse.
+// For every query row: -delta = -sum_d do o, and -lse in base 2 (-infinity where the row sees nothing, so
+// that its recomputed probabilities are 0).  Rows are padded to whole tiles: [batch][heads][2][rows], first lse.
 // Eight lanes to a row and head, 16 bytes a lane.
 __global__ void __launch_bounds__(256) attn_delta(const Sizes z, const View d_o, const View o, const float *__restrict__ lse,
                                                   float *__restrict__ out, int padded) {
@@ -365,7 +400,7 @@ __global__ void __launch_bounds__(256) attn_delta(const Sizes z, const View d_o,
   const int l = threadIdx.x & 7;
   const int h = (int)(group % z.heads), i = (int)(group / z.heads % padded), b = (int)(group / z.heads / padded);
   if (b >= z.batch) return;
-  float s = 0.0f, l2 = INFINITY;
+  float s = 0.0f, l2 = -INFINITY;
   if (i < used(z.q_lens, b, z.tq)) {
     const bf16 *x = d_o.p + b * d_o.b + i * d_o.t + h * d_o.h, *y = o.p + b * o.b + i * o.t + h * o.h;
 #pragma unroll
@@ -380,15 +415,15 @@ __global__ void __launch_bounds__(256) attn_delta(const Sizes z, const View d_o,
         s = fmaf(f.x, g.x, fmaf(f.y, g.y, s));
       }
     }
-    l2 = lse[((long long)b * z.heads + h) * z.tq + i] * kLog2e;
-    if (l2 == -INFINITY) l2 = INFINITY;
+    l2 = lse[((long long)b * z.heads + h) * z.tq + i] * -kLog2e;
+    if (l2 == INFINITY) l2 = -INFINITY;
   }
 #pragma unroll
   for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off, 8);
   if (l == 0) {
     float *row = out + ((long long)b * z.heads + h) * 2 * padded + i;
     row[0] = l2;
-    row[padded] = l2 == INFINITY ? 0.0f : s;
+    row[padded] = l2 == -INFINITY ? 0.0f : -s;
   }
 }
 
@@ -399,21 +434,76 @@ __device__ __forceinline__ void load_line(uint32_t dst, const float *src, uint32
 }
 
 // Both backward kernels: eight warps work on a tile of scores, four on its columns 0..63 and four on
-// 64..127, one row per thread.  Columns of tensor memory: S (then P, as bf16, over each half's own
-// scores) and dP (then dS likewise), then the accumulators.
+// 64..127, one row per thread.
 //   warps 0-7  P and dS        warp 8  bulk copies        warp 9  products
+// The rings are as deep as shared memory allows: a tile of Q (or K) is used twice, at the beginning and at
+// the end of its turn, and a copy takes about 1700 cycles; with two stages each the products waited for it
+// (3500 cycles a tile at 128 head dimensions).
 constexpr int kBwdThreads = 320;
+
+// Where there are few tiles of rows, the loop over the other axis is dealt out over a cluster of CTAs, whose
+// fp32 sums are joined through distributed shared memory, in the order of their ranks.
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 peer_load(uint32_t addr, uint32_t rank) {
+  uint32_t there;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+  return v;
+}
+// fp32 sums of a tile in shared memory, [128][DP] with 16-byte pieces permuted by row, so that neither a row
+// per thread nor a row per warp meets bank conflicts
+template <int NP> __device__ __forceinline__ uint32_t sum_at(int row, int piece) {
+  return (uint32_t)(row * NP * 256 + (((piece & ~7) | ((piece ^ row) & 7)) << 4));
+}
+template <int NP>
+__device__ __forceinline__ void keep_sums(uint8_t *sums, int row, int c0, const uint32_t (&w)[32]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *reinterpret_cast<uint4 *>(sums + sum_at<NP>(row, (c0 >> 2) + i)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+// this CTA's share of the rows of a tile: the cluster's sums added up, scaled and written
+template <int NP>
+__device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, int thread, int threads, int token0, int tokens, int used_tokens,
+                                          const Sizes &z, float f, bf16 *dst, long long stride) {
+  const int rows = kT / ranks, per = z.dim >> 3;
+  for (int i = thread; i < rows * per; i += threads) {
+    const int r = rank * rows + i / per, chunk = i % per, token = token0 + r;
+    if (token >= tokens) continue;
+    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+    if (token < used_tokens)
+      for (int k = 0; k < ranks; ++k) {
+        const float4 u = peer_load(sums + sum_at<NP>(r, 2 * chunk), k), v = peer_load(sums + sum_at<NP>(r, 2 * chunk + 1), k);
+        a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+        b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
+      }
+    *reinterpret_cast<uint4 *>(dst + (long long)token * stride + chunk * 8) =
+        make_uint4(pack(a.x * f, a.y * f), pack(a.z * f, a.w * f), pack(b.x * f, b.y * f), pack(b.z * f, b.w * f));
+  }
+}
 
 // dk and dv of 128 keys: the loop runs over the query tiles of every query head that reads this key head.
 // Scores are transposed (a row is a key), so that P^T and dS^T are the row operands of
 //   dv += P^T dO,  dk += dS^T Q,    with  S^T = K Q^T,  dP^T = V dO^T.
-// Summing over query tiles and heads inside one CTA makes the result the same bits every time.
+// Summing over query tiles and heads in a fixed order makes the result the same bits every time.
+// Tensor memory: S at 0, dP at 128, dv and dk from 256; up to 64 head dimensions P and dS lie apart behind
+// them, above they lie over S and dP, each half of the warps over its own columns.
 template <int NP> struct Dkv {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int ring = 2;
+  static constexpr int q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 4 : 2, line_ring = 2;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
-  static constexpr size_t smem = 2 * tile + ring * (2 * tile + line) + 1024;
-  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
+  static constexpr uint32_t lines = (2 + q_ring + do_ring) * tile, bars = lines + line_ring * line;
+  static constexpr size_t smem = bars + 256;
+  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP, p = NP == 1 ? 384 : 0, ds = NP == 1 ? 448 : 128, half = NP == 1 ? 32 : 64;
+};
+template <int NP> struct DkvBars {
+  uint64_t kv_full, q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring], do_empty[Dkv<NP>::do_ring],
+      line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, s_free, dp_full, dp_free, p_ready, ds_ready, dv_done, dk_done;
+  uint32_t tmem;
 };
 
 template <int NP>
@@ -422,34 +512,33 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                  const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
                  const float *__restrict__ lines, int padded, const View dk, const View dv) {
   typedef Dkv<NP> F;
-  extern __shared__ uint8_t raw[];
-  __shared__ __align__(8) uint64_t kv_full, q_full[F::ring], q_empty[F::ring], do_full[F::ring], do_empty[F::ring], s_full,
-      dp_full, p_ready, ds_ready, dv_done, dk_done;
-  __shared__ uint32_t tmem_slot;
+  extern __shared__ __align__(1024) uint8_t base[];         // all of the CTA's shared memory: starts on a 1024-byte boundary
+  static_assert(sizeof(DkvBars<NP>) <= 256, "barriers behind the tiles");
+  DkvBars<NP> &bar = *reinterpret_cast<DkvBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-  const uint32_t sk = smem_u32(base), sv = sk + F::tile, sq = sv + F::tile, sdo = sq + F::ring * F::tile;
-  float *sline = reinterpret_cast<float *>(base + 2 * F::tile + 2 * F::ring * F::tile);      // [ring][2][128]
-  const int kv_heads = z.heads / z.group;
-  const int hk = blockIdx.x % kv_heads, b = blockIdx.x / kv_heads;
+  const uint32_t sk = smem_u32(base), sv = sk + F::tile, sq = sv + F::tile, sdo = sq + F::q_ring * F::tile;
+  float *sline = reinterpret_cast<float *>(base + F::lines);      // [ring][2][128]
+  const int ranks = (int)cluster_size(), rank = (int)cluster_rank(), kv_heads = z.heads / z.group;
+  const int column = blockIdx.x / ranks, hk = column % kv_heads, b = column / kv_heads;
   const int j0 = blockIdx.y * kT;            // the first keys, which most queries see, start first
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&kv_full), 1);
-    for (int i = 0; i < F::ring; ++i) {
-      mbar_init(smem_u32(&q_full[i]), 1); mbar_init(smem_u32(&q_empty[i]), 1);
-      mbar_init(smem_u32(&do_full[i]), 1); mbar_init(smem_u32(&do_empty[i]), 1);
-    }
-    mbar_init(smem_u32(&s_full), 1); mbar_init(smem_u32(&dp_full), 1);
-    mbar_init(smem_u32(&p_ready), 8); mbar_init(smem_u32(&ds_ready), 8);
-    mbar_init(smem_u32(&dv_done), 1); mbar_init(smem_u32(&dk_done), 1);
+    if (sk & 1023u) atomicOr(z.status, CDG_ST_TIMEOUT);      // (the copies' swizzle counts on it)
+    mbar_init(smem_u32(&bar.kv_full), 1);
+    for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
+    for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 1); }
+    for (int i = 0; i < F::line_ring; ++i) { mbar_init(smem_u32(&bar.line_full[i]), 1); mbar_init(smem_u32(&bar.line_empty[i]), 8); }
+    mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
+    mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
+    mbar_init(smem_u32(&bar.p_ready), 8); mbar_init(smem_u32(&bar.ds_ready), 8);
+    mbar_init(smem_u32(&bar.dv_done), 1); mbar_init(smem_u32(&bar.dk_done), 1);
     mbar_init_fence();
   }
-  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  if (warp == 9) tc_alloc(&bar.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tm = tmem_slot;
+  const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
@@ -458,176 +547,252 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   // query tiles first .. last - 1 see key j0 or a later one of this tile
   const int first = j0 >= lk ? 0 : z.causal ? max(0, j0 - (lk - lq)) / kT : 0;
   const int last = j0 >= lk ? 0 : (lq + kT - 1) / kT;
-  const int per = max(0, last - first), total = per * z.group;
+  const int per = max(0, last - first), all = (sk & 1023u) ? 0 : per * z.group;
+  const int total = (all - rank + ranks - 1) / ranks;        // this CTA's: numbers rank, rank + ranks, ...
+  auto query0 = [&](int it) { return (first + (rank + it * ranks) % per) * kT; };
 
   if (warp == 8) {
     if (tc_elect() && total > 0) {
       bool ok = true;
-      int qn = 0, dn = 0;
-      mbar_expect_tx(smem_u32(&kv_full), 2 * F::tile);
-      load_tile<NP>(sk, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&kv_full));
-      load_tile<NP>(sv, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&kv_full));
+      int qn = 0, dn = 0, ln = 0;
+      mbar_expect_tx(smem_u32(&bar.kv_full), 2 * F::tile);
+      load_tile<NP>(sk, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&bar.kv_full));
+      load_tile<NP>(sv, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&bar.kv_full));
       for (int it = 0; it < total; ++it) {
-        const int s = it % F::ring, h = hk * z.group + it / per, i0 = (first + it % per) * kT;
-        const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i0;
-        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&q_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&q_full[s]), F::tile + F::line);
-        load_tile<NP>(sq + s * F::tile, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full[s]));
-        load_line(smem_u32(sline + s * 2 * kT), line, smem_u32(&q_full[s]));
-        load_line(smem_u32(sline + s * 2 * kT + kT), line + padded, smem_u32(&q_full[s]));
+        const int h = hk * z.group + (rank + it * ranks) / per, i0 = query0(it);
+        const int qs = it % F::q_ring, os = it % F::do_ring, ls = it % F::line_ring;
+        if (it >= F::q_ring && !(ok = mbar_wait(smem_u32(&bar.q_empty[qs]), (it / F::q_ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&bar.q_full[qs]), F::tile);
+        load_tile<NP>(sq + qs * F::tile, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&bar.q_full[qs]));
         ++qn;
-        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&do_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&do_full[s]), F::tile);
-        load_tile<NP>(sdo + s * F::tile, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&do_full[s]));
+        if (it >= F::line_ring && !(ok = mbar_wait(smem_u32(&bar.line_empty[ls]), (it / F::line_ring - 1) & 1, deadline))) break;
+        const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i0;
+        mbar_expect_tx(smem_u32(&bar.line_full[ls]), F::line);
+        load_line(smem_u32(sline + ls * 2 * kT), line, smem_u32(&bar.line_full[ls]));
+        load_line(smem_u32(sline + ls * 2 * kT + kT), line + padded, smem_u32(&bar.line_full[ls]));
+        ++ln;
+        if (it >= F::do_ring && !(ok = mbar_wait(smem_u32(&bar.do_empty[os]), (it / F::do_ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&bar.do_full[os]), F::tile);
+        load_tile<NP>(sdo + os * F::tile, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&bar.do_full[os]));
         ++dn;
       }
       if (!ok) {
         atomicOr(z.status, CDG_ST_TIMEOUT);
-        mbar_wait(smem_u32(&kv_full), 0, clock64() + kCdgWaitCycles);
-        for (int i = max(0, qn - F::ring); i < qn; ++i) mbar_wait(smem_u32(&q_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, dn - F::ring); i < dn; ++i) mbar_wait(smem_u32(&do_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+        mbar_wait(smem_u32(&bar.kv_full), 0, clock64() + kCdgWaitCycles);
+        for (int i = max(0, qn - F::q_ring); i < qn; ++i) mbar_wait(smem_u32(&bar.q_full[i % F::q_ring]), (i / F::q_ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, ln - F::line_ring); i < ln; ++i) mbar_wait(smem_u32(&bar.line_full[i % F::line_ring]), (i / F::line_ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, dn - F::do_ring); i < dn; ++i) mbar_wait(smem_u32(&bar.do_full[i % F::do_ring]), (i / F::do_ring) & 1, clock64() + kCdgWaitCycles);
       }
     }
   } else if (warp == 9) {
-    // A tile's rows past the sequence's queries are zeroed before any product reads them
-    auto arrived = [&](uint64_t *bars, uint32_t tiles, int it) {
-      const int s = it % F::ring;
-      if (!tc_wait(&bars[s], (it / F::ring) & 1, deadline)) return false;
-      const int left = lq - (first + it % per) * kT;
+    // a tile's rows past the sequence's queries are zeroed before any product reads them
+    auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
+      const int s = it % ring;
+      if (!tc_wait(&full[s], (it / ring) & 1, deadline)) return false;
+      const int left = lq - query0(it);
       if (z.q_lens && left < kT) zero_rows<NP>(base + (tiles - sk) + s * F::tile, left);
       return true;
     };
     bool ok = true;
     if (total > 0) {
-      ok = tc_wait(&kv_full, 0, deadline) && arrived(q_full, sq, 0);
-      if (ok) { mma_scores<NP>(tm, sk, sq); tc_commit(&s_full); }
-      ok = ok && arrived(do_full, sdo, 0);
-      if (ok) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(&dp_full); }
+      ok = tc_wait(&bar.kv_full, 0, deadline) && arrived(bar.q_full, sq, F::q_ring, 0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm, sk, sq); tc_commit(&bar.s_full); }
+      __syncwarp();
+      ok = ok && arrived(bar.do_full, sdo, F::do_ring, 0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(&bar.dp_full); }
+      __syncwarp();
     }
     for (int it = 0; it < total && ok; ++it) {
-      const int s = it % F::ring, sn = (it + 1) % F::ring;
+      const uint32_t q_this = sq + it % F::q_ring * F::tile, q_next = sq + (it + 1) % F::q_ring * F::tile;
+      const uint32_t do_this = sdo + it % F::do_ring * F::tile, do_next = sdo + (it + 1) % F::do_ring * F::tile;
       const bool next = it + 1 < total;
-      if (!(ok = tc_wait(&p_ready, it & 1, deadline))) break;
-      tc_fence_after();
-              mma_rows<NP>(tm + F::dv, tm, 64, sdo + s * F::tile, it > 0);
-        tc_commit(&dv_done);
-        tc_commit(&do_empty[s]);
-      if (next) {              // S lies under P: its product has to be over
-        if (!(ok = arrived(q_full, sq, it + 1) && tc_wait(&dv_done, it & 1, deadline))) break;
+      if (NP == 1 && next) {             // S is in registers: the next one may overwrite it
+        if (!(ok = arrived(bar.q_full, sq, F::q_ring, it + 1) && tc_wait(&bar.s_free, it & 1, deadline))) break;
         tc_fence_after();
-        mma_scores<NP>(tm, sk, sq + sn * F::tile); tc_commit(&s_full); 
+        if (tc_elect()) {
+          mma_scores<NP>(tm, sk, q_next);
+          tc_commit(&bar.s_full);
+        }
+        __syncwarp();
       }
-      if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
+      if (!(ok = tc_wait(&bar.p_ready, it & 1, deadline))) break;
       tc_fence_after();
-              mma_rows<NP>(tm + F::dk, tm + kT, 64, sq + s * F::tile, it > 0);
-        tc_commit(&dk_done);
-        tc_commit(&q_empty[s]);
-      if (next) {
-        if (!(ok = arrived(do_full, sdo, it + 1) && tc_wait(&dk_done, it & 1, deadline))) break;
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dv, tm + F::p, F::half, do_this, it > 0);
+        tc_commit(&bar.dv_done);
+        tc_commit(&bar.do_empty[it % F::do_ring]);
+      }
+      __syncwarp();
+      if (NP == 2 && next) {             // P lies over S: its product has to be over
+        if (!(ok = arrived(bar.q_full, sq, F::q_ring, it + 1) && tc_wait(&bar.dv_done, it & 1, deadline))) break;
         tc_fence_after();
-        mma_scores<NP>(tm + kT, sv, sdo + sn * F::tile); tc_commit(&dp_full); 
+        if (tc_elect()) {
+          mma_scores<NP>(tm, sk, q_next);
+          tc_commit(&bar.s_full);
+        }
+        __syncwarp();
+      }
+      if (NP == 1 && next) {
+        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it + 1) && tc_wait(&bar.dp_free, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) {
+          mma_scores<NP>(tm + kT, sv, do_next);
+          tc_commit(&bar.dp_full);
+        }
+        __syncwarp();
+      }
+      if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
+      tc_fence_after();
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dk, tm + F::ds, F::half, q_this, it > 0);
+        tc_commit(&bar.dk_done);
+        tc_commit(&bar.q_empty[it % F::q_ring]);
+      }
+      __syncwarp();
+      if (NP == 2 && next) {             // likewise dS over dP
+        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it + 1) && tc_wait(&bar.dk_done, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) {
+          mma_scores<NP>(tm + kT, sv, do_next);
+          tc_commit(&bar.dp_full);
+        }
+        __syncwarp();
       }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
     const int half = warp >> 2, row = (warp & 3) * 32 + lane, j = j0 + row;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
+    const uint32_t tp = tm + lanes + F::p + half * F::half, tds = tm + lanes + F::ds + half * F::half;
     const float a = z.negative ? -z.a : z.a;
     const int off = lk - lq;
     bool ok = true;
     for (int it = 0; it < total; ++it) {
-      const int s = it % F::ring, i0 = (first + it % per) * kT + half * 64;
-      const float *l2 = sline + s * 2 * kT + half * 64, *delta = l2 + kT;
-      // the lines came with Q, whose stage is released when dS of this tile has been used
-      if (!(ok = tc_wait(&q_full[s], (it / F::ring) & 1, deadline) && tc_wait(&s_full, it & 1, deadline))) break;
+      const int ls = it % F::line_ring, i0 = query0(it) + half * 64;
+      const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
+      if (!(ok = tc_wait(&bar.line_full[ls], (it / F::line_ring) & 1, deadline) && tc_wait(&bar.s_full, it & 1, deadline))) break;
       tc_fence_after();
+      uint32_t v[2][32];
+      tc_load32(ts, v[0]);
+      tc_load32(ts + 32, v[1]);
+      tc_wait_ld();
+      if (NP == 1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar.s_free));
+      }
       float p[64];
+#pragma unroll
+      for (int e = 0; e < 64; e += 4) {
+        const float4 l = *reinterpret_cast<const float4 *>(l2 + e);
+        const float2 x = fma2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(a, a), make_float2(l.x, l.y));
+        const float2 y = fma2(make_float2(__uint_as_float(v[e >> 5][(e & 31) + 2]), __uint_as_float(v[e >> 5][(e & 31) + 3])), make_float2(a, a), make_float2(l.z, l.w));
+        p[e] = exp2_fast(x.x); p[e + 1] = exp2_fast(x.y); p[e + 2] = exp2_fast(y.x); p[e + 3] = exp2_fast(y.y);
+      }
       // under the causal rule key j is seen by queries from j - off on
       const int from = z.causal ? j - off - i0 : 0;
-      const bool some_hidden = __any_sync(0xffffffffu, from > 0);
+      if (__any_sync(0xffffffffu, from > 0)) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t v[32], w[16];
-        tc_load32(ts + c * 32, v);
-        tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          const float4 l = *reinterpret_cast<const float4 *>(l2 + c * 32 + e);
-          p[c * 32 + e] = exp2_fast(fmaf(__uint_as_float(v[e]), a, -l.x));
-          p[c * 32 + e + 1] = exp2_fast(fmaf(__uint_as_float(v[e + 1]), a, -l.y));
-          p[c * 32 + e + 2] = exp2_fast(fmaf(__uint_as_float(v[e + 2]), a, -l.z));
-          p[c * 32 + e + 3] = exp2_fast(fmaf(__uint_as_float(v[e + 3]), a, -l.w));
-        }
-        if (some_hidden) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (c * 32 + e < from) p[c * 32 + e] = 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pack(p[c * 32 + 2 * e], p[c * 32 + 2 * e + 1]);
-        tc_store16(ts + c * 16, w);
+        for (int e = 0; e < 64; ++e)
+          if (e < from) p[e] = 0.0f;
       }
+      if (NP == 1 && it > 0) {           // the place of P is free when its last product is over
+        if (!(ok = tc_wait(&bar.dv_done, (it - 1) & 1, deadline))) break;
+        tc_fence_after();
+      }
+      uint32_t w[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) w[e] = pack(p[2 * e], p[2 * e + 1]);
+      tc_store32(tp, w);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&p_ready));
-      if (!(ok = tc_wait(&dp_full, it & 1, deadline))) break;
+      if (lane == 0) mbar_arrive(smem_u32(&bar.p_ready));
+      if (!(ok = tc_wait(&bar.dp_full, it & 1, deadline))) break;
       tc_fence_after();
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t v[32], w[16];
-        tc_load32(tdp + c * 32, v);
-        tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          const float4 d = *reinterpret_cast<const float4 *>(delta + c * 32 + e);
-          w[e / 2] = pack(p[c * 32 + e] * (__uint_as_float(v[e]) - d.x), p[c * 32 + e + 1] * (__uint_as_float(v[e + 1]) - d.y));
-          w[e / 2 + 1] = pack(p[c * 32 + e + 2] * (__uint_as_float(v[e + 2]) - d.z), p[c * 32 + e + 3] * (__uint_as_float(v[e + 3]) - d.w));
-        }
-        tc_store16(tdp + c * 16, w);
+      tc_load32(tdp, v[0]);
+      tc_load32(tdp + 32, v[1]);
+      tc_wait_ld();
+      if (NP == 1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
+        if (it > 0 && !(ok = tc_wait(&bar.dk_done, (it - 1) & 1, deadline))) break;
+        tc_fence_after();
       }
+#pragma unroll
+      for (int e = 0; e < 64; e += 4) {
+        const float4 d = *reinterpret_cast<const float4 *>(delta + e);
+        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(d.x, d.y)));
+        const float2 y = mul2(make_float2(p[e + 2], p[e + 3]), add2(make_float2(__uint_as_float(v[e >> 5][(e & 31) + 2]), __uint_as_float(v[e >> 5][(e & 31) + 3])), make_float2(d.z, d.w)));
+        w[e / 2] = pack(x.x, x.y);
+        w[e / 2 + 1] = pack(y.x, y.y);
+      }
+      tc_store32(tds, w);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ds_ready));
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&bar.ds_ready));
+        mbar_arrive(smem_u32(&bar.line_empty[ls]));
+      }
     }
-    // warps 0-3 bring dv out, 4-7 dk, through the tiles of K and V, which no product reads any more
-    if (ok && total > 0) ok = tc_wait(&dv_done, (total - 1) & 1, deadline) && tc_wait(&dk_done, (total - 1) & 1, deadline);
+    // warps 0-3 bring dv out, 4-7 dk, through shared memory that no product reads any more
+    if (ok && total > 0) ok = tc_wait(&bar.dv_done, (total - 1) & 1, deadline) && tc_wait(&bar.dk_done, (total - 1) & 1, deadline);
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     tc_fence_after();
-    uint8_t *tile = base + half * F::tile;
     const uint32_t from = tm + lanes + (half ? F::dk : F::dv);
     const float f = half ? z.scale : 1.0f;
+    const View &out = half ? dk : dv;
+    bf16 *dst = out.p + (long long)b * out.b + (long long)hk * out.h;
+    uint8_t *tile = base + half * (ranks > 1 ? 2 : 1) * F::tile;
 #pragma unroll
     for (int c = 0; c < 2 * NP; ++c) {
-      uint32_t w[32], u[16];
+      uint32_t w[32] = {}, u[16];
       if (total > 0) {
         tc_load32(from + c * 32, w);
         tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = j < lk ? pack(__uint_as_float(w[2 * e]) * f, __uint_as_float(w[2 * e + 1]) * f) : 0u;
+      }
+      if (ranks > 1) {
+        keep_sums<NP>(tile, row, c * 32, w);
       } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = 0u;
+        for (int e = 0; e < 16; ++e) u[e] = j < lk ? pack(__uint_as_float(w[2 * e]) * f, __uint_as_float(w[2 * e + 1]) * f) : 0u;
+        stage_row<NP>(tile, row, c * 32, u);
       }
-      stage_row<NP>(tile, row, c * 32, u);
     }
     __syncwarp();
-    const View &out = half ? dk : dv;
-    write_rows<NP>(tile, (warp & 3) * 32, j0, z.tk, z, out.p + (long long)b * out.b + (long long)hk * out.h, out.t);
+    if (ranks == 1) write_rows<NP>(tile, (warp & 3) * 32, j0, z.tk, z, dst, out.t);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
+  if (ranks > 1) {
+    cluster_sync();
+    if (warp < 8) {
+      const int half = warp >> 2;
+      const View &out = half ? dk : dv;
+      join_sums<NP>(sk + half * 2 * F::tile, ranks, rank, threadIdx.x & 127, 128, j0, z.tk, lk, z, half ? z.scale : 1.0f,
+                    out.p + (long long)b * out.b + (long long)hk * out.h, out.t);
+    }
+    cluster_sync();            // no CTA leaves while another reads its sums
+  }
 }
 
 // dq of 128 queries of a head: dq += dS K over the key tiles it sees, S = Q K^T, dP = dO V^T.  A pass of its
 // own: adding dq's parts up from the kernel above would need additions to memory in no fixed order.
+// Tensor memory: S at 0, dP at 128, dq at 256, dS in turn at 384 and 448.
 template <int NP> struct Dq {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int ring = 2;
-  static constexpr size_t smem = 2 * tile + ring * 2 * tile + 1024;
-  static constexpr uint32_t dq = 256;
+  static constexpr int k_ring = NP == 1 ? 4 : 3, v_ring = NP == 1 ? 3 : 2;
+  static constexpr uint32_t bars = (2 + k_ring + v_ring) * tile;
+  static constexpr size_t smem = bars + 256;
+  static constexpr uint32_t dq = 256, ds = 384;
+};
+template <int NP> struct DqBars {
+  uint64_t q_full, k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring], v_empty[Dq<NP>::v_ring], s_full, s_free,
+      dp_full, dp_free, ds_ready, dq_done[2];
+  uint32_t tmem;
 };
 
 template <int NP>
@@ -636,97 +801,108 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
                 const float *__restrict__ lines, int padded, const View dq) {
   typedef Dq<NP> F;
-  extern __shared__ uint8_t raw[];
-  __shared__ __align__(8) uint64_t q_full, k_full[F::ring], k_empty[F::ring], v_full[F::ring], v_empty[F::ring], s_full, dp_full,
-      s_free, ds_ready, dq_done;
-  __shared__ uint32_t tmem_slot;
+  extern __shared__ __align__(1024) uint8_t base[];
+  static_assert(sizeof(DqBars<NP>) <= 256, "barriers behind the tiles");
+  DqBars<NP> &bar = *reinterpret_cast<DqBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-  const uint32_t sq = smem_u32(base), sdo = sq + F::tile, sk = sdo + F::tile, sv = sk + F::ring * F::tile;
-  const int h = blockIdx.x % z.heads, b = blockIdx.x / z.heads, hk = h / z.group;
+  const uint32_t sq = smem_u32(base), sdo = sq + F::tile, sk = sdo + F::tile, sv = sk + F::k_ring * F::tile;
+  const int ranks = (int)cluster_size(), rank = (int)cluster_rank();
+  const int column = blockIdx.x / ranks, h = column % z.heads, b = column / z.heads, hk = h / z.group;
   const int i0 = (z.causal ? (int)gridDim.y - 1 - (int)blockIdx.y : (int)blockIdx.y) * kT;
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&q_full), 1);
-    for (int i = 0; i < F::ring; ++i) {
-      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1);
-      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
-    }
-    mbar_init(smem_u32(&s_full), 1); mbar_init(smem_u32(&dp_full), 1);
-    mbar_init(smem_u32(&s_free), 8); mbar_init(smem_u32(&ds_ready), 8);
-    mbar_init(smem_u32(&dq_done), 1);
+    if (sq & 1023u) atomicOr(z.status, CDG_ST_TIMEOUT);
+    mbar_init(smem_u32(&bar.q_full), 1);
+    for (int i = 0; i < F::k_ring; ++i) { mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 1); }
+    for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
+    mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
+    mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
+    mbar_init(smem_u32(&bar.ds_ready), 8);
+    mbar_init(smem_u32(&bar.dq_done[0]), 1); mbar_init(smem_u32(&bar.dq_done[1]), 1);
     mbar_init_fence();
   }
-  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  if (warp == 9) tc_alloc(&bar.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tm = tmem_slot;
+  const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
 
   const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
   const int seen = i0 >= lq ? 0 : z.causal ? min(lk, min(i0 + kT, lq) + lk - lq) : lk;
-  const int total = seen > 0 ? (seen + kT - 1) / kT : 0;
+  const int all = seen > 0 && !(sq & 1023u) ? (seen + kT - 1) / kT : 0;
+  const int total = (all - rank + ranks - 1) / ranks;        // this CTA's key tiles: rank, rank + ranks, ...
 
   if (warp == 8) {
     if (tc_elect() && total > 0) {
       bool ok = true;
       int kn = 0, vn = 0;
-      mbar_expect_tx(smem_u32(&q_full), 2 * F::tile);
-      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full));
-      load_tile<NP>(sdo, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&q_full));
+      mbar_expect_tx(smem_u32(&bar.q_full), 2 * F::tile);
+      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&bar.q_full));
+      load_tile<NP>(sdo, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&bar.q_full));
       for (int it = 0; it < total; ++it) {
-        const int s = it % F::ring;
-        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&k_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&k_full[s]), F::tile);
-        load_tile<NP>(sk + s * F::tile, &mk, it * kT, hk, batch_of(z, kK, b), smem_u32(&k_full[s]));
+        const int ks = it % F::k_ring, vs = it % F::v_ring, j0 = (rank + it * ranks) * kT;
+        if (it >= F::k_ring && !(ok = mbar_wait(smem_u32(&bar.k_empty[ks]), (it / F::k_ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&bar.k_full[ks]), F::tile);
+        load_tile<NP>(sk + ks * F::tile, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&bar.k_full[ks]));
         ++kn;
-        if (it >= F::ring && !(ok = mbar_wait(smem_u32(&v_empty[s]), (it / F::ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&v_full[s]), F::tile);
-        load_tile<NP>(sv + s * F::tile, &mv, it * kT, hk, batch_of(z, kV, b), smem_u32(&v_full[s]));
+        if (it >= F::v_ring && !(ok = mbar_wait(smem_u32(&bar.v_empty[vs]), (it / F::v_ring - 1) & 1, deadline))) break;
+        mbar_expect_tx(smem_u32(&bar.v_full[vs]), F::tile);
+        load_tile<NP>(sv + vs * F::tile, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&bar.v_full[vs]));
         ++vn;
       }
       if (!ok) {
         atomicOr(z.status, CDG_ST_TIMEOUT);
-        mbar_wait(smem_u32(&q_full), 0, clock64() + kCdgWaitCycles);
-        for (int i = max(0, kn - F::ring); i < kn; ++i) mbar_wait(smem_u32(&k_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, vn - F::ring); i < vn; ++i) mbar_wait(smem_u32(&v_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
+        mbar_wait(smem_u32(&bar.q_full), 0, clock64() + kCdgWaitCycles);
+        for (int i = max(0, kn - F::k_ring); i < kn; ++i) mbar_wait(smem_u32(&bar.k_full[i % F::k_ring]), (i / F::k_ring) & 1, clock64() + kCdgWaitCycles);
+        for (int i = max(0, vn - F::v_ring); i < vn; ++i) mbar_wait(smem_u32(&bar.v_full[i % F::v_ring]), (i / F::v_ring) & 1, clock64() + kCdgWaitCycles);
       }
     }
   } else if (warp == 9) {
     auto arrived = [&](int it) {         // K of tile it, its rows past the sequence zeroed
-      const int s = it % F::ring;
-      if (!tc_wait(&k_full[s], (it / F::ring) & 1, deadline)) return false;
-      if (z.kv_lens && (it + 1) * kT > lk) zero_rows<NP>(base + (sk - sq) + s * F::tile, lk - it * kT);
+      const int s = it % F::k_ring, left = lk - (rank + it * ranks) * kT;
+      if (!tc_wait(&bar.k_full[s], (it / F::k_ring) & 1, deadline)) return false;
+      if (z.kv_lens && left < kT) zero_rows<NP>(base + (sk - sq) + s * F::tile, left);
       return true;
     };
     bool ok = true;
     if (total > 0) {
-      ok = tc_wait(&q_full, 0, deadline) && arrived(0);
-      if (ok) { mma_scores<NP>(tm, sq, sk); tc_commit(&s_full); }
-      ok = ok && tc_wait(&v_full[0], 0, deadline);
-      if (ok) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(&dp_full); tc_commit(&v_empty[0]); }
+      ok = tc_wait(&bar.q_full, 0, deadline) && arrived(0);
+      if (ok && tc_elect()) { mma_scores<NP>(tm, sq, sk); tc_commit(&bar.s_full); }
+      __syncwarp();
+      ok = ok && tc_wait(&bar.v_full[0], 0, deadline);
+      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(&bar.dp_full); tc_commit(&bar.v_empty[0]); }
+      __syncwarp();
     }
     for (int it = 0; it < total && ok; ++it) {
-      const int s = it % F::ring, sn = (it + 1) % F::ring;
-      const bool next = it + 1 < total;
-      if (next) {              // S is in registers: the next one may overwrite it
-        if (!(ok = arrived(it + 1) && tc_wait(&s_free, it & 1, deadline))) break;
+      const int ks = it % F::k_ring, kn = (it + 1) % F::k_ring, vn = (it + 1) % F::v_ring;
+      if (it + 1 < total) {    // S, then dP, are in registers: the next ones may overwrite them
+        if (!(ok = arrived(it + 1) && tc_wait(&bar.s_free, it & 1, deadline))) break;
         tc_fence_after();
-        mma_scores<NP>(tm, sq, sk + sn * F::tile); tc_commit(&s_full); 
+        if (tc_elect()) {
+          mma_scores<NP>(tm, sq, sk + kn * F::tile);
+          tc_commit(&bar.s_full);
+        }
+        __syncwarp();
+        if (!(ok = tc_wait(&bar.v_full[vn], ((it + 1) / F::v_ring) & 1, deadline) && tc_wait(&bar.dp_free, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) {
+          mma_scores<NP>(tm + kT, sdo, sv + vn * F::tile);
+          tc_commit(&bar.dp_full);
+          tc_commit(&bar.v_empty[vn]);
+        }
+        __syncwarp();
       }
-      if (!(ok = tc_wait(&ds_ready, it & 1, deadline))) break;
+      if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
       tc_fence_after();
-              mma_rows<NP>(tm + F::dq, tm + kT, 64, sk + s * F::tile, it > 0);
-        tc_commit(&dq_done);
-        tc_commit(&k_empty[s]);
-      if (next) {              // dP lies under dS: its product has to be over
-        if (!(ok = tc_wait(&v_full[sn], ((it + 1) / F::ring) & 1, deadline) && tc_wait(&dq_done, it & 1, deadline))) break;
-        tc_fence_after();
-        mma_scores<NP>(tm + kT, sdo, sv + sn * F::tile); tc_commit(&dp_full); tc_commit(&v_empty[sn]); 
+      if (tc_elect()) {
+        mma_rows<NP>(tm + F::dq, tm + F::ds + (it & 1) * 64, 32, sk + ks * F::tile, it > 0);
+        tc_commit(&bar.dq_done[it & 1]);
+        tc_commit(&bar.k_empty[ks]);
       }
+      __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
@@ -734,7 +910,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
     const float a = z.negative ? -z.a : z.a;
     const int keys = i >= lq ? 0 : z.causal ? min(lk, i + lk - lq + 1) : lk;
-    float l2 = INFINITY, delta = 0.0f;
+    float l2 = -INFINITY, delta = 0.0f;          // both negated
     if (i < padded) {
       const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i;
       l2 = line[0];
@@ -742,7 +918,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     }
     bool ok = true;
     for (int it = 0; it < total; ++it) {
-      if (!(ok = tc_wait(&s_full, it & 1, deadline))) break;
+      if (!(ok = tc_wait(&bar.s_full, it & 1, deadline))) break;
       tc_fence_after();
       uint32_t v[2][32];
       tc_load32(ts, v[0]);
@@ -750,63 +926,81 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       tc_wait_ld();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_free));
-      const int left = keys - it * kT - half * 64;
+      if (lane == 0) mbar_arrive(smem_u32(&bar.s_free));
+      const int left = keys - (rank + it * ranks) * kT - half * 64;
       float p[64];
 #pragma unroll
-      for (int e = 0; e < 64; ++e) p[e] = exp2_fast(fmaf(__uint_as_float(v[e >> 5][e & 31]), a, -l2));
-      const bool some_hidden = __any_sync(0xffffffffu, left < 64);
-      if (!(ok = tc_wait(&dp_full, it & 1, deadline))) break;
-      tc_fence_after();
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t u[32], w[16];
-        tc_load32(tdp + c * 32, u);
-        tc_wait_ld();
-        float ds[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) ds[e] = p[c * 32 + e] * (__uint_as_float(u[e]) - delta);
-        if (some_hidden) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (c * 32 + e >= left) ds[e] = 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pack(ds[2 * e], ds[2 * e + 1]);
-        tc_store16(tdp + c * 16, w);
+      for (int e = 0; e < 64; e += 2) {
+        const float2 x = fma2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(a, a), make_float2(l2, l2));
+        p[e] = exp2_fast(x.x);
+        p[e + 1] = exp2_fast(x.y);
       }
+      if (!(ok = tc_wait(&bar.dp_full, it & 1, deadline))) break;
+      tc_fence_after();
+      tc_load32(tdp, v[0]);
+      tc_load32(tdp + 32, v[1]);
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
+#pragma unroll
+      for (int e = 0; e < 64; e += 2) {
+        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(delta, delta)));
+        p[e] = x.x;
+        p[e + 1] = x.y;
+      }
+      if (__any_sync(0xffffffffu, left < 64)) {
+#pragma unroll
+        for (int e = 0; e < 64; ++e)
+          if (e >= left) p[e] = 0.0f;
+      }
+      if (it > 1) {              // the place of dS is free when its last product is over
+        if (!(ok = tc_wait(&bar.dq_done[it & 1], (it / 2 - 1) & 1, deadline))) break;
+        tc_fence_after();
+      }
+      uint32_t w[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) w[e] = pack(p[2 * e], p[2 * e + 1]);
+      tc_store32(tm + lanes + F::ds + (it & 1) * 64 + half * 32, w);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ds_ready));
+      if (lane == 0) mbar_arrive(smem_u32(&bar.ds_ready));
     }
-    if (ok && total > 0) ok = tc_wait(&dq_done, (total - 1) & 1, deadline);
+    if (ok && total > 0) ok = tc_wait(&bar.dq_done[(total - 1) & 1], ((total - 1) / 2) & 1, deadline);
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     tc_fence_after();
-    // the two groups of warps bring out half of the head dimensions each, through the tile of Q
+    // the two groups of warps bring out half of the head dimensions each, through the tiles of Q and dO
     const uint32_t from = tm + lanes + F::dq;
 #pragma unroll
     for (int c = 0; c < NP; ++c) {
       const int col = (half * NP + c) * 32;
-      uint32_t w[32], u[16];
+      uint32_t w[32] = {}, u[16];
       if (total > 0) {
         tc_load32(from + col, w);
         tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * z.scale, __uint_as_float(w[2 * e + 1]) * z.scale) : 0u;
+      }
+      if (ranks > 1) {
+        keep_sums<NP>(base, row, col, w);
       } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = 0u;
+        for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * z.scale, __uint_as_float(w[2 * e + 1]) * z.scale) : 0u;
+        stage_row<NP>(base, row, col, u);
       }
-      stage_row<NP>(base, row, col, u);
     }
     asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (half == 0)
+    if (ranks == 1 && half == 0)
       write_rows<NP>(base, (warp & 3) * 32, i0, z.tq, z, dq.p + (long long)b * dq.b + (long long)h * dq.h, dq.t);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
+  if (ranks > 1) {
+    cluster_sync();
+    if (warp < 8)
+      join_sums<NP>(sq, ranks, rank, threadIdx.x, 256, i0, z.tq, lq, z, z.scale, dq.p + (long long)b * dq.b + (long long)h * dq.h, dq.t);
+    cluster_sync();
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -841,8 +1035,8 @@ bool shape_ok(const cdgrab_attention_shape *s) {
       s->heads > 65535 || s->heads % s->kv_heads != 0)
     return false;
   if (s->head_dim < 8 || s->head_dim > 128 || s->head_dim % 8 != 0 || (s->causal != 0 && s->causal != 1)) return false;
-  // the grid's axes: batch x heads, and tiles of tokens
-  if ((long long)s->batch * s->heads > 0x7fffffffll || s->len_q > kMaxTokens || s->len_kv > kMaxTokens) return false;
+  // the grid's axes: batch x heads x CTAs of a cluster (up to 8), and tiles of tokens
+  if ((long long)s->batch * s->heads > 0x0fffffffll || s->len_q > kMaxTokens || s->len_kv > kMaxTokens) return false;
   return isfinite(s->scale);
 }
 
@@ -876,18 +1070,48 @@ int forward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtens
                                       Fwd<NP>::smem, st, mq, mk, mv, z, o, lse));
 }
 
+// CTAs that share the loop of one tile of rows.  `longest` and `mean` are the turns of the loop for the
+// longest tile and on average, `tiles` the number of tiles: a loop is dealt out while the longest one
+// takes more than half of what every SM gets (so that the last CTAs to finish leave few SMs idle) and at
+// least two turns are left to each CTA.
+int split_of(double longest, double mean, double tiles, int sms) {
+  int c = 1;
+  while (c < 8 && longest / c > 0.5 * mean * tiles / sms && longest / (2 * c) >= 2.0) c *= 2;
+  return c;
+}
+template <typename... KArgs, typename... Args>
+int launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cdg_launch_rc(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
+}
+
 template <int NP>
 int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mdo,
-             const Sizes &z, const float *lines, int padded, const View &dq, const View &dk, const View &dv, cudaStream_t st) {
+             const Sizes &z, const float *lines, int padded, const View &dq, const View &dk, const View &dv, int sms, cudaStream_t st) {
   static CdgPerDevice kf, qf;
   if (!raise_limit(kf, attn_backward_kv<NP>, Dkv<NP>::smem) || !raise_limit(qf, attn_backward_q<NP>, Dq<NP>::smem)) return CDGRAB_ERR_CUDA;
   int rc = CDGRAB_OK;
-  if (s->len_kv > 0)
-    rc = cdg_launch_rc(cdg_ops_launch(attn_backward_kv<NP>, dim3(s->kv_heads * s->batch, (s->len_kv + kT - 1) / kT), kBwdThreads,
-                                      Dkv<NP>::smem, st, mq, mk, mv, mdo, z, lines, padded, dk, dv));
-  if (rc == CDGRAB_OK && s->len_q > 0)
-    rc = cdg_launch_rc(cdg_ops_launch(attn_backward_q<NP>, dim3(s->heads * s->batch, (s->len_q + kT - 1) / kT), kBwdThreads,
-                                      Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines, padded, dq));
+  const int qt = (s->len_q + kT - 1) / kT, kt = (s->len_kv + kT - 1) / kT;
+  const double part = s->causal ? 0.5 : 1.0;
+  if (kt > 0) {
+    const int c = split_of((double)qt * z.group, part * qt * z.group, (double)kt * s->kv_heads * s->batch, sms);
+    rc = launch_cluster(attn_backward_kv<NP>, dim3(s->kv_heads * s->batch * c, kt), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z,
+                        lines, padded, dk, dv);
+  }
+  if (rc == CDGRAB_OK && qt > 0) {
+    const int c = split_of(kt, part * kt, (double)qt * s->heads * s->batch, sms);
+    rc = launch_cluster(attn_backward_q<NP>, dim3(s->heads * s->batch * c, qt), c, kBwdThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines,
+                        padded, dq);
+  }
   return rc;
 }
 
@@ -972,6 +1196,6 @@ extern "C" int cdgrab_attention_backward(const cdgrab_attention_shape *s, const 
       !map_of(&mdo, has_q ? d_o : k, s->do_stride, s->batch, tq, s->heads, s->head_dim))
     return CDGRAB_ERR_CUDA;
   const View vdq = view(dq, s->dq_stride), vdk = view(dk, s->dk_stride), vdv = view(dv, s->dv_stride);
-  return s->head_dim <= 64 ? backward<1>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, st)
-                           : backward<2>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, st);
+  return s->head_dim <= 64 ? backward<1>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, dev->sms, st)
+                           : backward<2>(s, mq, mk, mv, mdo, z, lines, (int)padded, vdq, vdk, vdv, dev->sms, st);
 }

@@ -167,14 +167,18 @@ __global__ void __launch_bounds__(128) orth_product(const __grid_constant__ CUte
       if (!(ok = tc_wait(&full[s], (it / kStages) & 1, deadline))) break;
       tc_fence_after();
       const uint32_t a = ring + s * kStageBytes, b = a + kOperandBytes;
+      const uint64_t da = tc_desc_k(a), db = symmetric ? tc_desc_k(b) : tc_desc_mn(b, kOperandBytes / 2);
+      if (tc_elect()) {
 #pragma unroll
-      for (int kk = 0; kk < kK / 16; ++kk)
-        tc_mma(acc, tc_desc_k(a + kk * 32), symmetric ? tc_desc_k(b + kk * 32) : tc_desc_mn(b + kk * 2048, kOperandBytes / 2),
-               idesc, it > 0 || kk > 0);
-      tc_commit(&empty[s]);
+        for (int kk = 0; kk < kK / 16; ++kk)
+          tc_mma(acc, da + kk * 2, db + kk * (symmetric ? 2 : 128), idesc, it > 0 || kk > 0);
+        tc_commit(&empty[s]);
+      }
+      __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
-    tc_commit(&done);
+    if (tc_elect()) tc_commit(&done);
+    __syncwarp();
   }
   __syncwarp();
 

@@ -35,30 +35,23 @@ __device__ __forceinline__ bool tc_elect() {
   return pred != 0;
 }
 
-// The matrix instructions are called by a whole converged warp, of which one lane issues each: operands
-// computed under a lane test would have to be moved into uniform registers one by one, which holds the
-// thread about 80 cycles per instruction, more than a product of 128 x 128 x 16 takes.
-
-// D (tensor memory) = A B (+ D), A and B in shared memory
+// D (tensor memory) = A B (+ D), A and B in shared memory; issued by one thread
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  if (tc_elect())
-    asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
 // ... with A in tensor memory: lane = row, two 16-bit values of K to a 32-bit column
 __device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-  if (tc_elect())
-    asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// the barrier completes when the matrix instructions issued so far by this warp's lane have
+// the barrier completes when the matrix instructions issued so far by this thread have
 __device__ __forceinline__ void tc_commit(uint64_t *bar) {
-  if (tc_elect())
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // bounded wait of a whole warp; false in all its lanes when it expired in one
 __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity, long long deadline) {

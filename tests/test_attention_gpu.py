@@ -96,6 +96,23 @@ def test_lengths_in_use(d, causal):
         assert (out[3][b, c:] == 0).all() and (out[4][b, c:] == 0).all()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("tq,tk,h,hk,d", [(2500, 2500, 1, 1, 64), (2300, 2300, 4, 1, 128), (64, 4100, 2, 1, 128), (4100, 100, 1, 1, 64),
+                                          (1, 3000, 2, 2, 64)])
+def test_long_and_few(tq, tk, h, hk, d, causal):
+    """Few tiles of rows and a long other axis: the loop is dealt out over several blocks and joined."""
+    check(*draw(1, tq, tk, h, hk, d), causal=causal)
+
+
+def test_long_and_few_padded():
+    q, k, v, do = draw(2, 1500, 1700, 2, 1, 64)
+    ql, kl = [1500, 130], [700, 1653]
+    for b in range(2):
+        q[b, ql[b]:], do[b, ql[b]:], k[b, kl[b]:], v[b, kl[b]:] = math.nan, math.nan, math.inf, math.nan
+    check(q, k, v, do, causal=True, q_lens=ql, kv_lens=kl)
+    check(q, k, v, do, q_lens=ql, kv_lens=kl)
+
+
 def test_only_some_lengths_given():
     q, k, v, do = draw(2, 100, 260, 2, 2, 64)
     check(q, k, v, do, kv_lens=[70, 260])
