@@ -60,6 +60,34 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
+// 2^x for two values on the FMA units: x = n + f, |f| <= 1/2, a polynomial of degree 5 for 2^f (a weighted
+// least-squares fit of its relative error, 1.6e-7 at most), and n added to the exponent.  Below -126 the
+// result is about 1e-38 instead of 0.
+__device__ __forceinline__ float2 exp2_pair(float2 x) {
+  const float2 magic = make_float2(12582912.0f, 12582912.0f);      // 1.5 x 2^23: the sum's last bits are n
+  x.x = fmaxf(x.x, -126.0f);
+  x.y = fmaxf(x.y, -126.0f);
+  const float2 t = add2(x, magic);
+  const float2 f = fma2(add2(t, make_float2(-12582912.0f, -12582912.0f)), make_float2(-1.0f, -1.0f), x);
+  float2 r = make_float2(0.0013276375830173492f, 0.0013276375830173492f);
+  r = fma2(r, f, make_float2(0.009675533510744572f, 0.009675533510744572f));
+  r = fma2(r, f, make_float2(0.05550713464617729f, 0.05550713464617729f));
+  r = fma2(r, f, make_float2(0.24022120237350464f, 0.24022120237350464f));
+  r = fma2(r, f, make_float2(0.6931469440460205f, 0.6931469440460205f));
+  r = fma2(r, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
+  r.x = __uint_as_float(__float_as_uint(r.x) + (__float_as_uint(t.x) << 23));
+  r.y = __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(t.y) << 23));
+  return r;
+}
+// The exponentials are spread over both kinds of units: the special function units do 16 a cycle and SM,
+// which bounds a tile of 128 x 128 at 1024 cycles; every fourth pair goes to the FMA units instead.
+template <bool FMA> __device__ __forceinline__ float2 exp2_two(float2 x) {
+  if (FMA) return exp2_pair(x);
+  return make_float2(exp2_fast(x.x), exp2_fast(x.y));
+}
+__device__ __forceinline__ float2 two(const uint32_t (&v)[2][32], int e) {
+  return make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1]));
+}
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&h);
@@ -128,7 +156,9 @@ __device__ __forceinline__ void write_rows(const uint8_t *tile, int row0, int to
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per 256 queries of a head: two tiles of 128 that share every key and value tile, so that while
 // one tile's four warps are at their exponentials the other's products run.
-//   warps 0-3, 4-7   softmax of query tile 0, 1        warp 8  bulk copies        warp 9  products
+//   warps 0-3, 4-7   softmax of query tile 0, 1     warp 8  bulk copies     warps 9, 10  products of tile 0, 1
+// (one warp for the products of both spent half its time in waits while the tensor cores ran dry: a warp can
+// queue little ahead of them)
 // Tensor memory: scores S_t at 128 t; head dimensions up to 64: O_t at 256 + 64 t and P_t apart at
 // 384 + 64 t, so that S of the next key tile is computed while P of this one is formed; above 64: O_t at
 // 256 + 128 t and P_t over S_t.
@@ -161,8 +191,8 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&q_full), 1);
     for (int i = 0; i < F::ring; ++i) {
-      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 1);
-      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 1);
+      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 2);
+      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 2);
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&s_free[t]), 4);
@@ -223,58 +253,45 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         for (int i = max(0, vn - F::ring); i < vn; ++i) mbar_wait(smem_u32(&v_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
       }
     }
-  } else if (warp == 9) {
-    bool ok = tiles == 0 || tc_wait(&q_full, 0, deadline);
-    if (ok && tiles > 0) ok = tc_wait(&k_full[0], 0, deadline);
-    tc_fence_after();
-    if (ok && tiles > 0) {
-      for (int t = 0; t < 2; ++t)
-        if (n[t] > 0 && tc_elect()) { mma_scores<NP>(tm + t * kT, sq + t * F::tile, sk); tc_commit(&s_full[t]); }
+  } else if (warp < 11) {
+    const int t = warp - 9, mine = t == 0 ? n[0] : n[1];
+    const uint32_t q_tile = sq + t * F::tile, s_at = tm + t * kT;
+    // S_t of key tile j; the stage of K is released when both tiles have used it (or have no use for it)
+    auto scores = [&](int j, uint64_t *before, uint32_t parity) {
+      const int ks = j % F::ring;
+      if (!tc_wait(&k_full[ks], (j / F::ring) & 1, deadline)) return false;
+      if (j < mine && before && !tc_wait(before, parity, deadline)) return false;
+      tc_fence_after();
       if (tc_elect()) {
-        tc_commit(&k_empty[0]);
+        if (j < mine) {
+          mma_scores<NP>(s_at, q_tile, sk + ks * F::tile);
+          tc_commit(&s_full[t]);
+        }
+        tc_commit(&k_empty[ks]);
       }
       __syncwarp();
-    }
+      return true;
+    };
+    bool ok = tiles == 0 || (tc_wait(&q_full, 0, deadline) && scores(0, nullptr, 0));
     for (int j = 0; j < tiles && ok; ++j) {
-      const int vs = j % F::ring, ks = (j + 1) % F::ring;
-      const uint32_t k_next = sk + ks * F::tile, v_this = sv + vs * F::tile;
+      const int vs = j % F::ring;
+      // up to 64 head dimensions: S_t(j) is in registers, the next one may overwrite it
+      if (NP == 1 && j + 1 < tiles && !(ok = scores(j + 1, &s_free[t], j & 1))) break;
       if (!(ok = tc_wait(&v_full[vs], (j / F::ring) & 1, deadline))) break;
+      // (both warps zero the rows past the sequence, each before its own product)
       if (z.kv_lens && (j + 1) * kT > lk) zero_rows<NP>(base + 2 * F::tile + F::ring * F::tile + vs * F::tile, lk - j * kT);
-      if (j + 1 < tiles && !(ok = tc_wait(&k_full[ks], ((j + 1) / F::ring) & 1, deadline))) break;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (NP == 1 && j + 1 < n[t]) {               // S_t(j) is in registers: the next one may overwrite it
-          if (!(ok = tc_wait(&s_free[t], j & 1, deadline))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]);
-          }
-          __syncwarp();
+      if (j < mine && !(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
+      tc_fence_after();
+      if (tc_elect()) {
+        if (j < mine) {
+          mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, sv + vs * F::tile, j > 0);
+          tc_commit(&pv_done[t]);
         }
-        if (j < n[t]) {
-          if (!(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
-          tc_fence_after();
-                      if (tc_elect()) {
-                        mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, v_this, j > 0);
-                        tc_commit(&pv_done[t]);
-                      }
-                      __syncwarp();
-        }
-        if (NP == 2 && j + 1 < n[t]) {               // P_t lies over S_t: its product has to be over
-          if (!(ok = tc_wait(&pv_done[t], j & 1, deadline))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_scores<NP>(tm + t * kT, sq + t * F::tile, k_next); tc_commit(&s_full[t]);
-          }
-          __syncwarp();
-        }
+        tc_commit(&v_empty[vs]);
       }
-      if (!ok) break;
-              if (tc_elect()) {
-                tc_commit(&v_empty[vs]);
-                if (j + 1 < tiles) tc_commit(&k_empty[ks]);
-              }
-              __syncwarp();
+      __syncwarp();
+      // above: P_t lies over S_t, its product has to be over
+      if (NP == 2 && j + 1 < tiles && !(ok = scores(j + 1, &pv_done[t], j & 1))) break;
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
@@ -337,20 +354,21 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
           tc_store32(to + c * 32, w);
         }
       }
-      float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
       for (int c = 0; c < 4; c += 2) {
         uint32_t w[32];
 #pragma unroll
         for (int e = 0; e < 64; e += 2) {
-          const float p0 = exp2_fast(fmaf(__uint_as_float(v[c + (e >> 5)][e & 31]), a, shift));
-          const float p1 = exp2_fast(fmaf(__uint_as_float(v[c + (e >> 5)][(e & 31) + 1]), a, shift));
-          part[(e >> 1) & 3] += p0 + p1;
-          w[e >> 1] = pack(p0, p1);
+          const float2 x = fma2(make_float2(__uint_as_float(v[c + (e >> 5)][e & 31]), __uint_as_float(v[c + (e >> 5)][(e & 31) + 1])),
+                                make_float2(a, a), make_float2(shift, shift));
+          const float2 p = (e & 6) == 0 ? exp2_two<true>(x) : exp2_two<false>(x);
+          part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
+          w[e >> 1] = pack(p.x, p.y);
         }
         tc_store32(tp + c * 16, w);
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -435,11 +453,13 @@ __device__ __forceinline__ void load_line(uint32_t dst, const float *src, uint32
 
 // Both backward kernels: eight warps work on a tile of scores, four on its columns 0..63 and four on
 // 64..127, one row per thread.
-//   warps 0-7  P and dS        warp 8  bulk copies        warp 9  products
+//   warps 0-7  P and dS     warp 8  bulk copies     warp 9  S and dP     warp 10  the products with P and dS
+// (two warps issue products because one can queue little ahead of the tensor cores and spends some 200 cycles
+// between two products in its waits)
 // The rings are as deep as shared memory allows: a tile of Q (or K) is used twice, at the beginning and at
 // the end of its turn, and a copy takes about 1700 cycles; with two stages each the products waited for it
 // (3500 cycles a tile at 128 head dimensions).
-constexpr int kBwdThreads = 320;
+constexpr int kBwdThreads = 352;
 
 // Where there are few tiles of rows, the loop over the other axis is dealt out over a cluster of CTAs, whose
 // fp32 sums are joined through distributed shared memory, in the order of their ranks.
@@ -490,19 +510,21 @@ __device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, in
 // Scores are transposed (a row is a key), so that P^T and dS^T are the row operands of
 //   dv += P^T dO,  dk += dS^T Q,    with  S^T = K Q^T,  dP^T = V dO^T.
 // Summing over query tiles and heads in a fixed order makes the result the same bits every time.
-// Tensor memory: S at 0, dP at 128, dv and dk from 256; up to 64 head dimensions P and dS lie apart behind
-// them, above they lie over S and dP, each half of the warps over its own columns.
+// Tensor memory: dv and dk from 256; the scores move between two regions of 128 columns.  In turn `it`
+// region it & 1 holds S, then, over each half's own scores, P and dS; the other one holds dP.  Once dP is in
+// registers, S of the next turn is computed in its place while dS is being formed; dP of the next turn
+// follows when both products of this one are over.
 template <int NP> struct Dkv {
   static constexpr uint32_t tile = kT * 128 * NP;
   static constexpr int q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 4 : 2, line_ring = 2;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
   static constexpr uint32_t lines = (2 + q_ring + do_ring) * tile, bars = lines + line_ring * line;
   static constexpr size_t smem = bars + 256;
-  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP, p = NP == 1 ? 384 : 0, ds = NP == 1 ? 448 : 128, half = NP == 1 ? 32 : 64;
+  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
 };
 template <int NP> struct DkvBars {
   uint64_t kv_full, q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring], do_empty[Dkv<NP>::do_ring],
-      line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, s_free, dp_full, dp_free, p_ready, ds_ready, dv_done, dk_done;
+      line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, dp_full, dp_free, p_ready, ds_ready, done;
   uint32_t tmem;
 };
 
@@ -526,12 +548,11 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     if (sk & 1023u) atomicOr(z.status, CDG_ST_TIMEOUT);      // (the copies' swizzle counts on it)
     mbar_init(smem_u32(&bar.kv_full), 1);
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
-    for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 1); }
+    for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 2); }
     for (int i = 0; i < F::line_ring; ++i) { mbar_init(smem_u32(&bar.line_full[i]), 1); mbar_init(smem_u32(&bar.line_empty[i]), 8); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
-    mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
+    mbar_init(smem_u32(&bar.dp_free), 8); mbar_init(smem_u32(&bar.done), 1);
     mbar_init(smem_u32(&bar.p_ready), 8); mbar_init(smem_u32(&bar.ds_ready), 8);
-    mbar_init(smem_u32(&bar.dv_done), 1); mbar_init(smem_u32(&bar.dk_done), 1);
     mbar_init_fence();
   }
   if (warp == 9) tc_alloc(&bar.tmem, 512);
@@ -584,8 +605,8 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (int i = max(0, dn - F::do_ring); i < dn; ++i) mbar_wait(smem_u32(&bar.do_full[i % F::do_ring]), (i / F::do_ring) & 1, clock64() + kCdgWaitCycles);
       }
     }
-  } else if (warp == 9) {
-    // a tile's rows past the sequence's queries are zeroed before any product reads them
+  } else if (warp >= 9) {
+    // (by either warp, each before its own product) a tile's rows past the sequence's queries are zeroed before any product reads them
     auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
       const int s = it % ring;
       if (!tc_wait(&full[s], (it / ring) & 1, deadline)) return false;
@@ -594,67 +615,46 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       return true;
     };
     bool ok = true;
-    if (total > 0) {
-      ok = tc_wait(&bar.kv_full, 0, deadline) && arrived(bar.q_full, sq, F::q_ring, 0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm, sk, sq); tc_commit(&bar.s_full); }
-      __syncwarp();
-      ok = ok && arrived(bar.do_full, sdo, F::do_ring, 0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sv, sdo); tc_commit(&bar.dp_full); }
-      __syncwarp();
-    }
-    for (int it = 0; it < total && ok; ++it) {
-      const uint32_t q_this = sq + it % F::q_ring * F::tile, q_next = sq + (it + 1) % F::q_ring * F::tile;
-      const uint32_t do_this = sdo + it % F::do_ring * F::tile, do_next = sdo + (it + 1) % F::do_ring * F::tile;
-      const bool next = it + 1 < total;
-      if (NP == 1 && next) {             // S is in registers: the next one may overwrite it
-        if (!(ok = arrived(bar.q_full, sq, F::q_ring, it + 1) && tc_wait(&bar.s_free, it & 1, deadline))) break;
+    if (warp == 9) {
+      auto scores = [&](int it) {
+        if (!arrived(bar.q_full, sq, F::q_ring, it) || (it > 0 && !tc_wait(&bar.dp_free, (it - 1) & 1, deadline))) return false;
         tc_fence_after();
         if (tc_elect()) {
-          mma_scores<NP>(tm, sk, q_next);
+          mma_scores<NP>(tm + (it & 1) * kT, sk, sq + it % F::q_ring * F::tile);
           tc_commit(&bar.s_full);
         }
         __syncwarp();
-      }
-      if (!(ok = tc_wait(&bar.p_ready, it & 1, deadline))) break;
-      tc_fence_after();
-      if (tc_elect()) {
-        mma_rows<NP>(tm + F::dv, tm + F::p, F::half, do_this, it > 0);
-        tc_commit(&bar.dv_done);
-        tc_commit(&bar.do_empty[it % F::do_ring]);
-      }
-      __syncwarp();
-      if (NP == 2 && next) {             // P lies over S: its product has to be over
-        if (!(ok = arrived(bar.q_full, sq, F::q_ring, it + 1) && tc_wait(&bar.dv_done, it & 1, deadline))) break;
+        return true;
+      };
+      auto gradients = [&](int it) {
+        if (!arrived(bar.do_full, sdo, F::do_ring, it) || (it > 0 && !tc_wait(&bar.done, (it - 1) & 1, deadline))) return false;
         tc_fence_after();
         if (tc_elect()) {
-          mma_scores<NP>(tm, sk, q_next);
-          tc_commit(&bar.s_full);
+          mma_scores<NP>(tm + (~it & 1) * kT, sv, sdo + it % F::do_ring * F::tile);
+          tc_commit(&bar.dp_full);
+          tc_commit(&bar.do_empty[it % F::do_ring]);
         }
         __syncwarp();
-      }
-      if (NP == 1 && next) {
-        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it + 1) && tc_wait(&bar.dp_free, it & 1, deadline))) break;
+        return true;
+      };
+      if (total > 0) ok = tc_wait(&bar.kv_full, 0, deadline);
+      for (int it = 0; it < total && ok; ++it) ok = scores(it) && gradients(it);
+    } else {
+      for (int it = 0; it < total && ok; ++it) {
+        const uint32_t here = tm + (it & 1) * kT;
+        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it) && tc_wait(&bar.p_ready, it & 1, deadline))) break;
         tc_fence_after();
         if (tc_elect()) {
-          mma_scores<NP>(tm + kT, sv, do_next);
-          tc_commit(&bar.dp_full);
+          mma_rows<NP>(tm + F::dv, here, 64, sdo + it % F::do_ring * F::tile, it > 0);
+          tc_commit(&bar.do_empty[it % F::do_ring]);
         }
         __syncwarp();
-      }
-      if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
-      tc_fence_after();
-      if (tc_elect()) {
-        mma_rows<NP>(tm + F::dk, tm + F::ds, F::half, q_this, it > 0);
-        tc_commit(&bar.dk_done);
-        tc_commit(&bar.q_empty[it % F::q_ring]);
-      }
-      __syncwarp();
-      if (NP == 2 && next) {             // likewise dS over dP
-        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it + 1) && tc_wait(&bar.dk_done, it & 1, deadline))) break;
+        if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
         tc_fence_after();
         if (tc_elect()) {
-          mma_scores<NP>(tm + kT, sv, do_next);
-          tc_commit(&bar.dp_full);
+          mma_rows<NP>(tm + F::dk, here + 32, 64, sq + it % F::q_ring * F::tile, it > 0);
+          tc_commit(&bar.done);
+          tc_commit(&bar.q_empty[it % F::q_ring]);
         }
         __syncwarp();
       }
@@ -662,32 +662,31 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
     const int half = warp >> 2, row = (warp & 3) * 32 + lane, j = j0 + row;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
-    const uint32_t tp = tm + lanes + F::p + half * F::half, tds = tm + lanes + F::ds + half * F::half;
+    const uint32_t mine = tm + ((uint32_t)((warp & 3) * 32) << 16) + half * 64;
     const float a = z.negative ? -z.a : z.a;
     const int off = lk - lq;
     bool ok = true;
     for (int it = 0; it < total; ++it) {
       const int ls = it % F::line_ring, i0 = query0(it) + half * 64;
+      const uint32_t here = mine + (it & 1) * kT, there = mine + (~it & 1) * kT;
       const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
       if (!(ok = tc_wait(&bar.line_full[ls], (it / F::line_ring) & 1, deadline) && tc_wait(&bar.s_full, it & 1, deadline))) break;
       tc_fence_after();
-      uint32_t v[2][32];
-      tc_load32(ts, v[0]);
-      tc_load32(ts + 32, v[1]);
+      uint32_t v[2][32], w[32];
+      tc_load32(here, v[0]);
+      tc_load32(here + 32, v[1]);
       tc_wait_ld();
-      if (NP == 1) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar.s_free));
-      }
       float p[64];
 #pragma unroll
-      for (int e = 0; e < 64; e += 4) {
-        const float4 l = *reinterpret_cast<const float4 *>(l2 + e);
-        const float2 x = fma2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(a, a), make_float2(l.x, l.y));
-        const float2 y = fma2(make_float2(__uint_as_float(v[e >> 5][(e & 31) + 2]), __uint_as_float(v[e >> 5][(e & 31) + 3])), make_float2(a, a), make_float2(l.z, l.w));
-        p[e] = exp2_fast(x.x); p[e + 1] = exp2_fast(x.y); p[e + 2] = exp2_fast(y.x); p[e + 3] = exp2_fast(y.y);
+      for (int e = 0; e < 64; e += 8) {
+        const float4 l = *reinterpret_cast<const float4 *>(l2 + e), m = *reinterpret_cast<const float4 *>(l2 + e + 4);
+        const float2 aa = make_float2(a, a);
+        const float2 x0 = exp2_two<true>(fma2(two(v, e), aa, make_float2(l.x, l.y)));
+        const float2 x1 = exp2_two<false>(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
+        const float2 x2 = exp2_two<false>(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
+        const float2 x3 = exp2_two<false>(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
+        p[e] = x0.x; p[e + 1] = x0.y; p[e + 2] = x1.x; p[e + 3] = x1.y;
+        p[e + 4] = x2.x; p[e + 5] = x2.y; p[e + 6] = x3.x; p[e + 7] = x3.y;
       }
       // under the causal rule key j is seen by queries from j - off on
       const int from = z.causal ? j - off - i0 : 0;
@@ -696,39 +695,30 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (int e = 0; e < 64; ++e)
           if (e < from) p[e] = 0.0f;
       }
-      if (NP == 1 && it > 0) {           // the place of P is free when its last product is over
-        if (!(ok = tc_wait(&bar.dv_done, (it - 1) & 1, deadline))) break;
-        tc_fence_after();
-      }
-      uint32_t w[32];
 #pragma unroll
       for (int e = 0; e < 32; ++e) w[e] = pack(p[2 * e], p[2 * e + 1]);
-      tc_store32(tp, w);
+      tc_store32(here, w);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bar.p_ready));
       if (!(ok = tc_wait(&bar.dp_full, it & 1, deadline))) break;
       tc_fence_after();
-      tc_load32(tdp, v[0]);
-      tc_load32(tdp + 32, v[1]);
+      tc_load32(there, v[0]);
+      tc_load32(there + 32, v[1]);
       tc_wait_ld();
-      if (NP == 1) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
-        if (it > 0 && !(ok = tc_wait(&bar.dk_done, (it - 1) & 1, deadline))) break;
-        tc_fence_after();
-      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
 #pragma unroll
       for (int e = 0; e < 64; e += 4) {
         const float4 d = *reinterpret_cast<const float4 *>(delta + e);
-        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(d.x, d.y)));
-        const float2 y = mul2(make_float2(p[e + 2], p[e + 3]), add2(make_float2(__uint_as_float(v[e >> 5][(e & 31) + 2]), __uint_as_float(v[e >> 5][(e & 31) + 3])), make_float2(d.z, d.w)));
+        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(two(v, e), make_float2(d.x, d.y)));
+        const float2 y = mul2(make_float2(p[e + 2], p[e + 3]), add2(two(v, e + 2), make_float2(d.z, d.w)));
         w[e / 2] = pack(x.x, x.y);
         w[e / 2 + 1] = pack(y.x, y.y);
       }
-      tc_store32(tds, w);
+      tc_store32(here + 32, w);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -738,10 +728,10 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       }
     }
     // warps 0-3 bring dv out, 4-7 dk, through shared memory that no product reads any more
-    if (ok && total > 0) ok = tc_wait(&bar.dv_done, (total - 1) & 1, deadline) && tc_wait(&bar.dk_done, (total - 1) & 1, deadline);
+    if (ok && total > 0) ok = tc_wait(&bar.done, (total - 1) & 1, deadline);
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     tc_fence_after();
-    const uint32_t from = tm + lanes + (half ? F::dk : F::dv);
+    const uint32_t from = tm + ((uint32_t)((warp & 3) * 32) << 16) + (half ? F::dk : F::dv);
     const float f = half ? z.scale : 1.0f;
     const View &out = half ? dk : dv;
     bf16 *dst = out.p + (long long)b * out.b + (long long)hk * out.h;
@@ -782,9 +772,12 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 // dq of 128 queries of a head: dq += dS K over the key tiles it sees, S = Q K^T, dP = dO V^T.  A pass of its
 // own: adding dq's parts up from the kernel above would need additions to memory in no fixed order.
 // Tensor memory: S at 0, dP at 128, dq at 256, dS in turn at 384 and 448.
+// The exponentials of one key tile are formed together with dS of the one before, so that the special
+// function units work while the FMA units do.
+constexpr int kDqThreads = 384;        // three warpgroups: 168 registers a thread at launch, 64,512 in all
 template <int NP> struct Dq {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int k_ring = NP == 1 ? 4 : 3, v_ring = NP == 1 ? 3 : 2;
+  static constexpr int k_ring = NP == 1 ? 6 : 3, v_ring = NP == 1 ? 4 : 2;
   static constexpr uint32_t bars = (2 + k_ring + v_ring) * tile;
   static constexpr size_t smem = bars + 256;
   static constexpr uint32_t dq = 256, ds = 384;
@@ -796,7 +789,7 @@ template <int NP> struct DqBars {
 };
 
 template <int NP>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(kDqThreads, 1)
 attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
                 const float *__restrict__ lines, int padded, const View dq) {
@@ -835,6 +828,8 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   const int all = seen > 0 && !(sq & 1023u) ? (seen + kT - 1) / kT : 0;
   const int total = (all - rank + ranks - 1) / ranks;        // this CTA's key tiles: rank, rank + ranks, ...
 
+  if (warp >= 8) {
+  tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
   if (warp == 8) {
     if (tc_elect() && total > 0) {
       bool ok = true;
@@ -860,52 +855,56 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (int i = max(0, vn - F::v_ring); i < vn; ++i) mbar_wait(smem_u32(&bar.v_full[i % F::v_ring]), (i / F::v_ring) & 1, clock64() + kCdgWaitCycles);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == 9 || warp == 10) {
     auto arrived = [&](int it) {         // K of tile it, its rows past the sequence zeroed
       const int s = it % F::k_ring, left = lk - (rank + it * ranks) * kT;
       if (!tc_wait(&bar.k_full[s], (it / F::k_ring) & 1, deadline)) return false;
       if (z.kv_lens && left < kT) zero_rows<NP>(base + (sk - sq) + s * F::tile, left);
       return true;
     };
-    bool ok = true;
-    if (total > 0) {
-      ok = tc_wait(&bar.q_full, 0, deadline) && arrived(0);
-      if (ok && tc_elect()) { mma_scores<NP>(tm, sq, sk); tc_commit(&bar.s_full); }
-      __syncwarp();
-      ok = ok && tc_wait(&bar.v_full[0], 0, deadline);
-      if (ok && tc_elect()) { mma_scores<NP>(tm + kT, sdo, sv); tc_commit(&bar.dp_full); tc_commit(&bar.v_empty[0]); }
-      __syncwarp();
-    }
-    for (int it = 0; it < total && ok; ++it) {
-      const int ks = it % F::k_ring, kn = (it + 1) % F::k_ring, vn = (it + 1) % F::v_ring;
-      if (it + 1 < total) {    // S, then dP, are in registers: the next ones may overwrite them
-        if (!(ok = arrived(it + 1) && tc_wait(&bar.s_free, it & 1, deadline))) break;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_scores<NP>(tm, sq, sk + kn * F::tile);
-          tc_commit(&bar.s_full);
-        }
-        __syncwarp();
-        if (!(ok = tc_wait(&bar.v_full[vn], ((it + 1) / F::v_ring) & 1, deadline) && tc_wait(&bar.dp_free, it & 1, deadline))) break;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_scores<NP>(tm + kT, sdo, sv + vn * F::tile);
-          tc_commit(&bar.dp_full);
-          tc_commit(&bar.v_empty[vn]);
-        }
-        __syncwarp();
-      }
-      if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
+    auto scores = [&](int it) {          // S of tile it, when the one before is in registers
+      if (!arrived(it) || (it > 0 && !tc_wait(&bar.s_free, (it - 1) & 1, deadline))) return false;
       tc_fence_after();
       if (tc_elect()) {
-        mma_rows<NP>(tm + F::dq, tm + F::ds + (it & 1) * 64, 32, sk + ks * F::tile, it > 0);
-        tc_commit(&bar.dq_done[it & 1]);
-        tc_commit(&bar.k_empty[ks]);
+        mma_scores<NP>(tm, sq, sk + it % F::k_ring * F::tile);
+        tc_commit(&bar.s_full);
       }
       __syncwarp();
+      return true;
+    };
+    auto gradients = [&](int it) {       // dP likewise
+      const int s = it % F::v_ring;
+      if (!tc_wait(&bar.v_full[s], (it / F::v_ring) & 1, deadline) || (it > 0 && !tc_wait(&bar.dp_free, (it - 1) & 1, deadline))) return false;
+      tc_fence_after();
+      if (tc_elect()) {
+        mma_scores<NP>(tm + kT, sdo, sv + s * F::tile);
+        tc_commit(&bar.dp_full);
+        tc_commit(&bar.v_empty[s]);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = true;
+    if (warp == 9) {
+      ok = total == 0 || (tc_wait(&bar.q_full, 0, deadline) && scores(0));
+      for (int it = 0; it < total && ok; ++it) ok = gradients(it) && (it + 1 == total || scores(it + 1));
+    } else {
+      for (int it = 0; it < total && ok; ++it) {
+        const int ks = it % F::k_ring;
+        if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
+        tc_fence_after();
+        if (tc_elect()) {
+          mma_rows<NP>(tm + F::dq, tm + F::ds + (it & 1) * 64, 32, sk + ks * F::tile, it > 0);
+          tc_commit(&bar.dq_done[it & 1]);
+          tc_commit(&bar.k_empty[ks]);
+        }
+        __syncwarp();
+      }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+  }
   } else {
+    tc_regs_up<224>();
     const int half = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + row;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
     const float a = z.negative ? -z.a : z.a;
@@ -916,9 +915,10 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       l2 = line[0];
       delta = line[padded];
     }
+    const float2 aa = make_float2(a, a), ll = make_float2(l2, l2), dd = make_float2(delta, delta);
     bool ok = true;
-    for (int it = 0; it < total; ++it) {
-      if (!(ok = tc_wait(&bar.s_full, it & 1, deadline))) break;
+    float p[64];
+    if (total > 0 && (ok = tc_wait(&bar.s_full, 0, deadline))) {
       tc_fence_after();
       uint32_t v[2][32];
       tc_load32(ts, v[0]);
@@ -927,40 +927,49 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bar.s_free));
-      const int left = keys - (rank + it * ranks) * kT - half * 64;
-      float p[64];
 #pragma unroll
       for (int e = 0; e < 64; e += 2) {
-        const float2 x = fma2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(a, a), make_float2(l2, l2));
-        p[e] = exp2_fast(x.x);
-        p[e + 1] = exp2_fast(x.y);
-      }
-      if (!(ok = tc_wait(&bar.dp_full, it & 1, deadline))) break;
-      tc_fence_after();
-      tc_load32(tdp, v[0]);
-      tc_load32(tdp + 32, v[1]);
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) {
-        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])), make_float2(delta, delta)));
+        const float2 x = exp2_two<false>(fma2(two(v, e), aa, ll));
         p[e] = x.x;
         p[e + 1] = x.y;
       }
-      if (__any_sync(0xffffffffu, left < 64)) {
+    }
+    for (int it = 0; it < total && ok; ++it) {
+      const bool next = it + 1 < total;
+      if (!(ok = (!next || tc_wait(&bar.s_full, (it + 1) & 1, deadline)) && tc_wait(&bar.dp_full, it & 1, deadline))) break;
+      tc_fence_after();
+      uint32_t v[2][32] = {}, u[2][32], w[32];
+      tc_load32(tdp, u[0]);
+      tc_load32(tdp + 32, u[1]);
+      if (next) {
+        tc_load32(ts, v[0]);
+        tc_load32(ts + 32, v[1]);
+      }
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&bar.dp_free));
+        if (next) mbar_arrive(smem_u32(&bar.s_free));
+      }
+      const int left = keys - (rank + it * ranks) * kT - half * 64;
+      if (__any_sync(0xffffffffu, left < 64)) {       // replaces P and dP: whatever lies there is not used
 #pragma unroll
         for (int e = 0; e < 64; ++e)
-          if (e >= left) p[e] = 0.0f;
+          if (e >= left) { p[e] = 0.0f; u[e >> 5][e & 31] = 0u; }
+      }
+#pragma unroll
+      for (int e = 0; e < 64; e += 2) {
+        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(two(u, e), dd));
+        w[e / 2] = pack(x.x, x.y);
+        const float2 y = fma2(two(v, e), aa, ll), t = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
+        p[e] = t.x;
+        p[e + 1] = t.y;
       }
       if (it > 1) {              // the place of dS is free when its last product is over
         if (!(ok = tc_wait(&bar.dq_done[it & 1], (it / 2 - 1) & 1, deadline))) break;
         tc_fence_after();
       }
-      uint32_t w[32];
-#pragma unroll
-      for (int e = 0; e < 32; ++e) w[e] = pack(p[2 * e], p[2 * e + 1]);
       tc_store32(tm + lanes + F::ds + (it & 1) * 64 + half * 32, w);
       tc_wait_st();
       tc_fence_before();
@@ -1109,7 +1118,7 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
   }
   if (rc == CDGRAB_OK && qt > 0) {
     const int c = split_of(kt, part * kt, (double)qt * s->heads * s->batch, sms);
-    rc = launch_cluster(attn_backward_q<NP>, dim3(s->heads * s->batch * c, qt), c, kBwdThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines,
+    rc = launch_cluster(attn_backward_q<NP>, dim3(s->heads * s->batch * c, qt), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines,
                         padded, dq);
   }
   return rc;
