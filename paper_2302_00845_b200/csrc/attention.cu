@@ -142,15 +142,90 @@ __device__ __forceinline__ void stage_row(uint8_t *tile, int row, int c0, const 
         make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
 }
+// `rows` staged rows from row0 on (a whole warp)
 template <int NP>
-__device__ __forceinline__ void write_rows(const uint8_t *tile, int row0, int token0, int tokens, const Sizes &z, bf16 *dst, long long stride) {
+__device__ __forceinline__ void write_rows(const uint8_t *tile, int row0, int rows, int token0, int tokens, const Sizes &z, bf16 *dst, long long stride) {
   const int lane = threadIdx.x & 31, per = NP * 8;
-  for (int i = lane; i < 32 * per; i += 32) {
+  for (int i = lane; i < rows * per; i += 32) {
     const int r = row0 + i / per, chunk = i % per;
     if (token0 + r < tokens && chunk * 8 < z.dim)
       *reinterpret_cast<uint4 *>(dst + (long long)(token0 + r) * stride + chunk * 8) =
           *reinterpret_cast<const uint4 *>(tile + (chunk >> 3) * kT * 128 + r * 128 + (((chunk & 7) ^ (r & 7)) << 4));
   }
+}
+// ... and rows of zeros
+template <int NP>
+__device__ __forceinline__ void write_zeros(int row0, int rows, int token0, int tokens, const Sizes &z, bf16 *dst, long long stride) {
+  const int lane = threadIdx.x & 31, per = NP * 8;
+  for (int i = lane; i < rows * per; i += 32) {
+    const int r = row0 + i / per, chunk = i % per;
+    if (token0 + r < tokens && chunk * 8 < z.dim)
+      *reinterpret_cast<uint4 *>(dst + (long long)(token0 + r) * stride + chunk * 8) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// All three kernels are persistent: a CTA that has finished a block of rows takes over the next CTA of the
+// grid that has not been started (cluster launch control), so that setting up a CTA (barriers, tensor
+// memory, tensor maps: about 2500 cycles), the first copies of the next block and the last stores of this one
+// overlap, and the hardware still deals the blocks out as SMs become free, longest loops first.  One block
+// to a CTA spent half of its 18,600 cycles outside the loop at 1024 tokens and 64 dimensions.
+// Counters of turns and stages therefore run on over the blocks, and so do the barriers' phases: turn n of a
+// ring of R uses stage n % R in the phase of parity(n, R).
+struct Queue { uint4 answer[2]; uint64_t full[2], empty[2]; };       // in shared memory: the next block, one ahead
+constexpr int kQueueReaders = 11;                                    // warps that follow the blocks
+__device__ __forceinline__ void queue_init(Queue &q) {
+  for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&q.full[i]), 1); mbar_init(smem_u32(&q.empty[i]), kQueueReaders); }
+}
+struct Block { int at, h, b; };         // first row, head, sequence
+__device__ __forceinline__ Block block_of(long long w, int heads, int columns, int blocks, int rows, bool last_first) {
+  const int c = (int)(w % columns), k = (int)(w / columns);
+  return Block{(last_first ? blocks - 1 - k : k) * rows, c % heads, c / heads};
+}
+__device__ __forceinline__ uint32_t parity(int n, int ring) { return (uint32_t)(n / ring) & 1u; }
+// waits for the stage of turn n to have been released by turn n - ring (one thread)
+__device__ __forceinline__ bool wait_released(uint64_t *empty, int n, int ring, long long deadline) {
+  return n < ring || mbar_wait(smem_u32(&empty[n % ring]), parity(n - ring, ring), deadline);
+}
+// after a failure: the copies in flight have to land before the CTA gives up its shared memory
+__device__ __forceinline__ void drain(uint64_t *full, int n, int ring) {
+  for (int i = max(0, n - ring); i < n; ++i) mbar_wait(smem_u32(&full[i % ring]), parity(i, ring), clock64() + kCdgWaitCycles);
+}
+// asks for block number `seq` of this CTA (one thread)
+__device__ __forceinline__ bool queue_ask(Queue &q, int seq, long long deadline) {
+  const int s = seq & 1;
+  if (!wait_released(q.empty, seq, 2, deadline)) return false;
+  mbar_expect_tx(smem_u32(&q.full[s]), 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(smem_u32(&q.answer[s])), "r"(smem_u32(&q.full[s])) : "memory");
+  return true;
+}
+// ... and reads the answer: the block, or -1 when none is left
+__device__ __forceinline__ long long queue_answer(Queue &q, int seq) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n.reg .b128 h;\n.reg .pred p;\nld.shared.b128 h, [%2];\n"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, h;\n}"
+      : "=r"(got), "=r"(x) : "r"(smem_u32(&q.answer[seq & 1])) : "memory");
+  tc_proxy_fence();              // the next answer may be written once this one has been read
+  return got ? (long long)x : -1;
+}
+__device__ __forceinline__ long long queue_next(Queue &q, int seq, long long deadline, bool &ok) {        // a whole warp
+  if (!(ok = ok && tc_wait(&q.full[seq & 1], parity(seq, 2), deadline))) return -1;
+  const long long at = queue_answer(q, seq);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&q.empty[seq & 1]));
+  return at;
+}
+__device__ __forceinline__ long long queue_next_one(Queue &q, int seq, long long deadline, bool &ok) {    // one thread
+  if (!(ok = ok && mbar_wait(smem_u32(&q.full[seq & 1]), parity(seq, 2), deadline))) return -1;
+  const long long at = queue_answer(q, seq);
+  mbar_arrive(smem_u32(&q.empty[seq & 1]));
+  return at;
+}
+__device__ __forceinline__ void warp_arrive(uint64_t *bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(bar));
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -167,239 +242,293 @@ __device__ __forceinline__ void write_rows(const uint8_t *tile, int row0, int to
 constexpr int kFwdThreads = 384;       // three warpgroups: 168 registers a thread at launch, 64,512 in all
 template <int NP> struct Fwd {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int ring = NP == 1 ? 3 : 2;              // stages of K and of V
-  static constexpr size_t smem = 2 * tile + 2 * ring * tile + 1024;
+  static constexpr int q_ring = NP == 1 ? 2 : 1, ring = NP == 1 ? 3 : 2;              // pairs of Q tiles; stages of K and of V
+  static constexpr uint32_t k = 2 * q_ring * tile, v = k + ring * tile, bars = v + ring * tile;
+  static constexpr size_t smem = bars + 320;
   static constexpr uint32_t o = 256, p = NP == 1 ? 384 : 0, o_step = NP == 1 ? 64 : 128, p_step = NP == 1 ? 64 : 128;
+};
+template <int NP> struct FwdBars {
+  Queue queue;
+  uint64_t q_full[Fwd<NP>::q_ring], q_empty[Fwd<NP>::q_ring], k_full[Fwd<NP>::ring], k_empty[Fwd<NP>::ring], v_full[Fwd<NP>::ring],
+      v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2];
+  uint32_t tmem;
 };
 
 template <int NP>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-             const __grid_constant__ CUtensorMap mv, const Sizes z, const View o, float *__restrict__ lse) {
+             const __grid_constant__ CUtensorMap mv, const Sizes z, int blocks, const View o, float *__restrict__ lse) {
   typedef Fwd<NP> F;
-  extern __shared__ uint8_t raw[];
-  __shared__ __align__(8) uint64_t q_full, k_full[F::ring], k_empty[F::ring], v_full[F::ring], v_empty[F::ring], s_full[2],
-      s_free[2], p_ready[2], pv_done[2];
-  __shared__ uint32_t tmem_slot;
+  extern __shared__ __align__(1024) uint8_t base[];         // all of the CTA's shared memory: starts on a 1024-byte boundary
+  static_assert(sizeof(FwdBars<NP>) <= 320, "barriers behind the tiles");
+  FwdBars<NP> &bar = *reinterpret_cast<FwdBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint8_t *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-  const uint32_t sq = smem_u32(base), sk = sq + 2 * F::tile, sv = sk + F::ring * F::tile;
-  const int h = blockIdx.x % z.heads, b = blockIdx.x / z.heads, hk = h / z.group;
-  // the longest query blocks of a causal batch start first
-  const int i0 = (z.causal ? (int)gridDim.y - 1 - (int)blockIdx.y : (int)blockIdx.y) * 2 * kT;
+  const uint32_t sq = smem_u32(base), sk = sq + F::k, sv = sq + F::v;
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&q_full), 1);
+    queue_init(bar.queue);
+    for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 8); }
     for (int i = 0; i < F::ring; ++i) {
-      mbar_init(smem_u32(&k_full[i]), 1); mbar_init(smem_u32(&k_empty[i]), 2);
-      mbar_init(smem_u32(&v_full[i]), 1); mbar_init(smem_u32(&v_empty[i]), 2);
+      mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 2);
+      mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 2);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&s_free[t]), 4);
-      mbar_init(smem_u32(&p_ready[t]), 4); mbar_init(smem_u32(&pv_done[t]), 1);
+      mbar_init(smem_u32(&bar.s_full[t]), 1); mbar_init(smem_u32(&bar.s_free[t]), 4);
+      mbar_init(smem_u32(&bar.p_ready[t]), 4); mbar_init(smem_u32(&bar.pv_done[t]), 1);
+      mbar_init(smem_u32(&bar.o_free[t]), 4);
     }
     mbar_init_fence();
   }
-  if (warp == 9) tc_alloc(&tmem_slot, 512);
+  if (warp == 9) tc_alloc(&bar.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tm = tmem_slot;
+  const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
+  const int columns = z.heads * z.batch;
 
-  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
-  int n[2];                      // key tiles that query tile t sees
+  // the sequence's lengths and the key tiles that each query tile of a block sees
+  struct Work { int lq, lk, n[2], tiles; };
+  auto work_of = [&](const Block &w) {
+    Work k;
+    k.lq = used(z.q_lens, w.b, z.tq);
+    k.lk = used(z.kv_lens, w.b, z.tk);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int first = i0 + t * kT, last = min(first + kT, lq) - 1;
-    const int keys = first >= lq ? 0 : z.causal ? min(lk, last + lk - lq + 1) : lk;
-    n[t] = keys > 0 ? (keys + kT - 1) / kT : 0;
-  }
-  const int tiles = max(n[0], n[1]);
+    for (int t = 0; t < 2; ++t) {
+      const int first = w.at + t * kT, last = min(first + kT, k.lq) - 1;
+      const int keys = first >= k.lq ? 0 : z.causal ? min(k.lk, last + k.lk - k.lq + 1) : k.lk;
+      k.n[t] = keys > 0 ? (keys + kT - 1) / kT : 0;
+    }
+    k.tiles = max(k.n[0], k.n[1]);
+    return k;
+  };
+  auto block = [&](long long at) { return block_of(at, z.heads, columns, blocks, 2 * kT, z.causal); };
 
   if (warp >= 8) {
-  tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
-  if (warp == 8) {
-    if (tc_elect() && tiles > 0) {
+    tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+    if (warp == 8) {
+      if (tc_elect()) {
+        bool ok = true;
+        int qn = 0, kn = 0, vn = 0;        // blocks and tiles issued
+        int seq = 0;
+        for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next_one(bar.queue, seq++, deadline, ok)) {
+          if (!(ok = queue_ask(bar.queue, seq, deadline))) break;
+          const Block w = block(at);
+          const Work k = work_of(w);
+          if (k.tiles == 0) continue;
+          const int hk = w.h / z.group;
+          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          uint64_t *full = &bar.q_full[qn % F::q_ring];
+          const uint32_t q = sq + qn % F::q_ring * 2 * F::tile;
+          mbar_expect_tx(smem_u32(full), 2 * F::tile);
+          load_tile<NP>(q, &mq, w.at, w.h, batch_of(z, kQ, w.b), smem_u32(full));
+          load_tile<NP>(q + F::tile, &mq, w.at + kT, w.h, batch_of(z, kQ, w.b), smem_u32(full));
+          ++qn;
+          for (int j = 0; j <= k.tiles; ++j) {         // K runs one tile ahead of V
+            if (j < k.tiles) {
+              if (!(ok = wait_released(bar.k_empty, kn, F::ring, deadline))) break;
+              full = &bar.k_full[kn % F::ring];
+              mbar_expect_tx(smem_u32(full), F::tile);
+              load_tile<NP>(sk + kn % F::ring * F::tile, &mk, j * kT, hk, batch_of(z, kK, w.b), smem_u32(full));
+              ++kn;
+            }
+            if (j > 0) {
+              if (!(ok = wait_released(bar.v_empty, vn, F::ring, deadline))) break;
+              full = &bar.v_full[vn % F::ring];
+              mbar_expect_tx(smem_u32(full), F::tile);
+              load_tile<NP>(sv + vn % F::ring * F::tile, &mv, (j - 1) * kT, hk, batch_of(z, kV, w.b), smem_u32(full));
+              ++vn;
+            }
+          }
+        }
+        if (!ok) {
+          atomicOr(z.status, CDG_ST_TIMEOUT);
+          drain(bar.queue.full, seq + 1, 2);
+          drain(bar.q_full, qn, F::q_ring);
+          drain(bar.k_full, kn, F::ring);
+          drain(bar.v_full, vn, F::ring);
+        }
+      }
+    } else if (warp < 11) {
+      const int t = warp - 9;
+      const uint32_t s_at = tm + t * kT;
       bool ok = true;
-      int kn = 0, vn = 0;        // tiles issued
-      mbar_expect_tx(smem_u32(&q_full), 2 * F::tile);
-      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&q_full));
-      load_tile<NP>(sq + F::tile, &mq, i0 + kT, h, batch_of(z, kQ, b), smem_u32(&q_full));
-      for (int j = 0; j <= tiles && ok; ++j) {         // K runs one tile ahead of V
-        if (j < tiles) {
-          const int s = j % F::ring;
-          if (j >= F::ring) ok = mbar_wait(smem_u32(&k_empty[s]), (j / F::ring - 1) & 1, deadline);
-          if (!ok) break;
-          mbar_expect_tx(smem_u32(&k_full[s]), F::tile);
-          load_tile<NP>(sk + s * F::tile, &mk, j * kT, hk, batch_of(z, kK, b), smem_u32(&k_full[s]));
+      int qn = 0, kn = 0, vn = 0, sn = 0, pn = 0, on = 0;      // blocks, tiles of K and V, products S_t and P_t V, blocks with any
+      int seq = 0;
+      for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next(bar.queue, seq++, deadline, ok)) {
+        const Block w = block(at);
+        const Work k = work_of(w);
+        if (k.tiles == 0) continue;
+        const int mine = t == 0 ? k.n[0] : k.n[1];
+        const uint32_t q_tile = sq + (qn % F::q_ring * 2 + t) * F::tile;
+        // S_t of key tile j; the stage of K is released when both tiles have used it (or have no use for it)
+        auto scores = [&](int j) {
+          const int ks = kn % F::ring;
+          if (!tc_wait(&bar.k_full[ks], parity(kn, F::ring), deadline)) return false;
           ++kn;
-        }
-        if (j > 0) {
-          const int i = j - 1, s = i % F::ring;
-          if (i >= F::ring) ok = mbar_wait(smem_u32(&v_empty[s]), (i / F::ring - 1) & 1, deadline);
-          if (!ok) break;
-          mbar_expect_tx(smem_u32(&v_full[s]), F::tile);
-          load_tile<NP>(sv + s * F::tile, &mv, i * kT, hk, batch_of(z, kV, b), smem_u32(&v_full[s]));
+          // up to 64 head dimensions: the one before is in registers; above, P_t lies over it, and its product is over
+          if (j < mine && sn > 0 && !tc_wait(NP == 1 ? &bar.s_free[t] : &bar.pv_done[t], (sn - 1) & 1, deadline)) return false;
+          tc_fence_after();
+          if (tc_elect()) {
+            if (j < mine) {
+              mma_scores<NP>(s_at, q_tile, sk + ks * F::tile);
+              tc_commit(&bar.s_full[t]);
+            }
+            tc_commit(&bar.k_empty[ks]);
+          }
+          __syncwarp();
+          sn += j < mine;
+          return true;
+        };
+        if (!(ok = tc_wait(&bar.q_full[qn % F::q_ring], parity(qn, F::q_ring), deadline) && scores(0))) break;
+        for (int j = 0; j < k.tiles; ++j) {
+          const int vs = vn % F::ring;
+          if (NP == 1 && j + 1 < k.tiles && !(ok = scores(j + 1))) break;
+          if (!(ok = tc_wait(&bar.v_full[vs], parity(vn, F::ring), deadline))) break;
           ++vn;
+          // (both warps zero the rows past the sequence, each before its own product)
+          if (z.kv_lens && (j + 1) * kT > k.lk) zero_rows<NP>(base + F::v + vs * F::tile, k.lk - j * kT);
+          if (j < mine) {
+            if (j == 0 && on > 0 && !(ok = tc_wait(&bar.o_free[t], (on - 1) & 1, deadline))) break;
+            if (!(ok = tc_wait(&bar.p_ready[t], pn & 1, deadline))) break;
+            ++pn;
+          }
+          tc_fence_after();
+          if (tc_elect()) {
+            if (j < mine) {
+              mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, sv + vs * F::tile, j > 0);
+              tc_commit(&bar.pv_done[t]);
+            }
+            tc_commit(&bar.v_empty[vs]);
+          }
+          __syncwarp();
+          if (NP == 2 && j + 1 < k.tiles && !(ok = scores(j + 1))) break;
         }
+        ++qn;
+        on += mine > 0;
       }
-      if (!ok) {                 // let the copies in flight land before the CTA gives up its shared memory
-        atomicOr(z.status, CDG_ST_TIMEOUT);
-        mbar_wait(smem_u32(&q_full), 0, clock64() + kCdgWaitCycles);
-        for (int i = max(0, kn - F::ring); i < kn; ++i) mbar_wait(smem_u32(&k_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, vn - F::ring); i < vn; ++i) mbar_wait(smem_u32(&v_full[i % F::ring]), (i / F::ring) & 1, clock64() + kCdgWaitCycles);
-      }
+      if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     }
-  } else if (warp < 11) {
-    const int t = warp - 9, mine = t == 0 ? n[0] : n[1];
-    const uint32_t q_tile = sq + t * F::tile, s_at = tm + t * kT;
-    // S_t of key tile j; the stage of K is released when both tiles have used it (or have no use for it)
-    auto scores = [&](int j, uint64_t *before, uint32_t parity) {
-      const int ks = j % F::ring;
-      if (!tc_wait(&k_full[ks], (j / F::ring) & 1, deadline)) return false;
-      if (j < mine && before && !tc_wait(before, parity, deadline)) return false;
-      tc_fence_after();
-      if (tc_elect()) {
-        if (j < mine) {
-          mma_scores<NP>(s_at, q_tile, sk + ks * F::tile);
-          tc_commit(&s_full[t]);
-        }
-        tc_commit(&k_empty[ks]);
-      }
-      __syncwarp();
-      return true;
-    };
-    bool ok = tiles == 0 || (tc_wait(&q_full, 0, deadline) && scores(0, nullptr, 0));
-    for (int j = 0; j < tiles && ok; ++j) {
-      const int vs = j % F::ring;
-      // up to 64 head dimensions: S_t(j) is in registers, the next one may overwrite it
-      if (NP == 1 && j + 1 < tiles && !(ok = scores(j + 1, &s_free[t], j & 1))) break;
-      if (!(ok = tc_wait(&v_full[vs], (j / F::ring) & 1, deadline))) break;
-      // (both warps zero the rows past the sequence, each before its own product)
-      if (z.kv_lens && (j + 1) * kT > lk) zero_rows<NP>(base + 2 * F::tile + F::ring * F::tile + vs * F::tile, lk - j * kT);
-      if (j < mine && !(ok = tc_wait(&p_ready[t], j & 1, deadline))) break;
-      tc_fence_after();
-      if (tc_elect()) {
-        if (j < mine) {
-          mma_rows<NP>(tm + F::o + t * F::o_step, tm + F::p + t * F::p_step, 32, sv + vs * F::tile, j > 0);
-          tc_commit(&pv_done[t]);
-        }
-        tc_commit(&v_empty[vs]);
-      }
-      __syncwarp();
-      // above: P_t lies over S_t, its product has to be over
-      if (NP == 2 && j + 1 < tiles && !(ok = scores(j + 1, &pv_done[t], j & 1))) break;
-    }
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
-  }
   } else {
     tc_regs_up<224>();
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + t * kT + row;
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tm + lanes + t * kT, tp = tm + lanes + F::p + t * F::p_step, to = tm + lanes + F::o + t * F::o_step;
-    const int keys = i >= lq ? 0 : z.causal ? min(lk, i + lk - lq + 1) : lk;     // this row sees keys 0 .. keys - 1
     const float a = z.a;
-    float ref = -INFINITY, sum = 0.0f;
     bool ok = true;
-    for (int j = 0; j < n[t]; ++j) {
-      if (!(ok = tc_wait(&s_full[t], j & 1, deadline))) break;
-      tc_fence_after();
-      uint32_t v[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tc_load32(ts + c * 32, v[c]);
-      tc_wait_ld();
-      if (NP == 1) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_free[t]));
-      }
-      if (z.negative) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[c][e] ^= 0x80000000u;
-      }
-      const int left = keys - j * kT;
-      if (__any_sync(0xffffffffu, left < kT)) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (c * 32 + e >= left) v[c][e] = 0xff800000u;
-      }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int e = 0; e < 32; ++e)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(v[c][e]));
-      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      // raise the reference where the maximum has outgrown it by 2^8, or where there was none
-      const bool raise = mx > ref && (ref == -INFINITY || (mx - ref) * a > 8.0f);
-      const float factor = raise ? exp2_fast((ref - mx) * a) : 1.0f;
-      if (raise) { ref = mx; sum *= factor; }
-      const float shift = ref == -INFINITY ? 0.0f : -ref * a;
-      if (j > 0 && !(ok = tc_wait(&pv_done[t], (j - 1) & 1, deadline))) break;
-      if (j > 0 && __any_sync(0xffffffffu, raise)) {
+    int qn = 0, sn = 0;                  // blocks, and score tiles of this half
+    int seq = 0;
+    for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next(bar.queue, seq++, deadline, ok)) {
+      const Block w = block(at);
+      const Work k = work_of(w);
+      const int mine = t == 0 ? k.n[0] : k.n[1], i = w.at + t * kT + row;
+      const int keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;     // this row sees keys 0 .. keys - 1
+      float ref = -INFINITY, sum = 0.0f;
+      for (int j = 0; j < mine; ++j, ++sn) {
+        if (!(ok = tc_wait(&bar.s_full[t], sn & 1, deadline))) break;
         tc_fence_after();
+        uint32_t v[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc_load32(ts + c * 32, v[c]);
+        tc_wait_ld();
+        if (NP == 1) {
+          tc_fence_before();
+          warp_arrive(&bar.s_free[t]);
+        }
+        if (z.negative) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[c][e] ^= 0x80000000u;
+        }
+        const int left = keys - j * kT;
+        if (__any_sync(0xffffffffu, left < kT)) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (c * 32 + e >= left) v[c][e] = 0xff800000u;
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(v[c][e]));
+        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        // raise the reference where the maximum has outgrown it by 2^8, or where there was none
+        const bool raise = mx > ref && (ref == -INFINITY || (mx - ref) * a > 8.0f);
+        const float factor = raise ? exp2_fast((ref - mx) * a) : 1.0f;
+        if (raise) { ref = mx; sum *= factor; }
+        const float shift = ref == -INFINITY ? 0.0f : -ref * a;
+        if (j > 0 && !(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
+        if (j > 0 && __any_sync(0xffffffffu, raise)) {
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < 2 * NP; ++c) {
+            uint32_t u[32];
+            tc_load32(to + c * 32, u);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * factor);
+            tc_store32(to + c * 32, u);
+          }
+        }
+        float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+          uint32_t u[32];
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const float2 x = fma2(make_float2(__uint_as_float(v[c + (e >> 5)][e & 31]), __uint_as_float(v[c + (e >> 5)][(e & 31) + 1])),
+                                  make_float2(a, a), make_float2(shift, shift));
+            const float2 p = (e & 6) == 0 ? exp2_two<true>(x) : exp2_two<false>(x);
+            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
+            u[e >> 1] = pack(p.x, p.y);
+          }
+          tc_store32(tp + c * 16, u);
+        }
+        sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+        tc_wait_st();
+        tc_fence_before();
+        warp_arrive(&bar.p_ready[t]);
+      }
+      if (!ok) break;
+      bf16 *dst = o.p + (long long)w.b * o.b + (long long)w.h * o.h;
+      if (mine > 0) {
+        if (!(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
+        tc_fence_after();
+        // the tile of Q is no longer read: it takes O on its way out
+        uint8_t *tile = base + (qn % F::q_ring * 2 + t) * F::tile;
+        const float inv = keys > 0 && sum > 0.0f ? 1.0f / sum : 0.0f;
+        uint32_t u[2 * NP][16];
 #pragma unroll
         for (int c = 0; c < 2 * NP; ++c) {
-          uint32_t w[32];
-          tc_load32(to + c * 32, w);
+          uint32_t v[32];
+          tc_load32(to + c * 32, v);
           tc_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * factor);
-          tc_store32(to + c * 32, w);
+          for (int e = 0; e < 16; ++e) u[c][e] = keys > 0 ? pack(__uint_as_float(v[2 * e]) * inv, __uint_as_float(v[2 * e + 1]) * inv) : 0u;
         }
-      }
-      float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        tc_fence_before();
+        warp_arrive(&bar.o_free[t]);
 #pragma unroll
-      for (int c = 0; c < 4; c += 2) {
-        uint32_t w[32];
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float2 x = fma2(make_float2(__uint_as_float(v[c + (e >> 5)][e & 31]), __uint_as_float(v[c + (e >> 5)][(e & 31) + 1])),
-                                make_float2(a, a), make_float2(shift, shift));
-          const float2 p = (e & 6) == 0 ? exp2_two<true>(x) : exp2_two<false>(x);
-          part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
-          w[e >> 1] = pack(p.x, p.y);
-        }
-        tc_store32(tp + c * 16, w);
-      }
-      sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&p_ready[t]));
-    }
-    if (ok && n[t] > 0) ok = tc_wait(&pv_done[t], (n[t] - 1) & 1, deadline);
-    if (ok && n[t] == 0 && tiles > 0) ok = tc_wait(&q_full, 0, deadline);     // its copy of Q has landed
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
-    tc_fence_after();
-    // the tile of Q is no longer read: it takes O on its way out
-    uint8_t *tile = base + t * F::tile;
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int c = 0; c < 2 * NP; ++c) {
-      uint32_t w[32], u[16];
-      if (n[t] > 0) {
-        tc_load32(to + c * 32, w);
-        tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * inv, __uint_as_float(w[2 * e + 1]) * inv) : 0u;
+        for (int c = 0; c < 2 * NP; ++c) stage_row<NP>(tile, row, c * 32, u[c]);
+        __syncwarp();
+        write_rows<NP>(tile, (warp & 3) * 32, 32, w.at + t * kT, z.tq, z, dst, o.t);
       } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = 0u;
+        write_zeros<NP>((warp & 3) * 32, 32, w.at + t * kT, z.tq, z, dst, o.t);
       }
-      stage_row<NP>(tile, row, c * 32, u);
+      if (i < z.tq)
+        lse[((long long)w.b * z.heads + w.h) * z.tq + i] = keys > 0 ? fmaf(ref, a * kLn2, logf(sum)) : -INFINITY;
+      if (k.tiles > 0) {
+        tc_proxy_fence();                // the next copy into the tile comes after these reads
+        warp_arrive(&bar.q_empty[qn % F::q_ring]);
+        ++qn;
+      }
     }
-    __syncwarp();
-    write_rows<NP>(tile, (warp & 3) * 32, i0 + t * kT, z.tq, z, o.p + (long long)b * o.b + (long long)h * o.h, o.t);
-    if (i < z.tq)
-      lse[((long long)b * z.heads + h) * z.tq + i] = keys > 0 ? fmaf(ref, a * kLn2, logf(sum)) : -INFINITY;
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
@@ -516,43 +645,44 @@ __device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, in
 // follows when both products of this one are over.
 template <int NP> struct Dkv {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 4 : 2, line_ring = 2;
+  static constexpr int kv_ring = NP == 1 ? 2 : 1, q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 3 : 2, line_ring = 2;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
-  static constexpr uint32_t lines = (2 + q_ring + do_ring) * tile, bars = lines + line_ring * line;
-  static constexpr size_t smem = bars + 256;
+  static constexpr uint32_t q = 2 * kv_ring * tile, d_o = q + q_ring * tile, lines = d_o + do_ring * tile, bars = lines + line_ring * line;
+  static constexpr size_t smem = bars + 320;
   static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
 };
 template <int NP> struct DkvBars {
-  uint64_t kv_full, q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring], do_empty[Dkv<NP>::do_ring],
-      line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, dp_full, dp_free, p_ready, ds_ready, done;
+  Queue queue;
+  uint64_t kv_full[Dkv<NP>::kv_ring], kv_empty[Dkv<NP>::kv_ring], q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring],
+      do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, dp_full, dp_free, p_ready, ds_ready,
+      done, acc_free;
   uint32_t tmem;
 };
 
 template <int NP>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
+                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z, int blocks,
                  const float *__restrict__ lines, int padded, const View dk, const View dv) {
   typedef Dkv<NP> F;
-  extern __shared__ __align__(1024) uint8_t base[];         // all of the CTA's shared memory: starts on a 1024-byte boundary
-  static_assert(sizeof(DkvBars<NP>) <= 256, "barriers behind the tiles");
+  extern __shared__ __align__(1024) uint8_t base[];
+  static_assert(sizeof(DkvBars<NP>) <= 320, "barriers behind the tiles");
   DkvBars<NP> &bar = *reinterpret_cast<DkvBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t sk = smem_u32(base), sv = sk + F::tile, sq = sv + F::tile, sdo = sq + F::q_ring * F::tile;
+  const uint32_t s0 = smem_u32(base), sq = s0 + F::q, sdo = s0 + F::d_o;
   float *sline = reinterpret_cast<float *>(base + F::lines);      // [ring][2][128]
   const int ranks = (int)cluster_size(), rank = (int)cluster_rank(), kv_heads = z.heads / z.group;
-  const int column = blockIdx.x / ranks, hk = column % kv_heads, b = column / kv_heads;
-  const int j0 = blockIdx.y * kT;            // the first keys, which most queries see, start first
 
   if (threadIdx.x == 0) {
-    if (sk & 1023u) atomicOr(z.status, CDG_ST_TIMEOUT);      // (the copies' swizzle counts on it)
-    mbar_init(smem_u32(&bar.kv_full), 1);
+    queue_init(bar.queue);
+    for (int i = 0; i < F::kv_ring; ++i) { mbar_init(smem_u32(&bar.kv_full[i]), 1); mbar_init(smem_u32(&bar.kv_empty[i]), 8); }
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
     for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 2); }
     for (int i = 0; i < F::line_ring; ++i) { mbar_init(smem_u32(&bar.line_full[i]), 1); mbar_init(smem_u32(&bar.line_empty[i]), 8); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.dp_free), 8); mbar_init(smem_u32(&bar.done), 1);
     mbar_init(smem_u32(&bar.p_ready), 8); mbar_init(smem_u32(&bar.ds_ready), 8);
+    mbar_init(smem_u32(&bar.acc_free), 8);
     mbar_init_fence();
   }
   if (warp == 9) tc_alloc(&bar.tmem, 512);
@@ -563,207 +693,249 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
+  const int columns = kv_heads * z.batch;
 
-  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
-  // query tiles first .. last - 1 see key j0 or a later one of this tile
-  const int first = j0 >= lk ? 0 : z.causal ? max(0, j0 - (lk - lq)) / kT : 0;
-  const int last = j0 >= lk ? 0 : (lq + kT - 1) / kT;
-  const int per = max(0, last - first), all = (sk & 1023u) ? 0 : per * z.group;
-  const int total = (all - rank + ranks - 1) / ranks;        // this CTA's: numbers rank, rank + ranks, ...
-  auto query0 = [&](int it) { return (first + (rank + it * ranks) % per) * kT; };
+  // query tiles first .. first + per - 1 see a key of the block; over the heads of the group this CTA takes
+  // numbers rank, rank + ranks, ... of per * group, `total` of them
+  struct Work { int lq, lk, first, per, total; };
+  auto work_of = [&](const Block &w) {
+    Work k;
+    k.lq = used(z.q_lens, w.b, z.tq);
+    k.lk = used(z.kv_lens, w.b, z.tk);
+    k.first = w.at >= k.lk ? 0 : z.causal ? max(0, w.at - (k.lk - k.lq)) / kT : 0;
+    k.per = w.at >= k.lk ? 0 : max(0, (k.lq + kT - 1) / kT - k.first);
+    k.total = (k.per * z.group - rank + ranks - 1) / ranks;
+    return k;
+  };
+  auto query0 = [&](const Work &k, int it) { return (k.first + (rank + it * ranks) % k.per) * kT; };
+  // the first keys are seen by the most queries; a cluster takes one block and asks for no more
+  auto block = [&](long long at) { return block_of(at, kv_heads, columns, blocks, kT, false); };
+  const long long mine0 = blockIdx.x / ranks;
 
   if (warp == 8) {
-    if (tc_elect() && total > 0) {
+    if (tc_elect()) {
       bool ok = true;
-      int qn = 0, dn = 0, ln = 0;
-      mbar_expect_tx(smem_u32(&bar.kv_full), 2 * F::tile);
-      load_tile<NP>(sk, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&bar.kv_full));
-      load_tile<NP>(sv, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&bar.kv_full));
-      for (int it = 0; it < total; ++it) {
-        const int h = hk * z.group + (rank + it * ranks) / per, i0 = query0(it);
-        const int qs = it % F::q_ring, os = it % F::do_ring, ls = it % F::line_ring;
-        if (it >= F::q_ring && !(ok = mbar_wait(smem_u32(&bar.q_empty[qs]), (it / F::q_ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&bar.q_full[qs]), F::tile);
-        load_tile<NP>(sq + qs * F::tile, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&bar.q_full[qs]));
-        ++qn;
-        if (it >= F::line_ring && !(ok = mbar_wait(smem_u32(&bar.line_empty[ls]), (it / F::line_ring - 1) & 1, deadline))) break;
-        const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i0;
-        mbar_expect_tx(smem_u32(&bar.line_full[ls]), F::line);
-        load_line(smem_u32(sline + ls * 2 * kT), line, smem_u32(&bar.line_full[ls]));
-        load_line(smem_u32(sline + ls * 2 * kT + kT), line + padded, smem_u32(&bar.line_full[ls]));
-        ++ln;
-        if (it >= F::do_ring && !(ok = mbar_wait(smem_u32(&bar.do_empty[os]), (it / F::do_ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&bar.do_full[os]), F::tile);
-        load_tile<NP>(sdo + os * F::tile, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&bar.do_full[os]));
-        ++dn;
+      int cn = 0, qn = 0, dn = 0, ln = 0;
+      int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next_one(bar.queue, seq++, deadline, ok)) {
+if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
+        const Block w = block(at);
+        const Work k = work_of(w);
+        if (k.total == 0) continue;
+        if (!(ok = wait_released(bar.kv_empty, cn, F::kv_ring, deadline))) break;
+        uint64_t *full = &bar.kv_full[cn % F::kv_ring];
+        const uint32_t kv = s0 + cn % F::kv_ring * 2 * F::tile;
+        mbar_expect_tx(smem_u32(full), 2 * F::tile);
+        load_tile<NP>(kv, &mk, w.at, w.h, batch_of(z, kK, w.b), smem_u32(full));
+        load_tile<NP>(kv + F::tile, &mv, w.at, w.h, batch_of(z, kV, w.b), smem_u32(full));
+        ++cn;
+        for (int it = 0; it < k.total; ++it) {
+          const int h = w.h * z.group + (rank + it * ranks) / k.per, i0 = query0(k, it);
+          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          full = &bar.q_full[qn % F::q_ring];
+          mbar_expect_tx(smem_u32(full), F::tile);
+          load_tile<NP>(sq + qn % F::q_ring * F::tile, &mq, i0, h, batch_of(z, kQ, w.b), smem_u32(full));
+          ++qn;
+          if (!(ok = wait_released(bar.line_empty, ln, F::line_ring, deadline))) break;
+          full = &bar.line_full[ln % F::line_ring];
+          const float *line = lines + ((long long)w.b * z.heads + h) * 2 * padded + i0;
+          float *to = sline + ln % F::line_ring * 2 * kT;
+          mbar_expect_tx(smem_u32(full), F::line);
+          load_line(smem_u32(to), line, smem_u32(full));
+          load_line(smem_u32(to + kT), line + padded, smem_u32(full));
+          ++ln;
+          if (!(ok = wait_released(bar.do_empty, dn, F::do_ring, deadline))) break;
+          full = &bar.do_full[dn % F::do_ring];
+          mbar_expect_tx(smem_u32(full), F::tile);
+          load_tile<NP>(sdo + dn % F::do_ring * F::tile, &mdo, i0, h, batch_of(z, kDo, w.b), smem_u32(full));
+          ++dn;
+        }
       }
       if (!ok) {
         atomicOr(z.status, CDG_ST_TIMEOUT);
-        mbar_wait(smem_u32(&bar.kv_full), 0, clock64() + kCdgWaitCycles);
-        for (int i = max(0, qn - F::q_ring); i < qn; ++i) mbar_wait(smem_u32(&bar.q_full[i % F::q_ring]), (i / F::q_ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, ln - F::line_ring); i < ln; ++i) mbar_wait(smem_u32(&bar.line_full[i % F::line_ring]), (i / F::line_ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, dn - F::do_ring); i < dn; ++i) mbar_wait(smem_u32(&bar.do_full[i % F::do_ring]), (i / F::do_ring) & 1, clock64() + kCdgWaitCycles);
+        if (ranks == 1) drain(bar.queue.full, seq + 1, 2);
+        drain(bar.kv_full, cn, F::kv_ring);
+        drain(bar.q_full, qn, F::q_ring);
+        drain(bar.line_full, ln, F::line_ring);
+        drain(bar.do_full, dn, F::do_ring);
       }
     }
   } else if (warp >= 9) {
-    // (by either warp, each before its own product) a tile's rows past the sequence's queries are zeroed before any product reads them
-    auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
-      const int s = it % ring;
-      if (!tc_wait(&full[s], (it / ring) & 1, deadline)) return false;
-      const int left = lq - query0(it);
-      if (z.q_lens && left < kT) zero_rows<NP>(base + (tiles - sk) + s * F::tile, left);
-      return true;
-    };
     bool ok = true;
-    if (warp == 9) {
-      auto scores = [&](int it) {
-        if (!arrived(bar.q_full, sq, F::q_ring, it) || (it > 0 && !tc_wait(&bar.dp_free, (it - 1) & 1, deadline))) return false;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_scores<NP>(tm + (it & 1) * kT, sk, sq + it % F::q_ring * F::tile);
-          tc_commit(&bar.s_full);
-        }
-        __syncwarp();
+    int cn = 0, n = 0;                   // blocks and turns
+    int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+      const Block w = block(at);
+      const Work k = work_of(w);
+      if (k.total == 0) continue;
+      // a tile has landed; its rows past the sequence's queries are zeroed (by either warp, each before its own product)
+      auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
+        const int s = n % ring, left = k.lq - query0(k, it);
+        if (!tc_wait(&full[s], parity(n, ring), deadline)) return false;
+        if (z.q_lens && left < kT) zero_rows<NP>(base + tiles + s * F::tile, left);
         return true;
       };
-      auto gradients = [&](int it) {
-        if (!arrived(bar.do_full, sdo, F::do_ring, it) || (it > 0 && !tc_wait(&bar.done, (it - 1) & 1, deadline))) return false;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_scores<NP>(tm + (~it & 1) * kT, sv, sdo + it % F::do_ring * F::tile);
-          tc_commit(&bar.dp_full);
-          tc_commit(&bar.do_empty[it % F::do_ring]);
+      const uint32_t sk = s0 + cn % F::kv_ring * 2 * F::tile, sv = sk + F::tile;
+      if (warp == 9) {
+        if (!(ok = tc_wait(&bar.kv_full[cn % F::kv_ring], parity(cn, F::kv_ring), deadline))) break;
+        for (int it = 0; it < k.total; ++it, ++n) {
+          if (!(ok = arrived(bar.q_full, F::q, F::q_ring, it) && (n == 0 || tc_wait(&bar.dp_free, (n - 1) & 1, deadline)))) break;
+          tc_fence_after();
+          if (tc_elect()) {
+            mma_scores<NP>(tm + (n & 1) * kT, sk, sq + n % F::q_ring * F::tile);
+            tc_commit(&bar.s_full);
+          }
+          __syncwarp();
+          if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, it) && (n == 0 || tc_wait(&bar.done, (n - 1) & 1, deadline)))) break;
+          tc_fence_after();
+          if (tc_elect()) {
+            mma_scores<NP>(tm + (~n & 1) * kT, sv, sdo + n % F::do_ring * F::tile);
+            tc_commit(&bar.dp_full);
+            tc_commit(&bar.do_empty[n % F::do_ring]);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-        return true;
-      };
-      if (total > 0) ok = tc_wait(&bar.kv_full, 0, deadline);
-      for (int it = 0; it < total && ok; ++it) ok = scores(it) && gradients(it);
-    } else {
-      for (int it = 0; it < total && ok; ++it) {
-        const uint32_t here = tm + (it & 1) * kT;
-        if (!(ok = arrived(bar.do_full, sdo, F::do_ring, it) && tc_wait(&bar.p_ready, it & 1, deadline))) break;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_rows<NP>(tm + F::dv, here, 64, sdo + it % F::do_ring * F::tile, it > 0);
-          tc_commit(&bar.do_empty[it % F::do_ring]);
+      } else {
+        for (int it = 0; it < k.total; ++it, ++n) {
+          const uint32_t here = tm + (n & 1) * kT;
+          if (it == 0 && cn > 0 && !(ok = tc_wait(&bar.acc_free, (cn - 1) & 1, deadline))) break;
+          if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, it) && tc_wait(&bar.p_ready, n & 1, deadline))) break;
+          tc_fence_after();
+          if (tc_elect()) {
+            mma_rows<NP>(tm + F::dv, here, 64, sdo + n % F::do_ring * F::tile, it > 0);
+            tc_commit(&bar.do_empty[n % F::do_ring]);
+          }
+          __syncwarp();
+          if (!(ok = tc_wait(&bar.ds_ready, n & 1, deadline))) break;
+          tc_fence_after();
+          if (tc_elect()) {
+            mma_rows<NP>(tm + F::dk, here + 32, 64, sq + n % F::q_ring * F::tile, it > 0);
+            tc_commit(&bar.done);
+            tc_commit(&bar.q_empty[n % F::q_ring]);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-        if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_rows<NP>(tm + F::dk, here + 32, 64, sq + it % F::q_ring * F::tile, it > 0);
-          tc_commit(&bar.done);
-          tc_commit(&bar.q_empty[it % F::q_ring]);
-        }
-        __syncwarp();
       }
+      ++cn;
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
-    const int half = warp >> 2, row = (warp & 3) * 32 + lane, j = j0 + row;
-    const uint32_t mine = tm + ((uint32_t)((warp & 3) * 32) << 16) + half * 64;
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16), mine = lanes + half * 64;
     const float a = z.negative ? -z.a : z.a;
-    const int off = lk - lq;
+    const float2 aa = make_float2(a, a);
     bool ok = true;
-    for (int it = 0; it < total; ++it) {
-      const int ls = it % F::line_ring, i0 = query0(it) + half * 64;
-      const uint32_t here = mine + (it & 1) * kT, there = mine + (~it & 1) * kT;
-      const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
-      if (!(ok = tc_wait(&bar.line_full[ls], (it / F::line_ring) & 1, deadline) && tc_wait(&bar.s_full, it & 1, deadline))) break;
-      tc_fence_after();
-      uint32_t v[2][32], w[32];
-      tc_load32(here, v[0]);
-      tc_load32(here + 32, v[1]);
-      tc_wait_ld();
-      float p[64];
-#pragma unroll
-      for (int e = 0; e < 64; e += 8) {
-        const float4 l = *reinterpret_cast<const float4 *>(l2 + e), m = *reinterpret_cast<const float4 *>(l2 + e + 4);
-        const float2 aa = make_float2(a, a);
-        const float2 x0 = exp2_two<true>(fma2(two(v, e), aa, make_float2(l.x, l.y)));
-        const float2 x1 = exp2_two<false>(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
-        const float2 x2 = exp2_two<false>(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
-        const float2 x3 = exp2_two<false>(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
-        p[e] = x0.x; p[e + 1] = x0.y; p[e + 2] = x1.x; p[e + 3] = x1.y;
-        p[e + 4] = x2.x; p[e + 5] = x2.y; p[e + 6] = x3.x; p[e + 7] = x3.y;
-      }
-      // under the causal rule key j is seen by queries from j - off on
-      const int from = z.causal ? j - off - i0 : 0;
-      if (__any_sync(0xffffffffu, from > 0)) {
-#pragma unroll
-        for (int e = 0; e < 64; ++e)
-          if (e < from) p[e] = 0.0f;
-      }
-#pragma unroll
-      for (int e = 0; e < 32; ++e) w[e] = pack(p[2 * e], p[2 * e + 1]);
-      tc_store32(here, w);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.p_ready));
-      if (!(ok = tc_wait(&bar.dp_full, it & 1, deadline))) break;
-      tc_fence_after();
-      tc_load32(there, v[0]);
-      tc_load32(there + 32, v[1]);
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.dp_free));
-#pragma unroll
-      for (int e = 0; e < 64; e += 4) {
-        const float4 d = *reinterpret_cast<const float4 *>(delta + e);
-        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(two(v, e), make_float2(d.x, d.y)));
-        const float2 y = mul2(make_float2(p[e + 2], p[e + 3]), add2(two(v, e + 2), make_float2(d.z, d.w)));
-        w[e / 2] = pack(x.x, x.y);
-        w[e / 2 + 1] = pack(y.x, y.y);
-      }
-      tc_store32(here + 32, w);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(&bar.ds_ready));
-        mbar_arrive(smem_u32(&bar.line_empty[ls]));
-      }
-    }
-    // warps 0-3 bring dv out, 4-7 dk, through shared memory that no product reads any more
-    if (ok && total > 0) ok = tc_wait(&bar.done, (total - 1) & 1, deadline);
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
-    tc_fence_after();
-    const uint32_t from = tm + ((uint32_t)((warp & 3) * 32) << 16) + (half ? F::dk : F::dv);
-    const float f = half ? z.scale : 1.0f;
-    const View &out = half ? dk : dv;
-    bf16 *dst = out.p + (long long)b * out.b + (long long)hk * out.h;
-    uint8_t *tile = base + half * (ranks > 1 ? 2 : 1) * F::tile;
-#pragma unroll
-    for (int c = 0; c < 2 * NP; ++c) {
-      uint32_t w[32] = {}, u[16];
-      if (total > 0) {
-        tc_load32(from + c * 32, w);
+    int cn = 0, n = 0;
+    int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+      const Block w = block(at);
+      const Work k = work_of(w);
+      const int j = w.at + row, off = k.lk - k.lq;
+      for (int it = 0; it < k.total; ++it, ++n) {
+        const int ls = n % F::line_ring, i0 = query0(k, it) + half * 64;
+        const uint32_t here = mine + (n & 1) * kT, there = mine + (~n & 1) * kT;
+        const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
+        if (!(ok = tc_wait(&bar.line_full[ls], parity(n, F::line_ring), deadline) && tc_wait(&bar.s_full, n & 1, deadline))) break;
+        tc_fence_after();
+        uint32_t v[2][32], u[32];
+        tc_load32(here, v[0]);
+        tc_load32(here + 32, v[1]);
         tc_wait_ld();
-      }
-      if (ranks > 1) {
-        keep_sums<NP>(tile, row, c * 32, w);
-      } else {
+        float p[64];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = j < lk ? pack(__uint_as_float(w[2 * e]) * f, __uint_as_float(w[2 * e + 1]) * f) : 0u;
-        stage_row<NP>(tile, row, c * 32, u);
+        for (int e = 0; e < 64; e += 8) {
+          const float4 l = *reinterpret_cast<const float4 *>(l2 + e), m = *reinterpret_cast<const float4 *>(l2 + e + 4);
+          const float2 x0 = exp2_two<true>(fma2(two(v, e), aa, make_float2(l.x, l.y)));
+          const float2 x1 = exp2_two<false>(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
+          const float2 x2 = exp2_two<false>(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
+          const float2 x3 = exp2_two<false>(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
+          p[e] = x0.x; p[e + 1] = x0.y; p[e + 2] = x1.x; p[e + 3] = x1.y;
+          p[e + 4] = x2.x; p[e + 5] = x2.y; p[e + 6] = x3.x; p[e + 7] = x3.y;
+        }
+        // under the causal rule key j is seen by queries from j - off on
+        const int from = z.causal ? j - off - i0 : 0;
+        if (__any_sync(0xffffffffu, from > 0)) {
+#pragma unroll
+          for (int e = 0; e < 64; ++e)
+            if (e < from) p[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) u[e] = pack(p[2 * e], p[2 * e + 1]);
+        tc_store32(here, u);
+        tc_wait_st();
+        tc_fence_before();
+        warp_arrive(&bar.p_ready);
+        if (!(ok = tc_wait(&bar.dp_full, n & 1, deadline))) break;
+        tc_fence_after();
+        tc_load32(there, v[0]);
+        tc_load32(there + 32, v[1]);
+        tc_wait_ld();
+        tc_fence_before();
+        warp_arrive(&bar.dp_free);
+#pragma unroll
+        for (int e = 0; e < 64; e += 4) {
+          const float4 d = *reinterpret_cast<const float4 *>(delta + e);
+          const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(two(v, e), make_float2(d.x, d.y)));
+          const float2 y = mul2(make_float2(p[e + 2], p[e + 3]), add2(two(v, e + 2), make_float2(d.z, d.w)));
+          u[e / 2] = pack(x.x, x.y);
+          u[e / 2 + 1] = pack(y.x, y.y);
+        }
+        tc_store32(here + 32, u);
+        tc_wait_st();
+        tc_fence_before();
+        warp_arrive(&bar.ds_ready);
+        if (lane == 0) mbar_arrive(smem_u32(&bar.line_empty[ls]));
+      }
+      if (!ok) break;
+      // warps 0-3 bring dv out, 4-7 dk, through shared memory that no product reads any more
+      const View &out = half ? dk : dv;
+      const float f = half ? z.scale : 1.0f;
+      bf16 *dst = out.p + (long long)w.b * out.b + (long long)w.h * out.h;
+      if (k.total > 0 && !(ok = tc_wait(&bar.done, (n - 1) & 1, deadline))) break;
+      tc_fence_after();
+      if (ranks > 1 || k.total > 0) {
+        uint8_t *tile = base + (ranks > 1 ? half * 2 : cn % F::kv_ring * 2 + half) * F::tile;
+#pragma unroll
+        for (int c = 0; c < 2 * NP; ++c) {
+          uint32_t v[32] = {}, u[16];
+          if (k.total > 0) {
+            tc_load32(lanes + (half ? F::dk : F::dv) + c * 32, v);
+            tc_wait_ld();
+          }
+          if (ranks > 1) {
+            keep_sums<NP>(tile, row, c * 32, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = j < k.lk ? pack(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f) : 0u;
+            stage_row<NP>(tile, row, c * 32, u);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (ranks == 1) {
+          if (lane == 0) mbar_arrive(smem_u32(&bar.acc_free));
+          write_rows<NP>(tile, (warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
+          tc_proxy_fence();              // the next copy into the tile comes after these reads
+          warp_arrive(&bar.kv_empty[cn % F::kv_ring]);
+          ++cn;
+        }
+      } else {
+        write_zeros<NP>((warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
       }
     }
-    __syncwarp();
-    if (ranks == 1) write_rows<NP>(tile, (warp & 3) * 32, j0, z.tk, z, dst, out.t);
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
-  if (ranks > 1) {
+  if (ranks > 1) {             // one block to a cluster
     cluster_sync();
     if (warp < 8) {
       const int half = warp >> 2;
       const View &out = half ? dk : dv;
-      join_sums<NP>(sk + half * 2 * F::tile, ranks, rank, threadIdx.x & 127, 128, j0, z.tk, lk, z, half ? z.scale : 1.0f,
-                    out.p + (long long)b * out.b + (long long)hk * out.h, out.t);
+      const Block w = block_of(blockIdx.x / ranks, kv_heads, columns, blocks, kT, false);
+      join_sums<NP>(s0 + half * 2 * F::tile, ranks, rank, threadIdx.x & 127, 128, w.at, z.tk, used(z.kv_lens, w.b, z.tk), z,
+                    half ? z.scale : 1.0f, out.p + (long long)w.b * out.b + (long long)w.h * out.h, out.t);
     }
     cluster_sync();            // no CTA leaves while another reads its sums
   }
@@ -777,40 +949,39 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 constexpr int kDqThreads = 384;        // three warpgroups: 168 registers a thread at launch, 64,512 in all
 template <int NP> struct Dq {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int k_ring = NP == 1 ? 6 : 3, v_ring = NP == 1 ? 4 : 2;
-  static constexpr uint32_t bars = (2 + k_ring + v_ring) * tile;
-  static constexpr size_t smem = bars + 256;
+  static constexpr int q_ring = NP == 1 ? 2 : 1, k_ring = NP == 1 ? 5 : 3, v_ring = NP == 1 ? 3 : 2;       // q: Q and dO
+  static constexpr uint32_t k = 2 * q_ring * tile, v = k + k_ring * tile, bars = v + v_ring * tile;
+  static constexpr size_t smem = bars + 320;
   static constexpr uint32_t dq = 256, ds = 384;
 };
 template <int NP> struct DqBars {
-  uint64_t q_full, k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring], v_empty[Dq<NP>::v_ring], s_full, s_free,
-      dp_full, dp_free, ds_ready, dq_done[2];
+  Queue queue;
+  uint64_t q_full[Dq<NP>::q_ring], q_empty[Dq<NP>::q_ring], k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring],
+      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready, dq_done[2], acc_free;
   uint32_t tmem;
 };
 
 template <int NP>
 __global__ void __launch_bounds__(kDqThreads, 1)
 attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z,
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z, int blocks,
                 const float *__restrict__ lines, int padded, const View dq) {
   typedef Dq<NP> F;
   extern __shared__ __align__(1024) uint8_t base[];
-  static_assert(sizeof(DqBars<NP>) <= 256, "barriers behind the tiles");
+  static_assert(sizeof(DqBars<NP>) <= 320, "barriers behind the tiles");
   DqBars<NP> &bar = *reinterpret_cast<DqBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t sq = smem_u32(base), sdo = sq + F::tile, sk = sdo + F::tile, sv = sk + F::k_ring * F::tile;
+  const uint32_t s0 = smem_u32(base), sk = s0 + F::k, sv = s0 + F::v;
   const int ranks = (int)cluster_size(), rank = (int)cluster_rank();
-  const int column = blockIdx.x / ranks, h = column % z.heads, b = column / z.heads, hk = h / z.group;
-  const int i0 = (z.causal ? (int)gridDim.y - 1 - (int)blockIdx.y : (int)blockIdx.y) * kT;
 
   if (threadIdx.x == 0) {
-    if (sq & 1023u) atomicOr(z.status, CDG_ST_TIMEOUT);
-    mbar_init(smem_u32(&bar.q_full), 1);
+    queue_init(bar.queue);
+    for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 8); }
     for (int i = 0; i < F::k_ring; ++i) { mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 1); }
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
-    mbar_init(smem_u32(&bar.ds_ready), 8);
+    mbar_init(smem_u32(&bar.ds_ready), 8); mbar_init(smem_u32(&bar.acc_free), 8);
     mbar_init(smem_u32(&bar.dq_done[0]), 1); mbar_init(smem_u32(&bar.dq_done[1]), 1);
     mbar_init_fence();
   }
@@ -822,192 +993,242 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
+  const int columns = z.heads * z.batch;
 
-  const int lq = used(z.q_lens, b, z.tq), lk = used(z.kv_lens, b, z.tk);
-  const int seen = i0 >= lq ? 0 : z.causal ? min(lk, min(i0 + kT, lq) + lk - lq) : lk;
-  const int all = seen > 0 && !(sq & 1023u) ? (seen + kT - 1) / kT : 0;
-  const int total = (all - rank + ranks - 1) / ranks;        // this CTA's key tiles: rank, rank + ranks, ...
+  // key tiles rank, rank + ranks, ... of those that the block sees, `total` of them
+  struct Work { int lq, lk, total; };
+  auto work_of = [&](const Block &w) {
+    Work k;
+    k.lq = used(z.q_lens, w.b, z.tq);
+    k.lk = used(z.kv_lens, w.b, z.tk);
+    const int seen = w.at >= k.lq ? 0 : z.causal ? min(k.lk, min(w.at + kT, k.lq) + k.lk - k.lq) : k.lk;
+    k.total = ((seen > 0 ? (seen + kT - 1) / kT : 0) - rank + ranks - 1) / ranks;
+    return k;
+  };
+  auto block = [&](long long at) { return block_of(at, z.heads, columns, blocks, kT, z.causal); };
+  const long long mine0 = blockIdx.x / ranks;
 
   if (warp >= 8) {
-  tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
-  if (warp == 8) {
-    if (tc_elect() && total > 0) {
-      bool ok = true;
-      int kn = 0, vn = 0;
-      mbar_expect_tx(smem_u32(&bar.q_full), 2 * F::tile);
-      load_tile<NP>(sq, &mq, i0, h, batch_of(z, kQ, b), smem_u32(&bar.q_full));
-      load_tile<NP>(sdo, &mdo, i0, h, batch_of(z, kDo, b), smem_u32(&bar.q_full));
-      for (int it = 0; it < total; ++it) {
-        const int ks = it % F::k_ring, vs = it % F::v_ring, j0 = (rank + it * ranks) * kT;
-        if (it >= F::k_ring && !(ok = mbar_wait(smem_u32(&bar.k_empty[ks]), (it / F::k_ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&bar.k_full[ks]), F::tile);
-        load_tile<NP>(sk + ks * F::tile, &mk, j0, hk, batch_of(z, kK, b), smem_u32(&bar.k_full[ks]));
-        ++kn;
-        if (it >= F::v_ring && !(ok = mbar_wait(smem_u32(&bar.v_empty[vs]), (it / F::v_ring - 1) & 1, deadline))) break;
-        mbar_expect_tx(smem_u32(&bar.v_full[vs]), F::tile);
-        load_tile<NP>(sv + vs * F::tile, &mv, j0, hk, batch_of(z, kV, b), smem_u32(&bar.v_full[vs]));
-        ++vn;
-      }
-      if (!ok) {
-        atomicOr(z.status, CDG_ST_TIMEOUT);
-        mbar_wait(smem_u32(&bar.q_full), 0, clock64() + kCdgWaitCycles);
-        for (int i = max(0, kn - F::k_ring); i < kn; ++i) mbar_wait(smem_u32(&bar.k_full[i % F::k_ring]), (i / F::k_ring) & 1, clock64() + kCdgWaitCycles);
-        for (int i = max(0, vn - F::v_ring); i < vn; ++i) mbar_wait(smem_u32(&bar.v_full[i % F::v_ring]), (i / F::v_ring) & 1, clock64() + kCdgWaitCycles);
-      }
-    }
-  } else if (warp == 9 || warp == 10) {
-    auto arrived = [&](int it) {         // K of tile it, its rows past the sequence zeroed
-      const int s = it % F::k_ring, left = lk - (rank + it * ranks) * kT;
-      if (!tc_wait(&bar.k_full[s], (it / F::k_ring) & 1, deadline)) return false;
-      if (z.kv_lens && left < kT) zero_rows<NP>(base + (sk - sq) + s * F::tile, left);
-      return true;
-    };
-    auto scores = [&](int it) {          // S of tile it, when the one before is in registers
-      if (!arrived(it) || (it > 0 && !tc_wait(&bar.s_free, (it - 1) & 1, deadline))) return false;
-      tc_fence_after();
+    tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+    if (warp == 8) {
       if (tc_elect()) {
-        mma_scores<NP>(tm, sq, sk + it % F::k_ring * F::tile);
-        tc_commit(&bar.s_full);
-      }
-      __syncwarp();
-      return true;
-    };
-    auto gradients = [&](int it) {       // dP likewise
-      const int s = it % F::v_ring;
-      if (!tc_wait(&bar.v_full[s], (it / F::v_ring) & 1, deadline) || (it > 0 && !tc_wait(&bar.dp_free, (it - 1) & 1, deadline))) return false;
-      tc_fence_after();
-      if (tc_elect()) {
-        mma_scores<NP>(tm + kT, sdo, sv + s * F::tile);
-        tc_commit(&bar.dp_full);
-        tc_commit(&bar.v_empty[s]);
-      }
-      __syncwarp();
-      return true;
-    };
-    bool ok = true;
-    if (warp == 9) {
-      ok = total == 0 || (tc_wait(&bar.q_full, 0, deadline) && scores(0));
-      for (int it = 0; it < total && ok; ++it) ok = gradients(it) && (it + 1 == total || scores(it + 1));
-    } else {
-      for (int it = 0; it < total && ok; ++it) {
-        const int ks = it % F::k_ring;
-        if (!(ok = tc_wait(&bar.ds_ready, it & 1, deadline))) break;
-        tc_fence_after();
-        if (tc_elect()) {
-          mma_rows<NP>(tm + F::dq, tm + F::ds + (it & 1) * 64, 32, sk + ks * F::tile, it > 0);
-          tc_commit(&bar.dq_done[it & 1]);
-          tc_commit(&bar.k_empty[ks]);
+        bool ok = true;
+        int qn = 0, kn = 0, vn = 0;
+        int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next_one(bar.queue, seq++, deadline, ok)) {
+if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
+          const Block w = block(at);
+          const Work k = work_of(w);
+          if (k.total == 0) continue;
+          const int hk = w.h / z.group;
+          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          uint64_t *full = &bar.q_full[qn % F::q_ring];
+          const uint32_t q = s0 + qn % F::q_ring * 2 * F::tile;
+          mbar_expect_tx(smem_u32(full), 2 * F::tile);
+          load_tile<NP>(q, &mq, w.at, w.h, batch_of(z, kQ, w.b), smem_u32(full));
+          load_tile<NP>(q + F::tile, &mdo, w.at, w.h, batch_of(z, kDo, w.b), smem_u32(full));
+          ++qn;
+          for (int it = 0; it < k.total; ++it) {
+            const int j0 = (rank + it * ranks) * kT;
+            if (!(ok = wait_released(bar.k_empty, kn, F::k_ring, deadline))) break;
+            full = &bar.k_full[kn % F::k_ring];
+            mbar_expect_tx(smem_u32(full), F::tile);
+            load_tile<NP>(sk + kn % F::k_ring * F::tile, &mk, j0, hk, batch_of(z, kK, w.b), smem_u32(full));
+            ++kn;
+            if (!(ok = wait_released(bar.v_empty, vn, F::v_ring, deadline))) break;
+            full = &bar.v_full[vn % F::v_ring];
+            mbar_expect_tx(smem_u32(full), F::tile);
+            load_tile<NP>(sv + vn % F::v_ring * F::tile, &mv, j0, hk, batch_of(z, kV, w.b), smem_u32(full));
+            ++vn;
+          }
         }
-        __syncwarp();
+        if (!ok) {
+          atomicOr(z.status, CDG_ST_TIMEOUT);
+          if (ranks == 1) drain(bar.queue.full, seq + 1, 2);
+          drain(bar.q_full, qn, F::q_ring);
+          drain(bar.k_full, kn, F::k_ring);
+          drain(bar.v_full, vn, F::v_ring);
+        }
       }
+    } else if (warp < 11) {
+      bool ok = true;
+      int qn = 0, n = 0;                 // blocks, and turns whose S (warp 9) or dq (warp 10) has been issued
+      int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+        const Block w = block(at);
+        const Work k = work_of(w);
+        if (k.total == 0) continue;
+        const uint32_t q = s0 + qn % F::q_ring * 2 * F::tile;
+        if (warp == 9) {
+          auto scores = [&](int it) {    // S of tile it: K has landed, its rows past the sequence are zeroed, the S before is in registers
+            const int s = n % F::k_ring, left = k.lk - (rank + it * ranks) * kT;
+            if (!tc_wait(&bar.k_full[s], parity(n, F::k_ring), deadline)) return false;
+            if (z.kv_lens && left < kT) zero_rows<NP>(base + F::k + s * F::tile, left);
+            if (n > 0 && !tc_wait(&bar.s_free, (n - 1) & 1, deadline)) return false;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_scores<NP>(tm, q, sk + s * F::tile);
+              tc_commit(&bar.s_full);
+            }
+            __syncwarp();
+            ++n;
+            return true;
+          };
+          auto gradients = [&](int m) {  // dP of turn m likewise
+            const int s = m % F::v_ring;
+            if (!tc_wait(&bar.v_full[s], parity(m, F::v_ring), deadline) || (m > 0 && !tc_wait(&bar.dp_free, (m - 1) & 1, deadline))) return false;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_scores<NP>(tm + kT, q + F::tile, sv + s * F::tile);
+              tc_commit(&bar.dp_full);
+              tc_commit(&bar.v_empty[s]);
+            }
+            __syncwarp();
+            return true;
+          };
+          ok = tc_wait(&bar.q_full[qn % F::q_ring], parity(qn, F::q_ring), deadline) && scores(0);
+          for (int it = 0; it < k.total && ok; ++it) ok = gradients(n - 1) && (it + 1 == k.total || scores(it + 1));
+          if (!ok) break;
+        } else {
+          for (int it = 0; it < k.total; ++it, ++n) {
+            const int ks = n % F::k_ring;
+            if (it == 0 && qn > 0 && !(ok = tc_wait(&bar.acc_free, (qn - 1) & 1, deadline))) break;
+            if (!(ok = tc_wait(&bar.ds_ready, n & 1, deadline))) break;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_rows<NP>(tm + F::dq, tm + F::ds + (n & 1) * 64, 32, sk + ks * F::tile, it > 0);
+              tc_commit(&bar.dq_done[n & 1]);
+              tc_commit(&bar.k_empty[ks]);
+            }
+            __syncwarp();
+          }
+        }
+        ++qn;
+      }
+      if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     }
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
-  }
   } else {
     tc_regs_up<224>();
-    const int half = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + row;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tm + lanes + half * 64, tdp = ts + kT;
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + half * 64, tdp = ts + kT;
     const float a = z.negative ? -z.a : z.a;
-    const int keys = i >= lq ? 0 : z.causal ? min(lk, i + lk - lq + 1) : lk;
-    float l2 = -INFINITY, delta = 0.0f;          // both negated
-    if (i < padded) {
-      const float *line = lines + ((long long)b * z.heads + h) * 2 * padded + i;
-      l2 = line[0];
-      delta = line[padded];
-    }
-    const float2 aa = make_float2(a, a), ll = make_float2(l2, l2), dd = make_float2(delta, delta);
+    const float2 aa = make_float2(a, a);
     bool ok = true;
-    float p[64];
-    if (total > 0 && (ok = tc_wait(&bar.s_full, 0, deadline))) {
-      tc_fence_after();
-      uint32_t v[2][32];
-      tc_load32(ts, v[0]);
-      tc_load32(ts + 32, v[1]);
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.s_free));
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) {
-        const float2 x = exp2_two<false>(fma2(two(v, e), aa, ll));
-        p[e] = x.x;
-        p[e + 1] = x.y;
+    int qn = 0, n = 0;
+    int seq = 0;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+      const Block w = block(at);
+      const Work k = work_of(w);
+      const int i = w.at + row, keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;
+      float2 ll = make_float2(-INFINITY, -INFINITY), dd = make_float2(0.0f, 0.0f);          // -lse, -delta
+      if (i < padded) {
+        const float *line = lines + ((long long)w.b * z.heads + w.h) * 2 * padded + i;
+        ll.x = ll.y = line[0];
+        dd.x = dd.y = line[padded];
       }
-    }
-    for (int it = 0; it < total && ok; ++it) {
-      const bool next = it + 1 < total;
-      if (!(ok = (!next || tc_wait(&bar.s_full, (it + 1) & 1, deadline)) && tc_wait(&bar.dp_full, it & 1, deadline))) break;
-      tc_fence_after();
-      uint32_t v[2][32] = {}, u[2][32], w[32];
-      tc_load32(tdp, u[0]);
-      tc_load32(tdp + 32, u[1]);
-      if (next) {
+      float p[64];
+      if (k.total > 0) {
+        if (!(ok = tc_wait(&bar.s_full, n & 1, deadline))) break;
+        tc_fence_after();
+        uint32_t v[2][32];
         tc_load32(ts, v[0]);
         tc_load32(ts + 32, v[1]);
-      }
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(&bar.dp_free));
-        if (next) mbar_arrive(smem_u32(&bar.s_free));
-      }
-      const int left = keys - (rank + it * ranks) * kT - half * 64;
-      if (__any_sync(0xffffffffu, left < 64)) {       // replaces P and dP: whatever lies there is not used
-#pragma unroll
-        for (int e = 0; e < 64; ++e)
-          if (e >= left) { p[e] = 0.0f; u[e >> 5][e & 31] = 0u; }
-      }
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) {
-        const float2 x = mul2(make_float2(p[e], p[e + 1]), add2(two(u, e), dd));
-        w[e / 2] = pack(x.x, x.y);
-        const float2 y = fma2(two(v, e), aa, ll), t = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
-        p[e] = t.x;
-        p[e + 1] = t.y;
-      }
-      if (it > 1) {              // the place of dS is free when its last product is over
-        if (!(ok = tc_wait(&bar.dq_done[it & 1], (it / 2 - 1) & 1, deadline))) break;
-        tc_fence_after();
-      }
-      tc_store32(tm + lanes + F::ds + (it & 1) * 64 + half * 32, w);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.ds_ready));
-    }
-    if (ok && total > 0) ok = tc_wait(&bar.dq_done[(total - 1) & 1], ((total - 1) / 2) & 1, deadline);
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
-    tc_fence_after();
-    // the two groups of warps bring out half of the head dimensions each, through the tiles of Q and dO
-    const uint32_t from = tm + lanes + F::dq;
-#pragma unroll
-    for (int c = 0; c < NP; ++c) {
-      const int col = (half * NP + c) * 32;
-      uint32_t w[32] = {}, u[16];
-      if (total > 0) {
-        tc_load32(from + col, w);
         tc_wait_ld();
-      }
-      if (ranks > 1) {
-        keep_sums<NP>(base, row, col, w);
-      } else {
+        tc_fence_before();
+        warp_arrive(&bar.s_free);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(w[2 * e]) * z.scale, __uint_as_float(w[2 * e + 1]) * z.scale) : 0u;
-        stage_row<NP>(base, row, col, u);
+        for (int e = 0; e < 64; e += 2) {
+          const float2 y = fma2(two(v, e), aa, ll), x = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
+          p[e] = x.x;
+          p[e + 1] = x.y;
+        }
+      }
+      for (int it = 0; it < k.total; ++it, ++n) {
+        const bool next = it + 1 < k.total;
+        if (!(ok = (!next || tc_wait(&bar.s_full, (n + 1) & 1, deadline)) && tc_wait(&bar.dp_full, n & 1, deadline))) break;
+        tc_fence_after();
+        uint32_t v[2][32] = {}, u[2][32], x[32];
+        tc_load32(tdp, u[0]);
+        tc_load32(tdp + 32, u[1]);
+        if (next) {
+          tc_load32(ts, v[0]);
+          tc_load32(ts + 32, v[1]);
+        }
+        tc_wait_ld();
+        tc_fence_before();
+        warp_arrive(&bar.dp_free);
+        if (next && lane == 0) mbar_arrive(smem_u32(&bar.s_free));
+        const int left = keys - (rank + it * ranks) * kT - half * 64;
+        if (__any_sync(0xffffffffu, left < 64)) {       // replaces P and dP: whatever lies there is not used
+#pragma unroll
+          for (int e = 0; e < 64; ++e)
+            if (e >= left) { p[e] = 0.0f; u[e >> 5][e & 31] = 0u; }
+        }
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float2 d = mul2(make_float2(p[e], p[e + 1]), add2(two(u, e), dd));
+          x[e / 2] = pack(d.x, d.y);
+          const float2 y = fma2(two(v, e), aa, ll), t = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
+          p[e] = t.x;
+          p[e + 1] = t.y;
+        }
+        if (n > 1) {               // the place of dS is free when its last product is over
+          if (!(ok = tc_wait(&bar.dq_done[n & 1], parity(n - 2, 2), deadline))) break;
+          tc_fence_after();
+        }
+        tc_store32(lanes + F::ds + (n & 1) * 64 + half * 32, x);
+        tc_wait_st();
+        tc_fence_before();
+        warp_arrive(&bar.ds_ready);
+      }
+      if (!ok) break;
+      bf16 *dst = dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h;
+      if (k.total > 0 && !(ok = tc_wait(&bar.dq_done[(n - 1) & 1], parity(n - 1, 2), deadline))) break;
+      tc_fence_after();
+      if (ranks > 1 || k.total > 0) {
+        // the two groups of warps bring out half of the head dimensions each, through the tiles of Q and dO
+        uint8_t *tile = base + (ranks > 1 ? 0 : qn % F::q_ring * 2) * F::tile;
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+          const int col = (half * NP + c) * 32;
+          uint32_t v[32] = {}, u[16];
+          if (k.total > 0) {
+            tc_load32(lanes + F::dq + col, v);
+            tc_wait_ld();
+          }
+          if (ranks > 1) {
+            keep_sums<NP>(tile, row, col, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(v[2 * e]) * z.scale, __uint_as_float(v[2 * e + 1]) * z.scale) : 0u;
+            stage_row<NP>(tile, row, col, u);
+          }
+        }
+        tc_fence_before();
+        if (ranks == 1) {
+          warp_arrive(&bar.acc_free);
+          asm volatile("bar.sync 1, 256;" ::: "memory");
+          write_rows<NP>(tile, (warp & 3) * 32 + half * 16, 16, w.at, z.tq, z, dst, dq.t);
+          tc_proxy_fence();
+          warp_arrive(&bar.q_empty[qn % F::q_ring]);
+          ++qn;
+        }
+      } else {
+        write_zeros<NP>((warp & 3) * 32 + half * 16, 16, w.at, z.tq, z, dst, dq.t);
       }
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (ranks == 1 && half == 0)
-      write_rows<NP>(base, (warp & 3) * 32, i0, z.tq, z, dq.p + (long long)b * dq.b + (long long)h * dq.h, dq.t);
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
-  if (ranks > 1) {
+  if (ranks > 1) {             // one block to a cluster
     cluster_sync();
-    if (warp < 8)
-      join_sums<NP>(sq, ranks, rank, threadIdx.x, 256, i0, z.tq, lq, z, z.scale, dq.p + (long long)b * dq.b + (long long)h * dq.h, dq.t);
+    if (warp < 8) {
+      const Block w = block_of(blockIdx.x / ranks, z.heads, columns, blocks, kT, z.causal);
+      join_sums<NP>(s0, ranks, rank, threadIdx.x, 256, w.at, z.tq, used(z.q_lens, w.b, z.tq), z, z.scale,
+                    dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h, dq.t);
+    }
     cluster_sync();
   }
 }
@@ -1075,18 +1296,27 @@ int forward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtens
             const View &o, float *lse, cudaStream_t st) {
   static CdgPerDevice flags;
   if (!raise_limit(flags, attn_forward<NP>, Fwd<NP>::smem)) return CDGRAB_ERR_CUDA;
-  return cdg_launch_rc(cdg_ops_launch(attn_forward<NP>, dim3(s->heads * s->batch, (s->len_q + 2 * kT - 1) / (2 * kT)), kFwdThreads,
-                                      Fwd<NP>::smem, st, mq, mk, mv, z, o, lse));
+  const int blocks = (s->len_q + 2 * kT - 1) / (2 * kT);
+  const long long all = (long long)s->heads * s->batch * blocks;
+  if (all > 0x7fffffffll) return CDGRAB_ERR_INVALID;
+  return cdg_launch_rc(cdg_ops_launch(attn_forward<NP>, dim3((unsigned)all), kFwdThreads, Fwd<NP>::smem, st, mq, mk, mv,
+                                      z, blocks, o, lse));
 }
 
-// CTAs that share the loop of one tile of rows.  `longest` and `mean` are the turns of the loop for the
-// longest tile and on average, `tiles` the number of tiles: a loop is dealt out while the longest one
-// takes more than half of what every SM gets (so that the last CTAs to finish leave few SMs idle) and at
-// least two turns are left to each CTA.
-int split_of(double longest, double mean, double tiles, int sms) {
-  int c = 1;
-  while (c < 8 && longest / c > 0.5 * mean * tiles / sms && longest / (2 * c) >= 2.0) c *= 2;
-  return c;
+// CTAs that share the loop of one block of rows: the number for which the estimated time, in turns of a
+// loop, is least.  `longest` and `mean` are the turns of the longest block and on average, `all` the number of
+// blocks.  A cluster sets up and joins anew for each block, which costs some four turns, a single CTA about
+// two in all.  (dk and dv of one sequence of 4096, 16 query heads over 4, causal, us at 1, 2, 4 CTAs: 210, 116,
+// 161; of 3 x 257 keys, 6 heads over 2: 23, 20, 19; dq there: 139, 161, 282 and 12, 13, 25.)
+int split_of(double longest, double mean, long long all, int sms) {
+  int best = 1;
+  double least = 0.0;
+  for (int c = 1; c <= 8 && (c == 1 || longest / c >= 1.0); c *= 2) {
+    const double rounds = ceil((double)all * c / sms);
+    const double turns = fmax(longest / c, rounds * mean / c) + (c > 1 ? 4.0 * rounds : 2.0);
+    if (c == 1 || turns < least) { best = c; least = turns; }
+  }
+  return best;
 }
 template <typename... KArgs, typename... Args>
 int launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, Args... args) {
@@ -1112,14 +1342,17 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
   const int qt = (s->len_q + kT - 1) / kT, kt = (s->len_kv + kT - 1) / kT;
   const double part = s->causal ? 0.5 : 1.0;
   if (kt > 0) {
-    const int c = split_of((double)qt * z.group, part * qt * z.group, (double)kt * s->kv_heads * s->batch, sms);
-    rc = launch_cluster(attn_backward_kv<NP>, dim3(s->kv_heads * s->batch * c, kt), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z,
-                        lines, padded, dk, dv);
+    const long long all = (long long)kt * s->kv_heads * s->batch;
+    if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
+    const int c = split_of((double)qt * z.group, part * qt * z.group, all, sms);
+    rc = launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
+                        dk, dv);
   }
   if (rc == CDGRAB_OK && qt > 0) {
-    const int c = split_of(kt, part * kt, (double)qt * s->heads * s->batch, sms);
-    rc = launch_cluster(attn_backward_q<NP>, dim3(s->heads * s->batch * c, qt), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, lines,
-                        padded, dq);
+    const long long all = (long long)qt * s->heads * s->batch;
+    if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
+    const int c = split_of(kt, part * kt, all, sms);
+    rc = launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
   }
   return rc;
 }
