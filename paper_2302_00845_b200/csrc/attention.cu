@@ -39,6 +39,8 @@ struct View { bf16 *p; long long b, t, h; };
 enum { kQ = 1, kK = 2, kV = 4, kDo = 8 };
 __device__ __forceinline__ int batch_of(const Sizes &z, int which, int b) { return z.shared & which ? 0 : b; }
 __device__ __forceinline__ int used(const int *lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
+// (the special function units do 16 a cycle and SM, 1024 cycles for a tile of 128 x 128; a quarter of them as
+// polynomials on the FMA units made no kernel here faster)
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 // two fp32 operations to an instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -60,31 +62,7 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-// 2^x for two values on the FMA units: x = n + f, |f| <= 1/2, a polynomial of degree 5 for 2^f (a weighted
-// least-squares fit of its relative error, 1.6e-7 at most), and n added to the exponent.  Below -126 the
-// result is about 1e-38 instead of 0.
-__device__ __forceinline__ float2 exp2_pair(float2 x) {
-  const float2 magic = make_float2(12582912.0f, 12582912.0f);      // 1.5 x 2^23: the sum's last bits are n
-  x.x = fmaxf(x.x, -126.0f);
-  x.y = fmaxf(x.y, -126.0f);
-  const float2 t = add2(x, magic);
-  const float2 f = fma2(add2(t, make_float2(-12582912.0f, -12582912.0f)), make_float2(-1.0f, -1.0f), x);
-  float2 r = make_float2(0.0013276375830173492f, 0.0013276375830173492f);
-  r = fma2(r, f, make_float2(0.009675533510744572f, 0.009675533510744572f));
-  r = fma2(r, f, make_float2(0.05550713464617729f, 0.05550713464617729f));
-  r = fma2(r, f, make_float2(0.24022120237350464f, 0.24022120237350464f));
-  r = fma2(r, f, make_float2(0.6931469440460205f, 0.6931469440460205f));
-  r = fma2(r, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
-  r.x = __uint_as_float(__float_as_uint(r.x) + (__float_as_uint(t.x) << 23));
-  r.y = __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(t.y) << 23));
-  return r;
-}
-// The exponentials are spread over both kinds of units: the special function units do 16 a cycle and SM,
-// which bounds a tile of 128 x 128 at 1024 cycles; every fourth pair goes to the FMA units instead.
-template <bool FMA> __device__ __forceinline__ float2 exp2_two(float2 x) {
-  if (FMA) return exp2_pair(x);
-  return make_float2(exp2_fast(x.x), exp2_fast(x.y));
-}
+__device__ __forceinline__ float2 exp2_two(float2 x) { return make_float2(exp2_fast(x.x), exp2_fast(x.y)); }
 __device__ __forceinline__ float2 two(const uint32_t (&v)[2][32], int e) {
   return make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1]));
 }
@@ -250,7 +228,7 @@ template <int NP> struct Fwd {
 template <int NP> struct FwdBars {
   Queue queue;
   uint64_t q_full[Fwd<NP>::q_ring], q_empty[Fwd<NP>::q_ring], k_full[Fwd<NP>::ring], k_empty[Fwd<NP>::ring], v_full[Fwd<NP>::ring],
-      v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2];
+      v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2], turn[2];
   uint32_t tmem;
 };
 
@@ -275,7 +253,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&bar.s_full[t]), 1); mbar_init(smem_u32(&bar.s_free[t]), 4);
       mbar_init(smem_u32(&bar.p_ready[t]), 4); mbar_init(smem_u32(&bar.pv_done[t]), 1);
-      mbar_init(smem_u32(&bar.o_free[t]), 4);
+      mbar_init(smem_u32(&bar.o_free[t]), 4); mbar_init(smem_u32(&bar.turn[t]), 4);
     }
     mbar_init_fence();
   }
@@ -418,7 +396,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     const uint32_t ts = tm + lanes + t * kT, tp = tm + lanes + F::p + t * F::p_step, to = tm + lanes + F::o + t * F::o_step;
     const float a = z.a;
     bool ok = true;
-    int qn = 0, sn = 0;                  // blocks, and score tiles of this half
+    int qn = 0, sn = 0, gn = 0;          // blocks, score tiles of this half, and turns of both halves
     int seq = 0;
     for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next(bar.queue, seq++, deadline, ok)) {
       const Block w = block(at);
@@ -426,7 +404,18 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       const int mine = t == 0 ? k.n[0] : k.n[1], i = w.at + t * kT + row;
       const int keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;     // this row sees keys 0 .. keys - 1
       float ref = -INFINITY, sum = 0.0f;
-      for (int j = 0; j < mine; ++j, ++sn) {
+      for (int j = 0; j < k.tiles; ++j, ++gn) {
+        // Above 64 head dimensions the two halves take turns at the exponentials, so that one's fall into the
+        // other's products (2 x 4096, 16/4 heads of 128, ragged: 300 -> 273 us; at 64 dimensions the exponentials
+        // are the longer part and turns cost 58 -> 62 us).  A half that does not see the tile passes its turn on,
+        // so that both count the same turns.
+        auto my_turn = [&]() { return t == 0 ? gn == 0 || tc_wait(&bar.turn[1], (gn - 1) & 1, deadline) : tc_wait(&bar.turn[0], gn & 1, deadline); };
+        if (j >= mine) {
+          if (NP == 1) break;
+          if (!(ok = my_turn())) break;
+          warp_arrive(&bar.turn[t]);
+          continue;
+        }
         if (!(ok = tc_wait(&bar.s_full[t], sn & 1, deadline))) break;
         tc_fence_after();
         uint32_t v[4][32];
@@ -462,8 +451,8 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         const float factor = raise ? exp2_fast((ref - mx) * a) : 1.0f;
         if (raise) { ref = mx; sum *= factor; }
         const float shift = ref == -INFINITY ? 0.0f : -ref * a;
-        if (j > 0 && !(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
         if (j > 0 && __any_sync(0xffffffffu, raise)) {
+          if (!(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
           tc_fence_after();
 #pragma unroll
           for (int c = 0; c < 2 * NP; ++c) {
@@ -475,24 +464,28 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             tc_store32(to + c * 32, u);
           }
         }
+        if (NP == 2 && !(ok = my_turn())) break;
         float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        uint32_t u[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          uint32_t u[32];
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) {
-            const float2 x = fma2(make_float2(__uint_as_float(v[c + (e >> 5)][e & 31]), __uint_as_float(v[c + (e >> 5)][(e & 31) + 1])),
-                                  make_float2(a, a), make_float2(shift, shift));
-            const float2 p = (e & 6) == 0 ? exp2_two<true>(x) : exp2_two<false>(x);
-            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
-            u[e >> 1] = pack(p.x, p.y);
-          }
-          tc_store32(tp + c * 16, u);
+        for (int e = 0; e < 128; e += 2) {
+          const float2 x = fma2(make_float2(__uint_as_float(v[e >> 5][e & 31]), __uint_as_float(v[e >> 5][(e & 31) + 1])),
+                                make_float2(a, a), make_float2(shift, shift));
+          const float2 p = exp2_two(x);
+          part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
+          u[e >> 6][(e >> 1) & 31] = pack(p.x, p.y);
         }
+        if (NP == 2) warp_arrive(&bar.turn[t]);
+        // P's place is free when its last product is over (above 64 head dimensions S came after that)
+        if (NP == 1 && j > 0 && !(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
+        tc_fence_after();
+        tc_store32(tp, u[0]);
+        tc_store32(tp + 32, u[1]);
         sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         tc_wait_st();
         tc_fence_before();
         warp_arrive(&bar.p_ready[t]);
+        ++sn;
       }
       if (!ok) break;
       bf16 *dst = o.p + (long long)w.b * o.b + (long long)w.h * o.h;
@@ -845,10 +838,10 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
 #pragma unroll
         for (int e = 0; e < 64; e += 8) {
           const float4 l = *reinterpret_cast<const float4 *>(l2 + e), m = *reinterpret_cast<const float4 *>(l2 + e + 4);
-          const float2 x0 = exp2_two<true>(fma2(two(v, e), aa, make_float2(l.x, l.y)));
-          const float2 x1 = exp2_two<false>(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
-          const float2 x2 = exp2_two<false>(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
-          const float2 x3 = exp2_two<false>(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
+          const float2 x0 = exp2_two(fma2(two(v, e), aa, make_float2(l.x, l.y)));
+          const float2 x1 = exp2_two(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
+          const float2 x2 = exp2_two(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
+          const float2 x3 = exp2_two(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
           p[e] = x0.x; p[e + 1] = x0.y; p[e + 2] = x1.x; p[e + 3] = x1.y;
           p[e + 4] = x2.x; p[e + 5] = x2.y; p[e + 6] = x3.x; p[e + 7] = x3.y;
         }
@@ -1138,7 +1131,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         warp_arrive(&bar.s_free);
 #pragma unroll
         for (int e = 0; e < 64; e += 2) {
-          const float2 y = fma2(two(v, e), aa, ll), x = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
+          const float2 y = fma2(two(v, e), aa, ll), x = exp2_two(y);
           p[e] = x.x;
           p[e + 1] = x.y;
         }
@@ -1168,7 +1161,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         for (int e = 0; e < 64; e += 2) {
           const float2 d = mul2(make_float2(p[e], p[e + 1]), add2(two(u, e), dd));
           x[e / 2] = pack(d.x, d.y);
-          const float2 y = fma2(two(v, e), aa, ll), t = (e & 6) == 0 ? exp2_two<true>(y) : exp2_two<false>(y);
+          const float2 y = fma2(two(v, e), aa, ll), t = exp2_two(y);
           p[e] = t.x;
           p[e + 1] = t.y;
         }

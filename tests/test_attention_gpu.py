@@ -113,6 +113,18 @@ def test_long_and_few_padded():
     check(q, k, v, do, q_lens=ql, kv_lens=kl)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("tq,tk,d", [(520, 520, 64), (400, 700, 128), (700, 300, 64)])
+def test_more_blocks_than_multiprocessors(tq, tk, d, causal):
+    """Every SM takes several blocks of rows, of unequal lengths and some empty, one after another."""
+    b, h = 9, 12
+    ql, kl = [tq - 71 * i for i in range(b)], [tk - 30 * ((3 * i) % b) for i in range(b)]
+    ql = [max(0, t) for t in ql]
+    args = draw(b, tq, tk, h, h // 2, d)
+    check(*args, causal=causal)
+    check(*args, causal=causal, q_lens=ql, kv_lens=kl)
+
+
 def test_only_some_lengths_given():
     q, k, v, do = draw(2, 100, 260, 2, 2, 64)
     check(q, k, v, do, kv_lens=[70, 260])
