@@ -148,64 +148,12 @@ __device__ __forceinline__ void write_zeros(int row0, int rows, int token0, int 
 // overlap, and the hardware still deals the blocks out as SMs become free, longest loops first.  One block
 // to a CTA spent half of its 18,600 cycles outside the loop at 1024 tokens and 64 dimensions.
 // Counters of turns and stages therefore run on over the blocks, and so do the barriers' phases: turn n of a
-// ring of R uses stage n % R in the phase of parity(n, R).
-struct Queue { uint4 answer[2]; uint64_t full[2], empty[2]; };       // in shared memory: the next block, one ahead
-constexpr int kQueueReaders = 11;                                    // warps that follow the blocks
-__device__ __forceinline__ void queue_init(Queue &q) {
-  for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&q.full[i]), 1); mbar_init(smem_u32(&q.empty[i]), kQueueReaders); }
-}
+// ring of R uses stage n % R in the phase of tc_parity(n, R).
 struct Block { int at, h, b; };         // first row, head, sequence
 __device__ __forceinline__ Block block_of(long long w, int heads, int columns, int blocks, int rows, bool last_first) {
   const int c = (int)(w % columns), k = (int)(w / columns);
   return Block{(last_first ? blocks - 1 - k : k) * rows, c % heads, c / heads};
 }
-__device__ __forceinline__ uint32_t parity(int n, int ring) { return (uint32_t)(n / ring) & 1u; }
-// waits for the stage of turn n to have been released by turn n - ring (one thread)
-__device__ __forceinline__ bool wait_released(uint64_t *empty, int n, int ring, long long deadline) {
-  return n < ring || mbar_wait(smem_u32(&empty[n % ring]), parity(n - ring, ring), deadline);
-}
-// after a failure: the copies in flight have to land before the CTA gives up its shared memory
-__device__ __forceinline__ void drain(uint64_t *full, int n, int ring) {
-  for (int i = max(0, n - ring); i < n; ++i) mbar_wait(smem_u32(&full[i % ring]), parity(i, ring), clock64() + kCdgWaitCycles);
-}
-// asks for block number `seq` of this CTA (one thread)
-__device__ __forceinline__ bool queue_ask(Queue &q, int seq, long long deadline) {
-  const int s = seq & 1;
-  if (!wait_released(q.empty, seq, 2, deadline)) return false;
-  mbar_expect_tx(smem_u32(&q.full[s]), 16);
-  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
-               ::"r"(smem_u32(&q.answer[s])), "r"(smem_u32(&q.full[s])) : "memory");
-  return true;
-}
-// ... and reads the answer: the block, or -1 when none is left
-__device__ __forceinline__ long long queue_answer(Queue &q, int seq) {
-  uint32_t got, x;
-  asm volatile(
-      "{\n.reg .b128 h;\n.reg .pred p;\nld.shared.b128 h, [%2];\n"
-      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
-      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, h;\n}"
-      : "=r"(got), "=r"(x) : "r"(smem_u32(&q.answer[seq & 1])) : "memory");
-  tc_proxy_fence();              // the next answer may be written once this one has been read
-  return got ? (long long)x : -1;
-}
-__device__ __forceinline__ long long queue_next(Queue &q, int seq, long long deadline, bool &ok) {        // a whole warp
-  if (!(ok = ok && tc_wait(&q.full[seq & 1], parity(seq, 2), deadline))) return -1;
-  const long long at = queue_answer(q, seq);
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&q.empty[seq & 1]));
-  return at;
-}
-__device__ __forceinline__ long long queue_next_one(Queue &q, int seq, long long deadline, bool &ok) {    // one thread
-  if (!(ok = ok && mbar_wait(smem_u32(&q.full[seq & 1]), parity(seq, 2), deadline))) return -1;
-  const long long at = queue_answer(q, seq);
-  mbar_arrive(smem_u32(&q.empty[seq & 1]));
-  return at;
-}
-__device__ __forceinline__ void warp_arrive(uint64_t *bar) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(bar));
-}
-
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per 256 queries of a head: two tiles of 128 that share every key and value tile, so that while
 // one tile's four warps are at their exponentials the other's products run.
@@ -226,7 +174,7 @@ template <int NP> struct Fwd {
   static constexpr uint32_t o = 256, p = NP == 1 ? 384 : 0, o_step = NP == 1 ? 64 : 128, p_step = NP == 1 ? 64 : 128;
 };
 template <int NP> struct FwdBars {
-  Queue queue;
+  TcQueue queue;
   uint64_t q_full[Fwd<NP>::q_ring], q_empty[Fwd<NP>::q_ring], k_full[Fwd<NP>::ring], k_empty[Fwd<NP>::ring], v_full[Fwd<NP>::ring],
       v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2], turn[2];
   uint32_t tmem;
@@ -244,7 +192,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
   const uint32_t sq = smem_u32(base), sk = sq + F::k, sv = sq + F::v;
 
   if (threadIdx.x == 0) {
-    queue_init(bar.queue);
+    tc_queue_init(bar.queue, 11);
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 8); }
     for (int i = 0; i < F::ring; ++i) {
       mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 2);
@@ -291,13 +239,13 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         bool ok = true;
         int qn = 0, kn = 0, vn = 0;        // blocks and tiles issued
         int seq = 0;
-        for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next_one(bar.queue, seq++, deadline, ok)) {
-          if (!(ok = queue_ask(bar.queue, seq, deadline))) break;
+        for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+          if (!(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.tiles == 0) continue;
           const int hk = w.h / z.group;
-          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          if (!(ok = tc_wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
           uint64_t *full = &bar.q_full[qn % F::q_ring];
           const uint32_t q = sq + qn % F::q_ring * 2 * F::tile;
           mbar_expect_tx(smem_u32(full), 2 * F::tile);
@@ -306,14 +254,14 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
           ++qn;
           for (int j = 0; j <= k.tiles; ++j) {         // K runs one tile ahead of V
             if (j < k.tiles) {
-              if (!(ok = wait_released(bar.k_empty, kn, F::ring, deadline))) break;
+              if (!(ok = tc_wait_released(bar.k_empty, kn, F::ring, deadline))) break;
               full = &bar.k_full[kn % F::ring];
               mbar_expect_tx(smem_u32(full), F::tile);
               load_tile<NP>(sk + kn % F::ring * F::tile, &mk, j * kT, hk, batch_of(z, kK, w.b), smem_u32(full));
               ++kn;
             }
             if (j > 0) {
-              if (!(ok = wait_released(bar.v_empty, vn, F::ring, deadline))) break;
+              if (!(ok = tc_wait_released(bar.v_empty, vn, F::ring, deadline))) break;
               full = &bar.v_full[vn % F::ring];
               mbar_expect_tx(smem_u32(full), F::tile);
               load_tile<NP>(sv + vn % F::ring * F::tile, &mv, (j - 1) * kT, hk, batch_of(z, kV, w.b), smem_u32(full));
@@ -323,10 +271,10 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         }
         if (!ok) {
           atomicOr(z.status, CDG_ST_TIMEOUT);
-          drain(bar.queue.full, seq + 1, 2);
-          drain(bar.q_full, qn, F::q_ring);
-          drain(bar.k_full, kn, F::ring);
-          drain(bar.v_full, vn, F::ring);
+          tc_drain(bar.queue.full, seq + 1, 2);
+          tc_drain(bar.q_full, qn, F::q_ring);
+          tc_drain(bar.k_full, kn, F::ring);
+          tc_drain(bar.v_full, vn, F::ring);
         }
       }
     } else if (warp < 11) {
@@ -335,7 +283,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       bool ok = true;
       int qn = 0, kn = 0, vn = 0, sn = 0, pn = 0, on = 0;      // blocks, tiles of K and V, products S_t and P_t V, blocks with any
       int seq = 0;
-      for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next(bar.queue, seq++, deadline, ok)) {
+      for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.tiles == 0) continue;
@@ -344,7 +292,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         // S_t of key tile j; the stage of K is released when both tiles have used it (or have no use for it)
         auto scores = [&](int j) {
           const int ks = kn % F::ring;
-          if (!tc_wait(&bar.k_full[ks], parity(kn, F::ring), deadline)) return false;
+          if (!tc_wait(&bar.k_full[ks], tc_parity(kn, F::ring), deadline)) return false;
           ++kn;
           // up to 64 head dimensions: the one before is in registers; above, P_t lies over it, and its product is over
           if (j < mine && sn > 0 && !tc_wait(NP == 1 ? &bar.s_free[t] : &bar.pv_done[t], (sn - 1) & 1, deadline)) return false;
@@ -360,11 +308,11 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
           sn += j < mine;
           return true;
         };
-        if (!(ok = tc_wait(&bar.q_full[qn % F::q_ring], parity(qn, F::q_ring), deadline) && scores(0))) break;
+        if (!(ok = tc_wait(&bar.q_full[qn % F::q_ring], tc_parity(qn, F::q_ring), deadline) && scores(0))) break;
         for (int j = 0; j < k.tiles; ++j) {
           const int vs = vn % F::ring;
           if (NP == 1 && j + 1 < k.tiles && !(ok = scores(j + 1))) break;
-          if (!(ok = tc_wait(&bar.v_full[vs], parity(vn, F::ring), deadline))) break;
+          if (!(ok = tc_wait(&bar.v_full[vs], tc_parity(vn, F::ring), deadline))) break;
           ++vn;
           // (both warps zero the rows past the sequence, each before its own product)
           if (z.kv_lens && (j + 1) * kT > k.lk) zero_rows<NP>(base + F::v + vs * F::tile, k.lk - j * kT);
@@ -398,7 +346,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     bool ok = true;
     int qn = 0, sn = 0, gn = 0;          // blocks, score tiles of this half, and turns of both halves
     int seq = 0;
-    for (long long at = blockIdx.x; at >= 0 && ok; at = queue_next(bar.queue, seq++, deadline, ok)) {
+    for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
       const Block w = block(at);
       const Work k = work_of(w);
       const int mine = t == 0 ? k.n[0] : k.n[1], i = w.at + t * kT + row;
@@ -413,7 +361,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         if (j >= mine) {
           if (NP == 1) break;
           if (!(ok = my_turn())) break;
-          warp_arrive(&bar.turn[t]);
+          tc_warp_arrive(&bar.turn[t]);
           continue;
         }
         if (!(ok = tc_wait(&bar.s_full[t], sn & 1, deadline))) break;
@@ -424,7 +372,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         tc_wait_ld();
         if (NP == 1) {
           tc_fence_before();
-          warp_arrive(&bar.s_free[t]);
+          tc_warp_arrive(&bar.s_free[t]);
         }
         if (z.negative) {
 #pragma unroll
@@ -475,7 +423,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
           part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], p);
           u[e >> 6][(e >> 1) & 31] = pack(p.x, p.y);
         }
-        if (NP == 2) warp_arrive(&bar.turn[t]);
+        if (NP == 2) tc_warp_arrive(&bar.turn[t]);
         // P's place is free when its last product is over (above 64 head dimensions S came after that)
         if (NP == 1 && j > 0 && !(ok = tc_wait(&bar.pv_done[t], (sn - 1) & 1, deadline))) break;
         tc_fence_after();
@@ -484,7 +432,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         tc_wait_st();
         tc_fence_before();
-        warp_arrive(&bar.p_ready[t]);
+        tc_warp_arrive(&bar.p_ready[t]);
         ++sn;
       }
       if (!ok) break;
@@ -505,7 +453,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
           for (int e = 0; e < 16; ++e) u[c][e] = keys > 0 ? pack(__uint_as_float(v[2 * e]) * inv, __uint_as_float(v[2 * e + 1]) * inv) : 0u;
         }
         tc_fence_before();
-        warp_arrive(&bar.o_free[t]);
+        tc_warp_arrive(&bar.o_free[t]);
 #pragma unroll
         for (int c = 0; c < 2 * NP; ++c) stage_row<NP>(tile, row, c * 32, u[c]);
         __syncwarp();
@@ -517,7 +465,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         lse[((long long)w.b * z.heads + w.h) * z.tq + i] = keys > 0 ? fmaf(ref, a * kLn2, logf(sum)) : -INFINITY;
       if (k.tiles > 0) {
         tc_proxy_fence();                // the next copy into the tile comes after these reads
-        warp_arrive(&bar.q_empty[qn % F::q_ring]);
+        tc_warp_arrive(&bar.q_empty[qn % F::q_ring]);
         ++qn;
       }
     }
@@ -585,18 +533,6 @@ constexpr int kBwdThreads = 352;
 
 // Where there are few tiles of rows, the loop over the other axis is dealt out over a cluster of CTAs, whose
 // fp32 sums are joined through distributed shared memory, in the order of their ranks.
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float4 peer_load(uint32_t addr, uint32_t rank) {
-  uint32_t there;
-  float4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
-  return v;
-}
 // fp32 sums of a tile in shared memory, [128][DP] with 16-byte pieces permuted by row, so that neither a row
 // per thread nor a row per warp meets bank conflicts
 template <int NP> __device__ __forceinline__ uint32_t sum_at(int row, int piece) {
@@ -619,7 +555,7 @@ __device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, in
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
     if (token < used_tokens)
       for (int k = 0; k < ranks; ++k) {
-        const float4 u = peer_load(sums + sum_at<NP>(r, 2 * chunk), k), v = peer_load(sums + sum_at<NP>(r, 2 * chunk + 1), k);
+        const float4 u = tc_peer_load(sums + sum_at<NP>(r, 2 * chunk), k), v = tc_peer_load(sums + sum_at<NP>(r, 2 * chunk + 1), k);
         a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
         b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
       }
@@ -645,7 +581,7 @@ template <int NP> struct Dkv {
   static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
 };
 template <int NP> struct DkvBars {
-  Queue queue;
+  TcQueue queue;
   uint64_t kv_full[Dkv<NP>::kv_ring], kv_empty[Dkv<NP>::kv_ring], q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring],
       do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, dp_full, dp_free, p_ready, ds_ready,
       done, acc_free;
@@ -664,10 +600,10 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t s0 = smem_u32(base), sq = s0 + F::q, sdo = s0 + F::d_o;
   float *sline = reinterpret_cast<float *>(base + F::lines);      // [ring][2][128]
-  const int ranks = (int)cluster_size(), rank = (int)cluster_rank(), kv_heads = z.heads / z.group;
+  const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank(), kv_heads = z.heads / z.group;
 
   if (threadIdx.x == 0) {
-    queue_init(bar.queue);
+    tc_queue_init(bar.queue, 11);
     for (int i = 0; i < F::kv_ring; ++i) { mbar_init(smem_u32(&bar.kv_full[i]), 1); mbar_init(smem_u32(&bar.kv_empty[i]), 8); }
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
     for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 2); }
@@ -710,12 +646,12 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       bool ok = true;
       int cn = 0, qn = 0, dn = 0, ln = 0;
       int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next_one(bar.queue, seq++, deadline, ok)) {
-if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
-        if (!(ok = wait_released(bar.kv_empty, cn, F::kv_ring, deadline))) break;
+        if (!(ok = tc_wait_released(bar.kv_empty, cn, F::kv_ring, deadline))) break;
         uint64_t *full = &bar.kv_full[cn % F::kv_ring];
         const uint32_t kv = s0 + cn % F::kv_ring * 2 * F::tile;
         mbar_expect_tx(smem_u32(full), 2 * F::tile);
@@ -724,12 +660,12 @@ if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
         ++cn;
         for (int it = 0; it < k.total; ++it) {
           const int h = w.h * z.group + (rank + it * ranks) / k.per, i0 = query0(k, it);
-          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          if (!(ok = tc_wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
           full = &bar.q_full[qn % F::q_ring];
           mbar_expect_tx(smem_u32(full), F::tile);
           load_tile<NP>(sq + qn % F::q_ring * F::tile, &mq, i0, h, batch_of(z, kQ, w.b), smem_u32(full));
           ++qn;
-          if (!(ok = wait_released(bar.line_empty, ln, F::line_ring, deadline))) break;
+          if (!(ok = tc_wait_released(bar.line_empty, ln, F::line_ring, deadline))) break;
           full = &bar.line_full[ln % F::line_ring];
           const float *line = lines + ((long long)w.b * z.heads + h) * 2 * padded + i0;
           float *to = sline + ln % F::line_ring * 2 * kT;
@@ -737,7 +673,7 @@ if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
           load_line(smem_u32(to), line, smem_u32(full));
           load_line(smem_u32(to + kT), line + padded, smem_u32(full));
           ++ln;
-          if (!(ok = wait_released(bar.do_empty, dn, F::do_ring, deadline))) break;
+          if (!(ok = tc_wait_released(bar.do_empty, dn, F::do_ring, deadline))) break;
           full = &bar.do_full[dn % F::do_ring];
           mbar_expect_tx(smem_u32(full), F::tile);
           load_tile<NP>(sdo + dn % F::do_ring * F::tile, &mdo, i0, h, batch_of(z, kDo, w.b), smem_u32(full));
@@ -746,31 +682,31 @@ if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
       }
       if (!ok) {
         atomicOr(z.status, CDG_ST_TIMEOUT);
-        if (ranks == 1) drain(bar.queue.full, seq + 1, 2);
-        drain(bar.kv_full, cn, F::kv_ring);
-        drain(bar.q_full, qn, F::q_ring);
-        drain(bar.line_full, ln, F::line_ring);
-        drain(bar.do_full, dn, F::do_ring);
+        if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
+        tc_drain(bar.kv_full, cn, F::kv_ring);
+        tc_drain(bar.q_full, qn, F::q_ring);
+        tc_drain(bar.line_full, ln, F::line_ring);
+        tc_drain(bar.do_full, dn, F::do_ring);
       }
     }
   } else if (warp >= 9) {
     bool ok = true;
     int cn = 0, n = 0;                   // blocks and turns
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
       const Block w = block(at);
       const Work k = work_of(w);
       if (k.total == 0) continue;
       // a tile has landed; its rows past the sequence's queries are zeroed (by either warp, each before its own product)
       auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
         const int s = n % ring, left = k.lq - query0(k, it);
-        if (!tc_wait(&full[s], parity(n, ring), deadline)) return false;
+        if (!tc_wait(&full[s], tc_parity(n, ring), deadline)) return false;
         if (z.q_lens && left < kT) zero_rows<NP>(base + tiles + s * F::tile, left);
         return true;
       };
       const uint32_t sk = s0 + cn % F::kv_ring * 2 * F::tile, sv = sk + F::tile;
       if (warp == 9) {
-        if (!(ok = tc_wait(&bar.kv_full[cn % F::kv_ring], parity(cn, F::kv_ring), deadline))) break;
+        if (!(ok = tc_wait(&bar.kv_full[cn % F::kv_ring], tc_parity(cn, F::kv_ring), deadline))) break;
         for (int it = 0; it < k.total; ++it, ++n) {
           if (!(ok = arrived(bar.q_full, F::q, F::q_ring, it) && (n == 0 || tc_wait(&bar.dp_free, (n - 1) & 1, deadline)))) break;
           tc_fence_after();
@@ -820,7 +756,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
     bool ok = true;
     int cn = 0, n = 0;
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
       const Block w = block(at);
       const Work k = work_of(w);
       const int j = w.at + row, off = k.lk - k.lq;
@@ -828,7 +764,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         const int ls = n % F::line_ring, i0 = query0(k, it) + half * 64;
         const uint32_t here = mine + (n & 1) * kT, there = mine + (~n & 1) * kT;
         const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
-        if (!(ok = tc_wait(&bar.line_full[ls], parity(n, F::line_ring), deadline) && tc_wait(&bar.s_full, n & 1, deadline))) break;
+        if (!(ok = tc_wait(&bar.line_full[ls], tc_parity(n, F::line_ring), deadline) && tc_wait(&bar.s_full, n & 1, deadline))) break;
         tc_fence_after();
         uint32_t v[2][32], u[32];
         tc_load32(here, v[0]);
@@ -857,14 +793,14 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         tc_store32(here, u);
         tc_wait_st();
         tc_fence_before();
-        warp_arrive(&bar.p_ready);
+        tc_warp_arrive(&bar.p_ready);
         if (!(ok = tc_wait(&bar.dp_full, n & 1, deadline))) break;
         tc_fence_after();
         tc_load32(there, v[0]);
         tc_load32(there + 32, v[1]);
         tc_wait_ld();
         tc_fence_before();
-        warp_arrive(&bar.dp_free);
+        tc_warp_arrive(&bar.dp_free);
 #pragma unroll
         for (int e = 0; e < 64; e += 4) {
           const float4 d = *reinterpret_cast<const float4 *>(delta + e);
@@ -876,7 +812,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         tc_store32(here + 32, u);
         tc_wait_st();
         tc_fence_before();
-        warp_arrive(&bar.ds_ready);
+        tc_warp_arrive(&bar.ds_ready);
         if (lane == 0) mbar_arrive(smem_u32(&bar.line_empty[ls]));
       }
       if (!ok) break;
@@ -909,7 +845,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
           if (lane == 0) mbar_arrive(smem_u32(&bar.acc_free));
           write_rows<NP>(tile, (warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
           tc_proxy_fence();              // the next copy into the tile comes after these reads
-          warp_arrive(&bar.kv_empty[cn % F::kv_ring]);
+          tc_warp_arrive(&bar.kv_empty[cn % F::kv_ring]);
           ++cn;
         }
       } else {
@@ -922,7 +858,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
   if (ranks > 1) {             // one block to a cluster
-    cluster_sync();
+    tc_cluster_sync();
     if (warp < 8) {
       const int half = warp >> 2;
       const View &out = half ? dk : dv;
@@ -930,7 +866,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
       join_sums<NP>(s0 + half * 2 * F::tile, ranks, rank, threadIdx.x & 127, 128, w.at, z.tk, used(z.kv_lens, w.b, z.tk), z,
                     half ? z.scale : 1.0f, out.p + (long long)w.b * out.b + (long long)w.h * out.h, out.t);
     }
-    cluster_sync();            // no CTA leaves while another reads its sums
+    tc_cluster_sync();            // no CTA leaves while another reads its sums
   }
 }
 
@@ -948,7 +884,7 @@ template <int NP> struct Dq {
   static constexpr uint32_t dq = 256, ds = 384;
 };
 template <int NP> struct DqBars {
-  Queue queue;
+  TcQueue queue;
   uint64_t q_full[Dq<NP>::q_ring], q_empty[Dq<NP>::q_ring], k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring],
       v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready, dq_done[2], acc_free;
   uint32_t tmem;
@@ -965,10 +901,10 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   DqBars<NP> &bar = *reinterpret_cast<DqBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t s0 = smem_u32(base), sk = s0 + F::k, sv = s0 + F::v;
-  const int ranks = (int)cluster_size(), rank = (int)cluster_rank();
+  const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank();
 
   if (threadIdx.x == 0) {
-    queue_init(bar.queue);
+    tc_queue_init(bar.queue, 11);
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 8); }
     for (int i = 0; i < F::k_ring; ++i) { mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 1); }
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
@@ -1008,13 +944,13 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         bool ok = true;
         int qn = 0, kn = 0, vn = 0;
         int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next_one(bar.queue, seq++, deadline, ok)) {
-if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.total == 0) continue;
           const int hk = w.h / z.group;
-          if (!(ok = wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+          if (!(ok = tc_wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
           uint64_t *full = &bar.q_full[qn % F::q_ring];
           const uint32_t q = s0 + qn % F::q_ring * 2 * F::tile;
           mbar_expect_tx(smem_u32(full), 2 * F::tile);
@@ -1023,12 +959,12 @@ if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
           ++qn;
           for (int it = 0; it < k.total; ++it) {
             const int j0 = (rank + it * ranks) * kT;
-            if (!(ok = wait_released(bar.k_empty, kn, F::k_ring, deadline))) break;
+            if (!(ok = tc_wait_released(bar.k_empty, kn, F::k_ring, deadline))) break;
             full = &bar.k_full[kn % F::k_ring];
             mbar_expect_tx(smem_u32(full), F::tile);
             load_tile<NP>(sk + kn % F::k_ring * F::tile, &mk, j0, hk, batch_of(z, kK, w.b), smem_u32(full));
             ++kn;
-            if (!(ok = wait_released(bar.v_empty, vn, F::v_ring, deadline))) break;
+            if (!(ok = tc_wait_released(bar.v_empty, vn, F::v_ring, deadline))) break;
             full = &bar.v_full[vn % F::v_ring];
             mbar_expect_tx(smem_u32(full), F::tile);
             load_tile<NP>(sv + vn % F::v_ring * F::tile, &mv, j0, hk, batch_of(z, kV, w.b), smem_u32(full));
@@ -1037,17 +973,17 @@ if (ranks == 1 && !(ok = queue_ask(bar.queue, seq, deadline))) break;
         }
         if (!ok) {
           atomicOr(z.status, CDG_ST_TIMEOUT);
-          if (ranks == 1) drain(bar.queue.full, seq + 1, 2);
-          drain(bar.q_full, qn, F::q_ring);
-          drain(bar.k_full, kn, F::k_ring);
-          drain(bar.v_full, vn, F::v_ring);
+          if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
+          tc_drain(bar.q_full, qn, F::q_ring);
+          tc_drain(bar.k_full, kn, F::k_ring);
+          tc_drain(bar.v_full, vn, F::v_ring);
         }
       }
     } else if (warp < 11) {
       bool ok = true;
       int qn = 0, n = 0;                 // blocks, and turns whose S (warp 9) or dq (warp 10) has been issued
       int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
@@ -1055,7 +991,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         if (warp == 9) {
           auto scores = [&](int it) {    // S of tile it: K has landed, its rows past the sequence are zeroed, the S before is in registers
             const int s = n % F::k_ring, left = k.lk - (rank + it * ranks) * kT;
-            if (!tc_wait(&bar.k_full[s], parity(n, F::k_ring), deadline)) return false;
+            if (!tc_wait(&bar.k_full[s], tc_parity(n, F::k_ring), deadline)) return false;
             if (z.kv_lens && left < kT) zero_rows<NP>(base + F::k + s * F::tile, left);
             if (n > 0 && !tc_wait(&bar.s_free, (n - 1) & 1, deadline)) return false;
             tc_fence_after();
@@ -1069,7 +1005,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
           };
           auto gradients = [&](int m) {  // dP of turn m likewise
             const int s = m % F::v_ring;
-            if (!tc_wait(&bar.v_full[s], parity(m, F::v_ring), deadline) || (m > 0 && !tc_wait(&bar.dp_free, (m - 1) & 1, deadline))) return false;
+            if (!tc_wait(&bar.v_full[s], tc_parity(m, F::v_ring), deadline) || (m > 0 && !tc_wait(&bar.dp_free, (m - 1) & 1, deadline))) return false;
             tc_fence_after();
             if (tc_elect()) {
               mma_scores<NP>(tm + kT, q + F::tile, sv + s * F::tile);
@@ -1079,7 +1015,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
             __syncwarp();
             return true;
           };
-          ok = tc_wait(&bar.q_full[qn % F::q_ring], parity(qn, F::q_ring), deadline) && scores(0);
+          ok = tc_wait(&bar.q_full[qn % F::q_ring], tc_parity(qn, F::q_ring), deadline) && scores(0);
           for (int it = 0; it < k.total && ok; ++it) ok = gradients(n - 1) && (it + 1 == k.total || scores(it + 1));
           if (!ok) break;
         } else {
@@ -1109,7 +1045,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
     bool ok = true;
     int qn = 0, n = 0;
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.queue, seq++, deadline, ok)) {
+for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
       const Block w = block(at);
       const Work k = work_of(w);
       const int i = w.at + row, keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;
@@ -1128,7 +1064,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         tc_load32(ts + 32, v[1]);
         tc_wait_ld();
         tc_fence_before();
-        warp_arrive(&bar.s_free);
+        tc_warp_arrive(&bar.s_free);
 #pragma unroll
         for (int e = 0; e < 64; e += 2) {
           const float2 y = fma2(two(v, e), aa, ll), x = exp2_two(y);
@@ -1149,7 +1085,7 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         }
         tc_wait_ld();
         tc_fence_before();
-        warp_arrive(&bar.dp_free);
+        tc_warp_arrive(&bar.dp_free);
         if (next && lane == 0) mbar_arrive(smem_u32(&bar.s_free));
         const int left = keys - (rank + it * ranks) * kT - half * 64;
         if (__any_sync(0xffffffffu, left < 64)) {       // replaces P and dP: whatever lies there is not used
@@ -1166,17 +1102,17 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
           p[e + 1] = t.y;
         }
         if (n > 1) {               // the place of dS is free when its last product is over
-          if (!(ok = tc_wait(&bar.dq_done[n & 1], parity(n - 2, 2), deadline))) break;
+          if (!(ok = tc_wait(&bar.dq_done[n & 1], tc_parity(n - 2, 2), deadline))) break;
           tc_fence_after();
         }
         tc_store32(lanes + F::ds + (n & 1) * 64 + half * 32, x);
         tc_wait_st();
         tc_fence_before();
-        warp_arrive(&bar.ds_ready);
+        tc_warp_arrive(&bar.ds_ready);
       }
       if (!ok) break;
       bf16 *dst = dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h;
-      if (k.total > 0 && !(ok = tc_wait(&bar.dq_done[(n - 1) & 1], parity(n - 1, 2), deadline))) break;
+      if (k.total > 0 && !(ok = tc_wait(&bar.dq_done[(n - 1) & 1], tc_parity(n - 1, 2), deadline))) break;
       tc_fence_after();
       if (ranks > 1 || k.total > 0) {
         // the two groups of warps bring out half of the head dimensions each, through the tiles of Q and dO
@@ -1199,11 +1135,11 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
         }
         tc_fence_before();
         if (ranks == 1) {
-          warp_arrive(&bar.acc_free);
+          tc_warp_arrive(&bar.acc_free);
           asm volatile("bar.sync 1, 256;" ::: "memory");
           write_rows<NP>(tile, (warp & 3) * 32 + half * 16, 16, w.at, z.tq, z, dst, dq.t);
           tc_proxy_fence();
-          warp_arrive(&bar.q_empty[qn % F::q_ring]);
+          tc_warp_arrive(&bar.q_empty[qn % F::q_ring]);
           ++qn;
         }
       } else {
@@ -1216,13 +1152,13 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : queue_next(bar.q
   __syncthreads();
   if (warp == 9) { tc_fence_after(); tc_free(tm, 512); }
   if (ranks > 1) {             // one block to a cluster
-    cluster_sync();
+    tc_cluster_sync();
     if (warp < 8) {
       const Block w = block_of(blockIdx.x / ranks, z.heads, columns, blocks, kT, z.causal);
       join_sums<NP>(s0, ranks, rank, threadIdx.x, 256, w.at, z.tq, used(z.q_lens, w.b, z.tq), z, z.scale,
                     dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h, dq.t);
     }
-    cluster_sync();
+    tc_cluster_sync();
   }
 }
 
@@ -1278,17 +1214,11 @@ bool map_of(CUtensorMap *m, const void *p, const long long s[3], int batch, int 
   const long long strides[4] = {1, s[1] > 0 ? s[1] : 64, s[2] > 0 ? s[2] : 64, s[0] > 0 ? s[0] : 64};
   return tc_encode(m, true, p, 4, dims, strides, kT);
 }
-template <typename K>
-bool raise_limit(CdgPerDevice &flags, K *kernel, size_t bytes) {
-  int dev = 0;
-  return cudaGetDevice(&dev) == cudaSuccess && cdg_raise_smem_limit(flags, dev, kernel, bytes) == cudaSuccess;
-}
-
 template <int NP>
 int forward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const Sizes &z,
             const View &o, float *lse, cudaStream_t st) {
   static CdgPerDevice flags;
-  if (!raise_limit(flags, attn_forward<NP>, Fwd<NP>::smem)) return CDGRAB_ERR_CUDA;
+  if (!tc_raise_limit(flags, attn_forward<NP>, Fwd<NP>::smem)) return CDGRAB_ERR_CUDA;
   const int blocks = (s->len_q + 2 * kT - 1) / (2 * kT);
   const long long all = (long long)s->heads * s->batch * blocks;
   if (all > 0x7fffffffll) return CDGRAB_ERR_INVALID;
@@ -1311,26 +1241,11 @@ int split_of(double longest, double mean, long long all, int sms) {
   }
   return best;
 }
-template <typename... KArgs, typename... Args>
-int launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cdg_launch_rc(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
-}
-
 template <int NP>
 int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mdo,
              const Sizes &z, const float *lines, int padded, const View &dq, const View &dk, const View &dv, int sms, cudaStream_t st) {
   static CdgPerDevice kf, qf;
-  if (!raise_limit(kf, attn_backward_kv<NP>, Dkv<NP>::smem) || !raise_limit(qf, attn_backward_q<NP>, Dq<NP>::smem)) return CDGRAB_ERR_CUDA;
+  if (!tc_raise_limit(kf, attn_backward_kv<NP>, Dkv<NP>::smem) || !tc_raise_limit(qf, attn_backward_q<NP>, Dq<NP>::smem)) return CDGRAB_ERR_CUDA;
   int rc = CDGRAB_OK;
   const int qt = (s->len_q + kT - 1) / kT, kt = (s->len_kv + kT - 1) / kT;
   const double part = s->causal ? 0.5 : 1.0;
@@ -1338,14 +1253,14 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
     const long long all = (long long)kt * s->kv_heads * s->batch;
     if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of((double)qt * z.group, part * qt * z.group, all, sms);
-    rc = launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
+    rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
                         dk, dv);
   }
   if (rc == CDGRAB_OK && qt > 0) {
     const long long all = (long long)qt * s->heads * s->batch;
     if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of(kt, part * kt, all, sms);
-    rc = launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
+    rc = tc_launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
   }
   return rc;
 }

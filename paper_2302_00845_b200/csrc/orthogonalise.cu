@@ -25,16 +25,25 @@ constexpr float kScale = 256.0f;
 constexpr int kNormBlocks = 128;
 
 // ---- |G|_F ----------------------------------------------------------------------------------
-template <typename T>
+// VEC values to a load: 16 bytes where rows, stride and address allow it, else one
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_sumsq(const T *g, long long gb, long long gs, int rows, int cols,
                                                   double *part) {
+  struct __align__(sizeof(T) * VEC) Piece { T v[VEC]; };
   __shared__ double sm[8];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const T *p = g + blockIdx.y * gb;
+  const int per = cols / VEC;
+  const long long all = (long long)rows * per, step = (long long)gridDim.x * 256;
   double s = 0.0;       // squares in 64 bits: entries of 1e-18 and 1e18 are taken as they are
-  for (int r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < cols; c += 256) { const double v = cdg_ld(p + r * gs + c); s += v * v; }
+#pragma unroll 4
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
+    const long long r = i / per;
+    const Piece q = *reinterpret_cast<const Piece *>(p + r * gs + (i - r * per) * VEC);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { const double v = cdg_ld(&q.v[e]); s = fma(v, v, s); }
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = s;
@@ -45,14 +54,23 @@ __global__ void __launch_bounds__(256) orth_sumsq(const T *g, long long gb, long
   }
 }
 
-// x[m][ldx] = kScale G (or its transpose) / (norm + eps), tiles of 64 x 64 through shared memory
-template <typename T>
+// x[m][ldx] = kScale G (or its transpose) / (norm + eps), a tile of 64 x 64 to a block
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_start(const T *g, long long gb, long long gs, int rows, int cols, int tall,
                                                   const double *part, float eps, __half *x, int ldx, long long xb) {
+  struct __align__(sizeof(T) * VEC) Piece { T v[VEC]; };
+  struct __align__(2 * VEC) Half { __half v[VEC]; };
   __shared__ double sm[4];
-  __shared__ float tile[64][65];
+  __shared__ __half tile[64][66];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
+  constexpr int per = 64 / VEC, lines = 256 / per;        // loads to a row of the tile, rows at a time
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tx = threadIdx.x % per * VEC, ty = threadIdx.x / per;
+  const T *p = g + blockIdx.z * gb;
+  Piece q[64 / lines];
+#pragma unroll
+  for (int i = 0; i < 64 / lines; ++i)
+    if (r0 + ty + i * lines < rows && c0 + tx < cols) q[i] = *reinterpret_cast<const Piece *>(p + (r0 + ty + i * lines) * gs + c0 + tx);
   if (threadIdx.x < kNormBlocks) {
     double t = part[blockIdx.z * kNormBlocks + threadIdx.x];
 #pragma unroll
@@ -60,37 +78,49 @@ __global__ void __launch_bounds__(256) orth_start(const T *g, long long gb, long
     if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = t;
   }
   __syncthreads();
-  const double f = (double)kScale / (sqrt(sm[0] + sm[1] + sm[2] + sm[3]) + (double)eps);
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  const T *p = g + blockIdx.z * gb;
-  for (int i = ty; i < 64; i += 4)
-    if (r0 + i < rows && c0 + tx < cols) tile[i][tx] = (float)(f * (double)cdg_ld(p + (r0 + i) * gs + c0 + tx));
-  __syncthreads();
-  __half *q = x + blockIdx.z * xb;
-  for (int i = ty; i < 64; i += 4) {
+  const double norm = sqrt(sm[0] + sm[1] + sm[2] + sm[3]) + (double)eps;
+  const float f = norm > 0.0 ? (float)fmin((double)kScale / norm, 3e38) : 0.0f;
+  __half *out = x + blockIdx.z * xb;
+#pragma unroll
+  for (int i = 0; i < 64 / lines; ++i) {
+    const int r = ty + i * lines;
+    if (r0 + r >= rows || c0 + tx >= cols) continue;
+    Half h;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) h.v[e] = __float2half_rn(f * cdg_ld(&q[i].v[e]));
     if (tall) {
-      if (c0 + i < cols && r0 + tx < rows) q[(long long)(c0 + i) * ldx + r0 + tx] = __float2half_rn(tile[tx][i]);
-    } else if (r0 + i < rows && c0 + tx < cols) {
-      q[(long long)(r0 + i) * ldx + c0 + tx] = __float2half_rn(tile[i][tx]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) tile[tx + e][r] = h.v[e];
+    } else if (VEC == 1 || ldx % VEC == 0) {
+      *reinterpret_cast<Half *>(out + (long long)(r0 + r) * ldx + c0 + tx) = h;
     }
+  }
+  if (!tall) return;
+  __syncthreads();
+  // rows of x are columns of G: pairs of halves, whole 128-byte lines
+  for (int i = threadIdx.x; i < 64 * 32; i += 256) {
+    const int r = i >> 5, c = (i & 31) * 2;
+    if (c0 + r >= cols) continue;
+    __half *to = out + (long long)(c0 + r) * ldx + r0 + c;
+    if (r0 + c + 1 < rows) *reinterpret_cast<__half2 *>(to) = *reinterpret_cast<const __half2 *>(&tile[r][c]);
+    else if (r0 + c < rows) *to = tile[r][c];
   }
 }
 
 // ---- the products ----------------------------------------------------------------------------
-// One CTA per 128 x 128 tile of C = A op(B): warp 0 keeps a ring of kStages shared-memory stages full
-// (64 of K each), warp 1 issues the matrix instructions, then all four warps read the accumulator
-// (128 columns of tensor memory) and write the tile through shared memory in whole rows.  A CTA takes
-// 100 KB, so two share an SM and one's copies and epilogue run under the other's products.
-constexpr int kTile = 128, kK = 64, kStages = 3;
-constexpr uint32_t kOperandBytes = kTile * kK * 2, kStageBytes = 2 * kOperandBytes;
-constexpr int kPitch = kTile + 8;        // halves per staged row: 16-byte accesses of eight rows hit all banks
-constexpr size_t kProductSmem = kStages * kStageBytes + 1024;
-static_assert(2 * kTile * kPitch * 2 <= kStages * kStageBytes, "the staged tiles reuse the ring");
-
+// Persistent CTAs, one to an SM, take tiles of C = A op(B), 128 rows by BN columns: warp 0 keeps a ring of
+// shared-memory stages full (64 of K each), warp 1 issues the matrix instructions, warps 2 to 5 read the
+// accumulator, of which there are two in tensor memory so that one tile's products run under the other's
+// epilogue, and write it through shared memory in whole rows.
+// BN = 256 where there are tiles enough: a 128 x 128 product reads its operands from shared memory at the
+// full 128 bytes a cycle, one of 128 x 256 at three quarters of that.
+// Where there are few tiles, the K loop is dealt out over a cluster and the fp32 sums joined through
+// distributed shared memory in the order of the ranks.
+constexpr int kM = 128, kK = 64, kThreads = 192;
 enum Product { kGram, kPoly, kApply, kLast };   // A = X X^T; B = aI + bA + cAA; X = B X; the same into O
 
 struct ProductArgs {
-  int m, n, k;             // C is m x n
+  int m, n, k, tiles;      // C is m x n; tiles of one matrix
   float alpha, beta, diag; // C = alpha acc + beta D + diag I
   const __half *D;         // kPoly: A
   void *C;
@@ -100,180 +130,285 @@ struct ProductArgs {
   int *status;
 };
 
+template <int P, int BN> struct Shape {
+  static constexpr bool symmetric = P == kGram || P == kPoly;
+  static constexpr uint32_t a_bytes = kM * kK * 2, stage = a_bytes + BN * kK * 2;
+  static constexpr int ring = BN == 256 ? 4 : symmetric ? 5 : 6;
+  // per epilogue warp: rows of 64 halves (both halves of the tile's columns where a tile of D is fetched
+  // ahead), and a transposed piece of 64 rows of 32
+  static constexpr int row_pitch = 72, col_pitch = 40;
+  static constexpr uint32_t rows_bytes = 32 * row_pitch * 2, cols_bytes = 64 * col_pitch * 2;
+  static constexpr uint32_t cols_at = P == kPoly ? 2 * rows_bytes : P == kGram ? rows_bytes : 0;      // (O is written one way or the other)
+  static constexpr uint32_t warp_bytes = cols_at + cols_bytes;
+  static constexpr uint32_t staging = ring * stage, bars = staging + 4 * warp_bytes;
+  static constexpr size_t smem = bars + 256;
+};
+template <int P, int BN> struct Bars {
+  TcQueue queue;
+  uint64_t full[Shape<P, BN>::ring], empty[Shape<P, BN>::ring], acc_full[2], acc_empty[2];
+  uint32_t tmem;
+};
+
+__device__ __forceinline__ uint32_t sum_at(int row, int piece) {        // fp32 [128][128], 16-byte pieces permuted by row
+  return (uint32_t)(row * 512 + (((piece & ~7) | ((piece ^ row) & 7)) << 4));
+}
 template <int P>
-__global__ void __launch_bounds__(128) orth_product(const __grid_constant__ CUtensorMap ta,
-                                                    const __grid_constant__ CUtensorMap tb, const ProductArgs p) {
-  extern __shared__ uint8_t raw[];
-  __shared__ __align__(8) uint64_t full[kStages], empty[kStages], done;
-  __shared__ uint32_t tmem_slot;
-  constexpr bool symmetric = P == kGram || P == kPoly;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, z = blockIdx.y;
-  const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u;
-  int ti, tj;
-  if (symmetric) {         // tiles (ti, tj), ti <= tj, counted column by column
-    tj = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-    while ((tj + 1) * (tj + 2) / 2 <= (int)blockIdx.x) ++tj;
-    while (tj * (tj + 1) / 2 > (int)blockIdx.x) --tj;
-    ti = blockIdx.x - tj * (tj + 1) / 2;
-  } else {
-    const int nt = (p.m + kTile - 1) / kTile;
-    ti = blockIdx.x % nt;
-    tj = blockIdx.x / nt;
+__device__ __forceinline__ uint32_t finish(float x, float y, float dx, float dy, int i, int j, const ProductArgs &p) {
+  x *= p.alpha;
+  y *= p.alpha;
+  if (P == kPoly) {
+    x = fmaf(p.beta, dx, x) + (i == j ? p.diag : 0.0f);
+    y = fmaf(p.beta, dy, y) + (i == j + 1 ? p.diag : 0.0f);
   }
-  const int i0 = ti * kTile, j0 = tj * kTile, nk = (p.k + kK - 1) / kK;
+  if (P == kLast) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+  }
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+// `rows` rows of 8 * pieces halves from shared memory (pitch in halves) to C at (r0, c0), a whole warp; the
+// workspace's rows are padded to multiples of 8 values, so whole pieces are written there
+__device__ __forceinline__ void put(const __half *from, int pitch, int rows, int pieces, __half *C, long long ldc, int r0, int c0,
+                                    int nr, int nc, bool padded, bool vec) {
+  const int lane = threadIdx.x & 31;
+  if (vec) {
+    for (int i = lane; i < rows * pieces; i += 32) {
+      const int r = i / pieces, c = i % pieces * 8;
+      if (r0 + r >= nr || c0 + c >= nc) continue;
+      __half *to = C + (long long)(r0 + r) * ldc + c0 + c;
+      if (padded || c0 + c + 8 <= nc) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from + r * pitch + c);
+      else for (int e = 0; e < nc - c0 - c; ++e) to[e] = from[r * pitch + c + e];
+    }
+  } else {
+    for (int i = lane; i < rows * pieces * 8; i += 32) {
+      const int r = i / (pieces * 8), c = i % (pieces * 8);
+      if (r0 + r < nr && c0 + c < nc) C[(long long)(r0 + r) * ldc + c0 + c] = from[r * pitch + c];
+    }
+  }
+}
+
+template <int P, int BN>
+__global__ void __launch_bounds__(kThreads, 1) orth_product(const __grid_constant__ CUtensorMap ta,
+                                                            const __grid_constant__ CUtensorMap tb, const ProductArgs p) {
+  typedef Shape<P, BN> S;
+  extern __shared__ __align__(1024) uint8_t base[];
+  static_assert(sizeof(Bars<P, BN>) <= 256 && S::smem <= 232448, "");
+  Bars<P, BN> &bar = *reinterpret_cast<Bars<P, BN> *>(base + S::bars);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t ring = smem_u32(base);
+  const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank();
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
-    mbar_init(smem_u32(&done), 1);
+    tc_queue_init(bar.queue, 6);
+    for (int s = 0; s < S::ring; ++s) { mbar_init(smem_u32(&bar.full[s]), 1); mbar_init(smem_u32(&bar.empty[s]), 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bar.acc_full[s]), 1); mbar_init(smem_u32(&bar.acc_empty[s]), 4); }
     mbar_init_fence();
   }
-  if (warp == 1) tc_alloc(&tmem_slot, kTile);
+  if (warp == 1) tc_alloc(&bar.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t acc = tmem_slot;
+  const uint32_t acc = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const long long deadline = clock64() + kCdgWaitCycles;
+  const int nk = ((p.k + kK - 1) / kK - rank + ranks - 1) / ranks;       // this CTA's steps of K: rank, rank + ranks, ...
+
+  struct Tile { int i0, j0, z; };
+  auto tile_of = [&](long long at) {
+    const int z = (int)(at / p.tiles), t = (int)(at % p.tiles);
+    int ti, tj;
+    if (S::symmetric) {      // tiles (ti, tj), ti <= tj, counted column by column
+      tj = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+      while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
+      while (tj * (tj + 1) / 2 > t) --tj;
+      ti = t - tj * (tj + 1) / 2;
+    } else {
+      const int nt = (p.m + kM - 1) / kM;
+      ti = t % nt;
+      tj = t / nt;
+    }
+    return Tile{ti * kM, tj * BN, z};
+  };
+  const long long first = blockIdx.x / ranks;      // a cluster takes one tile and asks for no more
 
   if (warp == 0) {
     if (tc_elect()) {
-      int it = 0;
       bool ok = true;
-      for (; it < nk; ++it) {
-        const int s = it % kStages;
-        if (it >= kStages && !(ok = mbar_wait(smem_u32(&empty[s]), (it / kStages - 1) & 1, deadline))) break;
-        const uint32_t bar = smem_u32(&full[s]), a = ring + s * kStageBytes, b = a + kOperandBytes;
-        mbar_expect_tx(bar, kStageBytes);
-        tma_load_3d(a, &ta, it * kK, i0, z, bar);
-        if (P == kGram || P == kPoly) {
-          tma_load_3d(b, &tb, it * kK, j0, z, bar);
-        } else {          // two panels of 64 columns, 64 rows of K
-          tma_load_3d(b, &tb, j0, it * kK, z, bar);
-          tma_load_3d(b + kOperandBytes / 2, &tb, j0 + 64, it * kK, z, bar);
+      int n = 0, seq = 0;
+      for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+        if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+        const Tile t = tile_of(at);
+        for (int it = 0; it < nk; ++it, ++n) {
+          if (!(ok = tc_wait_released(bar.empty, n, S::ring, deadline))) break;
+          const uint32_t full = smem_u32(&bar.full[n % S::ring]), a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
+          const int k0 = (rank + it * ranks) * kK;
+          mbar_expect_tx(full, S::stage);
+          tma_load_3d(a, &ta, k0, t.i0, t.z, full);
+          if (S::symmetric) {
+            tma_load_3d(b, &tb, k0, t.j0, t.z, full);
+          } else {           // panels of 64 columns, 64 rows of K
+#pragma unroll
+            for (int c = 0; c < BN / 64; ++c) tma_load_3d(b + c * kK * 128, &tb, t.j0 + c * 64, k0, t.z, full);
+          }
         }
       }
-      if (!ok) {          // let the copies in flight land before the CTA gives up its shared memory
+      if (!ok) {
         atomicOr(p.status, CDG_ST_TIMEOUT);
-        for (int i = max(0, it - kStages); i < it; ++i)
-          mbar_wait(smem_u32(&full[i % kStages]), (i / kStages) & 1, clock64() + kCdgWaitCycles);
+        if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
+        tc_drain(bar.full, n, S::ring);
       }
     }
   } else if (warp == 1) {
-    constexpr uint32_t idesc = tc_idesc(false, kTile, kTile, false, !symmetric);
+    constexpr uint32_t idesc = tc_idesc(false, kM, BN, false, !S::symmetric);
     bool ok = true;
-    for (int it = 0; it < nk; ++it) {
-      const int s = it % kStages;
-      if (!(ok = tc_wait(&full[s], (it / kStages) & 1, deadline))) break;
-      tc_fence_after();
-      const uint32_t a = ring + s * kStageBytes, b = a + kOperandBytes;
-      const uint64_t da = tc_desc_k(a), db = symmetric ? tc_desc_k(b) : tc_desc_mn(b, kOperandBytes / 2);
-      if (tc_elect()) {
+    int n = 0, seq = 0;
+    for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      const uint32_t d = acc + (seq & 1) * BN;
+      if (seq >= 2 && !(ok = tc_wait(&bar.acc_empty[seq & 1], tc_parity(seq - 2, 2), deadline))) break;
+      for (int it = 0; it < nk; ++it, ++n) {
+        if (!(ok = tc_wait(&bar.full[n % S::ring], tc_parity(n, S::ring), deadline))) break;
+        tc_fence_after();
+        const uint32_t a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
+        const uint64_t da = tc_desc_k(a), db = S::symmetric ? tc_desc_k(b) : tc_desc_mn(b, kK * 128);
+        if (tc_elect()) {
 #pragma unroll
-        for (int kk = 0; kk < kK / 16; ++kk)
-          tc_mma(acc, da + kk * 2, db + kk * (symmetric ? 2 : 128), idesc, it > 0 || kk > 0);
-        tc_commit(&empty[s]);
+          for (int kk = 0; kk < kK / 16; ++kk) tc_mma(d, da + kk * 2, db + kk * (S::symmetric ? 2 : 128), idesc, it > 0 || kk > 0);
+          tc_commit(&bar.empty[n % S::ring]);
+        }
+        __syncwarp();
       }
+      if (!ok) break;
+      if (tc_elect()) tc_commit(&bar.acc_full[seq & 1]);
       __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
-    if (tc_elect()) tc_commit(&done);
-    __syncwarp();
-  }
-  __syncwarp();
-
-  // ---- epilogue: warp w holds rows 32 w ... of the tile
-  const bool ok = mbar_wait(smem_u32(&done), 0, deadline + kCdgWaitCycles);
-  if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
-  tc_fence_after();
-  __syncthreads();            // no thread writes into the ring before all have seen the products end
-  typedef __nv_bfloat16 bf16;
-  __half *rows = reinterpret_cast<__half *>(raw + (ring - smem_u32(raw)));      // [128][kPitch]
-  __half *cols = rows + kTile * kPitch;                                         // the transposed tile
-  const int r = warp * 32 + lane;
-  if (P == kPoly) {           // the tile of A that is added
-    const __half *D = p.D + z * p.db;
+  } else {
+    const int w = warp & 3, r = w * 32 + lane;         // warp w of the four reads lanes 32 w ... of the accumulator
+    __half *rows = reinterpret_cast<__half *>(base + S::staging + w * S::warp_bytes);
+    __half *cols = rows + S::cols_at / 2;
+    bool ok = true;
+    int seq = 0;
+    for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      const Tile t = tile_of(at);
+      __half *C = static_cast<__half *>(p.C) + t.z * p.cb;
+      if (P == kPoly && ranks == 1) {      // the tile of A that is added, while the products run
+        const __half *D = p.D + t.z * p.db;
 #pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-      const int rr = warp * 32 + 2 * i + (lane >> 4), c = (lane & 15) * 8;
-      if (i0 + rr < p.m && j0 + c < p.n)
-        *reinterpret_cast<uint4 *>(rows + rr * kPitch + c) = *reinterpret_cast<const uint4 *>(D + (long long)(i0 + rr) * p.ldc + j0 + c);
-    }
-    __syncwarp();
-  }
-  const bool mirror = (symmetric && ti != tj) || (P == kLast && p.tall);
-#pragma unroll
-  for (int c0 = 0; c0 < kTile; c0 += 32) {
-    uint32_t v[32];
-    tc_load32(acc + ((uint32_t)(warp * 32) << 16) + c0, v);
-    tc_wait_ld();
-#pragma unroll
-    for (int c = 0; c < 32; c += 8) {
-      uint4 out;
-      uint32_t *o = &out.x;
-      if (P == kPoly) out = *reinterpret_cast<const uint4 *>(rows + r * kPitch + c0 + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float2 f = make_float2(__uint_as_float(v[c + 2 * e]) * p.alpha, __uint_as_float(v[c + 2 * e + 1]) * p.alpha);
-        if (P == kPoly) {
-          const float2 d = __half22float2(*reinterpret_cast<const __half2 *>(&o[e]));
-          f.x += p.beta * d.x;
-          f.y += p.beta * d.y;
-          if (i0 + r == j0 + c0 + c + 2 * e) f.x += p.diag;
-          if (i0 + r == j0 + c0 + c + 2 * e + 1) f.y += p.diag;
+        for (int i = lane; i < 32 * 16; i += 32) {
+          const int rr = i >> 4, c = (i & 15) * 8;
+          if (t.i0 + w * 32 + rr < p.m && t.j0 + c < p.n)
+            *reinterpret_cast<uint4 *>(rows + ((c >> 6) * 32 + rr) * S::row_pitch + (c & 63)) =
+                *reinterpret_cast<const uint4 *>(D + (long long)(t.i0 + w * 32 + rr) * p.ldc + t.j0 + c);
         }
-        if (P == kLast) {
-          const __nv_bfloat162 h = __float22bfloat162_rn(f);
-          o[e] = *reinterpret_cast<const uint32_t *>(&h);
-        } else {
-          const __half2 h = __float22half2_rn(f);
-          o[e] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        if (mirror) {
-          reinterpret_cast<uint16_t *>(cols)[(c0 + c + 2 * e) * kPitch + r] = (uint16_t)(o[e] & 0xffffu);
-          reinterpret_cast<uint16_t *>(cols)[(c0 + c + 2 * e + 1) * kPitch + r] = (uint16_t)(o[e] >> 16);
-        }
+        __syncwarp();
       }
-      *reinterpret_cast<uint4 *>(rows + r * kPitch + c0 + c) = out;
+      if (!(ok = tc_wait(&bar.acc_full[seq & 1], tc_parity(seq, 2), deadline))) break;
+      tc_fence_after();
+      const uint32_t d = acc + ((uint32_t)(w * 32) << 16) + (seq & 1) * BN;
+      if (ranks > 1) {
+        // this CTA's sums into the ring, which no copy fills any more
+#pragma unroll
+        for (int c0 = 0; c0 < kM; c0 += 32) {
+          uint32_t v[32] = {};
+          if (nk > 0) { tc_load32(d + c0, v); tc_wait_ld(); }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4 *>(base + sum_at(r, (c0 >> 2) + i)) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+        break;
+      }
+      const bool mirror = S::symmetric && t.i0 != t.j0, turned = P == kLast && p.tall;
+#pragma unroll 1
+      for (int c0 = 0; c0 < BN; c0 += 64) {
+        uint32_t v[2][32];
+        tc_load32(d + c0, v[0]);
+        tc_load32(d + c0 + 32, v[1]);
+        tc_wait_ld();
+        if (c0 + 64 == BN) {               // the accumulator is in registers: the tile after next may use it
+          tc_fence_before();
+          tc_warp_arrive(&bar.acc_empty[seq & 1]);
+        }
+        __half *mine = rows + (P == kPoly ? (c0 >> 6) * 32 * S::row_pitch : 0) + lane * S::row_pitch;
+#pragma unroll
+        for (int c = 0; c < 64; c += 8) {
+          uint32_t o[4], dd[4] = {};
+          if (P == kPoly) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(mine + c);
+            dd[0] = q.x; dd[1] = q.y; dd[2] = q.z; dd[3] = q.w;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&dd[e]));
+            o[e] = finish<P>(__uint_as_float(v[c >> 5][(c & 31) + 2 * e]), __uint_as_float(v[c >> 5][(c & 31) + 2 * e + 1]), f.x, f.y,
+                             t.i0 + r, t.j0 + c0 + c + 2 * e, p);
+            if (mirror || turned) {
+              reinterpret_cast<uint16_t *>(cols)[(c + 2 * e) * S::col_pitch + lane] = (uint16_t)(o[e] & 0xffffu);
+              reinterpret_cast<uint16_t *>(cols)[(c + 2 * e + 1) * S::col_pitch + lane] = (uint16_t)(o[e] >> 16);
+            }
+          }
+          if (!turned) *reinterpret_cast<uint4 *>(mine + c) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        __syncwarp();
+        const int rr = t.i0 + w * 32, cc = t.j0 + c0;
+        if (!turned) put(mine - lane * S::row_pitch, S::row_pitch, 32, 8, C, p.ldc, rr, cc, p.m, p.n, P != kLast, P != kLast || p.vec);
+        if (mirror) put(cols, S::col_pitch, 64, 4, C, p.ldc, cc, rr, p.n, p.m, true, true);
+        if (turned) put(cols, S::col_pitch, 64, 4, C, p.ldc, cc, rr, p.n, p.m, false, p.vec);
+        __syncwarp();
+      }
     }
+    if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) { tc_fence_after(); tc_free(acc, kTile); }
-
-  __half *C = static_cast<__half *>(p.C) + z * p.cb;
-  if (P == kLast) {
-    // O as the caller has it: rows of n (or of m, transposed) values
-    const __half *src = p.tall ? cols : rows;
-    const int ra = p.tall ? j0 : i0, ca = p.tall ? i0 : j0, nr = p.tall ? p.n : p.m, nc = p.tall ? p.m : p.n;
-    if (p.vec) {
-      for (int i = 0; i < 16; ++i) {
-        const int rr = warp * 32 + 2 * i + (lane >> 4), c = (lane & 15) * 8;
-        if (ra + rr >= nr) continue;
-        __half *dst = C + (long long)(ra + rr) * p.ldc + ca + c;
-        if (ca + c + 8 <= nc) {
-          *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(src + rr * kPitch + c);
-        } else {
-          for (int e = 0; e < 8 && ca + c + e < nc; ++e) dst[e] = src[rr * kPitch + c + e];
+  if (warp == 1) { tc_fence_after(); tc_free(acc, 512); }
+  if (ranks > 1) {
+    tc_cluster_sync();
+    // rank's share of the tile's rows: the cluster's sums added up, finished and written
+    const Tile t = tile_of(first);
+    const int share = kM / ranks, r0 = rank * share, e = threadIdx.x - 64;
+    __half *C = static_cast<__half *>(p.C) + t.z * p.cb;
+    __half *out = reinterpret_cast<__half *>(base + kM * 512);          // behind the sums: [share][136]
+    if (e >= 0) {
+      for (int i = e; i < share * 32; i += 128) {
+        const int r = r0 + i / 32, piece = i % 32, c = piece * 4;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < ranks; ++k) {
+          const float4 u = tc_peer_load(ring + sum_at(r, piece), k);
+          s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
         }
+        float2 d0 = make_float2(0.0f, 0.0f), d1 = d0;
+        if (P == kPoly && t.i0 + r < p.m && t.j0 + c < p.n) {
+          const uint2 q = *reinterpret_cast<const uint2 *>(p.D + t.z * p.db + (long long)(t.i0 + r) * p.ldc + t.j0 + c);
+          d0 = __half22float2(*reinterpret_cast<const __half2 *>(&q.x));
+          d1 = __half22float2(*reinterpret_cast<const __half2 *>(&q.y));
+        }
+        *reinterpret_cast<uint2 *>(out + (i / 32) * 136 + c) =
+            make_uint2(finish<P>(s.x, s.y, d0.x, d0.y, t.i0 + r, t.j0 + c, p), finish<P>(s.z, s.w, d1.x, d1.y, t.i0 + r, t.j0 + c + 2, p));
       }
-    } else {
-      for (int i = 0; i < 32; ++i) {
-        const int rr = warp * 32 + i;
-        if (ra + rr >= nr) break;
-        for (int c = lane; c < kTile; c += 32)
-          if (ca + c < nc) C[(long long)(ra + rr) * p.ldc + ca + c] = src[rr * kPitch + c];
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const int w = e >> 5, per = share / 4;
+      if (P == kLast && p.tall) {
+        for (int i = e; i < kM * share; i += 128) {
+          const int c = i / share, r = i % share;
+          if (t.j0 + c < p.n && t.i0 + r0 + r < p.m) C[(long long)(t.j0 + c) * p.ldc + t.i0 + r0 + r] = out[r * 136 + c];
+        }
+      } else {
+        put(out + w * per * 136, 136, per, 16, C, p.ldc, t.i0 + r0 + w * per, t.j0, p.m, p.n, P != kLast, P != kLast || p.vec);
       }
+      if (S::symmetric && t.i0 != t.j0)
+        for (int i = e; i < kM * (share / 8); i += 128) {
+          const int c = i / (share / 8), r = i % (share / 8) * 8;
+          if (t.j0 + c >= p.n || t.i0 + r0 + r >= p.m) continue;
+          uint32_t q[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            q[k] = (uint32_t)__half_as_ushort(out[(r + 2 * k) * 136 + c]) | (uint32_t)__half_as_ushort(out[(r + 2 * k + 1) * 136 + c]) << 16;
+          *reinterpret_cast<uint4 *>(C + (long long)(t.j0 + c) * p.ldc + t.i0 + r0 + r) = make_uint4(q[0], q[1], q[2], q[3]);
+        }
     }
-    return;
-  }
-  // workspace rows are padded to multiples of 8 values: whole 16-byte pieces, the padding is never read
-  for (int i = 0; i < 16; ++i) {
-    const int rr = warp * 32 + 2 * i + (lane >> 4), c = (lane & 15) * 8;
-    if (i0 + rr < p.m && j0 + c < p.n)
-      *reinterpret_cast<uint4 *>(C + (long long)(i0 + rr) * p.ldc + j0 + c) = *reinterpret_cast<const uint4 *>(rows + rr * kPitch + c);
-    if (symmetric && mirror && j0 + rr < p.n && i0 + c < p.m)
-      *reinterpret_cast<uint4 *>(C + (long long)(j0 + rr) * p.ldc + i0 + c) = *reinterpret_cast<const uint4 *>(cols + rr * kPitch + c);
+    tc_cluster_sync();           // no CTA leaves while another reads its sums
   }
 }
 
@@ -299,15 +434,30 @@ Plan plan_of(long long batch, int rows, int cols) {
   return p;
 }
 
-template <int P>
-int product(const CUtensorMap &ta, const CUtensorMap &tb, const ProductArgs &a, int batch, cudaStream_t st) {
+template <int P, int BN>
+int launch(const CUtensorMap &ta, const CUtensorMap &tb, const ProductArgs &a, int batch, int cluster, cudaStream_t st) {
   static CdgPerDevice flags;
-  int dev = 0;
-  cudaGetDevice(&dev);
-  if (cdg_raise_smem_limit(flags, dev, orth_product<P>, kProductSmem) != cudaSuccess) return CDGRAB_ERR_CUDA;
-  const int mt = (a.m + kTile - 1) / kTile, nt = (a.n + kTile - 1) / kTile;
-  const int tiles = P == kGram || P == kPoly ? mt * (mt + 1) / 2 : mt * nt;
-  return cdg_launch_rc(cdg_ops_launch(orth_product<P>, dim3(tiles, batch), 128, kProductSmem, st, ta, tb, a));
+  if (!tc_raise_limit(flags, orth_product<P, BN>, Shape<P, BN>::smem)) return CDGRAB_ERR_CUDA;
+  return tc_launch_cluster(orth_product<P, BN>, dim3((unsigned)(a.tiles * batch * cluster)), cluster, kThreads, Shape<P, BN>::smem, st, ta, tb, a);
+}
+
+template <int P>
+int product(const CUtensorMap &ta, const CUtensorMap &tb, ProductArgs a, int batch, int sms, cudaStream_t st) {
+  const int mt = (a.m + kM - 1) / kM, nt = (a.n + kM - 1) / kM, wide = (a.n + 255) / 256;
+  if (P == kApply || P == kLast) {
+    // tiles of 256 columns while they still give every SM one
+    if ((long long)mt * wide * batch >= sms) {
+      a.tiles = mt * wide;
+      return launch<P, P == kApply || P == kLast ? 256 : 128>(ta, tb, a, batch, 1, st);
+    }
+    a.tiles = mt * nt;
+  } else {
+    a.tiles = mt * (mt + 1) / 2;
+  }
+  // few tiles: as many CTAs to each as fit the SMs and leave two steps of K (64 each) to a CTA
+  int c = 1;
+  while (c < 8 && (long long)a.tiles * batch * 2 * c <= sms && (a.k + kK - 1) / kK >= 4 * c) c *= 2;
+  return launch<P, 128>(ta, tb, a, batch, c, st);
 }
 
 }  // namespace
@@ -343,34 +493,36 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   CUtensorMap tx[2], tk[2], ta, tb;
   const long long dx[3] = {n, m, batch}, sx[3] = {1, p.ldx, xb}, da[3] = {m, m, batch}, sa[3] = {1, p.lda, ab};
   for (int i = 0; i < 2; ++i)
-    if (!tc_encode(&tx[i], false, x[i], 3, dx, sx, kTile) || !tc_encode(&tk[i], false, x[i], 3, dx, sx, kK)) return CDGRAB_ERR_CUDA;
-  if (!tc_encode(&ta, false, A, 3, da, sa, kTile) || !tc_encode(&tb, false, B, 3, da, sa, kTile)) return CDGRAB_ERR_CUDA;
+    if (!tc_encode(&tx[i], false, x[i], 3, dx, sx, kM) || !tc_encode(&tk[i], false, x[i], 3, dx, sx, kK)) return CDGRAB_ERR_CUDA;
+  if (!tc_encode(&ta, false, A, 3, da, sa, kM) || !tc_encode(&tb, false, B, 3, da, sa, kM)) return CDGRAB_ERR_CUDA;
 
   const dim3 gt((cols + 63) / 64, (rows + 63) / 64, batch);
+  const int e = dtype == CDGRAB_F32 ? 4 : 2;
+  const bool wide = cdg_aligned(g, 16) && gs % (16 / e) == 0 && gb % (16 / e) == 0 && cols % (16 / e) == 0;
   int rc;
-  if (dtype == CDGRAB_F32) {
-    rc = cdg_launch_rc(cdg_ops_launch(orth_sumsq<float>, dim3(kNormBlocks, batch), 256, 0, st, (const float *)g, gb, gs, rows, cols, part));
-    if (rc == CDGRAB_OK)
-      rc = cdg_launch_rc(cdg_ops_launch(orth_start<float>, gt, 256, 0, st, (const float *)g, gb, gs, rows, cols, tall, part, eps, x[0], p.ldx, xb));
-  } else {
-    rc = cdg_launch_rc(cdg_ops_launch(orth_sumsq<__nv_bfloat16>, dim3(kNormBlocks, batch), 256, 0, st, (const __nv_bfloat16 *)g, gb, gs, rows, cols, part));
-    if (rc == CDGRAB_OK)
-      rc = cdg_launch_rc(cdg_ops_launch(orth_start<__nv_bfloat16>, gt, 256, 0, st, (const __nv_bfloat16 *)g, gb, gs, rows, cols, tall, part, eps, x[0], p.ldx, xb));
-  }
-  const ProductArgs gram = {m, m, n, 1.0f / (kScale * kScale), 0.0f, 0.0f, nullptr, A, p.lda, ab, 0, 0, 1, dev->status};
-  const ProductArgs poly = {m, m, m, coeffs[2], coeffs[1], coeffs[0], A, B, p.lda, ab, ab, 0, 1, dev->status};
-  const ProductArgs last = {m, n, m, 1.0f / kScale, 0.0f, 0.0f, nullptr, o, (int)os, ob, 0, tall,
+  auto begin = [&](auto *sumsq, auto *start, const auto *from) {
+    const int r = cdg_launch_rc(cdg_ops_launch(sumsq, dim3(kNormBlocks, batch), 256, 0, st, from, gb, gs, rows, cols, part));
+    return r != CDGRAB_OK ? r : cdg_launch_rc(cdg_ops_launch(start, gt, 256, 0, st, from, gb, gs, rows, cols, tall, part, eps, x[0], p.ldx, xb));
+  };
+  if (dtype == CDGRAB_F32)
+    rc = wide ? begin(orth_sumsq<float, 4>, orth_start<float, 4>, (const float *)g) : begin(orth_sumsq<float, 1>, orth_start<float, 1>, (const float *)g);
+  else
+    rc = wide ? begin(orth_sumsq<__nv_bfloat16, 8>, orth_start<__nv_bfloat16, 8>, (const __nv_bfloat16 *)g)
+              : begin(orth_sumsq<__nv_bfloat16, 1>, orth_start<__nv_bfloat16, 1>, (const __nv_bfloat16 *)g);
+  const ProductArgs gram = {m, m, n, 0, 1.0f / (kScale * kScale), 0.0f, 0.0f, nullptr, A, p.lda, ab, 0, 0, 1, dev->status};
+  const ProductArgs poly = {m, m, m, 0, coeffs[2], coeffs[1], coeffs[0], A, B, p.lda, ab, ab, 0, 1, dev->status};
+  const ProductArgs last = {m, n, m, 0, 1.0f / kScale, 0.0f, 0.0f, nullptr, o, (int)os, ob, 0, tall,
                             cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, dev->status};
   for (int i = 0; i < steps && rc == CDGRAB_OK; ++i) {
     const int at = i & 1;
-    rc = product<kGram>(tx[at], tx[at], gram, batch, st);
-    if (rc == CDGRAB_OK) rc = product<kPoly>(ta, ta, poly, batch, st);
+    rc = product<kGram>(tx[at], tx[at], gram, batch, dev->sms, st);
+    if (rc == CDGRAB_OK) rc = product<kPoly>(ta, ta, poly, batch, dev->sms, st);
     if (rc != CDGRAB_OK) break;
     if (i + 1 < steps) {
-      const ProductArgs apply = {m, n, m, 1.0f, 0.0f, 0.0f, nullptr, x[1 - at], p.ldx, xb, 0, 0, 1, dev->status};
-      rc = product<kApply>(tb, tk[at], apply, batch, st);
+      const ProductArgs apply = {m, n, m, 0, 1.0f, 0.0f, 0.0f, nullptr, x[1 - at], p.ldx, xb, 0, 0, 1, dev->status};
+      rc = product<kApply>(tb, tk[at], apply, batch, dev->sms, st);
     } else {
-      rc = product<kLast>(tb, tk[at], last, batch, st);
+      rc = product<kLast>(tb, tk[at], last, batch, dev->sms, st);
     }
   }
   return rc;

@@ -105,6 +105,75 @@ __device__ __forceinline__ void tc_store16(uint32_t addr, const uint32_t (&v)[16
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
 
+// ---- rings, persistent CTAs, clusters -------------------------------------------------------------
+// Turn n of a ring of R stages uses stage n % R in the phase of tc_parity(n, R); counters run on over a
+// persistent CTA's blocks.
+__device__ __forceinline__ uint32_t tc_parity(int n, int ring) { return (uint32_t)(n / ring) & 1u; }
+// waits for the stage of turn n to have been released by turn n - ring (one thread)
+__device__ __forceinline__ bool tc_wait_released(uint64_t *empty, int n, int ring, long long deadline) {
+  return n < ring || mbar_wait(smem_u32(&empty[n % ring]), tc_parity(n - ring, ring), deadline);
+}
+// after a failure: the copies in flight have to land before the CTA gives up its shared memory
+__device__ __forceinline__ void tc_drain(uint64_t *full, int n, int ring) {
+  for (int i = max(0, n - ring); i < n; ++i) mbar_wait(smem_u32(&full[i % ring]), tc_parity(i, ring), clock64() + kCdgWaitCycles);
+}
+// Cluster launch control: a CTA that has finished its block takes over the next CTA of the grid that has
+// not been started.  One answer is fetched ahead; `readers` warps (or single threads) follow it.
+struct TcQueue { uint4 answer[2]; uint64_t full[2], empty[2]; };       // in shared memory: the next block, one ahead
+__device__ __forceinline__ void tc_queue_init(TcQueue &q, int readers) {
+  for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&q.full[i]), 1); mbar_init(smem_u32(&q.empty[i]), readers); }
+}
+// asks for block number `seq` of this CTA (one thread)
+__device__ __forceinline__ bool tc_queue_ask(TcQueue &q, int seq, long long deadline) {
+  const int s = seq & 1;
+  if (!tc_wait_released(q.empty, seq, 2, deadline)) return false;
+  mbar_expect_tx(smem_u32(&q.full[s]), 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(smem_u32(&q.answer[s])), "r"(smem_u32(&q.full[s])) : "memory");
+  return true;
+}
+// ... and reads the answer: the block, or -1 when none is left
+__device__ __forceinline__ long long tc_queue_answer(TcQueue &q, int seq) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n.reg .b128 h;\n.reg .pred p;\nld.shared.b128 h, [%2];\n"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, h;\n}"
+      : "=r"(got), "=r"(x) : "r"(smem_u32(&q.answer[seq & 1])) : "memory");
+  tc_proxy_fence();              // the next answer may be written once this one has been read
+  return got ? (long long)x : -1;
+}
+__device__ __forceinline__ long long tc_queue_next(TcQueue &q, int seq, long long deadline, bool &ok) {        // a whole warp
+  if (!(ok = ok && tc_wait(&q.full[seq & 1], tc_parity(seq, 2), deadline))) return -1;
+  const long long at = tc_queue_answer(q, seq);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&q.empty[seq & 1]));
+  return at;
+}
+__device__ __forceinline__ long long tc_queue_next_one(TcQueue &q, int seq, long long deadline, bool &ok) {    // one thread
+  if (!(ok = ok && mbar_wait(smem_u32(&q.full[seq & 1]), tc_parity(seq, 2), deadline))) return -1;
+  const long long at = tc_queue_answer(q, seq);
+  mbar_arrive(smem_u32(&q.empty[seq & 1]));
+  return at;
+}
+__device__ __forceinline__ void tc_warp_arrive(uint64_t *bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(bar));
+}
+
+__device__ __forceinline__ uint32_t tc_cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t tc_cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void tc_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 tc_peer_load(uint32_t addr, uint32_t rank) {
+  uint32_t there;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+  return v;
+}
+
 // ---- host side ----------------------------------------------------------------------------------
 // Tensor map of 16-bit values: dims / strides[i] (elements; the innermost axis is contiguous), box of
 // 64 columns by `box_rows` rows with the 128-byte swizzle; out-of-range elements read as zeros.
@@ -127,3 +196,25 @@ inline bool tc_encode(CUtensorMap *map, bool bf16, const void *base, int rank, c
             const_cast<void *>(base), d, s, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+template <typename... KArgs, typename... Args>
+inline int tc_launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cdg_launch_rc(cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...));
+}
+
+template <typename K>
+inline bool tc_raise_limit(CdgPerDevice &flags, K *kernel, size_t bytes) {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cdg_raise_smem_limit(flags, dev, kernel, bytes) == cudaSuccess;
+}
+
