@@ -28,11 +28,12 @@ constexpr int kNormBlocks = 128;
 // VEC values to a load: 16 bytes where rows, stride and address allow it, else one
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_sumsq(const T *g, long long gb, long long gs, int rows, int cols,
-                                                  double *part) {
+                                                  double *part, unsigned *arrived) {
   struct __align__(sizeof(T) * VEC) Piece { T v[VEC]; };
   __shared__ double sm[8];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *arrived = 0;       // the counter of orth_steps
   const T *p = g + blockIdx.y * gb;
   const int per = cols / VEC;
   const long long all = (long long)rows * per, step = (long long)gridDim.x * 256;
@@ -107,102 +108,225 @@ __global__ void __launch_bounds__(256) orth_start(const T *g, long long gb, long
   }
 }
 
-// ---- the products ----------------------------------------------------------------------------
-// Persistent CTAs, one to an SM, take tiles of C = A op(B), 128 rows by BN columns: warp 0 keeps a ring of
+// ---- the steps ---------------------------------------------------------------------------------
+// One cooperative launch runs all steps: 3 x steps products with a barrier of the whole grid between them
+// (17 launches took 164 us for one 650 x 2600 matrix, ten microseconds each whatever they did).  Persistent
+// CTAs, one to an SM, take tiles of C = A op(B), 128 rows by 128 or BN columns: warp 0 keeps a ring of
 // shared-memory stages full (64 of K each), warp 1 issues the matrix instructions, warps 2 to 5 read the
 // accumulator, of which there are two in tensor memory so that one tile's products run under the other's
 // epilogue, and write it through shared memory in whole rows.
-// BN = 256 where there are tiles enough: a 128 x 128 product reads its operands from shared memory at the
-// full 128 bytes a cycle, one of 128 x 256 at three quarters of that.
-// Where there are few tiles, the K loop is dealt out over a cluster and the fp32 sums joined through
-// distributed shared memory in the order of the ranks.
+//   BN = 256    for X = B X where there are tiles enough: what bounds large matrices is the operands' way
+//               from L2 (11 TB/s), and the wider tile reads a quarter less of them
+//   RANKS > 1   few tiles: CTAs form clusters, whose ranks share the K loop of a tile of A or B and join
+//               their fp32 sums through distributed shared memory in the order of the ranks
 constexpr int kM = 128, kK = 64, kThreads = 192;
 enum Product { kGram, kPoly, kApply, kLast };   // A = X X^T; B = aI + bA + cAA; X = B X; the same into O
 
-struct ProductArgs {
-  int m, n, k, tiles;      // C is m x n; tiles of one matrix
-  float alpha, beta, diag; // C = alpha acc + beta D + diag I
-  const __half *D;         // kPoly: A
-  void *C;
-  int ldc;                 // kLast: row stride of O
-  long long cb, db;        // batch strides
-  int tall, vec;           // kLast: write the transpose; rows of O are 16-byte aligned
+struct StepArgs {
+  int m, n, batch, steps, ldx, lda, tall, vec;   // C is m x m, or m x n; vec: rows of O are 16-byte aligned
+  float a, b, c;
+  __half *x[2], *A, *B;
+  void *o;
+  long long xb, ab, ob, os;
+  unsigned *arrived;         // CTAs past each product, counted on
   int *status;
 };
+// X as rows of K and as panels of N, A and B; the same written in pieces of 32 x 32
+struct StepMaps { CUtensorMap rows[2], panels[2], A, B, to_x[2], to_A, to_B; };
 
-template <int P, int BN> struct Shape {
-  static constexpr bool symmetric = P == kGram || P == kPoly;
+template <int BN, int RANKS> struct Shape {
   static constexpr uint32_t a_bytes = kM * kK * 2, stage = a_bytes + BN * kK * 2;
-  static constexpr int ring = BN == 256 ? 4 : symmetric ? 5 : 6;
-  // per epilogue warp: rows of 64 halves (both halves of the tile's columns where a tile of D is fetched
-  // ahead), and a transposed piece of 64 rows of 32
-  static constexpr int row_pitch = 72, col_pitch = 40;
-  static constexpr uint32_t rows_bytes = 32 * row_pitch * 2, cols_bytes = 64 * col_pitch * 2;
-  static constexpr uint32_t cols_at = P == kPoly ? 2 * rows_bytes : P == kGram ? rows_bytes : 0;      // (O is written one way or the other)
-  static constexpr uint32_t warp_bytes = cols_at + cols_bytes;
-  static constexpr uint32_t staging = ring * stage, bars = staging + 4 * warp_bytes;
+  static constexpr int ring = 4;
+  // per epilogue warp two buffers of 32 x 32 halves and their transpose, swizzled as the copies read them (or,
+  // written out by the warp itself, rows with these pitches)
+  static constexpr uint32_t warp_bytes = 8192;
+  static constexpr uint32_t sums = ring * stage, staging = sums + (RANKS > 1 ? kM * kM * 4 : 0), bars = staging + 4 * warp_bytes;
   static constexpr size_t smem = bars + 256;
 };
-template <int P, int BN> struct Bars {
-  TcQueue queue;
-  uint64_t full[Shape<P, BN>::ring], empty[Shape<P, BN>::ring], acc_full[2], acc_empty[2];
+template <int BN, int RANKS> struct Bars {
+  uint64_t full[Shape<BN, RANKS>::ring], empty[Shape<BN, RANKS>::ring], acc_full[2], acc_empty[2], joined, read;
   uint32_t tmem;
 };
 
 __device__ __forceinline__ uint32_t sum_at(int row, int piece) {        // fp32 [128][128], 16-byte pieces permuted by row
   return (uint32_t)(row * 512 + (((piece & ~7) | ((piece ^ row) & 7)) << 4));
 }
-template <int P>
-__device__ __forceinline__ uint32_t finish(float x, float y, float dx, float dy, int i, int j, const ProductArgs &p) {
-  x *= p.alpha;
-  y *= p.alpha;
-  if (P == kPoly) {
-    x = fmaf(p.beta, dx, x) + (i == j ? p.diag : 0.0f);
-    y = fmaf(p.beta, dy, y) + (i == j + 1 ? p.diag : 0.0f);
+// two values of a product as they are stored; d: the two of A that kPoly adds
+template <int KIND>
+__device__ __forceinline__ uint32_t finish(const StepArgs &p, float x, float y, uint32_t d, int i, int j) {
+  if (KIND == kGram) { x *= 1.0f / (kScale * kScale); y *= 1.0f / (kScale * kScale); }
+  if (KIND == kPoly) {
+    const float2 q = __half22float2(*reinterpret_cast<const __half2 *>(&d));
+    x = fmaf(p.b, q.x, x * p.c) + (i == j ? p.a : 0.0f);
+    y = fmaf(p.b, q.y, y * p.c) + (i == j + 1 ? p.a : 0.0f);
   }
-  if (P == kLast) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  if (KIND == kLast) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x * (1.0f / kScale), y * (1.0f / kScale));
     return *reinterpret_cast<const uint32_t *>(&h);
   }
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t *>(&h);
 }
-// `rows` rows of 8 * pieces halves from shared memory (pitch in halves) to C at (r0, c0), a whole warp; the
-// workspace's rows are padded to multiples of 8 values, so whole pieces are written there
-__device__ __forceinline__ void put(const __half *from, int pitch, int rows, int pieces, __half *C, long long ldc, int r0, int c0,
-                                    int nr, int nc, bool padded, bool vec) {
+// O as the caller has it: nr x nc values, rows ld apart, on 16-byte boundaries where vec is set
+struct Out { __half *p; long long ld; int nr, nc; bool vec; };
+// ROWS rows of 8 * PIECES halves from shared memory (pitch in halves) to (r0, c0), a whole warp
+template <int ROWS, int PIECES>
+__device__ __forceinline__ void put(const __half *from, int pitch, const Out &o, int r0, int c0) {
   const int lane = threadIdx.x & 31;
-  if (vec) {
-    for (int i = lane; i < rows * pieces; i += 32) {
-      const int r = i / pieces, c = i % pieces * 8;
-      if (r0 + r >= nr || c0 + c >= nc) continue;
-      __half *to = C + (long long)(r0 + r) * ldc + c0 + c;
-      if (padded || c0 + c + 8 <= nc) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from + r * pitch + c);
-      else for (int e = 0; e < nc - c0 - c; ++e) to[e] = from[r * pitch + c + e];
+  if (o.vec) {
+#pragma unroll
+    for (int i = 0; i < ROWS * PIECES / 32; ++i) {
+      const int r = (i * 32 + lane) / PIECES, c = (i * 32 + lane) % PIECES * 8;
+      if (r0 + r >= o.nr || c0 + c >= o.nc) continue;
+      __half *to = o.p + (long long)(r0 + r) * o.ld + c0 + c;
+      if (c0 + c + 8 <= o.nc) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from + r * pitch + c);
+      else for (int e = 0; e < o.nc - c0 - c; ++e) to[e] = from[r * pitch + c + e];
     }
   } else {
-    for (int i = lane; i < rows * pieces * 8; i += 32) {
-      const int r = i / (pieces * 8), c = i % (pieces * 8);
-      if (r0 + r < nr && c0 + c < nc) C[(long long)(r0 + r) * ldc + c0 + c] = from[r * pitch + c];
+    for (int i = lane; i < ROWS * PIECES * 8; i += 32) {
+      const int r = i / (PIECES * 8), c = i % (PIECES * 8);
+      if (r0 + r < o.nr && c0 + c < o.nc) o.p[(long long)(r0 + r) * o.ld + c0 + c] = from[r * pitch + c];
     }
   }
 }
 
-template <int P, int BN>
-__global__ void __launch_bounds__(kThreads, 1) orth_product(const __grid_constant__ CUtensorMap ta,
-                                                            const __grid_constant__ CUtensorMap tb, const ProductArgs p) {
-  typedef Shape<P, BN> S;
+__device__ __forceinline__ bool wait_count(const unsigned *count, unsigned want, long long deadline) {
+  unsigned got;
+  while (true) {
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(got) : "l"(count) : "memory");
+    if (got >= want) return true;
+    if (clock64() > deadline) return false;
+  }
+}
+
+// A warp's 32 rows of a tile's accumulator, 32 columns at a time, to memory.  The loops are kept short and
+// rolled up: written out straight, a tile's epilogue was three times as slow, waiting for its instructions.
+struct Piece { uint32_t acc; int i0, j0, z, wide; bool mirror; };       // this warp's part of a tile
+template <int KIND>
+__device__ __forceinline__ void write_tile(const StepArgs &p, const CUtensorMap *rows_map, const CUtensorMap *cols_map, uint8_t *stage,
+                                           const Piece &t, uint64_t *acc_empty) {
+  const int lane = threadIdx.x & 31, i = t.i0 + lane, nc = KIND == kGram || KIND == kPoly ? p.m : p.n;
+  const __half *D = p.A + t.z * p.ab + (long long)i * p.lda;
+  uint4 ahead[4];            // kPoly: this lane's row of A, one piece of 32 columns ahead
+  auto fetch = [&](int j) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      ahead[c] = i < p.m && j + c * 8 < p.m ? *reinterpret_cast<const uint4 *>(D + j + c * 8) : make_uint4(0, 0, 0, 0);
+  };
+  if (KIND == kPoly) fetch(t.j0);
+#pragma unroll 1
+  for (int c0 = 0; c0 < t.wide; c0 += 32) {
+    uint32_t v[32], q[16];
+    tc_load32(t.acc + c0, v);
+    uint8_t *rows = stage + ((c0 >> 5) & 1) * 4096, *cols = rows + 2048;
+    if (KIND != kLast) {
+      if (lane == 0) tc_store_read1();           // the buffer's last pieces have been read
+      __syncwarp();
+    }
+    tc_wait_ld();
+    if (c0 + 32 == t.wide) {                     // all of it is in registers: the tile after next may use the accumulator
+      tc_fence_before();
+      tc_warp_arrive(acc_empty);
+    }
+    const uint32_t *dd = reinterpret_cast<const uint32_t *>(ahead);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      q[e] = finish<KIND>(p, __uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), KIND == kPoly ? dd[e] : 0u, i, t.j0 + c0 + 2 * e);
+    if (KIND == kPoly && c0 + 32 < t.wide) fetch(t.j0 + c0 + 32);
+    const int j = t.j0 + c0;
+    if (KIND != kLast) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4 *>(rows + lane * 64 + ((c ^ (lane >> 1) & 3) << 4)) = make_uint4(q[4 * c], q[4 * c + 1], q[4 * c + 2], q[4 * c + 3]);
+      if (t.mirror) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          uint16_t *to = reinterpret_cast<uint16_t *>(cols + 2 * e * 64 + (((lane >> 3) ^ (e & 3)) << 4)) + (lane & 7);
+          to[0] = (uint16_t)(q[e] & 0xffffu);
+          to[32] = (uint16_t)(q[e] >> 16);       // the next row, in the same place: the swizzle goes by pairs of rows
+        }
+      }
+      tc_proxy_fence();
+      __syncwarp();
+      if (lane == 0) {
+        if (t.i0 < p.m && j < nc) tc_store_3d(rows_map, smem_u32(rows), j, t.i0, t.z);
+        if (t.mirror && t.i0 < p.m && j < nc) tc_store_3d(cols_map, smem_u32(cols), t.i0, j, t.z);
+        tc_store_commit();
+      }
+    } else {
+      const Out o = {static_cast<__half *>(p.o) + t.z * p.ob, p.os, p.tall ? p.n : p.m, p.tall ? p.m : p.n, p.vec != 0};
+      if (p.tall) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          reinterpret_cast<uint16_t *>(rows)[(2 * e) * 40 + lane] = (uint16_t)(q[e] & 0xffffu);
+          reinterpret_cast<uint16_t *>(rows)[(2 * e + 1) * 40 + lane] = (uint16_t)(q[e] >> 16);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(rows + lane * 80 + c * 16) = make_uint4(q[4 * c], q[4 * c + 1], q[4 * c + 2], q[4 * c + 3]);
+      }
+      __syncwarp();
+      put<32, 4>(reinterpret_cast<const __half *>(rows), 40, o, p.tall ? j : t.i0, p.tall ? t.i0 : j);
+      __syncwarp();
+    }
+  }
+}
+// ... and, where the ranks of a cluster have parts of the sums, this warp's rows r0 .. r0 + SHARE - 1 of a tile:
+// added up, finished and written
+template <int KIND, int RANKS>
+__device__ __forceinline__ void write_share(const StepArgs &p, uint32_t sums, __half *stage, int r0, int i0, int j0, int z, bool mirror) {
+  constexpr int share = kM / RANKS / 4, pitch = 136;
+  const int lane = threadIdx.x & 31;
+  const __half *D = p.A + z * p.ab;
+  __half *C = (KIND == kGram ? p.A : p.B) + z * p.ab;
+#pragma unroll 4
+  for (int k = 0; k < share; ++k) {              // a row of 128 values to a turn
+    const int i = i0 + r0 + k, j = j0 + lane * 4;
+    float4 y[RANKS];
+#pragma unroll
+    for (int o = 0; o < RANKS; ++o) y[o] = tc_peer_load(sums + sum_at(r0 + k, lane), o);
+    uint2 d = make_uint2(0, 0);
+    const bool inside = i < p.m && j < p.m;      // (rows of the workspace are padded to multiples of 8 values)
+    if (KIND == kPoly && inside) d = *reinterpret_cast<const uint2 *>(D + (long long)i * p.lda + j);
+    float4 x = y[0];
+#pragma unroll
+    for (int o = 1; o < RANKS; ++o) { x.x += y[o].x; x.y += y[o].y; x.z += y[o].z; x.w += y[o].w; }
+    const uint2 h = make_uint2(finish<KIND>(p, x.x, x.y, d.x, i, j), finish<KIND>(p, x.z, x.w, d.y, i, j + 2));
+    *reinterpret_cast<uint2 *>(stage + k * pitch + lane * 4) = h;
+    if (inside) *reinterpret_cast<uint2 *>(C + (long long)i * p.lda + j) = h;
+  }
+  __syncwarp();
+  if (!mirror) return;
+#pragma unroll 2
+  for (int k = lane; k < kM * (share / 8); k += 32) {           // transposed: pieces of eight rows
+    const int c = k / (share / 8), rr = k % (share / 8) * 8;
+    if (j0 + c >= p.m || i0 + r0 + rr >= p.m) continue;
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      o[e] = (uint32_t)__half_as_ushort(stage[(rr + 2 * e) * pitch + c]) | (uint32_t)__half_as_ushort(stage[(rr + 2 * e + 1) * pitch + c]) << 16;
+    *reinterpret_cast<uint4 *>(C + (long long)(j0 + c) * p.lda + i0 + r0 + rr) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+  __syncwarp();
+}
+
+template <int BN, int RANKS>
+__global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant__ StepMaps maps, const StepArgs p) {
+  typedef Shape<BN, RANKS> S;
   extern __shared__ __align__(1024) uint8_t base[];
-  static_assert(sizeof(Bars<P, BN>) <= 256 && S::smem <= 232448, "");
-  Bars<P, BN> &bar = *reinterpret_cast<Bars<P, BN> *>(base + S::bars);
+  static_assert(sizeof(Bars<BN, RANKS>) <= 256 && S::smem <= 232448, "shared memory");
+  Bars<BN, RANKS> &bar = *reinterpret_cast<Bars<BN, RANKS> *>(base + S::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ring = smem_u32(base);
-  const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank();
+  constexpr bool kSplit = RANKS > 1;
+  const int rank = kSplit ? (int)tc_cluster_rank() : 0;
+  const int cta = blockIdx.x, ctas = gridDim.x, cluster = cta / RANKS, clusters = ctas / RANKS;
 
   if (threadIdx.x == 0) {
-    tc_queue_init(bar.queue, 6);
     for (int s = 0; s < S::ring; ++s) { mbar_init(smem_u32(&bar.full[s]), 1); mbar_init(smem_u32(&bar.empty[s]), 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bar.acc_full[s]), 1); mbar_init(smem_u32(&bar.acc_empty[s]), 4); }
+    mbar_init(smem_u32(&bar.joined), 4 * RANKS);
+    mbar_init(smem_u32(&bar.read), 4 * RANKS);
     mbar_init_fence();
   }
   if (warp == 1) tc_alloc(&bar.tmem, 512);
@@ -210,152 +334,170 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product(const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t acc = bar.tmem;
+  if (kSplit) tc_cluster_sync();            // the peers' barriers are ready
   cdg_grid_dep_wait();
-  cdg_grid_dep_trigger();
-  const long long deadline = clock64() + kCdgWaitCycles;
-  const int nk = ((p.k + kK - 1) / kK - rank + ranks - 1) / ranks;       // this CTA's steps of K: rank, rank + ranks, ...
 
-  struct Tile { int i0, j0, z; };
-  auto tile_of = [&](long long at) {
-    const int z = (int)(at / p.tiles), t = (int)(at % p.tiles);
-    int ti, tj;
-    if (S::symmetric) {      // tiles (ti, tj), ti <= tj, counted column by column
-      tj = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-      while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
-      while (tj * (tj + 1) / 2 > t) --tj;
-      ti = t - tj * (tj + 1) / 2;
-    } else {
-      const int nt = (p.m + kM - 1) / kM;
-      ti = t % nt;
-      tj = t / nt;
-    }
-    return Tile{ti * kM, tj * BN, z};
+  const int mt = (p.m + kM - 1) / kM, nt = (p.n + BN - 1) / BN, sym = mt * (mt + 1) / 2;
+  // the products in turn; the tiles of one are dealt out over the CTAs, or over the clusters where those
+  // share the K loop
+  struct Turn { int kind, at, tiles, nk, k0, dk, first, step; };       // at: which X is read
+  auto turn_of = [&](int t) {
+    Turn u;
+    const int which = t % 3;
+    u.at = (t / 3) & 1;
+    u.kind = which < 2 ? which : t / 3 + 1 == p.steps ? kLast : kApply;
+    u.tiles = (which < 2 ? sym : mt * nt) * p.batch;
+    const bool shared = kSplit && which < 2;
+    const int steps = ((which == 0 ? p.n : p.m) + kK - 1) / kK;
+    u.k0 = shared ? rank : 0;
+    u.dk = shared ? RANKS : 1;
+    u.nk = (steps - u.k0 + u.dk - 1) / u.dk;
+    u.first = shared ? cluster : cta;
+    u.step = shared ? clusters : ctas;
+    return u;
   };
-  const long long first = blockIdx.x / ranks;      // a cluster takes one tile and asks for no more
+  struct Tile { int i0, j0, z; };
+  auto tile_of = [&](const Turn &u, int at) {
+    if (u.kind < 2) {        // tiles (i, j), i <= j, counted column by column
+      const int z = at / sym, t = at % sym;
+      int j = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+      while ((j + 1) * (j + 2) / 2 <= t) ++j;
+      while (j * (j + 1) / 2 > t) --j;
+      return Tile{(t - j * (j + 1) / 2) * kM, j * kM, z};
+    }
+    const int z = at / (mt * nt), t = at % (mt * nt);
+    return Tile{t % mt * kM, t / mt * BN, z};
+  };
+  const int turns = 3 * p.steps;
 
   if (warp == 0) {
     if (tc_elect()) {
       bool ok = true;
-      int n = 0, seq = 0;
-      for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-        if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
-        const Tile t = tile_of(at);
-        for (int it = 0; it < nk; ++it, ++n) {
-          if (!(ok = tc_wait_released(bar.empty, n, S::ring, deadline))) break;
-          const uint32_t full = smem_u32(&bar.full[n % S::ring]), a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
-          const int k0 = (rank + it * ranks) * kK;
-          mbar_expect_tx(full, S::stage);
-          tma_load_3d(a, &ta, k0, t.i0, t.z, full);
-          if (S::symmetric) {
-            tma_load_3d(b, &tb, k0, t.j0, t.z, full);
-          } else {           // panels of 64 columns, 64 rows of K
+      int n = 0;
+      for (int t = 0; t < turns && ok; ++t) {
+        const Turn u = turn_of(t);
+        long long deadline = clock64() + kCdgWaitCycles;
+        if (t > 0) {           // every CTA has written its part of the product before
+          const unsigned want = (unsigned)t * (unsigned)ctas;
+          if (!(ok = wait_count(p.arrived, want, deadline))) break;
+          asm volatile("fence.proxy.async;" ::: "memory");         // ... and the copies see it
+        }
+        const CUtensorMap *ma = u.kind == kGram ? &maps.rows[u.at] : u.kind == kPoly ? &maps.A : &maps.B;
+        const CUtensorMap *mb = u.kind == kGram ? &maps.rows[u.at] : u.kind == kPoly ? &maps.A : &maps.panels[u.at];
+        for (int at = u.first; at < u.tiles && ok; at += u.step) {
+          const Tile w = tile_of(u, at);
+          deadline = clock64() + kCdgWaitCycles;
+          for (int it = 0; it < u.nk; ++it, ++n) {
+            if (!(ok = tc_wait_released(bar.empty, n, S::ring, deadline))) break;
+            const uint32_t full = smem_u32(&bar.full[n % S::ring]), a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
+            const int k0 = (u.k0 + it * u.dk) * kK;
+            mbar_expect_tx(full, u.kind < 2 ? 2 * S::a_bytes : S::stage);
+            tma_load_3d(a, ma, k0, w.i0, w.z, full);
+            if (u.kind < 2) {
+              tma_load_3d(b, mb, k0, w.j0, w.z, full);
+            } else {           // panels of 64 columns, 64 rows of K
 #pragma unroll
-            for (int c = 0; c < BN / 64; ++c) tma_load_3d(b + c * kK * 128, &tb, t.j0 + c * 64, k0, t.z, full);
+              for (int c = 0; c < BN / 64; ++c) tma_load_3d(b + c * kK * 128, mb, w.j0 + c * 64, k0, w.z, full);
+            }
           }
         }
       }
       if (!ok) {
         atomicOr(p.status, CDG_ST_TIMEOUT);
-        if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
         tc_drain(bar.full, n, S::ring);
       }
     }
   } else if (warp == 1) {
-    constexpr uint32_t idesc = tc_idesc(false, kM, BN, false, !S::symmetric);
     bool ok = true;
     int n = 0, seq = 0;
-    for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      const uint32_t d = acc + (seq & 1) * BN;
-      if (seq >= 2 && !(ok = tc_wait(&bar.acc_empty[seq & 1], tc_parity(seq - 2, 2), deadline))) break;
-      for (int it = 0; it < nk; ++it, ++n) {
-        if (!(ok = tc_wait(&bar.full[n % S::ring], tc_parity(n, S::ring), deadline))) break;
-        tc_fence_after();
-        const uint32_t a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
-        const uint64_t da = tc_desc_k(a), db = S::symmetric ? tc_desc_k(b) : tc_desc_mn(b, kK * 128);
-        if (tc_elect()) {
+    for (int t = 0; t < turns && ok; ++t) {
+      const Turn u = turn_of(t);
+      const uint32_t idesc = u.kind < 2 ? tc_idesc(false, kM, kM, false, false) : tc_idesc(false, kM, BN, false, true);
+      const uint32_t kb = u.kind < 2 ? 2 : 128;          // 16 of K further on in B, in units of 16 bytes
+      for (int at = u.first; at < u.tiles && ok; at += u.step, ++seq) {
+        const long long deadline = clock64() + 2 * kCdgWaitCycles;       // (the copies may wait for the grid)
+        const uint32_t d = acc + (seq & 1) * 256;
+        if (seq >= 2 && !(ok = tc_wait(&bar.acc_empty[seq & 1], tc_parity(seq - 2, 2), deadline))) break;
+        for (int it = 0; it < u.nk; ++it, ++n) {
+          if (!(ok = tc_wait(&bar.full[n % S::ring], tc_parity(n, S::ring), deadline))) break;
+          tc_fence_after();
+          const uint32_t a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
+          const uint64_t da = tc_desc_k(a), db = u.kind < 2 ? tc_desc_k(b) : tc_desc_mn(b, kK * 128);
+          if (tc_elect()) {
 #pragma unroll
-          for (int kk = 0; kk < kK / 16; ++kk) tc_mma(d, da + kk * 2, db + kk * (S::symmetric ? 2 : 128), idesc, it > 0 || kk > 0);
-          tc_commit(&bar.empty[n % S::ring]);
+            for (int kk = 0; kk < kK / 16; ++kk) tc_mma(d, da + kk * 2, db + kk * kb, idesc, it > 0 || kk > 0);
+            tc_commit(&bar.empty[n % S::ring]);
+          }
+          __syncwarp();
         }
+        if (!ok) break;
+        if (tc_elect()) tc_commit(&bar.acc_full[seq & 1]);
         __syncwarp();
       }
-      if (!ok) break;
-      if (tc_elect()) tc_commit(&bar.acc_full[seq & 1]);
-      __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
   } else {
     const int w = warp & 3, r = w * 32 + lane;         // warp w of the four reads lanes 32 w ... of the accumulator
-    __half *rows = reinterpret_cast<__half *>(base + S::staging + w * S::warp_bytes);
-    __half *cols = rows + S::cols_at / 2;
+    uint8_t *stage = base + S::staging + w * S::warp_bytes;
     bool ok = true;
-    int seq = 0;
-    for (long long at = first; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      const Tile t = tile_of(at);
-      __half *C = static_cast<__half *>(p.C) + t.z * p.cb;
-      if (P == kPoly && ranks == 1) {      // the tile of A that is added, while the products run
-        const __half *D = p.D + t.z * p.db;
-#pragma unroll 4
-        for (int i = lane; i < 32 * 16; i += 32) {
-          const int rr = i >> 4, c = (i & 15) * 8;
-          if (t.i0 + w * 32 + rr < p.m && t.j0 + c < p.n)
-            *reinterpret_cast<uint4 *>(rows + ((c >> 6) * 32 + rr) * S::row_pitch + (c & 63)) =
-                *reinterpret_cast<const uint4 *>(D + (long long)(t.i0 + w * 32 + rr) * p.ldc + t.j0 + c);
-        }
-        __syncwarp();
+    int seq = 0, joins = 0;
+    for (int t = 0; t < turns && ok; ++t) {
+      const Turn u = turn_of(t);
+      const bool split = kSplit && u.kind < 2;
+      if (u.kind == kPoly && u.first < u.tiles) {      // A, which is added, is read here too
+        ok = lane != 0 || wait_count(p.arrived, (unsigned)t * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
       }
-      if (!(ok = tc_wait(&bar.acc_full[seq & 1], tc_parity(seq, 2), deadline))) break;
-      tc_fence_after();
-      const uint32_t d = acc + ((uint32_t)(w * 32) << 16) + (seq & 1) * BN;
-      if (ranks > 1) {
-        // this CTA's sums into the ring, which no copy fills any more
-#pragma unroll
-        for (int c0 = 0; c0 < kM; c0 += 32) {
-          uint32_t v[32] = {};
-          if (nk > 0) { tc_load32(d + c0, v); tc_wait_ld(); }
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4 *>(base + sum_at(r, (c0 >> 2) + i)) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      for (int at = u.first; at < u.tiles; at += u.step, ++seq) {
+        const Tile tile = tile_of(u, at);
+        const long long deadline = clock64() + 3 * kCdgWaitCycles;
+        const Piece piece = {acc + ((uint32_t)(w * 32) << 16) + (seq & 1) * 256, tile.i0 + w * 32, tile.j0, tile.z, u.kind < 2 ? kM : BN,
+                             u.kind < 2 && tile.i0 != tile.j0};
+        uint64_t *empty = &bar.acc_empty[seq & 1];
+        if (!(ok = tc_wait(&bar.acc_full[seq & 1], tc_parity(seq, 2), deadline))) break;
+        tc_fence_after();
+        if (!split) {
+          if (u.kind == kGram) write_tile<kGram>(p, &maps.to_A, &maps.to_A, stage, piece, empty);
+          else if (u.kind == kPoly) write_tile<kPoly>(p, &maps.to_B, &maps.to_B, stage, piece, empty);
+          else if (u.kind == kApply) write_tile<kApply>(p, &maps.to_x[1 - u.at], nullptr, stage, piece, empty);
+          else write_tile<kLast>(p, nullptr, nullptr, stage, piece, empty);
+          continue;
         }
-        break;
-      }
-      const bool mirror = S::symmetric && t.i0 != t.j0, turned = P == kLast && p.tall;
+        // this CTA's sums, after the peers have read those of the tile before
+        if (joins > 0 && !(ok = tc_wait_cluster(&bar.read, (joins - 1) & 1, deadline))) break;
 #pragma unroll 1
-      for (int c0 = 0; c0 < BN; c0 += 64) {
-        uint32_t v[2][32];
-        tc_load32(d + c0, v[0]);
-        tc_load32(d + c0 + 32, v[1]);
-        tc_wait_ld();
-        if (c0 + 64 == BN) {               // the accumulator is in registers: the tile after next may use it
-          tc_fence_before();
-          tc_warp_arrive(&bar.acc_empty[seq & 1]);
-        }
-        __half *mine = rows + (P == kPoly ? (c0 >> 6) * 32 * S::row_pitch : 0) + lane * S::row_pitch;
+        for (int c0 = 0; c0 < kM; c0 += 32) {
+          uint32_t v[32];
+          tc_load32(piece.acc + c0, v);
+          tc_wait_ld();
 #pragma unroll
-        for (int c = 0; c < 64; c += 8) {
-          uint32_t o[4], dd[4] = {};
-          if (P == kPoly) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(mine + c);
-            dd[0] = q.x; dd[1] = q.y; dd[2] = q.z; dd[3] = q.w;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&dd[e]));
-            o[e] = finish<P>(__uint_as_float(v[c >> 5][(c & 31) + 2 * e]), __uint_as_float(v[c >> 5][(c & 31) + 2 * e + 1]), f.x, f.y,
-                             t.i0 + r, t.j0 + c0 + c + 2 * e, p);
-            if (mirror || turned) {
-              reinterpret_cast<uint16_t *>(cols)[(c + 2 * e) * S::col_pitch + lane] = (uint16_t)(o[e] & 0xffffu);
-              reinterpret_cast<uint16_t *>(cols)[(c + 2 * e + 1) * S::col_pitch + lane] = (uint16_t)(o[e] >> 16);
-            }
-          }
-          if (!turned) *reinterpret_cast<uint4 *>(mine + c) = make_uint4(o[0], o[1], o[2], o[3]);
+          for (int i = 0; i < 8; ++i)            // (where no step of K fell to this rank, another tile's products lie there)
+            *reinterpret_cast<uint4 *>(base + S::sums + sum_at(r, (c0 >> 2) + i)) =
+                u.nk == 0 ? make_uint4(0, 0, 0, 0) : make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         }
-        __syncwarp();
-        const int rr = t.i0 + w * 32, cc = t.j0 + c0;
-        if (!turned) put(mine - lane * S::row_pitch, S::row_pitch, 32, 8, C, p.ldc, rr, cc, p.m, p.n, P != kLast, P != kLast || p.vec);
-        if (mirror) put(cols, S::col_pitch, 64, 4, C, p.ldc, cc, rr, p.n, p.m, true, true);
-        if (turned) put(cols, S::col_pitch, 64, 4, C, p.ldc, cc, rr, p.n, p.m, false, p.vec);
-        __syncwarp();
+        tc_fence_before();
+        tc_warp_arrive(empty);
+        if (lane < RANKS) tc_arrive_peer(&bar.joined, lane);
+        if (!(ok = tc_wait_cluster(&bar.joined, joins & 1, deadline))) break;
+        ++joins;
+        const int r0 = rank * (kM / RANKS) + w * (kM / RANKS / 4);
+        __half *mine = reinterpret_cast<__half *>(stage);
+        if (u.kind == kGram) write_share<kGram, RANKS>(p, ring + S::sums, mine, r0, tile.i0, tile.j0, tile.z, piece.mirror);
+        else write_share<kPoly, RANKS>(p, ring + S::sums, mine, r0, tile.i0, tile.j0, tile.z, piece.mirror);
+        if (lane < RANKS) tc_arrive_peer(&bar.read, lane);
+      }
+      if (lane == 0) tc_store_done();            // this lane's copies are written
+      if (!ok) break;
+      if (t + 1 < turns) {       // this CTA's part is written: visible to the copies of all, then counted
+        asm volatile("fence.proxy.async;" ::: "memory");
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        // (one without a part is counted no earlier than the product before is complete)
+        if (threadIdx.x == 64 && u.first >= u.tiles && t > 0)
+          ok = wait_count(p.arrived, (unsigned)t * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        if (threadIdx.x == 64) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrived) : "memory");
       }
     }
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
@@ -363,60 +505,14 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product(const __grid_constan
   tc_fence_before();
   __syncthreads();
   if (warp == 1) { tc_fence_after(); tc_free(acc, 512); }
-  if (ranks > 1) {
-    tc_cluster_sync();
-    // rank's share of the tile's rows: the cluster's sums added up, finished and written
-    const Tile t = tile_of(first);
-    const int share = kM / ranks, r0 = rank * share, e = threadIdx.x - 64;
-    __half *C = static_cast<__half *>(p.C) + t.z * p.cb;
-    __half *out = reinterpret_cast<__half *>(base + kM * 512);          // behind the sums: [share][136]
-    if (e >= 0) {
-      for (int i = e; i < share * 32; i += 128) {
-        const int r = r0 + i / 32, piece = i % 32, c = piece * 4;
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = 0; k < ranks; ++k) {
-          const float4 u = tc_peer_load(ring + sum_at(r, piece), k);
-          s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
-        }
-        float2 d0 = make_float2(0.0f, 0.0f), d1 = d0;
-        if (P == kPoly && t.i0 + r < p.m && t.j0 + c < p.n) {
-          const uint2 q = *reinterpret_cast<const uint2 *>(p.D + t.z * p.db + (long long)(t.i0 + r) * p.ldc + t.j0 + c);
-          d0 = __half22float2(*reinterpret_cast<const __half2 *>(&q.x));
-          d1 = __half22float2(*reinterpret_cast<const __half2 *>(&q.y));
-        }
-        *reinterpret_cast<uint2 *>(out + (i / 32) * 136 + c) =
-            make_uint2(finish<P>(s.x, s.y, d0.x, d0.y, t.i0 + r, t.j0 + c, p), finish<P>(s.z, s.w, d1.x, d1.y, t.i0 + r, t.j0 + c + 2, p));
-      }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      const int w = e >> 5, per = share / 4;
-      if (P == kLast && p.tall) {
-        for (int i = e; i < kM * share; i += 128) {
-          const int c = i / share, r = i % share;
-          if (t.j0 + c < p.n && t.i0 + r0 + r < p.m) C[(long long)(t.j0 + c) * p.ldc + t.i0 + r0 + r] = out[r * 136 + c];
-        }
-      } else {
-        put(out + w * per * 136, 136, per, 16, C, p.ldc, t.i0 + r0 + w * per, t.j0, p.m, p.n, P != kLast, P != kLast || p.vec);
-      }
-      if (S::symmetric && t.i0 != t.j0)
-        for (int i = e; i < kM * (share / 8); i += 128) {
-          const int c = i / (share / 8), r = i % (share / 8) * 8;
-          if (t.j0 + c >= p.n || t.i0 + r0 + r >= p.m) continue;
-          uint32_t q[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            q[k] = (uint32_t)__half_as_ushort(out[(r + 2 * k) * 136 + c]) | (uint32_t)__half_as_ushort(out[(r + 2 * k + 1) * 136 + c]) << 16;
-          *reinterpret_cast<uint4 *>(C + (long long)(t.j0 + c) * p.ldc + t.i0 + r0 + r) = make_uint4(q[0], q[1], q[2], q[3]);
-        }
-    }
-    tc_cluster_sync();           // no CTA leaves while another reads its sums
-  }
+  if (kSplit) tc_cluster_sync();            // no CTA leaves while another reads its sums
 }
 
 inline long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 struct Plan {
   int m, n, ldx, lda;
-  long long part, x0, x1, a, b, total;    // byte offsets in the workspace
+  long long part, arrived, x0, x1, a, b, total;    // byte offsets in the workspace
 };
 Plan plan_of(long long batch, int rows, int cols) {
   Plan p;
@@ -426,7 +522,8 @@ Plan plan_of(long long batch, int rows, int cols) {
   p.lda = (int)up(p.m, 8);
   const long long xb = up(2 * batch * p.m * p.ldx, 256), ab = up(2 * batch * p.m * p.lda, 256);
   p.part = 0;
-  p.x0 = up(8 * batch * kNormBlocks, 256);
+  p.arrived = 8 * batch * kNormBlocks;
+  p.x0 = up(p.arrived + 4, 256);
   p.x1 = p.x0 + xb;
   p.a = p.x1 + xb;
   p.b = p.a + ab;
@@ -434,30 +531,31 @@ Plan plan_of(long long batch, int rows, int cols) {
   return p;
 }
 
-template <int P, int BN>
-int launch(const CUtensorMap &ta, const CUtensorMap &tb, const ProductArgs &a, int batch, int cluster, cudaStream_t st) {
+template <int BN, int RANKS>
+int launch(const StepMaps &maps, const StepArgs &a, int sms, int device, cudaStream_t st) {
   static CdgPerDevice flags;
-  if (!tc_raise_limit(flags, orth_product<P, BN>, Shape<P, BN>::smem)) return CDGRAB_ERR_CUDA;
-  return tc_launch_cluster(orth_product<P, BN>, dim3((unsigned)(a.tiles * batch * cluster)), cluster, kThreads, Shape<P, BN>::smem, st, ta, tb, a);
-}
-
-template <int P>
-int product(const CUtensorMap &ta, const CUtensorMap &tb, ProductArgs a, int batch, int sms, cudaStream_t st) {
-  const int mt = (a.m + kM - 1) / kM, nt = (a.n + kM - 1) / kM, wide = (a.n + 255) / 256;
-  if (P == kApply || P == kLast) {
-    // tiles of 256 columns while they still give every SM one
-    if ((long long)mt * wide * batch >= sms) {
-      a.tiles = mt * wide;
-      return launch<P, P == kApply || P == kLast ? 256 : 128>(ta, tb, a, batch, 1, st);
-    }
-    a.tiles = mt * nt;
-  } else {
-    a.tiles = mt * (mt + 1) / 2;
+  static int room[64];           // CTAs that are resident at once, by device
+  if (!tc_raise_limit(flags, orth_steps<BN, RANKS>, Shape<BN, RANKS>::smem)) return CDGRAB_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = RANKS;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeCooperative;             // all CTAs at once: they wait for one another
+  at[1].val.cooperative = 1;
+  cfg.gridDim = dim3(sms / RANKS * RANKS); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = Shape<BN, RANKS>::smem; cfg.stream = st;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  int n = device < 64 ? room[device] : 0;
+  if (n == 0) {
+    if (RANKS == 1) n = sms;
+    else if (cudaOccupancyMaxActiveClusters(&n, orth_steps<BN, RANKS>, &cfg) != cudaSuccess || n < 1) return cdg_launch_rc(cudaErrorUnknown);
+    else n = n * RANKS < sms ? n * RANKS : sms / RANKS * RANKS;
+    if (device < 64) room[device] = n;
   }
-  // few tiles: as many CTAs to each as fit the SMs and leave two steps of K (64 each) to a CTA
-  int c = 1;
-  while (c < 8 && (long long)a.tiles * batch * 2 * c <= sms && (a.k + kK - 1) / kK >= 4 * c) c *= 2;
-  return launch<P, 128>(ta, tb, a, batch, c, st);
+  cfg.gridDim = dim3(n);
+  cfg.numAttrs = 2;
+  return cdg_launch_rc(cudaLaunchKernelEx(&cfg, orth_steps<BN, RANKS>, maps, a));
 }
 
 }  // namespace
@@ -471,7 +569,7 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
                                     int steps, const float *coeffs, float eps, void *o, long long ob, long long os,
                                     void *workspace, long long workspace_bytes, void *stream) {
   const long long need = cdgrab_orthogonalise_workspace_bytes(batch, rows, cols);
-  if (need < 0 || steps < 1 || steps > 64 || !coeffs || !(eps >= 0.0f) || (dtype != CDGRAB_F32 && dtype != CDGRAB_BF16))
+  if (need < 0 || (long long)rows * cols / (64 * 64) * (batch > 0 ? batch : 1) > (1 << 28) || steps < 1 || steps > 64 || !coeffs || !(eps >= 0.0f) || (dtype != CDGRAB_F32 && dtype != CDGRAB_BF16))
     return CDGRAB_ERR_INVALID;
   if (!isfinite(coeffs[0]) || !isfinite(coeffs[1]) || !isfinite(coeffs[2])) return CDGRAB_ERR_INVALID;
   if (batch == 0 || rows == 0 || cols == 0) return CDGRAB_OK;
@@ -486,22 +584,27 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   const int tall = rows > cols, m = p.m, n = p.n;
   char *w = (char *)up((long long)(uintptr_t)workspace, 256);
   double *part = (double *)(w + p.part);
+  unsigned *arrived = (unsigned *)(w + p.arrived);
   __half *x[2] = {(__half *)(w + p.x0), (__half *)(w + p.x1)}, *A = (__half *)(w + p.a), *B = (__half *)(w + p.b);
   const long long xb = (long long)m * p.ldx, ab = (long long)m * p.lda;
 
-  // X as 128-row boxes of 64 columns (operand of A) and as 64-row boxes (operand of B X); A and B
-  CUtensorMap tx[2], tk[2], ta, tb;
+  StepMaps maps;
   const long long dx[3] = {n, m, batch}, sx[3] = {1, p.ldx, xb}, da[3] = {m, m, batch}, sa[3] = {1, p.lda, ab};
   for (int i = 0; i < 2; ++i)
-    if (!tc_encode(&tx[i], false, x[i], 3, dx, sx, kM) || !tc_encode(&tk[i], false, x[i], 3, dx, sx, kK)) return CDGRAB_ERR_CUDA;
-  if (!tc_encode(&ta, false, A, 3, da, sa, kM) || !tc_encode(&tb, false, B, 3, da, sa, kM)) return CDGRAB_ERR_CUDA;
+    if (!tc_encode(&maps.rows[i], false, x[i], 3, dx, sx, kM) || !tc_encode(&maps.panels[i], false, x[i], 3, dx, sx, kK)) return CDGRAB_ERR_CUDA;
+  for (int i = 0; i < 2; ++i)
+    if (!tc_encode(&maps.to_x[i], false, x[i], 3, dx, sx, 32, 32)) return CDGRAB_ERR_CUDA;
+  if (!tc_encode(&maps.A, false, A, 3, da, sa, kM) || !tc_encode(&maps.B, false, B, 3, da, sa, kM) ||
+      !tc_encode(&maps.to_A, false, A, 3, da, sa, 32, 32) || !tc_encode(&maps.to_B, false, B, 3, da, sa, 32, 32) ||
+      !tc_encode(&maps.to_A, false, A, 3, da, sa, 32, 32) || !tc_encode(&maps.to_B, false, B, 3, da, sa, 32, 32))
+    return CDGRAB_ERR_CUDA;
 
   const dim3 gt((cols + 63) / 64, (rows + 63) / 64, batch);
   const int e = dtype == CDGRAB_F32 ? 4 : 2;
   const bool wide = cdg_aligned(g, 16) && gs % (16 / e) == 0 && gb % (16 / e) == 0 && cols % (16 / e) == 0;
   int rc;
   auto begin = [&](auto *sumsq, auto *start, const auto *from) {
-    const int r = cdg_launch_rc(cdg_ops_launch(sumsq, dim3(kNormBlocks, batch), 256, 0, st, from, gb, gs, rows, cols, part));
+    const int r = cdg_launch_rc(cdg_ops_launch(sumsq, dim3(kNormBlocks, batch), 256, 0, st, from, gb, gs, rows, cols, part, arrived));
     return r != CDGRAB_OK ? r : cdg_launch_rc(cdg_ops_launch(start, gt, 256, 0, st, from, gb, gs, rows, cols, tall, part, eps, x[0], p.ldx, xb));
   };
   if (dtype == CDGRAB_F32)
@@ -509,21 +612,15 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   else
     rc = wide ? begin(orth_sumsq<__nv_bfloat16, 8>, orth_start<__nv_bfloat16, 8>, (const __nv_bfloat16 *)g)
               : begin(orth_sumsq<__nv_bfloat16, 1>, orth_start<__nv_bfloat16, 1>, (const __nv_bfloat16 *)g);
-  const ProductArgs gram = {m, m, n, 0, 1.0f / (kScale * kScale), 0.0f, 0.0f, nullptr, A, p.lda, ab, 0, 0, 1, dev->status};
-  const ProductArgs poly = {m, m, m, 0, coeffs[2], coeffs[1], coeffs[0], A, B, p.lda, ab, ab, 0, 1, dev->status};
-  const ProductArgs last = {m, n, m, 0, 1.0f / kScale, 0.0f, 0.0f, nullptr, o, (int)os, ob, 0, tall,
-                            cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, dev->status};
-  for (int i = 0; i < steps && rc == CDGRAB_OK; ++i) {
-    const int at = i & 1;
-    rc = product<kGram>(tx[at], tx[at], gram, batch, dev->sms, st);
-    if (rc == CDGRAB_OK) rc = product<kPoly>(ta, ta, poly, batch, dev->sms, st);
-    if (rc != CDGRAB_OK) break;
-    if (i + 1 < steps) {
-      const ProductArgs apply = {m, n, m, 0, 1.0f, 0.0f, 0.0f, nullptr, x[1 - at], p.ldx, xb, 0, 0, 1, dev->status};
-      rc = product<kApply>(tb, tk[at], apply, batch, dev->sms, st);
-    } else {
-      rc = product<kLast>(tb, tk[at], last, batch, dev->sms, st);
-    }
-  }
-  return rc;
+  if (rc != CDGRAB_OK) return rc;
+  const StepArgs a = {m, n, batch, steps, p.ldx, p.lda, tall, cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, coeffs[0], coeffs[1], coeffs[2],
+                      {x[0], x[1]}, A, B, o, xb, ab, ob, os, arrived, dev->status};
+  // tiles of 256 columns while they still give every SM one; CTAs share a tile of A or B where there are fewer
+  // than half as many tiles as SMs, up to four of them and at least two steps of K each
+  const long long mt = (m + kM - 1) / kM, sym = mt * (mt + 1) / 2 * batch;
+  if (mt * ((n + 255) / 256) * batch >= dev->sms) return launch<256, 1>(maps, a, dev->sms, dev->index, st);
+  const int k = (m + kK - 1) / kK;
+  if (sym * 4 <= dev->sms && k >= 8) return launch<128, 4>(maps, a, dev->sms, dev->index, st);
+  if (sym * 2 <= dev->sms && k >= 4) return launch<128, 2>(maps, a, dev->sms, dev->index, st);
+  return launch<128, 1>(maps, a, dev->sms, dev->index, st);
 }

@@ -57,6 +57,15 @@ __device__ __forceinline__ void tc_commit(uint64_t *bar) {
 __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity, long long deadline) {
   return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, deadline));
 }
+// tile from shared memory to a tensor (one thread; coordinates inside the tensor); the end of a group of such
+// copies, and waits for this thread's groups: all but the last to have read shared memory, all to be written
+__device__ __forceinline__ void tc_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+               ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tc_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void tc_store_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+__device__ __forceinline__ void tc_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // moves registers between warpgroups: all four warps of one execute it.  The shares have to add up to
 // no more than the block was launched with.
 template <int N> __device__ __forceinline__ void tc_regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -166,6 +175,22 @@ __device__ __forceinline__ uint32_t tc_cluster_size() { uint32_t r; asm("mov.u32
 __device__ __forceinline__ void tc_cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// arrives at the barrier of another CTA of the cluster, and waits for such arrivals (a whole warp)
+__device__ __forceinline__ void tc_arrive_peer(uint64_t *bar, uint32_t rank) {
+  asm volatile("{\n.reg .b32 there;\nmapa.shared::cluster.u32 there, %0, %1;\n"
+               "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [there];\n}" ::"r"(smem_u32(bar)), "r"(rank) : "memory");
+}
+__device__ __forceinline__ bool tc_wait_cluster(uint64_t *bar, uint32_t parity, long long deadline) {
+  uint32_t done;
+  while (true) {
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    if (done || clock64() > deadline) break;
+  }
+  return __all_sync(0xffffffffu, done != 0);
+}
+// 16 bytes of another CTA's shared memory
 __device__ __forceinline__ float4 tc_peer_load(uint32_t addr, uint32_t rank) {
   uint32_t there;
   float4 v;
@@ -176,9 +201,10 @@ __device__ __forceinline__ float4 tc_peer_load(uint32_t addr, uint32_t rank) {
 
 // ---- host side ----------------------------------------------------------------------------------
 // Tensor map of 16-bit values: dims / strides[i] (elements; the innermost axis is contiguous), box of
-// 64 columns by `box_rows` rows with the 128-byte swizzle; out-of-range elements read as zeros.
+// 64 columns by `box_rows` rows with the 128-byte swizzle (or of 32 columns with the 64-byte one);
+// out-of-range elements read as zeros and are not written.
 inline bool tc_encode(CUtensorMap *map, bool bf16, const void *base, int rank, const long long *dims,
-                      const long long *strides, int box_rows) {
+                      const long long *strides, int box_rows, int box_cols = 64) {
   typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -189,11 +215,12 @@ inline bool tc_encode(CUtensorMap *map, bool bf16, const void *base, int rank, c
   for (int i = 0; i < rank; ++i) {
     d[i] = (cuuint64_t)dims[i];
     if (i > 0) s[i - 1] = (cuuint64_t)strides[i] * 2;
-    box[i] = i == 0 ? 64 : i == 1 ? (cuuint32_t)box_rows : 1;
+    box[i] = i == 0 ? (cuuint32_t)box_cols : i == 1 ? (cuuint32_t)box_rows : 1;
     one[i] = 1;
   }
   return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
-            const_cast<void *>(base), d, s, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            const_cast<void *>(base), d, s, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
