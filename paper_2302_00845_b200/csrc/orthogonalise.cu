@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(256) orth_sumsq(const T *g, long long gb, long
   __shared__ double sm[8];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *arrived = 0;       // the counter of orth_steps
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) arrived[threadIdx.x] = 0;       // the counters of orth_steps
   const T *p = g + blockIdx.y * gb;
   const int per = cols / VEC;
   const long long all = (long long)rows * per, step = (long long)gridDim.x * 256;
@@ -128,7 +128,7 @@ struct StepArgs {
   __half *x[2], *A, *B;
   void *o;
   long long xb, ab, ob, os;
-  unsigned *arrived;         // CTAs past each product, counted on
+  unsigned *arrived;         // [2] CTAs past each product of a part of the batch, counted on
   int *status;
 };
 // X as rows of K and as panels of N, A and B; the same written in pieces of 32 x 32
@@ -338,22 +338,34 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
   cdg_grid_dep_wait();
 
   const int mt = (p.m + kM - 1) / kM, nt = (p.n + BN - 1) / BN, sym = mt * (mt + 1) / 2;
-  // the products in turn; the tiles of one are dealt out over the CTAs, or over the clusters where those
-  // share the K loop
-  struct Turn { int kind, at, tiles, nk, k0, dk, first, step; };       // at: which X is read
+  // The products in turn.  A batch goes in two parts, of which one's products run while the other's are being
+  // waited for.  The tiles are dealt out over the CTAs (or over the clusters, where those share the K loop) from
+  // where the turn before ended, so that CTAs with a tile less in one turn have theirs first in the next.
+  struct Turn { int kind, at, z0, tiles, nk, k0, dk, first, step; };       // at: which X is read
+  const int parts = p.batch > 1 ? 2 : 1, turns = 3 * p.steps * parts;
+  int dealt_to = 0;                        // the CTA that the next turn begins with
   auto turn_of = [&](int t) {
     Turn u;
-    const int which = t % 3;
-    u.at = (t / 3) & 1;
-    u.kind = which < 2 ? which : t / 3 + 1 == p.steps ? kLast : kApply;
-    u.tiles = (which < 2 ? sym : mt * nt) * p.batch;
+    const int product = t / parts, which = product % 3, half = p.batch / 2;
+    const int z0 = t % parts == 0 ? 0 : half, zn = parts == 1 ? p.batch : t % parts == 0 ? half : p.batch - half;
+    u.at = (product / 3) & 1;
+    u.kind = which < 2 ? which : product / 3 + 1 == p.steps ? kLast : kApply;
+    u.z0 = z0;
+    u.tiles = (which < 2 ? sym : mt * nt) * zn;
     const bool shared = kSplit && which < 2;
     const int steps = ((which == 0 ? p.n : p.m) + kK - 1) / kK;
     u.k0 = shared ? rank : 0;
     u.dk = shared ? RANKS : 1;
     u.nk = (steps - u.k0 + u.dk - 1) / u.dk;
-    u.first = shared ? cluster : cta;
-    u.step = shared ? clusters : ctas;
+    if (kSplit) {
+      u.first = shared ? cluster : cta;
+      u.step = shared ? clusters : ctas;
+    } else {
+      const int from = cta - dealt_to;
+      u.first = from < 0 ? from + ctas : from;
+      u.step = ctas;
+      dealt_to = (dealt_to + u.tiles) % ctas;
+    }
     return u;
   };
   struct Tile { int i0, j0, z; };
@@ -363,12 +375,11 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       int j = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
       while ((j + 1) * (j + 2) / 2 <= t) ++j;
       while (j * (j + 1) / 2 > t) --j;
-      return Tile{(t - j * (j + 1) / 2) * kM, j * kM, z};
+      return Tile{(t - j * (j + 1) / 2) * kM, j * kM, u.z0 + z};
     }
     const int z = at / (mt * nt), t = at % (mt * nt);
-    return Tile{t % mt * kM, t / mt * BN, z};
+    return Tile{t % mt * kM, t / mt * BN, u.z0 + z};
   };
-  const int turns = 3 * p.steps;
 
   if (warp == 0) {
     if (tc_elect()) {
@@ -377,9 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       for (int t = 0; t < turns && ok; ++t) {
         const Turn u = turn_of(t);
         long long deadline = clock64() + kCdgWaitCycles;
-        if (t > 0) {           // every CTA has written its part of the product before
-          const unsigned want = (unsigned)t * (unsigned)ctas;
-          if (!(ok = wait_count(p.arrived, want, deadline))) break;
+        if (t >= parts && u.first < u.tiles) {         // every CTA has written its share of this part's product before
+          if (!(ok = wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, deadline))) break;
           asm volatile("fence.proxy.async;" ::: "memory");         // ... and the copies see it
         }
         const CUtensorMap *ma = u.kind == kGram ? &maps.rows[u.at] : u.kind == kPoly ? &maps.A : &maps.B;
@@ -445,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       const Turn u = turn_of(t);
       const bool split = kSplit && u.kind < 2;
       if (u.kind == kPoly && u.first < u.tiles) {      // A, which is added, is read here too
-        ok = lane != 0 || wait_count(p.arrived, (unsigned)t * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        ok = lane != 0 || wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
       }
       for (int at = u.first; at < u.tiles; at += u.step, ++seq) {
@@ -486,26 +496,268 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
         else write_share<kPoly, RANKS>(p, ring + S::sums, mine, r0, tile.i0, tile.j0, tile.z, piece.mirror);
         if (lane < RANKS) tc_arrive_peer(&bar.read, lane);
       }
-      if (lane == 0) tc_store_done();            // this lane's copies are written
       if (!ok) break;
-      if (t + 1 < turns) {       // this CTA's part is written: visible to the copies of all, then counted
-        asm volatile("fence.proxy.async;" ::: "memory");
-        __threadfence();
+      if (t + parts < turns) {
+        // this CTA's share is written (by lane 0's copies, or by all lanes): visible to all, then counted; one
+        // without a share is counted no earlier than the product before is complete, so that the count tells
+        if (lane == 0) tc_store_done();
+        if (split || lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        // (one without a part is counted no earlier than the product before is complete)
-        if (threadIdx.x == 64 && u.first >= u.tiles && t > 0)
-          ok = wait_count(p.arrived, (unsigned)t * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        if (threadIdx.x == 64) {
+          unsigned *count = p.arrived + t % parts;
+          if (u.first >= u.tiles && t >= parts) ok = wait_count(count, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+          if (ok) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory");
+        }
         ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        if (threadIdx.x == 64) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrived) : "memory");
       }
     }
+    if (lane == 0) tc_store_done();
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) { tc_fence_after(); tc_free(acc, 512); }
   if (kSplit) tc_cluster_sync();            // no CTA leaves while another reads its sums
+}
+
+// ---- small matrices -----------------------------------------------------------------------------
+// Up to 128 x 576: X, A and B stay in one CTA's shared memory for all steps, one CTA to a matrix and one launch in
+// all.  X lies in panels of 64 columns (128 rows of 128 bytes, swizzled), which serve as they are as the K-major
+// operands of X X^T and as the MN-major one of B X; a block of 128 columns of X is replaced where it lies when
+// its product is over.
+constexpr int kSmallThreads = 512, kSmallCols = 576;         // (eight of the warps read accumulators, all move G and O)
+constexpr uint32_t kPanel = 16384;
+inline size_t small_smem(int n) { return (size_t)((n + 63) / 64 + 4) * kPanel + 1024; }
+
+struct SmallArgs {
+  int rows, cols, tall, steps, vec;
+  float a, b, c, eps;
+  long long gb, gs, ob, os;
+  int *status;
+};
+
+// where 8 values from column c (a multiple of 8) of row r lie
+__device__ __forceinline__ uint32_t small_at(int r, int c) { return (uint32_t)(c >> 6) * kPanel + r * 128 + ((((c >> 3) ^ r) & 7) << 4); }
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_bfloat16 *o, const SmallArgs p) {
+  extern __shared__ __align__(1024) uint8_t base[];
+  __shared__ double part[kSmallThreads / 32];
+  __shared__ __align__(8) uint64_t bar[4];
+  __shared__ uint32_t slot;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int m = p.tall ? p.cols : p.rows, n = p.tall ? p.rows : p.cols, panels = (n + 63) / 64;
+  uint8_t *A = base + panels * kPanel, *B = A + 2 * kPanel;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bar[i]), 1);
+    mbar_init_fence();
+  }
+  if (warp == 0) tc_alloc(&slot, 512);
+  for (uint32_t i = threadIdx.x * 16; i < panels * kPanel; i += kSmallThreads * 16) *reinterpret_cast<uint4 *>(base + i) = make_uint4(0, 0, 0, 0);
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  g += blockIdx.x * p.gb;
+  o += blockIdx.x * p.ob;
+
+  // X = kScale G / (|G| + eps); G twice, the second time out of L2, VEC values to a load and eight loads at a time
+  struct __align__(sizeof(T) * VEC) Load { T v[VEC]; };
+  const int per = p.cols / VEC, all = p.rows * per;
+  auto each = [&](auto &&use) {
+    for (int i = threadIdx.x; i < all; i += 8 * kSmallThreads) {
+      Load q[8];
+      int r[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = i + k * kSmallThreads;
+        r[k] = at / per;
+        if (at < all) q[k] = *reinterpret_cast<const Load *>(g + (long long)r[k] * p.gs + (at - r[k] * per) * VEC);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = i + k * kSmallThreads;
+        if (at < all) use(r[k], (at - r[k] * per) * VEC, q[k]);
+      }
+    }
+  };
+  double s = 0.0;
+  each([&](int, int, const Load &q) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { const double v = cdg_ld(&q.v[e]); s = fma(v, v, s); }
+  });
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  if (lane == 0) part[warp] = s;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  s = 0.0;
+  for (int i = 0; i < kSmallThreads / 32; ++i) s += part[i];
+  const double norm = sqrt(s) + (double)p.eps;
+  const float f = norm > 0.0 ? (float)fmin((double)kScale / norm, 3e38) : 0.0f;
+  each([&](int gr, int gc, const Load &q) {
+    struct __align__(2 * VEC) Halves { __half v[VEC]; } h;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) h.v[e] = __float2half_rn(f * cdg_ld(&q.v[e]));
+    if (p.tall) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) *reinterpret_cast<__half *>(base + small_at(gc + e, gr & ~7) + (gr & 7) * 2) = h.v[e];
+    } else {
+      *reinterpret_cast<Halves *>(base + small_at(gr, gc & ~7) + (gc & 7) * 2) = h;
+    }
+  });
+  tc_proxy_fence();
+  __syncthreads();
+
+  const uint32_t tm = slot, mine = tm + ((uint32_t)((warp & 3) * 32) << 16);
+  const uint32_t sx = smem_u32(base), sa = smem_u32(A), sb = smem_u32(B);
+  const int r = (warp & 3) * 32 + lane, half = warp >> 2;          // (warps 8 to 15: half 2 and 3, none of the columns)
+  const bool aligned = (sx & 1023u) == 0;
+  bool ok = aligned;
+  uint32_t turn[4] = {0, 0, 0, 0};             // phases of the barriers
+  // products whose K index runs along the rows of both operands, `panels_` panels of 64
+  auto gram = [&](uint32_t x, int panels_) {
+    if (warp == 0) {
+      if (tc_elect()) {
+        constexpr uint32_t idesc = tc_idesc(false, 128, 128, false, false);
+        const uint64_t d = tc_desc_k(x);
+        for (int q = 0; q < panels_; ++q)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tc_mma(tm, d + q * (kPanel >> 4) + k * 2, d + q * (kPanel >> 4) + k * 2, idesc, q > 0 || k > 0);
+        tc_commit(&bar[0]);
+      }
+      __syncwarp();
+    }
+    ok = tc_wait(&bar[0], turn[0]++ & 1, clock64() + kCdgWaitCycles);
+    tc_fence_after();
+  };
+  auto settle = [&]() {          // what was written is an operand of the next product, what was read may be overwritten
+    tc_proxy_fence();
+    tc_fence_before();
+    ok = __syncthreads_and(ok);
+    tc_fence_after();
+  };
+  for (int step = 0; step < p.steps && ok; ++step) {
+    const bool last = step + 1 == p.steps;
+    gram(sx, panels);
+#pragma unroll 1
+    for (int c0 = half * 64; c0 < half * 64 + 64 && half < 2; c0 += 32) {
+      uint32_t v[32];
+      tc_load32(mine + c0, v);
+      tc_wait_ld();
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) {
+        uint32_t q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __half2 h = __floats2half2_rn(__uint_as_float(v[c + 2 * e]) * (1.0f / (kScale * kScale)), __uint_as_float(v[c + 2 * e + 1]) * (1.0f / (kScale * kScale)));
+          q[e] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        *reinterpret_cast<uint4 *>(A + small_at(r, c0 + c)) = make_uint4(q[0], q[1], q[2], q[3]);
+      }
+    }
+    settle();
+    if (!ok) break;
+    gram(sa, 2);
+#pragma unroll 1
+    for (int c0 = half * 64; c0 < half * 64 + 64 && half < 2; c0 += 32) {
+      uint32_t v[32];
+      tc_load32(mine + c0, v);
+      tc_wait_ld();
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(A + small_at(r, c0 + c));
+        const uint32_t d[4] = {x.x, x.y, x.z, x.w};
+        uint32_t q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 w = __half22float2(*reinterpret_cast<const __half2 *>(&d[e]));
+          const int j = c0 + c + 2 * e;
+          const __half2 h = __floats2half2_rn(fmaf(p.b, w.x, __uint_as_float(v[c + 2 * e]) * p.c) + (r == j ? p.a : 0.0f),
+                                              fmaf(p.b, w.y, __uint_as_float(v[c + 2 * e + 1]) * p.c) + (r == j + 1 ? p.a : 0.0f));
+          q[e] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        *reinterpret_cast<uint4 *>(B + small_at(r, c0 + c)) = make_uint4(q[0], q[1], q[2], q[3]);
+      }
+    }
+    settle();
+    if (!ok) break;
+    for (int q0 = 0; q0 < panels && ok; q0 += 6) {           // three blocks of 128 columns at a time
+      if (warp == 0) {
+        if (tc_elect()) {
+          for (int q = q0; q < panels && q < q0 + 6; q += 2) {
+            const uint32_t idesc = tc_idesc(false, 128, q + 1 < panels ? 128 : 64, false, true);
+            const uint64_t da = tc_desc_k(sb), db = tc_desc_mn(sx + q * kPanel, kPanel);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) tc_mma(tm + 128 + (q - q0) * 64, da + (k >> 2) * (kPanel >> 4) + (k & 3) * 2, db + k * 128, idesc, k > 0);
+            tc_commit(&bar[1 + (q - q0) / 2]);
+          }
+        }
+        __syncwarp();
+      }
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        const int q = q0 + 2 * t;
+        if (q >= panels || !ok) continue;
+        if (!(ok = tc_wait(&bar[1 + t], turn[1 + t]++ & 1, clock64() + kCdgWaitCycles))) continue;
+        tc_fence_after();
+        if (half > 1 || q + half >= panels) continue;
+#pragma unroll 1
+        for (int c0 = half * 64; c0 < half * 64 + 64; c0 += 32) {
+          uint32_t v[32];
+          tc_load32(mine + 128 + t * 128 + c0, v);
+          tc_wait_ld();
+          const int j = q * 64 + c0;
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = __uint_as_float(v[c + 2 * e]), y = __uint_as_float(v[c + 2 * e + 1]);
+              if (last) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x * (1.0f / kScale), y * (1.0f / kScale));
+                w[e] = *reinterpret_cast<const uint32_t *>(&h);
+              } else {
+                const __half2 h = __floats2half2_rn(x, y);
+                w[e] = *reinterpret_cast<const uint32_t *>(&h);
+              }
+            }
+            *reinterpret_cast<uint4 *>(base + small_at(r, j + c)) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      settle();
+    }
+  }
+  // O, rows of it in pieces of eight values, out of X's place
+  const int pieces = (p.cols + 7) / 8;
+  for (int i = threadIdx.x; i < p.rows * pieces && ok; i += kSmallThreads) {
+    const int orow = i / pieces, c0 = (i - orow * pieces) * 8;
+    __nv_bfloat16 *to = o + (long long)orow * p.os + c0;
+    uint32_t w[4];
+    if (p.tall) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint8_t *at = base + (orow & 7) * 2;
+        const int r0 = c0 + 2 * e;                // (rows up to 127 are there)
+        w[e] = (uint32_t)*reinterpret_cast<const uint16_t *>(at + small_at(r0, orow & ~7)) |
+               (uint32_t)*reinterpret_cast<const uint16_t *>(at + small_at(r0 + 1, orow & ~7)) << 16;
+      }
+    } else {
+      const uint4 x = *reinterpret_cast<const uint4 *>(base + small_at(orow, c0));
+      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    }
+    if (p.vec && c0 + 8 <= p.cols) {
+      *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c0 + e < p.cols) to[e] = __ushort_as_bfloat16((unsigned short)(w[e >> 1] >> (16 * (e & 1))));
+    }
+  }
+  if (!ok && threadIdx.x == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) { tc_fence_after(); tc_free(tm, 512); }
 }
 
 inline long long up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -523,7 +775,7 @@ Plan plan_of(long long batch, int rows, int cols) {
   const long long xb = up(2 * batch * p.m * p.ldx, 256), ab = up(2 * batch * p.m * p.lda, 256);
   p.part = 0;
   p.arrived = 8 * batch * kNormBlocks;
-  p.x0 = up(p.arrived + 4, 256);
+  p.x0 = up(p.arrived + 8, 256);
   p.x1 = p.x0 + xb;
   p.a = p.x1 + xb;
   p.b = p.a + ab;
@@ -582,6 +834,21 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   cudaStream_t st = (cudaStream_t)stream;
   const Plan p = plan_of(batch, rows, cols);
   const int tall = rows > cols, m = p.m, n = p.n;
+  const int e = dtype == CDGRAB_F32 ? 4 : 2;
+  const bool wide = cdg_aligned(g, 16) && gs % (16 / e) == 0 && gb % (16 / e) == 0 && cols % (16 / e) == 0;
+  if (m <= 128 && n <= kSmallCols) {
+    const SmallArgs a = {rows, cols, tall, steps, cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, coeffs[0], coeffs[1], coeffs[2], eps, gb, gs, ob, os,
+                         dev->status};
+    auto run = [&](auto *kernel, const auto *from, CdgPerDevice &flags) {
+      if (!tc_raise_limit(flags, kernel, small_smem(kSmallCols))) return (int)CDGRAB_ERR_CUDA;
+      return cdg_launch_rc(cdg_ops_launch(kernel, dim3(batch), kSmallThreads, small_smem(n), st, from, (__nv_bfloat16 *)o, a));
+    };
+    static CdgPerDevice flags[4];
+    if (dtype == CDGRAB_F32)
+      return wide ? run(orth_small<float, 4>, (const float *)g, flags[0]) : run(orth_small<float, 1>, (const float *)g, flags[1]);
+    return wide ? run(orth_small<__nv_bfloat16, 8>, (const __nv_bfloat16 *)g, flags[2])
+                : run(orth_small<__nv_bfloat16, 1>, (const __nv_bfloat16 *)g, flags[3]);
+  }
   char *w = (char *)up((long long)(uintptr_t)workspace, 256);
   double *part = (double *)(w + p.part);
   unsigned *arrived = (unsigned *)(w + p.arrived);
@@ -600,8 +867,6 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
     return CDGRAB_ERR_CUDA;
 
   const dim3 gt((cols + 63) / 64, (rows + 63) / 64, batch);
-  const int e = dtype == CDGRAB_F32 ? 4 : 2;
-  const bool wide = cdg_aligned(g, 16) && gs % (16 / e) == 0 && gb % (16 / e) == 0 && cols % (16 / e) == 0;
   int rc;
   auto begin = [&](auto *sumsq, auto *start, const auto *from) {
     const int r = cdg_launch_rc(cdg_ops_launch(sumsq, dim3(kNormBlocks, batch), 256, 0, st, from, gb, gs, rows, cols, part, arrived));

@@ -35,7 +35,8 @@ def check(g, **kw):
 
 @pytest.mark.parametrize("rows,cols", [(16, 16), (17, 40), (40, 17), (31, 33), (64, 64), (65, 64), (64, 200), (127, 129),
                                        (128, 128), (129, 257), (257, 129), (200, 1000), (1000, 200), (255, 384),
-                                       (650, 650), (500, 777), (1030, 640)])
+                                       (650, 650), (500, 777), (1030, 640), (128, 576), (576, 128), (128, 577), (100, 321), (449, 65), (64, 385),
+                                       (129, 130), (33, 515)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_shapes(rows, cols, dtype):
     check(gradient(1, rows, cols, dtype=dtype)[0])
