@@ -212,7 +212,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
   const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const long long deadline = clock64() + kCdgWaitCycles;
+  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
   const int columns = z.heads * z.batch;
 
   // the sequence's lengths and the key tiles that each query tile of a block sees
@@ -240,6 +240,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         int qn = 0, kn = 0, vn = 0;        // blocks and tiles issued
         int seq = 0;
         for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+          deadline = clock64() + kCdgWaitCycles;
           if (!(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
           const Block w = block(at);
           const Work k = work_of(w);
@@ -284,6 +285,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       int qn = 0, kn = 0, vn = 0, sn = 0, pn = 0, on = 0;      // blocks, tiles of K and V, products S_t and P_t V, blocks with any
       int seq = 0;
       for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
+        deadline = clock64() + kCdgWaitCycles;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.tiles == 0) continue;
@@ -347,6 +349,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     int qn = 0, sn = 0, gn = 0;          // blocks, score tiles of this half, and turns of both halves
     int seq = 0;
     for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
       const Block w = block(at);
       const Work k = work_of(w);
       const int mine = t == 0 ? k.n[0] : k.n[1], i = w.at + t * kT + row;
@@ -621,7 +624,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const long long deadline = clock64() + kCdgWaitCycles;
+  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
   const int columns = kv_heads * z.batch;
 
   // query tiles first .. first + per - 1 see a key of the block; over the heads of the group this CTA takes
@@ -646,8 +649,9 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       bool ok = true;
       int cn = 0, qn = 0, dn = 0, ln = 0;
       int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+      for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+        deadline = clock64() + kCdgWaitCycles;
+        if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
@@ -693,7 +697,8 @@ if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
     bool ok = true;
     int cn = 0, n = 0;                   // blocks and turns
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
       const Block w = block(at);
       const Work k = work_of(w);
       if (k.total == 0) continue;
@@ -756,7 +761,8 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(ba
     bool ok = true;
     int cn = 0, n = 0;
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
       const Block w = block(at);
       const Work k = work_of(w);
       const int j = w.at + row, off = k.lk - k.lq;
@@ -921,7 +927,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const long long deadline = clock64() + kCdgWaitCycles;
+  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
   const int columns = z.heads * z.batch;
 
   // key tiles rank, rank + ranks, ... of those that the block sees, `total` of them
@@ -944,8 +950,9 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         bool ok = true;
         int qn = 0, kn = 0, vn = 0;
         int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+        for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+          deadline = clock64() + kCdgWaitCycles;
+          if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.total == 0) continue;
@@ -983,7 +990,8 @@ if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
       bool ok = true;
       int qn = 0, n = 0;                 // blocks, and turns whose S (warp 9) or dq (warp 10) has been issued
       int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+        deadline = clock64() + kCdgWaitCycles;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
@@ -1045,7 +1053,8 @@ for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(ba
     bool ok = true;
     int qn = 0, n = 0;
     int seq = 0;
-for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
       const Block w = block(at);
       const Work k = work_of(w);
       const int i = w.at + row, keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;
