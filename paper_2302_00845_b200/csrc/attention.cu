@@ -532,7 +532,6 @@ __device__ __forceinline__ void load_line(uint32_t dst, const float *src, uint32
 // The rings are as deep as shared memory allows: a tile of Q (or K) is used twice, at the beginning and at
 // the end of its turn, and a copy takes about 1700 cycles; with two stages each the products waited for it
 // (3500 cycles a tile at 128 head dimensions).
-constexpr int kBwdThreads = 352;
 
 // Where there are few tiles of rows, the loop over the other axis is dealt out over a cluster of CTAs, whose
 // fp32 sums are joined through distributed shared memory, in the order of their ranks.
@@ -571,34 +570,36 @@ __device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, in
 // Scores are transposed (a row is a key), so that P^T and dS^T are the row operands of
 //   dv += P^T dO,  dk += dS^T Q,    with  S^T = K Q^T,  dP^T = V dO^T.
 // Summing over query tiles and heads in a fixed order makes the result the same bits every time.
-// Tensor memory: dv and dk from 256; the scores move between two regions of 128 columns.  In turn `it`
-// region it & 1 holds S, then, over each half's own scores, P and dS; the other one holds dP.  Once dP is in
-// registers, S of the next turn is computed in its place while dS is being formed; dP of the next turn
-// follows when both products of this one are over.
+// Tensor memory holds dv and dk and regions of 128 columns for the scores.  In turn n region n & 1 holds S, then,
+// over each half's own scores, P and dS.  Up to 64 head dimensions dP has a third region, so that S of the next
+// turn is computed while this one's P is formed.  Above, dP takes the region that S of this turn does not lie
+// in; once it is in registers, S of the next turn is computed in its place while dS is being formed, and dP of
+// the next turn follows when both products of this one are over.
 template <int NP> struct Dkv {
   static constexpr uint32_t tile = kT * 128 * NP;
-  static constexpr int kv_ring = NP == 1 ? 2 : 1, q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 3 : 2, line_ring = 2;
+  static constexpr int kv_ring = NP == 1 ? 2 : 1, q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 3 : 2, line_ring = NP == 1 ? 4 : 2;
+  static constexpr int threads = NP == 1 ? 384 : 352;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
   static constexpr uint32_t q = 2 * kv_ring * tile, d_o = q + q_ring * tile, lines = d_o + do_ring * tile, bars = lines + line_ring * line;
-  static constexpr size_t smem = bars + 320;
-  static constexpr uint32_t dv = 256, dk = 256 + 64 * NP;
+  static constexpr size_t smem = bars + 384;
+  static constexpr uint32_t dv = 512 - 128 * NP, dk = dv + 64 * NP;
 };
 template <int NP> struct DkvBars {
   TcQueue queue;
   uint64_t kv_full[Dkv<NP>::kv_ring], kv_empty[Dkv<NP>::kv_ring], q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring],
-      do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full, dp_full, dp_free, p_ready, ds_ready,
-      done, acc_free;
+      do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full[2], dp_full, dp_free,
+      p_ready[2], ds_ready[2], done[2], acc_free;       // [2]: even and odd turns
   uint32_t tmem;
 };
 
 template <int NP>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(Dkv<NP>::threads, 1)
 attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                  const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z, int blocks,
                  const float *__restrict__ lines, int padded, const View dk, const View dv) {
   typedef Dkv<NP> F;
   extern __shared__ __align__(1024) uint8_t base[];
-  static_assert(sizeof(DkvBars<NP>) <= 320, "barriers behind the tiles");
+  static_assert(sizeof(DkvBars<NP>) <= 384, "barriers behind the tiles");
   DkvBars<NP> &bar = *reinterpret_cast<DkvBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t s0 = smem_u32(base), sq = s0 + F::q, sdo = s0 + F::d_o;
@@ -611,9 +612,11 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
     for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 2); }
     for (int i = 0; i < F::line_ring; ++i) { mbar_init(smem_u32(&bar.line_full[i]), 1); mbar_init(smem_u32(&bar.line_empty[i]), 8); }
-    mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
-    mbar_init(smem_u32(&bar.dp_free), 8); mbar_init(smem_u32(&bar.done), 1);
-    mbar_init(smem_u32(&bar.p_ready), 8); mbar_init(smem_u32(&bar.ds_ready), 8);
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.s_full[i]), 1); mbar_init(smem_u32(&bar.done[i]), 1); }
+    mbar_init(smem_u32(&bar.dp_full), 1); mbar_init(smem_u32(&bar.dp_free), 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bar.p_ready[i]), 8); mbar_init(smem_u32(&bar.ds_ready[i]), 8);
+    }
     mbar_init(smem_u32(&bar.acc_free), 8);
     mbar_init_fence();
   }
@@ -622,6 +625,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tm = bar.tmem;
+  const auto dp_at = [](int n) { return NP == 1 ? 256u : (uint32_t)(~n & 1) * kT; };
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
@@ -639,121 +643,150 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     k.total = (k.per * z.group - rank + ranks - 1) / ranks;
     return k;
   };
-  auto query0 = [&](const Work &k, int it) { return (k.first + (rank + it * ranks) % k.per) * kT; };
+  // where the loop stands: query tile first + tile of head `head` of the group
+  struct Turn { int head, tile; };
+  auto step = [&](Turn &t, const Work &k, int by) {
+    for (t.tile += by; t.tile >= k.per; t.tile -= k.per) ++t.head;
+  };
+  auto start = [&](const Work &k) {
+    Turn t = {0, 0};
+    if (k.total > 0) step(t, k, rank);
+    return t;
+  };
+  auto query0 = [&](const Work &k, const Turn &t) { return (k.first + t.tile) * kT; };
   // the first keys are seen by the most queries; a cluster takes one block and asks for no more
   auto block = [&](long long at) { return block_of(at, kv_heads, columns, blocks, kT, false); };
   const long long mine0 = blockIdx.x / ranks;
 
-  if (warp == 8) {
-    if (tc_elect()) {
+  if (warp >= 8) {
+    if (NP == 1) tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+    if (warp == 8) {
+      if (tc_elect()) {
+        bool ok = true;
+        int cn = 0, qn = 0, dn = 0, ln = 0;
+        int seq = 0;
+        for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+          deadline = clock64() + kCdgWaitCycles;
+          if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+          const Block w = block(at);
+          const Work k = work_of(w);
+          if (k.total == 0) continue;
+          if (!(ok = tc_wait_released(bar.kv_empty, cn, F::kv_ring, deadline))) break;
+          uint64_t *full = &bar.kv_full[cn % F::kv_ring];
+          const uint32_t kv = s0 + cn % F::kv_ring * 2 * F::tile;
+          mbar_expect_tx(smem_u32(full), 2 * F::tile);
+          load_tile<NP>(kv, &mk, w.at, w.h, batch_of(z, kK, w.b), smem_u32(full));
+          load_tile<NP>(kv + F::tile, &mv, w.at, w.h, batch_of(z, kV, w.b), smem_u32(full));
+          ++cn;
+          Turn t = start(k);
+          for (int it = 0; it < k.total; ++it, step(t, k, ranks)) {
+            const int h = w.h * z.group + t.head, i0 = query0(k, t);
+            if (!(ok = tc_wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
+            full = &bar.q_full[qn % F::q_ring];
+            mbar_expect_tx(smem_u32(full), F::tile);
+            load_tile<NP>(sq + qn % F::q_ring * F::tile, &mq, i0, h, batch_of(z, kQ, w.b), smem_u32(full));
+            ++qn;
+            if (!(ok = tc_wait_released(bar.line_empty, ln, F::line_ring, deadline))) break;
+            full = &bar.line_full[ln % F::line_ring];
+            const float *line = lines + ((long long)w.b * z.heads + h) * 2 * padded + i0;
+            float *to = sline + ln % F::line_ring * 2 * kT;
+            mbar_expect_tx(smem_u32(full), F::line);
+            load_line(smem_u32(to), line, smem_u32(full));
+            load_line(smem_u32(to + kT), line + padded, smem_u32(full));
+            ++ln;
+            if (!(ok = tc_wait_released(bar.do_empty, dn, F::do_ring, deadline))) break;
+            full = &bar.do_full[dn % F::do_ring];
+            mbar_expect_tx(smem_u32(full), F::tile);
+            load_tile<NP>(sdo + dn % F::do_ring * F::tile, &mdo, i0, h, batch_of(z, kDo, w.b), smem_u32(full));
+            ++dn;
+          }
+        }
+        if (!ok) {
+          atomicOr(z.status, CDG_ST_TIMEOUT);
+          if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
+          tc_drain(bar.kv_full, cn, F::kv_ring);
+          tc_drain(bar.q_full, qn, F::q_ring);
+          tc_drain(bar.line_full, ln, F::line_ring);
+          tc_drain(bar.do_full, dn, F::do_ring);
+        }
+      }
+    } else if (warp <= 10) {
       bool ok = true;
-      int cn = 0, qn = 0, dn = 0, ln = 0;
+      int cn = 0, n = 0;                   // blocks and turns
       int seq = 0;
-      for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
+      for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
         deadline = clock64() + kCdgWaitCycles;
-        if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
-        if (!(ok = tc_wait_released(bar.kv_empty, cn, F::kv_ring, deadline))) break;
-        uint64_t *full = &bar.kv_full[cn % F::kv_ring];
-        const uint32_t kv = s0 + cn % F::kv_ring * 2 * F::tile;
-        mbar_expect_tx(smem_u32(full), 2 * F::tile);
-        load_tile<NP>(kv, &mk, w.at, w.h, batch_of(z, kK, w.b), smem_u32(full));
-        load_tile<NP>(kv + F::tile, &mv, w.at, w.h, batch_of(z, kV, w.b), smem_u32(full));
+        // a tile has landed; its rows past the sequence's queries are zeroed (by either warp, each before its own product)
+        auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, const Turn &t, int m) {
+          const int s = m % ring, left = k.lq - query0(k, t);
+          if (!tc_wait(&full[s], tc_parity(m, ring), deadline)) return false;
+          if (z.q_lens && left < kT) zero_rows<NP>(base + tiles + s * F::tile, left);
+          return true;
+        };
+        const uint32_t sk = s0 + cn % F::kv_ring * 2 * F::tile, sv = sk + F::tile;
+        if (warp == 9) {
+          if (!(ok = tc_wait(&bar.kv_full[cn % F::kv_ring], tc_parity(cn, F::kv_ring), deadline))) break;
+          // S of turn `t`, number m: its region was last used by the products of turn m - 2, or by dP of turn m - 1
+          auto scores = [&](const Turn &t, int m) {
+            if (!arrived(bar.q_full, F::q, F::q_ring, t, m)) return false;
+            if (NP == 1 ? m > 1 && !tc_wait(&bar.done[m & 1], tc_parity(m - 2, 2), deadline)
+                        : m > 0 && !tc_wait(&bar.dp_free, (m - 1) & 1, deadline)) return false;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_scores<NP>(tm + (m & 1) * kT, sk, sq + m % F::q_ring * F::tile);
+              tc_commit(&bar.s_full[m & 1]);
+            }
+            __syncwarp();
+            return true;
+          };
+          Turn t = start(k);
+          ok = scores(t, n);
+          for (int it = 0; it < k.total && ok; ++it, ++n) {
+            if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, t, n))) break;
+            if (n > 0 && !(ok = NP == 1 ? tc_wait(&bar.dp_free, (n - 1) & 1, deadline)
+                                        : tc_wait(&bar.done[(n - 1) & 1], tc_parity(n - 1, 2), deadline))) break;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_scores<NP>(tm + dp_at(n), sv, sdo + n % F::do_ring * F::tile);
+              tc_commit(&bar.dp_full);
+              tc_commit(&bar.do_empty[n % F::do_ring]);
+            }
+            __syncwarp();
+            step(t, k, ranks);
+            ok = it + 1 == k.total || scores(t, n + 1);
+          }
+          if (!ok) break;
+        } else {
+          Turn t = start(k);
+          for (int it = 0; it < k.total; ++it, ++n, step(t, k, ranks)) {
+            const uint32_t here = tm + (n & 1) * kT;
+            if (it == 0 && cn > 0 && !(ok = tc_wait(&bar.acc_free, (cn - 1) & 1, deadline))) break;
+            if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, t, n) && tc_wait(&bar.p_ready[n & 1], tc_parity(n, 2), deadline))) break;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_rows<NP>(tm + F::dv, here, 64, sdo + n % F::do_ring * F::tile, it > 0);
+              tc_commit(&bar.do_empty[n % F::do_ring]);
+            }
+            __syncwarp();
+            if (!(ok = tc_wait(&bar.ds_ready[n & 1], tc_parity(n, 2), deadline))) break;
+            tc_fence_after();
+            if (tc_elect()) {
+              mma_rows<NP>(tm + F::dk, here + 32, 64, sq + n % F::q_ring * F::tile, it > 0);
+              tc_commit(&bar.done[n & 1]);
+              tc_commit(&bar.q_empty[n % F::q_ring]);
+            }
+            __syncwarp();
+          }
+        }
         ++cn;
-        for (int it = 0; it < k.total; ++it) {
-          const int h = w.h * z.group + (rank + it * ranks) / k.per, i0 = query0(k, it);
-          if (!(ok = tc_wait_released(bar.q_empty, qn, F::q_ring, deadline))) break;
-          full = &bar.q_full[qn % F::q_ring];
-          mbar_expect_tx(smem_u32(full), F::tile);
-          load_tile<NP>(sq + qn % F::q_ring * F::tile, &mq, i0, h, batch_of(z, kQ, w.b), smem_u32(full));
-          ++qn;
-          if (!(ok = tc_wait_released(bar.line_empty, ln, F::line_ring, deadline))) break;
-          full = &bar.line_full[ln % F::line_ring];
-          const float *line = lines + ((long long)w.b * z.heads + h) * 2 * padded + i0;
-          float *to = sline + ln % F::line_ring * 2 * kT;
-          mbar_expect_tx(smem_u32(full), F::line);
-          load_line(smem_u32(to), line, smem_u32(full));
-          load_line(smem_u32(to + kT), line + padded, smem_u32(full));
-          ++ln;
-          if (!(ok = tc_wait_released(bar.do_empty, dn, F::do_ring, deadline))) break;
-          full = &bar.do_full[dn % F::do_ring];
-          mbar_expect_tx(smem_u32(full), F::tile);
-          load_tile<NP>(sdo + dn % F::do_ring * F::tile, &mdo, i0, h, batch_of(z, kDo, w.b), smem_u32(full));
-          ++dn;
-        }
       }
-      if (!ok) {
-        atomicOr(z.status, CDG_ST_TIMEOUT);
-        if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
-        tc_drain(bar.kv_full, cn, F::kv_ring);
-        tc_drain(bar.q_full, qn, F::q_ring);
-        tc_drain(bar.line_full, ln, F::line_ring);
-        tc_drain(bar.do_full, dn, F::do_ring);
-      }
+      if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     }
-  } else if (warp >= 9) {
-    bool ok = true;
-    int cn = 0, n = 0;                   // blocks and turns
-    int seq = 0;
-    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
-      const Block w = block(at);
-      const Work k = work_of(w);
-      if (k.total == 0) continue;
-      // a tile has landed; its rows past the sequence's queries are zeroed (by either warp, each before its own product)
-      auto arrived = [&](uint64_t *full, uint32_t tiles, int ring, int it) {
-        const int s = n % ring, left = k.lq - query0(k, it);
-        if (!tc_wait(&full[s], tc_parity(n, ring), deadline)) return false;
-        if (z.q_lens && left < kT) zero_rows<NP>(base + tiles + s * F::tile, left);
-        return true;
-      };
-      const uint32_t sk = s0 + cn % F::kv_ring * 2 * F::tile, sv = sk + F::tile;
-      if (warp == 9) {
-        if (!(ok = tc_wait(&bar.kv_full[cn % F::kv_ring], tc_parity(cn, F::kv_ring), deadline))) break;
-        for (int it = 0; it < k.total; ++it, ++n) {
-          if (!(ok = arrived(bar.q_full, F::q, F::q_ring, it) && (n == 0 || tc_wait(&bar.dp_free, (n - 1) & 1, deadline)))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_scores<NP>(tm + (n & 1) * kT, sk, sq + n % F::q_ring * F::tile);
-            tc_commit(&bar.s_full);
-          }
-          __syncwarp();
-          if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, it) && (n == 0 || tc_wait(&bar.done, (n - 1) & 1, deadline)))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_scores<NP>(tm + (~n & 1) * kT, sv, sdo + n % F::do_ring * F::tile);
-            tc_commit(&bar.dp_full);
-            tc_commit(&bar.do_empty[n % F::do_ring]);
-          }
-          __syncwarp();
-        }
-      } else {
-        for (int it = 0; it < k.total; ++it, ++n) {
-          const uint32_t here = tm + (n & 1) * kT;
-          if (it == 0 && cn > 0 && !(ok = tc_wait(&bar.acc_free, (cn - 1) & 1, deadline))) break;
-          if (!(ok = arrived(bar.do_full, F::d_o, F::do_ring, it) && tc_wait(&bar.p_ready, n & 1, deadline))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_rows<NP>(tm + F::dv, here, 64, sdo + n % F::do_ring * F::tile, it > 0);
-            tc_commit(&bar.do_empty[n % F::do_ring]);
-          }
-          __syncwarp();
-          if (!(ok = tc_wait(&bar.ds_ready, n & 1, deadline))) break;
-          tc_fence_after();
-          if (tc_elect()) {
-            mma_rows<NP>(tm + F::dk, here + 32, 64, sq + n % F::q_ring * F::tile, it > 0);
-            tc_commit(&bar.done);
-            tc_commit(&bar.q_empty[n % F::q_ring]);
-          }
-          __syncwarp();
-        }
-      }
-      ++cn;
-    }
-    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
+    if (NP == 1) tc_regs_up<224>();
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16), mine = lanes + half * 64;
     const float a = z.negative ? -z.a : z.a;
@@ -766,11 +799,16 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       const Block w = block(at);
       const Work k = work_of(w);
       const int j = w.at + row, off = k.lk - k.lq;
-      for (int it = 0; it < k.total; ++it, ++n) {
-        const int ls = n % F::line_ring, i0 = query0(k, it) + half * 64;
-        const uint32_t here = mine + (n & 1) * kT, there = mine + (~n & 1) * kT;
+      Turn t = start(k);
+      for (int it = 0; it < k.total; ++it, ++n, step(t, k, ranks)) {
+        const int ls = n % F::line_ring, i0 = query0(k, t) + half * 64;
+        const uint32_t here = mine + (n & 1) * kT, there = mine + dp_at(n);
         const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
-        if (!(ok = tc_wait(&bar.line_full[ls], tc_parity(n, F::line_ring), deadline) && tc_wait(&bar.s_full, n & 1, deadline))) break;
+        if (!(ok = tc_wait(&bar.line_full[ls], tc_parity(n, F::line_ring), deadline))) break;
+        float4 l[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) l[e] = *reinterpret_cast<const float4 *>(l2 + 4 * e);
+        if (!(ok = tc_wait(&bar.s_full[n & 1], tc_parity(n, 2), deadline))) break;
         tc_fence_after();
         uint32_t v[2][32], u[32];
         tc_load32(here, v[0]);
@@ -778,14 +816,11 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         tc_wait_ld();
         float p[64];
 #pragma unroll
-        for (int e = 0; e < 64; e += 8) {
-          const float4 l = *reinterpret_cast<const float4 *>(l2 + e), m = *reinterpret_cast<const float4 *>(l2 + e + 4);
-          const float2 x0 = exp2_two(fma2(two(v, e), aa, make_float2(l.x, l.y)));
-          const float2 x1 = exp2_two(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
-          const float2 x2 = exp2_two(fma2(two(v, e + 4), aa, make_float2(m.x, m.y)));
-          const float2 x3 = exp2_two(fma2(two(v, e + 6), aa, make_float2(m.z, m.w)));
-          p[e] = x0.x; p[e + 1] = x0.y; p[e + 2] = x1.x; p[e + 3] = x1.y;
-          p[e + 4] = x2.x; p[e + 5] = x2.y; p[e + 6] = x3.x; p[e + 7] = x3.y;
+        for (int e = 0; e < 64; e += 4) {
+          const float4 m = l[e / 4 & 7];
+          if (e < 32) l[e / 4] = *reinterpret_cast<const float4 *>(l2 + 32 + e);
+          const float2 x = exp2_two(fma2(two(v, e), aa, make_float2(m.x, m.y))), y = exp2_two(fma2(two(v, e + 2), aa, make_float2(m.z, m.w)));
+          p[e] = x.x; p[e + 1] = x.y; p[e + 2] = y.x; p[e + 3] = y.y;
         }
         // under the causal rule key j is seen by queries from j - off on
         const int from = z.causal ? j - off - i0 : 0;
@@ -799,7 +834,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         tc_store32(here, u);
         tc_wait_st();
         tc_fence_before();
-        tc_warp_arrive(&bar.p_ready);
+        tc_warp_arrive(&bar.p_ready[n & 1]);
         if (!(ok = tc_wait(&bar.dp_full, n & 1, deadline))) break;
         tc_fence_after();
         tc_load32(there, v[0]);
@@ -818,7 +853,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         tc_store32(here + 32, u);
         tc_wait_st();
         tc_fence_before();
-        tc_warp_arrive(&bar.ds_ready);
+        tc_warp_arrive(&bar.ds_ready[n & 1]);
         if (lane == 0) mbar_arrive(smem_u32(&bar.line_empty[ls]));
       }
       if (!ok) break;
@@ -826,7 +861,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       const View &out = half ? dk : dv;
       const float f = half ? z.scale : 1.0f;
       bf16 *dst = out.p + (long long)w.b * out.b + (long long)w.h * out.h;
-      if (k.total > 0 && !(ok = tc_wait(&bar.done, (n - 1) & 1, deadline))) break;
+      if (k.total > 0 && !(ok = tc_wait(&bar.done[(n - 1) & 1], tc_parity(n - 1, 2), deadline))) break;
       tc_fence_after();
       if (ranks > 1 || k.total > 0) {
         uint8_t *tile = base + (ranks > 1 ? half * 2 : cn % F::kv_ring * 2 + half) * F::tile;
@@ -892,7 +927,7 @@ template <int NP> struct Dq {
 template <int NP> struct DqBars {
   TcQueue queue;
   uint64_t q_full[Dq<NP>::q_ring], q_empty[Dq<NP>::q_ring], k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring],
-      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready, dq_done[2], acc_free;
+      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready[2], dq_done[2], acc_free;       // [2]: even and odd turns
   uint32_t tmem;
 };
 
@@ -916,8 +951,8 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
-    mbar_init(smem_u32(&bar.ds_ready), 8); mbar_init(smem_u32(&bar.acc_free), 8);
-    mbar_init(smem_u32(&bar.dq_done[0]), 1); mbar_init(smem_u32(&bar.dq_done[1]), 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1);}
+    mbar_init(smem_u32(&bar.acc_free), 8);
     mbar_init_fence();
   }
   if (warp == 9) tc_alloc(&bar.tmem, 512);
@@ -1030,7 +1065,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
           for (int it = 0; it < k.total; ++it, ++n) {
             const int ks = n % F::k_ring;
             if (it == 0 && qn > 0 && !(ok = tc_wait(&bar.acc_free, (qn - 1) & 1, deadline))) break;
-            if (!(ok = tc_wait(&bar.ds_ready, n & 1, deadline))) break;
+            if (!(ok = tc_wait(&bar.ds_ready[n & 1], tc_parity(n, 2), deadline))) break;
             tc_fence_after();
             if (tc_elect()) {
               mma_rows<NP>(tm + F::dq, tm + F::ds + (n & 1) * 64, 32, sk + ks * F::tile, it > 0);
@@ -1117,7 +1152,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_store32(lanes + F::ds + (n & 1) * 64 + half * 32, x);
         tc_wait_st();
         tc_fence_before();
-        tc_warp_arrive(&bar.ds_ready);
+        tc_warp_arrive(&bar.ds_ready[n & 1]);
       }
       if (!ok) break;
       bf16 *dst = dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h;
@@ -1262,7 +1297,7 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
     const long long all = (long long)kt * s->kv_heads * s->batch;
     if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of((double)qt * z.group, part * qt * z.group, all, sms);
-    rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
+    rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, Dkv<NP>::threads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
                         dk, dv);
   }
   if (rc == CDGRAB_OK && qt > 0) {

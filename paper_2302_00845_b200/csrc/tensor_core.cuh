@@ -53,9 +53,18 @@ __device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint64_t b, ui
 __device__ __forceinline__ void tc_commit(uint64_t *bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// bounded wait of a whole warp; false in all its lanes when it expired in one
+// bounded wait of a whole warp, whose lanes stay together; false when it expired
 __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity, long long deadline) {
-  return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, deadline));
+  while (true) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    if (__all_sync(0xffffffffu, done)) return true;
+    if (__any_sync(0xffffffffu, clock64() > deadline)) return false;
+  }
 }
 // tile from shared memory to a tensor (one thread; coordinates inside the tensor); the end of a group of such
 // copies, and waits for this thread's groups: all but the last to have read shared memory, all to be written
