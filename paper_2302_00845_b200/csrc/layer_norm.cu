@@ -192,7 +192,7 @@ ln_backward(long long rows, long long per, int cols, const T *dy, long long dys,
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  float sw[NV][VEC] = {}, sb[NV][VEC] = {};
+  float2 sw[E / 2] = {}, sb[E / 2] = {};
   if (ringed) {
 #pragma unroll
     for (int k = 0; k < kAhead - 1; ++k) request(r + k * step, k);
@@ -200,55 +200,95 @@ ln_backward(long long rows, long long per, int cols, const T *dy, long long dys,
   float mu = 0.0f, rs = 0.0f;
   if (r < end) { mu = mean[r]; rs = rstd[r]; }
   for (int stage = 0; r < end; r += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
-    raw cx[NV], cd[NV];
     if (E > 24) asm volatile("" ::: "memory");       // the weight is read again for each row: it would not fit in registers
     if (ringed) {
       request(r + (kAhead - 1) * step, stage == 0 ? kAhead - 1 : stage - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (l + i * span < nv) {
-        cx[i] = ringed ? ring[(stage * 2 * NV + i) * span] : reinterpret_cast<const raw *>(x + r * xs)[l + i * span];
-        cd[i] = ringed ? ring[(stage * 2 * NV + NV + i) * span] : reinterpret_cast<const raw *>(dy + r * dys)[l + i * span];
-      }
     float mu_next = 0.0f, rs_next = 0.0f;
     if (r + step < end) { mu_next = mean[r + step]; rs_next = rstd[r + step]; }
-    float s1 = 0.0f, s2 = 0.0f;
+    // past the row's end x, dy and w are 0, and with them every term.  Between the two passes x stays as it was
+    // read and g = dy w in fp32, up to 24 values a thread; reading dy and w again cost half of the shared
+    // memory's and L1's bandwidth
+    raw cx[NV] = {};
+    auto dy_of = [&](int i) {
+      return ringed ? ring[(stage * 2 * NV + NV + i) * span] : reinterpret_cast<const raw *>(dy + r * dys)[l + i * span];
+    };
+    float2 g[E / 2], s1 = make_float2(0.0f, 0.0f), s2 = s1;
+    const float2 off = make_float2(-mu, -mu), by = make_float2(rs, rs);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = l + i * span;
+      raw cd = {};
+      float fx[VEC], fd[VEC], fw[VEC] = {};
       if (c < nv) {
-        float fw[VEC], n[VEC], g[VEC];
-        V::open(cx[i], n);
-        V::open(cd[i], g);
+        cx[i] = ringed ? ring[(stage * 2 * NV + i) * span] : reinterpret_cast<const raw *>(x + r * xs)[c];
+        cd = dy_of(i);
         param<VEC>(w, c * VEC, 1.0f, fw);
+      }
+      V::open(cx[i], fx);
+      V::open(cd, fd);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          n[e] = (n[e] - mu) * rs;
-          sw[i][e] = fmaf(g[e], n[e], sw[i][e]);
-          sb[i][e] += g[e];
-          g[e] *= fw[e];
-          s1 += g[e];
-          s2 = fmaf(g[e], n[e], s2);
+      for (int e = 0; e < VEC; e += 2) {
+        const int k = (i * VEC + e) / 2;
+        if (VEC == 1 && i % 2 == 1) {                // the other half of the pair before
+          const float n = (fx[0] - mu) * rs;
+          sw[k].y = fmaf(fd[0], n, sw[k].y);
+          sb[k].y += fd[0];
+          g[k].y = fd[0] * fw[0];
+          s1.y += g[k].y;
+          s2.y = fmaf(g[k].y, n, s2.y);
+        } else if (VEC == 1) {
+          const float n = (fx[0] - mu) * rs;
+          sw[k].x = fmaf(fd[0], n, sw[k].x);
+          sb[k].x += fd[0];
+          g[k].x = fd[0] * fw[0];
+          s1.x += g[k].x;
+          s2.x = fmaf(g[k].x, n, s2.x);
+        } else {
+          const int f = (e + 1) % VEC;
+          const float2 n = mul2(add2(make_float2(fx[e], fx[f]), off), by), d = make_float2(fd[e], fd[f]);
+          sw[k] = fma2(d, n, sw[k]);
+          sb[k] = add2(sb[k], d);
+          g[k] = mul2(d, make_float2(fw[e], fw[f]));
+          s1 = add2(s1, g[k]);
+          s2 = fma2(g[k], n, s2);
         }
       }
     }
     if (dx) {
-      const float2 t = row_sum<BLOCK>(s1, s2, sm);
-      const float c1 = t.x * inv, c2 = t.y * inv;
+      if (E > 24) asm volatile("" ::: "memory");
+      const float2 t = row_sum<BLOCK>(s1.x + s1.y, s2.x + s2.y, sm);
+      const float2 c1 = make_float2(-t.x * inv, -t.x * inv), c2 = make_float2(-t.y * inv, -t.y * inv);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = l + i * span;
         if (c < nv) {
-          float fw[VEC], n[VEC], g[VEC];
-          V::open(cx[i], n);
-          V::open(cd[i], g);
-          param<VEC>(w, c * VEC, 1.0f, fw);
+          float fx[VEC], fd[VEC], fw[VEC];
+          V::open(cx[i], fx);
+          if (E > 24) {
+            V::open(dy_of(i), fd);
+            param<VEC>(w, c * VEC, 1.0f, fw);
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) g[e] = rs * (g[e] * fw[e] - c1 - (n[e] - mu) * rs * c2);
-          reinterpret_cast<raw *>(dx + r * dxs)[c] = V::close(g);
+            for (int e = 0; e < VEC; ++e) {
+              const int k = i * VEC + e;
+              (k % 2 ? g[k / 2].y : g[k / 2].x) = fd[e] * fw[e];
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < VEC; e += 2) {
+            const int k = (i * VEC + e) / 2, f = (e + 1) % VEC;
+            if (VEC == 1) {
+              fx[0] = rs * ((i % 2 ? g[k].y : g[k].x) + c1.x + (fx[0] - mu) * rs * c2.x);
+            } else {
+              const float2 n = mul2(add2(make_float2(fx[e], fx[f]), off), by), d = mul2(by, fma2(n, c2, add2(g[k], c1)));
+              fx[e] = d.x;
+              fx[f] = d.y;
+            }
+          }
+          reinterpret_cast<raw *>(dx + r * dxs)[c] = V::close(fx);
         }
+        if (E > 24) asm volatile("" ::: "memory");
       }
     }
     mu = mu_next;
@@ -272,7 +312,10 @@ ln_backward(long long rows, long long per, int cols, const T *dy, long long dys,
     for (int i = 0; i < NV; ++i)
       if (l + i * span < nv) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) put((l + i * span) * VEC + e, sw[i][e], sb[i][e]);
+        for (int e = 0; e < VEC; ++e) {
+          const int k = i * VEC + e;
+          put((l + i * span) * VEC + e, k % 2 ? sw[k / 2].y : sw[k / 2].x, k % 2 ? sb[k / 2].y : sb[k / 2].x);
+        }
       }
     return;
   }
@@ -280,12 +323,10 @@ ln_backward(long long rows, long long per, int cols, const T *dy, long long dys,
   float *sums = reinterpret_cast<float *>(dyn);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      sums[(warp * 2 * E + i * VEC + e) * 32 + l] = sw[i][e];
-      sums[(warp * 2 * E + E + i * VEC + e) * 32 + l] = sb[i][e];
-    }
+  for (int k = 0; k < E; ++k) {
+    sums[(warp * 2 * E + k) * 32 + l] = k % 2 ? sw[k / 2].y : sw[k / 2].x;
+    sums[(warp * 2 * E + E + k) * 32 + l] = k % 2 ? sb[k / 2].y : sb[k / 2].x;
+  }
   __syncthreads();
   for (int k = warp; k < E; k += kWarps) {
     const int c = (l + k / VEC * 32) * VEC + k % VEC;
