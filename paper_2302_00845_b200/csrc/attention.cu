@@ -131,8 +131,8 @@ __device__ __forceinline__ void write_zeros(int row0, int rows, int token0, int 
 // ring of R uses stage n % R in the phase of tc_parity(n, R).
 struct Block { int at, h, b; };         // first row, head, sequence
 __device__ __forceinline__ Block block_of(long long w, int heads, int columns, int blocks, int rows, bool last_first) {
-  const int c = (int)(w % columns), k = (int)(w / columns);
-  return Block{(last_first ? blocks - 1 - k : k) * rows, c % heads, c / heads};
+  const unsigned u = (unsigned)w, c = u % (unsigned)columns, k = u / (unsigned)columns;         // w: below 2^31, like any grid
+  return Block{(last_first ? blocks - 1 - (int)k : (int)k) * rows, (int)(c % (unsigned)heads), (int)(c / (unsigned)heads)};
 }
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per 256 queries of a head: two tiles of 128 that share every key and value tile, so that while
@@ -555,10 +555,10 @@ __device__ __forceinline__ void join_sums(uint32_t sums, int ranks, int rank, in
 // turn is computed while this one's P is formed.  Above, dP takes the region that S of this turn does not lie
 // in; once it is in registers, S of the next turn is computed in its place while dS is being formed, and dP of
 // the next turn follows when both products of this one are over.
+constexpr int kBwdThreads = 512;       // 128 registers a thread at launch: 128 x 56 + 128 x 88 + 256 x 184 after they are moved
 template <int NP> struct Dkv {
   static constexpr uint32_t tile = kT * 128 * NP;
   static constexpr int kv_ring = NP == 1 ? 2 : 1, q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 3 : 2, line_ring = NP == 1 ? 4 : 2;
-  static constexpr int threads = NP == 1 ? 384 : 352;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
   static constexpr uint32_t q = 2 * kv_ring * tile, d_o = q + q_ring * tile, lines = d_o + do_ring * tile, bars = lines + line_ring * line;
   static constexpr size_t smem = bars + 384;
@@ -568,12 +568,12 @@ template <int NP> struct DkvBars {
   TcQueue queue;
   uint64_t kv_full[Dkv<NP>::kv_ring], kv_empty[Dkv<NP>::kv_ring], q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring],
       do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full[2], dp_full, dp_free,
-      p_ready[2], ds_ready[2], done[2], acc_free;       // [2]: even and odd turns
+      p_ready[2], ds_ready[2], done[2], block_done, acc_free;       // [2]: even and odd turns
   uint32_t tmem;
 };
 
 template <int NP>
-__global__ void __launch_bounds__(Dkv<NP>::threads, 1)
+__global__ void __launch_bounds__(kBwdThreads, 1)
 attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                  const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z, int blocks,
                  const float *__restrict__ lines, int padded, const View dk, const View dv) {
@@ -587,8 +587,8 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank(), kv_heads = z.heads / z.group;
 
   if (threadIdx.x == 0) {
-    tc_queue_init(bar.queue, 11);
-    for (int i = 0; i < F::kv_ring; ++i) { mbar_init(smem_u32(&bar.kv_full[i]), 1); mbar_init(smem_u32(&bar.kv_empty[i]), 8); }
+    tc_queue_init(bar.queue, 15);
+    for (int i = 0; i < F::kv_ring; ++i) { mbar_init(smem_u32(&bar.kv_full[i]), 1); mbar_init(smem_u32(&bar.kv_empty[i]), 4); }
     for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 1); }
     for (int i = 0; i < F::do_ring; ++i) { mbar_init(smem_u32(&bar.do_full[i]), 1); mbar_init(smem_u32(&bar.do_empty[i]), 2); }
     for (int i = 0; i < F::line_ring; ++i) { mbar_init(smem_u32(&bar.line_full[i]), 1); mbar_init(smem_u32(&bar.line_empty[i]), 8); }
@@ -597,7 +597,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bar.p_ready[i]), 8); mbar_init(smem_u32(&bar.ds_ready[i]), 8);
     }
-    mbar_init(smem_u32(&bar.acc_free), 8);
+    mbar_init(smem_u32(&bar.block_done), 1); mbar_init(smem_u32(&bar.acc_free), 4);
     mbar_init_fence();
   }
   if (warp == 9) tc_alloc(&bar.tmem, 512);
@@ -638,8 +638,8 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   auto block = [&](long long at) { return block_of(at, kv_heads, columns, blocks, kT, false); };
   const long long mine0 = blockIdx.x / ranks;
 
-  if (warp >= 8) {
-    if (NP == 1) tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+  if (warp >= 8 && warp < 12) {
+    tc_regs_down<56>();
     if (warp == 8) {
       if (tc_elect()) {
         bool ok = true;
@@ -756,6 +756,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             if (tc_elect()) {
               mma_rows<NP>(tm + F::dk, here + 32, 64, sq + n % F::q_ring * F::tile, it > 0);
               tc_commit(&bar.done[n & 1]);
+              if (it + 1 == k.total) tc_commit(&bar.block_done);
               tc_commit(&bar.q_empty[n % F::q_ring]);
             }
             __syncwarp();
@@ -765,14 +766,69 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       }
       if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     }
+  } else if (warp >= 12) {
+    tc_regs_down<88>();
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16);
+    bool ok = true;
+    int cn = 0;
+    int seq = 0;
+    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
+      const Block w = block(at);
+      const Work k = work_of(w);
+      const int j = w.at + row;
+      // through shared memory that no product reads any more
+      if (k.total > 0 && !(ok = tc_wait(&bar.block_done, cn & 1, deadline))) break;
+      tc_fence_after();
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        const View &out = which ? dk : dv;
+        const float f = which ? z.scale : 1.0f;
+        bf16 *dst = out.p + (long long)w.b * out.b + (long long)w.h * out.h;
+        if (ranks == 1 && k.total == 0) {
+          write_zeros<NP>((warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
+          continue;
+        }
+        uint8_t *tile = base + (ranks > 1 ? which * 2 : cn % F::kv_ring * 2 + which) * F::tile;
+#pragma unroll
+        for (int c = 0; c < 2 * NP; ++c) {
+          uint32_t v[32] = {}, u[16];
+          if (k.total > 0) {
+            tc_load32(lanes + (which ? F::dk : F::dv) + c * 32, v);
+            tc_wait_ld();
+          }
+          if (ranks > 1) {
+            keep_sums<NP>(tile, row, c * 32, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = j < k.lk ? pack(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f) : 0u;
+            stage_row<NP>(tile, row, c * 32, u);
+          }
+        }
+      }
+      if (ranks == 1 && k.total > 0) {
+        tc_fence_before();
+        tc_warp_arrive(&bar.acc_free);
+        for (int which = 0; which < 2; ++which) {
+          const View &out = which ? dk : dv;
+          write_rows<NP>(base + (cn % F::kv_ring * 2 + which) * F::tile, (warp & 3) * 32, 32, w.at, z.tk, z,
+                         out.p + (long long)w.b * out.b + (long long)w.h * out.h, out.t);
+        }
+        tc_proxy_fence();              // the next copy into the tiles comes after these reads
+        tc_warp_arrive(&bar.kv_empty[cn % F::kv_ring]);
+        ++cn;
+      }
+    }
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
-    if (NP == 1) tc_regs_up<224>();
+    tc_regs_up<184>();
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16), mine = lanes + half * 64;
     const float a = z.negative ? -z.a : z.a;
     const float2 aa = make_float2(a, a);
     bool ok = true;
-    int cn = 0, n = 0;
+    int n = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
       deadline = clock64() + kCdgWaitCycles;
@@ -785,9 +841,6 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         const uint32_t here = mine + (n & 1) * kT, there = mine + dp_at(n);
         const float *l2 = sline + ls * 2 * kT + half * 64, *delta = l2 + kT;
         if (!(ok = tc_wait(&bar.line_full[ls], tc_parity(n, F::line_ring), deadline))) break;
-        float4 l[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) l[e] = *reinterpret_cast<const float4 *>(l2 + 4 * e);
         if (!(ok = tc_wait(&bar.s_full[n & 1], tc_parity(n, 2), deadline))) break;
         tc_fence_after();
         uint32_t v[2][32], u[32];
@@ -797,9 +850,8 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         float p[64];
 #pragma unroll
         for (int e = 0; e < 64; e += 4) {
-          const float4 m = l[e / 4 & 7];
-          if (e < 32) l[e / 4] = *reinterpret_cast<const float4 *>(l2 + 32 + e);
-          const float2 x = exp2_two(fma2(two(v, e), aa, make_float2(m.x, m.y))), y = exp2_two(fma2(two(v, e + 2), aa, make_float2(m.z, m.w)));
+          const float4 l = *reinterpret_cast<const float4 *>(l2 + e);
+          const float2 x = exp2_two(fma2(two(v, e), aa, make_float2(l.x, l.y))), y = exp2_two(fma2(two(v, e + 2), aa, make_float2(l.z, l.w)));
           p[e] = x.x; p[e + 1] = x.y; p[e + 2] = y.x; p[e + 3] = y.y;
         }
         // under the causal rule key j is seen by queries from j - off on
@@ -836,42 +888,6 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         tc_warp_arrive(&bar.ds_ready[n & 1]);
         if (lane == 0) mbar_arrive(smem_u32(&bar.line_empty[ls]));
       }
-      if (!ok) break;
-      // warps 0-3 bring dv out, 4-7 dk, through shared memory that no product reads any more
-      const View &out = half ? dk : dv;
-      const float f = half ? z.scale : 1.0f;
-      bf16 *dst = out.p + (long long)w.b * out.b + (long long)w.h * out.h;
-      if (k.total > 0 && !(ok = tc_wait(&bar.done[(n - 1) & 1], tc_parity(n - 1, 2), deadline))) break;
-      tc_fence_after();
-      if (ranks > 1 || k.total > 0) {
-        uint8_t *tile = base + (ranks > 1 ? half * 2 : cn % F::kv_ring * 2 + half) * F::tile;
-#pragma unroll
-        for (int c = 0; c < 2 * NP; ++c) {
-          uint32_t v[32] = {}, u[16];
-          if (k.total > 0) {
-            tc_load32(lanes + (half ? F::dk : F::dv) + c * 32, v);
-            tc_wait_ld();
-          }
-          if (ranks > 1) {
-            keep_sums<NP>(tile, row, c * 32, v);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = j < k.lk ? pack(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f) : 0u;
-            stage_row<NP>(tile, row, c * 32, u);
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (ranks == 1) {
-          if (lane == 0) mbar_arrive(smem_u32(&bar.acc_free));
-          write_rows<NP>(tile, (warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
-          tc_proxy_fence();              // the next copy into the tile comes after these reads
-          tc_warp_arrive(&bar.kv_empty[cn % F::kv_ring]);
-          ++cn;
-        }
-      } else {
-        write_zeros<NP>((warp & 3) * 32, 32, w.at, z.tk, z, dst, out.t);
-      }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
@@ -896,7 +912,6 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 // Tensor memory: S at 0, dP at 128, dq at 256, dS in turn at 384 and 448.
 // The exponentials of one key tile are formed together with dS of the one before, so that the special
 // function units work while the FMA units do.
-constexpr int kDqThreads = 384;        // three warpgroups: 168 registers a thread at launch, 64,512 in all
 template <int NP> struct Dq {
   static constexpr uint32_t tile = kT * 128 * NP;
   static constexpr int q_ring = NP == 1 ? 2 : 1, k_ring = NP == 1 ? 5 : 3, v_ring = NP == 1 ? 3 : 2;       // q: Q and dO
@@ -907,12 +922,12 @@ template <int NP> struct Dq {
 template <int NP> struct DqBars {
   TcQueue queue;
   uint64_t q_full[Dq<NP>::q_ring], q_empty[Dq<NP>::q_ring], k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring],
-      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready[2], dq_done[2], acc_free;       // [2]: even and odd turns
+      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready[2], dq_done[2], block_done, acc_free;       // [2]: even and odd turns
   uint32_t tmem;
 };
 
 template <int NP>
-__global__ void __launch_bounds__(kDqThreads, 1)
+__global__ void __launch_bounds__(kBwdThreads, 1)
 attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const Sizes z, int blocks,
                 const float *__restrict__ lines, int padded, const View dq) {
@@ -925,14 +940,14 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   const int ranks = (int)tc_cluster_size(), rank = (int)tc_cluster_rank();
 
   if (threadIdx.x == 0) {
-    tc_queue_init(bar.queue, 11);
-    for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 8); }
+    tc_queue_init(bar.queue, 15);
+    for (int i = 0; i < F::q_ring; ++i) { mbar_init(smem_u32(&bar.q_full[i]), 1); mbar_init(smem_u32(&bar.q_empty[i]), 4); }
     for (int i = 0; i < F::k_ring; ++i) { mbar_init(smem_u32(&bar.k_full[i]), 1); mbar_init(smem_u32(&bar.k_empty[i]), 1); }
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
     for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1);}
-    mbar_init(smem_u32(&bar.acc_free), 8);
+    mbar_init(smem_u32(&bar.block_done), 1); mbar_init(smem_u32(&bar.acc_free), 4);
     mbar_init_fence();
   }
   if (warp == 9) tc_alloc(&bar.tmem, 512);
@@ -958,8 +973,8 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   auto block = [&](long long at) { return block_of(at, z.heads, columns, blocks, kT, z.causal); };
   const long long mine0 = blockIdx.x / ranks;
 
-  if (warp >= 8) {
-    tc_regs_down<56>();            // 128 x 56 + 256 x 224 = 64,512
+  if (warp >= 8 && warp < 12) {
+    tc_regs_down<56>();
     if (warp == 8) {
       if (tc_elect()) {
         bool ok = true;
@@ -1050,6 +1065,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             if (tc_elect()) {
               mma_rows<NP>(tm + F::dq, tm + F::ds + (n & 1) * 64, 32, sk + ks * F::tile, it > 0);
               tc_commit(&bar.dq_done[n & 1]);
+              if (it + 1 == k.total) tc_commit(&bar.block_done);
               tc_commit(&bar.k_empty[ks]);
             }
             __syncwarp();
@@ -1059,14 +1075,61 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       }
       if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
     }
+  } else if (warp >= 12) {
+    tc_regs_down<88>();
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16);
+    bool ok = true;
+    int qn = 0;
+    int seq = 0;
+    for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
+      deadline = clock64() + kCdgWaitCycles;
+      const Block w = block(at);
+      const Work k = work_of(w);
+      const int i = w.at + row;
+      const bool sees = i < k.lq && (z.causal ? i + k.lk - k.lq + 1 : k.lk) > 0;
+      bf16 *dst = dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h;
+      if (ranks == 1 && k.total == 0) {
+        write_zeros<NP>((warp & 3) * 32, 32, w.at, z.tq, z, dst, dq.t);
+        continue;
+      }
+      // through the tile of Q, which no product reads any more
+      if (k.total > 0 && !(ok = tc_wait(&bar.block_done, qn & 1, deadline))) break;
+      tc_fence_after();
+      uint8_t *tile = base + (ranks > 1 ? 0 : qn % F::q_ring * 2) * F::tile;
+#pragma unroll
+      for (int c = 0; c < 2 * NP; ++c) {
+        uint32_t v[32] = {}, u[16];
+        if (k.total > 0) {
+          tc_load32(lanes + F::dq + c * 32, v);
+          tc_wait_ld();
+        }
+        if (ranks > 1) {
+          keep_sums<NP>(tile, row, c * 32, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) u[e] = sees ? pack(__uint_as_float(v[2 * e]) * z.scale, __uint_as_float(v[2 * e + 1]) * z.scale) : 0u;
+          stage_row<NP>(tile, row, c * 32, u);
+        }
+      }
+      if (ranks == 1) {
+        tc_fence_before();
+        tc_warp_arrive(&bar.acc_free);
+        write_rows<NP>(tile, (warp & 3) * 32, 32, w.at, z.tq, z, dst, dq.t);
+        tc_proxy_fence();              // the next copy into the tile comes after these reads
+        tc_warp_arrive(&bar.q_empty[qn % F::q_ring]);
+        ++qn;
+      }
+    }
+    if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   } else {
-    tc_regs_up<224>();
+    tc_regs_up<184>();
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = tm + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + half * 64, tdp = ts + kT;
     const float a = z.negative ? -z.a : z.a;
     const float2 aa = make_float2(a, a);
     bool ok = true;
-    int qn = 0, n = 0;
+    int n = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
       deadline = clock64() + kCdgWaitCycles;
@@ -1100,17 +1163,13 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         const bool next = it + 1 < k.total;
         if (!(ok = (!next || tc_wait(&bar.s_full, (n + 1) & 1, deadline)) && tc_wait(&bar.dp_full, n & 1, deadline))) break;
         tc_fence_after();
-        uint32_t v[2][32] = {}, u[2][32], x[32];
+        uint32_t v[32] = {}, u[2][32], x[32];
         tc_load32(tdp, u[0]);
         tc_load32(tdp + 32, u[1]);
-        if (next) {
-          tc_load32(ts, v[0]);
-          tc_load32(ts + 32, v[1]);
-        }
+        if (next) tc_load32(ts, v);
         tc_wait_ld();
         tc_fence_before();
         tc_warp_arrive(&bar.dp_free);
-        if (next && lane == 0) mbar_arrive(smem_u32(&bar.s_free));
         const int left = keys - (rank + it * ranks) * kT - half * 64;
         if (__any_sync(0xffffffffu, left < 64)) {       // replaces P and dP: whatever lies there is not used
 #pragma unroll
@@ -1118,12 +1177,22 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             if (e >= left) { p[e] = 0.0f; u[e >> 5][e & 31] = 0u; }
         }
 #pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float2 d = mul2(make_float2(p[e], p[e + 1]), add2(two(u, e), dd));
-          x[e / 2] = pack(d.x, d.y);
-          const float2 y = fma2(two(v, e), aa, ll), t = exp2_two(y);
-          p[e] = t.x;
-          p[e + 1] = t.y;
+        for (int c = 0; c < 2; ++c) {
+          if (c == 1) {                // S's other half, when there are registers for it
+            if (next) tc_load32(ts + 32, v);
+            tc_wait_ld();
+            tc_fence_before();
+            if (next) tc_warp_arrive(&bar.s_free);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const int f = c * 32 + e;
+            const float2 d = mul2(make_float2(p[f], p[f + 1]), add2(two(u, f), dd));
+            x[f / 2] = pack(d.x, d.y);
+            const float2 t = exp2_two(fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), aa, ll));
+            p[f] = t.x;
+            p[f + 1] = t.y;
+          }
         }
         if (n > 1) {               // the place of dS is free when its last product is over
           if (!(ok = tc_wait(&bar.dq_done[n & 1], tc_parity(n - 2, 2), deadline))) break;
@@ -1133,41 +1202,6 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_wait_st();
         tc_fence_before();
         tc_warp_arrive(&bar.ds_ready[n & 1]);
-      }
-      if (!ok) break;
-      bf16 *dst = dq.p + (long long)w.b * dq.b + (long long)w.h * dq.h;
-      if (k.total > 0 && !(ok = tc_wait(&bar.dq_done[(n - 1) & 1], tc_parity(n - 1, 2), deadline))) break;
-      tc_fence_after();
-      if (ranks > 1 || k.total > 0) {
-        // the two groups of warps bring out half of the head dimensions each, through the tiles of Q and dO
-        uint8_t *tile = base + (ranks > 1 ? 0 : qn % F::q_ring * 2) * F::tile;
-#pragma unroll
-        for (int c = 0; c < NP; ++c) {
-          const int col = (half * NP + c) * 32;
-          uint32_t v[32] = {}, u[16];
-          if (k.total > 0) {
-            tc_load32(lanes + F::dq + col, v);
-            tc_wait_ld();
-          }
-          if (ranks > 1) {
-            keep_sums<NP>(tile, row, col, v);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = keys > 0 ? pack(__uint_as_float(v[2 * e]) * z.scale, __uint_as_float(v[2 * e + 1]) * z.scale) : 0u;
-            stage_row<NP>(tile, row, col, u);
-          }
-        }
-        tc_fence_before();
-        if (ranks == 1) {
-          tc_warp_arrive(&bar.acc_free);
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-          write_rows<NP>(tile, (warp & 3) * 32 + half * 16, 16, w.at, z.tq, z, dst, dq.t);
-          tc_proxy_fence();
-          tc_warp_arrive(&bar.q_empty[qn % F::q_ring]);
-          ++qn;
-        }
-      } else {
-        write_zeros<NP>((warp & 3) * 32 + half * 16, 16, w.at, z.tq, z, dst, dq.t);
       }
     }
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
@@ -1277,14 +1311,14 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
     const long long all = (long long)kt * s->kv_heads * s->batch;
     if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of((double)qt * z.group, part * qt * z.group, all, sms);
-    rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, Dkv<NP>::threads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
+    rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
                         dk, dv);
   }
   if (rc == CDGRAB_OK && qt > 0) {
     const long long all = (long long)qt * s->heads * s->batch;
     if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of(kt, part * kt, all, sms);
-    rc = tc_launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kDqThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
+    rc = tc_launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
   }
   return rc;
 }

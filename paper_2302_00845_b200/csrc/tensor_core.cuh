@@ -116,12 +116,6 @@ __device__ __forceinline__ void tc_store32(uint32_t addr, const uint32_t (&v)[32
         "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]),
         "r"(v[30]), "r"(v[31]) : "memory");
 }
-__device__ __forceinline__ void tc_store16(uint32_t addr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
 
 // ---- rings, persistent CTAs, clusters -------------------------------------------------------------
 // Turn n of a ring of R stages uses stage n % R in the phase of tc_parity(n, R); counters run on over a
