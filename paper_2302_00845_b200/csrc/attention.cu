@@ -134,6 +134,7 @@ __device__ __forceinline__ Block block_of(long long w, int heads, int columns, i
   const unsigned u = (unsigned)w, c = u % (unsigned)columns, k = u / (unsigned)columns;         // w: below 2^31, like any grid
   return Block{(last_first ? blocks - 1 - (int)k : (int)k) * rows, (int)(c % (unsigned)heads), (int)(c / (unsigned)heads)};
 }
+
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per 256 queries of a head: two tiles of 128 that share every key and value tile, so that while
 // one tile's four warps are at their exponentials the other's products run.
@@ -145,6 +146,9 @@ __device__ __forceinline__ Block block_of(long long w, int heads, int columns, i
 // 256 + 128 t and P_t over S_t.
 // The maximum that the exponents refer to is only raised when it has grown by more than 2^8 (P then
 // stays below 256, and the sum and O below that times the length): rescaling O is rare.
+// Measured: 16 x 1024, 12 heads of 64, causal: 58 us (446 TFLOP/s), bound by the softmax warps: a pair of 128 x 128
+// tiles takes them some 3800 cycles, of which the exponentials alone need 2048.  2 x 4096, 16 heads of 128 over 4,
+// ragged: 265 us (811 TFLOP/s), where S, softmax and P V of a tile follow one another because P lies over S.
 constexpr int kFwdThreads = 384;       // three warpgroups: 168 registers a thread at launch, 64,512 in all
 template <int NP> struct Fwd {
   static constexpr uint32_t tile = kT * 128 * NP;
@@ -507,12 +511,19 @@ __device__ __forceinline__ void load_line(uint32_t dst, const float *src, uint32
 // Both backward kernels: eight warps work on a tile of scores, four on its columns 0..63 and four on
 // 64..127, one row per thread.
 //   warps 0-7  P and dS     warp 8  bulk copies     warp 9  S and dP     warp 10  the products with P and dS
+//   warps 12-15  the results of a block, on their way out while the next block's scores are worked on (with
+//                warps 0-7 doing it a block of 5 tiles spent 4800 of its 15,600 cycles there: 98 -> 86 us each)
 // (two warps issue products because one can queue little ahead of the tensor cores and spends some 200 cycles
 // between two products in its waits)
+// What a warp reports as ready, or is told is done, has a barrier for even and one for odd turns: a warp may be
+// a turn ahead of another, and with one barrier it would complete a phase in the other's place.
+// Measured, 16 x 1024, 12 heads of 64, causal: dk and dv 85 us, dq 87 us.  A tile takes 2050 cycles, of which the
+// exponentials need 1024; the rest is dS and the way of S, dP, P and dS to and from tensor memory.  Letting the
+// two halves take turns at the exponentials is no faster, since a warp by itself does only one in 14 cycles.
 // The rings are as deep as shared memory allows: a tile of Q (or K) is used twice, at the beginning and at
 // the end of its turn, and a copy takes about 1700 cycles; with two stages each the products waited for it
 // (3500 cycles a tile at 128 head dimensions).
-
+//
 // Where there are few tiles of rows, the loop over the other axis is dealt out over a cluster of CTAs, whose
 // fp32 sums are joined through distributed shared memory, in the order of their ranks.
 // fp32 sums of a tile in shared memory, [128][DP] with 16-byte pieces permuted by row, so that neither a row
@@ -909,7 +920,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 
 // dq of 128 queries of a head: dq += dS K over the key tiles it sees, S = Q K^T, dP = dO V^T.  A pass of its
 // own: adding dq's parts up from the kernel above would need additions to memory in no fixed order.
-// Tensor memory: S at 0, dP at 128, dq at 256, dS in turn at 384 and 448.
+// Tensor memory: S at 0, dP at 128, dq at 256, dS in turn at 384 and 448 (so that one is being read by the product).
 // The exponentials of one key tile are formed together with dS of the one before, so that the special
 // function units work while the FMA units do.
 template <int NP> struct Dq {
@@ -946,7 +957,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
-    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1);}
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1); }
     mbar_init(smem_u32(&bar.block_done), 1); mbar_init(smem_u32(&bar.acc_free), 4);
     mbar_init_fence();
   }
@@ -1286,15 +1297,16 @@ int forward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUtens
 
 // CTAs that share the loop of one block of rows: the number for which the estimated time, in turns of a
 // loop, is least.  `longest` and `mean` are the turns of the longest block and on average, `all` the number of
-// blocks.  A cluster sets up and joins anew for each block, which costs some four turns, a single CTA about
-// two in all.  (dk and dv of one sequence of 4096, 16 query heads over 4, causal, us at 1, 2, 4 CTAs: 210, 116,
-// 161; of 3 x 257 keys, 6 heads over 2: 23, 20, 19; dq there: 139, 161, 282 and 12, 13, 25.)
+// blocks.  A cluster sets up and joins anew for each block, which costs some three turns and half a turn for
+// each of its CTAs, a single CTA about two in all.  (us at 1, 2, 4 CTAs, causal: dk and dv of one sequence of 4096, 16
+// query heads of 128 over 4: 244, 139, 185; of 3 x 357 queries on 257 keys, 6 heads of 80 over 2: 28, 22, 20, and 22
+// at 8; dq: 111, 154, 271 and 12, 14, 25.)
 int split_of(double longest, double mean, long long all, int sms) {
   int best = 1;
   double least = 0.0;
   for (int c = 1; c <= 8 && (c == 1 || longest / c >= 1.0); c *= 2) {
     const double rounds = ceil((double)all * c / sms);
-    const double turns = fmax(longest / c, rounds * mean / c) + (c > 1 ? 4.0 * rounds : 2.0);
+    const double turns = fmax(longest / c, rounds * mean / c) + (c > 1 ? (3.0 + 0.5 * c) * rounds : 2.0);
     if (c == 1 || turns < least) { best = c; least = turns; }
   }
   return best;
