@@ -32,8 +32,8 @@ __device__ __forceinline__ float2 block_sum(float a, float b, float2 *sm) {
 // A row belongs to a warp (up to 1024 columns) or to a block; a thread holds E = VEC x NV of its values,
 // VEC adjacent ones to a load.  VEC is the widest that the row length and every pointer and stride
 // allow: 16 bytes, two values, or one.  The next row is requested before the current one is reduced, so
-// that loads are in flight during the shuffles.  (32 x 512 rows of 650 bf16, 4 bytes to a load: 16 us, 2.6 TB/s,
-// of which about 3 are the launch's; 32 rows of 64: 14 us, all of it the host's call.)
+// that loads are in flight during the shuffles.  (32 x 512 rows of 650 bf16, 4 bytes to a load: 13 us, 3.3 TB/s,
+// and 15 with the host's call; 32 rows of 64: 14 us, all of it the host's call.)
 template <int BYTES> struct Raw;
 template <> struct Raw<16> { typedef uint4 type; };
 template <> struct Raw<8> { typedef uint2 type; };
@@ -500,7 +500,9 @@ struct ForwardCall {
   float *mean, *rstd; Layout l; int sms; cudaStream_t st;
   template <typename T, int VEC, int NV, bool BLOCK> cudaError_t operator()() {
     const long long blocks = BLOCK ? rows : (rows + kWarps - 1) / kWarps;
-    const long long most = (long long)sms * (BLOCK ? 2048 / l.threads : 6);    // about what is resident; rows beyond are looped over
+    // rows beyond are looped over.  Eight blocks to an SM, one to two rounds of what is resident, even the loops out: at 4,
+    // 6, 8 and 16, us: 16,384 rows of 650 bf16 14.0, 14.8, 13.0, 13.7; 65,536 of 768 40, 50, 41, 42; of 256 25, 18, 19, 18
+    const long long most = (long long)sms * (BLOCK ? 2048 / l.threads : 8);
     return cdg_ops_launch(ln_forward<T, VEC, NV, BLOCK>, dim3((unsigned)(blocks < most ? blocks : most)), l.threads, 0, st, rows,
                           cols, (const T *)x, xs, w, b, eps, (T *)y, ys, mean, rstd);
   }
