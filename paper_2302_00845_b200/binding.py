@@ -431,7 +431,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, s
         y, ys = out, _row_stride(out, "out", rows, cols)
         if out.dtype != x.dtype:
             raise ValueError("out: the type of x")
-    mean, rstd = _empty(x, (rows,), torch.float32, other), _empty(x, (rows,), torch.float32, other)
+    mean = _empty(x, (rows,), torch.float32, other)
+    rstd = _empty_like(mean, other)
     rc = lib().cdgrab_layer_norm_forward(rows, cols, code, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys, mean.data_ptr(),
                                          rstd.data_ptr(), handle)
     if rc:
