@@ -508,6 +508,11 @@ int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, const void *g
  * while a stream capture is open. */
 int cdgrab_operators_status(void);
 
+/* How long a device-side wait of the calls that follow (of every thread) may last, in SM clock cycles up to
+ * 2^40; 0: the default of 4e9, about two seconds.  A wait that lasts longer ends its kernel with
+ * CDGRAB_ERR_TIMEOUT in the status above; the context stays usable.  CDGRAB_ERR_INVALID: out of range. */
+int cdgrab_operators_wait_limit(long long cycles);
+
 #ifdef __cplusplus
 }
 #endif

@@ -94,6 +94,7 @@ SIGNATURES = {
                                        C.c_int, C.POINTER(C.c_float), C.c_float, C.c_void_p, C.c_longlong,
                                        C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p]),
     "cdgrab_operators_status": (C.c_int, []),
+    "cdgrab_operators_wait_limit": (C.c_int, [C.c_longlong]),
 }
 
 _lib = None
@@ -597,6 +598,11 @@ def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: floa
 def operators_status() -> int:
     """cdgrab_operators_status: what the training operators' kernels reported so far (read and cleared)."""
     return int(lib().cdgrab_operators_status())
+
+
+def operators_wait_limit(cycles: int = 0):
+    """How long a device-side wait of the calls that follow may last, in SM clock cycles; 0: the default."""
+    _check(lib().cdgrab_operators_wait_limit(cycles), "cdgrab_operators_wait_limit")
 
 
 class ShardedCdGrab:

@@ -32,6 +32,7 @@ struct Sizes {
   int negative;              // scale < 0
   int shared;                // bits q, k, v, do: one for the whole batch (a batch stride of 0)
   const int *q_lens, *kv_lens;
+  long long wait;            // how long the waits of one block of rows may last, in clock cycles
   int *status;
 };
 struct View { bf16 *p; long long b, t, h; };
@@ -160,7 +161,7 @@ template <int NP> struct Fwd {
 template <int NP> struct FwdBars {
   TcQueue queue;
   uint64_t q_full[Fwd<NP>::q_ring], q_empty[Fwd<NP>::q_ring], k_full[Fwd<NP>::ring], k_empty[Fwd<NP>::ring], v_full[Fwd<NP>::ring],
-      v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2], turn[2];
+      v_empty[Fwd<NP>::ring], s_full[2], s_free[2], p_ready[2], pv_done[2], o_free[2], turn[2], finished[2];
   uint32_t tmem;
 };
 
@@ -186,6 +187,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       mbar_init(smem_u32(&bar.s_full[t]), 1); mbar_init(smem_u32(&bar.s_free[t]), 4);
       mbar_init(smem_u32(&bar.p_ready[t]), 4); mbar_init(smem_u32(&bar.pv_done[t]), 1);
       mbar_init(smem_u32(&bar.o_free[t]), 4); mbar_init(smem_u32(&bar.turn[t]), 4);
+      mbar_init(smem_u32(&bar.finished[t]), 1);
     }
     mbar_init_fence();
   }
@@ -196,7 +198,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
   const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
+  long long deadline = clock64() + z.wait;       // of the waits for one block of rows
   const int columns = z.heads * z.batch;
 
   // the sequence's lengths and the key tiles that each query tile of a block sees
@@ -222,10 +224,11 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       if (tc_elect()) {
         bool ok = true;
         int qn = 0, kn = 0, vn = 0;        // blocks and tiles issued
-        int seq = 0;
+        int seq = 0, asked = 0;
         for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-          deadline = clock64() + kCdgWaitCycles;
+          deadline = clock64() + z.wait;
           if (!(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+          ++asked;
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.tiles == 0) continue;
@@ -254,13 +257,11 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             }
           }
         }
-        if (!ok) {
-          atomicOr(z.status, CDG_ST_TIMEOUT);
-          tc_drain(bar.queue.full, seq + 1, 2);
-          tc_drain(bar.q_full, qn, F::q_ring);
-          tc_drain(bar.k_full, kn, F::ring);
-          tc_drain(bar.v_full, vn, F::ring);
-        }
+        if (!ok) atomicOr(z.status, CDG_ST_TIMEOUT);
+        tc_drain(bar.queue.full, asked, 2);
+        tc_drain(bar.q_full, qn, F::q_ring);
+        tc_drain(bar.k_full, kn, F::ring);
+        tc_drain(bar.v_full, vn, F::ring);
       }
     } else if (warp < 11) {
       const int t = warp - 9;
@@ -269,7 +270,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
       int qn = 0, kn = 0, vn = 0, sn = 0, pn = 0, on = 0;      // blocks, tiles of K and V, products S_t and P_t V, blocks with any
       int seq = 0;
       for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
-        deadline = clock64() + kCdgWaitCycles;
+        deadline = clock64() + z.wait;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.tiles == 0) continue;
@@ -322,6 +323,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         on += mine > 0;
       }
       if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+      tc_finish(&bar.finished[t]);
     }
   } else {
     tc_regs_up<224>();
@@ -333,7 +335,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     int qn = 0, sn = 0, gn = 0;          // blocks, score tiles of this half, and turns of both halves
     int seq = 0;
     for (long long at = blockIdx.x; at >= 0 && ok; at = tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
+      deadline = clock64() + z.wait;
       const Block w = block(at);
       const Work k = work_of(w);
       const int mine = t == 0 ? k.n[0] : k.n[1], i = w.at + t * kT + row;
@@ -456,6 +458,7 @@ attn_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         ++qn;
       }
     }
+    tc_wait_st();                        // (of a rescaled O, where a wait expired after it)
     if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
   }
   tc_fence_before();
@@ -572,14 +575,14 @@ template <int NP> struct Dkv {
   static constexpr int kv_ring = NP == 1 ? 2 : 1, q_ring = NP == 1 ? 4 : 3, do_ring = NP == 1 ? 3 : 2, line_ring = NP == 1 ? 4 : 2;
   static constexpr uint32_t line = 2 * kT * 4;              // lse and delta of a query tile
   static constexpr uint32_t q = 2 * kv_ring * tile, d_o = q + q_ring * tile, lines = d_o + do_ring * tile, bars = lines + line_ring * line;
-  static constexpr size_t smem = bars + 384;
+  static constexpr size_t smem = bars + 448;
   static constexpr uint32_t dv = 512 - 128 * NP, dk = dv + 64 * NP;
 };
 template <int NP> struct DkvBars {
   TcQueue queue;
   uint64_t kv_full[Dkv<NP>::kv_ring], kv_empty[Dkv<NP>::kv_ring], q_full[Dkv<NP>::q_ring], q_empty[Dkv<NP>::q_ring], do_full[Dkv<NP>::do_ring],
       do_empty[Dkv<NP>::do_ring], line_full[Dkv<NP>::line_ring], line_empty[Dkv<NP>::line_ring], s_full[2], dp_full, dp_free,
-      p_ready[2], ds_ready[2], done[2], block_done, acc_free;       // [2]: even and odd turns
+      p_ready[2], ds_ready[2], done[2], block_done, acc_free, finished[2];       // [2]: even and odd turns
   uint32_t tmem;
 };
 
@@ -590,7 +593,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                  const float *__restrict__ lines, int padded, const View dk, const View dv) {
   typedef Dkv<NP> F;
   extern __shared__ __align__(1024) uint8_t base[];
-  static_assert(sizeof(DkvBars<NP>) <= 384, "barriers behind the tiles");
+  static_assert(sizeof(DkvBars<NP>) <= 448, "barriers behind the tiles");
   DkvBars<NP> &bar = *reinterpret_cast<DkvBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t s0 = smem_u32(base), sq = s0 + F::q, sdo = s0 + F::d_o;
@@ -607,6 +610,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     mbar_init(smem_u32(&bar.dp_full), 1); mbar_init(smem_u32(&bar.dp_free), 8);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bar.p_ready[i]), 8); mbar_init(smem_u32(&bar.ds_ready[i]), 8);
+      mbar_init(smem_u32(&bar.finished[i]), 1);
     }
     mbar_init(smem_u32(&bar.block_done), 1); mbar_init(smem_u32(&bar.acc_free), 4);
     mbar_init_fence();
@@ -619,7 +623,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   const auto dp_at = [](int n) { return NP == 1 ? 256u : (uint32_t)(~n & 1) * kT; };
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
+  long long deadline = clock64() + z.wait;       // of the waits for one block of rows
   const int columns = kv_heads * z.batch;
 
   // query tiles first .. first + per - 1 see a key of the block; over the heads of the group this CTA takes
@@ -655,10 +659,13 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
       if (tc_elect()) {
         bool ok = true;
         int cn = 0, qn = 0, dn = 0, ln = 0;
-        int seq = 0;
+        int seq = 0, asked = 0;
         for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-          deadline = clock64() + kCdgWaitCycles;
-          if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+          deadline = clock64() + z.wait;
+          if (ranks == 1) {
+            if (!(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+            ++asked;
+          }
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.total == 0) continue;
@@ -692,21 +699,19 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             ++dn;
           }
         }
-        if (!ok) {
-          atomicOr(z.status, CDG_ST_TIMEOUT);
-          if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
-          tc_drain(bar.kv_full, cn, F::kv_ring);
-          tc_drain(bar.q_full, qn, F::q_ring);
-          tc_drain(bar.line_full, ln, F::line_ring);
-          tc_drain(bar.do_full, dn, F::do_ring);
-        }
+        if (!ok) atomicOr(z.status, CDG_ST_TIMEOUT);
+        tc_drain(bar.queue.full, asked, 2);
+        tc_drain(bar.kv_full, cn, F::kv_ring);
+        tc_drain(bar.q_full, qn, F::q_ring);
+        tc_drain(bar.line_full, ln, F::line_ring);
+        tc_drain(bar.do_full, dn, F::do_ring);
       }
     } else if (warp <= 10) {
       bool ok = true;
       int cn = 0, n = 0;                   // blocks and turns
       int seq = 0;
       for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-        deadline = clock64() + kCdgWaitCycles;
+        deadline = clock64() + z.wait;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
@@ -776,6 +781,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         ++cn;
       }
       if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+      tc_finish(&bar.finished[warp - 9]);
     }
   } else if (warp >= 12) {
     tc_regs_down<88>();
@@ -785,7 +791,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     int cn = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
+      deadline = clock64() + z.wait;
       const Block w = block(at);
       const Work k = work_of(w);
       const int j = w.at + row;
@@ -842,7 +848,7 @@ attn_backward_kv(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     int n = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
+      deadline = clock64() + z.wait;
       const Block w = block(at);
       const Work k = work_of(w);
       const int j = w.at + row, off = k.lk - k.lq;
@@ -927,13 +933,13 @@ template <int NP> struct Dq {
   static constexpr uint32_t tile = kT * 128 * NP;
   static constexpr int q_ring = NP == 1 ? 2 : 1, k_ring = NP == 1 ? 5 : 3, v_ring = NP == 1 ? 3 : 2;       // q: Q and dO
   static constexpr uint32_t k = 2 * q_ring * tile, v = k + k_ring * tile, bars = v + v_ring * tile;
-  static constexpr size_t smem = bars + 320;
+  static constexpr size_t smem = bars + 384;
   static constexpr uint32_t dq = 256, ds = 384;
 };
 template <int NP> struct DqBars {
   TcQueue queue;
   uint64_t q_full[Dq<NP>::q_ring], q_empty[Dq<NP>::q_ring], k_full[Dq<NP>::k_ring], k_empty[Dq<NP>::k_ring], v_full[Dq<NP>::v_ring],
-      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready[2], dq_done[2], block_done, acc_free;       // [2]: even and odd turns
+      v_empty[Dq<NP>::v_ring], s_full, s_free, dp_full, dp_free, ds_ready[2], dq_done[2], block_done, acc_free, finished[2];       // [2]: even and odd turns
   uint32_t tmem;
 };
 
@@ -944,7 +950,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 const float *__restrict__ lines, int padded, const View dq) {
   typedef Dq<NP> F;
   extern __shared__ __align__(1024) uint8_t base[];
-  static_assert(sizeof(DqBars<NP>) <= 320, "barriers behind the tiles");
+  static_assert(sizeof(DqBars<NP>) <= 384, "barriers behind the tiles");
   DqBars<NP> &bar = *reinterpret_cast<DqBars<NP> *>(base + F::bars);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t s0 = smem_u32(base), sk = s0 + F::k, sv = s0 + F::v;
@@ -957,7 +963,10 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     for (int i = 0; i < F::v_ring; ++i) { mbar_init(smem_u32(&bar.v_full[i]), 1); mbar_init(smem_u32(&bar.v_empty[i]), 1); }
     mbar_init(smem_u32(&bar.s_full), 1); mbar_init(smem_u32(&bar.dp_full), 1);
     mbar_init(smem_u32(&bar.s_free), 8); mbar_init(smem_u32(&bar.dp_free), 8);
-    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bar.ds_ready[i]), 8); mbar_init(smem_u32(&bar.dq_done[i]), 1);
+      mbar_init(smem_u32(&bar.finished[i]), 1);
+    }
     mbar_init(smem_u32(&bar.block_done), 1); mbar_init(smem_u32(&bar.acc_free), 4);
     mbar_init_fence();
   }
@@ -968,7 +977,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   const uint32_t tm = bar.tmem;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  long long deadline = clock64() + kCdgWaitCycles;       // of the waits for one block of rows
+  long long deadline = clock64() + z.wait;       // of the waits for one block of rows
   const int columns = z.heads * z.batch;
 
   // key tiles rank, rank + ranks, ... of those that the block sees, `total` of them
@@ -990,10 +999,13 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
       if (tc_elect()) {
         bool ok = true;
         int qn = 0, kn = 0, vn = 0;
-        int seq = 0;
+        int seq = 0, asked = 0;
         for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next_one(bar.queue, seq++, deadline, ok)) {
-          deadline = clock64() + kCdgWaitCycles;
-          if (ranks == 1 && !(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+          deadline = clock64() + z.wait;
+          if (ranks == 1) {
+            if (!(ok = tc_queue_ask(bar.queue, seq, deadline))) break;
+            ++asked;
+          }
           const Block w = block(at);
           const Work k = work_of(w);
           if (k.total == 0) continue;
@@ -1019,20 +1031,18 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             ++vn;
           }
         }
-        if (!ok) {
-          atomicOr(z.status, CDG_ST_TIMEOUT);
-          if (ranks == 1) tc_drain(bar.queue.full, seq + 1, 2);
-          tc_drain(bar.q_full, qn, F::q_ring);
-          tc_drain(bar.k_full, kn, F::k_ring);
-          tc_drain(bar.v_full, vn, F::v_ring);
-        }
+        if (!ok) atomicOr(z.status, CDG_ST_TIMEOUT);
+        tc_drain(bar.queue.full, asked, 2);
+        tc_drain(bar.q_full, qn, F::q_ring);
+        tc_drain(bar.k_full, kn, F::k_ring);
+        tc_drain(bar.v_full, vn, F::v_ring);
       }
     } else if (warp < 11) {
       bool ok = true;
       int qn = 0, n = 0;                 // blocks, and turns whose S (warp 9) or dq (warp 10) has been issued
       int seq = 0;
       for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-        deadline = clock64() + kCdgWaitCycles;
+        deadline = clock64() + z.wait;
         const Block w = block(at);
         const Work k = work_of(w);
         if (k.total == 0) continue;
@@ -1085,6 +1095,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         ++qn;
       }
       if (!ok && lane == 0) atomicOr(z.status, CDG_ST_TIMEOUT);
+      tc_finish(&bar.finished[warp - 9]);
     }
   } else if (warp >= 12) {
     tc_regs_down<88>();
@@ -1094,7 +1105,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     int qn = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
+      deadline = clock64() + z.wait;
       const Block w = block(at);
       const Work k = work_of(w);
       const int i = w.at + row;
@@ -1143,7 +1154,7 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     int n = 0;
     int seq = 0;
     for (long long at = mine0; at >= 0 && ok; at = ranks > 1 ? -1 : tc_queue_next(bar.queue, seq++, deadline, ok)) {
-      deadline = clock64() + kCdgWaitCycles;
+      deadline = clock64() + z.wait;
       const Block w = block(at);
       const Work k = work_of(w);
       const int i = w.at + row, keys = i >= k.lq ? 0 : z.causal ? min(k.lk, i + k.lk - k.lq + 1) : k.lk;
@@ -1272,7 +1283,8 @@ Sizes sizes_of(const cdgrab_attention_shape *s, const int32_t *q_lens, const int
   const int shared = (s->q_stride[0] > 0 ? 0 : kQ) | (s->k_stride[0] > 0 ? 0 : kK) | (s->v_stride[0] > 0 ? 0 : kV) |
                      (s->do_stride[0] > 0 ? 0 : kDo);
   return Sizes{s->batch, s->len_q, s->len_kv, s->heads, s->heads / s->kv_heads, s->head_dim, s->causal, s->scale,
-               fmaxf(fabsf(s->scale) * kLog2e, 1e-30f), s->scale < 0.0f, shared, q_lens, kv_lens, status};
+               fmaxf(fabsf(s->scale) * kLog2e, 1e-30f), s->scale < 0.0f, shared, q_lens, kv_lens,
+               cdg_ops_wait_limit(), status};
 }
 View view(const void *p, const long long s[3]) { return View{(bf16 *)const_cast<void *>(p), s[0], s[1], s[2]}; }
 

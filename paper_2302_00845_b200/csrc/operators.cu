@@ -2,12 +2,14 @@
 #include <atomic>
 
 #include "operators.cuh"
+#include "ptx.cuh"
 
 namespace {
 __device__ int g_ops_status;
 constexpr int kMaxDevices = 64;
 CdgOpsDevice g_ops[kMaxDevices];
 std::atomic<int> g_ready[kMaxDevices];
+std::atomic<long long> g_wait_limit{kCdgWaitCycles};
 }  // namespace
 
 int cdg_ops_device(const CdgOpsDevice **out) {
@@ -30,6 +32,14 @@ int cdg_ops_device(const CdgOpsDevice **out) {
     g_ready[dev].store(1, std::memory_order_release);
   }
   *out = &g_ops[dev];
+  return CDGRAB_OK;
+}
+
+long long cdg_ops_wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
+
+extern "C" int cdgrab_operators_wait_limit(long long cycles) {
+  if (cycles < 0 || cycles > (1ll << 40)) return CDGRAB_ERR_INVALID;
+  g_wait_limit.store(cycles > 0 ? cycles : kCdgWaitCycles, std::memory_order_relaxed);
   return CDGRAB_OK;
 }
 

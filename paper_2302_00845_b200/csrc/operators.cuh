@@ -11,6 +11,8 @@ struct CdgOpsDevice {
 };
 // the current device, looked up once per device; CDGRAB_ERR_DEVICE when it is no sm_100
 int cdg_ops_device(const CdgOpsDevice **out);
+// how long a device-side wait of the next launches may last, in clock cycles
+long long cdg_ops_wait_limit();
 
 inline bool cdg_aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 

@@ -146,7 +146,7 @@ template <int BN, int RANKS> struct Shape {
   static constexpr size_t smem = bars + 256;
 };
 template <int BN, int RANKS> struct Bars {
-  uint64_t full[Shape<BN, RANKS>::ring], empty[Shape<BN, RANKS>::ring], acc_full[2], acc_empty[2], joined, read;
+  uint64_t full[Shape<BN, RANKS>::ring], empty[Shape<BN, RANKS>::ring], acc_full[2], acc_empty[2], joined, read, finished;
   uint32_t tmem;
 };
 
@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
     for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bar.acc_full[s]), 1); mbar_init(smem_u32(&bar.acc_empty[s]), 4); }
     mbar_init(smem_u32(&bar.joined), 4 * RANKS);
     mbar_init(smem_u32(&bar.read), 4 * RANKS);
+    mbar_init(smem_u32(&bar.finished), 1);
     mbar_init_fence();
   }
   if (warp == 1) tc_alloc(&bar.tmem, 512);
@@ -414,10 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
           }
         }
       }
-      if (!ok) {
-        atomicOr(p.status, CDG_ST_TIMEOUT);
-        tc_drain(bar.full, n, S::ring);
-      }
+      if (!ok) atomicOr(p.status, CDG_ST_TIMEOUT);
+      tc_drain(bar.full, n, S::ring);
     }
   } else if (warp == 1) {
     bool ok = true;
@@ -448,6 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       }
     }
     if (!ok && lane == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
+    tc_finish(&bar.finished);
   } else {
     const int w = warp & 3, r = w * 32 + lane;         // warp w of the four reads lanes 32 w ... of the accumulator
     uint8_t *stage = base + S::staging + w * S::warp_bytes;
@@ -534,7 +534,7 @@ inline size_t small_smem(int n) { return (size_t)((n + 63) / 64 + 4) * kPanel + 
 struct SmallArgs {
   int rows, cols, tall, steps, vec;
   float a, b, c, eps;
-  long long gb, gs, ob, os;
+  long long gb, gs, ob, os, wait;                // wait: how long one may last, in clock cycles
   int *status;
 };
 
@@ -545,13 +545,13 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_bfloat16 *o, const SmallArgs p) {
   extern __shared__ __align__(1024) uint8_t base[];
   __shared__ double part[kSmallThreads / 32];
-  __shared__ __align__(8) uint64_t bar[4];
+  __shared__ __align__(8) uint64_t bar[5];         // A and A A; three blocks of X; the end
   __shared__ uint32_t slot;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int m = p.tall ? p.cols : p.rows, n = p.tall ? p.rows : p.cols, panels = (n + 63) / 64;
   uint8_t *A = base + panels * kPanel, *B = A + 2 * kPanel;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bar[i]), 1);
+    for (int i = 0; i < 5; ++i) mbar_init(smem_u32(&bar[i]), 1);
     mbar_init_fence();
   }
   if (warp == 0) tc_alloc(&slot, 512);
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_
       }
       __syncwarp();
     }
-    ok = tc_wait(&bar[0], turn[0]++ & 1, clock64() + kCdgWaitCycles);
+    ok = tc_wait(&bar[0], turn[0]++ & 1, clock64() + p.wait);
     tc_fence_after();
   };
   auto settle = [&]() {          // what was written is an operand of the next product, what was read may be overwritten
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_
       for (int t = 0; t < 3; ++t) {
         const int q = q0 + 2 * t;
         if (q >= panels || !ok) continue;
-        if (!(ok = tc_wait(&bar[1 + t], turn[1 + t]++ & 1, clock64() + kCdgWaitCycles))) continue;
+        if (!(ok = tc_wait(&bar[1 + t], turn[1 + t]++ & 1, clock64() + p.wait))) continue;
         tc_fence_after();
         if (half > 1 || q + half >= panels) continue;
 #pragma unroll 1
@@ -757,6 +757,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_
     }
   }
   if (!ok && threadIdx.x == 0) atomicOr(p.status, CDG_ST_TIMEOUT);
+  if (warp == 0) tc_finish(&bar[4]);
   tc_fence_before();
   __syncthreads();
   if (warp == 0) { tc_fence_after(); tc_free(tm, 512); }
@@ -840,7 +841,7 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   const bool wide = cdg_aligned(g, 16) && gs % (16 / e) == 0 && gb % (16 / e) == 0 && cols % (16 / e) == 0;
   if (m <= 128 && n <= kSmallCols) {
     const SmallArgs a = {rows, cols, tall, steps, cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, coeffs[0], coeffs[1], coeffs[2], eps, gb, gs, ob, os,
-                         dev->status};
+                         cdg_ops_wait_limit(), dev->status};
     auto run = [&](auto *kernel, const auto *from, CdgPerDevice &flags) {
       if (!tc_raise_limit(flags, kernel, small_smem(kSmallCols))) return (int)CDGRAB_ERR_CUDA;
       return cdg_launch_rc(cdg_ops_launch(kernel, dim3(batch), kSmallThreads, small_smem(n), st, from, (__nv_bfloat16 *)o, a));

@@ -66,6 +66,15 @@ __device__ __forceinline__ bool tc_wait(uint64_t *bar, uint32_t parity, long lon
     if (__any_sync(0xffffffffu, clock64() > deadline)) return false;
   }
 }
+// The matrix instructions that this warp has issued are over.  At a kernel's end, before the tensor memory and the tiles
+// that they use are given up: where another role's wait has expired nobody else has waited for them.  `bar`: initialised
+// with one arrival, used for nothing else.
+__device__ __forceinline__ void tc_finish(uint64_t *bar) {
+  __syncwarp();
+  if (tc_elect()) tc_commit(bar);
+  __syncwarp();
+  tc_wait(bar, 0, clock64() + kCdgWaitCycles);
+}
 // tile from shared memory to a tensor (one thread; coordinates inside the tensor); the end of a group of such
 // copies, and waits for this thread's groups: all but the last to have read shared memory, all to be written
 __device__ __forceinline__ void tc_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z) {
@@ -125,7 +134,8 @@ __device__ __forceinline__ uint32_t tc_parity(int n, int ring) { return (uint32_
 __device__ __forceinline__ bool tc_wait_released(uint64_t *empty, int n, int ring, long long deadline) {
   return n < ring || mbar_wait(smem_u32(&empty[n % ring]), tc_parity(n - ring, ring), deadline);
 }
-// after a failure: the copies in flight have to land before the CTA gives up its shared memory
+// the last copies of a ring have to land before the CTA gives up its shared memory (where a wait has expired, nobody
+// else has waited for them)
 __device__ __forceinline__ void tc_drain(uint64_t *full, int n, int ring) {
   for (int i = max(0, n - ring); i < n; ++i) mbar_wait(smem_u32(&full[i % ring]), tc_parity(i, ring), clock64() + kCdgWaitCycles);
 }

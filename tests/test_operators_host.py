@@ -131,3 +131,9 @@ def test_layer_norm_formulas_against_autograd():
         dx = rstd * (g - g.mean(1, keepdim=True) - n * (g * n).mean(1, keepdim=True))
         assert torch.allclose(dx, xs.grad, atol=n_err)
         assert torch.allclose((dy[i * rows:(i + 1) * rows] * n).sum(0), w.grad, atol=n_err)
+
+
+def test_wait_limit_arguments(lib):
+    for bad in (-1, (1 << 40) + 1):
+        assert lib.cdgrab_operators_wait_limit(bad) == binding.ERR_INVALID
+    assert lib.cdgrab_operators_wait_limit(1 << 40) == binding.OK and lib.cdgrab_operators_wait_limit(0) == binding.OK

@@ -1,0 +1,43 @@
+"""The training operators' bounded waits run out: the kernels end, the status says so, the context stays usable.
+
+A limit of one cycle lets a wait last as long as the hardware suspends it (some 8000 cycles), so that what is
+waited for longer, such as the end of a loop over 32 tiles, is given up.  Nothing is made to fail but the waiting."""
+import pytest
+import torch
+
+from paper_2302_00845_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def short_waits():
+    binding.operators_status()
+    yield lambda: binding.operators_wait_limit(1)
+    binding.operators_wait_limit(0)
+    torch.cuda.synchronize()
+    binding.operators_status()
+
+
+@pytest.mark.parametrize("b,t,h,hk,d", [(4, 4096, 12, 12, 64), (4, 4096, 8, 2, 128), (1, 4096, 2, 1, 64), (1, 4096, 1, 1, 128)])
+def test_attention(short_waits, b, t, h, hk, d):
+    """Many blocks of rows to a CTA, and few that are shared by clusters."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    r = lambda n: torch.randn(b, t, n, d, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    q, k, v, do = r(h), r(hk), r(hk), r(h)
+    o, lse = binding.attention_forward(q, k, v)
+    want = (o, lse) + binding.attention_backward(do, q, k, v, o, lse)
+    assert binding.operators_status() == binding.OK
+    short_waits()
+    if b > 1:                # (a single block of rows to a CTA: nothing in the forward pass waits for long)
+        binding.attention_forward(q, k, v)
+        assert binding.operators_status() == binding.ERR_TIMEOUT
+    binding.attention_backward(do, q, k, v, o, lse)
+    assert binding.operators_status() == binding.ERR_TIMEOUT
+    assert binding.operators_status() == binding.OK          # read and cleared
+    binding.operators_wait_limit(0)
+    o, lse = binding.attention_forward(q, k, v)
+    got = (o, lse) + binding.attention_backward(do, q, k, v, o, lse)
+    assert binding.operators_status() == binding.OK
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)
