@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       const bool split = kSplit && u.kind < 2;
       if (u.kind == kPoly && u.first < u.tiles) {      // A, which is added, is read here too
         ok = lane != 0 || wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        __syncwarp();            // lane 0 has acquired the other CTAs' writes: the lanes' reads come after that (a vote orders no memory)
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
       }
       for (int at = u.first; at < u.tiles; at += u.step, ++seq) {
