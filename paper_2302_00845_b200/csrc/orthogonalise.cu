@@ -131,6 +131,7 @@ struct StepArgs {
   void *o;
   long long xb, ab, ob, os;
   unsigned *arrived;         // [2] CTAs past each product of a part of the batch, counted on
+  long long wait;            // how long the copies may wait for the grid or a stage, in clock cycles; what waits for them, twice and three times that
   int *status;
 };
 // X as rows of K and as panels of N, A and B; the same written in pieces of 32 x 32
@@ -199,6 +200,14 @@ __device__ __forceinline__ bool wait_count(const unsigned *count, unsigned want,
     if (got >= want) return true;
     if (clock64() > deadline) return false;
   }
+}
+// barrier of the four epilogue warps, and whether all of them are well: they go on, or leave, together
+__device__ __forceinline__ bool epilogue_barrier(bool ok) {
+  uint32_t all;
+  __syncwarp();
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.and.pred q, 1, 128, p;\nselp.u32 %0, 1, 0, q;\n}"
+               : "=r"(all) : "r"((uint32_t)ok) : "memory");
+  return all != 0;
 }
 
 // A warp's 32 rows of a tile's accumulator, 32 columns at a time, to memory.  The loops are kept short and
@@ -390,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       int n = 0;
       for (int t = 0; t < turns && ok; ++t) {
         const Turn u = turn_of(t);
-        long long deadline = clock64() + kCdgWaitCycles;
+        long long deadline = clock64() + p.wait;
         if (t >= parts && u.first < u.tiles) {         // every CTA has written its share of this part's product before
           if (!(ok = wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, deadline))) break;
           asm volatile("fence.proxy.async;" ::: "memory");         // ... and the copies see it
@@ -399,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
         const CUtensorMap *mb = u.kind == kGram ? &maps.rows[u.at] : u.kind == kPoly ? &maps.A : &maps.panels[u.at];
         for (int at = u.first; at < u.tiles && ok; at += u.step) {
           const Tile w = tile_of(u, at);
-          deadline = clock64() + kCdgWaitCycles;
+          deadline = clock64() + p.wait;
           for (int it = 0; it < u.nk; ++it, ++n) {
             if (!(ok = tc_wait_released(bar.empty, n, S::ring, deadline))) break;
             const uint32_t full = smem_u32(&bar.full[n % S::ring]), a = ring + n % S::ring * S::stage, b = a + S::a_bytes;
@@ -426,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       const uint32_t idesc = u.kind < 2 ? tc_idesc(false, kM, kM, false, false) : tc_idesc(false, kM, BN, false, true);
       const uint32_t kb = u.kind < 2 ? 2 : 128;          // 16 of K further on in B, in units of 16 bytes
       for (int at = u.first; at < u.tiles && ok; at += u.step, ++seq) {
-        const long long deadline = clock64() + 2 * kCdgWaitCycles;       // (the copies may wait for the grid)
+        const long long deadline = clock64() + 2 * p.wait;       // (the copies may wait for the grid)
         const uint32_t d = acc + (seq & 1) * 256;
         if (seq >= 2 && !(ok = tc_wait(&bar.acc_empty[seq & 1], tc_parity(seq - 2, 2), deadline))) break;
         for (int it = 0; it < u.nk; ++it, ++n) {
@@ -457,13 +466,13 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
       const Turn u = turn_of(t);
       const bool split = kSplit && u.kind < 2;
       if (u.kind == kPoly && u.first < u.tiles) {      // A, which is added, is read here too
-        ok = lane != 0 || wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
+        ok = lane != 0 || wait_count(p.arrived + t % parts, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * p.wait);
         __syncwarp();            // lane 0 has acquired the other CTAs' writes: the lanes' reads come after that (a vote orders no memory)
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        ok = __all_sync(0xffffffffu, ok);
       }
-      for (int at = u.first; at < u.tiles; at += u.step, ++seq) {
+      for (int at = u.first; at < u.tiles && ok; at += u.step, ++seq) {
         const Tile tile = tile_of(u, at);
-        const long long deadline = clock64() + 3 * kCdgWaitCycles;
+        const long long deadline = clock64() + 3 * p.wait;
         const Piece piece = {acc + ((uint32_t)(w * 32) << 16) + (seq & 1) * 256, tile.i0 + w * 32, tile.j0, tile.z, u.kind < 2 ? kM : BN,
                              u.kind < 2 && tile.i0 != tile.j0};
         uint64_t *empty = &bar.acc_empty[seq & 1];
@@ -499,19 +508,16 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
         else write_share<kPoly, RANKS>(p, ring + S::sums, mine, r0, tile.i0, tile.j0, tile.z, piece.mirror);
         if (lane < RANKS) tc_arrive_peer(&bar.read, lane);
       }
-      if (!ok) break;
       if (t + parts < turns) {
         // this CTA's share is written (by lane 0's copies, or by all lanes): visible to all, then counted; one
         // without a share is counted no earlier than the product before is complete, so that the count tells
+        unsigned *count = p.arrived + t % parts;
         if (lane == 0) tc_store_done();
         if (split || lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (threadIdx.x == 64) {
-          unsigned *count = p.arrived + t % parts;
-          if (u.first >= u.tiles && t >= parts) ok = wait_count(count, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * kCdgWaitCycles);
-          if (ok) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory");
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (threadIdx.x == 64 && u.first >= u.tiles && t >= parts)
+          ok = wait_count(count, (unsigned)(t / parts) * (unsigned)ctas, clock64() + 2 * p.wait);
+        ok = epilogue_barrier(ok);       // (a warp that left alone would keep the others at this barrier for good)
+        if (ok && threadIdx.x == 64) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory");
       }
     }
     if (lane == 0) tc_store_done();
@@ -883,7 +889,7 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
               : begin(orth_sumsq<__nv_bfloat16, 1>, orth_start<__nv_bfloat16, 1>, (const __nv_bfloat16 *)g);
   if (rc != CDGRAB_OK) return rc;
   const StepArgs a = {m, n, batch, steps, p.ldx, p.lda, tall, cdg_aligned(o, 16) && os % 8 == 0 && ob % 8 == 0, coeffs[0], coeffs[1], coeffs[2],
-                      {x[0], x[1]}, A, B, o, xb, ab, ob, os, arrived, dev->status};
+                      {x[0], x[1]}, A, B, o, xb, ab, ob, os, arrived, cdg_ops_wait_limit(), dev->status};
   // tiles of 256 columns while they still give every SM one; CTAs share a tile of A or B where there are fewer
   // than half as many tiles as SMs, up to four of them and at least two steps of K each
   const long long mt = (m + kM - 1) / kM, sym = mt * (mt + 1) / 2 * batch;

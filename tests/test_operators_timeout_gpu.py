@@ -41,3 +41,19 @@ def test_attention(short_waits, b, t, h, hk, d):
     assert binding.operators_status() == binding.OK
     for a, c in zip(got, want):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 650, 2600), (1, 300, 900), (1, 1030, 640), (6, 600, 180), (4, 1500, 2600)])
+def test_orthogonalise(short_waits, batch, rows, cols):
+    """Clusters of four and of two, most of whose blocks have no tile in two products of three; no clusters; several
+    tiles to a block."""
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda")
+    want = binding.orthogonalise(g)
+    assert binding.operators_status() == binding.OK
+    short_waits()
+    for _ in range(3):
+        binding.orthogonalise(g)
+        assert binding.operators_status() == binding.ERR_TIMEOUT
+    binding.operators_wait_limit(0)
+    assert torch.equal(binding.orthogonalise(g), want)
+    assert binding.operators_status() == binding.OK
