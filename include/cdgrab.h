@@ -492,7 +492,8 @@ int cdgrab_attention_backward(const cdgrab_attention_shape *shape, const void *d
  * (of the transposed matrix where rows > cols), which drives the singular values towards one.
  *   batch, rows, cols   >= 0 (nothing to do where any is 0);  steps 1 to 64
  *   dtype    of G: [batch] matrices g_batch_stride apart, rows of cols contiguous values g_stride apart
- *   coeffs   HOST float [3]: a, b, c
+ *   coeffs   HOST float [3]: a, b, c.  X, A and B are held in 16 bits: refused where a singular value that starts in
+ *            [0, 1] may pass 234 before the last step, or |a + b s^2 + c s^4| 60000
  *   o        bf16 output, strides likewise; o may not overlap G
  *   workspace  16-byte aligned, cdgrab_orthogonalise_workspace_bytes(batch, rows, cols) bytes (-1: invalid)
  */

@@ -566,7 +566,8 @@ def attention_backward(do, q, k, v, o, lse, causal: bool = False, scale: float |
 
 def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, stream=None):
     """The orthogonalised update of a gradient g [rows][cols] or [batch][rows][cols] (float32 or bfloat16):
-    `steps` Newton-Schulz products on g / (|g| + eps).  Returns a bfloat16 tensor of g's shape."""
+    `steps` Newton-Schulz products on g / (|g| + eps).  Coefficients that do not keep singular values out of [0, 1]
+    below 234 until the last step are refused.  Returns a bfloat16 tensor of g's shape."""
     handle, other = _place(stream, g, out)
     o = _empty(g, g.shape, torch.bfloat16, other) if out is None else out
     if g.dim() not in (2, 3):

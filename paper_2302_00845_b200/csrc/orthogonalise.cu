@@ -8,8 +8,9 @@
 //   X = B X             X's tiles as they lie are the MN-major operand: nothing is transposed
 //
 // Numerics.  Operands are fp16 (11 significant bits), sums fp32 in tensor memory.  X is held times
-// kScale, so that entries down to 2.4e-7 stay normal numbers; nothing exceeds about 1.3 in X and 7 in
-// B by the iteration's own bounds.  Each rounding is a choice: with bf16 operands the result is 1.1e-2
+// kScale, so that entries down to 2.4e-7 stay normal numbers; with the usual coefficients (3.4445, -4.7750, 2.0315)
+// nothing exceeds about 1.3 in X and 4 in B, and others are refused where X, A or B might leave the
+// type's range (in_range).  Each rounding is a choice: with bf16 operands the result is 1.1e-2
 // off (2-norm, 768 x 768, half the energy in rank 16), with fp16 2.1e-3, of which 1.7e-3 is the bf16
 // output's own rounding; a second fp16 term for X gained nothing more there.  Directions whose
 // singular value is below about 2^-12 of the largest are dominated by that rounding, as they are by
@@ -770,6 +771,38 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_
   if (warp == 0) { tc_fence_after(); tc_free(tm, 512); }
 }
 
+// Whether X (times kScale), A and B stay within fp16 (65504) for these coefficients.  An entry is no larger than the
+// largest singular value.  Those of X start in [0, 1] and go through s (a + b s^2 + c s^4), so they stay below the
+// largest magnitude of that on [0, top], step by step: at an end or where the derivative a + 3 b t + 5 c t^2 is zero
+// (t = s^2).  Roundings are allowed 2^-8 a step.  A has their squares, and B the magnitudes of a + b t + c t^2, largest
+// at an end or at t = -b / 2c.
+bool in_range(const float *coeffs, int steps) {
+  const double a = coeffs[0], b = coeffs[1], c = coeffs[2], slack = 1.0 + 1.0 / 256, most = 60000.0;
+  double top = slack;
+  for (int i = 0; i < steps; ++i) {
+    if (!(top * kScale <= most)) return false;            // (then A's entries, up to top squared, are in range too)
+    const double end = top * top;
+    double x = 0.0, y = fabs(a);
+    const auto at = [&](double t) {
+      if (!(t > 0.0 && t <= end)) return;
+      const double f = fabs(a + t * (b + t * c));
+      x = fmax(x, sqrt(t) * f);
+      y = fmax(y, f);
+    };
+    at(end);
+    if (c != 0.0) {
+      const double root = 9.0 * b * b - 20.0 * a * c;
+      at(-b / (2.0 * c));
+      if (root >= 0.0) { at((-3.0 * b + sqrt(root)) / (10.0 * c)); at((-3.0 * b - sqrt(root)) / (10.0 * c)); }
+    } else if (b != 0.0) {
+      at(-a / (3.0 * b));
+    }
+    if (!(y <= most)) return false;
+    top = x * slack;                                      // (the last X is written as bf16)
+  }
+  return true;
+}
+
 inline long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 struct Plan {
@@ -835,6 +868,7 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
     return CDGRAB_ERR_INVALID;
   if (!isfinite(coeffs[0]) || !isfinite(coeffs[1]) || !isfinite(coeffs[2])) return CDGRAB_ERR_INVALID;
   if (batch == 0 || rows == 0 || cols == 0) return CDGRAB_OK;
+  if (!in_range(coeffs, steps)) return CDGRAB_ERR_INVALID;
   if (!g || !o || !workspace || workspace_bytes < need || !cdg_aligned(workspace, 16) || gs < cols || os < cols ||
       os > 0x7fffffffll || (batch > 1 && (gb < 0 || ob < (long long)(rows - 1) * os + cols)))
     return CDGRAB_ERR_INVALID;

@@ -137,3 +137,18 @@ def test_wait_limit_arguments(lib):
     for bad in (-1, (1 << 40) + 1):
         assert lib.cdgrab_operators_wait_limit(bad) == binding.ERR_INVALID
     assert lib.cdgrab_operators_wait_limit(1 << 40) == binding.OK and lib.cdgrab_operators_wait_limit(0) == binding.OK
+
+
+def test_coefficients_that_leave_the_range_of_16_bits(lib):
+    """X, A and B are held in fp16: where a singular value could outgrow that, the call is refused; before any use of a
+    device, so that the others get as far as finding none here."""
+    def call(co, steps):
+        return lib.cdgrab_orthogonalise(2, 8, 16, 0, P, 128, 16, steps, (C.c_float * 3)(*co), 0.0, P, 128, 16, P, 1 << 40, None)
+    for co, steps in (((2.0, 0.0, 0.0), 10), ((2.0, 0.0, 0.0), 64), ((1e5, 0.0, 0.0), 1), ((0.0, 300.0, 0.0), 2), ((4.0, 0.0, 1.0), 3),
+                      ((0.0, 0.0, -250.0), 2), ((1.0, 1.0, 1.0), 8), ((3e38, -3e38, 3e38), 2)):
+        assert call(co, steps) == binding.ERR_INVALID, (co, steps)
+    if torch.cuda.is_available():
+        return               # (the addresses are not real)
+    for co, steps in (((3.4445, -4.7750, 2.0315), 64), ((1.5, -0.5, 0.0), 64), ((1.875, -1.25, 0.375), 64), ((2.0, -1.5, 0.5), 64),
+                      ((3.0, -3.2, 1.2), 30), ((1.0, 0.0, 0.0), 64), ((0.0, 0.0, 0.0), 64), ((2.0, 0.0, 0.0), 8), ((0.0, 300.0, 0.0), 1), ((-1.0, 0.5, 0.0), 9)):
+        assert call(co, steps) == binding.ERR_DEVICE, (co, steps)

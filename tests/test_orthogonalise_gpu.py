@@ -135,3 +135,16 @@ def test_refusals():
     for kw in (dict(steps=0), dict(steps=65), dict(eps=-1.0), dict(coeffs=(float("nan"), 0.0, 0.0))):
         with pytest.raises(binding.CdgrabError):
             binding.orthogonalise(g, **kw)
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 70), (300, 700)])
+def test_coefficients_at_the_edge_of_the_range(rows, cols):
+    """One singular value that doubles with every step: 128 is the last that X is stored with; one step more is refused."""
+    g = torch.zeros(rows, cols, device="cuda")
+    g[3, 5] = 1.0
+    want = torch.zeros(rows, cols, device="cuda")
+    want[3, 5] = 256.0
+    assert torch.equal(binding.orthogonalise(g, steps=8, coeffs=(2.0, 0.0, 0.0), eps=0.0).float(), want)
+    for steps in (9, 10):
+        with pytest.raises(binding.CdgrabError):
+            binding.orthogonalise(g, steps=steps, coeffs=(2.0, 0.0, 0.0), eps=0.0)
