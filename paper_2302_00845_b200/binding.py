@@ -11,8 +11,6 @@ import ctypes as C
 import os
 import struct
 
-import torch
-
 HERE = os.path.dirname(os.path.abspath(__file__))
 # CDGRAB_LIB: file name (inside the package) of a diagnostic build to load instead
 LIB_PATH = os.path.join(HERE, os.path.basename(os.environ.get("CDGRAB_LIB", "libcdgrab.so")))
@@ -354,14 +352,23 @@ def herding_objective(z, perms, stream=None) -> float:
 # ---- training operators --------------------------------------------------------------------------
 # A call costs a few microseconds of host time, as much as a small operator takes on the device: checks
 # build their messages only when they fail, and shapes cross the boundary as one packed struct.
-_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+torch = None          # imported by the first call: the module itself loads, and finds the library, without it
 _SHAPE = struct.Struct("7if24q")          # cdgrab_attention_shape
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _use_torch():
+    global torch, _CODES, _raw_stream
+    import torch as t
+    _CODES = {t.float32: F32, t.bfloat16: BF16}
+    _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda dev: t.cuda.current_stream(dev).cuda_stream)
+    torch = t             # last: it tells other threads that the rest is there
 
 
 def _place(stream, *tensors):
     """Where an operator runs: the raw stream, and the torch stream whose pool its outputs and scratch come
     from when that is not the current one (so that freeing them is ordered after the launches)."""
+    if torch is None:
+        _use_torch()
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:

@@ -2,6 +2,9 @@
 that the GPU tests compare with, against automatic differentiation."""
 import ctypes as C
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -152,3 +155,11 @@ def test_coefficients_that_leave_the_range_of_16_bits(lib):
     for co, steps in (((3.4445, -4.7750, 2.0315), 64), ((1.5, -0.5, 0.0), 64), ((1.875, -1.25, 0.375), 64), ((2.0, -1.5, 0.5), 64),
                       ((3.0, -3.2, 1.2), 30), ((1.0, 0.0, 0.0), 64), ((0.0, 0.0, 0.0), 64), ((2.0, 0.0, 0.0), 8), ((0.0, 300.0, 0.0), 1), ((-1.0, 0.5, 0.0), 9)):
         assert call(co, steps) == binding.ERR_DEVICE, (co, steps)
+
+
+def test_the_binding_loads_without_torch(lib):
+    """torch provides buffers to the calls that take them; the module and the library need none of it."""
+    code = ("import sys; sys.modules['torch'] = None\n"
+            "from paper_2302_00845_b200 import binding\n"
+            "assert binding.lib().cdgrab_strerror(-1) and binding.lib().cdgrab_layer_norm_workspace_bytes(4, 100, 64) >= 0\n")
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=120)
