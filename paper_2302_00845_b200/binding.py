@@ -470,7 +470,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=None, dx=
             pw = dweight.data_ptr()
         if dbias is not None:
             pb = dbias.data_ptr()
-            if dbias is not g and (dbias.dtype != g.dtype or _row_stride(dbias, "dbias", m, cols) != ws):
+            # (with one worker the row stride is not used)
+            if dbias is not g and (dbias.dtype != g.dtype or (_row_stride(dbias, "dbias", m, cols) != ws and m > 1)):
                 raise ValueError("dweight and dbias: one type and one row stride")
     if dx is None:
         dx, dxs = _empty_like(x, other), cols

@@ -179,3 +179,15 @@ def test_refusals():
         binding.layer_norm_forward(x, w, b, eps=-1.0)
     with pytest.raises(binding.CdgrabError):
         binding.layer_norm_forward(x, w, b, eps=float("nan"))
+
+
+def test_one_worker_with_gradients_in_different_buffers():
+    """With a single worker there is no distance from row to row: views of buffers of any width go together."""
+    x, dy, w, b = draw(1, 6, 40, "f32")
+    wide, narrow = torch.full((1, 90), 3.0, device="cuda"), torch.full((1, 55), 3.0, device="cuda")
+    check(x, dy, w, b, 1, "f32", dweight=wide[:, 20:60], dbias=narrow[:, 4:44])
+    assert (wide[:, :20] == 3).all() and (wide[:, 60:] == 3).all() and (narrow[:, :4] == 3).all() and (narrow[:, 44:] == 3).all()
+    x, dy, w, b = draw(2, 3, 40, "f32")
+    _, mean, rstd = binding.layer_norm_forward(x, w, b)
+    with pytest.raises(ValueError):
+        binding.layer_norm_backward(dy, x, w, mean, rstd, torch.empty(2, 90, device="cuda")[:, :40], torch.empty(2, 40, device="cuda"))
