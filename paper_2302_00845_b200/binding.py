@@ -354,6 +354,7 @@ def herding_objective(z, perms, stream=None) -> float:
 # build their messages only when they fail, and shapes cross the boundary as one packed struct.
 torch = None          # imported by the first call: the module itself loads, and finds the library, without it
 _SHAPE = struct.Struct("7if24q")          # cdgrab_attention_shape
+_INT_MAX = 2 ** 31 - 1                    # ctypes passes the low 32 bits of a larger number without a word
 
 
 def _use_torch():
@@ -430,6 +431,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, s
     if x.dim() != 2:
         raise ValueError(f"x: [rows][cols], not {tuple(x.shape)}")
     rows, cols = x.shape
+    if cols > _INT_MAX:
+        raise ValueError(f"x: {cols} columns")
     code = _code(x, "x")
     xs = _row_stride(x, "x", rows, cols)
     w, b = _vector(weight, "weight", cols), _vector(bias, "bias", cols)
@@ -456,6 +459,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dweight=None, dbias=None, dx=
     if x.dim() != 2:
         raise ValueError(f"x: [rows][cols], not {tuple(x.shape)}")
     rows, cols = x.shape
+    if cols > _INT_MAX:
+        raise ValueError(f"x: {cols} columns")
     code = _code(x, "x")
     if dy.dtype != x.dtype:
         raise ValueError("dy: the type of x")
@@ -577,15 +582,17 @@ def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: floa
     `steps` Newton-Schulz products on g / (|g| + eps).  Coefficients that do not keep singular values out of [0, 1]
     below 234 until the last step are refused.  Returns a bfloat16 tensor of g's shape."""
     handle, other = _place(stream, g, out)
-    o = _empty(g, g.shape, torch.bfloat16, other) if out is None else out
     if g.dim() not in (2, 3):
         raise ValueError("g: [rows][cols] or [batch][rows][cols]")
+    rows, cols = g.shape[-2:]
+    batch = g.shape[0] if g.dim() == 3 else 1
+    if max(batch, rows, cols, abs(steps)) > _INT_MAX:
+        raise ValueError(f"g: {tuple(g.shape)}, {steps} steps: beyond 32 bits")
+    o = _empty(g, g.shape, torch.bfloat16, other) if out is None else out
     if o.dtype != torch.bfloat16 or o.shape != g.shape:
         raise ValueError("out: a bfloat16 tensor of g's shape")
     if len(coeffs) != 3:
         raise ValueError("coeffs: three numbers")
-    rows, cols = g.shape[-2:]
-    batch = g.shape[0] if g.dim() == 3 else 1
     strides = []
     for t, name in ((g, "g"), (o, "out")):
         s = t.stride()
