@@ -352,6 +352,9 @@ def herding_objective(z, perms, stream=None) -> float:
 # ---- training operators --------------------------------------------------------------------------
 # A call costs a few microseconds of host time, as much as a small operator takes on the device: checks
 # build their messages only when they fail, and shapes cross the boundary as one packed struct.
+# `stream`: the torch stream to run on, the current one by default.  The caller orders it after what makes the inputs;
+# the tensors that are passed are kept from reuse until it has got past the call, and what is returned belongs to it, as
+# under torch.cuda.stream.
 torch = None          # imported by the first call: the module itself loads, and finds the library, without it
 _SHAPE = struct.Struct("7if24q")          # cdgrab_attention_shape
 _INT_MAX = 2 ** 31 - 1                    # ctypes passes the low 32 bits of a larger number without a word
@@ -367,7 +370,8 @@ def _use_torch():
 
 def _place(stream, *tensors):
     """Where an operator runs: the raw stream, and the torch stream whose pool its outputs and scratch come
-    from when that is not the current one (so that freeing them is ordered after the launches)."""
+    from when that is not the current one (so that freeing them is ordered after the launches).  The tensors, which
+    come from other streams' pools then, are recorded on it."""
     if torch is None:
         _use_torch()
     dev = torch.cuda.current_device()
@@ -377,6 +381,9 @@ def _place(stream, *tensors):
     current = _raw_stream(dev)
     if stream is None or stream.cuda_stream == current:
         return current, None
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
     return stream.cuda_stream, stream
 
 

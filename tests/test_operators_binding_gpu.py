@@ -21,3 +21,46 @@ def test_numbers_beyond_32_bits_are_refused():
         binding.layer_norm_forward(wide, out=wide)
     with pytest.raises(ValueError):
         binding.layer_norm_backward(wide, wide, None, stats, stats, dx=wide)
+
+
+def late(call, *tensors):
+    """call(stream, *copies) on a stream that has 20 ms of other work to do first, with copies of the tensors that are
+    given up, and their memory asked for again and overwritten, before it gets there."""
+    copies = [t.clone() for t in tensors]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(40_000_000)
+    out = call(s, *copies)
+    del copies
+    again = [torch.full_like(t, 7) for t in tensors for _ in range(3)]
+    torch.cuda.synchronize()
+    del again
+    assert binding.operators_status() == binding.OK
+    return out
+
+
+def test_inputs_given_up_after_a_call_on_another_stream():
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, dy, w, b = r(512, 1000), r(512, 1000), r(1000), r(1000)
+    want = binding.layer_norm_forward(x, w, b)
+    for got, val in zip(late(lambda s, *t: binding.layer_norm_forward(*t, stream=s), x, w, b), want):
+        assert torch.equal(got, val)
+    grads = torch.empty(4, 1000, device="cuda")
+    dx = binding.layer_norm_backward(dy, x, w, *want[1:], grads)
+    grads2 = torch.empty_like(grads)
+    assert torch.equal(late(lambda s, *t: binding.layer_norm_backward(*t, grads2, stream=s), dy, x, w, *want[1:]), dx)
+    assert torch.equal(grads2, grads)
+    q, k, v, do = (r(2, 600, h, 64).bfloat16() for h in (4, 2, 2, 4))
+    lens = torch.tensor([600, 333], dtype=torch.int32, device="cuda")
+    want = binding.attention_forward(q, k, v, True, None, lens, lens)
+    fwd = lambda s, *t: binding.attention_forward(*t[:3], True, None, *t[3:], stream=s)  # noqa: E731
+    for got, val in zip(late(fwd, q, k, v, lens, lens), want):
+        assert torch.equal(got, val)
+    grads = binding.attention_backward(do, q, k, v, *want, True, None, lens, lens)
+    bwd = lambda s, *t: binding.attention_backward(*t[:6], True, None, *t[6:], stream=s)  # noqa: E731
+    for got, val in zip(late(bwd, do, q, k, v, *want, lens, lens), grads):
+        assert torch.equal(got, val)
+    g = r(300, 700)
+    assert torch.equal(late(lambda s, t: binding.orthogonalise(t, stream=s), g), binding.orthogonalise(g))
