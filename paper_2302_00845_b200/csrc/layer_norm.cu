@@ -351,14 +351,15 @@ __global__ void __launch_bounds__(kThreads) ln_backward_join(int chunks, int col
   __shared__ float sm[8][33];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), k0 = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 32 + (threadIdx.x & 31), both = 2ll * cols;
+  const int k0 = threadIdx.x >> 5;
   float s = 0.0f;
-  if (c < 2 * cols)
+  if (c < both)
 #pragma unroll 8
-    for (int k = k0; k < chunks; k += 8) s += part[((long long)blockIdx.y * chunks + k) * 2 * cols + c];
+    for (int k = k0; k < chunks; k += 8) s += part[((long long)blockIdx.y * chunks + k) * both + c];
   sm[k0][threadIdx.x & 31] = s;
   __syncthreads();
-  if (k0 == 0 && c < 2 * cols) {
+  if (k0 == 0 && c < both) {
     for (int k = 1; k < 8; ++k) s += sm[k][threadIdx.x];
     G *out = c < cols ? dw : db;
     if (out) out[(long long)blockIdx.y * ws + (c < cols ? c : c - cols)] = cdg_cast<G>(s);
@@ -394,26 +395,35 @@ __global__ void __launch_bounds__(kThreads) ln_forward_long(int cols, const T *_
   }
 }
 
-// the worker's sums of dy n and dy, one thread per column (before dx: it may overwrite dy or x)
+// a worker's (blockIdx.z) sums of dy n and dy over a chunk (blockIdx.y) of its rows, one thread per column, before
+// dx, which may overwrite dy or x; to part[worker][chunk][2][cols] where there are several chunks, else to the gradients
+// (a worker's rows in one chain of additions: 20,000 equal gradients drifted by 1.7e-4 of their sum, and 4096 rows of 8193
+// bf16 took 1602 us; in chunks 126 us, of which the two passes of dx are the larger part)
 template <typename T, typename G>
-__global__ void __launch_bounds__(kThreads) ln_backward_columns(long long rows, int cols, const T *__restrict__ dy,
+__global__ void __launch_bounds__(kThreads) ln_backward_columns(long long rows, long long per, int cols, const T *__restrict__ dy,
                                                                 long long dys, const T *__restrict__ x, long long xs,
                                                                 const float *__restrict__ mean,
-                                                                const float *__restrict__ rstd, G *dw, G *db,
+                                                                const float *__restrict__ rstd, float *part, G *dw, G *db,
                                                                 long long ws) {
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int c = blockIdx.x * kThreads + threadIdx.x;
   if (c >= cols) return;
-  const long long r0 = (long long)blockIdx.y * rows;
+  const long long r0 = (long long)blockIdx.z * rows, end = r0 + min(rows, (long long)(blockIdx.y + 1) * per);
   float sw = 0.0f, sb = 0.0f;
-  for (long long r = r0; r < r0 + rows; ++r) {
+  for (long long r = r0 + blockIdx.y * per; r < end; ++r) {
     const float d = cdg_ld(dy + r * dys + c);
     sw += d * ((cdg_ld(x + r * xs + c) - mean[r]) * rstd[r]);
     sb += d;
   }
-  if (dw) dw[(long long)blockIdx.y * ws + c] = cdg_cast<G>(sw);
-  if (db) db[(long long)blockIdx.y * ws + c] = cdg_cast<G>(sb);
+  if (part) {
+    float *mine = part + ((long long)blockIdx.z * gridDim.y + blockIdx.y) * 2 * cols;
+    mine[c] = sw;
+    mine[(long long)cols + c] = sb;
+    return;
+  }
+  if (dw) dw[(long long)blockIdx.z * ws + c] = cdg_cast<G>(sw);
+  if (db) db[(long long)blockIdx.z * ws + c] = cdg_cast<G>(sb);
 }
 
 template <typename T>
@@ -529,6 +539,11 @@ struct BackwardCall {
 constexpr int kSms = 148;
 int chunks_of(int m, long long rows, int cols) {
   const Layout l = layout_of(4, cols, 1);           // the threads depend on the columns alone
+  if (l.long_row) {        // blocks of 256 columns, eight to an SM; at least 16 rows
+    const long long blocks = ((long long)cols + kThreads - 1) / kThreads * m, most = 2 * 8 * kSms / blocks, fit = (rows + 15) / 16;
+    const long long c = most < fit ? most : fit;
+    return (int)(c < 1 ? 1 : c);
+  }
   const long long resident = l.block ? 512 / l.threads : 2;
   const long long most = 2 * resident * kSms / m, fit = l.block ? (rows + 1) / 2 : (rows + kWarps - 1) / kWarps;
   const long long c = most < fit ? most : fit;
@@ -565,7 +580,7 @@ extern "C" int cdgrab_layer_norm_forward(long long rows, int cols, int dtype, co
 extern "C" long long cdgrab_layer_norm_workspace_bytes(int m, long long rows, int cols) {
   if (m < 1 || m > 65535 || rows < 0 || cols < 1 || (rows > 0 && m >= (1ll << 31) / rows)) return -1;
   const int chunks = chunks_of(m, rows, cols);
-  return chunks > 1 && cols <= kMaxWide * 16 ? 8ll * m * chunks * cols : 16;
+  return chunks > 1 ? 8ll * m * chunks * cols : 16;
 }
 
 template <typename T, typename G>
@@ -573,8 +588,8 @@ static cudaError_t backward_long(const BackwardCall &c) {
   cudaError_t e = cudaSuccess;
   // (before dx, which may overwrite dy or x)
   if (c.dw || c.db)
-    e = cdg_ops_launch(ln_backward_columns<T, G>, dim3((c.cols + kThreads - 1) / kThreads, c.m), kThreads, 0, c.st, c.rows, c.cols,
-                       (const T *)c.dy, c.dys, (const T *)c.x, c.xs, c.mean, c.rstd, (G *)c.dw, (G *)c.db, c.ws);
+    e = cdg_ops_launch(ln_backward_columns<T, G>, dim3((c.cols + kThreads - 1) / kThreads, c.chunks, c.m), kThreads, 0, c.st, c.rows,
+                       c.per, c.cols, (const T *)c.dy, c.dys, (const T *)c.x, c.xs, c.mean, c.rstd, c.part, (G *)c.dw, (G *)c.db, c.ws);
   if (e == cudaSuccess && c.dx && c.rows)
     e = cdg_ops_launch(ln_backward_long<T>, dim3((unsigned)(c.m * c.rows)), kThreads, 0, c.st, c.cols, (const T *)c.dy, c.dys,
                        (const T *)c.x, c.xs, c.w, c.mean, c.rstd, (T *)c.dx, c.dxs);
@@ -602,13 +617,15 @@ extern "C" int cdgrab_layer_norm_backward(int m, long long rows, int cols, int d
   const int chunks = chunks_of(m, rows, cols), gbf = grad_dtype == CDGRAB_BF16;
   BackwardCall c = {m, rows, (rows + chunks - 1) / chunks, chunks, cols, dy, dys, x, xs, w, mean, rstd, dx, dxs,
                     chunks > 1 ? (float *)workspace : nullptr, dw, db, ws, gbf, l, dev->index, st};
+  int rc;
   if (l.long_row) {
-    if (dtype == CDGRAB_F32) return cdg_launch_rc(gbf ? backward_long<float, __nv_bfloat16>(c) : backward_long<float, float>(c));
-    return cdg_launch_rc(gbf ? backward_long<__nv_bfloat16, __nv_bfloat16>(c) : backward_long<__nv_bfloat16, float>(c));
+    if (dtype == CDGRAB_F32) rc = cdg_launch_rc(gbf ? backward_long<float, __nv_bfloat16>(c) : backward_long<float, float>(c));
+    else rc = cdg_launch_rc(gbf ? backward_long<__nv_bfloat16, __nv_bfloat16>(c) : backward_long<__nv_bfloat16, float>(c));
+  } else {
+    rc = cdg_launch_rc(dtype == CDGRAB_F32 ? by_layout<float>(l, c) : by_layout<__nv_bfloat16>(l, c));
   }
-  int rc = cdg_launch_rc(dtype == CDGRAB_F32 ? by_layout<float>(l, c) : by_layout<__nv_bfloat16>(l, c));
   if (rc == CDGRAB_OK && chunks > 1 && (dw || db)) {
-    const dim3 grid((2 * cols + 31) / 32, m);
+    const dim3 grid((unsigned)((2ll * cols + 31) / 32), m);
     rc = cdg_launch_rc(gbf ? cdg_ops_launch(ln_backward_join<__nv_bfloat16>, grid, kThreads, 0, st, chunks, cols, c.part,
                                             (__nv_bfloat16 *)dw, (__nv_bfloat16 *)db, ws)
                            : cdg_ops_launch(ln_backward_join<float>, grid, kThreads, 0, st, chunks, cols, c.part, (float *)dw,

@@ -191,3 +191,34 @@ def test_one_worker_with_gradients_in_different_buffers():
     _, mean, rstd = binding.layer_norm_forward(x, w, b)
     with pytest.raises(ValueError):
         binding.layer_norm_backward(dy, x, w, mean, rstd, torch.empty(2, 90, device="cuda")[:, :40], torch.empty(2, 40, device="cuda"))
+
+
+@pytest.mark.parametrize("cols", [8192, 8193, 16384])
+def test_sums_over_many_rows_are_no_single_chain(cols):
+    """20,000 rows that all add 0.1: one chain of 32-bit additions drifts by 1e-4 of the sum.  The rows are added up in
+    parts, so that no value goes through more than about a thousand additions, whatever the number of columns."""
+    rows = 20000
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(rows, cols, generator=g, device="cuda")
+    x[:, ::2] = x[:, ::2].abs() + 0.5          # the sums of dy n have a sign too
+    dy = torch.full_like(x, 0.1)
+    _, mean, rstd = binding.layer_norm_forward(x)
+    dw, db = torch.empty(1, cols, device="cuda"), torch.empty(1, cols, device="cuda")
+    binding.layer_norm_backward(dy, x, None, mean, rstd, dw, db)
+    value = dy[0, 0].double()
+    n = torch.zeros(cols, dtype=torch.float64, device="cuda")
+    size, off = n.clone(), n.clone()
+    for i in range(0, rows, 2000):
+        part = (x[i:i + 2000].double() - mean[i:i + 2000, None].double()) * rstd[i:i + 2000, None].double()
+        n += part.sum(0)
+        size += part.abs().sum(0)
+        off += 3 * part.abs().sum(0) + (x[i:i + 2000].abs() + mean[i:i + 2000, None].abs()).mul(rstd[i:i + 2000, None]).double().sum(0)
+    chain = 1088 * ref.U32
+    assert (db[0].double() - rows * value).abs().max() <= chain * rows * value
+    assert ((dw[0].double() - value * n).abs() <= value * (chain * size + ref.U32 * off)).all()
+
+
+@pytest.mark.parametrize("m,rows,cols,dtype", [(1, 4097, 8193, "bf16"), (5, 333, 16384, "bf16"), (3, 50, 9001, "f32"), (64, 17, 8200, "f32")])
+@pytest.mark.parametrize("grads", ["f32", "bf16"])
+def test_long_rows_of_workers(m, rows, cols, dtype, grads):
+    check(*draw(m, rows, cols, dtype), m, grads)
