@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(kThreads) ln_backward_join(int chunks, int col
 }
 
 // ---- longer rows ------------------------------------------------------------------------------------
-// one block per row, three passes over it
+// one block per row, three passes over it (columns counted without a sign: the last step may pass 2^31)
 template <typename T>
 __global__ void __launch_bounds__(kThreads) ln_forward_long(int cols, const T *__restrict__ x, long long xs,
                                                             const float *__restrict__ w, const float *__restrict__ b,
@@ -378,14 +378,15 @@ __global__ void __launch_bounds__(kThreads) ln_forward_long(int cols, const T *_
   cdg_grid_dep_trigger();
   const T *xr = x + (long long)blockIdx.x * xs;
   T *yr = y + (long long)blockIdx.x * ys;
+  const unsigned n_cols = cols;
   const float inv = 1.0f / (float)cols;
   float s = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += kThreads) s += cdg_ld(xr + c);
+  for (unsigned c = threadIdx.x; c < n_cols; c += kThreads) s += cdg_ld(xr + c);
   const float mean = block_sum(s, 0.0f, sm).x * inv;
   s = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += kThreads) { const float d = cdg_ld(xr + c) - mean; s += d * d; }
+  for (unsigned c = threadIdx.x; c < n_cols; c += kThreads) { const float d = cdg_ld(xr + c) - mean; s += d * d; }
   const float rstd = 1.0f / sqrtf(block_sum(s, 0.0f, sm).x * inv + eps);
-  for (int c = threadIdx.x; c < cols; c += kThreads) {
+  for (unsigned c = threadIdx.x; c < n_cols; c += kThreads) {
     const float n = (cdg_ld(xr + c) - mean) * rstd;
     yr[c] = cdg_cast<T>(n * (w ? w[c] : 1.0f) + (b ? b[c] : 0.0f));
   }
@@ -407,8 +408,8 @@ __global__ void __launch_bounds__(kThreads) ln_backward_columns(long long rows, 
                                                                 long long ws) {
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= cols) return;
+  const unsigned c = blockIdx.x * kThreads + threadIdx.x;
+  if (c >= (unsigned)cols) return;
   const long long r0 = (long long)blockIdx.z * rows, end = r0 + min(rows, (long long)(blockIdx.y + 1) * per);
   float sw = 0.0f, sb = 0.0f;
   for (long long r = r0 + blockIdx.y * per; r < end; ++r) {
@@ -437,15 +438,16 @@ __global__ void __launch_bounds__(kThreads) ln_backward_long(int cols, const T *
   const long long r = blockIdx.x;
   const T *dyr = dy + r * dys, *xr = x + r * xs;
   T *dxr = dx + r * dxs;
+  const unsigned n_cols = cols;
   const float mu = mean[r], rs = rstd[r], inv = 1.0f / (float)cols;
   float s1 = 0.0f, s2 = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += kThreads) {
+  for (unsigned c = threadIdx.x; c < n_cols; c += kThreads) {
     const float g = cdg_ld(dyr + c) * (w ? w[c] : 1.0f);
     s1 += g;
     s2 += g * ((cdg_ld(xr + c) - mu) * rs);
   }
   const float2 t = block_sum(s1, s2, sm);
-  for (int c = threadIdx.x; c < cols; c += kThreads) {
+  for (unsigned c = threadIdx.x; c < n_cols; c += kThreads) {
     const float g = cdg_ld(dyr + c) * (w ? w[c] : 1.0f);
     const float n = (cdg_ld(xr + c) - mu) * rs;
     dxr[c] = cdg_cast<T>(rs * (g - t.x * inv - n * (t.y * inv)));
@@ -482,6 +484,7 @@ Layout layout_of(int elem, int cols, int vec) {
   l.long_row = cols > kMaxWide * 16;
   // up to 1024 columns a warp holds the row (32 values a lane) and needs no barrier; above, blocks of
   // ceil(cols / 16) threads
+  if (l.long_row) return l;
   l.block = cols > 1024;
   l.e = l.block ? 16 : (cols + 255) / 256 * 8;
   l.threads = l.block ? ((cols + 15) / 16 + 31) / 32 * 32 : kThreads;
@@ -588,7 +591,7 @@ static cudaError_t backward_long(const BackwardCall &c) {
   cudaError_t e = cudaSuccess;
   // (before dx, which may overwrite dy or x)
   if (c.dw || c.db)
-    e = cdg_ops_launch(ln_backward_columns<T, G>, dim3((c.cols + kThreads - 1) / kThreads, c.chunks, c.m), kThreads, 0, c.st, c.rows,
+    e = cdg_ops_launch(ln_backward_columns<T, G>, dim3(((unsigned)c.cols + kThreads - 1) / kThreads, c.chunks, c.m), kThreads, 0, c.st, c.rows,
                        c.per, c.cols, (const T *)c.dy, c.dys, (const T *)c.x, c.xs, c.mean, c.rstd, c.part, (G *)c.dw, (G *)c.db, c.ws);
   if (e == cudaSuccess && c.dx && c.rows)
     e = cdg_ops_launch(ln_backward_long<T>, dim3((unsigned)(c.m * c.rows)), kThreads, 0, c.st, c.cols, (const T *)c.dy, c.dys,
