@@ -510,7 +510,8 @@ int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, const void *g
 int cdgrab_operators_status(void);
 
 /* How long a device-side wait of the calls that follow (of every thread) may last, in SM clock cycles up to
- * 2^40; 0: the default of 4e9, about two seconds.  A wait that lasts longer ends its kernel with
+ * 2^40; 0: the default of 4e9, about two seconds; longer in proportion where an attention call loops over more than
+ * 65,536 tiles of 128 tokens and a query head.  A wait that lasts longer ends its kernel with
  * CDGRAB_ERR_TIMEOUT in the status above; the context stays usable.  CDGRAB_ERR_INVALID: out of range. */
 int cdgrab_operators_wait_limit(long long cycles);
 

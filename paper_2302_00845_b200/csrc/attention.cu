@@ -1280,11 +1280,15 @@ bool shape_ok(const cdgrab_attention_shape *s) {
 }
 
 Sizes sizes_of(const cdgrab_attention_shape *s, const int32_t *q_lens, const int32_t *kv_lens, int *status) {
+  // a wait may span a block's whole loop: the limit grows with loops of more than 65,536 tiles (a tile takes 2000 to 3800
+  // cycles, the default limit allows 61,000)
+  const double tiles = fmax((double)((s->len_q + kT - 1) / kT) * (s->heads / s->kv_heads), (double)((s->len_kv + kT - 1) / kT));
+  const long long wait = (long long)((double)cdg_ops_wait_limit() * fmax(1.0, tiles / 65536));
   const int shared = (s->q_stride[0] > 0 ? 0 : kQ) | (s->k_stride[0] > 0 ? 0 : kK) | (s->v_stride[0] > 0 ? 0 : kV) |
                      (s->do_stride[0] > 0 ? 0 : kDo);
   return Sizes{s->batch, s->len_q, s->len_kv, s->heads, s->heads / s->kv_heads, s->head_dim, s->causal, s->scale,
                fmaxf(fabsf(s->scale) * kLog2e, 1e-30f), s->scale < 0.0f, shared, q_lens, kv_lens,
-               cdg_ops_wait_limit(), status};
+               wait, status};
 }
 View view(const void *p, const long long s[3]) { return View{(bf16 *)const_cast<void *>(p), s[0], s[1], s[2]}; }
 

@@ -57,3 +57,23 @@ def test_orthogonalise(short_waits, batch, rows, cols):
     binding.operators_wait_limit(0)
     assert torch.equal(binding.orthogonalise(g), want)
     assert binding.operators_status() == binding.OK
+
+
+def test_a_long_loop_is_no_expired_wait():
+    """262,144 tiles of queries and heads share one key head: the loop over them, in a cluster of eight, takes longer than
+    the limit for short loops, and nothing is wrong.  (With the default limit it would take ten million tiles.)"""
+    t, h, d = 262144, 128, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda n, heads: torch.randn(1, n, heads, d, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    q, k, v, do = r(t, h), r(128, 1), r(128, 1), r(t, h)
+    o, lse = binding.attention_forward(q, k, v)
+    want = binding.attention_backward(do, q, k, v, o, lse)
+    assert binding.operators_status() == binding.OK
+    try:
+        binding.operators_wait_limit(30_000_000)
+        got = binding.attention_backward(do, q, k, v, o, lse)
+        assert binding.operators_status() == binding.OK
+    finally:
+        binding.operators_wait_limit(0)
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)
