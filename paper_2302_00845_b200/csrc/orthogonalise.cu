@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) orth_start(const T *g, long long gb, long
     if (tall) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) tile[tx + e][r] = h.v[e];
-    } else if (VEC == 1 || ldx % VEC == 0) {
+    } else {                 // (whole pieces: ldx is a multiple of 8)
       *reinterpret_cast<Half *>(out + (long long)(r0 + r) * ldx + c0 + tx) = h;
     }
   }
@@ -494,9 +494,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
           tc_load32(piece.acc + c0, v);
           tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)            // (where no step of K fell to this rank, another tile's products lie there)
-            *reinterpret_cast<uint4 *>(base + S::sums + sum_at(r, (c0 >> 2) + i)) =
-                u.nk == 0 ? make_uint4(0, 0, 0, 0) : make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          for (int i = 0; i < 8; ++i)            // (every rank has had two steps of K at least)
+            *reinterpret_cast<uint4 *>(base + S::sums + sum_at(r, (c0 >> 2) + i)) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         }
         tc_fence_before();
         tc_warp_arrive(empty);
@@ -906,7 +905,6 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   for (int i = 0; i < 2; ++i)
     if (!tc_encode(&maps.to_x[i], false, x[i], 3, dx, sx, 32, 32)) return CDGRAB_ERR_CUDA;
   if (!tc_encode(&maps.A, false, A, 3, da, sa, kM) || !tc_encode(&maps.B, false, B, 3, da, sa, kM) ||
-      !tc_encode(&maps.to_A, false, A, 3, da, sa, 32, 32) || !tc_encode(&maps.to_B, false, B, 3, da, sa, 32, 32) ||
       !tc_encode(&maps.to_A, false, A, 3, da, sa, 32, 32) || !tc_encode(&maps.to_B, false, B, 3, da, sa, 32, 32))
     return CDGRAB_ERR_CUDA;
 
