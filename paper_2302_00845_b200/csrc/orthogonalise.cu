@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_steps(const __grid_constant_
 // its product is over.
 constexpr int kSmallThreads = 512, kSmallCols = 576;         // (eight of the warps read accumulators, all move G and O)
 constexpr uint32_t kPanel = 16384;
-inline size_t small_smem(int n) { return (size_t)((n + 63) / 64 + 4) * kPanel + 1024; }
+inline size_t small_smem(int n) { return (size_t)((n + 63) / 64 + 4) * kPanel + 1024; }       // 1024: to a boundary of the swizzle
 
 struct SmallArgs {
   int rows, cols, tall, steps, vec;
@@ -550,7 +550,8 @@ __device__ __forceinline__ uint32_t small_at(int r, int c) { return (uint32_t)(c
 
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_bfloat16 *o, const SmallArgs p) {
-  extern __shared__ __align__(1024) uint8_t base[];
+  extern __shared__ __align__(16) uint8_t dyn[];
+  uint8_t *const base = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   __shared__ double part[kSmallThreads / 32];
   __shared__ __align__(8) uint64_t bar[5];         // A and A A; three blocks of X; the end
   __shared__ uint32_t slot;
@@ -620,8 +621,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small(const T *g, __nv_
   const uint32_t tm = slot, mine = tm + ((uint32_t)((warp & 3) * 32) << 16);
   const uint32_t sx = smem_u32(base), sa = smem_u32(A), sb = smem_u32(B);
   const int r = (warp & 3) * 32 + lane, half = warp >> 2;          // (warps 8 to 15: half 2 and 3, none of the columns)
-  const bool aligned = (sx & 1023u) == 0;
-  bool ok = aligned;
+  bool ok = true;
   uint32_t turn[4] = {0, 0, 0, 0};             // phases of the barriers
   // products whose K index runs along the rows of both operands, `panels_` panels of 64
   auto gram = [&](uint32_t x, int panels_) {
