@@ -18,6 +18,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "tensor_core.cuh"
 
 namespace {
@@ -828,7 +830,7 @@ Plan plan_of(long long batch, int rows, int cols) {
 template <int BN, int RANKS>
 int launch(const StepMaps &maps, const StepArgs &a, int sms, int device, cudaStream_t st) {
   static CdgPerDevice flags;
-  static int room[64];           // CTAs that are resident at once, by device
+  static std::atomic<int> room[64];           // CTAs that are resident at once, by device
   if (!tc_raise_limit(flags, orth_steps<BN, RANKS>, Shape<BN, RANKS>::smem)) return CDGRAB_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
@@ -840,12 +842,12 @@ int launch(const StepMaps &maps, const StepArgs &a, int sms, int device, cudaStr
   cfg.gridDim = dim3(sms / RANKS * RANKS); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = Shape<BN, RANKS>::smem; cfg.stream = st;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  int n = device < 64 ? room[device] : 0;
+  int n = device < 64 ? room[device].load(std::memory_order_relaxed) : 0;
   if (n == 0) {
     if (RANKS == 1) n = sms;
     else if (cudaOccupancyMaxActiveClusters(&n, orth_steps<BN, RANKS>, &cfg) != cudaSuccess || n < 1) return cdg_launch_rc(cudaErrorUnknown);
     else n = n * RANKS < sms ? n * RANKS : sms / RANKS * RANKS;
-    if (device < 64) room[device] = n;
+    if (device < 64) room[device].store(n, std::memory_order_relaxed);
   }
   cfg.gridDim = dim3(n);
   cfg.numAttrs = 2;
