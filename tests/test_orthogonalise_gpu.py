@@ -148,3 +148,18 @@ def test_coefficients_at_the_edge_of_the_range(rows, cols):
     for steps in (9, 10):
         with pytest.raises(binding.CdgrabError):
             binding.orthogonalise(g, steps=steps, coeffs=(2.0, 0.0, 0.0), eps=0.0)
+
+
+# tiles of 256 columns (there are as many of them as SMs), several to a block and product, batches in two parts of unequal
+# size, remainders in both directions; then tiles of 128 with more of them than SMs
+@pytest.mark.parametrize("batch,rows,cols,dtype", [(12, 2304, 768, torch.bfloat16), (13, 770, 2310, torch.float32), (7, 1030, 1300, torch.bfloat16),
+                                                   (7, 1300, 1030, torch.float32), (200, 100, 600, torch.float32), (31, 600, 1021, torch.bfloat16),
+                                                   (1, 1960, 2040, torch.float32), (1, 2041, 1961, torch.bfloat16), (2, 1300, 1290, torch.float32)])
+def test_more_tiles_than_multiprocessors(batch, rows, cols, dtype):
+    g = gradient(batch, rows, cols, dtype=dtype)
+    o = check(g)
+    want = ref.orthogonalise(g)
+    for i in range(batch):
+        assert off(o[i], want[i]) <= 4e-3
+    for _ in range(3):
+        assert torch.equal(binding.orthogonalise(g), o)
