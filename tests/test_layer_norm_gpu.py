@@ -222,3 +222,10 @@ def test_sums_over_many_rows_are_no_single_chain(cols):
 @pytest.mark.parametrize("grads", ["f32", "bf16"])
 def test_long_rows_of_workers(m, rows, cols, dtype, grads):
     check(*draw(m, rows, cols, dtype), m, grads)
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(9473, 64, "bf16"), (20001, 650, "bf16"), (30011, 33, "f32"), (40000, 1000, "bf16"), (3111, 1025, "f32"),
+                                             (7001, 1026, "bf16"), (5003, 2048, "f32"), (1500, 8192, "bf16"), (1301, 8191, "f32")])
+def test_more_rows_than_the_grid_takes_at_once(rows, cols, dtype):
+    """Warps, and blocks, that go on to further rows with the next one already requested."""
+    check(*draw(1, rows, cols, dtype), 1, "f32")
