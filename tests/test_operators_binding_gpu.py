@@ -64,3 +64,37 @@ def test_inputs_given_up_after_a_call_on_another_stream():
         assert torch.equal(got, val)
     g = r(300, 700)
     assert torch.equal(late(lambda s, t: binding.orthogonalise(t, stream=s), g), binding.orthogonalise(g))
+
+
+def test_captured_calls_run_on_what_the_buffers_hold():
+    """Every operator captured once and replayed on other data in the same buffers, and as it is called directly."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, dy, w, b = r(300, 768).bfloat16(), r(300, 768).bfloat16(), r(768), r(768)
+    grads = torch.empty(3, 2 * 768, device="cuda")
+    q, k, v, do = (r(2, 700, h, 64).bfloat16() for h in (4, 2, 2, 4))
+    g1, g2, g3 = r(3, 100, 200), r(650, 2600), r(4, 1000, 2600)      # one block; a cluster for a tile; many tiles
+
+    def calls():
+        y, mean, rstd = binding.layer_norm_forward(x, w, b)
+        dx = binding.layer_norm_backward(dy, x, w, mean, rstd, grads[:, :768], grads[:, 768:])
+        o, lse = binding.attention_forward(q, k, v, causal=True)
+        back = binding.attention_backward(do, q, k, v, o, lse, causal=True)
+        return (y, mean, rstd, dx, grads, o, lse) + tuple(back) + tuple(binding.orthogonalise(g) for g in (g1, g2, g3))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    for _ in range(3):
+        for t in (x, dy, w, b, q, k, v, do, g1, g2, g3):
+            t.copy_(r(*t.shape))
+        graph.replay()
+        got = [t.clone() for t in out]
+        for a, c in zip(got, calls()):
+            assert torch.equal(a, c)
+        assert binding.operators_status() == binding.OK
