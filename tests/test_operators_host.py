@@ -163,3 +163,23 @@ def test_the_binding_loads_without_torch(lib):
             "from paper_2302_00845_b200 import binding\n"
             "assert binding.lib().cdgrab_strerror(-1) and binding.lib().cdgrab_layer_norm_workspace_bytes(4, 100, 64) >= 0\n")
     subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=120)
+
+
+def test_layer_norm_reference_against_autograd():
+    """ref.layer_norm_backward itself, which the GPU tests compare with, and its forward pass."""
+    torch.manual_seed(1)
+    m, rows, cols = 3, 4, 11
+    x, dy = torch.randn(m * rows, cols), torch.randn(m * rows, cols)
+    w, b = torch.randn(cols), torch.randn(cols)
+    for weight in (w, None):
+        (y, _), (mean, _), (rstd, _) = ref.layer_norm_forward(x, weight, None if weight is None else b, 1e-5)
+        (dx, _), (dw, _), (db, _) = ref.layer_norm_backward(dy, x, weight, mean, rstd, m, torch.float32)
+        for i in range(m):
+            own = slice(i * rows, (i + 1) * rows)
+            xs = x[own].double().requires_grad_(True)
+            ws = (torch.ones(cols) if weight is None else weight).double().requires_grad_(True)
+            bs = (torch.zeros(cols) if weight is None else b).double().requires_grad_(True)
+            out = torch.nn.functional.layer_norm(xs, (cols,), ws, bs, 1e-5)
+            out.backward(dy[own].double())
+            for got, want in ((y[own], out.detach()), (dx[own], xs.grad), (dw[i], ws.grad), (db[i], bs.grad)):
+                assert torch.allclose(got, want, rtol=1e-11, atol=1e-12)
