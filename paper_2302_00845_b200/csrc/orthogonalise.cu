@@ -804,6 +804,7 @@ bool in_range(const float *coeffs, int steps) {
   return true;
 }
 
+constexpr long long kMaxStride = 1ll << 38;   // elements, as for attention: products with a row number stay below 2^63
 inline long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 struct Plan {
@@ -871,7 +872,7 @@ extern "C" int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, co
   if (batch == 0 || rows == 0 || cols == 0) return CDGRAB_OK;
   if (!in_range(coeffs, steps)) return CDGRAB_ERR_INVALID;
   if (!g || !o || !workspace || workspace_bytes < need || !cdg_aligned(workspace, 16) || gs < cols || os < cols ||
-      os > 0x7fffffffll || (batch > 1 && (gb < 0 || ob < (long long)(rows - 1) * os + cols)))
+      gs > kMaxStride || os > kMaxStride || (batch > 1 && (gb < 0 || ob < (long long)(rows - 1) * os + cols)))
     return CDGRAB_ERR_INVALID;
   if (!cdg_aligned(g, dtype == CDGRAB_F32 ? 4 : 2) || !cdg_aligned(o, 2)) return CDGRAB_ERR_INVALID;
   const CdgOpsDevice *dev;

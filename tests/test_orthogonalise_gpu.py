@@ -163,3 +163,11 @@ def test_more_tiles_than_multiprocessors(batch, rows, cols, dtype):
         assert off(o[i], want[i]) <= 4e-3
     for _ in range(3):
         assert torch.equal(binding.orthogonalise(g), o)
+
+
+@pytest.mark.parametrize("rows,cols", [(2, 40), (130, 70)])
+def test_output_rows_further_apart_than_32_bits(rows, cols):
+    g = gradient(1, rows, cols)[0]
+    far = torch.empty((rows - 1) * (1 << 24) + cols if rows > 2 else (1 << 31) + 8 + cols, dtype=torch.bfloat16, device="cuda")
+    out = far.as_strided((rows, cols), ((1 << 24) if rows > 2 else (1 << 31) + 8, 1))        # 4 GB, the last row past 2^31
+    assert torch.equal(binding.orthogonalise(g, out=out), binding.orthogonalise(g))
