@@ -412,7 +412,7 @@ int cdgrab_noalloc_status(void);
 /*
  * Layer normalisation over the last axis:  y = (x - mean) * rstd * weight + bias,
  * mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps).
- *   rows, cols   rows >= 0 (0: nothing to do), cols >= 1
+ *   rows, cols   rows from 0 (nothing to do) to 2^31 - 1, cols >= 1
  *   dtype        type of x and y
  *   x, y         [rows] rows of cols values, row starts x_stride / y_stride (>= cols) apart; y may be x
  *   weight, bias float [cols]; NULL: 1 and 0
@@ -435,7 +435,7 @@ int cdgrab_layer_norm_forward(long long rows, int cols, int dtype, const void *x
  *                NULL (not computed).  With rows_per_worker = 0 they are set to zero.
  *                worker_stride >= cols where m > 1.  The two may lie side by side in one row.
  *   workspace    16-byte aligned, cdgrab_layer_norm_workspace_bytes(m, rows_per_worker, cols) bytes
- *                (-1 for invalid sizes)
+ *                (-1 for invalid sizes: m from 1 to 65535, m * rows_per_worker below 2^31)
  */
 long long cdgrab_layer_norm_workspace_bytes(int m, long long rows_per_worker, int cols);
 int cdgrab_layer_norm_backward(int m, long long rows_per_worker, int cols, int dtype, const void *dy_dev,
@@ -455,7 +455,8 @@ int cdgrab_layer_norm_backward(int m, long long rows_per_worker, int cols, int d
  *
  * Shape (HOST struct): strides of q, k, v, o and of the gradients, in elements, for batch, token
  * and head; the head's values are contiguous.
- *   batch, len_q, len_kv   >= 0, lengths up to 4,194,304;  heads >= 1 a multiple of kv_heads >= 1
+ *   batch, len_q, len_kv   >= 0, batch up to 65535, lengths up to 4,194,304;  heads, up to 65535, >= 1 a multiple of
+ *                kv_heads >= 1;  batch x heads below 2^28; times tiles of 128 tokens below 2^32 forward, 2^28 backward
  *   head_dim     a multiple of 8 from 8 to 128
  *   strides      multiples of 8 and every base address a multiple of 16 bytes, as the bulk copies need;
  *                token and head strides at least head_dim where that axis is longer than 1
@@ -490,7 +491,8 @@ int cdgrab_attention_backward(const cdgrab_attention_shape *shape, const void *d
  * The orthogonalised update of a batch of matrices by Newton-Schulz products:
  *   X = G / (|G|_F + eps), then `steps` times   X <- a X + (b A + c A A) X,   A = X X^T
  * (of the transposed matrix where rows > cols), which drives the singular values towards one.
- *   batch, rows, cols   >= 0 (nothing to do where any is 0);  steps 1 to 64
+ *   batch, rows, cols   >= 0 (nothing to do where any is 0), batch up to 65535, rows and cols up to 2^20, together up
+ *                to 2^40 values;  steps 1 to 64;  row strides from cols to 2^38
  *   dtype    of G: [batch] matrices g_batch_stride apart, rows of cols contiguous values g_stride apart
  *   coeffs   HOST float [3]: a, b, c.  X, A and B are held in 16 bits: refused where a singular value that starts in
  *            [0, 1] may pass 234 before the last step, or |a + b s^2 + c s^4| 60000

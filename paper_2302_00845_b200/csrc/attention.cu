@@ -1337,14 +1337,12 @@ int backward(const cdgrab_attention_shape *s, const CUtensorMap &mq, const CUten
   const double part = s->causal ? 0.5 : 1.0;
   if (kt > 0) {
     const long long all = (long long)kt * s->kv_heads * s->batch;
-    if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of((double)qt * z.group, part * qt * z.group, all, sms);
     rc = tc_launch_cluster(attn_backward_kv<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dkv<NP>::smem, st, mq, mk, mv, mdo, z, kt, lines, padded,
                         dk, dv);
   }
   if (rc == CDGRAB_OK && qt > 0) {
     const long long all = (long long)qt * s->heads * s->batch;
-    if (all > 0x0fffffffll) return CDGRAB_ERR_INVALID;
     const int c = split_of(kt, part * kt, all, sms);
     rc = tc_launch_cluster(attn_backward_q<NP>, dim3((unsigned)(all * c)), c, kBwdThreads, Dq<NP>::smem, st, mq, mk, mv, mdo, z, qt, lines, padded, dq);
   }
@@ -1409,6 +1407,10 @@ extern "C" int cdgrab_attention_backward(const cdgrab_attention_shape *s, const 
       !out_ok(s->dv_stride, s->batch, s->len_kv, s->kv_heads, s->head_dim))
     return CDGRAB_ERR_INVALID;
   if (!workspace || workspace_bytes < cdgrab_attention_workspace_bytes(s)) return CDGRAB_ERR_INVALID;
+  // the grids: a block to a tile of rows, up to eight CTAs to a block
+  if ((long long)((s->len_q + kT - 1) / kT) * s->heads * s->batch > 0x0fffffffll ||
+      (long long)((s->len_kv + kT - 1) / kT) * s->kv_heads * s->batch > 0x0fffffffll)
+    return CDGRAB_ERR_INVALID;
   const CdgOpsDevice *dev;
   if (const int rc = cdg_ops_device(&dev)) return rc;
   cudaStream_t st = (cudaStream_t)stream;
@@ -1416,8 +1418,7 @@ extern "C" int cdgrab_attention_backward(const cdgrab_attention_shape *s, const 
   float *lines = (float *)workspace;
   const long long padded = ((long long)s->len_q + kT - 1) / kT * kT;
   if (s->len_q > 0) {
-    const long long blocks = (s->batch * padded * s->heads * 8 + 255) / 256;
-    if (blocks > 0x7fffffffll) return CDGRAB_ERR_INVALID;
+    const long long blocks = (s->batch * padded * s->heads * 8 + 255) / 256;       // four to a tile
     const int rc = cdg_launch_rc(cdg_ops_launch(attn_delta, dim3((unsigned)blocks), 256, 0, st, z, view(d_o, s->do_stride),
                                                 view(o, s->o_stride), lse, lines, (int)padded));
     if (rc != CDGRAB_OK) return rc;

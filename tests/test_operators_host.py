@@ -183,3 +183,11 @@ def test_layer_norm_reference_against_autograd():
             out.backward(dy[own].double())
             for got, want in ((y[own], out.detach()), (dx[own], xs.grad), (dw[i], ws.grad), (db[i], bs.grad)):
                 assert torch.allclose(got, want, rtol=1e-11, atol=1e-12)
+
+
+def test_attention_backward_refuses_too_many_tiles_before_anything_runs(lib):
+    b, h, t, d = 65535, 4096, 129, 8          # two tiles for each of 2^28 - 4096 heads
+    sh = shape(batch=b, len_q=t, len_kv=1, heads=h, kv_heads=h, head_dim=d, causal=0,
+               **{n: (256 * h * d, h * d, d) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")})
+    assert lib.cdgrab_attention_workspace_bytes(C.byref(sh)) > 0
+    assert lib.cdgrab_attention_backward(C.byref(sh), P, P, P, P, P, P, None, None, P, P, P, P, 1 << 60, None) == binding.ERR_INVALID
