@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(256) orth_start(const T *g, long long gb, long
 
 // ---- the steps ---------------------------------------------------------------------------------
 // One cooperative launch runs all steps: 3 x steps products with a barrier of the whole grid between them
-// (17 launches took 164 us for one 650 x 2600 matrix, ten microseconds each whatever they did; at present 154 us in
-// all there, mostly the latency of 15 dependent products, and 399 us, 681 TFLOP/s, for twelve of 2304 x 768, of which
-// 38 are the norm and the cast).  Persistent
+// (17 launches took 164 us for one 650 x 2600 matrix, ten microseconds each whatever they did; at present 150 us in
+// all there, mostly the latency of 15 dependent products, and 412 us, 660 TFLOP/s, for twelve of 2304 x 768: call after
+// call, under the power cap, 17 and 28 us for the norm and the cast and 357 for the steps, which take 316 alone).  Persistent
 // CTAs, one to an SM, take tiles of C = A op(B), 128 rows by 128 or BN columns: warp 0 keeps a ring of
 // shared-memory stages full (64 of K each), warp 1 issues the matrix instructions, warps 2 to 5 read the
 // accumulator, of which there are two in tensor memory so that one tile's products run under the other's
