@@ -396,8 +396,9 @@ int cdgrab_noalloc_status(void);
 
 /* ------------------------------------------------------------------------------------------------
  * Training operators beside the order server.  They make the stale gradients that are balanced
- * (layer norm and attention, forward and backward) and use the averaged gradient that
- * cdgrab_step_mean returns (the orthogonalised update).  None of them needs a handle.
+ * (layer norm, attention, the norms and the rotation of queries and keys, embedding and dropout, forward
+ * and backward) and use the averaged gradient that cdgrab_step_mean returns (the orthogonalised update).
+ * None of them needs a handle.
  *
  * All pointers are DEVICE pointers on the current device unless said otherwise; tensors are
  * CDGRAB_F32 or CDGRAB_BF16.  Strides are in elements.  Every call only enqueues work on
@@ -505,9 +506,135 @@ int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, const void *g
                          long long o_batch_stride, long long o_stride, void *workspace_dev,
                          long long workspace_bytes, void *stream);
 
+/*
+ * Embedding lookup:  y[g * length + j] = scale * table[tokens[g][j]].
+ *   groups, length   tokens come in `groups` rows of `length`, row starts token_stride (>= length) apart (a slice
+ *                of longer sequences); from 0 (nothing to do), together below 2^31
+ *   cols, vocab  >= 1
+ *   token_bits   32 or 64: tokens are signed integers of that size
+ *   padding      a token that stands for none: its row of y is zero and it has no gradient.  Any number; INT64_MIN where
+ *                there is none.  Any other token outside [0, vocab) is treated likewise and reported by
+ *                cdgrab_operators_status (CDGRAB_ERR_INVALID).
+ *   scale        finite
+ *   dtype        of the table: [vocab] rows of cols values, table_stride (>= cols) apart
+ *   out_dtype    of y: rows y_stride (>= cols) apart; y may not overlap the table
+ */
+int cdgrab_embedding_forward(long long groups, long long length, int cols, int vocab, int token_bits,
+                             const void *tokens_dev, long long token_stride, long long padding, float scale,
+                             int dtype, const void *table_dev, long long table_stride, int out_dtype, void *y_dev,
+                             long long y_stride, void *stream);
+
+/*
+ * Its gradient for m workers with `groups` rows of `length` tokens each (m * groups rows of tokens):
+ *   dtable[i][v] = scale * sum of dy over worker i's tokens that are v
+ * every row of every worker's table written, zero where no token names it: that worker's part of the gather
+ * buffer.  With accumulate = 1 the sums are added to what dtable holds (the gradient of a product that shares
+ * the matrix) and the other rows are left as they are.  The sums run over the tokens in the order of their
+ * positions, whatever the grid: results are the same bits every time.
+ *   dy           of `dtype`, a row for every token, dy_stride (>= cols) apart; rows of padding are not used
+ *   dtable       of grad_dtype: worker i's row v starts at i * worker_stride + v * row_stride;
+ *                row_stride >= cols where vocab > 1, worker_stride >= (vocab - 1) * row_stride + cols where m > 1
+ *   workspace    16-byte aligned, cdgrab_embedding_workspace_bytes(m, groups * length, cols, vocab) bytes
+ *                (-1 for invalid sizes: m from 1 to 65535, m * groups * length below 2^31)
+ */
+long long cdgrab_embedding_workspace_bytes(int m, long long tokens_per_worker, int cols, int vocab);
+int cdgrab_embedding_backward(int m, long long groups, long long length, int cols, int vocab, int token_bits,
+                              const void *tokens_dev, long long token_stride, long long padding, float scale,
+                              int dtype, const void *dy_dev, long long dy_stride, int grad_dtype, void *dtable_dev,
+                              long long worker_stride, long long row_stride, int accumulate, void *workspace_dev,
+                              long long workspace_bytes, void *stream);
+
+/*
+ * Dropout onto a residual stream:  y = residual + keep * x / q, with the mask drawn from a counter-based generator
+ * and never stored.  Element i = row * cols + column takes 16 bits of Philox4x32-10 (Salmon et al., SC 2011) with the
+ * two words of the seed, low first, as key and the counter (low and high word of i / 8, call, step): half i % 8 of the
+ * four output words, low half first.  keep where these bits are at least T = p * 65536 rounded to the nearest (halves
+ * up), q = 1 - T / 65536: p is taken to the nearest 2^-16, and the mean is kept exactly.  The mask depends on neither
+ * types nor strides.
+ *   rows, cols   from 0 (nothing to do), below 2^31 each; below 2^62 together
+ *   dtype, out_dtype   of x; of the residual and y.  Rows x_stride, residual_stride, y_stride (>= cols) apart.
+ *   residual     may be NULL: none.  y may be the residual, or x where the types are equal.
+ *   p            from 0 to 1; a dropped element is 0 whatever x holds there
+ *   call, step   which use of the generator this is (a layer and a training step, for instance)
+ *   step_dev     NULL, or a DEVICE number whose low 32 bits are added to step: a captured call that is
+ *                replayed draws another mask each time if the caller counts it up
+ */
+int cdgrab_dropout_forward(long long rows, long long cols, int dtype, const void *x_dev, long long x_stride,
+                           int out_dtype, const void *residual_dev, long long residual_stride, void *y_dev,
+                           long long y_stride, double p, unsigned long long seed, unsigned call, unsigned step,
+                           const long long *step_dev, void *stream);
+
+/* Its backward pass:  dx = keep * dy / q with the same mask (the residual's gradient is dy itself).
+ *   dtype, out_dtype   of dy; of dx, which may be dy where the types are equal */
+int cdgrab_dropout_backward(long long rows, long long cols, int dtype, const void *dy_dev, long long dy_stride,
+                            int out_dtype, void *dx_dev, long long dx_stride, double p, unsigned long long seed,
+                            unsigned call, unsigned step, const long long *step_dev, void *stream);
+
+/*
+ * Norms of queries and keys for each head, and the rotation by the token's position, in one pass: for the head_dim
+ * values x of a head
+ *   n = x * rstd,  rstd = 1 / sqrt(sum x^2 / head_dim + eps),  g = n * weight,
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = position * base^(-2 i / rotary_dim)
+ * over the pairs i of the first rotary_dim values of g: (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with
+ * interleaved = 1.  Angles are reduced in 64 bits: positions of millions keep their digits.
+ *
+ * Shape (HOST struct): strides in elements for batch, token and head; the head's values are contiguous.
+ *   batch, len, heads, kv_heads   >= 0 (nothing to do where batch or len is 0, or both head counts); heads up to
+ *                65535, batch * len and (heads + kv_heads) * head_dim below 2^31
+ *   head_dim     a multiple of 8 from 8 to 256;  rotary_dim a multiple of 8 from 0 (norms alone) to head_dim
+ *   dtype        of q, k, their gradients and the outputs
+ *   eps          >= 0;  base > 0, finite
+ *   strides      multiples of 8, and every base address a multiple of 16 bytes; token and head strides at least
+ *                head_dim where that axis is longer than 1
+ */
+typedef struct {
+  int batch, len, heads, kv_heads, head_dim, rotary_dim;
+  int interleaved;           /* 0 or 1 */
+  int dtype;
+  double base;
+  float eps;
+  int reserved;              /* 0 */
+  long long q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];  /* batch, token, head */
+  long long dq_stride[3], dk_stride[3];                                  /* backward pass only */
+} cdgrab_rotary_shape;
+
+/*
+ *   q_weight, k_weight   float [head_dim]; NULL: 1
+ *   positions    signed integers of position_bits (32 or 64) bits, [batch][len] with sequence b's at
+ *                b * position_stride (0: the same for all sequences); NULL: the token's index.  Up to 2^31 in size.
+ *   lens         int32 [batch], the tokens in use, or NULL: all.  What lies past a length is never used, and the
+ *                outputs there are zero.
+ *   q_out, k_out may be q and k themselves
+ */
+int cdgrab_rotary_forward(const cdgrab_rotary_shape *shape, const void *q_dev, const void *k_dev,
+                          const float *q_weight_dev, const float *k_weight_dev, const void *positions_dev,
+                          int position_bits, long long position_stride, const int32_t *lens_dev, void *q_out_dev,
+                          void *k_out_dev, void *stream);
+
+/*
+ * Its backward pass for the sequences of m workers, batch / m consecutive ones each, from the gradients dq, dk of the
+ * outputs and the inputs q, k:
+ *   g' = the gradient turned back,  h = g' * weight,  dx = rstd * (h - n * (sum h n) / head_dim)  into q_out, k_out,
+ *   dq_weight[i] = sum over worker i's tokens and heads of g' * n, dk_weight likewise
+ * so that a worker's gradient of the two weights lands in its row of the gather buffer.
+ *   q_out, k_out may be dq and dk, or q and k
+ *   dq_weight, dk_weight   of grad_dtype, worker i's head_dim values start at i * worker_stride (>= head_dim
+ *                where m > 1); either may be NULL (not computed)
+ *   workspace    16-byte aligned, cdgrab_rotary_workspace_bytes(shape, m) bytes (-1 for an invalid shape, or where the
+ *                batch is no multiple of m, 1 to 65535)
+ */
+long long cdgrab_rotary_workspace_bytes(const cdgrab_rotary_shape *shape, int m);
+int cdgrab_rotary_backward(const cdgrab_rotary_shape *shape, int m, const void *dq_dev, const void *dk_dev,
+                           const void *q_dev, const void *k_dev, const float *q_weight_dev, const float *k_weight_dev,
+                           const void *positions_dev, int position_bits, long long position_stride,
+                           const int32_t *lens_dev, void *q_out_dev, void *k_out_dev, int grad_dtype,
+                           void *dq_weight_dev, void *dk_weight_dev, long long worker_stride, void *workspace_dev,
+                           long long workspace_bytes, void *stream);
+
 /* What the training operators' kernels reported on the current device since the last call of this
- * function: CDGRAB_OK, or CDGRAB_ERR_TIMEOUT when a bounded device-side wait expired (the outputs of
- * the calls since then are not valid).  Synchronises the device and clears the word; not to be called
+ * function: CDGRAB_OK, CDGRAB_ERR_TIMEOUT when a bounded device-side wait expired (the outputs of
+ * the calls since then are not valid), or CDGRAB_ERR_INVALID when an embedding call met a token outside its
+ * vocabulary.  Synchronises the device and clears the word; not to be called
  * while a stream capture is open. */
 int cdgrab_operators_status(void);
 

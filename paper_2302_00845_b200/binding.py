@@ -32,6 +32,13 @@ class AttentionShape(C.Structure):
                [(n + "_stride", C.c_longlong * 3) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")]
 
 
+class RotaryShape(C.Structure):
+    """cdgrab_rotary_shape: sizes, and strides in elements for (batch, token, head)."""
+    _fields_ = [(n, C.c_int) for n in ("batch", "len", "heads", "kv_heads", "head_dim", "rotary_dim", "interleaved", "dtype")] + \
+               [("base", C.c_double), ("eps", C.c_float), ("reserved", C.c_int)] + \
+               [(n + "_stride", C.c_longlong * 3) for n in ("q", "k", "q_out", "k_out", "dq", "dk")]
+
+
 # name -> (restype, argtypes); the single list of what include/cdgrab.h declares
 SIGNATURES = {
     "cdgrab_create": (C.c_int, [C.c_int, C.c_int, C.c_longlong, C.c_int, C.POINTER(C.c_void_p)]),
@@ -91,6 +98,24 @@ SIGNATURES = {
     "cdgrab_orthogonalise": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_longlong, C.c_longlong,
                                        C.c_int, C.POINTER(C.c_float), C.c_float, C.c_void_p, C.c_longlong,
                                        C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p]),
+    "cdgrab_embedding_forward": (C.c_int, [C.c_longlong, C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_longlong,
+                                           C.c_longlong, C.c_float, C.c_int, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p,
+                                           C.c_longlong, C.c_void_p]),
+    "cdgrab_embedding_workspace_bytes": (C.c_longlong, [C.c_int, C.c_longlong, C.c_int, C.c_int]),
+    "cdgrab_embedding_backward": (C.c_int, [C.c_int, C.c_longlong, C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_void_p,
+                                            C.c_longlong, C.c_longlong, C.c_float, C.c_int, C.c_void_p, C.c_longlong, C.c_int,
+                                            C.c_void_p, C.c_longlong, C.c_longlong, C.c_int, C.c_void_p, C.c_longlong,
+                                            C.c_void_p]),
+    "cdgrab_dropout_forward": (C.c_int, [C.c_longlong, C.c_longlong, C.c_int, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p,
+                                         C.c_longlong, C.c_void_p, C.c_longlong, C.c_double, C.c_ulonglong, C.c_uint, C.c_uint,
+                                         C.c_void_p, C.c_void_p]),
+    "cdgrab_dropout_backward": (C.c_int, [C.c_longlong, C.c_longlong, C.c_int, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p,
+                                          C.c_longlong, C.c_double, C.c_ulonglong, C.c_uint, C.c_uint, C.c_void_p, C.c_void_p]),
+    "cdgrab_rotary_forward": (C.c_int, [C.POINTER(RotaryShape)] + [C.c_void_p] * 5 + [C.c_int, C.c_longlong] + [C.c_void_p] * 4),
+    "cdgrab_rotary_workspace_bytes": (C.c_longlong, [C.POINTER(RotaryShape), C.c_int]),
+    "cdgrab_rotary_backward": (C.c_int, [C.POINTER(RotaryShape), C.c_int] + [C.c_void_p] * 7 + [C.c_int, C.c_longlong] +
+                               [C.c_void_p] * 3 + [C.c_int, C.c_void_p, C.c_void_p, C.c_longlong, C.c_void_p, C.c_longlong,
+                                                   C.c_void_p]),
     "cdgrab_operators_status": (C.c_int, []),
     "cdgrab_operators_wait_limit": (C.c_int, [C.c_longlong]),
 }
@@ -616,6 +641,253 @@ def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: floa
     if rc:
         _check(rc, "cdgrab_orthogonalise")
     return o
+
+
+_NO_PADDING = -2 ** 63
+
+
+def _tokens(t):
+    """(groups, length, row stride, bits) of tokens [length] or [groups][length]."""
+    if t.dtype is torch.int64:
+        bits = 64
+    elif t.dtype is torch.int32:
+        bits = 32
+    else:
+        raise ValueError(f"tokens: int32 or int64, not {t.dtype}")
+    if t.dim() == 1:
+        (length,), (inner,), groups, step = t.shape, t.stride(), 1, 0
+    elif t.dim() == 2:
+        (groups, length), (step, inner) = t.shape, t.stride()
+    else:
+        raise ValueError(f"tokens: [length] or [groups][length], not {tuple(t.shape)}")
+    if inner != 1 and length > 1:
+        raise ValueError("tokens: those of a row have to be contiguous")
+    return groups, length, step if groups > 1 else max(step, length), bits
+
+
+def embedding_forward(tokens, table, scale: float = 1.0, padding: int | None = None, out=None, dtype=None, stream=None):
+    """scale * table[token] for tokens [length] or [groups][length] (int32 or int64; rows may be strided): a row
+    [cols] for each, [tokens][cols] in all, of `dtype` (the table's by default).  table [vocab][cols], float32 or
+    bfloat16.  Tokens equal to `padding` give zeros; others outside the vocabulary as well, and operators_status
+    reports them."""
+    handle, other = _place(stream, tokens, table, out)
+    groups, length, ts, bits = _tokens(tokens)
+    if table.dim() != 2:
+        raise ValueError(f"table: [vocab][cols], not {tuple(table.shape)}")
+    vocab, cols = table.shape
+    rows = groups * length
+    if vocab > _INT_MAX or cols > _INT_MAX:
+        raise ValueError(f"table: {tuple(table.shape)}")
+    code = _code(table, "table")
+    if out is None:
+        y = _empty(table, (rows, cols), table.dtype if dtype is None else dtype, other)
+        ys, ycode = cols, code if dtype is None else _code(y, "dtype")
+    else:
+        y, ys, ycode = out, _row_stride(out, "out", rows, cols), _code(out, "out")
+        if dtype is not None and dtype != out.dtype:
+            raise ValueError("out: of another type than dtype")
+    rc = lib().cdgrab_embedding_forward(
+        groups, length, cols, vocab, bits, tokens.data_ptr(), ts, _NO_PADDING if padding is None else padding, scale, code,
+        table.data_ptr(), _row_stride(table, "table", vocab, cols), ycode, y.data_ptr(), ys, handle)
+    if rc:
+        _check(rc, "cdgrab_embedding_forward")
+    return y
+
+
+def embedding_backward(dy, tokens, dtable, scale: float = 1.0, padding: int | None = None, accumulate: bool = False, stream=None):
+    """Gradient of embedding_forward's table: dy [tokens][cols]; tokens [length], or [groups][length] with an equal
+    number of groups for each worker.  dtable [m][vocab][cols] (or [vocab][cols] for one worker; float32 or
+    bfloat16, views into the gather buffer as a rule) receives each worker's own sums, zeros where no token of
+    its names a row; with accumulate they are added to what is there.  Returns dtable."""
+    handle, other = _place(stream, dy, tokens, dtable)
+    groups, length, ts, bits = _tokens(tokens)
+    if dtable.dim() == 2:
+        (vocab, cols), m, (rs, inner), ws = dtable.shape, 1, dtable.stride(), 0
+    elif dtable.dim() == 3:
+        (m, vocab, cols), (ws, rs, inner) = dtable.shape, dtable.stride()
+    else:
+        raise ValueError(f"dtable: [m][vocab][cols] or [vocab][cols], not {tuple(dtable.shape)}")
+    if inner != 1 and cols > 1:
+        raise ValueError("dtable: the values of a row have to be contiguous")
+    if max(vocab, cols, m) > _INT_MAX:
+        raise ValueError(f"dtable: {tuple(dtable.shape)}")
+    if m < 1 or groups % m:
+        raise ValueError(f"{groups} rows of tokens are not {m} workers' equal shares")
+    code, gcode = _code(dy, "dy"), _code(dtable, "dtable")
+    dys = _row_stride(dy, "dy", groups * length, cols)
+    L = lib()
+    nbytes = L.cdgrab_embedding_workspace_bytes(m, groups // m * length, cols, vocab)
+    scratch = _scratch(dtable, nbytes, other)
+    rc = L.cdgrab_embedding_backward(
+        m, groups // m, length, cols, vocab, bits, tokens.data_ptr(), ts, _NO_PADDING if padding is None else padding, scale,
+        code, dy.data_ptr(), dys, gcode, dtable.data_ptr(), ws, rs, 1 if accumulate else 0, scratch.data_ptr(), max(16, nbytes), handle)
+    if rc:
+        _check(rc, "cdgrab_embedding_backward")
+    return dtable
+
+
+def _dropout(x, residual, out, dtype, name, p, seed, call, step, stream):
+    steps = None if isinstance(step, int) else step
+    handle, other = _place(stream, x, residual, out, steps)
+    if x.dim() != 2:
+        raise ValueError(f"[rows][cols], not {tuple(x.shape)}")
+    rows, cols = x.shape
+    code = _code(x, "x")
+    if steps is not None:
+        if steps.dtype != torch.int64 or steps.numel() != 1:
+            raise ValueError("step: a number, or one int64 on the device")
+        step = 0
+    if not (0 <= seed < 2 ** 64 and 0 <= call < 2 ** 32 and 0 <= step < 2 ** 32):
+        raise ValueError(f"seed {seed}, call {call}, step {step}: 64, 32 and 32 bits without a sign")
+    if out is None:
+        if dtype is None:
+            dtype = x.dtype if residual is None else residual.dtype
+        y = _empty(x, (rows, cols), dtype, other)
+        ys, ycode = cols, code if dtype is x.dtype else _code(y, "dtype")
+    else:
+        y, ys, ycode = out, _row_stride(out, "out", rows, cols), _code(out, "out")
+        if dtype is not None and dtype != out.dtype:
+            raise ValueError("out: of another type than dtype")
+    res, rs = None, 0
+    if residual is not None:
+        if residual.dtype != y.dtype:
+            raise ValueError("residual: the type of the result")
+        res, rs = residual.data_ptr(), _row_stride(residual, "residual", rows, cols)
+    at = None if steps is None else steps.data_ptr()
+    if name == "cdgrab_dropout_forward":
+        rc = lib().cdgrab_dropout_forward(rows, cols, code, x.data_ptr(), _row_stride(x, "x", rows, cols), ycode, res, rs,
+                                          y.data_ptr(), ys, p, seed, call, step, at, handle)
+    else:
+        rc = lib().cdgrab_dropout_backward(rows, cols, code, x.data_ptr(), _row_stride(x, "dy", rows, cols), ycode, y.data_ptr(),
+                                           ys, p, seed, call, step, at, handle)
+    if rc:
+        _check(rc, name)
+    return y
+
+
+def dropout_forward(x, p: float, seed: int, call: int = 0, step=0, residual=None, out=None, dtype=None, stream=None):
+    """residual + x * keep / (1 - p) of x [rows][cols] (float32 or bfloat16; rows may be strided), keep drawn from
+    (seed, call, step) and the element's index, p taken to the nearest 2^-16.  step: a number, or an int64 CUDA
+    tensor [1] that a captured graph reads when it runs.  The result has the residual's type, x's without one, or
+    `dtype`, which the residual then has to have."""
+    return _dropout(x, residual, out, dtype, "cdgrab_dropout_forward", p, seed, call, step, stream)
+
+
+def dropout_backward(dy, p: float, seed: int, call: int = 0, step=0, out=None, dtype=None, stream=None):
+    """Gradient of dropout_forward's x: dy * keep / (1 - p) with the mask of the same (seed, call, step), of `dtype`
+    (dy's by default).  The residual's gradient is dy itself."""
+    return _dropout(dy, None, out, dtype, "cdgrab_dropout_backward", p, seed, call, step, stream)
+
+
+_ROTARY = struct.Struct("8idfi18q")          # cdgrab_rotary_shape
+
+
+def _heads(t, name: str, shape, dtype):
+    """(batch, token, head) strides of a [batch][token][head][head_dim] tensor; nothing is asked of an empty one."""
+    if t is None:
+        return _NONE
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)}, not {tuple(t.shape)} {t.dtype}")
+    a, b, c, inner = t.stride()
+    if inner != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: the values of a head have to be contiguous")
+    if (a | b | c) & 7:         # an axis of length one has no stride of its own
+        a, b, c = ((v + 7) & ~7 if n <= 1 else v for v, n in zip((a, b, c), shape))
+    return a, b, c
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens):
+    """The sizes of cdgrab_rotary_shape, and the arguments for positions and lengths."""
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q, k: [batch][token][head][head_dim]")
+    b, t, h, d = q.shape
+    hk = 0
+    if k is not None:
+        kb, kt, hk, kd = k.shape
+        if kb != b or kt != t or kd != d or k.dtype != q.dtype:
+            raise ValueError("q and k do not go together")
+    if max(b, t, h, hk, d) > _INT_MAX:
+        raise ValueError(f"q: {tuple(q.shape)}")
+    sizes = (b, t, h, hk, d, d if rotary_dim is None else rotary_dim, 1 if interleaved else 0, _code(q, "q"), base, eps, 0)
+    pos, bits, step = None, 0, 0
+    if positions is not None:
+        bits = 64 if positions.dtype is torch.int64 else 32
+        if positions.dtype not in (torch.int64, torch.int32) or positions.shape not in ((t,), (b, t)):
+            raise ValueError("positions: int32 or int64, [token] or [batch][token]")
+        if t > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions: those of a sequence have to be contiguous")
+        pos, step = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 and b > 1 else 0
+    return sizes, pos, bits, step, _lens(lens, "lens", b)
+
+
+def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: float = 10000.0, rotary_dim: int | None = None,
+                   interleaved: bool = False, eps: float = 1e-6, lens=None, q_out=None, k_out=None, stream=None):
+    """Every head of q [b][t][h][d] and k [b][t][h_kv][d] (float32 or bfloat16; any strides that are multiples of 8;
+    k may be None) divided by its root mean square, times its float32 weight [d], its first rotary_dim values (all by
+    default) rotated by the token's position: pairs (i, i + rotary_dim / 2), or neighbours with interleaved.
+    positions: int32 or int64 [t] or [b][t], the token's index by default.  lens: int32 [b], the tokens in use; the
+    others become zero.  Returns (q_out, k_out), which may be q and k."""
+    handle, other = _place(stream, q, k, q_weight, k_weight, positions, lens, q_out, k_out)
+    sizes, pos, bits, step, ln = _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens)
+    d, dt = sizes[4], q.dtype
+    if q_out is None:
+        q_out = _empty_like(q, other)
+    if k is not None and k_out is None:
+        k_out = _empty_like(k, other)
+    ks = None if k is None else k.shape
+    sh = RotaryShape.from_buffer_copy(_ROTARY.pack(*sizes, *_heads(q, "q", q.shape, dt), *_heads(k, "k", ks, dt),
+                                                   *_heads(q_out, "q_out", q.shape, dt), *_heads(k_out, "k_out", ks, dt), *_NONE, *_NONE))
+    rc = lib().cdgrab_rotary_forward(sh, q.data_ptr(), _at(k), _vector(q_weight, "q_weight", d), _vector(k_weight, "k_weight", d),
+                                     pos, bits, step, ln, q_out.data_ptr(), _at(k_out), handle)
+    if rc:
+        _check(rc, "cdgrab_rotary_forward")
+    return q_out, k_out
+
+
+def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, base: float = 10000.0,
+                    rotary_dim: int | None = None, interleaved: bool = False, eps: float = 1e-6, lens=None, dq_weight=None,
+                    dk_weight=None, q_out=None, k_out=None, stream=None):
+    """Backward pass of rotary_forward from the gradients dq, dk of its outputs and its inputs q, k, for m workers'
+    sequences: dq_weight and dk_weight [m][d] (float32 or bfloat16, equal row strides, views into the gather buffer
+    as a rule) receive each worker's own sums, either may be None.  Returns the gradients of q and k, in q_out and
+    k_out where given (dq and dk themselves, or views of one buffer)."""
+    handle, other = _place(stream, dq, dk, q, k, q_weight, k_weight, positions, lens, dq_weight, dk_weight, q_out, k_out)
+    sizes, pos, bits, step, ln = _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens)
+    d, dt = sizes[4], q.dtype
+    g = dq_weight if dq_weight is not None else dk_weight
+    m, gcode, ws = 1, F32, d
+    if g is not None:
+        m = g.shape[0]
+        if m < 1 or sizes[0] % m:
+            raise ValueError(f"{sizes[0]} sequences are not {m} workers' equal shares")
+        gcode, ws = _code(g, "dq_weight, dk_weight"), _row_stride(g, "dq_weight, dk_weight", m, d)
+        # (with one worker the row stride is not used)
+        if dk_weight is not None and dk_weight is not g and (
+                dk_weight.dtype != g.dtype or (_row_stride(dk_weight, "dk_weight", m, d) != ws and m > 1)):
+            raise ValueError("dq_weight and dk_weight: one type and one row stride")
+    if (k is None) != (dk is None):
+        raise ValueError("k and dk: both or neither")
+    if q_out is None:
+        q_out = _empty_like(q, other)
+    if k is not None and k_out is None:
+        k_out = _empty_like(k, other)
+    qs, ks = q.shape, None if k is None else k.shape
+    sh = RotaryShape.from_buffer_copy(_ROTARY.pack(
+        *sizes, *_heads(q, "q", qs, dt), *_heads(k, "k", ks, dt), *_heads(q_out, "q_out", qs, dt), *_heads(k_out, "k_out", ks, dt),
+        *_heads(dq, "dq", qs, dt), *_heads(dk, "dk", ks, dt)))
+    L = lib()
+    nbytes = L.cdgrab_rotary_workspace_bytes(sh, m)
+    scratch = _scratch(q, nbytes, other)
+    rc = L.cdgrab_rotary_backward(sh, m, dq.data_ptr(), _at(dk), q.data_ptr(), _at(k), _vector(q_weight, "q_weight", d),
+                                  _vector(k_weight, "k_weight", d), pos, bits, step, ln, q_out.data_ptr(), _at(k_out), gcode,
+                                  _at(dq_weight), _at(dk_weight), ws, scratch.data_ptr(), max(16, nbytes), handle)
+    if rc:
+        _check(rc, "cdgrab_rotary_backward")
+    return q_out, k_out
 
 
 def operators_status() -> int:

@@ -14,6 +14,7 @@
 #define CDG_ST_NONFINITE 1
 #define CDG_ST_TIMEOUT 2
 #define CDG_ST_BOUNDS 4       // debug build: an index check failed (the write was skipped)
+#define CDG_ST_INDEX 8        // a caller's index outside its range (its row was skipped)
 
 // Debug build (-DCDGRAB_DEBUG, python -m paper_2302_00845_b200.build --debug): index checks in
 // front of the writes of the decision routines, and every handle-owned allocation wrapped in two

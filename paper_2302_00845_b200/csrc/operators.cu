@@ -51,5 +51,5 @@ extern "C" int cdgrab_operators_status(void) {
   int st = 0;
   if (cudaMemcpy(&st, d->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
   if (st != 0 && cudaMemset(d->status, 0, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
-  return st & CDG_ST_TIMEOUT ? CDGRAB_ERR_TIMEOUT : CDGRAB_OK;
+  return st & CDG_ST_TIMEOUT ? CDGRAB_ERR_TIMEOUT : st & CDG_ST_INDEX ? CDGRAB_ERR_INVALID : CDGRAB_OK;
 }

@@ -6,6 +6,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "philox.cuh"
 
 // Which balance rule decides the signs.  Greedy (Algorithm 6): +1 iff <r,c> < 0.
 // Randomized (Algorithm 2's subroutine with the bound w of Algorithm 5): p = 1/2 - <r,c>/(2w),
@@ -20,23 +21,10 @@ struct CdgRule {
   unsigned epoch, k;
 };
 
-// Philox4x32-10 (Salmon et al., SC 2011): ten rounds of
-//   (c0, c1, c2, c3) <- (hi(M1 c2) ^ c1 ^ k0, lo(M1 c2), hi(M0 c0) ^ c3 ^ k1, lo(M0 c0)),
-// the key advancing by the Weyl constants after each round.  Returns the first output word.
-__host__ __device__ inline uint32_t cdg_philox4x32_10_first(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3,
-                                                            uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int round = 0; round < 10; ++round) {
-    const unsigned long long p0 = 0xD2511F53ull * c0, p1 = 0xCD9E8D57ull * c2;
-    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0, n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-    c1 = (uint32_t)p1; c3 = (uint32_t)p0; c0 = n0; c2 = n2;
-    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-  }
-  return c0;
-}
 // the draw of worker i at pair index k of an epoch: top 24 bits of the word, times 2^-24
 __host__ __device__ inline float cdg_seeded_uniform(unsigned long long seed, unsigned epoch, unsigned k, unsigned i) {
-  const uint32_t x = cdg_philox4x32_10_first(i, k, epoch, 0u, (uint32_t)seed, (uint32_t)(seed >> 32));
+  uint32_t x = i, c1 = k, c2 = epoch, c3 = 0u;
+  cdg_philox4x32_10(x, c1, c2, c3, (uint32_t)seed, (uint32_t)(seed >> 32));
   return (float)(x >> 8) * (1.0f / 16777216.0f);
 }
 
