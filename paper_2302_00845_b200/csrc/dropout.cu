@@ -10,83 +10,107 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBlocks = 2;         // blocks of eight elements to a thread
 
 struct Draw {
-  uint32_t seed_lo, seed_hi, call, step;
+  uint32_t key[10][2];         // of each round
+  uint32_t call, step;
   const long long *step_dev;
-  uint32_t limit;      // T 2^16
-  float factor;        // 1 / q
+  uint32_t limit;              // T 2^16
+  float factor;                // 1 / q
 };
 
-// A thread takes blocks of eight elements, kBlocks of them at a time: their values are requested, then the generator runs
-// while they are on their way.  Sixteen bits an element rather than a word: ten rounds cost 60 to 70 instructions, and at two
-// words of memory traffic an element, bf16 in and out, an SM has 22 issue slots for each.
+// the four words of block b
+__device__ __forceinline__ void draw_block(const Draw &d, uint32_t step, long long b, uint32_t (&c)[4]) {
+  c[0] = (uint32_t)b;
+  c[1] = (uint32_t)(b >> 32);
+  c[2] = d.call;
+  c[3] = step;
+#pragma unroll
+  for (int i = 0; i < 10; ++i) cdg_philox_round(c[0], c[1], c[2], c[3], d.key[i][0], d.key[i][1]);
+}
 // A half-word is compared where it stands at the top of a word: what lies below it cannot change the result against T 2^16.
-// With T = 65536 there is no such number; x is not read at all then.
-// WIDE: the eight values of a block are one access, 16 or 32 bytes; else one by one, in rows of any stride.
-template <typename T, typename R, bool WIDE>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(long long n, long long cols, const T *x, long long xs, const R *res,
-                                                           long long rs, R *y, long long ys, Draw d) {
-  constexpr int kBlocks = 2;
+__device__ __forceinline__ bool kept(const Draw &d, uint32_t word, int e) { return (e % 2 ? word : word << 16) >= d.limit; }
+
+// A thread takes kBlocks blocks of eight elements, each one access of 16 or 32 bytes: their values are requested, then the generator
+// runs while they are on their way.  Sixteen bits an element rather than a word: the ten rounds are 40 instructions, and at two
+// bytes in and two out an element an SM has 22 issue slots for each.
+// Blocks are numbered through rows of per_row blocks; FLAT: one row of n values, the last block perhaps cut short.
+// x = NULL: all is dropped.
+// (65,536 x 768 bf16: 36.6 us, 5.5 TB/s; one block to a thread 38.3, four 36.7.  Held to 48 registers, four spill.)
+template <typename T, typename R, bool RES, bool FLAT>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(long long n, long long blocks, CdgDivisor per_row, const T *x, long long xs,
+                                                           const R *res, long long rs, R *y, long long ys,
+                                                           const __grid_constant__ Draw d) {
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const uint32_t step = d.step + (d.step_dev ? (uint32_t)*d.step_dev : 0u);
-  const long long blocks = (n + 7) / 8;
-  for (long long b0 = (long long)blockIdx.x * kThreads * kBlocks + threadIdx.x; b0 < blocks; b0 += (long long)gridDim.x * kThreads * kBlocks) {
-    CdgVec<T, 8> vx[kBlocks];
-    CdgVec<R, 8> vr[kBlocks];
-    long long row[kBlocks], col[kBlocks];
+  const long long base = (long long)blockIdx.x * (kThreads * kBlocks);
+  const long long first = FLAT ? 0 : base / per_row.d;
+  const uint32_t off = FLAT ? threadIdx.x : (uint32_t)(base - first * per_row.d) + threadIdx.x;
+  CdgVec<T, 8> vx[kBlocks];
+  CdgVec<R, 8> vr[kBlocks];
+  auto place = [&](int u, long long stride) {
+    if (FLAT) return (base + threadIdx.x + u * kThreads) * 8;
+    const uint32_t i = off + u * kThreads, q = cdg_divide(i, per_row);
+    return (first + q) * stride + (i - q * per_row.d) * 8ll;
+  };
 #pragma unroll
-    for (int u = 0; u < kBlocks; ++u) {
-      const long long at = (b0 + u * kThreads) * 8;
-      row[u] = 0;
-      col[u] = at;
-      if (cols < n) {        // (what is contiguous throughout comes as one row)
-        row[u] = n <= 0xffffffffll ? (uint32_t)at / (uint32_t)cols : at / cols;
-        col[u] = at - row[u] * cols;
-      }
-      if (WIDE && at + 8 <= n) {
-        if (x) vx[u].load(x + row[u] * xs + col[u]);
-        else vx[u].zero();
-        if (res) vr[u].load(res + row[u] * rs + col[u]);
-        else vr[u].zero();
-      }
+  for (int u = 0; u < kBlocks; ++u) {
+    const long long b = base + threadIdx.x + u * kThreads;
+    vx[u].zero();
+    if (FLAT ? b * 8 + 8 <= n : b < blocks) {
+      if (x) vx[u].load(x + place(u, xs));
+      if (RES) vr[u].load(res + place(u, rs));
     }
+  }
 #pragma unroll
-    for (int u = 0; u < kBlocks; ++u) {
-      const long long b = b0 + u * kThreads;
-      if (b >= blocks) break;
-      uint32_t c[4] = {(uint32_t)b, (uint32_t)(b >> 32), d.call, step};
-      cdg_philox4x32_10(c[0], c[1], c[2], c[3], d.seed_lo, d.seed_hi);
-      if (WIDE && b * 8 + 8 <= n) {
-        float f[8];
+  for (int u = 0; u < kBlocks; ++u) {
+    const long long b = base + threadIdx.x + u * kThreads;
+    if (b >= blocks) break;
+    uint32_t c[4];
+    draw_block(d, step, b, c);
+    if (!FLAT || b * 8 + 8 <= n) {
+      float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool keep = (e % 2 ? c[e / 2] : c[e / 2] << 16) >= d.limit;
-          f[e] = fmaf(keep ? vx[u].get(e) : 0.0f, d.factor, vr[u].get(e));
-        }
-        vr[u].set(f);
-        vr[u].store(y + row[u] * ys + col[u]);
-        continue;
+      for (int e = 0; e < 8; ++e) {
+        const float v = kept(d, c[e / 2], e) ? vx[u].get(e) : 0.0f;
+        f[e] = RES ? fmaf(v, d.factor, vr[u].get(e)) : v * d.factor;
       }
-      long long r = row[u], k = col[u];
-      for (int e = 0; e < 8 && b * 8 + e < n; ++e) {
-        const uint32_t word = e < 2 ? c[0] : e < 4 ? c[1] : e < 6 ? c[2] : c[3];
-        const bool keep = (e % 2 ? word : word << 16) >= d.limit;
-        const float v = keep && x ? cdg_ld(x + r * xs + k) : 0.0f;
-        y[r * ys + k] = cdg_cast<R>(fmaf(v, d.factor, res ? cdg_ld(res + r * rs + k) : 0.0f));
-        if (++k == cols) { k = 0; ++r; }
+      CdgVec<R, 8> o;
+      o.set(f);
+      o.store(y + place(u, ys));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const long long i = b * 8 + e;
+        if (i >= n) break;
+        const float v = x && kept(d, c[e / 2], e) ? cdg_ld(x + i) : 0.0f;
+        y[i] = cdg_cast<R>(RES ? fmaf(v, d.factor, cdg_ld(res + i)) : v * d.factor);
       }
     }
   }
 }
 
-template <typename T, typename R, bool WIDE>
-cudaError_t launch(long long n, long long cols, const void *x, long long xs, const void *res, long long rs, void *y, long long ys,
-                   const Draw &d, cudaStream_t st) {
-  const long long blocks = ((n + 7) / 8 + 2 * kThreads - 1) / (2 * kThreads);
-  return cdg_ops_launch(dropout_kernel<T, R, WIDE>, dim3((unsigned)(blocks < (1ll << 30) ? blocks : 1ll << 30)), kThreads, 0, st, n, cols,
-                        (const T *)x, xs, (const R *)res, rs, (R *)y, ys, d);
+// rows that no wide access fits: a thread to a block, value by value
+template <typename T, typename R>
+__global__ void __launch_bounds__(kThreads) dropout_narrow_kernel(long long n, long long cols, const T *x, long long xs, const R *res,
+                                                                  long long rs, R *y, long long ys, const __grid_constant__ Draw d) {
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const uint32_t step = d.step + (d.step_dev ? (uint32_t)*d.step_dev : 0u);
+  const long long b = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (b * 8 >= n) return;
+  uint32_t c[4];
+  draw_block(d, step, b, c);
+  long long r = b * 8 / cols, k = b * 8 - r * cols;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (b * 8 + e >= n) break;
+    const float v = x && kept(d, c[e / 2], e) ? cdg_ld(x + r * xs + k) : 0.0f;
+    y[r * ys + k] = cdg_cast<R>(fmaf(v, d.factor, res ? cdg_ld(res + r * rs + k) : 0.0f));
+    if (++k == cols) { k = 0; ++r; }
+  }
 }
 
 int dropout(long long rows, long long cols, int dtype, const void *x, long long xs, int out_dtype, const void *res, long long rs,
@@ -104,19 +128,36 @@ int dropout(long long rows, long long cols, int dtype, const void *x, long long 
   if (const int rc = cdg_ops_device(&dev)) return rc;
   const uint32_t limit = (uint32_t)std::floor(p * 65536.0 + 0.5);
   const bool none = limit == 65536;
-  const Draw d = {(uint32_t)seed, (uint32_t)(seed >> 32), call, step, step_dev, none ? 0u : limit << 16,
-                  none ? 0.0f : (float)(65536.0 / (65536.0 - limit))};
-  const long long n = rows * cols;
-  if (xs == cols && ys == cols && (!res || rs == cols)) cols = n;          // one row
-  // (the last elements of a single row go one by one)
-  const bool wide = cdg_widest(cols == n ? 8 : cols, {{x, cols == n ? 0 : xs, e}, {res, cols == n ? 0 : rs, oe}, {y, cols == n ? 0 : ys, oe}}) == 8;
+  Draw d = {};
+  for (int i = 0; i < 10; ++i) {
+    d.key[i][0] = (uint32_t)seed + i * kPhiloxWeyl0;
+    d.key[i][1] = (uint32_t)(seed >> 32) + i * kPhiloxWeyl1;
+  }
+  d.call = call;
+  d.step = step;
+  d.step_dev = step_dev;
+  d.limit = none ? 0u : limit << 16;
+  d.factor = none ? 0.0f : (float)(65536.0 / (65536.0 - limit));
+  const long long n = rows * cols, blocks = (n + 7) / 8;
+  const bool flat = rows == 1 || (xs == cols && ys == cols && (!res || rs == cols));
+  const bool wide = flat ? cdg_widest(8, {{x, 0, e}, {res, 0, oe}, {y, 0, oe}}) == 8
+                         : cdg_widest(cols, {{x, xs, e}, {res, rs, oe}, {y, ys, oe}}) == 8;
+  const long long grid = wide ? (blocks + kBlocks * kThreads - 1) / (kBlocks * kThreads) : (blocks + kThreads - 1) / kThreads;
+  if (grid >= (1ll << 31)) return CDGRAB_ERR_INVALID;
   if (none) x = nullptr;
   cudaStream_t st = (cudaStream_t)stream;
   return cdg_by_types(dtype, out_dtype, [&](auto t, auto r) {
     using T = decltype(t);
     using R = decltype(r);
-    return cdg_launch_rc(wide ? launch<T, R, true>(n, cols, x, xs, res, rs, y, ys, d, st)
-                              : launch<T, R, false>(n, cols, x, xs, res, rs, y, ys, d, st));
+    if (!wide)
+      return cdg_launch_rc(cdg_ops_launch(dropout_narrow_kernel<T, R>, dim3((unsigned)grid), kThreads, 0, st, n, cols, (const T *)x, xs,
+                                          (const R *)res, rs, (R *)y, ys, d));
+    auto go = [&](auto *kernel) {
+      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)grid), kThreads, 0, st, n, blocks, cdg_divisor(flat ? 1u : (uint32_t)(cols / 8)),
+                                          (const T *)x, xs, (const R *)res, rs, (R *)y, ys, d));
+    };
+    if (res) return flat ? go(dropout_kernel<T, R, true, true>) : go(dropout_kernel<T, R, true, false>);
+    return flat ? go(dropout_kernel<T, R, false, true>) : go(dropout_kernel<T, R, false, false>);
   });
 }
 

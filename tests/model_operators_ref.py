@@ -114,6 +114,7 @@ def rotary(x, w, pos, base, rotary_dim, interleaved, eps, lens, dy=None, m=1, gr
     angle = pos[:, :, None] * freq
     far = angle.abs() * 2.0 ** -50            # products of 53 bits on both sides
     rstd = 1.0 / torch.sqrt(x.square().mean(-1, keepdim=True) + float(np.float32(eps)))
+    rstd = torch.where(live, rstd, 0.0)       # (with eps = 0 what is padded has none)
     rel = (d / 2 + 6) * U32                   # a sum of d squares, halved by the root; the root, the division
     n = x * rstd
     if dy is None:

@@ -49,6 +49,12 @@ def test_columns(cols, dtype):
     check(*draw(2, 37, 19, cols, dtype), 2, "f32")
 
 
+@pytest.mark.parametrize("vocab", [2 ** 24 - 1, 2 ** 24, 2 ** 26])
+def test_large_vocabularies(vocab):
+    """Three and four digits of a sort."""
+    check(*draw(1, 5000, vocab, 1, skew=1.0), 1)
+
+
 # vocabularies around the digits of a sort and single rows; lengths from one token to more than a block takes at once
 @pytest.mark.parametrize("vocab", [1, 2, 31, 255, 256, 257, 511, 4095, 65535, 65536, 70001])
 @pytest.mark.parametrize("bits", [torch.int32, torch.int64])

@@ -125,6 +125,12 @@ def test_lengths_outside_the_range():
     assert torch.equal(y[0][0], full[0][0]) and (y[0][1] == 0).all() and (y[1][1] == 0).all()
 
 
+def test_no_epsilon():
+    """Padded tokens have no size, and with eps = 0 no norm: they are left out all the same."""
+    x = draw(2, 30, 3, 2, 40, "f32")
+    check(*x, m=2, eps=0.0, lens=torch.tensor([30, 4], dtype=torch.int32, device="cuda"))
+
+
 def test_slices_of_one_projection_and_of_its_gradient():
     q, k, qw, kw, dq, dk = x = draw(3, 50, 6, 2, 64, packed=True)
     assert not q.is_contiguous()
