@@ -6,6 +6,7 @@
 // The angle of a far position is many turns: position x (frequency / 2 pi) is taken in 64 bits and only its fraction
 // goes on in 32.
 #include <cmath>
+#include <type_traits>
 
 #include "rows.cuh"
 
@@ -14,10 +15,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxDim = 256, kMaxPairs = kMaxDim / 2;
-constexpr int kMaxTokens = 64;             // of a tile
-constexpr int kMaxSlots = 2048;            // pairs of a tile
 
-// turns per position of each pair: base^(-2 i / rotary_dim) / (2 pi), 0 for the pairs that stay
+// turns per position of each pair: base^(-2 i / rotary_dim) / (2 pi)
 struct Frequencies { double turns[kMaxPairs]; };
 
 struct Side {                              // queries or keys
@@ -33,111 +32,105 @@ struct Args {
   int pos_bits;
   long long pos_stride;
   const int *lens;
-  CdgDivisor len, lanes;                   // tokens to a sequence; lanes to a head, V pairs each
-  CdgDivisor heads[3];                     // of queries, keys, both
-  int dim, rot, interleaved, group, tile;  // group: lanes to a head, the next power of two; tile: tokens
+  CdgDivisor len, parts[2];                // tokens to a sequence; shares that a token's heads are dealt out in (forward: [0])
+  int dim, rot, lanes, group;              // lanes: those that hold a head, V pairs each; group: the next power of two
   float eps;
 };
 
-// A lane holds the values A = x[a .. a + V) and B = x[b .. b + V) of a head, one access each: V pairs, either (A_i, B_i), or with
-// neighbours in pairs (A_2i, A_2i+1) and (B_2i, B_2i+1).  Both halves of the rotated part, then both of the rest.
+// A group of lanes takes a token, or a share of its heads, head by head; the angles stay in registers meanwhile.
+// A lane holds the values A = x[a .. a + V) and B = x[b .. b + V) of a head, one access each: V pairs, either (A_i, B_i), or
+// (NEAR) neighbours, (A_2i, A_2i+1) and (B_2i, B_2i+1).  A and B lie in the halves of the rotated part, or of the rest.
 template <int V>
 __device__ __forceinline__ int2 places(const Args &a, int lane) {
   const int i = lane * V, half = a.rot / 2;
   if (i < half) return make_int2(i, half + i);
   return make_int2(a.rot + i - half, a.rot + (a.dim - a.rot) / 2 + i - half);
 }
-// which pair of the head the lane's j-th is, -1 for one that stays
-template <int V>
-__device__ __forceinline__ int pair_of(const Args &a, int lane, int j) {
-  const int i = lane * V, half = a.rot / 2;
-  if (i >= half) return -1;
-  if (!a.interleaved) return i + j;
-  return j < V / 2 ? i / 2 + j : (half + i) / 2 + j - V / 2;
-}
 
-// What a tile of tokens shares, in shared memory.  Pieces of 16 bytes are kept lane after lane, so that a warp's reads meet no
-// bank twice.
-struct Tile {
-  float2 turn[kMaxSlots];                  // cos and sin: [token][V / 2 pieces][lane][2 pairs]
-  float weight[2][2][kMaxPairs];           // of queries and keys, A and B: [V / 4 pieces][lane][4]
-  long long at[kMaxTokens][2];             // batch and token
-  int live[kMaxTokens];
+struct Shared {
+  double turns[kMaxPairs];                 // of each lane's pairs, [V][lane]
+  float weight[2][2][kMaxPairs];           // of queries and keys, A and B: [V / 4][lane][4]
+  float sums[kWarps][kMaxDim];
 };
 
-template <int V>
-__device__ __forceinline__ void load_weights(const Args &a, Tile &s) {
-  const int lanes = a.lanes.d;
-  for (int i = threadIdx.x; i < 2 * a.dim / 2; i += kThreads) {
-    const int k = i >= a.dim / 2, slot = i - k * (a.dim / 2), lane = slot / V, j = slot % V;
+template <int V, bool NEAR>
+__device__ __forceinline__ void load_shared(const Args &a, const Frequencies &f, Shared &s) {
+  for (int i = threadIdx.x; i < a.lanes * V; i += kThreads) {
+    const int lane = i / V, j = i % V, at = lane * V, half = a.rot / 2;
+    // which pair of the head it is; one that stays turns by nothing
+    const int pair = !NEAR ? at + j : j < V / 2 ? at / 2 + j : (half + at) / 2 + j - V / 2;
+    s.turns[j * a.lanes + lane] = at < half ? f.turns[pair] : 0.0;
     const int2 p = places<V>(a, lane);
-    const int to = (j / 4 * lanes + lane) * 4 + j % 4;
-    const float *w = a.side[k].w;
-    s.weight[k][0][to] = w ? w[p.x + j] : 1.0f;
-    s.weight[k][1][to] = w ? w[p.y + j] : 1.0f;
-  }
-}
-
-// angles, places and lengths of `tokens` tokens from token `first` on
-template <int V>
-__device__ __forceinline__ void load_tile(const Args &a, const Frequencies &f, Tile &s, long long first, int tokens) {
-  const int lanes = a.lanes.d, slots = lanes * V;
-  for (int i = threadIdx.x; i < tokens * slots; i += kThreads) {
-    const uint32_t q = cdg_divide(i / V, a.lanes);               // token
-    const int lane = i / V - q * lanes, j = i % V;
-    const uint32_t tok = (uint32_t)(first + q), b = cdg_divide(tok, a.len);
-    const uint32_t t = tok - b * a.len.d;
-    if (i - q * slots == 0) {
-      s.at[q][0] = b;
-      s.at[q][1] = t;
-      s.live[q] = !a.lens || (int)t < a.lens[b];
-    }
-    float2 cs = make_float2(1.0f, 0.0f);
-    const int p = pair_of<V>(a, lane, j);
-    if (p >= 0) {
-      const long long at = b * a.pos_stride + t;
-      const double pos = !a.pos ? (double)t : a.pos_bits == 64 ? (double)static_cast<const long long *>(a.pos)[at]
-                                                               : (double)static_cast<const int *>(a.pos)[at];
-      const double turns = pos * f.turns[p];
-      sincospif(2.0f * (float)(turns - rint(turns)), &cs.y, &cs.x);
-    }
-    s.turn[q * slots + (j / 2 * lanes + lane) * 2 + j % 2] = cs;
-  }
-}
-
-// the pairs of (p, q) turned, or turned back
-template <int V, bool BACK>
-__device__ __forceinline__ void turn_pairs(const Args &a, const float2 *turn, float (&p)[V], float (&q)[V]) {
-  const float4 *c = reinterpret_cast<const float4 *>(turn);
-  const int lanes = a.lanes.d;
-  auto rotate = [](float cos, float sin, float &x, float &y) {
-    const float u = BACK ? fmaf(x, cos, y * sin) : fmaf(x, cos, -(y * sin));
-    y = BACK ? fmaf(y, cos, -(x * sin)) : fmaf(y, cos, x * sin);
-    x = u;
-  };
+    const int to = (j / 4 * a.lanes + lane) * 4 + j % 4;
 #pragma unroll
-  for (int j = 0; j < V; j += 2) {
-    const float4 cs = c[j / 2 * lanes];
-    if (a.interleaved) {
-      float *v = j < V / 2 ? p : q;
-      const int i = j < V / 2 ? 2 * j : 2 * j - V;
-      rotate(cs.x, cs.y, v[i], v[i + 1]);
-      rotate(cs.z, cs.w, v[i + 2], v[i + 3]);
-    } else {
-      rotate(cs.x, cs.y, p[j], q[j]);
-      rotate(cs.z, cs.w, p[j + 1], q[j + 1]);
+    for (int k = 0; k < 2; ++k) {
+      const float *w = a.side[k].w;
+      s.weight[k][0][to] = w ? w[p.x + j] : 1.0f;
+      s.weight[k][1][to] = w ? w[p.y + j] : 1.0f;
     }
   }
 }
 
-// times the weight
-template <int V>
-__device__ __forceinline__ void weigh(const Args &a, const float *weight, float (&p)[V]) {
-  const float4 *c = reinterpret_cast<const float4 *>(weight);
+// cos and sin of a lane's V angles.  Half layout: as they come, sin negated to turn back; neighbours: (cos, cos), (-sin, sin).
+template <int V, bool NEAR>
+struct Turn {
+  float2 c[NEAR ? V : V / 2], s[NEAR ? V : V / 2];
+  __device__ __forceinline__ void set(const Args &a, const Shared &sh, long long pos, int lane, bool back) {
 #pragma unroll
-  for (int j = 0; j < V; j += 4) {
-    const float4 w = c[j / 4 * a.lanes.d];
-    p[j] *= w.x; p[j + 1] *= w.y; p[j + 2] *= w.z; p[j + 3] *= w.w;
+    for (int j = 0; j < V; ++j) {
+      const double turns = (double)pos * sh.turns[j * a.lanes + lane];
+      float sin, cos;
+      sincospif(2.0f * (float)(turns - rint(turns)), &sin, &cos);
+      if (back) sin = -sin;
+      if (NEAR) {
+        c[j] = make_float2(cos, cos);
+        s[j] = make_float2(-sin, sin);
+      } else if (j % 2) {
+        c[j / 2].y = cos;
+        s[j / 2].y = sin;
+      } else {
+        c[j / 2].x = cos;
+        s[j / 2].x = sin;
+      }
+    }
+  }
+  // (p, q) turned
+  __device__ __forceinline__ void apply(float2 (&p)[V / 2], float2 (&q)[V / 2]) const {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      if (NEAR) {
+        p[j] = fma2(make_float2(p[j].y, p[j].x), s[j], mul2(p[j], c[j]));
+        q[j] = fma2(make_float2(q[j].y, q[j].x), s[V / 2 + j], mul2(q[j], c[V / 2 + j]));
+      } else {
+        const float2 t = mul2(q[j], s[j]), u = mul2(p[j], c[j]);
+        q[j] = fma2(p[j], s[j], mul2(q[j], c[j]));
+        p[j] = make_float2(u.x - t.x, u.y - t.y);
+      }
+    }
+  }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const CdgVec<T, V> &v, float2 (&p)[V / 2]) {
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) p[j] = make_float2(v.get(2 * j), v.get(2 * j + 1));
+}
+template <typename T, int V>
+__device__ __forceinline__ void pack_store(const float2 (&p)[V / 2], T *to) {
+  float f[V];
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) { f[2 * j] = p[j].x; f[2 * j + 1] = p[j].y; }
+  CdgVec<T, V> v;
+  v.set(f);
+  v.store(to);
+}
+template <int V>
+__device__ __forceinline__ void weigh(const Args &a, const float *weight, float2 (&p)[V / 2]) {
+#pragma unroll
+  for (int j = 0; j < V / 4; ++j) {
+    const float4 w = *reinterpret_cast<const float4 *>(weight + j * a.lanes * 4);
+    p[2 * j] = mul2(p[2 * j], make_float2(w.x, w.y));
+    p[2 * j + 1] = mul2(p[2 * j + 1], make_float2(w.z, w.w));
   }
 }
 
@@ -149,179 +142,186 @@ __device__ __forceinline__ float head_sum(float v, int group) {
   return v;
 }
 
-// A block takes a tile of tokens, all heads of queries and keys: the tile's angles once, then a group of lanes to a head.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(long long tokens, const __grid_constant__ Args a,
+__device__ __forceinline__ long long position(const Args &a, uint32_t b, uint32_t t) {
+  if (!a.pos) return t;
+  const long long at = b * a.pos_stride + t;
+  return a.pos_bits == 64 ? static_cast<const long long *>(a.pos)[at] : static_cast<const int *>(a.pos)[at];
+}
+
+template <typename T, int V, bool NEAR>
+__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t items, const __grid_constant__ Args a,
                                                                   const __grid_constant__ Frequencies f) {
-  constexpr int U = 2;                     // heads to a group at a time
-  __shared__ __align__(16) Tile s;
+  constexpr int U = 2;                     // heads at a time
+  __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const long long first = (long long)blockIdx.x * a.tile;
-  const int count = (int)min((long long)a.tile, tokens - first), items = count * (int)a.heads[2].d;
-  const int group = a.group, lane = threadIdx.x & (group - 1), groups = kThreads / group;
-  const bool mine = lane < (int)a.lanes.d;
+  const int group = a.group, lane = threadIdx.x & (group - 1);
+  const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
-  load_weights<V>(a, s);
-  load_tile<V>(a, f, s, first, count);
+  load_shared<V, NEAR>(a, f, s);
   __syncthreads();
-  for (int i0 = 0; i0 < items; i0 += U * groups) {
+  const uint32_t item = blockIdx.x * (kThreads / group) + threadIdx.x / group;
+  const bool some = item < items;
+  const uint32_t tok = some ? cdg_divide(item, a.parts[0]) : 0, part = item - tok * a.parts[0].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
+  const int heads = a.side[0].heads + a.side[1].heads, per = (heads + a.parts[0].d - 1) / a.parts[0].d;
+  const int h0 = part * per, h1 = some ? min(heads, h0 + per) : h0;
+  const bool live = some && mine && (!a.lens || (int)t < a.lens[b]);
+  Turn<V, NEAR> turn;
+  turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, false);
+  const T *x[2];
+  T *y[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const Side &z = a.side[k];
+    const int back = k ? a.side[0].heads : 0;            // the head index counts queries first
+    x[k] = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] - back * z.xs[2];
+    y[k] = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] - back * z.ys[2];
+  }
+  for (int i = 0; i < per; i += U) {                      // (the same number for every group of a warp)
     CdgVec<T, V> va[U], vb[U];
-    T *y[U];
-    int tok[U], key[U];
-    bool live[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * groups + threadIdx.x / group;
+      const int h = h0 + i + u, k = h >= a.side[0].heads;
       va[u].zero();
       vb[u].zero();
-      y[u] = nullptr;
-      tok[u] = key[u] = 0;
-      live[u] = false;
-      if (i < items) {
-        tok[u] = cdg_divide(i, a.heads[2]);
-        int h = i - tok[u] * (int)a.heads[2].d;
-        key[u] = h >= a.side[0].heads;
-        if (key[u]) h -= a.side[0].heads;
-        const Side &z = key[u] ? a.side[1] : a.side[0];
-        live[u] = s.live[tok[u]];
-        const long long b = s.at[tok[u]][0], t = s.at[tok[u]][1];
-        y[u] = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + h * z.ys[2];
-        if (live[u] && mine) {
-          const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + h * z.xs[2];
-          va[u].load(x + at.x);
-          vb[u].load(x + at.y);
-        }
+      if (live && h < h1) {
+        const T *from = (k ? x[1] : x[0]) + h * (k ? a.side[1].xs[2] : a.side[0].xs[2]);
+        va[u].load(from + at.x);
+        vb[u].load(from + at.y);
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float p[V], q[V], sum = 0.0f;
+      const int h = h0 + i + u, k = h >= a.side[0].heads;
+      float2 p[V / 2], q[V / 2], sum = make_float2(0.0f, 0.0f);
+      unpack(va[u], p);
+      unpack(vb[u], q);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        p[j] = va[u].get(j);
-        q[j] = vb[u].get(j);
-        sum = fmaf(p[j], p[j], fmaf(q[j], q[j], sum));
-      }
-      const float rstd = 1.0f / sqrtf(head_sum(sum, group) / (float)a.dim + a.eps);
-      if (!y[u] || !mine) continue;
-      if (live[u]) {
+      for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+      const float total = head_sum(sum.x + sum.y, group);
+      if (h >= h1 || !mine) continue;
+      // (0 where there is nothing: with eps = 0 it would be infinite)
+      const float rstd = live ? 1.0f / sqrtf(total / (float)a.dim + a.eps) : 0.0f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) { p[j] *= rstd; q[j] *= rstd; }
-        weigh<V>(a, s.weight[key[u]][0] + lane * 4, p);
-        weigh<V>(a, s.weight[key[u]][1] + lane * 4, q);
-        turn_pairs<V, false>(a, s.turn + tok[u] * (int)a.lanes.d * V + lane * 2, p, q);
-        va[u].set(p);
-        vb[u].set(q);
+      for (int j = 0; j < V / 2; ++j) {
+        p[j] = mul2(p[j], make_float2(rstd, rstd));
+        q[j] = mul2(q[j], make_float2(rstd, rstd));
       }
-      va[u].store(y[u] + at.x);
-      vb[u].store(y[u] + at.y);
+      weigh<V>(a, s.weight[k][0] + lane * 4, p);
+      weigh<V>(a, s.weight[k][1] + lane * 4, q);
+      turn.apply(p, q);
+      T *to = (k ? y[1] : y[0]) + h * (k ? a.side[1].ys[2] : a.side[0].ys[2]);
+      pack_store<T, V>(p, to + at.x);
+      pack_store<T, V>(q, to + at.y);
     }
   }
 }
 
-// A block takes a chunk of one worker's tokens (blockIdx.y), of its queries or of its keys, tile by tile, and keeps its sums of
-// g' n in registers; at the end they go to part[worker][chunk][dim], queries' chunks first.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) rotary_backward_kernel(long long tokens, int q_chunks, int k_chunks, const __grid_constant__ Args a,
-                                                                   const __grid_constant__ Frequencies f, float *part) {
-  __shared__ __align__(16) Tile s;
+// A block takes a chunk of one worker's (blockIdx.y) tokens, of its queries or of its keys, and keeps its sums of g' n in registers;
+// at the end they go to part[worker][chunk][dim], queries' chunks first.  The next head is requested before this one is worked on.
+template <typename T, int V, bool NEAR>
+__global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t tokens, int q_chunks, int k_chunks, const __grid_constant__ Args a,
+                                                                      const __grid_constant__ Frequencies f, float *part) {
+  __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int key = (int)blockIdx.x >= q_chunks, chunk = blockIdx.x - key * q_chunks, chunks = key ? k_chunks : q_chunks;
   const Side &z = a.side[key];
-  // tiles are dealt out evenly
-  const long long tiles = (tokens + a.tile - 1) / a.tile, t0 = tiles * chunk / chunks, t1 = tiles * (chunk + 1) / chunks;
-  const long long base = (long long)blockIdx.y * tokens;
-  const int group = a.group, lane = threadIdx.x & (group - 1), groups = kThreads / group;
-  const bool mine = lane < (int)a.lanes.d;
+  const int group = a.group, groups = kThreads / group, lane = threadIdx.x & (group - 1);
+  const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
   const float inv = 1.0f / (float)a.dim;
-  float wa[V] = {}, wb[V] = {};
-  load_weights<V>(a, s);
-  for (long long tile = t0; tile < t1; ++tile) {
-    const long long first = tile * a.tile;
-    const int count = (int)min((long long)a.tile, tokens - first), items = count * z.heads;
-    __syncthreads();
-    load_tile<V>(a, f, s, base + first, count);
-    __syncthreads();
-    for (int i0 = 0; i0 < items; i0 += groups) {
-      const int i = i0 + threadIdx.x / group;
-      CdgVec<T, V> va, vb, da, db;
-      va.zero(); vb.zero(); da.zero(); db.zero();
-      T *y = nullptr;
-      int tok = 0;
-      bool live = false;
-      if (i < items) {
-        tok = cdg_divide(i, a.heads[key]);
-        const int h = i - tok * z.heads;
-        const long long b = s.at[tok][0], t = s.at[tok][1];
-        y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + h * z.ys[2];
-        live = s.live[tok];
-        if (live && mine) {
-          const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + h * z.xs[2];
-          const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + h * z.dys[2];
-          va.load(x + at.x); vb.load(x + at.y);
-          da.load(dy + at.x); db.load(dy + at.y);
-        }
+  const uint32_t items = tokens * a.parts[key].d, rounds = (items + groups - 1) / groups;           // each group an item
+  const uint32_t r0 = (uint32_t)((unsigned long long)rounds * chunk / chunks), r1 = (uint32_t)((unsigned long long)rounds * (chunk + 1) / chunks);
+  const int per = (z.heads + a.parts[key].d - 1) / a.parts[key].d;
+  float2 wa[V / 2] = {}, wb[V / 2] = {};
+  load_shared<V, NEAR>(a, f, s);
+  __syncthreads();
+  const float *weight_a = s.weight[key][0] + lane * 4, *weight_b = s.weight[key][1] + lane * 4;
+  for (uint32_t r = r0; r < r1; ++r) {
+    const uint32_t item = r * groups + threadIdx.x / group;
+    const bool some = item < items;
+    const uint32_t local = some ? cdg_divide(item, a.parts[key]) : 0, share = item - local * a.parts[key].d;
+    const uint32_t tok = blockIdx.y * tokens + local, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
+    const int h0 = share * per, count = some && mine ? min(z.heads - h0, per) : 0;
+    const bool live = some && mine && (!a.lens || (int)t < a.lens[b]);
+    const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + h0 * z.xs[2];
+    const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + h0 * z.dys[2];
+    T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + h0 * z.ys[2];
+    CdgVec<T, V> va, vb, da, db;
+    auto request = [&](int h) {
+      if (live && h < count) {
+        va.load(x + at.x); vb.load(x + at.y);
+        da.load(dy + at.x); db.load(dy + at.y);
+      } else {
+        va.zero(); vb.zero(); da.zero(); db.zero();
       }
-      float p[V], q[V], g[V], h[V], sum = 0.0f;
+      x += z.xs[2];
+      dy += z.dys[2];
+    };
+    request(0);
+    Turn<V, NEAR> turn;
+    turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, true);
+    for (int h = 0; h < per; ++h) {
+      float2 p[V / 2], q[V / 2], g[V / 2], e[V / 2], sum = make_float2(0.0f, 0.0f);
+      unpack(va, p); unpack(vb, q);
+      unpack(da, g); unpack(db, e);
+      request(h + 1);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        p[j] = va.get(j); q[j] = vb.get(j);
-        g[j] = da.get(j); h[j] = db.get(j);
-        sum = fmaf(p[j], p[j], fmaf(q[j], q[j], sum));
-      }
+      for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+      const float total = head_sum(sum.x + sum.y, group);
+      turn.apply(g, e);
       // (0 where there is nothing: with eps = 0 it would be infinite)
-      sum = head_sum(sum, group);
-      const float rstd = live ? 1.0f / sqrtf(sum * inv + a.eps) : 0.0f;
-      if (mine) turn_pairs<V, true>(a, s.turn + tok * (int)a.lanes.d * V + lane * 2, g, h);
+      const float rstd = live && h < count ? 1.0f / sqrtf(total * inv + a.eps) : 0.0f;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        p[j] *= rstd; q[j] *= rstd;
-        wa[j] = fmaf(g[j], p[j], wa[j]);
-        wb[j] = fmaf(h[j], q[j], wb[j]);
+      for (int j = 0; j < V / 2; ++j) {
+        p[j] = mul2(p[j], make_float2(rstd, rstd));
+        q[j] = mul2(q[j], make_float2(rstd, rstd));
+        wa[j] = fma2(g[j], p[j], wa[j]);
+        wb[j] = fma2(e[j], q[j], wb[j]);
       }
-      float hn = 0.0f;
       if (mine) {
-        weigh<V>(a, s.weight[key][0] + lane * 4, g);
-        weigh<V>(a, s.weight[key][1] + lane * 4, h);
+        weigh<V>(a, weight_a, g);
+        weigh<V>(a, weight_b, e);
       }
+      sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-      for (int j = 0; j < V; ++j) hn = fmaf(g[j], p[j], fmaf(h[j], q[j], hn));
-      hn = head_sum(hn, group) * inv;
-      if (!y || !mine) continue;
+      for (int j = 0; j < V / 2; ++j) sum = fma2(g[j], p[j], fma2(e[j], q[j], sum));
+      const float hn = -head_sum(sum.x + sum.y, group) * inv;
+      if (h < count) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        p[j] = rstd * fmaf(-hn, p[j], g[j]);
-        q[j] = rstd * fmaf(-hn, q[j], h[j]);
+        for (int j = 0; j < V / 2; ++j) {
+          p[j] = mul2(fma2(p[j], make_float2(hn, hn), g[j]), make_float2(rstd, rstd));
+          q[j] = mul2(fma2(q[j], make_float2(hn, hn), e[j]), make_float2(rstd, rstd));
+        }
+        pack_store<T, V>(p, y + at.x);
+        pack_store<T, V>(q, y + at.y);
+        y += z.ys[2];
       }
-      va.set(p); vb.set(q);
-      va.store(y + at.x);
-      vb.store(y + at.y);
     }
   }
   if (!part) return;
-  // the groups of a warp, then the warps, in order; the tile's memory is free by then
-  __syncthreads();
-  float *sums = reinterpret_cast<float *>(s.turn);               // [warp][dim]
+  // the groups of a warp, then the warps, in order
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
+  for (int j = 0; j < V / 2; ++j) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
       if (o >= group) {
-        wa[j] += __shfl_xor_sync(0xffffffffu, wa[j], o);
-        wb[j] += __shfl_xor_sync(0xffffffffu, wb[j], o);
+        wa[j] = add2(wa[j], make_float2(__shfl_xor_sync(0xffffffffu, wa[j].x, o), __shfl_xor_sync(0xffffffffu, wa[j].y, o)));
+        wb[j] = add2(wb[j], make_float2(__shfl_xor_sync(0xffffffffu, wb[j].x, o), __shfl_xor_sync(0xffffffffu, wb[j].y, o)));
       }
     if (mine && (threadIdx.x & 31) < group) {
-      sums[(threadIdx.x >> 5) * a.dim + at.x + j] = wa[j];
-      sums[(threadIdx.x >> 5) * a.dim + at.y + j] = wb[j];
+      float *to = s.sums[threadIdx.x >> 5];
+      to[at.x + 2 * j] = wa[j].x;
+      to[at.x + 2 * j + 1] = wa[j].y;
+      to[at.y + 2 * j] = wb[j].x;
+      to[at.y + 2 * j + 1] = wb[j].y;
     }
   }
   __syncthreads();
   for (int c = threadIdx.x; c < a.dim; c += kThreads) {
     float t = 0.0f;
-    for (int o = 0; o < kWarps; ++o) t += sums[o * a.dim + c];
+    for (int o = 0; o < kWarps; ++o) t += s.sums[o][c];
     part[((long long)blockIdx.y * gridDim.x + blockIdx.x) * a.dim + c] = t;
   }
 }
@@ -370,31 +370,30 @@ bool shape_ok(const cdgrab_rotary_shape *s) {
 int pairs_to_lane(const cdgrab_rotary_shape *s) {
   return s->dtype == CDGRAB_BF16 && s->rotary_dim % 16 == 0 && s->head_dim % 16 == 0 ? 8 : 4;
 }
-// tokens to a tile: at most `items` heads to each group of lanes, as far as the angles' room goes
-int tile_of(const cdgrab_rotary_shape *s, int heads, int items) {
-  const int lanes = s->head_dim / 2 / pairs_to_lane(s), room = kMaxSlots / (s->head_dim / 2) < kMaxTokens ? kMaxSlots / (s->head_dim / 2) : kMaxTokens;
+int lanes_of(const cdgrab_rotary_shape *s) { return s->head_dim / 2 / pairs_to_lane(s); }
+int group_of(const cdgrab_rotary_shape *s) {
   int group = 1;
-  while (group < lanes) group *= 2;
-  const int want = items * (kThreads / group) / heads;
-  return want < 1 ? 1 : want < room ? want : room;
+  while (group < lanes_of(s)) group *= 2;
+  return group;
 }
+// Shares that each token's heads are dealt out in: one where the tokens fill the SMs, up to a share for every two heads where
+// there are few (each share computes the token's angles again).
 constexpr int kSms = 148;
-// Chunks of a worker's tokens, for queries and keys: in proportion to their heads about two rounds of the blocks that are resident
-// at once (four to an SM), a tile to each at least.
-void chunks_of(const cdgrab_rotary_shape *s, int m, int tile, int &q, int &k) {
-  const long long tiles = ((long long)s->batch / m * s->len + tile - 1) / tile;
-  const int all = s->heads + s->kv_heads;
-  auto share = [&](int heads) {
-    if (heads == 0 || tiles == 0) return 1ll;
-    const long long c = (8ll * kSms * heads + (long long)all * m - 1) / ((long long)all * m);
-    return c < tiles ? c : tiles;
-  };
-  q = (int)share(s->heads);
-  k = (int)share(s->kv_heads);
+int parts_of(const cdgrab_rotary_shape *s, int heads) {
+  const long long tokens = (long long)s->batch * s->len, fill = 2ll * kSms * (kThreads / group_of(s));
+  const long long most = (heads + 1) / 2, want = tokens > 0 ? fill / tokens : 1, parts = want < most ? want : most;
+  if (parts <= 1) return 1;
+  const long long per = (heads + parts - 1) / parts;
+  return (int)((heads + per - 1) / per);
 }
-int backward_tile(const cdgrab_rotary_shape *s) {
-  const int most = s->heads > s->kv_heads ? s->heads : s->kv_heads;
-  return tile_of(s, most > 0 ? most : 1, 2);
+// Chunks of a worker's queries or keys: 32,768 values to a block, an item to each group of lanes at least, about four rounds of the
+// blocks that are resident at once (two to an SM) at most.
+int chunks_of(const cdgrab_rotary_shape *s, int m, int heads) {
+  const long long tokens = (long long)s->batch / m * s->len, groups = kThreads / group_of(s);
+  if (tokens == 0 || heads == 0) return 1;
+  const long long rounds = (tokens * parts_of(s, heads) + groups - 1) / groups, work = (tokens * heads * s->head_dim + 32767) / 32768;
+  const long long most = 8ll * kSms / m, c = rounds < work ? rounds : work;
+  return (int)(c < most ? c : most < 1 ? 1 : most);
 }
 
 void fill(const cdgrab_rotary_shape *s, Args &a, Frequencies &f) {
@@ -406,11 +405,9 @@ void fill(const cdgrab_rotary_shape *s, Args &a, Frequencies &f) {
   a.side[0].heads = s->heads;
   a.side[1].heads = s->kv_heads;
   a.len = cdg_divisor((uint32_t)(s->len > 0 ? s->len : 1));
-  const int lanes = s->head_dim / 2 / pairs_to_lane(s), counts[3] = {s->heads, s->kv_heads, s->heads + s->kv_heads};
-  a.lanes = cdg_divisor(lanes);
-  for (int i = 0; i < 3; ++i) a.heads[i] = cdg_divisor(counts[i] > 0 ? counts[i] : 1);
-  for (a.group = 1; a.group < lanes;) a.group *= 2;
-  a.dim = s->head_dim; a.rot = s->rotary_dim; a.interleaved = s->interleaved; a.eps = s->eps;
+  a.lanes = lanes_of(s);
+  a.group = group_of(s);
+  a.dim = s->head_dim; a.rot = s->rotary_dim; a.eps = s->eps;
   // (a power for each pair costs more than the launch: each thread keeps its last table)
   static thread_local struct { double base; int rot; Frequencies f; } last = {};
   if (last.base != s->base || last.rot != s->rotary_dim) {
@@ -420,6 +417,14 @@ void fill(const cdgrab_rotary_shape *s, Args &a, Frequencies &f) {
     last.rot = s->rotary_dim;
   }
   f = last.f;
+}
+
+// f(T(), V, NEAR) for a shape's kernel
+template <typename F>
+int by_kind(const cdgrab_rotary_shape *s, F &&f) {
+  auto near = [&](auto t, auto v) { return s->interleaved ? f(t, v, std::true_type()) : f(t, v, std::false_type()); };
+  if (s->dtype == CDGRAB_F32) return near(0.0f, std::integral_constant<int, 4>());
+  return pairs_to_lane(s) == 8 ? near(__nv_bfloat16(), std::integral_constant<int, 8>()) : near(__nv_bfloat16(), std::integral_constant<int, 4>());
 }
 
 // the checks that both directions share; backward: with the gradients
@@ -454,20 +459,20 @@ extern "C" int cdgrab_rotary_forward(const cdgrab_rotary_shape *s, const void *q
   if (const int rc = cdg_ops_device(&dev)) return rc;
   Frequencies f;
   fill(s, a, f);
-  a.tile = tile_of(s, s->heads + s->kv_heads, 4);
-  const long long tokens = (long long)s->batch * s->len;
-  const dim3 grid((unsigned)((tokens + a.tile - 1) / a.tile));
+  a.parts[0] = cdg_divisor(parts_of(s, s->heads + s->kv_heads));
+  const long long items = (long long)s->batch * s->len * a.parts[0].d;
+  if (items >= (1ll << 31)) return CDGRAB_ERR_INVALID;
+  const int groups = kThreads / a.group;
+  const dim3 grid((unsigned)((items + groups - 1) / groups));
   cudaStream_t st = (cudaStream_t)stream;
-  auto go = [&](auto *kernel) { return cdg_launch_rc(cdg_ops_launch(kernel, grid, kThreads, 0, st, tokens, a, f)); };
-  if (s->dtype == CDGRAB_F32) return go(rotary_forward_kernel<float, 4>);
-  return pairs_to_lane(s) == 8 ? go(rotary_forward_kernel<__nv_bfloat16, 8>) : go(rotary_forward_kernel<__nv_bfloat16, 4>);
+  return by_kind(s, [&](auto t, auto v, auto near) {
+    return cdg_launch_rc(cdg_ops_launch(rotary_forward_kernel<decltype(t), v(), near()>, grid, kThreads, 0, st, (uint32_t)items, a, f));
+  });
 }
 
 extern "C" long long cdgrab_rotary_workspace_bytes(const cdgrab_rotary_shape *s, int m) {
   if (!shape_ok(s) || m < 1 || m > 65535 || s->batch % m) return -1;
-  int q, k;
-  chunks_of(s, m, backward_tile(s), q, k);
-  return 4ll * m * (q + k) * s->head_dim;
+  return 4ll * m * (chunks_of(s, m, s->heads) + chunks_of(s, m, s->kv_heads)) * s->head_dim;
 }
 
 extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const void *dq, const void *dk, const void *q, const void *k,
@@ -489,14 +494,15 @@ extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const
   if (const int rc = cdg_ops_device(&dev)) return rc;
   Frequencies f;
   fill(s, a, f);
-  a.tile = backward_tile(s);
-  int qc, kc;
-  chunks_of(s, m, a.tile, qc, kc);
+  a.parts[0] = cdg_divisor(parts_of(s, s->heads));
+  a.parts[1] = cdg_divisor(parts_of(s, s->kv_heads));
+  const int qc = chunks_of(s, m, s->heads), kc = chunks_of(s, m, s->kv_heads);
   cudaStream_t st = (cudaStream_t)stream;
   float *part = dqw || dkw ? static_cast<float *>(workspace) : nullptr;
-  auto go = [&](auto *kernel) { return cdg_launch_rc(cdg_ops_launch(kernel, dim3(qc + kc, m), kThreads, 0, st, tokens, qc, kc, a, f, part)); };
-  int rc = s->dtype == CDGRAB_F32 ? go(rotary_backward_kernel<float, 4>)
-           : pairs_to_lane(s) == 8 ? go(rotary_backward_kernel<__nv_bfloat16, 8>) : go(rotary_backward_kernel<__nv_bfloat16, 4>);
+  const int rc = by_kind(s, [&](auto t, auto v, auto near) {
+    return cdg_launch_rc(cdg_ops_launch(rotary_backward_kernel<decltype(t), v(), near()>, dim3(qc + kc, m), kThreads, 0, st, (uint32_t)tokens, qc,
+                                        kc, a, f, part));
+  });
   if (rc != CDGRAB_OK || !part) return rc;
   const dim3 grid((s->head_dim + 31) / 32, m, 2);
   return cdg_launch_rc(grad_dtype == CDGRAB_F32
