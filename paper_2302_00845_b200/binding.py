@@ -8,6 +8,7 @@ handle are what crosses the boundary.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -782,13 +783,21 @@ def dropout_backward(dy, p: float, seed: int, call: int = 0, step=0, out=None, d
 _ROTARY = struct.Struct("8idfi18q")          # cdgrab_rotary_shape
 
 
-def _heads(t, name: str, shape, dtype):
-    """(batch, token, head) strides of a [batch][token][head][head_dim] tensor; nothing is asked of an empty one."""
-    if t is None:
+def _geometry(t):
+    """What the checks ask of a tensor."""
+    return None if t is None else (t.shape, t.stride(), t.dtype)
+
+
+def _head_steps(g, name: str, shape, dtype):
+    """(batch, token, head) strides of a [batch][token][head][head_dim] tensor; contiguous where it is still to be made."""
+    if shape is None:
         return _NONE
-    if t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)}, not {tuple(t.shape)} {t.dtype}")
-    a, b, c, inner = t.stride()
+    if g is None:
+        _, t, h, d = shape
+        return t * h * d, h * d, d
+    if g[2] != dtype or g[0] != shape:
+        raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)}, not {tuple(g[0])} {g[2]}")
+    a, b, c, inner = g[1]
     if inner != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the values of a head have to be contiguous")
     if (a | b | c) & 7:         # an axis of length one has no stride of its own
@@ -796,32 +805,75 @@ def _heads(t, name: str, shape, dtype):
     return a, b, c
 
 
+# Checks and shape of a call, which depend on sizes, strides and types alone: kept for the calls that follow, as they would take
+# half of a call's time.
+@functools.lru_cache(maxsize=512)
+def _rotary_plan(q, k, q_weight, k_weight, positions, lens, q_out, k_out, base, rotary_dim, interleaved, eps):
+    """(cdgrab_rotary_shape, position bits, position stride) from tensors' geometries."""
+    if len(q[0]) != 4 or (k is not None and len(k[0]) != 4):
+        raise ValueError("q, k: [batch][token][head][head_dim]")
+    qs, ks = q[0], None if k is None else k[0]
+    b, t, h, d = qs
+    dt, hk = q[2], 0
+    if k is not None:
+        kb, kt, hk, kd = ks
+        if kb != b or kt != t or kd != d or k[2] != dt:
+            raise ValueError("q and k do not go together")
+    if dt not in _CODES:
+        raise ValueError(f"q: float32 or bfloat16, not {dt}")
+    rotary_dim = d if rotary_dim is None else rotary_dim
+    if max(b, t, h, hk, d, abs(rotary_dim)) > _INT_MAX:
+        raise ValueError(f"q: {tuple(qs)}, rotary_dim {rotary_dim}")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and (w[2] != torch.float32 or w[0] != (d,) or (w[1] != (1,) and d > 1)):
+            raise ValueError(f"{name}: a contiguous float32 tensor [{d}]")
+    if lens is not None and (lens[2] != torch.int32 or lens[0] != (b,) or (lens[1] != (1,) and b > 1)):
+        raise ValueError(f"lens: an int32 tensor [{b}]")
+    bits, step = 0, 0
+    if positions is not None:
+        shape, stride, dtype = positions
+        if dtype not in (torch.int64, torch.int32) or shape not in ((t,), (b, t)):
+            raise ValueError("positions: int32 or int64, [token] or [batch][token]")
+        if t > 1 and stride[-1] != 1:
+            raise ValueError("positions: those of a sequence have to be contiguous")
+        bits = 64 if dtype == torch.int64 else 32
+        step = stride[0] if len(shape) == 2 and b > 1 else 0
+    return RotaryShape.from_buffer_copy(_ROTARY.pack(
+        b, t, h, hk, d, rotary_dim, 1 if interleaved else 0, _CODES[dt], base, eps, 0, *_head_steps(q, "q", qs, dt),
+        *_head_steps(k, "k", ks, dt), *_head_steps(q_out, "q_out", qs, dt), *_head_steps(k_out, "k_out", ks, dt), *_NONE, *_NONE)), bits, step
+
+
+@functools.lru_cache(maxsize=512)
+def _rotary_backward_plan(dq, dk, dq_weight, dk_weight, *forward):
+    """What _rotary_plan gives, with the gradients' strides, and (workers, their gradients' type and stride, scratch bytes)."""
+    sh, bits, step = _rotary_plan(*forward)
+    q, k = forward[:2]
+    sh = RotaryShape.from_buffer_copy(sh)
+    if (k is None) != (dk is None):
+        raise ValueError("k and dk: both or neither")
+    sh.dq_stride[:] = _head_steps(dq, "dq", q[0], q[2])
+    sh.dk_stride[:] = _head_steps(dk, "dk", None if k is None else k[0], q[2])
+    b, d = sh.batch, sh.head_dim
+    m, gcode, ws, first = 1, F32, d, None
+    for g, name in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
+        if g is None:
+            continue
+        shape, stride, dtype = g
+        if dtype not in _CODES or len(shape) != 2 or shape[1] != d or (stride[1] != 1 and d > 1):
+            raise ValueError(f"{name}: [workers][{d}], float32 or bfloat16, not {tuple(shape)} {dtype}")
+        if first is not None:
+            # (with one worker the row stride is not used)
+            if dtype != first[2] or shape != first[0] or (stride[0] != ws and m > 1):
+                raise ValueError("dq_weight and dk_weight: one type and one row stride")
+            continue
+        first, m, gcode, ws = g, shape[0], _CODES[dtype], stride[0] if shape[0] > 1 else d
+        if m < 1 or b % m:
+            raise ValueError(f"{b} sequences are not {m} workers' equal shares")
+    return sh, bits, step, m, gcode, ws, int(lib().cdgrab_rotary_workspace_bytes(sh, m))
+
+
 def _at(t):
     return None if t is None else t.data_ptr()
-
-
-def _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens):
-    """The sizes of cdgrab_rotary_shape, and the arguments for positions and lengths."""
-    if q.dim() != 4 or (k is not None and k.dim() != 4):
-        raise ValueError("q, k: [batch][token][head][head_dim]")
-    b, t, h, d = q.shape
-    hk = 0
-    if k is not None:
-        kb, kt, hk, kd = k.shape
-        if kb != b or kt != t or kd != d or k.dtype != q.dtype:
-            raise ValueError("q and k do not go together")
-    if max(b, t, h, hk, d) > _INT_MAX:
-        raise ValueError(f"q: {tuple(q.shape)}")
-    sizes = (b, t, h, hk, d, d if rotary_dim is None else rotary_dim, 1 if interleaved else 0, _code(q, "q"), base, eps, 0)
-    pos, bits, step = None, 0, 0
-    if positions is not None:
-        bits = 64 if positions.dtype is torch.int64 else 32
-        if positions.dtype not in (torch.int64, torch.int32) or positions.shape not in ((t,), (b, t)):
-            raise ValueError("positions: int32 or int64, [token] or [batch][token]")
-        if t > 1 and positions.stride(-1) != 1:
-            raise ValueError("positions: those of a sequence have to be contiguous")
-        pos, step = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 and b > 1 else 0
-    return sizes, pos, bits, step, _lens(lens, "lens", b)
 
 
 def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: float = 10000.0, rotary_dim: int | None = None,
@@ -832,17 +884,15 @@ def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: flo
     positions: int32 or int64 [t] or [b][t], the token's index by default.  lens: int32 [b], the tokens in use; the
     others become zero.  Returns (q_out, k_out), which may be q and k."""
     handle, other = _place(stream, q, k, q_weight, k_weight, positions, lens, q_out, k_out)
-    sizes, pos, bits, step, ln = _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens)
-    d, dt = sizes[4], q.dtype
+    sh, bits, step = _rotary_plan(
+        _geometry(q), _geometry(k), _geometry(q_weight), _geometry(k_weight), _geometry(positions), _geometry(lens),
+        _geometry(q_out), _geometry(k_out), base, rotary_dim, interleaved, eps)
     if q_out is None:
         q_out = _empty_like(q, other)
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
-    ks = None if k is None else k.shape
-    sh = RotaryShape.from_buffer_copy(_ROTARY.pack(*sizes, *_heads(q, "q", q.shape, dt), *_heads(k, "k", ks, dt),
-                                                   *_heads(q_out, "q_out", q.shape, dt), *_heads(k_out, "k_out", ks, dt), *_NONE, *_NONE))
-    rc = lib().cdgrab_rotary_forward(sh, q.data_ptr(), _at(k), _vector(q_weight, "q_weight", d), _vector(k_weight, "k_weight", d),
-                                     pos, bits, step, ln, q_out.data_ptr(), _at(k_out), handle)
+    rc = lib().cdgrab_rotary_forward(sh, q.data_ptr(), _at(k), _at(q_weight), _at(k_weight), _at(positions), bits, step, _at(lens),
+                                     q_out.data_ptr(), _at(k_out), handle)
     if rc:
         _check(rc, "cdgrab_rotary_forward")
     return q_out, k_out
@@ -856,35 +906,18 @@ def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, 
     as a rule) receive each worker's own sums, either may be None.  Returns the gradients of q and k, in q_out and
     k_out where given (dq and dk themselves, or views of one buffer)."""
     handle, other = _place(stream, dq, dk, q, k, q_weight, k_weight, positions, lens, dq_weight, dk_weight, q_out, k_out)
-    sizes, pos, bits, step, ln = _rotary_sizes(q, k, base, rotary_dim, interleaved, eps, positions, lens)
-    d, dt = sizes[4], q.dtype
-    g = dq_weight if dq_weight is not None else dk_weight
-    m, gcode, ws = 1, F32, d
-    if g is not None:
-        m = g.shape[0]
-        if m < 1 or sizes[0] % m:
-            raise ValueError(f"{sizes[0]} sequences are not {m} workers' equal shares")
-        gcode, ws = _code(g, "dq_weight, dk_weight"), _row_stride(g, "dq_weight, dk_weight", m, d)
-        # (with one worker the row stride is not used)
-        if dk_weight is not None and dk_weight is not g and (
-                dk_weight.dtype != g.dtype or (_row_stride(dk_weight, "dk_weight", m, d) != ws and m > 1)):
-            raise ValueError("dq_weight and dk_weight: one type and one row stride")
-    if (k is None) != (dk is None):
-        raise ValueError("k and dk: both or neither")
+    sh, bits, step, m, gcode, ws, nbytes = _rotary_backward_plan(
+        _geometry(dq), _geometry(dk), _geometry(dq_weight), _geometry(dk_weight), _geometry(q), _geometry(k), _geometry(q_weight),
+        _geometry(k_weight), _geometry(positions), _geometry(lens), _geometry(q_out), _geometry(k_out), base, rotary_dim,
+        interleaved, eps)
     if q_out is None:
         q_out = _empty_like(q, other)
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
-    qs, ks = q.shape, None if k is None else k.shape
-    sh = RotaryShape.from_buffer_copy(_ROTARY.pack(
-        *sizes, *_heads(q, "q", qs, dt), *_heads(k, "k", ks, dt), *_heads(q_out, "q_out", qs, dt), *_heads(k_out, "k_out", ks, dt),
-        *_heads(dq, "dq", qs, dt), *_heads(dk, "dk", ks, dt)))
-    L = lib()
-    nbytes = L.cdgrab_rotary_workspace_bytes(sh, m)
     scratch = _scratch(q, nbytes, other)
-    rc = L.cdgrab_rotary_backward(sh, m, dq.data_ptr(), _at(dk), q.data_ptr(), _at(k), _vector(q_weight, "q_weight", d),
-                                  _vector(k_weight, "k_weight", d), pos, bits, step, ln, q_out.data_ptr(), _at(k_out), gcode,
-                                  _at(dq_weight), _at(dk_weight), ws, scratch.data_ptr(), max(16, nbytes), handle)
+    rc = lib().cdgrab_rotary_backward(
+        sh, m, dq.data_ptr(), _at(dk), q.data_ptr(), _at(k), _at(q_weight), _at(k_weight), _at(positions), bits, step, _at(lens),
+        q_out.data_ptr(), _at(k_out), gcode, _at(dq_weight), _at(dk_weight), ws, scratch.data_ptr(), max(16, nbytes), handle)
     if rc:
         _check(rc, "cdgrab_rotary_backward")
     return q_out, k_out

@@ -3,11 +3,11 @@
 //
 // Forward:   n = x rstd,  rstd = 1 / sqrt(sum x^2 / D + eps),  g = n w,  pairs of g turned by the angle t.
 // Backward:  g' = the gradient turned by -t,  h = g' w,  dx = rstd (h - n (sum h n) / D),  dw = sum g' n.
-// The angle of a far position is many turns: position x (frequency / 2 pi) is taken in 64 bits and only its fraction
-// goes on in 32.
+// The angle of a far position is many turns: it is reduced in 64-bit integers, and only the fraction of a turn goes on in 32 bits.
 #include <cmath>
 #include <type_traits>
 
+#include "ptx.cuh"
 #include "rows.cuh"
 
 namespace {
@@ -15,9 +15,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxDim = 256, kMaxPairs = kMaxDim / 2;
+constexpr int kAhead = 4;                  // heads on their way
 
-// turns per position of each pair: base^(-2 i / rotary_dim) / (2 pi)
-struct Frequencies { double turns[kMaxPairs]; };
+// Turns per position of each pair, base^(-2 i / rotary_dim) / (2 pi), less whole turns, in units of 2^-64: a position, which is whole,
+// times that is the angle modulo a turn, exactly but for the unit's half, in integer arithmetic that wraps.
+struct Frequencies { unsigned long long turns[kMaxPairs]; };
+
+constexpr long double kPi = 3.14159265358979323846264338327950288L;
 
 struct Side {                              // queries or keys
   const void *x, *dy;
@@ -32,7 +36,7 @@ struct Args {
   int pos_bits;
   long long pos_stride;
   const int *lens;
-  CdgDivisor len, parts[2];                // tokens to a sequence; shares that a token's heads are dealt out in (forward: [0])
+  CdgDivisor len, parts[2];                // tokens to a sequence; shares that a token's heads are dealt out in 
   int dim, rot, lanes, group;              // lanes: those that hold a head, V pairs each; group: the next power of two
   float eps;
 };
@@ -48,7 +52,7 @@ __device__ __forceinline__ int2 places(const Args &a, int lane) {
 }
 
 struct Shared {
-  double turns[kMaxPairs];                 // of each lane's pairs, [V][lane]
+  unsigned long long turns[kMaxPairs];     // of each lane's pairs, [V][lane]
   float weight[2][2][kMaxPairs];           // of queries and keys, A and B: [V / 4][lane][4]
   float sums[kWarps][kMaxDim];
 };
@@ -59,7 +63,7 @@ __device__ __forceinline__ void load_shared(const Args &a, const Frequencies &f,
     const int lane = i / V, j = i % V, at = lane * V, half = a.rot / 2;
     // which pair of the head it is; one that stays turns by nothing
     const int pair = !NEAR ? at + j : j < V / 2 ? at / 2 + j : (half + at) / 2 + j - V / 2;
-    s.turns[j * a.lanes + lane] = at < half ? f.turns[pair] : 0.0;
+    s.turns[j * a.lanes + lane] = at < half ? f.turns[pair] : 0ull;
     const int2 p = places<V>(a, lane);
     const int to = (j / 4 * a.lanes + lane) * 4 + j % 4;
 #pragma unroll
@@ -71,30 +75,76 @@ __device__ __forceinline__ void load_shared(const Args &a, const Frequencies &f,
   }
 }
 
-// cos and sin of a lane's V angles.  Half layout: as they come, sin negated to turn back; neighbours: (cos, cos), (-sin, sin).
+// cos and sin of a lane's j-th angle at a position
+template <int V>
+__device__ __forceinline__ float2 angle(const Args &a, const Shared &sh, long long pos, int lane, int j) {
+  const int part = (int)((unsigned long long)pos * sh.turns[j * a.lanes + lane] >> 32);      // of a turn, from -1/2
+  float2 cs;
+  sincospif((float)part * 0x1p-31f, &cs.y, &cs.x);
+  return cs;
+}
+
+// What turns a lane's V pairs, in registers.  Halves: p c + q (-s), q c + p s; neighbours (x, y): (x, y) (c, c) + (y, x) (-s, s).
+// Forward, the weight is in it: every factor times the weight of the value that it meets.
 template <int V, bool NEAR>
 struct Turn {
-  float2 c[NEAR ? V : V / 2], s[NEAR ? V : V / 2];
-  __device__ __forceinline__ void set(const Args &a, const Shared &sh, long long pos, int lane, bool back) {
+  float2 cp[V / 2], sp[V / 2], cq[V / 2], sq[V / 2];       // what p meets in p' and q', q in q' and p'; neighbours: p, swapped p, q, swapped q
+  __device__ __forceinline__ void set(const Args &a, const Shared &sh, long long pos, int lane, const float *wa, const float *wb) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const double turns = (double)pos * sh.turns[j * a.lanes + lane];
-      float sin, cos;
-      sincospif(2.0f * (float)(turns - rint(turns)), &sin, &cos);
-      if (back) sin = -sin;
+    for (int j = 0; j < V; j += 2) {
       if (NEAR) {
-        c[j] = make_float2(cos, cos);
-        s[j] = make_float2(-sin, sin);
-      } else if (j % 2) {
-        c[j / 2].y = cos;
-        s[j / 2].y = sin;
+        const float2 p = angle<V>(a, sh, pos, lane, j / 2), q = angle<V>(a, sh, pos, lane, V / 2 + j / 2);
+        const float2 u = *reinterpret_cast<const float2 *>(wa + j / 4 * a.lanes * 4 + j % 4), v = *reinterpret_cast<const float2 *>(wb + j / 4 * a.lanes * 4 + j % 4);
+        cp[j / 2] = make_float2(p.x * u.x, p.x * u.y);
+        sp[j / 2] = make_float2(-p.y * u.y, p.y * u.x);
+        cq[j / 2] = make_float2(q.x * v.x, q.x * v.y);
+        sq[j / 2] = make_float2(-q.y * v.y, q.y * v.x);
       } else {
-        c[j / 2].x = cos;
-        s[j / 2].x = sin;
+        const float2 k = angle<V>(a, sh, pos, lane, j), l = angle<V>(a, sh, pos, lane, j + 1);
+        const float2 u = *reinterpret_cast<const float2 *>(wa + j / 4 * a.lanes * 4 + j % 4), v = *reinterpret_cast<const float2 *>(wb + j / 4 * a.lanes * 4 + j % 4);
+        cp[j / 2] = make_float2(k.x * u.x, l.x * u.y);
+        sp[j / 2] = make_float2(k.y * u.x, l.y * u.y);
+        cq[j / 2] = make_float2(k.x * v.x, l.x * v.y);
+        sq[j / 2] = make_float2(-k.y * v.x, -l.y * v.y);
       }
     }
   }
-  // (p, q) turned
+  __device__ __forceinline__ void apply(float2 (&p)[V / 2], float2 (&q)[V / 2]) const {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      if (NEAR) {
+        p[j] = fma2(make_float2(p[j].y, p[j].x), sp[j], mul2(p[j], cp[j]));
+        q[j] = fma2(make_float2(q[j].y, q[j].x), sq[j], mul2(q[j], cq[j]));
+      } else {
+        const float2 t = mul2(p[j], cp[j]);
+        const float2 u = mul2(q[j], cq[j]);
+        const float2 v = fma2(q[j], sq[j], t);
+        q[j] = fma2(p[j], sp[j], u);
+        p[j] = v;
+      }
+    }
+  }
+};
+// The gradients turned back, without the weight: halves p c + q s, q c - p s.
+template <int V, bool NEAR>
+struct TurnBack {
+  float2 c[NEAR ? V : V / 2], s[NEAR ? V : V / 2];
+  __device__ __forceinline__ void set(const Args &a, const Shared &sh, long long pos, int lane) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float2 cs = angle<V>(a, sh, pos, lane, j);
+      if (NEAR) {
+        c[j] = make_float2(cs.x, cs.x);
+        s[j] = make_float2(cs.y, -cs.y);
+      } else if (j % 2) {
+        c[j / 2].y = cs.x;
+        s[j / 2].y = cs.y;
+      } else {
+        c[j / 2].x = cs.x;
+        s[j / 2].x = cs.y;
+      }
+    }
+  }
   __device__ __forceinline__ void apply(float2 (&p)[V / 2], float2 (&q)[V / 2]) const {
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) {
@@ -102,9 +152,9 @@ struct Turn {
         p[j] = fma2(make_float2(p[j].y, p[j].x), s[j], mul2(p[j], c[j]));
         q[j] = fma2(make_float2(q[j].y, q[j].x), s[V / 2 + j], mul2(q[j], c[V / 2 + j]));
       } else {
-        const float2 t = mul2(q[j], s[j]), u = mul2(p[j], c[j]);
-        q[j] = fma2(p[j], s[j], mul2(q[j], c[j]));
-        p[j] = make_float2(u.x - t.x, u.y - t.y);
+        const float2 t = mul2(p[j], s[j]), u = mul2(q[j], c[j]);
+        p[j] = fma2(q[j], s[j], mul2(p[j], c[j]));
+        q[j] = make_float2(u.x - t.x, u.y - t.y);
       }
     }
   }
@@ -124,15 +174,31 @@ __device__ __forceinline__ void pack_store(const float2 (&p)[V / 2], T *to) {
   v.set(f);
   v.store(to);
 }
-template <int V>
-__device__ __forceinline__ void weigh(const Args &a, const float *weight, float2 (&p)[V / 2]) {
-#pragma unroll
-  for (int j = 0; j < V / 4; ++j) {
-    const float4 w = *reinterpret_cast<const float4 *>(weight + j * a.lanes * 4);
-    p[2 * j] = mul2(p[2 * j], make_float2(w.x, w.y));
-    p[2 * j + 1] = mul2(p[2 * j + 1], make_float2(w.z, w.w));
+// A thread's own ring in shared memory: AHEAD stages of K accesses of V values, filled by asynchronous copies some heads ahead.
+// A thread reads only what it copied, so the ring needs no barrier.  (What is on its way would fill the registers otherwise:
+// with the next two or three heads in registers the forward pass took 22.6 and 21.5 us at 16 x 1024, 12 + 12 heads of 64.)
+template <typename T, int V, int K, int AHEAD>
+struct Ring {
+  static constexpr int kBytes = V * sizeof(T);
+  static constexpr size_t kSize = (size_t)AHEAD * K * kThreads * kBytes;
+  uint32_t base;
+  __device__ __forceinline__ explicit Ring(void *smem) : base(smem_u32(smem) + threadIdx.x * kBytes) {}
+  __device__ __forceinline__ void copy(int stage, int k, const T *from) {
+    const uint32_t to = base + (stage * K + k) * (kThreads * kBytes);
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
   }
-}
+  __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  // all but the last AHEAD - 1 commits have arrived
+  __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory"); }
+  __device__ __forceinline__ void read(int stage, int k, CdgVec<T, V> &v) const {
+    const uint32_t at = base + (stage * K + k) * (kThreads * kBytes);
+    if constexpr (kBytes == 16)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(at) : "memory");
+    else
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "r"(at) : "memory");
+  }
+};
 
 // sum over a head's lanes
 __device__ __forceinline__ float head_sum(float v, int group) {
@@ -142,90 +208,97 @@ __device__ __forceinline__ float head_sum(float v, int group) {
   return v;
 }
 
+// two at once
+__device__ __forceinline__ float2 head_sums(float2 v, int group) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < group) v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+  return v;
+}
+
 __device__ __forceinline__ long long position(const Args &a, uint32_t b, uint32_t t) {
   if (!a.pos) return t;
   const long long at = b * a.pos_stride + t;
   return a.pos_bits == 64 ? static_cast<const long long *>(a.pos)[at] : static_cast<const int *>(a.pos)[at];
 }
 
+// the first q_blocks blocks take queries, the others keys
 template <typename T, int V, bool NEAR>
-__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t items, const __grid_constant__ Args a,
+__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t tokens, uint32_t q_blocks, const __grid_constant__ Args a,
                                                                   const __grid_constant__ Frequencies f) {
-  constexpr int U = 2;                     // heads at a time
+  extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
+  const int key = blockIdx.x >= q_blocks;
+  const Side &z = a.side[key];
   const int group = a.group, lane = threadIdx.x & (group - 1);
   const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
+  const float inv = 1.0f / (float)a.dim;
+  const uint32_t item = (blockIdx.x - (key ? q_blocks : 0)) * (kThreads / group) + threadIdx.x / group;
+  const bool some = item < tokens * a.parts[key].d;
+  const uint32_t tok = some ? cdg_divide(item, a.parts[key]) : 0, share = item - tok * a.parts[key].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
+  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, count = some && mine ? (z.heads - (int)share + parts - 1) / parts : 0;
+  const bool live = count > 0 && (!a.lens || (int)t < a.lens[b]);
+  const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
+  T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
+  const long long x_step = parts * z.xs[2], y_step = parts * z.ys[2];
+  Ring<T, V, 2, kAhead> ring(dyn);
+  auto request = [&](int h, int stage) {
+    if (live && h < count) {
+      ring.copy(stage, 0, x + at.x);
+      ring.copy(stage, 1, x + at.y);
+    }
+    ring.commit();
+    x += x_step;
+  };
+#pragma unroll
+  for (int h = 0; h < kAhead - 1; ++h) request(h, h);
   load_shared<V, NEAR>(a, f, s);
   __syncthreads();
-  const uint32_t item = blockIdx.x * (kThreads / group) + threadIdx.x / group;
-  const bool some = item < items;
-  const uint32_t tok = some ? cdg_divide(item, a.parts[0]) : 0, part = item - tok * a.parts[0].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-  const int heads = a.side[0].heads + a.side[1].heads, per = (heads + a.parts[0].d - 1) / a.parts[0].d;
-  const int h0 = part * per, h1 = some ? min(heads, h0 + per) : h0;
-  const bool live = some && mine && (!a.lens || (int)t < a.lens[b]);
   Turn<V, NEAR> turn;
-  turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, false);
-  const T *x[2];
-  T *y[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const Side &z = a.side[k];
-    const int back = k ? a.side[0].heads : 0;            // the head index counts queries first
-    x[k] = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] - back * z.xs[2];
-    y[k] = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] - back * z.ys[2];
-  }
-  for (int i = 0; i < per; i += U) {                      // (the same number for every group of a warp)
-    CdgVec<T, V> va[U], vb[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + i + u, k = h >= a.side[0].heads;
-      va[u].zero();
-      vb[u].zero();
-      if (live && h < h1) {
-        const T *from = (k ? x[1] : x[0]) + h * (k ? a.side[1].xs[2] : a.side[0].xs[2]);
-        va[u].load(from + at.x);
-        vb[u].load(from + at.y);
-      }
+  turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, s.weight[key][0] + (mine ? lane * 4 : 0), s.weight[key][1] + (mine ? lane * 4 : 0));
+  for (int h = 0, stage = 0; h < per; ++h, stage = stage + 1 == kAhead ? 0 : stage + 1) {      // (as often for every group)
+    request(h + kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
+    ring.wait();
+    CdgVec<T, V> va, vb;
+    va.zero();
+    vb.zero();
+    if (live && h < count) {
+      ring.read(stage, 0, va);
+      ring.read(stage, 1, vb);
     }
+    float2 p[V / 2], q[V / 2], sum = make_float2(0.0f, 0.0f);
+    unpack(va, p);
+    unpack(vb, q);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + i + u, k = h >= a.side[0].heads;
-      float2 p[V / 2], q[V / 2], sum = make_float2(0.0f, 0.0f);
-      unpack(va[u], p);
-      unpack(vb[u], q);
+    for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+    const float total = head_sum(sum.x + sum.y, group);
+    if (h >= count) continue;
+    // (0 where there is nothing: with eps = 0 it would be infinite)
+    const float rstd = live ? rsqrtf(total * inv + a.eps) : 0.0f;
 #pragma unroll
-      for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
-      const float total = head_sum(sum.x + sum.y, group);
-      if (h >= h1 || !mine) continue;
-      // (0 where there is nothing: with eps = 0 it would be infinite)
-      const float rstd = live ? 1.0f / sqrtf(total / (float)a.dim + a.eps) : 0.0f;
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        p[j] = mul2(p[j], make_float2(rstd, rstd));
-        q[j] = mul2(q[j], make_float2(rstd, rstd));
-      }
-      weigh<V>(a, s.weight[k][0] + lane * 4, p);
-      weigh<V>(a, s.weight[k][1] + lane * 4, q);
-      turn.apply(p, q);
-      T *to = (k ? y[1] : y[0]) + h * (k ? a.side[1].ys[2] : a.side[0].ys[2]);
-      pack_store<T, V>(p, to + at.x);
-      pack_store<T, V>(q, to + at.y);
+    for (int j = 0; j < V / 2; ++j) {
+      p[j] = mul2(p[j], make_float2(rstd, rstd));
+      q[j] = mul2(q[j], make_float2(rstd, rstd));
     }
+    turn.apply(p, q);
+    pack_store<T, V>(p, y + at.x);
+    pack_store<T, V>(q, y + at.y);
+    y += y_step;
   }
 }
 
 // A block takes a chunk of one worker's (blockIdx.y) tokens, of its queries or of its keys, and keeps its sums of g' n in registers;
-// at the end they go to part[worker][chunk][dim], queries' chunks first.  The next head is requested before this one is worked on.
+// at the end they go to part[worker][chunk][dim], queries' chunks first.
 template <typename T, int V, bool NEAR>
 __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t tokens, int q_chunks, int k_chunks, const __grid_constant__ Args a,
                                                                       const __grid_constant__ Frequencies f, float *part) {
   __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
-  const int key = (int)blockIdx.x >= q_chunks, chunk = blockIdx.x - key * q_chunks, chunks = key ? k_chunks : q_chunks;
+  const int key = blockIdx.x >= (unsigned)q_chunks, chunk = blockIdx.x - key * q_chunks, chunks = key ? k_chunks : q_chunks;
   const Side &z = a.side[key];
   const int group = a.group, groups = kThreads / group, lane = threadIdx.x & (group - 1);
   const bool mine = lane < a.lanes;
@@ -233,70 +306,88 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t t
   const float inv = 1.0f / (float)a.dim;
   const uint32_t items = tokens * a.parts[key].d, rounds = (items + groups - 1) / groups;           // each group an item
   const uint32_t r0 = (uint32_t)((unsigned long long)rounds * chunk / chunks), r1 = (uint32_t)((unsigned long long)rounds * (chunk + 1) / chunks);
-  const int per = (z.heads + a.parts[key].d - 1) / a.parts[key].d;
+  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts;
+  const long long x_step = parts * z.xs[2], dy_step = parts * z.dys[2], y_step = parts * z.ys[2];
+  extern __shared__ __align__(16) uint8_t dyn[];
+  Ring<T, V, 4, kAhead> ring(dyn);
   float2 wa[V / 2] = {}, wb[V / 2] = {};
   load_shared<V, NEAR>(a, f, s);
   __syncthreads();
-  const float *weight_a = s.weight[key][0] + lane * 4, *weight_b = s.weight[key][1] + lane * 4;
+  const float *weight_a = s.weight[key][0] + (mine ? lane * 4 : 0), *weight_b = s.weight[key][1] + (mine ? lane * 4 : 0);
   for (uint32_t r = r0; r < r1; ++r) {
     const uint32_t item = r * groups + threadIdx.x / group;
     const bool some = item < items;
     const uint32_t local = some ? cdg_divide(item, a.parts[key]) : 0, share = item - local * a.parts[key].d;
     const uint32_t tok = blockIdx.y * tokens + local, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-    const int h0 = share * per, count = some && mine ? min(z.heads - h0, per) : 0;
+    const int count = some && mine ? (z.heads - (int)share + parts - 1) / parts : 0;
     const bool live = some && mine && (!a.lens || (int)t < a.lens[b]);
-    const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + h0 * z.xs[2];
-    const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + h0 * z.dys[2];
-    T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + h0 * z.ys[2];
-    CdgVec<T, V> va, vb, da, db;
-    auto request = [&](int h) {
+    const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
+    const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + share * z.dys[2];
+    T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
+    auto request = [&](int h, int stage) {
       if (live && h < count) {
-        va.load(x + at.x); vb.load(x + at.y);
-        da.load(dy + at.x); db.load(dy + at.y);
-      } else {
-        va.zero(); vb.zero(); da.zero(); db.zero();
+        ring.copy(stage, 0, x + at.x);
+        ring.copy(stage, 1, x + at.y);
+        ring.copy(stage, 2, dy + at.x);
+        ring.copy(stage, 3, dy + at.y);
       }
-      x += z.xs[2];
-      dy += z.dys[2];
+      ring.commit();
+      x += x_step;
+      dy += dy_step;
     };
-    request(0);
-    Turn<V, NEAR> turn;
-    turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, true);
-    for (int h = 0; h < per; ++h) {
+#pragma unroll
+    for (int h = 0; h < kAhead - 1; ++h) request(h, h);
+    TurnBack<V, NEAR> turn;
+    turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0);
+    for (int h = 0, stage = 0; h < per; ++h, stage = stage + 1 == kAhead ? 0 : stage + 1) {
+      request(h + kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
+      ring.wait();
       float2 p[V / 2], q[V / 2], g[V / 2], e[V / 2], sum = make_float2(0.0f, 0.0f);
+      CdgVec<T, V> va, vb, da, db;
+      va.zero(); vb.zero(); da.zero(); db.zero();
+      if (live && h < count) {
+        ring.read(stage, 0, va);
+        ring.read(stage, 1, vb);
+        ring.read(stage, 2, da);
+        ring.read(stage, 3, db);
+      }
       unpack(va, p); unpack(vb, q);
       unpack(da, g); unpack(db, e);
-      request(h + 1);
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
-      const float total = head_sum(sum.x + sum.y, group);
+      // with x = n / rstd: both sums before rstd is known
       turn.apply(g, e);
-      // (0 where there is nothing: with eps = 0 it would be infinite)
-      const float rstd = live && h < count ? 1.0f / sqrtf(total * inv + a.eps) : 0.0f;
+      float2 along = make_float2(0.0f, 0.0f), ga[V / 2], gb[V / 2];
 #pragma unroll
       for (int j = 0; j < V / 2; ++j) {
-        p[j] = mul2(p[j], make_float2(rstd, rstd));
-        q[j] = mul2(q[j], make_float2(rstd, rstd));
-        wa[j] = fma2(g[j], p[j], wa[j]);
-        wb[j] = fma2(e[j], q[j], wb[j]);
+        sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+        ga[j] = mul2(g[j], p[j]);
+        gb[j] = mul2(e[j], q[j]);
       }
-      if (mine) {
-        weigh<V>(a, weight_a, g);
-        weigh<V>(a, weight_b, e);
-      }
-      sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-      for (int j = 0; j < V / 2; ++j) sum = fma2(g[j], p[j], fma2(e[j], q[j], sum));
-      const float hn = -head_sum(sum.x + sum.y, group) * inv;
-      if (h < count) {
+      for (int j = 0; j < V / 4; ++j) {
+        const float4 u = *reinterpret_cast<const float4 *>(weight_a + j * a.lanes * 4), v = *reinterpret_cast<const float4 *>(weight_b + j * a.lanes * 4);
+        const float2 w[4] = {make_float2(u.x, u.y), make_float2(u.z, u.w), make_float2(v.x, v.y), make_float2(v.z, v.w)};
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-          p[j] = mul2(fma2(p[j], make_float2(hn, hn), g[j]), make_float2(rstd, rstd));
-          q[j] = mul2(fma2(q[j], make_float2(hn, hn), e[j]), make_float2(rstd, rstd));
+        for (int i = 0; i < 2; ++i) {
+          along = fma2(ga[2 * j + i], w[i], fma2(gb[2 * j + i], w[2 + i], along));
+          g[2 * j + i] = mul2(g[2 * j + i], w[i]);
+          e[2 * j + i] = mul2(e[2 * j + i], w[2 + i]);
         }
+      }
+      const float2 both = head_sums(make_float2(sum.x + sum.y, along.x + along.y), group);
+      // (0 where there is nothing: with eps = 0 it would be infinite)
+      const float rstd = live && h < count ? rsqrtf(both.x * inv + a.eps) : 0.0f;
+      const float off = -(both.y * inv * rstd * rstd) * rstd;
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        wa[j] = fma2(ga[j], make_float2(rstd, rstd), wa[j]);
+        wb[j] = fma2(gb[j], make_float2(rstd, rstd), wb[j]);
+        p[j] = fma2(p[j], make_float2(off, off), mul2(g[j], make_float2(rstd, rstd)));
+        q[j] = fma2(q[j], make_float2(off, off), mul2(e[j], make_float2(rstd, rstd)));
+      }
+      if (h < count) {
         pack_store<T, V>(p, y + at.x);
         pack_store<T, V>(q, y + at.y);
-        y += z.ys[2];
+        y += y_step;
       }
     }
   }
@@ -326,12 +417,13 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t t
   }
 }
 
-// the chunks' sums of one worker (blockIdx.y) added up in order, of queries (blockIdx.z = 0) or keys: 32 columns to a block, eight
+// the chunks' sums of one worker (blockIdx.y) added up in order, of queries (blockIdx.z = 0) or keys: 32 columns to a block, 32
 // threads to a column
+constexpr int kJoinThreads = 1024, kJoinWarps = 32;
 template <typename G>
-__global__ void __launch_bounds__(kThreads) rotary_join_kernel(int q_chunks, int k_chunks, int dim, const float *__restrict__ part, G *dqw, G *dkw,
+__global__ void __launch_bounds__(kJoinThreads) rotary_join_kernel(int q_chunks, int k_chunks, int dim, const float *__restrict__ part, G *dqw, G *dkw,
                                                                long long ws) {
-  __shared__ float sm[kWarps][33];
+  __shared__ float sm[kJoinWarps][33];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), k0 = threadIdx.x >> 5, key = blockIdx.z;
@@ -342,11 +434,11 @@ __global__ void __launch_bounds__(kThreads) rotary_join_kernel(int q_chunks, int
   float t = 0.0f;
   if (c < dim)
 #pragma unroll 8
-    for (int k = k0; k < chunks; k += kWarps) t += part[(long long)k * dim + c];
+    for (int k = k0; k < chunks; k += kJoinWarps) t += part[(long long)k * dim + c];
   sm[k0][threadIdx.x & 31] = t;
   __syncthreads();
   if (k0 == 0 && c < dim) {
-    for (int k = 1; k < kWarps; ++k) t += sm[k][threadIdx.x];
+    for (int k = 1; k < kJoinWarps; ++k) t += sm[k][threadIdx.x];
     out[(long long)blockIdx.y * ws + c] = cdg_cast<G>(t);
   }
 }
@@ -376,22 +468,24 @@ int group_of(const cdgrab_rotary_shape *s) {
   while (group < lanes_of(s)) group *= 2;
   return group;
 }
-// Shares that each token's heads are dealt out in: one where the tokens fill the SMs, up to a share for every two heads where
-// there are few (each share computes the token's angles again).
+// Shares that each token's heads are dealt out in, one by one, so that neighbouring groups read neighbouring heads: as many as fill
+// five blocks to an SM, a share for every two heads at most; each share computes the token's angles again.  (16 x 1024, 12 + 12 heads
+// of 64, in one share 21.5 us, in two 20.5, in three 23.3; 4 x 4096, 16 + 4 heads of 128, backward in one 49, in two 55.)
 constexpr int kSms = 148;
 int parts_of(const cdgrab_rotary_shape *s, int heads) {
-  const long long tokens = (long long)s->batch * s->len, fill = 2ll * kSms * (kThreads / group_of(s));
+  const long long tokens = (long long)s->batch * s->len, fill = 5ll * kSms * (kThreads / group_of(s));
   const long long most = (heads + 1) / 2, want = tokens > 0 ? fill / tokens : 1, parts = want < most ? want : most;
   if (parts <= 1) return 1;
   const long long per = (heads + parts - 1) / parts;
   return (int)((heads + per - 1) / per);
 }
-// Chunks of a worker's queries or keys: 32,768 values to a block, an item to each group of lanes at least, about four rounds of the
-// blocks that are resident at once (two to an SM) at most.
+// Chunks of a worker's queries or keys: 16,384 values to a block, an item to each group of lanes at least, about four rounds of the
+// blocks that are resident at once (two to an SM) at most.  (4 x 4096, 16 + 4 heads of 128: 48 us, with 65,536 values 55.)
+constexpr int kChunk = 16384;
 int chunks_of(const cdgrab_rotary_shape *s, int m, int heads) {
   const long long tokens = (long long)s->batch / m * s->len, groups = kThreads / group_of(s);
   if (tokens == 0 || heads == 0) return 1;
-  const long long rounds = (tokens * parts_of(s, heads) + groups - 1) / groups, work = (tokens * heads * s->head_dim + 32767) / 32768;
+  const long long rounds = (tokens * parts_of(s, heads) + groups - 1) / groups, work = (tokens * heads * s->head_dim + kChunk - 1) / kChunk;
   const long long most = 8ll * kSms / m, c = rounds < work ? rounds : work;
   return (int)(c < most ? c : most < 1 ? 1 : most);
 }
@@ -411,8 +505,10 @@ void fill(const cdgrab_rotary_shape *s, Args &a, Frequencies &f) {
   // (a power for each pair costs more than the launch: each thread keeps its last table)
   static thread_local struct { double base; int rot; Frequencies f; } last = {};
   if (last.base != s->base || last.rot != s->rotary_dim) {
-    for (int i = 0; i < kMaxPairs; ++i)
-      last.f.turns[i] = 2 * i < s->rotary_dim ? std::pow(s->base, -2.0 * i / s->rotary_dim) / (2.0 * M_PI) : 0.0;
+    for (int i = 0; i < kMaxPairs; ++i) {
+      long double whole, turns = 2 * i < s->rotary_dim ? std::pow((long double)s->base, -2.0L * i / s->rotary_dim) / (2.0L * kPi) : 0.0L;
+      last.f.turns[i] = (unsigned long long)(std::modf(turns, &whole) * 0x1p64L);
+    }
     last.base = s->base;
     last.rot = s->rotary_dim;
   }
@@ -459,14 +555,23 @@ extern "C" int cdgrab_rotary_forward(const cdgrab_rotary_shape *s, const void *q
   if (const int rc = cdg_ops_device(&dev)) return rc;
   Frequencies f;
   fill(s, a, f);
-  a.parts[0] = cdg_divisor(parts_of(s, s->heads + s->kv_heads));
-  const long long items = (long long)s->batch * s->len * a.parts[0].d;
-  if (items >= (1ll << 31)) return CDGRAB_ERR_INVALID;
+  const long long tokens = (long long)s->batch * s->len;
   const int groups = kThreads / a.group;
-  const dim3 grid((unsigned)((items + groups - 1) / groups));
+  unsigned blocks[2];
+  for (int i = 0; i < 2; ++i) {
+    const int heads = i ? s->kv_heads : s->heads;
+    a.parts[i] = cdg_divisor(parts_of(s, heads));
+    blocks[i] = heads ? (unsigned)((tokens * a.parts[i].d + groups - 1) / groups) : 0;
+  }
+  const dim3 grid(blocks[0] + blocks[1]);
   cudaStream_t st = (cudaStream_t)stream;
   return by_kind(s, [&](auto t, auto v, auto near) {
-    return cdg_launch_rc(cdg_ops_launch(rotary_forward_kernel<decltype(t), v(), near()>, grid, kThreads, 0, st, (uint32_t)items, a, f));
+    using T = decltype(t);
+    static CdgPerDevice flags;
+    constexpr size_t smem = Ring<T, v(), 2, kAhead>::kSize;
+    const cudaError_t e = cdg_raise_smem_limit(flags, dev->index, rotary_forward_kernel<T, v(), near()>, smem);
+    return e != cudaSuccess ? cdg_launch_rc(e) : cdg_launch_rc(cdg_ops_launch(rotary_forward_kernel<T, v(), near()>, grid, kThreads, smem, st,
+                                                                              (uint32_t)tokens, blocks[0], a, f));
   });
 }
 
@@ -500,13 +605,17 @@ extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const
   cudaStream_t st = (cudaStream_t)stream;
   float *part = dqw || dkw ? static_cast<float *>(workspace) : nullptr;
   const int rc = by_kind(s, [&](auto t, auto v, auto near) {
-    return cdg_launch_rc(cdg_ops_launch(rotary_backward_kernel<decltype(t), v(), near()>, dim3(qc + kc, m), kThreads, 0, st, (uint32_t)tokens, qc,
-                                        kc, a, f, part));
+    using T = decltype(t);
+    static CdgPerDevice flags;
+    constexpr size_t smem = Ring<T, v(), 4, kAhead>::kSize;
+    const cudaError_t e = cdg_raise_smem_limit(flags, dev->index, rotary_backward_kernel<T, v(), near()>, smem);
+    return e != cudaSuccess ? cdg_launch_rc(e) : cdg_launch_rc(cdg_ops_launch(rotary_backward_kernel<T, v(), near()>, dim3(qc + kc, m), kThreads,
+                                                                              smem, st, (uint32_t)tokens, qc, kc, a, f, part));
   });
   if (rc != CDGRAB_OK || !part) return rc;
   const dim3 grid((s->head_dim + 31) / 32, m, 2);
   return cdg_launch_rc(grad_dtype == CDGRAB_F32
-                           ? cdg_ops_launch(rotary_join_kernel<float>, grid, kThreads, 0, st, qc, kc, s->head_dim, part, (float *)dqw, (float *)dkw, worker_stride)
-                           : cdg_ops_launch(rotary_join_kernel<__nv_bfloat16>, grid, kThreads, 0, st, qc, kc, s->head_dim, part,
+                           ? cdg_ops_launch(rotary_join_kernel<float>, grid, kJoinThreads, 0, st, qc, kc, s->head_dim, part, (float *)dqw, (float *)dkw, worker_stride)
+                           : cdg_ops_launch(rotary_join_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, st, qc, kc, s->head_dim, part,
                                             (__nv_bfloat16 *)dqw, (__nv_bfloat16 *)dkw, worker_stride));
 }
