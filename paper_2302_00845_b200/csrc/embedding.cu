@@ -13,6 +13,9 @@
 #include "rows.cuh"
 #include "tensor_core.cuh"
 
+#ifndef AH
+#define AH 8
+#endif
 namespace {
 
 constexpr int kThreads = 256;
@@ -74,16 +77,20 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(uint32_t rows, int per
 
 // ---- gradient, step 1: sorted tokens, cleared tables -------------------------------------------------------
 // A cluster sorts a worker's n tokens by a stable radix sort, digits of up to 8 bits, least first: the shortest form whose
-// result does not depend on timing.  Each CTA of the cluster owns a contiguous share of the positions.  In a pass it counts its
-// share's digits, learns the other CTAs' counts through distributed shared memory, and moves its items to their places, tile by
-// tile: a warp ranks its items by matching digits among its lanes, the warps' counts are added up in order.  Items are (token,
-// row) pairs in two buffers that stay in L2.  Tokens without a gradient sort behind the vocabulary.
-// (16 workers x 1024 tokens of 50,257: the sort alone takes 11 us, hidden behind 1.2 GB of zeros.)
+// result does not depend on timing.  Each CTA of the cluster owns a contiguous share of the positions.  In a pass a warp ranks its
+// items by matching digits among its lanes, the warps' counts are added up in order, the CTAs learn one another's counts through
+// distributed shared memory, and the items move to their places.  A share of up to 4096 items is held in registers during a pass;
+// of a longer one the digits are counted first, then it goes tile by tile.  Items are (token, row) pairs in two buffers that stay
+// in L2.  Tokens without a gradient sort behind the vocabulary.
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kBins = 256;
-constexpr int kRounds = 4;             // items to a thread in a tile, at most
+constexpr int kRounds = 8;             // items to a thread in a tile, at most
 constexpr int kTile = kSortThreads * kRounds;
+#ifndef KSH
+#define KSH 1024
+#endif
+constexpr long long kShare = KSH;     // items to a CTA while more CTAs can be had
 
 struct Sort {
   Tokens tok;
@@ -117,30 +124,92 @@ __device__ __forceinline__ uint2 first_item(const Sort &s, long long w, uint32_t
 __device__ void sort_worker(const Sort &s, long long w, uint32_t rank, uint32_t ctas) {
   __shared__ uint32_t hist[kBins];                       // this CTA's digits in the pass
   __shared__ uint32_t place[kBins];                      // where the next item of a digit goes
-  __shared__ uint32_t count[kSortWarps][kBins + 1];      // of a tile, by warp
+  __shared__ uint32_t count[kSortWarps][kBins + 1];      // of a tile, by warp; then of the warps before
   __shared__ uint32_t part[kBins / 32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << s.bits;
   const uint32_t share = (s.n + ctas - 1) / ctas, begin = min((uint32_t)s.n, rank * share), end = min((uint32_t)s.n, begin + share);
-  const uint32_t mask = (1u << s.bits) - 1;
+  const uint32_t mask = bins - 1;
+  const bool single = share <= (uint32_t)kTile;
   for (int pass = 0; pass < s.passes; ++pass) {
     const uint2 *from = ((s.passes - pass) & 1 ? s.other : s.items) + w * s.n;
     uint2 *to = ((s.passes - pass) & 1 ? s.items : s.other) + w * s.n;
     const int shift = pass * s.bits;
-    auto item = [&](uint32_t i) { return pass == 0 ? first_item(s, w, i) : __ldcg(from + i); };
-    // the share's digits
-    for (int d = tid; d < kBins; d += kSortThreads) hist[d] = 0;
-    __syncthreads();
-    for (uint32_t i0 = begin + warp * 32; i0 < end; i0 += kSortThreads) {
-      const uint32_t i = i0 + lane;
-      const uint32_t d = i < end ? item(i).x >> shift & mask : kBins;
-      const uint32_t same = __match_any_sync(0xffffffffu, d);
-      if (d < kBins && lane == __ffs(same) - 1) atomicAdd(&hist[d], __popc(same));
+    uint2 it[kRounds];
+    uint32_t at[kRounds];
+    int rounds = 0;
+    uint32_t mine = 0;                                   // this thread's first item
+    // items from i0 on, 32 to a warp and round
+    auto load = [&](uint32_t t0) {
+      const uint32_t left = end - t0;
+      rounds = left >= (uint32_t)kTile ? kRounds : (int)((left + kSortThreads - 1) / kSortThreads);
+      mine = t0 + warp * rounds * 32 + lane;
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r) {
+        const uint32_t i = mine + r * 32;
+        if (r < rounds && i < end) it[r] = pass == 0 ? first_item(s, w, i) : __ldcg(from + i);
+      }
+    };
+    // each item's rank in its warp, counts of the warps before in count, the tile's digits in total (of thread d for digit d)
+    auto rank_tile = [&]() {
+      for (int d = lane; d < bins; d += 32) count[warp][d] = 0;
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r) {
+        if (r >= rounds) break;
+        const uint32_t d = mine + r * 32 < end ? it[r].x >> shift & mask : kBins;
+        const uint32_t same = __match_any_sync(0xffffffffu, d);
+        at[r] = 0;
+        if (d < kBins) at[r] = count[warp][d] + __popc(same & ((1u << lane) - 1));
+        __syncwarp();
+        if (d < kBins && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
+        __syncwarp();
+      }
+      __syncthreads();
+      uint32_t total = 0;
+      if (tid < bins) {
+        uint32_t c[kSortWarps];
+#pragma unroll
+        for (int k = 0; k < kSortWarps; ++k) c[k] = count[k][tid];
+#pragma unroll
+        for (int k = 0; k < kSortWarps; ++k) {
+          count[k][tid] = total;
+          total += c[k];
+        }
+      }
+      return total;
+    };
+    auto scatter = [&]() {
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r)
+        if (r < rounds && mine + r * 32 < end) {
+          const uint32_t d = it[r].x >> shift & mask;
+          to[place[d] + count[warp][d] + at[r]] = it[r];
+        }
+    };
+    uint32_t digits = 0;
+    if (single) {
+      load(begin);
+      digits = rank_tile();
+      if (tid < bins) hist[tid] = digits;
+    } else {
+      for (int d = tid; d < bins; d += kSortThreads) hist[d] = 0;
+      __syncthreads();
+      for (uint32_t t0 = begin; t0 < end; t0 += kTile) {
+        load(t0);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+          if (r >= rounds) break;
+          const uint32_t d = mine + r * 32 < end ? it[r].x >> shift & mask : kBins;
+          const uint32_t same = __match_any_sync(0xffffffffu, d);
+          if (d < kBins && lane == __ffs(same) - 1) atomicAdd(&hist[d], __popc(same));
+        }
+      }
     }
     __syncthreads();
     if (ctas > 1) tc_cluster_sync();
     // a digit's first place: all items of lower digits, and this digit's of the CTAs before
     uint32_t total = 0, before = 0;
-    if (tid < kBins) {
+    if (tid < bins) {
       if (ctas > 1) {
         for (uint32_t c = 0; c < ctas; ++c) {
           const uint32_t h = cluster_read(&hist[tid], c);
@@ -161,56 +230,23 @@ __device__ void sort_worker(const Sort &s, long long w, uint32_t rank, uint32_t 
       if (lane == 31) part[warp] = sum;
     }
     __syncthreads();
-    if (tid < kBins) {
+    if (tid < bins) {
       uint32_t lower = sum - total + before;
       for (int k = 0; k < warp; ++k) lower += part[k];
       place[tid] = lower;
     }
-    // tile by tile: ranks within the tile, then to the items' places
-    for (uint32_t t0 = begin; t0 < end; t0 += kTile) {
-      const uint32_t left = end - t0;
-      const int rounds = left >= (uint32_t)kTile ? kRounds : (int)((left + kSortThreads - 1) / kSortThreads);
-      const uint32_t w0 = t0 + warp * rounds * 32 + lane;
-      for (int d = lane; d < kBins; d += 32) count[warp][d] = 0;
-      __syncwarp();
-      uint2 it[kRounds];
-      uint32_t at[kRounds];
-#pragma unroll
-      for (int r = 0; r < kRounds; ++r) {
-        const uint32_t i = w0 + r * 32;
-        if (r < rounds && i < end) it[r] = item(i);
+    __syncthreads();
+    if (single) {
+      scatter();
+    } else {
+      for (uint32_t t0 = begin; t0 < end; t0 += kTile) {
+        load(t0);
+        digits = rank_tile();
+        __syncthreads();
+        scatter();
+        __syncthreads();
+        if (tid < bins) place[tid] += digits;
       }
-#pragma unroll
-      for (int r = 0; r < kRounds; ++r) {
-        if (r >= rounds) break;
-        const uint32_t d = w0 + r * 32 < end ? it[r].x >> shift & mask : kBins;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        at[r] = 0;
-        if (d < kBins) at[r] = count[warp][d] + __popc(same & ((1u << lane) - 1));
-        __syncwarp();
-        if (d < kBins && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
-        __syncwarp();
-      }
-      __syncthreads();
-      // counts of the warps before, a warp to each sixteenth digit, its lanes over the warps
-      for (int d = warp; d < kBins; d += kSortWarps) {
-        const uint32_t c = lane < kSortWarps ? count[lane][d] : 0;
-        uint32_t run = c;
-#pragma unroll
-        for (int o = 1; o < kSortWarps; o <<= 1) {
-          const uint32_t v = __shfl_up_sync(0xffffffffu, run, o);
-          if (lane >= o) run += v;
-        }
-        const uint32_t p = place[d];
-        if (lane < kSortWarps) count[lane][d] = p + run - c;
-        __syncwarp();
-        if (lane == kSortWarps - 1) place[d] = p + run;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int r = 0; r < kRounds; ++r)
-        if (r < rounds && w0 + r * 32 < end) to[count[warp][it[r].x >> shift & mask] + at[r]] = it[r];
-      __syncthreads();
     }
     __syncthreads();
     if (ctas > 1) tc_cluster_sync();
@@ -235,7 +271,10 @@ __device__ __forceinline__ void clear_span(uint8_t *p, long long bytes, int elem
   if (i < tail) *reinterpret_cast<uint16_t *>(p + lead + body + i) = 0;
 }
 
-__global__ void __launch_bounds__(kSortThreads) sort_and_clear_kernel(const __grid_constant__ Sort s, const __grid_constant__ Clear z,
+#ifndef SMB
+#define SMB 2
+#endif
+__global__ void __launch_bounds__(kSortThreads, SMB) sort_and_clear_kernel(const __grid_constant__ Sort s, const __grid_constant__ Clear z,
                                                                       unsigned sorting) {
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
@@ -277,7 +316,7 @@ constexpr int kSlab = 256;             // columns to a warp, eight to a lane
 
 template <typename T, typename G, int VEC>
 __global__ void __launch_bounds__(kThreads) run_sums_kernel(const __grid_constant__ Sums a, long long all) {
-  constexpr int NV = 8 / VEC, kAhead = 4;
+  constexpr int NV = 8 / VEC, kAhead = AH;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int lane = threadIdx.x & 31;
@@ -438,8 +477,9 @@ extern "C" int cdgrab_embedding_forward(long long groups, long long length, int 
   const Tokens tok = {tokens, token_bits, token_stride, length, padding, vocab};
   const int vec = cdg_widest(cols, {{table, vocab > 1 ? table_stride : 0, e}, {y, rows > 1 ? y_stride : 0, oe}});
   const int per_row = cols / vec;
+  // four accesses to a lane, but eight lanes where a row has work for them
   int group = 1;
-  while (group < 32 && group < per_row) group *= 2;
+  while (group < 32 && (4 * group < per_row || (group < 8 && group < per_row))) group *= 2;
   const long long blocks = (rows + kThreads / group - 1) / (kThreads / group);
   cudaStream_t st = (cudaStream_t)stream;
   return cdg_by_types(dtype, out_dtype, [&](auto t, auto r) {
@@ -496,9 +536,9 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
   s.items = static_cast<uint2 *>(workspace);
   s.other = reinterpret_cast<uint2 *>(static_cast<uint8_t *>(workspace) + up16(8 * m * n));
   s.status = dev->status;
-  // a CTA for each two tiles of a worker's tokens, up to eight, while there are SMs for them
+  // a CTA for every kShare of a worker's tokens, up to eight, while there are SMs for them
   int ctas = 1;
-  while (ctas < 8 && n > 2ll * kTile * ctas && 2ll * ctas * m <= dev->sms) ctas *= 2;
+  while (ctas < 8 && n > kShare * ctas && 2ll * ctas * m <= dev->sms) ctas *= 2;
   const unsigned sorting = n > 0 ? (unsigned)(m * ctas) : 0;
   Clear z = {};
   if (!accumulate) {
