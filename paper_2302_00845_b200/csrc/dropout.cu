@@ -58,10 +58,12 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(long long n, long lon
 #pragma unroll
   for (int u = 0; u < kBlocks; ++u) {
     const long long b = base + threadIdx.x + u * kThreads;
+    const bool some = FLAT ? b * 8 + 8 <= n : b < blocks;
     vx[u].zero();
-    if (FLAT ? b * 8 + 8 <= n : b < blocks) {
-      if (x) vx[u].load(x + place(u, xs));
-      if (RES) vr[u].load(res + place(u, rs));
+    vx[u].load_if(some && x, x + place(u, xs));
+    if (RES) {
+      vr[u].zero();
+      vr[u].load_if(some, res + place(u, rs));
     }
   }
 #pragma unroll

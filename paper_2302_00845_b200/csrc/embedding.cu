@@ -5,7 +5,7 @@
 // The lookup is bound by memory: a row read (from L2 where tokens repeat) and a row written.  The gradient writes every row of
 // every worker's table, most of them zero, and reads dy once.  It runs in three launches:
 //   1. each worker's tokens are sorted by value, stably, by a cluster of its own, while the other blocks clear the tables;
-//   2. runs of equal tokens are summed in the order of their positions, a warp to 32 sorted positions and 256 columns;
+//   2. runs of equal tokens are summed in the order of their positions, a warp to 16 sorted positions and up to 256 columns;
 //   3. runs that go on over more than two such windows, which step 2 leaves as a sum for each window, are joined in order.
 // No sum depends on the order in which blocks run, and nothing is added to memory by atomics.
 #include <cmath>
@@ -13,9 +13,6 @@
 #include "rows.cuh"
 #include "tensor_core.cuh"
 
-#ifndef AH
-#define AH 8
-#endif
 namespace {
 
 constexpr int kThreads = 256;
@@ -59,7 +56,7 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(uint32_t rows, int per
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       v[u].zero();
-      if (valid && c + u * group < per_row) v[u].load(from + u * step);
+      v[u].load_if(valid && c + u * group < per_row, from + u * step);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -75,6 +72,55 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(uint32_t rows, int per
   }
 }
 
+// Rows that are no whole number of 8-value accesses, into a contiguous y: a thread takes eight adjacent values of y, in one row or
+// two (rows have eight at least), read LV at a time and stored at once.  (33 x 3773 rows of 37 bf16: 6.6 us, row by row 25.)
+template <typename T, typename R, int LV>
+__global__ void __launch_bounds__(kThreads) lookup_flat_kernel(uint32_t rows, CdgDivisor cols, CdgDivisor length, Tokens tok, float scale,
+                                                               const T *__restrict__ table, long long ts, R *__restrict__ y, int *status) {
+  cdg_grid_dep_wait();
+  cdg_grid_dep_trigger();
+  const long long base = (long long)blockIdx.x * (kThreads * 8), first = base / cols.d;
+  const uint32_t off = (uint32_t)(base - first * cols.d) + threadIdx.x * 8, q = cdg_divide(off, cols), c = off - q * cols.d;
+  const long long r = first + q;
+  if (r >= rows) return;
+  // the row that the values start in, and the next
+  const T *from[2];
+  bool valid[2];
+  const int here = min(8u, cols.d - c), n = here < 8 && r + 1 >= rows ? here : 8;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    valid[k] = false;
+    if (k == 0 || here < n) {
+      const uint32_t row = (uint32_t)r + k, g = cdg_divide(row, length);
+      const long long t = tok.at(g, row - g * length.d);
+      valid[k] = tok.valid(t);
+      if (!valid[k] && t != tok.padding && (k == 1 || c == 0)) atomicOr(status, CDG_ST_INDEX);
+      from[k] = table + (valid[k] ? t * ts : 0) + (k ? -here : (int)c);
+    }
+  }
+  if (here == n) from[1] = from[0];
+  CdgVec<T, LV> v[8 / LV];
+#pragma unroll
+  for (int i = 0; i < 8 / LV; ++i) {
+    const bool second = i * LV >= here;
+    v[i].zero();
+    v[i].load_if(i * LV < n && (second ? valid[1] : valid[0]), (second ? from[1] : from[0]) + i * LV);
+  }
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = v[e / LV].get(e % LV) * scale;
+  R *to = y + base + threadIdx.x * 8;
+  if (n == 8) {
+    CdgVec<R, 8> o;
+    o.set(f);
+    o.store(to);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) to[e] = cdg_cast<R>(f[e]);
+  }
+}
+
 // ---- gradient, step 1: sorted tokens, cleared tables -------------------------------------------------------
 // A cluster sorts a worker's n tokens by a stable radix sort, digits of up to 8 bits, least first: the shortest form whose
 // result does not depend on timing.  Each CTA of the cluster owns a contiguous share of the positions.  In a pass a warp ranks its
@@ -87,10 +133,7 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kBins = 256;
 constexpr int kRounds = 8;             // items to a thread in a tile, at most
 constexpr int kTile = kSortThreads * kRounds;
-#ifndef KSH
-#define KSH 1024
-#endif
-constexpr long long kShare = KSH;     // items to a CTA while more CTAs can be had
+constexpr long long kShare = 1024;    // items to a CTA while more CTAs can be had
 
 struct Sort {
   Tokens tok;
@@ -271,10 +314,8 @@ __device__ __forceinline__ void clear_span(uint8_t *p, long long bytes, int elem
   if (i < tail) *reinterpret_cast<uint16_t *>(p + lead + body + i) = 0;
 }
 
-#ifndef SMB
-#define SMB 2
-#endif
-__global__ void __launch_bounds__(kSortThreads, SMB) sort_and_clear_kernel(const __grid_constant__ Sort s, const __grid_constant__ Clear z,
+// (two blocks to an SM, 64 registers: with one, 16 tables of 50,257 x 768 bf16 are cleared 6 % slower)
+__global__ void __launch_bounds__(kSortThreads, 2) sort_and_clear_kernel(const __grid_constant__ Sort s, const __grid_constant__ Clear z,
                                                                       unsigned sorting) {
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
@@ -296,9 +337,9 @@ __global__ void __launch_bounds__(kSortThreads, SMB) sort_and_clear_kernel(const
 }
 
 // ---- gradient, steps 2 and 3: sums over runs of equal tokens -----------------------------------------------
-// A window is 32 sorted positions.  A run that starts in window w and ends in it or in the next one belongs to w, which sums all of it.
-// A longer one is summed window by window: its part in the window it starts in goes to part[w][0], its parts in the windows it
-// goes on in to part[.][1].  Keys 33 positions back and 64 ahead tell which case it is, without a search.
+// A window is kWindow sorted positions.  A run that starts in window w and ends in it or in the next one belongs to w, which sums all
+// of it.  A longer one is summed window by window: its part in the window it starts in goes to part[w][0], its parts in the windows
+// it goes on in to part[.][1].  Keys kWindow + 1 positions back and 2 kWindow ahead tell which case it is, without a search.
 struct Sums {
   const uint2 *items;
   int n, windows, vocab, cols;
@@ -312,129 +353,141 @@ struct Sums {
 };
 
 constexpr uint32_t kNoKey = 0xffffffffu;
-constexpr int kSlab = 256;             // columns to a warp, eight to a lane
+constexpr int kWindow = 16;            // half a warp: its lanes hold a window and the next one
 
-template <typename T, typename G, int VEC>
+// a warp to a window and 32 VEC NV columns; kAhead rows are on their way together
+template <typename T, typename G, int VEC, int NV>
 __global__ void __launch_bounds__(kThreads) run_sums_kernel(const __grid_constant__ Sums a, long long all) {
-  constexpr int NV = 8 / VEC, kAhead = AH;
+  constexpr int kAhead = 8, kSlab = 32 * VEC * NV;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int lane = threadIdx.x & 31;
   const long long at = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);      // worker and window
   if (at >= all) return;
   const long long w = at / a.windows;
-  const int p0 = (int)(at - w * a.windows) * 32;
+  const int win = (int)(at - w * a.windows);
+  const long long p0 = (long long)win * kWindow;
   const uint2 *items = a.items + w * a.n;
   auto key = [&](long long p) { return p >= 0 && p < a.n ? items[p].x : kNoKey; };
-  uint2 e[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) e[k] = (long long)p0 + 32 * k + lane < a.n ? items[p0 + 32 * k + lane] : make_uint2(kNoKey, 0u);
-  const uint32_t back1 = key((long long)p0 - 1), back33 = key((long long)p0 - 33), ahead = key((long long)p0 + 64);
-  const uint32_t first = __shfl_sync(0xffffffffu, e[0].x, 0), last = __shfl_sync(0xffffffffu, e[0].x, 31);
-  const uint32_t next = __shfl_sync(0xffffffffu, e[1].x, 0);
+  const uint2 e = p0 + lane < a.n ? items[p0 + lane] : make_uint2(kNoKey, 0u);
+  const uint32_t back1 = key(p0 - 1), back2 = key(p0 - kWindow - 1), ahead = key(p0 + 2 * kWindow);
+  const uint32_t first = __shfl_sync(0xffffffffu, e.x, 0), last = __shfl_sync(0xffffffffu, e.x, kWindow - 1);
+  const uint32_t next = __shfl_sync(0xffffffffu, e.x, kWindow);
+  constexpr uint32_t here = (1u << kWindow) - 1;
   // tokens without a gradient are past the others, and what is past the end behind them
-  const int live = __popc(__ballot_sync(0xffffffffu, e[0].x < (uint32_t)a.vocab));
+  const int live = __popc(__ballot_sync(0xffffffffu, e.x < (uint32_t)a.vocab) & here);
   if (live == 0) return;
   const bool goes_on = first == back1;                                  // the first run began before
-  const bool head_long = goes_on && (first == back33 || first == next);
-  const int head = __popc(__ballot_sync(0xffffffffu, e[0].x == first)); // its positions here
-  const bool whole = head == 32 && goes_on;                             // nothing begins here
-  const bool tail_long = !whole && live == 32 && last == ahead;
-  int begin = goes_on && !head_long ? head : 0, end = live;
-  if (!whole && live == 32 && !tail_long) end += __popc(__ballot_sync(0xffffffffu, e[1].x == last));
+  const bool head_long = goes_on && (first == back2 || first == next);
+  const int head = __popc(__ballot_sync(0xffffffffu, e.x == first) & here);      // its positions here
+  const bool whole = head == kWindow && goes_on;                        // nothing begins here
+  const uint32_t lasts = __ballot_sync(0xffffffffu, e.x == last);
+  const bool tail_long = !whole && live == kWindow && last == ahead;
+  const int begin = goes_on && !head_long ? head : 0;
+  const int end = live + (!whole && live == kWindow && !tail_long ? __popc(lasts >> kWindow) : 0);
   if (begin >= end) return;
-  const long long rows = w * a.n;
+  // positions at which a run ends
+  const uint32_t after = __shfl_down_sync(0xffffffffu, e.x, 1);
+  const uint32_t ends = __ballot_sync(0xffffffffu, lane + 1 >= end || e.x != after);
   for (int c0 = blockIdx.y * kSlab; c0 < a.cols; c0 += gridDim.y * kSlab) {
     float acc[NV][VEC] = {};
-    const T *dy = static_cast<const T *>(a.dy) + c0 + lane * VEC;
-    auto flush = [&](uint32_t k, float *part) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = c0 + (i * 32 + lane) * VEC;
-        if (c < a.cols) {
-          if (part) {
-#pragma unroll
-            for (int f = 0; f < VEC; ++f) part[c + f] = acc[i][f];
-          } else {
-            G *out = static_cast<G *>(a.dtable) + w * a.worker_stride + k * a.row_stride + c;
-            CdgVec<G, VEC> o;
-            float v[VEC];
-            if (a.accumulate) o.load(out);
-#pragma unroll
-            for (int f = 0; f < VEC; ++f) v[f] = a.accumulate ? fmaf(acc[i][f], a.scale, o.get(f)) : acc[i][f] * a.scale;
-            o.set(v);
-            o.store(out);
-          }
-        }
-#pragma unroll
-        for (int f = 0; f < VEC; ++f) acc[i][f] = 0.0f;
-      }
-    };
-    float *part = a.part + ((w * a.windows + p0 / 32) * 2) * (long long)a.cols;
+    const T *dy = static_cast<const T *>(a.dy) + w * a.n * a.dy_stride + c0 + lane * VEC;
+    float *part = a.part + (w * a.windows + win) * 2 * (long long)a.cols;
     for (int p = begin; p < end; p += kAhead) {
       CdgVec<T, VEC> v[kAhead][NV];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int q = min(p + u, end - 1);
-        const uint32_t r0 = __shfl_sync(0xffffffffu, e[0].y, q & 31), r1 = __shfl_sync(0xffffffffu, e[1].y, q & 31);
-        const T *row = dy + (rows + (q < 32 ? r0 : r1)) * a.dy_stride;
+        const uint32_t r = __shfl_sync(0xffffffffu, e.y, min(p + u, end - 1));
+        const T *row = dy + r * a.dy_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          if (c0 + (i * 32 + lane) * VEC < a.cols) v[u][i].load(row + i * 32 * VEC);
-          else v[u][i].zero();
+          v[u][i].zero();
+          v[u][i].load_if(p + u < end && c0 + (i * 32 + lane) * VEC < a.cols, row + i * 32 * VEC);
         }
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const int q = p + u;
         if (q >= end) break;
-        const uint32_t k0 = __shfl_sync(0xffffffffu, e[0].x, q & 31), k1 = __shfl_sync(0xffffffffu, e[1].x, q & 31);
-        const uint32_t n0 = __shfl_sync(0xffffffffu, e[0].x, (q + 1) & 31), n1 = __shfl_sync(0xffffffffu, e[1].x, (q + 1) & 31);
-        const uint32_t k = q < 32 ? k0 : k1;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
           for (int f = 0; f < VEC; ++f) acc[i][f] += v[u][i].get(f);
-        if (q + 1 == end || k != (q + 1 < 32 ? n0 : n1)) {
-          const bool is_head = goes_on && q + 1 == head;
-          flush(k, is_head ? part + a.cols : tail_long && q + 1 == end ? part : nullptr);
+        if (!(ends >> q & 1)) continue;
+        const uint32_t k = __shfl_sync(0xffffffffu, e.x, q);
+        float *piece = goes_on && q + 1 == head ? part + a.cols : tail_long && q + 1 == end ? part : nullptr;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int c = c0 + (i * 32 + lane) * VEC;
+          if (c < a.cols) {
+            if (piece) {
+#pragma unroll
+              for (int f = 0; f < VEC; ++f) piece[c + f] = acc[i][f];
+            } else {
+              G *out = static_cast<G *>(a.dtable) + w * a.worker_stride + k * a.row_stride + c;
+              CdgVec<G, VEC> o;
+              float g[VEC];
+              if (a.accumulate) o.load(out);
+#pragma unroll
+              for (int f = 0; f < VEC; ++f) g[f] = a.accumulate ? fmaf(acc[i][f], a.scale, o.get(f)) : acc[i][f] * a.scale;
+              o.set(g);
+              o.store(out);
+            }
+          }
+#pragma unroll
+          for (int f = 0; f < VEC; ++f) acc[i][f] = 0.0f;
         }
       }
     }
   }
 }
 
-// a block to kJoin windows and 256 columns: the parts of each long run that starts there, warp q taking every eighth
-constexpr int kJoin = 8;
+// A block to kJoin windows and 256 columns: the parts of each long run that starts there, warp q taking every eighth.
+constexpr int kJoin = 8, kJoinCols = 256;
 template <typename G>
 __global__ void __launch_bounds__(kThreads) join_runs_kernel(const __grid_constant__ Sums a, long long all) {
-  __shared__ float sm[kWarps][kSlab];
+  __shared__ float sm[kWarps][kJoinCols];
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int j = 0; j < kJoin; ++j) {
-    const long long at = (long long)blockIdx.x * kJoin + j;
-    if (at >= all) return;
-    const long long w = at / a.windows;
-    const int win = (int)(at - w * a.windows), p0 = win * 32;
+  const long long at0 = (long long)blockIdx.x * kJoin;
+  // which of the windows a long run starts in
+  bool starts = false;
+  if (lane < kJoin && at0 + lane < all) {
+    const long long w = (at0 + lane) / a.windows, p0 = (at0 + lane - w * a.windows) * kWindow;
     const uint2 *items = a.items + w * a.n;
-    if ((long long)p0 + 64 >= a.n) continue;
-    const uint32_t k = items[p0 + 31].x;
-    if (k >= (uint32_t)a.vocab || items[p0 + 64].x != k || (p0 > 0 && items[p0 - 1].x == k)) continue;
-    for (int c0 = blockIdx.y * kSlab; c0 < a.cols; c0 += gridDim.y * kSlab) {
-      const float *part = a.part + (w * a.windows + win) * 2 * (long long)a.cols;
-      float s[kSlab / 32] = {};
-      for (int v = win + warp; v < a.windows && items[(long long)v * 32 + (v == win ? 31 : 0)].x == k; v += kWarps) {
-        const float *from = part + ((long long)(v - win) * 2 + (v == win ? 0 : 1)) * a.cols;
+    if (p0 + 2 * kWindow < a.n) {
+      const uint32_t k = items[p0 + kWindow - 1].x, ahead = items[p0 + 2 * kWindow].x, back = p0 > 0 ? items[p0 - 1].x : kNoKey;
+      starts = k < (uint32_t)a.vocab && k == ahead && k != back;
+    }
+  }
+  for (uint32_t todo = __ballot_sync(0xffffffffu, starts); todo; todo &= todo - 1) {
+    const long long at = at0 + __ffs(todo) - 1, w = at / a.windows;
+    const int win = (int)(at - w * a.windows);
+    const uint2 *items = a.items + w * a.n;
+    const uint32_t k = items[(long long)win * kWindow + kWindow - 1].x;
+    // how many windows it reaches into: keys are sorted, so the last is bracketed by powers of two, then by 32 steps at a time
+    auto holds = [&](long long v) { return win + v < a.windows && items[(win + v) * kWindow].x == k; };
+    const int power = __popc(__ballot_sync(0xffffffffu, holds(1ll << lane)));        // 2^(power - 1) windows on still, 2^power not
+    long long in = power ? 1ll << (power - 1) : 0, step = in;
+    while (step > 1) {                       // in holds, in + step does not
+      step = (step + 31) / 32;
+      in += step * (__popc(__ballot_sync(0xffffffffu, holds(in + step * (lane + 1)))));
+    }
+    const int pieces = (int)in + 1;
+    const float *part = a.part + (w * a.windows + win) * 2 * (long long)a.cols;
+    for (int c0 = blockIdx.y * kJoinCols; c0 < a.cols; c0 += gridDim.y * kJoinCols) {
+      float s[kJoinCols / 32] = {};
+#pragma unroll 4
+      for (int v = warp; v < pieces; v += kWarps) {
+        const float *from = part + ((long long)v * 2 + (v > 0)) * a.cols + c0 + lane;
 #pragma unroll
-        for (int i = 0; i < kSlab / 32; ++i) {
-          const int c = c0 + i * 32 + lane;
-          if (c < a.cols) s[i] += from[c];
-        }
+        for (int i = 0; i < kJoinCols / 32; ++i)
+          if (c0 + i * 32 + lane < a.cols) s[i] += from[i * 32];
       }
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kSlab / 32; ++i) sm[warp][i * 32 + lane] = s[i];
+      for (int i = 0; i < kJoinCols / 32; ++i) sm[warp][i * 32 + lane] = s[i];
       __syncthreads();
       const int c = c0 + threadIdx.x;
       if (c < a.cols) {
@@ -477,10 +530,16 @@ extern "C" int cdgrab_embedding_forward(long long groups, long long length, int 
   const Tokens tok = {tokens, token_bits, token_stride, length, padding, vocab};
   const int vec = cdg_widest(cols, {{table, vocab > 1 ? table_stride : 0, e}, {y, rows > 1 ? y_stride : 0, oe}});
   const int per_row = cols / vec;
+  // One row after another, and a store of eight values everywhere: for short rows, which leave lanes idle row by row.  (2 million bf16
+  // values in rows of 37, 106, 257, 515 and 650: 10.1, 8.5, 9.8, 9.4 and 7.7 us, row by row 25.5, 8.6, 12.6, 9.6 and 6.0; of 108 and
+  // 260, four values to an access, 7.9 and 7.4, row by row 5.8 and 7.9.)
+  const bool flat = vec < 8 && cols >= 8 && cols <= (vec < 4 ? 320 : 64) && (rows == 1 || y_stride == cols) && cdg_aligned(y, 8 * oe);
+  const int lv = cdg_widest(cols, {{table, vocab > 1 ? table_stride : 0, e}});
   // four accesses to a lane, but eight lanes where a row has work for them
   int group = 1;
   while (group < 32 && (4 * group < per_row || (group < 8 && group < per_row))) group *= 2;
-  const long long blocks = (rows + kThreads / group - 1) / (kThreads / group);
+  const long long blocks = flat ? (rows * cols + 8 * kThreads - 1) / (8 * kThreads) : (rows + kThreads / group - 1) / (kThreads / group);
+  if (blocks >= (1ll << 31)) return CDGRAB_ERR_INVALID;
   cudaStream_t st = (cudaStream_t)stream;
   return cdg_by_types(dtype, out_dtype, [&](auto t, auto r) {
     using T = decltype(t);
@@ -490,6 +549,11 @@ extern "C" int cdgrab_embedding_forward(long long groups, long long length, int 
                                           cdg_divisor((uint32_t)length), tok, scale, (const T *)table, table_stride, (R *)y, y_stride,
                                           dev->status));
     };
+    auto go_flat = [&](auto *kernel) {
+      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)blocks), kThreads, 0, st, (uint32_t)rows, cdg_divisor((uint32_t)cols),
+                                          cdg_divisor((uint32_t)length), tok, scale, (const T *)table, table_stride, (R *)y, dev->status));
+    };
+    if (flat) return lv >= 4 ? go_flat(lookup_flat_kernel<T, R, 4>) : lv == 2 ? go_flat(lookup_flat_kernel<T, R, 2>) : go_flat(lookup_flat_kernel<T, R, 1>);
     return vec == 8 ? go(lookup_kernel<T, R, 8>) : vec == 4 ? go(lookup_kernel<T, R, 4>) : vec == 2 ? go(lookup_kernel<T, R, 2>)
                                                                                         : go(lookup_kernel<T, R, 1>);
   });
@@ -498,7 +562,7 @@ extern "C" int cdgrab_embedding_forward(long long groups, long long length, int 
 extern "C" long long cdgrab_embedding_workspace_bytes(int m, long long tokens, int cols, int vocab) {
   if (m < 1 || m > 65535 || cols < 1 || vocab < 1 || !tokens_fit(m, 1, tokens)) return -1;
   // the items twice, two sums for each window
-  return 2 * up16(8ll * m * tokens) + 8ll * m * ((tokens + 31) / 32) * cols + 16;
+  return 2 * up16(8ll * m * tokens) + 8ll * m * ((tokens + kWindow - 1) / kWindow) * cols + 16;
 }
 
 extern "C" int cdgrab_embedding_backward(int m, long long groups, long long length, int cols, int vocab, int token_bits,
@@ -557,22 +621,37 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
   if (const int rc = tc_launch_cluster(sort_and_clear_kernel, dim3((unsigned)(sorting + clearing)), ctas, kSortThreads, 0, st, s, z, sorting)) return rc;
   if (n == 0) return CDGRAB_OK;
 
-  Sums a = {s.items, (int)n, (int)((n + 31) / 32), vocab, cols, nullptr, dy, dy_stride, dtable, worker_stride, row_stride, scale, accumulate};
+  Sums a = {s.items, (int)n, (int)((n + kWindow - 1) / kWindow), vocab, cols, nullptr, dy, dy_stride, dtable, worker_stride, row_stride, scale,
+            accumulate};
   a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + 2 * up16(8 * m * n));
   const long long all = (long long)m * a.windows;
-  const unsigned slabs = (unsigned)((cols + kSlab - 1) / kSlab < 65535 ? (cols + kSlab - 1) / kSlab : 65535);
   const int vec = cdg_widest(cols, {{dy, m * n > 1 ? dy_stride : 0, e}, {dtable, vocab > 1 ? row_stride : 0, ge}, {dtable, m > 1 ? worker_stride : 0, ge}});
+  // up to eight values or 16 bytes to a lane, as many as the columns need.  (32 x 700 rows of 650 fp32: 144 us, with 32 bytes 165: too
+  // few warps)
+  int nv = 1;
+  while (vec * nv < 8 && vec * nv * e < 16 && 32 * vec * nv < cols) nv *= 2;
+  auto slabs = [&](int width) { return (unsigned)((cols + width - 1) / width < 65535 ? (cols + width - 1) / width : 65535); };
   const int rc = cdg_by_types(dtype, grad_dtype, [&](auto t, auto g) {
     using T = decltype(t);
     using G = decltype(g);
     auto go = [&](auto *kernel) {
-      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)((all + kWarps - 1) / kWarps), slabs), kThreads, 0, st, a, all));
+      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)((all + kWarps - 1) / kWarps), slabs(32 * vec * nv)), kThreads, 0, st, a, all));
     };
-    return vec == 8 ? go(run_sums_kernel<T, G, 8>) : vec == 4 ? go(run_sums_kernel<T, G, 4>) : vec == 2 ? go(run_sums_kernel<T, G, 2>)
-                                                                                             : go(run_sums_kernel<T, G, 1>);
+    switch (vec * 10 + nv) {
+      case 81: return go(run_sums_kernel<T, G, 8, 1>);
+      case 41: return go(run_sums_kernel<T, G, 4, 1>);
+      case 42: return go(run_sums_kernel<T, G, 4, 2>);
+      case 21: return go(run_sums_kernel<T, G, 2, 1>);
+      case 22: return go(run_sums_kernel<T, G, 2, 2>);
+      case 24: return go(run_sums_kernel<T, G, 2, 4>);
+      case 11: return go(run_sums_kernel<T, G, 1, 1>);
+      case 12: return go(run_sums_kernel<T, G, 1, 2>);
+      case 14: return go(run_sums_kernel<T, G, 1, 4>);
+      default: return go(run_sums_kernel<T, G, 1, 8>);
+    }
   });
-  if (rc != CDGRAB_OK || n <= 64) return rc;         // no run goes on past two windows
-  const dim3 grid((unsigned)((all + kJoin - 1) / kJoin), slabs);
+  if (rc != CDGRAB_OK || n <= 2 * kWindow) return rc;         // no run goes on past two windows
+  const dim3 grid((unsigned)((all + kJoin - 1) / kJoin), slabs(kJoinCols));
   return cdg_launch_rc(grad_dtype == CDGRAB_F32 ? cdg_ops_launch(join_runs_kernel<float>, grid, kThreads, 0, st, a, all)
                                                 : cdg_ops_launch(join_runs_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, all));
 }

@@ -45,17 +45,25 @@ struct CdgVec {
   uint32_t w[kWords];
 
   __device__ __forceinline__ void load(const T *p) {
+    zero();
+    load_if(true, p);
+  }
+  // What p points to, or what was there before.  One instruction under a predicate: as a branch around a load, each of several
+  // loads was waited for before the next was issued.
+  __device__ __forceinline__ void load_if(bool yes, const T *p) {
+    const int go = yes;
     if constexpr (kBytes == 32)
-      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %9, 0;\n@q ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n}"
+                   : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]), "+r"(w[4]), "+r"(w[5]), "+r"(w[6]), "+r"(w[7]) : "l"(p), "r"(go));
     else if constexpr (kBytes == 16)
-      asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %5, 0;\n@q ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n}"
+                   : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"(go));
     else if constexpr (kBytes == 8)
-      asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %3, 0;\n@q ld.global.v2.b32 {%0, %1}, [%2];\n}" : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"(go));
     else if constexpr (kBytes == 4)
-      asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %2, 0;\n@q ld.global.b32 %0, [%1];\n}" : "+r"(w[0]) : "l"(p), "r"(go));
     else
-      w[0] = *reinterpret_cast<const volatile uint16_t *>(p);
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %2, 0;\n@q ld.global.u16 %0, [%1];\n}" : "+r"(w[0]) : "l"(p), "r"(go));
   }
   __device__ __forceinline__ void store(T *p) const {
     if constexpr (kBytes == 32)
