@@ -4,9 +4,11 @@
 
 m workers hold n sequences each (an order-1 Markov source of their own, so that workers differ).  Per pair of
 positions every worker's two sequences go through the model; the per-worker gradients land in the gather buffer
-[2][m][d] that the order server balances: those of the layer norms straight from layer_norm_backward, those of
-the matrices from one product per worker.  step_mean balances the pair and averages it; the averages of the
-matrices, with momentum, are orthogonalised, those of vectors and embeddings follow their root mean square.
+[2][m][d] that the order server balances: those of the layer norms straight from layer_norm_backward, the embedding's
+from embedding_backward, those of the matrices from one product per worker.  Optionally queries and keys are normed
+and rotated by position in place of learned positions, and the residual branches dropped out.  step_mean balances
+the pair and averages it; the averages of the matrices, with momentum, are orthogonalised, those of vectors and
+embeddings follow their root mean square.
 The paper's workers compute their gradients the same way (Algorithm 3); the model is its GPT-2 in small.
 """
 from __future__ import annotations
@@ -24,12 +26,14 @@ class Gpt:
     """Pre-norm transformer with its backward pass written out; parameters are views of one flat float32
     vector, gradients of worker i views of row i of a gather buffer."""
 
-    def __init__(self, vocab=64, width=128, heads=4, kv_heads=2, layers=2, length=128, seed=0):
+    def __init__(self, vocab=64, width=128, heads=4, kv_heads=2, layers=2, length=128, seed=0, rotary=False, dropout=0.0):
         self.vocab, self.width, self.heads, self.kv_heads, self.layers, self.length = vocab, width, heads, kv_heads, layers, length
+        self.rotary, self.dropout, self.seed, self.steps = rotary, dropout, seed, 0      # steps: masks drawn so far
         self.head_dim = width // heads
         qkv = (heads + 2 * kv_heads) * self.head_dim
-        spec = [("embed", (vocab, width)), ("pos", (length, width))]
+        spec = [("embed", (vocab, width))] + ([] if rotary else [("pos", (length, width))])
         for l in range(layers):
+            spec += [(f"{l}.q.w", (self.head_dim,)), (f"{l}.k.w", (self.head_dim,))] if rotary else []
             spec += [(f"{l}.ln1.w", (width,)), (f"{l}.ln1.b", (width,)), (f"{l}.qkv", (qkv, width)), (f"{l}.out", (width, width)),
                      (f"{l}.ln2.w", (width,)), (f"{l}.ln2.b", (width,)), (f"{l}.up", (4 * width, width)), (f"{l}.down", (width, 4 * width))]
         spec += [("ln.w", (width,)), ("ln.b", (width,)), ("head", (vocab, width))]
@@ -58,30 +62,43 @@ class Gpt:
         m, t, c, p = tokens.shape[0], self.length, self.width, self.p
         h, hk, hd = self.heads, self.kv_heads, self.head_dim
         bf = {n: p[n].bfloat16() for n in self.matrices + ["head"]}
-        inp, want = tokens[:, :-1].long(), tokens[:, 1:].long()
+        want = tokens[:, 1:].long()
         per = lambda y: y.view(m, t, -1)  # noqa: E731
 
         def weight_gradient(name, dy, x):        # worker i's dW = dy_i^T x_i
             self.grad(buf, name).copy_(torch.bmm(per(dy).transpose(1, 2), per(x)))
 
+        def branch(call, y, x):                  # x + y, with y dropped out
+            if not self.dropout:
+                return x + y.float()
+            return binding.dropout_forward(y, self.dropout, self.seed, call, self.steps, residual=x)
+
+        def branch_backward(call, dx):           # y's gradient
+            if not self.dropout:
+                return dx.bfloat16()
+            return binding.dropout_backward(dx, self.dropout, self.seed, call, self.steps, dtype=torch.bfloat16)
+
         def norm_backward(name, dy, x, stats):
             return binding.layer_norm_backward(dy, x, p[name + ".w"], *stats, self.grad(buf, name + ".w"), self.grad(buf, name + ".b"))
 
-        x = (p["embed"][inp] + p["pos"]).view(m * t, c)
+        x = binding.embedding_forward(tokens[:, :-1], p["embed"])
+        if not self.rotary:
+            x = (x.view(m, t, c) + p["pos"]).view(m * t, c)
         tape = []
         for l in range(self.layers):
             y1, *s1 = binding.layer_norm_forward(x, p[f"{l}.ln1.w"], p[f"{l}.ln1.b"])
             y1 = y1.bfloat16()
             qkv = (y1 @ bf[f"{l}.qkv"].T).view(m, t, h + 2 * hk, hd)
             q, k, v = qkv[:, :, :h], qkv[:, :, h:h + hk], qkv[:, :, h + hk:]
-            o, lse = binding.attention_forward(q, k, v, causal=True)
-            x1 = x + (o.view(m * t, c) @ bf[f"{l}.out"].T).float()
+            q2, k2 = binding.rotary_forward(q, k, p[f"{l}.q.w"], p[f"{l}.k.w"]) if self.rotary else (q, k)
+            o, lse = binding.attention_forward(q2, k2, v, causal=True)
+            x1 = branch(2 * l, o.view(m * t, c) @ bf[f"{l}.out"].T, x)
             y2, *s2 = binding.layer_norm_forward(x1, p[f"{l}.ln2.w"], p[f"{l}.ln2.b"])
             y2 = y2.bfloat16()
             u = y2 @ bf[f"{l}.up"].T
             a = torch.nn.functional.gelu(u)
-            tape.append((x, s1, y1, qkv, o, lse, x1, s2, y2, u, a))
-            x = x1 + (a @ bf[f"{l}.down"].T).float()
+            tape.append((x, s1, y1, qkv, q2, k2, o, lse, x1, s2, y2, u, a))
+            x = branch(2 * l + 1, a @ bf[f"{l}.down"].T, x1)
         y, *s = binding.layer_norm_forward(x, p["ln.w"], p["ln.b"])
         y = y.bfloat16()
         logits = (y @ bf["head"].T).float()
@@ -94,24 +111,28 @@ class Gpt:
         weight_gradient("head", dlogits, y)
         dx = norm_backward("ln", (dlogits @ bf["head"]).float(), x, s)
         for l in reversed(range(self.layers)):
-            x0, s1, y1, qkv, o, lse, x1, s2, y2, u, a = tape[l]
-            dy = dx.bfloat16()
+            x0, s1, y1, qkv, q2, k2, o, lse, x1, s2, y2, u, a = tape[l]
+            dy = branch_backward(2 * l + 1, dx)
             weight_gradient(f"{l}.down", dy, a)
             du = torch.ops.aten.gelu_backward(dy @ bf[f"{l}.down"], u)
             weight_gradient(f"{l}.up", du, y2)
             dx = dx + norm_backward(f"{l}.ln2", (du @ bf[f"{l}.up"]).float(), x1, s2)
-            dy = dx.bfloat16()
+            dy = branch_backward(2 * l, dx)
             weight_gradient(f"{l}.out", dy, o.view(m * t, c))
             d_o = (dy @ bf[f"{l}.out"]).view(m, t, h, hd)
             dqkv = torch.empty_like(qkv)
-            binding.attention_backward(d_o, qkv[:, :, :h], qkv[:, :, h:h + hk], qkv[:, :, h + hk:], o, lse, causal=True,
-                                       dq=dqkv[:, :, :h], dk=dqkv[:, :, h:h + hk], dv=dqkv[:, :, h + hk:])
+            dq, dk, dv = dqkv[:, :, :h], dqkv[:, :, h:h + hk], dqkv[:, :, h + hk:]
+            binding.attention_backward(d_o, q2, k2, qkv[:, :, h + hk:], o, lse, causal=True, dq=dq, dk=dk, dv=dv)
+            if self.rotary:
+                binding.rotary_backward(dq, dk, qkv[:, :, :h], qkv[:, :, h:h + hk], p[f"{l}.q.w"], p[f"{l}.k.w"],
+                                        dq_weight=self.grad(buf, f"{l}.q.w"), dk_weight=self.grad(buf, f"{l}.k.w"), q_out=dq, k_out=dk)
             dqkv = dqkv.view(m * t, -1)
             weight_gradient(f"{l}.qkv", dqkv, y1)
             dx = dx + norm_backward(f"{l}.ln1", (dqkv @ bf[f"{l}.qkv"]).float(), x0, s1)
-        dx = dx.view(m, t, c)
-        self.grad(buf, "pos").copy_(dx)
-        self.grad(buf, "embed").zero_().scatter_add_(1, inp[:, :, None].expand(m, t, c), dx)
+        if not self.rotary:
+            self.grad(buf, "pos").copy_(dx.view(m, t, c))
+        binding.embedding_backward(dx, tokens[:, :-1], self.grad(buf, "embed"))
+        self.steps += 1
         return losses
 
 
@@ -197,9 +218,11 @@ def main():
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--length", type=int, default=128)
     ap.add_argument("--lr", type=float, default=0.02)
+    ap.add_argument("--rotary", action="store_true", help="norms and rotation of queries and keys in place of learned positions")
+    ap.add_argument("--dropout", type=float, default=0.0)
     ap.add_argument("--order", choices=("cdgrab", "random"), default="cdgrab")
     a = ap.parse_args()
-    model = Gpt(width=a.width, layers=a.layers, length=a.length)
+    model = Gpt(width=a.width, layers=a.layers, length=a.length, rotary=a.rotary, dropout=a.dropout)
     print(f"{model.d} parameters, {a.workers} workers x {a.examples} sequences of {a.length}")
     train(model, a.workers, a.examples, a.epochs, a.order, a.lr)
 
