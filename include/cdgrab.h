@@ -621,7 +621,7 @@ int cdgrab_rotary_forward(const cdgrab_rotary_shape *shape, const void *q_dev, c
  *   dq_weight, dk_weight   of grad_dtype, worker i's head_dim values start at i * worker_stride (>= head_dim
  *                where m > 1); either may be NULL (not computed)
  *   workspace    16-byte aligned, cdgrab_rotary_workspace_bytes(shape, m) bytes (-1 for an invalid shape, or where the
- *                batch is no multiple of m, 1 to 65535)
+ *                batch is no multiple of m, 1 to 65535; 0 where none is needed: it may be NULL then)
  */
 long long cdgrab_rotary_workspace_bytes(const cdgrab_rotary_shape *shape, int m);
 int cdgrab_rotary_backward(const cdgrab_rotary_shape *shape, int m, const void *dq_dev, const void *dk_dev,

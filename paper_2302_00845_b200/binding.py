@@ -914,10 +914,10 @@ def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, 
         q_out = _empty_like(q, other)
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
-    scratch = _scratch(q, nbytes, other)
+    scratch = _scratch(q, nbytes, other) if nbytes else None
     rc = lib().cdgrab_rotary_backward(
         sh, m, dq.data_ptr(), _at(dk), q.data_ptr(), _at(k), _at(q_weight), _at(k_weight), _at(positions), bits, step, _at(lens),
-        q_out.data_ptr(), _at(k_out), gcode, _at(dq_weight), _at(dk_weight), ws, scratch.data_ptr(), max(16, nbytes), handle)
+        q_out.data_ptr(), _at(k_out), gcode, _at(dq_weight), _at(dk_weight), ws, _at(scratch), nbytes, handle)
     if rc:
         _check(rc, "cdgrab_rotary_backward")
     return q_out, k_out

@@ -496,9 +496,9 @@ int group_of(const cdgrab_rotary_shape *s) {
   while (group < lanes_of(s)) group *= 2;
   return group;
 }
-// Shares that each token's heads are dealt out in, one by one, so that neighbouring groups read neighbouring heads: as many as fill
-// five blocks to an SM, a share for every two heads at most; each share computes the token's angles again.  (16 x 1024, 12 + 12 heads
-// of 64, in one share 21.5 us, in two 20.5, in three 23.3; 4 x 4096, 16 + 4 heads of 128, backward in one 49, in two 55.)
+// Forward: shares that each token's heads are dealt out in, one by one, so that neighbouring groups read neighbouring heads: as many
+// as fill five blocks to an SM, a share for every two heads at most; each share computes the token's angles again.  (16 x 1024, 12 + 12
+// heads of 64, in one share 21.5 us, in two 20.5, in three 23.3.)
 constexpr int kSms = 148;
 int parts_of(const cdgrab_rotary_shape *s, int heads) {
   const long long tokens = (long long)s->batch * s->len, fill = 5ll * kSms * (kThreads / group_of(s));
@@ -507,26 +507,40 @@ int parts_of(const cdgrab_rotary_shape *s, int heads) {
   const long long per = (heads + parts - 1) / parts;
   return (int)((heads + per - 1) / per);
 }
-// Blocks to a worker's queries or keys: 16,384 values to a block, an item to each group of lanes at least, about four rounds of the
-// blocks that are resident at once (two to an SM) at most.  (4 x 4096, 16 + 4 heads of 128: 48 us, with 65,536 values 55.)
+// Backward: how each worker's queries and keys are dealt out.  About 16,384 values to a block, but no more blocks than four rounds of
+// what is resident at once (two to an SM).  (4 x 4096, 16 + 4 heads of 128: 48 us, with 65,536 values 55.)
+// Up to two clusters' worth of blocks is made one cluster, which needs no second launch.  More blocks run on their own: in clusters
+// they wait for room for all eight (the same case: 57 us instead of 49).
+// A token's heads are dealt out in shares only where the blocks would otherwise lack tokens: a share of two heads spends as long on
+// its angles and on waiting as on the heads (3 x 357, 6 + 2 heads of 80 fp32: 17 us in three shares, 13 in one).
+struct Blocks { int q, k, cluster, parts[2]; };
 constexpr int kChunk = 16384, kCluster = 8;
-int chunks_of(const cdgrab_rotary_shape *s, int m, int heads) {
-  const long long tokens = (long long)s->batch / m * s->len, groups = kThreads / group_of(s);
-  if (tokens == 0 || heads == 0) return 1;
-  const long long rounds = (tokens * parts_of(s, heads) + groups - 1) / groups, work = (tokens * heads * s->head_dim + kChunk - 1) / kChunk;
-  const long long most = 8ll * kSms / m, c = rounds < work ? rounds : work;
-  return (int)(c < most ? c : most < 1 ? 1 : most);
-}
-// Up to two clusters' worth of blocks is made one cluster, which needs no second launch (3 x 357, 6 + 2 heads of 80 fp32: 26 -> 23 us
-// with the host's part).  More blocks run on their own: in clusters they wait for room for all eight (4 x 4096, 16 + 4 heads of 128:
-// 57 us instead of 49).
-struct Blocks { int q, k, cluster; };
 Blocks blocks_of(const cdgrab_rotary_shape *s, int m) {
-  Blocks b = {chunks_of(s, m, s->heads), chunks_of(s, m, s->kv_heads), 1};
-  const int most = b.q > b.k ? b.q : b.k;
-  if (most > 2 * kCluster) return b;
-  while (b.cluster < kCluster && b.cluster < most) b.cluster *= 2;
-  b.q = b.k = b.cluster;
+  const long long tokens = (long long)s->batch / m * s->len, groups = kThreads / group_of(s);
+  const long long most = 8ll * kSms / m < 1 ? 1 : 8ll * kSms / m, resident = 2ll * kSms / m < 1 ? 1 : 2ll * kSms / m;
+  long long want[2];
+  for (int i = 0; i < 2; ++i) want[i] = (tokens * (i ? s->kv_heads : s->heads) * s->head_dim + kChunk - 1) / kChunk;
+  const bool one = (want[0] > want[1] ? want[0] : want[1]) <= 2 * kCluster;
+  Blocks b = {1, 1, 1, {1, 1}};
+  long long rounds[2] = {1, 1};
+  for (int i = 0; i < 2; ++i) {
+    const int heads = i ? s->kv_heads : s->heads;
+    if (tokens == 0 || heads == 0) continue;
+    const long long fill = one ? kCluster : want[i], blocks = fill < resident ? fill : resident, parts = blocks * groups / tokens, limit = (heads + 1) / 2;
+    b.parts[i] = (int)(parts < 1 ? 1 : parts < limit ? parts : limit);
+    const int per = (heads + b.parts[i] - 1) / b.parts[i];
+    b.parts[i] = (heads + per - 1) / per;
+    rounds[i] = (tokens * b.parts[i] + groups - 1) / groups;
+  }
+  if (one) {
+    while (b.cluster < kCluster && (b.cluster < rounds[0] || b.cluster < rounds[1])) b.cluster *= 2;
+    b.q = b.k = b.cluster;
+  } else {
+    for (int i = 0; i < 2; ++i) {
+      const long long c = want[i] < most ? want[i] : most, n = c < rounds[i] ? c : rounds[i];
+      (i ? b.k : b.q) = (int)(n < 1 ? 1 : n);
+    }
+  }
   return b;
 }
 
@@ -618,7 +632,7 @@ extern "C" int cdgrab_rotary_forward(const cdgrab_rotary_shape *s, const void *q
 extern "C" long long cdgrab_rotary_workspace_bytes(const cdgrab_rotary_shape *s, int m) {
   if (!shape_ok(s) || m < 1 || m > 65535 || s->batch % m) return -1;
   const Blocks b = blocks_of(s, m);
-  return 4ll * m * ((b.q + b.k) / b.cluster) * s->head_dim;
+  return b.q == b.cluster && b.k == b.cluster ? 0 : 4ll * m * ((b.q + b.k) / b.cluster) * s->head_dim;
 }
 
 extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const void *dq, const void *dk, const void *q, const void *k,
@@ -635,14 +649,13 @@ extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const
   if (tokens > 0 && !call_ok(s, a, true)) return CDGRAB_ERR_INVALID;
   const int ge = grad_dtype == CDGRAB_F32 ? 4 : 2;
   if (((dqw || dkw) && m > 1 && worker_stride < s->head_dim) || !cdg_aligned(dqw, ge) || !cdg_aligned(dkw, ge)) return CDGRAB_ERR_INVALID;
-  if (!workspace || workspace_bytes < need || !cdg_aligned(workspace, 16)) return CDGRAB_ERR_INVALID;
+  if (need > 0 && (!workspace || workspace_bytes < need || !cdg_aligned(workspace, 16))) return CDGRAB_ERR_INVALID;
   const CdgOpsDevice *dev;
   if (const int rc = cdg_ops_device(&dev)) return rc;
   Frequencies f;
   fill(s, a, f);
-  a.parts[0] = cdg_divisor(parts_of(s, s->heads));
-  a.parts[1] = cdg_divisor(parts_of(s, s->kv_heads));
   const Blocks n = blocks_of(s, m);
+  for (int i = 0; i < 2; ++i) a.parts[i] = cdg_divisor(n.parts[i]);
   cudaStream_t st = (cudaStream_t)stream;
   const Grads out = {{dqw, dkw}, worker_stride, grad_dtype == CDGRAB_BF16, static_cast<float *>(workspace)};
   const int rc = by_kind(s, [&](auto t, auto v, auto near) {

@@ -88,8 +88,14 @@ def test_rotary_arguments(lib):
         assert fwd(rotary_shape(), **bad) == binding.ERR_INVALID, bad
         assert bwd(rotary_shape(), **bad) == binding.ERR_INVALID, bad
     for bad in (dict(m=0), dict(m=3), dict(m=65536), dict(dq=None), dict(dk=None), dict(dq=P + 8), dict(dk=P + 2), dict(gd=2), dict(dqw=P + 2), dict(dkw=P + 1),
-                dict(ws=63), dict(work=None), dict(size=0), dict(work=P + 8)):
+                dict(ws=63)):
         assert bwd(rotary_shape(), **bad) == binding.ERR_INVALID, bad
+    # long sequences need a workspace, short ones none
+    long = rotary_shape(len=100_000)
+    need = lib.cdgrab_rotary_workspace_bytes(C.byref(long), 2)
+    assert need > 0 and lib.cdgrab_rotary_workspace_bytes(C.byref(rotary_shape()), 2) == 0
+    for bad in (dict(work=None), dict(size=need - 1), dict(work=P + 8)):
+        assert bwd(long, **bad) == binding.ERR_INVALID, bad
     for bad in (dict(dq=(1536, 256, 4)), dict(dk=(768, 0, 64))):
         assert bwd(rotary_shape(**bad)) == binding.ERR_INVALID, bad
     assert fwd(rotary_shape(batch=0)) == binding.OK and fwd(rotary_shape(len=0)) == binding.OK
