@@ -510,7 +510,7 @@ int cdgrab_orthogonalise(int batch, int rows, int cols, int dtype, const void *g
  * Embedding lookup:  y[g * length + j] = scale * table[tokens[g][j]].
  *   groups, length   tokens come in `groups` rows of `length`, row starts token_stride (>= length) apart (a slice
  *                of longer sequences); from 0 (nothing to do), together below 2^31
- *   cols, vocab  >= 1
+ *   cols, vocab  >= 1; cols up to 2^24
  *   token_bits   32 or 64: tokens are signed integers of that size
  *   padding      a token that stands for none: its row of y is zero and it has no gradient.  Any number; INT64_MIN where
  *                there is none.  Any other token outside [0, vocab) is treated likewise and reported by
@@ -531,7 +531,8 @@ int cdgrab_embedding_forward(long long groups, long long length, int cols, int v
  * buffer.  With accumulate = 1 the sums are added to what dtable holds (the gradient of a product that shares
  * the matrix) and the other rows are left as they are.  The sums run over the tokens in the order of their
  * positions, whatever the grid: results are the same bits every time.
- *   dy           of `dtype`, a row for every token, dy_stride (>= cols) apart; rows of padding are not used
+ *   dy           of `dtype`, a row for every token, dy_stride (>= cols) apart; rows of padding are not used.  Neither
+ *                dy nor the tokens may overlap dtable.
  *   dtable       of grad_dtype: worker i's row v starts at i * worker_stride + v * row_stride;
  *                row_stride >= cols where vocab > 1, worker_stride >= (vocab - 1) * row_stride + cols where m > 1
  *   workspace    16-byte aligned, cdgrab_embedding_workspace_bytes(m, groups * length, cols, vocab) bytes
@@ -551,9 +552,10 @@ int cdgrab_embedding_backward(int m, long long groups, long long length, int col
  * four output words, low half first.  keep where these bits are at least T = p * 65536 rounded to the nearest (halves
  * up), q = 1 - T / 65536: p is taken to the nearest 2^-16, and the mean is kept exactly.  The mask depends on neither
  * types nor strides.
- *   rows, cols   from 0 (nothing to do), below 2^31 each; below 2^62 together
+ *   rows, cols   from 0 (nothing to do), below 2^31 each; below 2^42 together
  *   dtype, out_dtype   of x; of the residual and y.  Rows x_stride, residual_stride, y_stride (>= cols) apart.
- *   residual     may be NULL: none.  y may be the residual, or x where the types are equal.
+ *   residual     may be NULL: none.  y may be the residual, or x where the types are equal, with the same stride;
+ *                they may not overlap in other ways.
  *   p            from 0 to 1; a dropped element is 0 whatever x holds there
  *   call, step   which use of the generator this is (a layer and a training step, for instance)
  *   step_dev     NULL, or a DEVICE number whose low 32 bits are added to step: a captured call that is
@@ -565,7 +567,7 @@ int cdgrab_dropout_forward(long long rows, long long cols, int dtype, const void
                            const long long *step_dev, void *stream);
 
 /* Its backward pass:  dx = keep * dy / q with the same mask (the residual's gradient is dy itself).
- *   dtype, out_dtype   of dy; of dx, which may be dy where the types are equal */
+ *   dtype, out_dtype   of dy; of dx, which may be dy where the types and strides are equal */
 int cdgrab_dropout_backward(long long rows, long long cols, int dtype, const void *dy_dev, long long dy_stride,
                             int out_dtype, void *dx_dev, long long dx_stride, double p, unsigned long long seed,
                             unsigned call, unsigned step, const long long *step_dev, void *stream);
@@ -604,7 +606,8 @@ typedef struct {
  *                b * position_stride (0: the same for all sequences); NULL: the token's index.  Up to 2^31 in size.
  *   lens         int32 [batch], the tokens in use, or NULL: all.  What lies past a length is never used, and the
  *                outputs there are zero.
- *   q_out, k_out may be q and k themselves
+ *   q_out, k_out may be q and k themselves, with the same strides
+ * A NaN or an infinity in a head in use spoils that head, in the backward pass the worker's sums for the weight as well.
  */
 int cdgrab_rotary_forward(const cdgrab_rotary_shape *shape, const void *q_dev, const void *k_dev,
                           const float *q_weight_dev, const float *k_weight_dev, const void *positions_dev,
@@ -617,7 +620,7 @@ int cdgrab_rotary_forward(const cdgrab_rotary_shape *shape, const void *q_dev, c
  *   g' = the gradient turned back,  h = g' * weight,  dx = rstd * (h - n * (sum h n) / head_dim)  into q_out, k_out,
  *   dq_weight[i] = sum over worker i's tokens and heads of g' * n, dk_weight likewise
  * so that a worker's gradient of the two weights lands in its row of the gather buffer.
- *   q_out, k_out may be dq and dk, or q and k
+ *   q_out, k_out may be dq and dk, or q and k, with the same strides
  *   dq_weight, dk_weight   of grad_dtype, worker i's head_dim values start at i * worker_stride (>= head_dim
  *                where m > 1); either may be NULL (not computed)
  *   workspace    16-byte aligned, cdgrab_rotary_workspace_bytes(shape, m) bytes (-1 for an invalid shape, or where the

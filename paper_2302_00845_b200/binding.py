@@ -647,6 +647,14 @@ def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: floa
 _NO_PADDING = -2 ** 63
 
 
+def _padding(padding) -> int:
+    if padding is None:
+        return _NO_PADDING
+    if not -2 ** 63 <= padding < 2 ** 63:
+        raise ValueError(f"padding: {padding}, beyond 64 bits")
+    return padding
+
+
 def _tokens(t):
     """(groups, length, row stride, bits) of tokens [length] or [groups][length]."""
     if t.dtype is torch.int64:
@@ -688,7 +696,7 @@ def embedding_forward(tokens, table, scale: float = 1.0, padding: int | None = N
         if dtype is not None and dtype != out.dtype:
             raise ValueError("out: of another type than dtype")
     rc = lib().cdgrab_embedding_forward(
-        groups, length, cols, vocab, bits, tokens.data_ptr(), ts, _NO_PADDING if padding is None else padding, scale, code,
+        groups, length, cols, vocab, bits, tokens.data_ptr(), ts, _padding(padding), scale, code,
         table.data_ptr(), _row_stride(table, "table", vocab, cols), ycode, y.data_ptr(), ys, handle)
     if rc:
         _check(rc, "cdgrab_embedding_forward")
@@ -720,7 +728,7 @@ def embedding_backward(dy, tokens, dtable, scale: float = 1.0, padding: int | No
     nbytes = L.cdgrab_embedding_workspace_bytes(m, groups // m * length, cols, vocab)
     scratch = _scratch(dtable, nbytes, other)
     rc = L.cdgrab_embedding_backward(
-        m, groups // m, length, cols, vocab, bits, tokens.data_ptr(), ts, _NO_PADDING if padding is None else padding, scale,
+        m, groups // m, length, cols, vocab, bits, tokens.data_ptr(), ts, _padding(padding), scale,
         code, dy.data_ptr(), dys, gcode, dtable.data_ptr(), ws, rs, 1 if accumulate else 0, scratch.data_ptr(), max(16, nbytes), handle)
     if rc:
         _check(rc, "cdgrab_embedding_backward")

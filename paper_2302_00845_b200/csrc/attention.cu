@@ -1245,26 +1245,9 @@ attn_backward_q(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 // ---- host ---------------------------------------------------------------------------------------
 constexpr long long kMaxStride = 1ll << 38;   // elements; a tensor map holds byte strides below 2^40
 
-// strides of a tensor that is read: multiples of 16 bytes, tokens and heads apart from each other
-bool in_ok(const long long s[3], int tokens, int heads, int dim) {
-  for (int i = 0; i < 3; ++i)
-    if (s[i] < 0 || s[i] % 8 != 0 || s[i] > kMaxStride) return false;
-  return (tokens <= 1 || s[1] >= dim) && (heads <= 1 || s[2] >= dim);
-}
-// ... and of one that is written: no two heads' values on top of each other
+bool in_ok(const long long s[3], int tokens, int heads, int dim) { return cdg_heads_in_ok(s, tokens, heads, dim, kMaxStride); }
 bool out_ok(const long long s[3], int batch, int tokens, int heads, int dim) {
-  if (!in_ok(s, tokens, heads, dim)) return false;
-  long long ext[3] = {batch, tokens, heads}, str[3] = {s[0], s[1], s[2]}, span = dim;
-  for (int round = 0; round < 3; ++round) {
-    int at = -1;                                    // the axis with the smallest stride that is left
-    for (int i = 0; i < 3; ++i)
-      if (ext[i] > 1 && (at < 0 || str[i] < str[at])) at = i;
-    if (at < 0) return true;
-    if (str[at] < span) return false;
-    span += (ext[at] - 1) * str[at];
-    ext[at] = 1;
-  }
-  return true;
+  return cdg_heads_out_ok(s, batch, tokens, heads, dim, kMaxStride);
 }
 
 constexpr int kMaxTokens = 1 << 22;

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) dropout_narrow_kernel(long long n, l
 int dropout(long long rows, long long cols, int dtype, const void *x, long long xs, int out_dtype, const void *res, long long rs,
             void *y, long long ys, double p, unsigned long long seed, unsigned call, unsigned step, const long long *step_dev,
             void *stream) {
-  if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31) || !cdg_dtype_ok(dtype) || !cdg_dtype_ok(out_dtype) ||
+  if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31) || rows * cols >= (1ll << 42) || !cdg_dtype_ok(dtype) || !cdg_dtype_ok(out_dtype) ||
       !(p >= 0.0 && p <= 1.0))
     return CDGRAB_ERR_INVALID;
   if (rows == 0 || cols == 0) return CDGRAB_OK;
@@ -145,7 +145,6 @@ int dropout(long long rows, long long cols, int dtype, const void *x, long long 
   const bool wide = flat ? cdg_widest(8, {{x, 0, e}, {res, 0, oe}, {y, 0, oe}}) == 8
                          : cdg_widest(cols, {{x, xs, e}, {res, rs, oe}, {y, ys, oe}}) == 8;
   const long long grid = wide ? (blocks + kBlocks * kThreads - 1) / (kBlocks * kThreads) : (blocks + kThreads - 1) / kThreads;
-  if (grid >= (1ll << 31)) return CDGRAB_ERR_INVALID;
   if (none) x = nullptr;
   cudaStream_t st = (cudaStream_t)stream;
   return cdg_by_types(dtype, out_dtype, [&](auto t, auto r) {

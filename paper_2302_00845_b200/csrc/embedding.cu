@@ -509,6 +509,8 @@ bool tokens_fit(long long m, long long groups, long long length) {
   return groups <= most / length && groups * length <= most / m;
 }
 
+constexpr int kMaxCols = 1 << 24;       // columns are counted in 32 bits, in steps of up to 2^24
+
 inline long long up16(long long v) { return (v + 15) & ~15ll; }
 
 }  // namespace
@@ -516,7 +518,7 @@ inline long long up16(long long v) { return (v + 15) & ~15ll; }
 extern "C" int cdgrab_embedding_forward(long long groups, long long length, int cols, int vocab, int token_bits, const void *tokens,
                                         long long token_stride, long long padding, float scale, int dtype, const void *table,
                                         long long table_stride, int out_dtype, void *y, long long y_stride, void *stream) {
-  if (!tokens_fit(1, groups, length) || cols < 1 || vocab < 1 || (token_bits != 32 && token_bits != 64) || !std::isfinite(scale) ||
+  if (!tokens_fit(1, groups, length) || cols < 1 || cols > kMaxCols || vocab < 1 || (token_bits != 32 && token_bits != 64) || !std::isfinite(scale) ||
       !cdg_dtype_ok(dtype) || !cdg_dtype_ok(out_dtype))
     return CDGRAB_ERR_INVALID;
   if (groups == 0 || length == 0) return CDGRAB_OK;
@@ -560,7 +562,7 @@ extern "C" int cdgrab_embedding_forward(long long groups, long long length, int 
 }
 
 extern "C" long long cdgrab_embedding_workspace_bytes(int m, long long tokens, int cols, int vocab) {
-  if (m < 1 || m > 65535 || cols < 1 || vocab < 1 || !tokens_fit(m, 1, tokens)) return -1;
+  if (m < 1 || m > 65535 || cols < 1 || cols > kMaxCols || vocab < 1 || !tokens_fit(m, 1, tokens)) return -1;
   // the items twice, two sums for each window
   return 2 * up16(8ll * m * tokens) + 8ll * m * ((tokens + kWindow - 1) / kWindow) * cols + 16;
 }

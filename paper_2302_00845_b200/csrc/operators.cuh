@@ -16,6 +16,29 @@ long long cdg_ops_wait_limit();
 
 inline bool cdg_aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
+// Strides (batch, token, head) of a [batch][token][head][dim] tensor that is read: multiples of 8 values, tokens and heads apart
+// from each other.
+inline bool cdg_heads_in_ok(const long long s[3], int tokens, int heads, int dim, long long most) {
+  for (int i = 0; i < 3; ++i)
+    if (s[i] < 0 || s[i] % 8 != 0 || s[i] > most) return false;
+  return (tokens <= 1 || s[1] >= dim) && (heads <= 1 || s[2] >= dim);
+}
+// ... and of one that is written: no two heads' values on top of each other
+inline bool cdg_heads_out_ok(const long long s[3], int batch, int tokens, int heads, int dim, long long most) {
+  if (!cdg_heads_in_ok(s, tokens, heads, dim, most)) return false;
+  long long ext[3] = {batch, tokens, heads}, str[3] = {s[0], s[1], s[2]}, span = dim;
+  for (int round = 0; round < 3; ++round) {
+    int at = -1;                                    // the axis with the smallest stride that is left
+    for (int i = 0; i < 3; ++i)
+      if (ext[i] > 1 && (at < 0 || str[i] < str[at])) at = i;
+    if (at < 0) return true;
+    if (str[at] < span) return false;
+    span += (ext[at] - 1) * str[at];
+    ext[at] = 1;
+  }
+  return true;
+}
+
 // the error of the launches since the last check, as a CDGRAB_* code
 inline int cdg_launch_rc(cudaError_t e = cudaSuccess) {
   const cudaError_t l = cudaGetLastError();

@@ -471,12 +471,7 @@ __global__ void __launch_bounds__(kJoinThreads) rotary_join_kernel(int q_cluster
   }
 }
 
-bool strides_ok(const long long (&s)[3], int len, int heads, int dim) {
-  if (heads == 0) return true;
-  for (long long v : s)
-    if (v < 0 || v % 8 || v > (1ll << 40)) return false;
-  return (len <= 1 || s[1] >= dim) && (heads <= 1 || s[2] >= dim);
-}
+constexpr long long kMaxStride = 1ll << 40;
 
 bool shape_ok(const cdgrab_rotary_shape *s) {
   return s && s->batch >= 0 && s->len >= 0 && s->heads >= 0 && s->kv_heads >= 0 && s->heads <= 65535 && s->kv_heads <= 65535 &&
@@ -579,11 +574,15 @@ int by_kind(const cdgrab_rotary_shape *s, F &&f) {
 
 // the checks that both directions share; backward: with the gradients
 bool call_ok(const cdgrab_rotary_shape *s, const Args &a, bool backward) {
-  if (!strides_ok(s->q_stride, s->len, s->heads, s->head_dim) || !strides_ok(s->k_stride, s->len, s->kv_heads, s->head_dim) ||
-      !strides_ok(s->q_out_stride, s->len, s->heads, s->head_dim) || !strides_ok(s->k_out_stride, s->len, s->kv_heads, s->head_dim))
-    return false;
-  if (backward && (!strides_ok(s->dq_stride, s->len, s->heads, s->head_dim) || !strides_ok(s->dk_stride, s->len, s->kv_heads, s->head_dim)))
-    return false;
+  const long long *in[] = {s->q_stride, s->k_stride, s->dq_stride, s->dk_stride}, *out[] = {s->q_out_stride, s->k_out_stride};
+  for (int i = 0; i < (backward ? 4 : 2); ++i) {
+    const int heads = i % 2 ? s->kv_heads : s->heads;
+    if (heads > 0 && !cdg_heads_in_ok(in[i], s->len, heads, s->head_dim, kMaxStride)) return false;
+  }
+  for (int i = 0; i < 2; ++i) {
+    const int heads = i ? s->kv_heads : s->heads;
+    if (heads > 0 && !cdg_heads_out_ok(out[i], s->batch, s->len, heads, s->head_dim, kMaxStride)) return false;
+  }
   for (int i = 0; i < 2; ++i) {
     const Side &z = a.side[i];
     if ((i ? s->kv_heads : s->heads) > 0 && (!z.x || !z.y || (backward && !z.dy))) return false;

@@ -181,3 +181,32 @@ def test_other_device_is_refused():
         binding.embedding_backward(torch.zeros(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int64), torch.zeros(9, 8, device="cuda"))
     with pytest.raises(ValueError):
         binding.rotary_forward(torch.zeros(1, 2, 1, 8, device="cuda"), torch.zeros(1, 2, 1, 8))
+
+
+def test_numbers_beyond_their_bits_are_refused():
+    """Not taken modulo a power of two, as the boundary would."""
+    t, table = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(9, 8, device="cuda")
+    for padding in (2 ** 63, -2 ** 63 - 1, 2 ** 64 - 1):
+        with pytest.raises(ValueError):
+            binding.embedding_forward(t, table, padding=padding)
+        with pytest.raises(ValueError):
+            binding.embedding_backward(torch.zeros(4, 8, device="cuda"), t, table, padding=padding)
+    q = torch.zeros(1, 2, 1, 64, device="cuda")
+    for rotary_dim in (2 ** 32 + 64, -2 ** 32):
+        with pytest.raises(ValueError):
+            binding.rotary_forward(q, q, rotary_dim=rotary_dim)
+
+
+def test_keys_shared_over_the_batch():
+    """Inputs may be broadcast, outputs not."""
+    r, _ = draws(2)
+    q, k = r(3, 20, 4, 64), r(1, 20, 2, 64)
+    shared = k.expand(3, 20, 2, 64)
+    got, want = binding.rotary_forward(q, shared), binding.rotary_forward(q, shared.contiguous())
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    dq, dk, dw, dw2 = r(3, 20, 4, 64), r(3, 20, 2, 64), torch.empty(3, 64, device="cuda"), torch.empty(3, 64, device="cuda")
+    got = binding.rotary_backward(dq, dk, q, shared, dk_weight=dw)
+    want = binding.rotary_backward(dq, dk, q, shared.contiguous(), dk_weight=dw2)
+    assert all(torch.equal(a, c) for a, c in zip(got, want)) and torch.equal(dw, dw2)
+    with pytest.raises(binding.CdgrabError):
+        binding.rotary_forward(q, shared, k_out=torch.empty_like(k).expand(3, 20, 2, 64))

@@ -27,6 +27,8 @@ def test_embedding_arguments(lib):
                 dict(tabs=7), dict(y=None), dict(ys=7), dict(tok=P + 4), dict(bits=32, tok=P + 2), dict(table=P + 2), dict(out=1, y=P + 1)):
         assert fwd(**bad) == binding.ERR_INVALID, bad
     assert fwd(groups=0) == binding.OK and fwd(length=0) == binding.OK
+    assert fwd(cols=(1 << 24) + 1, tabs=1 << 25, ys=1 << 25) == binding.ERR_INVALID
+    assert lib.cdgrab_embedding_workspace_bytes(1, 1, (1 << 24) + 1, 1) == -1
 
     def bwd(m=2, groups=1, length=4, cols=8, vocab=10, bits=64, tok=P, ts=4, pad=-1, scale=1.0, dtype=0, dy=P, dys=8, gd=0, dt=P, ws=80, rs=8,
             acc=0, work=P, size=1 << 40):
@@ -52,6 +54,7 @@ def test_dropout_arguments(lib):
     for bad in both:
         assert fwd(**bad) == binding.ERR_INVALID, bad
         assert bwd(**bad) == binding.ERR_INVALID, bad
+    assert fwd(rows=1 << 21, cols=1 << 21, xs=1 << 21, ys=1 << 21, res=None) == binding.ERR_INVALID
     assert fwd(rs=7) == binding.ERR_INVALID and fwd(res=P + 2) == binding.ERR_INVALID
     for call in (fwd, bwd):
         assert call(rows=0) == binding.OK and call(cols=0) == binding.OK
@@ -78,7 +81,8 @@ def test_rotary_arguments(lib):
     for bad in (dict(batch=-1), dict(len=-1), dict(heads=-1), dict(kv_heads=-1), dict(heads=65536), dict(head_dim=0), dict(head_dim=12), dict(head_dim=264),
                 dict(rotary_dim=-8), dict(rotary_dim=4), dict(rotary_dim=72), dict(interleaved=2), dict(dtype=2), dict(base=0.0), dict(base=-1.0), dict(base=math.inf),
                 dict(base=math.nan), dict(eps=-1e-9), dict(eps=math.nan), dict(eps=math.inf), dict(reserved=1), dict(batch=1 << 16, len=1 << 15),
-                dict(q=(1536, 256, 60)), dict(k=(-8, 128, 64)), dict(q_out=(1536, 0, 64)), dict(k_out=(768, 128, 0))):
+                dict(q=(1536, 256, 60)), dict(k=(-8, 128, 64)), dict(q_out=(1536, 0, 64)), dict(k_out=(768, 128, 0)),
+                dict(q_out=(0, 256, 64)), dict(q_out=(1528, 256, 64)), dict(k_out=(768, 120, 64)), dict(k_out=(64, 128, 128)), dict(k=(1 << 41, 128, 64))):
         assert fwd(rotary_shape(**bad)) == binding.ERR_INVALID, bad
         assert bwd(rotary_shape(**bad)) == binding.ERR_INVALID, bad
         if not {"q", "k", "q_out", "k_out"} & set(bad):
