@@ -355,10 +355,13 @@ struct Sums {
 constexpr uint32_t kNoKey = 0xffffffffu;
 constexpr int kWindow = 16;            // half a warp: its lanes hold a window and the next one
 
-// a warp to a window and 32 VEC NV columns; kAhead rows are on their way together
+// A warp to a window and 32 VEC NV columns; kAhead rows are on their way together.  What bounds it is instructions, not memory: a
+// warp goes through a few dozen rows in its life, so each case that is spelled out for each row in flight costs its fetching, and each
+// predicate on a load its issue slots (2 x 7892 tokens of 1377 bf16 columns: 124 us with all cases for eight rows, predicated, 53 in a
+// graph with sort and join so).
 template <typename T, typename G, int VEC, int NV>
 __global__ void __launch_bounds__(kThreads) run_sums_kernel(const __grid_constant__ Sums a, long long all) {
-  constexpr int kAhead = 8, kSlab = 32 * VEC * NV;
+  constexpr int kAhead = 4, kSlab = 32 * VEC * NV;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int lane = threadIdx.x & 31;
@@ -388,55 +391,66 @@ __global__ void __launch_bounds__(kThreads) run_sums_kernel(const __grid_constan
   if (begin >= end) return;
   // positions at which a run ends
   const uint32_t after = __shfl_down_sync(0xffffffffu, e.x, 1);
-  const uint32_t ends = __ballot_sync(0xffffffffu, lane + 1 >= end || e.x != after);
+  const uint32_t ends = __ballot_sync(0xffffffffu, e.x != after);
+  const int split = head_long ? head : begin;                           // a part of a longer run comes first, by itself
   for (int c0 = blockIdx.y * kSlab; c0 < a.cols; c0 += gridDim.y * kSlab) {
-    float acc[NV][VEC] = {};
-    const T *dy = static_cast<const T *>(a.dy) + w * a.n * a.dy_stride + c0 + lane * VEC;
-    float *part = a.part + (w * a.windows + win) * 2 * (long long)a.cols;
-    for (int p = begin; p < end; p += kAhead) {
+    const int c = c0 + lane * VEC;
+    // (lanes past the last column read it again and keep nothing)
+    const T *dy = static_cast<const T *>(a.dy) + w * a.n * a.dy_stride;
+    int off[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) off[i] = min(c + i * 32 * VEC, a.cols - VEC);
+    G *table = static_cast<G *>(a.dtable) + w * a.worker_stride + c;
+    float *part = a.part + (w * a.windows + win) * 2 * (long long)a.cols + c;
+    for (int half = head_long ? 0 : 1; half < 2; ++half) {
+      const int from = half ? split : begin, to = half ? end : split;
+      const bool piece = half ? tail_long : true;                       // the last run's sum is part of a longer one's
+      float acc[NV][VEC] = {};
       CdgVec<T, VEC> v[kAhead][NV];
+      auto load = [&](int q, CdgVec<T, VEC> (&row)[NV]) {
+        const T *p = dy + __shfl_sync(0xffffffffu, e.y, min(q, to - 1)) * a.dy_stride;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const uint32_t r = __shfl_sync(0xffffffffu, e.y, min(p + u, end - 1));
-        const T *row = dy + r * a.dy_stride;
+        for (int i = 0; i < NV; ++i) row[i].load(p + off[i]);
+      };
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          v[u][i].zero();
-          v[u][i].load_if(p + u < end && c0 + (i * 32 + lane) * VEC < a.cols, row + i * 32 * VEC);
+      for (int u = 0; u < kAhead; ++u) load(from + u, v[u]);
+#pragma unroll 1
+      for (int p = from; p < to; p += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int q = p + u;
+          if (q >= to) break;
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int f = 0; f < VEC; ++f) acc[i][f] += v[u][i].get(f);
+          load(q + kAhead, v[u]);
+          if (q + 1 < to ? ends >> q & 1 : !piece) {
+            G *out = table + __shfl_sync(0xffffffffu, e.x, q) * a.row_stride;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+              CdgVec<G, VEC> o;
+              float g[VEC];
+              o.zero();
+              o.load_if(a.accumulate && c + i * 32 * VEC < a.cols, out + i * 32 * VEC);
+#pragma unroll
+              for (int f = 0; f < VEC; ++f) {
+                g[f] = fmaf(acc[i][f], a.scale, o.get(f));
+                acc[i][f] = 0.0f;
+              }
+              o.set(g);
+              o.store_if(c + i * 32 * VEC < a.cols, out + i * 32 * VEC);
+            }
+          }
         }
       }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int q = p + u;
-        if (q >= end) break;
+      if (piece) {
+        float *sum = half ? part : part + a.cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-          for (int f = 0; f < VEC; ++f) acc[i][f] += v[u][i].get(f);
-        if (!(ends >> q & 1)) continue;
-        const uint32_t k = __shfl_sync(0xffffffffu, e.x, q);
-        float *piece = goes_on && q + 1 == head ? part + a.cols : tail_long && q + 1 == end ? part : nullptr;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int c = c0 + (i * 32 + lane) * VEC;
-          if (c < a.cols) {
-            if (piece) {
-#pragma unroll
-              for (int f = 0; f < VEC; ++f) piece[c + f] = acc[i][f];
-            } else {
-              G *out = static_cast<G *>(a.dtable) + w * a.worker_stride + k * a.row_stride + c;
-              CdgVec<G, VEC> o;
-              float g[VEC];
-              if (a.accumulate) o.load(out);
-#pragma unroll
-              for (int f = 0; f < VEC; ++f) g[f] = a.accumulate ? fmaf(acc[i][f], a.scale, o.get(f)) : acc[i][f] * a.scale;
-              o.set(g);
-              o.store(out);
-            }
-          }
-#pragma unroll
-          for (int f = 0; f < VEC; ++f) acc[i][f] = 0.0f;
-        }
+          for (int f = 0; f < VEC; ++f)
+            if (c + i * 32 * VEC < a.cols) sum[i * 32 * VEC + f] = acc[i][f];
       }
     }
   }
@@ -510,6 +524,8 @@ bool tokens_fit(long long m, long long groups, long long length) {
 }
 
 constexpr int kMaxCols = 1 << 24;       // columns are counted in 32 bits, in steps of up to 2^24
+
+constexpr int kSms = 148;
 
 inline long long up16(long long v) { return (v + 15) & ~15ll; }
 
@@ -628,10 +644,10 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
   a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + 2 * up16(8 * m * n));
   const long long all = (long long)m * a.windows;
   const int vec = cdg_widest(cols, {{dy, m * n > 1 ? dy_stride : 0, e}, {dtable, vocab > 1 ? row_stride : 0, ge}, {dtable, m > 1 ? worker_stride : 0, ge}});
-  // up to eight values or 16 bytes to a lane, as many as the columns need.  (32 x 700 rows of 650 fp32: 144 us, with 32 bytes 165: too
-  // few warps)
+  // up to eight values, four accesses or 16 bytes to a lane, as many as the columns need.  (32 x 700 rows of 650 fp32: 144 us, with 32 bytes 165: too
+  // few warps)  And no more than leave 32 warps to an SM.
   int nv = 1;
-  while (vec * nv < 8 && vec * nv * e < 16 && 32 * vec * nv < cols) nv *= 2;
+  while (vec * nv < 8 && nv < 4 && vec * nv * e < 16 && 32 * vec * nv < cols && all * cols > 32ll * vec * nv * 32 * kSms) nv *= 2;
   auto slabs = [&](int width) { return (unsigned)((cols + width - 1) / width < 65535 ? (cols + width - 1) / width : 65535); };
   const int rc = cdg_by_types(dtype, grad_dtype, [&](auto t, auto g) {
     using T = decltype(t);
@@ -648,8 +664,7 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
       case 24: return go(run_sums_kernel<T, G, 2, 4>);
       case 11: return go(run_sums_kernel<T, G, 1, 1>);
       case 12: return go(run_sums_kernel<T, G, 1, 2>);
-      case 14: return go(run_sums_kernel<T, G, 1, 4>);
-      default: return go(run_sums_kernel<T, G, 1, 8>);
+      default: return go(run_sums_kernel<T, G, 1, 4>);
     }
   });
   if (rc != CDGRAB_OK || n <= 2 * kWindow) return rc;         // no run goes on past two windows

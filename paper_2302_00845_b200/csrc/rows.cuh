@@ -45,8 +45,17 @@ struct CdgVec {
   uint32_t w[kWords];
 
   __device__ __forceinline__ void load(const T *p) {
-    zero();
-    load_if(true, p);
+    if constexpr (kBytes == 32)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+    else if constexpr (kBytes == 16)
+      asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+    else if constexpr (kBytes == 8)
+      asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    else if constexpr (kBytes == 4)
+      asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    else
+      asm volatile("ld.global.u16 %0, [%1];" : "=r"(w[0]) : "l"(p));
   }
   // What p points to, or what was there before.  One instruction under a predicate: as a branch around a load, each of several
   // loads was waited for before the next was issued.
@@ -65,18 +74,21 @@ struct CdgVec {
     else
       asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %2, 0;\n@q ld.global.u16 %0, [%1];\n}" : "+r"(w[0]) : "l"(p), "r"(go));
   }
-  __device__ __forceinline__ void store(T *p) const {
+  __device__ __forceinline__ void store(T *p) const { store_if(true, p); }
+  __device__ __forceinline__ void store_if(bool yes, T *p) const {
+    const int go = yes;
     if constexpr (kBytes == 32)
-      asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
-                   ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %9, 0;\n@q st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n}"
+                   ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p), "r"(go) : "memory");
     else if constexpr (kBytes == 16)
-      asm volatile("st.global.v4.b32 [%4], {%0, %1, %2, %3};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(p) : "memory");
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %5, 0;\n@q st.global.v4.b32 [%4], {%0, %1, %2, %3};\n}"
+                   ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(p), "r"(go) : "memory");
     else if constexpr (kBytes == 8)
-      asm volatile("st.global.v2.b32 [%2], {%0, %1};" ::"r"(w[0]), "r"(w[1]), "l"(p) : "memory");
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %3, 0;\n@q st.global.v2.b32 [%2], {%0, %1};\n}" ::"r"(w[0]), "r"(w[1]), "l"(p), "r"(go) : "memory");
     else if constexpr (kBytes == 4)
-      asm volatile("st.global.b32 [%1], %0;" ::"r"(w[0]), "l"(p) : "memory");
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %2, 0;\n@q st.global.b32 [%1], %0;\n}" ::"r"(w[0]), "l"(p), "r"(go) : "memory");
     else
-      *reinterpret_cast<volatile uint16_t *>(p) = (uint16_t)w[0];
+      asm volatile("{\n.reg .pred q;\nsetp.ne.s32 q, %2, 0;\n@q st.global.u16 [%1], %0;\n}" ::"r"(w[0]), "l"(p), "r"(go) : "memory");
   }
   __device__ __forceinline__ void zero() {
 #pragma unroll
