@@ -13,8 +13,9 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kForward = 128, kBackward = 256;           // threads to a block
+constexpr int kWarps = kBackward / 32;
+constexpr int kResident = 2;               // blocks of the backward pass to an SM: 124 registers a thread
 constexpr int kMaxDim = 256, kMaxPairs = kMaxDim / 2;
 constexpr int kAhead = 4;                  // heads on their way
 
@@ -60,7 +61,7 @@ struct Shared {
 
 template <int V, bool NEAR>
 __device__ __forceinline__ void load_shared(const Args &a, const Frequencies &f, Shared &s) {
-  for (int i = threadIdx.x; i < a.lanes * V; i += kThreads) {
+  for (int i = threadIdx.x; i < a.lanes * V; i += blockDim.x) {
     const int lane = i / V, j = i % V, at = lane * V, half = a.rot / 2;
     // which pair of the head it is; one that stays turns by nothing
     const int pair = !NEAR ? at + j : j < V / 2 ? at / 2 + j : (half + at) / 2 + j - V / 2;
@@ -178,14 +179,14 @@ __device__ __forceinline__ void pack_store(const float2 (&p)[V / 2], T *to) {
 // A thread's own ring in shared memory: AHEAD stages of K accesses of V values, filled by asynchronous copies some heads ahead.
 // A thread reads only what it copied, so the ring needs no barrier.  (What is on its way would fill the registers otherwise:
 // with the next two or three heads in registers the forward pass took 22.6 and 21.5 us at 16 x 1024, 12 + 12 heads of 64.)
-template <typename T, int V, int K, int AHEAD>
+template <typename T, int V, int K, int AHEAD, int THREADS>
 struct Ring {
   static constexpr int kBytes = V * sizeof(T);
-  static constexpr size_t kSize = (size_t)AHEAD * K * kThreads * kBytes;
+  static constexpr size_t kSize = (size_t)AHEAD * K * THREADS * kBytes;
   uint32_t base;
   __device__ __forceinline__ explicit Ring(void *smem) : base(smem_u32(smem) + threadIdx.x * kBytes) {}
   __device__ __forceinline__ void copy(int stage, int k, const T *from) {
-    const uint32_t to = base + (stage * K + k) * (kThreads * kBytes);
+    const uint32_t to = base + (stage * K + k) * (THREADS * kBytes);
     if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
   }
@@ -193,7 +194,7 @@ struct Ring {
   // all but the last AHEAD - 1 commits have arrived
   __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory"); }
   __device__ __forceinline__ void read(int stage, int k, CdgVec<T, V> &v) const {
-    const uint32_t at = base + (stage * K + k) * (kThreads * kBytes);
+    const uint32_t at = base + (stage * K + k) * (THREADS * kBytes);
     if constexpr (kBytes == 16)
       asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(at) : "memory");
     else
@@ -225,7 +226,7 @@ __device__ __forceinline__ long long position(const Args &a, uint32_t b, uint32_
 
 // the first q_blocks blocks take queries, the others keys
 template <typename T, int V, bool NEAR>
-__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t tokens, uint32_t q_blocks, const __grid_constant__ Args a,
+__global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t tokens, uint32_t q_blocks, const __grid_constant__ Args a,
                                                                   const __grid_constant__ Frequencies f) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ __align__(16) Shared s;
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t token
   const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
   const float inv = 1.0f / (float)a.dim;
-  const uint32_t item = (blockIdx.x - (key ? q_blocks : 0)) * (kThreads / group) + threadIdx.x / group;
+  const uint32_t item = (blockIdx.x - (key ? q_blocks : 0)) * (kForward / group) + threadIdx.x / group;
   const bool some = item < tokens * a.parts[key].d;
   const uint32_t tok = some ? cdg_divide(item, a.parts[key]) : 0, share = item - tok * a.parts[key].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
   const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, count = some && mine ? (z.heads - (int)share + parts - 1) / parts : 0;
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(uint32_t token
   const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
   T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
   const long long x_step = parts * z.xs[2], y_step = parts * z.ys[2];
-  Ring<T, V, 2, kAhead> ring(dyn);
+  Ring<T, V, 2, kAhead, kForward> ring(dyn);
   auto request = [&](int h, int stage) {
     if (live && h < count) {
       ring.copy(stage, 0, x + at.x);
@@ -301,14 +302,14 @@ struct Grads {
   float *part;
 };
 template <typename T, int V, bool NEAR>
-__global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t tokens, int q_chunks, int k_chunks, const __grid_constant__ Args a,
+__global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(uint32_t tokens, int q_chunks, int k_chunks, const __grid_constant__ Args a,
                                                                       const __grid_constant__ Frequencies f, const __grid_constant__ Grads out) {
   __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int key = blockIdx.x >= (unsigned)q_chunks, chunk = blockIdx.x - key * q_chunks, chunks = key ? k_chunks : q_chunks;
   const Side &z = a.side[key];
-  const int group = a.group, groups = kThreads / group, lane = threadIdx.x & (group - 1);
+  const int group = a.group, groups = kBackward / group, lane = threadIdx.x & (group - 1);
   const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
   const float inv = 1.0f / (float)a.dim;
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t t
   const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts;
   const long long x_step = parts * z.xs[2], dy_step = parts * z.dys[2], y_step = parts * z.ys[2];
   extern __shared__ __align__(16) uint8_t dyn[];
-  Ring<T, V, 4, kAhead> ring(dyn);
+  Ring<T, V, 4, kAhead, kBackward> ring(dyn);
   float2 wa[V / 2] = {}, wb[V / 2] = {};
   load_shared<V, NEAR>(a, f, s);
   __syncthreads();
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t t
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < a.dim; c += kThreads) {
+  for (int c = threadIdx.x; c < a.dim; c += kBackward) {
     float t = 0.0f;
     for (int o = 0; o < kWarps; ++o) t += s.sums[o][c];
     s.total[c] = t;
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 2) rotary_backward_kernel(uint32_t t
   const uint32_t ctas = tc_cluster_size(), rank = tc_cluster_rank();
   if (ctas > 1) tc_cluster_sync();
   const int clusters = chunks / (int)ctas;
-  for (int c = (int)rank + threadIdx.x * (int)ctas; c < a.dim; c += kThreads * (int)ctas) {
+  for (int c = (int)rank + threadIdx.x * (int)ctas; c < a.dim; c += kBackward * (int)ctas) {
     float t = 0.0f;
     for (uint32_t o = 0; o < ctas; ++o) {
       uint32_t there;
@@ -493,35 +494,37 @@ int group_of(const cdgrab_rotary_shape *s) {
 }
 // Forward: shares that each token's heads are dealt out in, one by one, so that neighbouring groups read neighbouring heads: as many
 // as fill five blocks to an SM, a share for every two heads at most; each share computes the token's angles again.  (16 x 1024, 12 + 12
-// heads of 64, in one share 21.5 us, in two 20.5, in three 23.3.)
+// heads of 64: 15.6 us in one share, 16.8 in two; in blocks of 256 threads 19.7, of 64 threads 17.9: a block's tokens are its grain.)
 constexpr int kSms = 148;
 int parts_of(const cdgrab_rotary_shape *s, int heads) {
-  const long long tokens = (long long)s->batch * s->len, fill = 5ll * kSms * (kThreads / group_of(s));
+  const long long tokens = (long long)s->batch * s->len, fill = 5ll * kSms * (kForward / group_of(s));
   const long long most = (heads + 1) / 2, want = tokens > 0 ? fill / tokens : 1, parts = want < most ? want : most;
   if (parts <= 1) return 1;
   const long long per = (heads + parts - 1) / parts;
   return (int)((heads + per - 1) / per);
 }
-// Backward: how each worker's queries and keys are dealt out.  About 16,384 values to a block, but no more blocks than four rounds of
-// what is resident at once (two to an SM).  (4 x 4096, 16 + 4 heads of 128: 48 us, with 65,536 values 55.)
-// Up to two clusters' worth of blocks is made one cluster, which needs no second launch.  More blocks run on their own: in clusters
-// they wait for room for all eight (the same case: 57 us instead of 49).
-// A token's heads are dealt out in shares only where the blocks would otherwise lack tokens: a share of two heads spends as long on
-// its angles and on waiting as on the heads (3 x 357, 6 + 2 heads of 80 fp32: 17 us in three shares, 13 in one).
+// Backward: how each worker's queries and keys are dealt out.  About kChunk values to a block, an item to each group of lanes at
+// least, but no more blocks than four rounds of what is resident at once.  (2 x 300, 4 + 1 heads of 256 fp32: 6.8 us with 4096 values
+// to a block, 8.7 with 8192, 12.5 with 16,384.)
+// Where neither side of a worker has more than kOne values, each is one cluster, which needs no second launch: 20 us a call instead
+// of 24, although the eight blocks take 13 us of them and more blocks 8 (3 x 357, 6 + 2 heads of 80 fp32).  Larger ones run as blocks
+// of their own: in clusters they wait for room for all eight (4 x 4096, 16 + 4 heads of 128: 57 us instead of 49).
+// A token's heads are dealt out in shares of four or more only where the blocks would otherwise lack tokens: each share computes the
+// token's angles again and waits for its first head (the first case: 17 us in shares of two heads, 13 in one).
 struct Blocks { int q, k, cluster, parts[2]; };
-constexpr int kChunk = 16384, kCluster = 8;
+constexpr int kChunk = 4096, kCluster = 8, kOne = 1 << 18;
 Blocks blocks_of(const cdgrab_rotary_shape *s, int m) {
-  const long long tokens = (long long)s->batch / m * s->len, groups = kThreads / group_of(s);
-  const long long most = 8ll * kSms / m < 1 ? 1 : 8ll * kSms / m, resident = 2ll * kSms / m < 1 ? 1 : 2ll * kSms / m;
+  const long long tokens = (long long)s->batch / m * s->len, groups = kBackward / group_of(s);
+  const long long most = 4ll * kResident * kSms / m < 1 ? 1 : 4ll * kResident * kSms / m, resident = 1ll * kResident * kSms / m < 1 ? 1 : 1ll * kResident * kSms / m;
   long long want[2];
   for (int i = 0; i < 2; ++i) want[i] = (tokens * (i ? s->kv_heads : s->heads) * s->head_dim + kChunk - 1) / kChunk;
-  const bool one = (want[0] > want[1] ? want[0] : want[1]) <= 2 * kCluster;
+  const bool one = (want[0] > want[1] ? want[0] : want[1]) * kChunk <= kOne;
   Blocks b = {1, 1, 1, {1, 1}};
   long long rounds[2] = {1, 1};
   for (int i = 0; i < 2; ++i) {
     const int heads = i ? s->kv_heads : s->heads;
     if (tokens == 0 || heads == 0) continue;
-    const long long fill = one ? kCluster : want[i], blocks = fill < resident ? fill : resident, parts = blocks * groups / tokens, limit = (heads + 1) / 2;
+    const long long fill = one ? kCluster : want[i], blocks = fill < resident ? fill : resident, parts = blocks * groups / tokens, limit = (heads + 3) / 4;
     b.parts[i] = (int)(parts < 1 ? 1 : parts < limit ? parts : limit);
     const int per = (heads + b.parts[i] - 1) / b.parts[i];
     b.parts[i] = (heads + per - 1) / per;
@@ -609,7 +612,7 @@ extern "C" int cdgrab_rotary_forward(const cdgrab_rotary_shape *s, const void *q
   Frequencies f;
   fill(s, a, f);
   const long long tokens = (long long)s->batch * s->len;
-  const int groups = kThreads / a.group;
+  const int groups = kForward / a.group;
   unsigned blocks[2];
   for (int i = 0; i < 2; ++i) {
     const int heads = i ? s->kv_heads : s->heads;
@@ -621,9 +624,9 @@ extern "C" int cdgrab_rotary_forward(const cdgrab_rotary_shape *s, const void *q
   return by_kind(s, [&](auto t, auto v, auto near) {
     using T = decltype(t);
     static CdgPerDevice flags;
-    constexpr size_t smem = Ring<T, v(), 2, kAhead>::kSize;
+    constexpr size_t smem = Ring<T, v(), 2, kAhead, kForward>::kSize;
     const cudaError_t e = cdg_raise_smem_limit(flags, dev->index, rotary_forward_kernel<T, v(), near()>, smem);
-    return e != cudaSuccess ? cdg_launch_rc(e) : cdg_launch_rc(cdg_ops_launch(rotary_forward_kernel<T, v(), near()>, grid, kThreads, smem, st,
+    return e != cudaSuccess ? cdg_launch_rc(e) : cdg_launch_rc(cdg_ops_launch(rotary_forward_kernel<T, v(), near()>, grid, kForward, smem, st,
                                                                               (uint32_t)tokens, blocks[0], a, f));
   });
 }
@@ -660,9 +663,9 @@ extern "C" int cdgrab_rotary_backward(const cdgrab_rotary_shape *s, int m, const
   const int rc = by_kind(s, [&](auto t, auto v, auto near) {
     using T = decltype(t);
     static CdgPerDevice flags;
-    constexpr size_t smem = Ring<T, v(), 4, kAhead>::kSize;
+    constexpr size_t smem = Ring<T, v(), 4, kAhead, kBackward>::kSize;
     const cudaError_t e = cdg_raise_smem_limit(flags, dev->index, rotary_backward_kernel<T, v(), near()>, smem);
-    return e != cudaSuccess ? cdg_launch_rc(e) : tc_launch_cluster(rotary_backward_kernel<T, v(), near()>, dim3(n.q + n.k, m), n.cluster, kThreads,
+    return e != cudaSuccess ? cdg_launch_rc(e) : tc_launch_cluster(rotary_backward_kernel<T, v(), near()>, dim3(n.q + n.k, m), n.cluster, kBackward,
                                                                    smem, st, (uint32_t)tokens, n.q, n.k, a, f, out);
   });
   if (rc != CDGRAB_OK || (!dqw && !dkw) || (n.q == n.cluster && n.k == n.cluster)) return rc;
