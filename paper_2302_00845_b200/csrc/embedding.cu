@@ -354,18 +354,19 @@ struct Sums {
 
 constexpr uint32_t kNoKey = 0xffffffffu;
 constexpr int kWindow = 16;            // half a warp: its lanes hold a window and the next one
+constexpr int kSumThreads = 128;       // (a block stays until its longest window is done: with 256 the case below takes 53 us)
 
 // A warp to a window and 32 VEC NV columns; kAhead rows are on their way together.  What bounds it is instructions, not memory: a
 // warp goes through a few dozen rows in its life, so each case that is spelled out for each row in flight costs its fetching, and each
-// predicate on a load its issue slots (2 x 7892 tokens of 1377 bf16 columns: 124 us with all cases for eight rows, predicated, 53 in a
+// predicate on a load its issue slots (2 x 7892 tokens of 1377 bf16 columns: 124 us with all cases for eight rows, predicated, 47 in a
 // graph with sort and join so).
 template <typename T, typename G, int VEC, int NV>
-__global__ void __launch_bounds__(kThreads) run_sums_kernel(const __grid_constant__ Sums a, long long all) {
+__global__ void __launch_bounds__(kSumThreads) run_sums_kernel(const __grid_constant__ Sums a, long long all) {
   constexpr int kAhead = 4, kSlab = 32 * VEC * NV;
   cdg_grid_dep_wait();
   cdg_grid_dep_trigger();
   const int lane = threadIdx.x & 31;
-  const long long at = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);      // worker and window
+  const long long at = (long long)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);      // worker and window
   if (at >= all) return;
   const long long w = at / a.windows;
   const int win = (int)(at - w * a.windows);
@@ -653,7 +654,7 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
     using T = decltype(t);
     using G = decltype(g);
     auto go = [&](auto *kernel) {
-      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)((all + kWarps - 1) / kWarps), slabs(32 * vec * nv)), kThreads, 0, st, a, all));
+      return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)((all + kSumThreads / 32 - 1) / (kSumThreads / 32)), slabs(32 * vec * nv)), kSumThreads, 0, st, a, all));
     };
     switch (vec * 10 + nv) {
       case 81: return go(run_sums_kernel<T, G, 8, 1>);
