@@ -57,8 +57,7 @@ struct CdgVec {
     else
       asm volatile("ld.global.u16 %0, [%1];" : "=r"(w[0]) : "l"(p));
   }
-  // What p points to, or what was there before.  One instruction under a predicate: as a branch around a load, each of several
-  // loads was waited for before the next was issued.
+  // What p points to, or what was there before: one instruction under a predicate, no branch.
   __device__ __forceinline__ void load_if(bool yes, const T *p) {
     const int go = yes;
     if constexpr (kBytes == 32)

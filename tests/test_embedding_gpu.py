@@ -141,6 +141,16 @@ def test_several_rows_to_a_worker_and_strided_tokens():
     assert torch.equal(binding.embedding_backward(dy, t.reshape(-1), flat)[0], one)
 
 
+@pytest.mark.parametrize("m,rows", [(1, 1), (1, 200), (4, 50), (200, 1)])
+def test_single_tokens(m, rows):
+    """One token of each sequence, the newest of longer rows: rows of one token, far apart."""
+    long, table, dy = draw(m * rows, 9, 60, 72, "bf16")
+    dy = dy[:m * rows]
+    a = check(long[:, -1:], table, dy, m)
+    b = check(long[:, -1].contiguous().view(m, rows), table, dy, m)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_strides_and_what_lies_between():
     m, vocab, cols = 3, 50, 72
     t, table, dy = draw(m, 40, vocab, cols, "bf16")
