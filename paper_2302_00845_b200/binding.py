@@ -791,9 +791,13 @@ def dropout_backward(dy, p: float, seed: int, call: int = 0, step=0, out=None, d
 _ROTARY = struct.Struct("8idfi18q")          # cdgrab_rotary_shape
 
 
-def _geometry(t):
-    """What the checks ask of a tensor."""
-    return None if t is None else (t.shape, t.stride(), t.dtype)
+def _geometries(*tensors):
+    """What the checks ask of tensors."""
+    return [None if t is None else (t.shape, t.stride(), t.dtype) for t in tensors]
+
+
+def _addresses(*tensors):
+    return [None if t is None else t.data_ptr() for t in tensors]
 
 
 def _head_steps(g, name: str, shape, dtype):
@@ -880,10 +884,6 @@ def _rotary_backward_plan(dq, dk, dq_weight, dk_weight, *forward):
     return sh, bits, step, m, gcode, ws, int(lib().cdgrab_rotary_workspace_bytes(sh, m))
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
 def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: float = 10000.0, rotary_dim: int | None = None,
                    interleaved: bool = False, eps: float = 1e-6, lens=None, q_out=None, k_out=None, stream=None):
     """Every head of q [b][t][h][d] and k [b][t][h_kv][d] (float32 or bfloat16; any strides that are multiples of 8;
@@ -892,15 +892,14 @@ def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: flo
     positions: int32 or int64 [t] or [b][t], the token's index by default.  lens: int32 [b], the tokens in use; the
     others become zero.  Returns (q_out, k_out), which may be q and k."""
     handle, other = _place(stream, q, k, q_weight, k_weight, positions, lens, q_out, k_out)
-    sh, bits, step = _rotary_plan(
-        _geometry(q), _geometry(k), _geometry(q_weight), _geometry(k_weight), _geometry(positions), _geometry(lens),
-        _geometry(q_out), _geometry(k_out), base, rotary_dim, interleaved, eps)
+    sh, bits, step = _rotary_plan(*_geometries(q, k, q_weight, k_weight, positions, lens, q_out, k_out), base, rotary_dim,
+                                  interleaved, eps)
     if q_out is None:
         q_out = _empty_like(q, other)
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
-    rc = lib().cdgrab_rotary_forward(sh, q.data_ptr(), _at(k), _at(q_weight), _at(k_weight), _at(positions), bits, step, _at(lens),
-                                     q_out.data_ptr(), _at(k_out), handle)
+    pq, pk, pqw, pkw, pos, ln, pqo, pko = _addresses(q, k, q_weight, k_weight, positions, lens, q_out, k_out)
+    rc = lib().cdgrab_rotary_forward(sh, pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, handle)
     if rc:
         _check(rc, "cdgrab_rotary_forward")
     return q_out, k_out
@@ -915,17 +914,17 @@ def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, 
     k_out where given (dq and dk themselves, or views of one buffer)."""
     handle, other = _place(stream, dq, dk, q, k, q_weight, k_weight, positions, lens, dq_weight, dk_weight, q_out, k_out)
     sh, bits, step, m, gcode, ws, nbytes = _rotary_backward_plan(
-        _geometry(dq), _geometry(dk), _geometry(dq_weight), _geometry(dk_weight), _geometry(q), _geometry(k), _geometry(q_weight),
-        _geometry(k_weight), _geometry(positions), _geometry(lens), _geometry(q_out), _geometry(k_out), base, rotary_dim,
+        *_geometries(dq, dk, dq_weight, dk_weight, q, k, q_weight, k_weight, positions, lens, q_out, k_out), base, rotary_dim,
         interleaved, eps)
     if q_out is None:
         q_out = _empty_like(q, other)
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
     scratch = _scratch(q, nbytes, other) if nbytes else None
-    rc = lib().cdgrab_rotary_backward(
-        sh, m, dq.data_ptr(), _at(dk), q.data_ptr(), _at(k), _at(q_weight), _at(k_weight), _at(positions), bits, step, _at(lens),
-        q_out.data_ptr(), _at(k_out), gcode, _at(dq_weight), _at(dk_weight), ws, _at(scratch), nbytes, handle)
+    pdq, pdk, pq, pk, pqw, pkw, pos, ln, pqo, pko, pgq, pgk, work = _addresses(
+        dq, dk, q, k, q_weight, k_weight, positions, lens, q_out, k_out, dq_weight, dk_weight, scratch)
+    rc = lib().cdgrab_rotary_backward(sh, m, pdq, pdk, pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, gcode, pgq, pgk, ws, work,
+                                      nbytes, handle)
     if rc:
         _check(rc, "cdgrab_rotary_backward")
     return q_out, k_out

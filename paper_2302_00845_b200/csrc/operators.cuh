@@ -1,4 +1,4 @@
-// Shared by the training operators (layer norm, attention, orthogonalised update): the device they
+// Shared by the training operators (layer norm, attention, orthogonalised update, embedding, dropout, rotation): the device they
 // run on, their status word, and small device helpers.
 #pragma once
 
