@@ -634,6 +634,22 @@ int cdgrab_rotary_backward(const cdgrab_rotary_shape *shape, int m, const void *
                            void *dq_weight_dev, void *dk_weight_dev, long long worker_stride, void *workspace_dev,
                            long long workspace_bytes, void *stream);
 
+/*
+ * The calls above from embedding_forward on with their arguments in one record, in the same order, each in eight bytes:
+ * integers and pointers as signed 64-bit numbers (refused where the parameter is narrower and does not hold them), the
+ * seed without a sign, scale and p as doubles, the shape as the whole struct.  For callers that pay for every argument they
+ * pass.  CDGRAB_ERR_INVALID also for a NULL record and an unknown call.
+ */
+enum {
+  CDGRAB_CALL_EMBEDDING_FORWARD = 1,
+  CDGRAB_CALL_EMBEDDING_BACKWARD = 2,
+  CDGRAB_CALL_DROPOUT_FORWARD = 3,
+  CDGRAB_CALL_DROPOUT_BACKWARD = 4,
+  CDGRAB_CALL_ROTARY_FORWARD = 5,
+  CDGRAB_CALL_ROTARY_BACKWARD = 6
+};
+int cdgrab_call(int call, const void *record);
+
 /* What the training operators' kernels reported on the current device since the last call of this
  * function: CDGRAB_OK, CDGRAB_ERR_TIMEOUT when a bounded device-side wait expired (the outputs of
  * the calls since then are not valid), or CDGRAB_ERR_INVALID when an embedding call met a token outside its

@@ -99,6 +99,7 @@ SIGNATURES = {
     "cdgrab_orthogonalise": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_longlong, C.c_longlong,
                                        C.c_int, C.POINTER(C.c_float), C.c_float, C.c_void_p, C.c_longlong,
                                        C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p]),
+    "cdgrab_call": (C.c_int, [C.c_int, C.c_char_p]),
     "cdgrab_embedding_forward": (C.c_int, [C.c_longlong, C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_longlong,
                                            C.c_longlong, C.c_float, C.c_int, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p,
                                            C.c_longlong, C.c_void_p]),
@@ -644,6 +645,11 @@ def orthogonalise(g, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: floa
     return o
 
 
+# The calls below go through cdgrab_call: converting an argument takes 0.15 us, of the ten that a small call takes.
+_EMBEDDING_FORWARD, _EMBEDDING_BACKWARD, _DROPOUT_FORWARD, _DROPOUT_BACKWARD, _ROTARY_FORWARD, _ROTARY_BACKWARD = range(1, 7)
+_EMBEDDING_FORWARD_RECORD, _EMBEDDING_BACKWARD_RECORD = struct.Struct("8qd7q"), struct.Struct("9qd11q")
+_DROPOUT_FORWARD_RECORD, _DROPOUT_BACKWARD_RECORD = struct.Struct("10qdQ4q"), struct.Struct("8qdQ4q")
+_ROTARY_FORWARD_RECORD, _ROTARY_BACKWARD_RECORD = struct.Struct("11q"), struct.Struct("20q")      # after the shape
 _NO_PADDING = -2 ** 63
 
 
@@ -695,9 +701,9 @@ def embedding_forward(tokens, table, scale: float = 1.0, padding: int | None = N
         y, ys, ycode = out, _row_stride(out, "out", rows, cols), _code(out, "out")
         if dtype is not None and dtype != out.dtype:
             raise ValueError("out: of another type than dtype")
-    rc = lib().cdgrab_embedding_forward(
+    rc = lib().cdgrab_call(_EMBEDDING_FORWARD, _EMBEDDING_FORWARD_RECORD.pack(
         groups, length, cols, vocab, bits, tokens.data_ptr(), ts, _padding(padding), scale, code,
-        table.data_ptr(), _row_stride(table, "table", vocab, cols), ycode, y.data_ptr(), ys, handle)
+        table.data_ptr(), _row_stride(table, "table", vocab, cols), ycode, y.data_ptr(), ys, handle))
     if rc:
         _check(rc, "cdgrab_embedding_forward")
     return y
@@ -727,9 +733,9 @@ def embedding_backward(dy, tokens, dtable, scale: float = 1.0, padding: int | No
     L = lib()
     nbytes = L.cdgrab_embedding_workspace_bytes(m, groups // m * length, cols, vocab)
     scratch = _scratch(dtable, nbytes, other)
-    rc = L.cdgrab_embedding_backward(
+    rc = L.cdgrab_call(_EMBEDDING_BACKWARD, _EMBEDDING_BACKWARD_RECORD.pack(
         m, groups // m, length, cols, vocab, bits, tokens.data_ptr(), ts, _padding(padding), scale,
-        code, dy.data_ptr(), dys, gcode, dtable.data_ptr(), ws, rs, 1 if accumulate else 0, scratch.data_ptr(), max(16, nbytes), handle)
+        code, dy.data_ptr(), dys, gcode, dtable.data_ptr(), ws, rs, 1 if accumulate else 0, scratch.data_ptr(), max(16, nbytes), handle))
     if rc:
         _check(rc, "cdgrab_embedding_backward")
     return dtable
@@ -757,18 +763,18 @@ def _dropout(x, residual, out, dtype, name, p, seed, call, step, stream):
         y, ys, ycode = out, _row_stride(out, "out", rows, cols), _code(out, "out")
         if dtype is not None and dtype != out.dtype:
             raise ValueError("out: of another type than dtype")
-    res, rs = None, 0
+    res, rs = 0, 0
     if residual is not None:
         if residual.dtype != y.dtype:
             raise ValueError("residual: the type of the result")
         res, rs = residual.data_ptr(), _row_stride(residual, "residual", rows, cols)
-    at = None if steps is None else steps.data_ptr()
+    at = 0 if steps is None else steps.data_ptr()
     if name == "cdgrab_dropout_forward":
-        rc = lib().cdgrab_dropout_forward(rows, cols, code, x.data_ptr(), _row_stride(x, "x", rows, cols), ycode, res, rs,
-                                          y.data_ptr(), ys, p, seed, call, step, at, handle)
+        rc = lib().cdgrab_call(_DROPOUT_FORWARD, _DROPOUT_FORWARD_RECORD.pack(
+            rows, cols, code, x.data_ptr(), _row_stride(x, "x", rows, cols), ycode, res, rs, y.data_ptr(), ys, p, seed, call, step, at, handle))
     else:
-        rc = lib().cdgrab_dropout_backward(rows, cols, code, x.data_ptr(), _row_stride(x, "dy", rows, cols), ycode, y.data_ptr(),
-                                           ys, p, seed, call, step, at, handle)
+        rc = lib().cdgrab_call(_DROPOUT_BACKWARD, _DROPOUT_BACKWARD_RECORD.pack(
+            rows, cols, code, x.data_ptr(), _row_stride(x, "dy", rows, cols), ycode, y.data_ptr(), ys, p, seed, call, step, at, handle))
     if rc:
         _check(rc, name)
     return y
@@ -797,7 +803,7 @@ def _geometries(*tensors):
 
 
 def _addresses(*tensors):
-    return [None if t is None else t.data_ptr() for t in tensors]
+    return [0 if t is None else t.data_ptr() for t in tensors]
 
 
 def _head_steps(g, name: str, shape, dtype):
@@ -821,7 +827,7 @@ def _head_steps(g, name: str, shape, dtype):
 # half of a call's time.
 @functools.lru_cache(maxsize=512)
 def _rotary_plan(q, k, q_weight, k_weight, positions, lens, q_out, k_out, base, rotary_dim, interleaved, eps):
-    """(cdgrab_rotary_shape, position bits, position stride) from tensors' geometries."""
+    """(bytes of cdgrab_rotary_shape, position bits, position stride) from tensors' geometries."""
     if len(q[0]) != 4 or (k is not None and len(k[0]) != 4):
         raise ValueError("q, k: [batch][token][head][head_dim]")
     qs, ks = q[0], None if k is None else k[0]
@@ -850,9 +856,9 @@ def _rotary_plan(q, k, q_weight, k_weight, positions, lens, q_out, k_out, base, 
             raise ValueError("positions: those of a sequence have to be contiguous")
         bits = 64 if dtype == torch.int64 else 32
         step = stride[0] if len(shape) == 2 and b > 1 else 0
-    return RotaryShape.from_buffer_copy(_ROTARY.pack(
+    return _ROTARY.pack(
         b, t, h, hk, d, rotary_dim, 1 if interleaved else 0, _CODES[dt], base, eps, 0, *_head_steps(q, "q", qs, dt),
-        *_head_steps(k, "k", ks, dt), *_head_steps(q_out, "q_out", qs, dt), *_head_steps(k_out, "k_out", ks, dt), *_NONE, *_NONE)), bits, step
+        *_head_steps(k, "k", ks, dt), *_head_steps(q_out, "q_out", qs, dt), *_head_steps(k_out, "k_out", ks, dt), *_NONE, *_NONE), bits, step
 
 
 @functools.lru_cache(maxsize=512)
@@ -881,7 +887,7 @@ def _rotary_backward_plan(dq, dk, dq_weight, dk_weight, *forward):
         first, m, gcode, ws = g, shape[0], _CODES[dtype], stride[0] if shape[0] > 1 else d
         if m < 1 or b % m:
             raise ValueError(f"{b} sequences are not {m} workers' equal shares")
-    return sh, bits, step, m, gcode, ws, int(lib().cdgrab_rotary_workspace_bytes(sh, m))
+    return bytes(sh), bits, step, m, gcode, ws, int(lib().cdgrab_rotary_workspace_bytes(sh, m))
 
 
 def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: float = 10000.0, rotary_dim: int | None = None,
@@ -899,7 +905,7 @@ def rotary_forward(q, k, q_weight=None, k_weight=None, positions=None, base: flo
     if k is not None and k_out is None:
         k_out = _empty_like(k, other)
     pq, pk, pqw, pkw, pos, ln, pqo, pko = _addresses(q, k, q_weight, k_weight, positions, lens, q_out, k_out)
-    rc = lib().cdgrab_rotary_forward(sh, pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, handle)
+    rc = lib().cdgrab_call(_ROTARY_FORWARD, sh + _ROTARY_FORWARD_RECORD.pack(pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, handle))
     if rc:
         _check(rc, "cdgrab_rotary_forward")
     return q_out, k_out
@@ -923,8 +929,8 @@ def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, 
     scratch = _scratch(q, nbytes, other) if nbytes else None
     pdq, pdk, pq, pk, pqw, pkw, pos, ln, pqo, pko, pgq, pgk, work = _addresses(
         dq, dk, q, k, q_weight, k_weight, positions, lens, q_out, k_out, dq_weight, dk_weight, scratch)
-    rc = lib().cdgrab_rotary_backward(sh, m, pdq, pdk, pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, gcode, pgq, pgk, ws, work,
-                                      nbytes, handle)
+    rc = lib().cdgrab_call(_ROTARY_BACKWARD, sh + _ROTARY_BACKWARD_RECORD.pack(
+        m, pdq, pdk, pq, pk, pqw, pkw, pos, bits, step, ln, pqo, pko, gcode, pgq, pgk, ws, work, nbytes, handle))
     if rc:
         _check(rc, "cdgrab_rotary_backward")
     return q_out, k_out

@@ -1,5 +1,7 @@
 // State shared by the training operators: per-device lookups and the status word their kernels raise.
 #include <atomic>
+#include <climits>
+#include <cstring>
 
 #include "operators.cuh"
 #include "ptx.cuh"
@@ -52,4 +54,124 @@ extern "C" int cdgrab_operators_status(void) {
   if (cudaMemcpy(&st, d->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
   if (st != 0 && cudaMemset(d->status, 0, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
   return st & CDG_ST_TIMEOUT ? CDGRAB_ERR_TIMEOUT : st & CDG_ST_INDEX ? CDGRAB_ERR_INVALID : CDGRAB_OK;
+}
+
+namespace {
+// the fields of a record, eight bytes each, in turn
+struct Record {
+  const unsigned char *p;
+  bool ok = true;            // every number fitted its parameter
+  template <typename T> T take() { T v; memcpy(&v, p, sizeof(T)); p += sizeof(T); return v; }
+  long long wide() { return take<long long>(); }
+  int narrow() {
+    const long long v = wide();
+    ok = ok && v >= INT_MIN && v <= INT_MAX;
+    return (int)v;
+  }
+  unsigned word() {
+    const long long v = wide();
+    ok = ok && v >= 0 && v <= (long long)UINT_MAX;
+    return (unsigned)v;
+  }
+  void *pointer() { return reinterpret_cast<void *>(wide()); }
+};
+}  // namespace
+
+extern "C" int cdgrab_call(int call, const void *record) {
+  if (!record) return CDGRAB_ERR_INVALID;
+  Record r = {static_cast<const unsigned char *>(record)};
+  // (fields are taken one statement after another: the order of a call's arguments is not given)
+  switch (call) {
+    case CDGRAB_CALL_EMBEDDING_FORWARD: {
+      const long long groups = r.wide(), length = r.wide();
+      const int cols = r.narrow(), vocab = r.narrow(), bits = r.narrow();
+      const void *tokens = r.pointer();
+      const long long token_stride = r.wide(), padding = r.wide();
+      const double scale = r.take<double>();
+      const int dtype = r.narrow();
+      const void *table = r.pointer();
+      const long long table_stride = r.wide();
+      const int out_dtype = r.narrow();
+      void *y = r.pointer();
+      const long long y_stride = r.wide();
+      void *stream = r.pointer();
+      return !r.ok ? CDGRAB_ERR_INVALID
+                   : cdgrab_embedding_forward(groups, length, cols, vocab, bits, tokens, token_stride, padding, (float)scale, dtype, table,
+                                              table_stride, out_dtype, y, y_stride, stream);
+    }
+    case CDGRAB_CALL_EMBEDDING_BACKWARD: {
+      const int m = r.narrow();
+      const long long groups = r.wide(), length = r.wide();
+      const int cols = r.narrow(), vocab = r.narrow(), bits = r.narrow();
+      const void *tokens = r.pointer();
+      const long long token_stride = r.wide(), padding = r.wide();
+      const double scale = r.take<double>();
+      const int dtype = r.narrow();
+      const void *dy = r.pointer();
+      const long long dy_stride = r.wide();
+      const int grad_dtype = r.narrow();
+      void *dtable = r.pointer();
+      const long long worker_stride = r.wide(), row_stride = r.wide();
+      const int accumulate = r.narrow();
+      void *workspace = r.pointer();
+      const long long bytes = r.wide();
+      void *stream = r.pointer();
+      return !r.ok ? CDGRAB_ERR_INVALID
+                   : cdgrab_embedding_backward(m, groups, length, cols, vocab, bits, tokens, token_stride, padding, (float)scale, dtype, dy,
+                                               dy_stride, grad_dtype, dtable, worker_stride, row_stride, accumulate, workspace, bytes, stream);
+    }
+    case CDGRAB_CALL_DROPOUT_FORWARD:
+    case CDGRAB_CALL_DROPOUT_BACKWARD: {
+      const long long rows = r.wide(), cols = r.wide();
+      const int dtype = r.narrow();
+      const void *x = r.pointer();
+      const long long xs = r.wide();
+      const int out_dtype = r.narrow();
+      const bool forward = call == CDGRAB_CALL_DROPOUT_FORWARD;
+      const void *res = forward ? r.pointer() : nullptr;
+      const long long rs = forward ? r.wide() : 0;
+      void *y = r.pointer();
+      const long long ys = r.wide();
+      const double p = r.take<double>();
+      const unsigned long long seed = r.take<unsigned long long>();
+      const unsigned which = r.word(), step = r.word();
+      const long long *step_dev = static_cast<const long long *>(r.pointer());
+      void *stream = r.pointer();
+      return !r.ok ? CDGRAB_ERR_INVALID
+             : forward ? cdgrab_dropout_forward(rows, cols, dtype, x, xs, out_dtype, res, rs, y, ys, p, seed, which, step, step_dev, stream)
+                       : cdgrab_dropout_backward(rows, cols, dtype, x, xs, out_dtype, y, ys, p, seed, which, step, step_dev, stream);
+    }
+    case CDGRAB_CALL_ROTARY_FORWARD: {
+      const cdgrab_rotary_shape shape = r.take<cdgrab_rotary_shape>();
+      const void *q = r.pointer(), *k = r.pointer();
+      const float *qw = static_cast<const float *>(r.pointer()), *kw = static_cast<const float *>(r.pointer());
+      const void *pos = r.pointer();
+      const int bits = r.narrow();
+      const long long pos_stride = r.wide();
+      const int32_t *lens = static_cast<const int32_t *>(r.pointer());
+      void *qo = r.pointer(), *ko = r.pointer(), *stream = r.pointer();
+      return !r.ok ? CDGRAB_ERR_INVALID : cdgrab_rotary_forward(&shape, q, k, qw, kw, pos, bits, pos_stride, lens, qo, ko, stream);
+    }
+    case CDGRAB_CALL_ROTARY_BACKWARD: {
+      const cdgrab_rotary_shape shape = r.take<cdgrab_rotary_shape>();
+      const int m = r.narrow();
+      const void *dq = r.pointer(), *dk = r.pointer(), *q = r.pointer(), *k = r.pointer();
+      const float *qw = static_cast<const float *>(r.pointer()), *kw = static_cast<const float *>(r.pointer());
+      const void *pos = r.pointer();
+      const int bits = r.narrow();
+      const long long pos_stride = r.wide();
+      const int32_t *lens = static_cast<const int32_t *>(r.pointer());
+      void *qo = r.pointer(), *ko = r.pointer();
+      const int grad_dtype = r.narrow();
+      void *dqw = r.pointer(), *dkw = r.pointer();
+      const long long worker_stride = r.wide();
+      void *workspace = r.pointer();
+      const long long bytes = r.wide();
+      void *stream = r.pointer();
+      return !r.ok ? CDGRAB_ERR_INVALID
+                   : cdgrab_rotary_backward(&shape, m, dq, dk, q, k, qw, kw, pos, bits, pos_stride, lens, qo, ko, grad_dtype, dqw, dkw,
+                                            worker_stride, workspace, bytes, stream);
+    }
+    default: return CDGRAB_ERR_INVALID;
+  }
 }

@@ -506,8 +506,8 @@ int parts_of(const cdgrab_rotary_shape *s, int heads) {
 // Backward: how each worker's queries and keys are dealt out.  About kChunk values to a block, an item to each group of lanes at
 // least, but no more blocks than four rounds of what is resident at once.  (2 x 300, 4 + 1 heads of 256 fp32: 6.8 us with 4096 values
 // to a block, 8.7 with 8192, 12.5 with 16,384.)
-// Where neither side of a worker has more than kOne values, each is one cluster, which needs no second launch: 20 us a call instead
-// of 24, although the eight blocks take 13 us of them and more blocks 8 (3 x 357, 6 + 2 heads of 80 fp32).  Larger ones run as blocks
+// Where neither side of a worker has more than kOne values, each is one cluster, which needs no second launch: 19 us a call instead
+// of 23, although the eight blocks take 13 us of them and more blocks 8 (3 x 357, 6 + 2 heads of 80 fp32).  Larger ones run as blocks
 // of their own: in clusters they wait for room for all eight (4 x 4096, 16 + 4 heads of 128: 57 us instead of 49).
 // A token's heads are dealt out in shares of four or more only where the blocks would otherwise lack tokens: each share computes the
 // token's angles again and waits for its first head (the first case: 17 us in shares of two heads, 13 in one).

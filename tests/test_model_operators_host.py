@@ -171,3 +171,32 @@ def test_rotary_forms_against_autograd(rotary_dim, interleaved):
         (dx, _), (dw, _) = ref.rotary(x, w, *args, dy=dy, m=b)
         assert torch.allclose(dx[i], xs.grad, rtol=1e-9, atol=1e-12) and torch.allclose(dw[i], ws.grad, rtol=1e-9, atol=1e-12)
     del ref.U16[torch.float64]
+
+
+def test_records(lib):
+    """cdgrab_call takes the same arguments in the same order: each kind of call gets as far as the call itself, and a number that
+    its parameter does not hold is refused."""
+    import struct
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    shape = bytes(rotary_shape())
+    good = {1: ("8qd7q", [2, 4, 8, 10, 64, P, 4, -1, 1.0, 0, P, 8, 0, P, 8, 0]),
+            2: ("9qd11q", [2, 1, 4, 8, 10, 64, P, 4, -1, 1.0, 0, P, 8, 0, P, 80, 8, 0, P, 1 << 40, 0]),
+            3: ("10qdQ4q", [4, 8, 0, P, 8, 0, P, 8, P, 8, 0.1, 2 ** 64 - 1, 2 ** 32 - 1, 2 ** 32 - 1, 0, 0]),
+            4: ("8qdQ4q", [4, 8, 0, P, 8, 0, P, 8, 0.1, 1, 2, 3, 0, 0]),
+            5: ("11q", [P, P, P, P, 0, 0, 0, 0, P, P, 0]),
+            6: ("20q", [2, P, P, P, P, P, P, 0, 0, 0, 0, P, P, 0, P, P, 64, 0, 0, 0])}
+    call = lambda n, fmt, v: lib.cdgrab_call(n, (shape if n > 4 else b"") + struct.pack(fmt, *v))  # noqa: E731
+    for n, (fmt, v) in good.items():
+        assert call(n, fmt, v) == binding.ERR_DEVICE, n
+    bad = [(1, 2, 2 ** 32 + 8), (1, 3, -2 ** 32 + 10), (1, 4, 2 ** 32 + 64), (1, 5, 0), (1, 6, 3), (1, 8, math.inf), (1, 8, 1e300), (1, 9, 2 ** 32), (1, 11, 7),
+           (1, 12, 2), (1, 13, 0), (1, 14, 7), (2, 0, 2 ** 32 + 2), (2, 2, -1), (2, 7, 3), (2, 12, 7), (2, 13, 2 ** 33), (2, 15, 79), (2, 16, 7), (2, 17, 2), (2, 18, 0),
+           (2, 19, 15), (3, 0, -1), (3, 4, 7), (3, 5, 2 ** 32), (3, 7, 7), (3, 9, 7), (3, 10, 1.5), (3, 12, 2 ** 32), (3, 13, -1), (3, 14, P + 4), (4, 4, 7), (4, 7, 7),
+           (4, 8, -0.5), (4, 10, 2 ** 32), (4, 12, P + 4), (5, 0, P + 8), (5, 1, 0), (5, 2, P + 2), (5, 7, P + 2), (5, 9, 0), (6, 0, 2 ** 32 + 2), (6, 1, 0), (6, 4, P + 4),
+           (6, 11, 0), (6, 13, 2 ** 32), (6, 13, 2), (6, 16, 63)]
+    for n, at, value in bad:
+        fmt, v = good[n]
+        assert call(n, fmt, v[:at] + [value] + v[at + 1:]) == binding.ERR_INVALID, (n, at, value)
+    assert lib.cdgrab_call(1, None) == binding.ERR_INVALID
+    for n in (0, 7, -1):
+        assert lib.cdgrab_call(n, bytes(400)) == binding.ERR_INVALID
