@@ -241,14 +241,14 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
   const uint32_t item = (blockIdx.x - (key ? q_blocks : 0)) * (kForward / group) + threadIdx.x / group;
   const bool some = item < tokens * a.parts[key].d;
   const uint32_t tok = some ? cdg_divide(item, a.parts[key]) : 0, share = item - tok * a.parts[key].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, count = some && mine ? (z.heads - (int)share + parts - 1) / parts : 0;
-  const bool live = count > 0 && (!a.lens || (int)t < a.lens[b]);
+  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, count = some ? (z.heads - (int)share + parts - 1) / parts : 0;
+  const bool used = some && (!a.lens || (int)t < a.lens[b]);
   const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
   T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
   const long long x_step = parts * z.xs[2], y_step = parts * z.ys[2];
   Ring<T, V, 2, kAhead, kForward> ring(dyn);
   auto request = [&](int h, int stage) {
-    if (live && h < count) {
+    if (used && mine && h < count) {
       ring.copy(stage, 0, x + at.x);
       ring.copy(stage, 1, x + at.y);
     }
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
     CdgVec<T, V> va, vb;
     va.zero();
     vb.zero();
-    if (live && h < count) {
+    if (used && mine && h < count) {
       ring.read(stage, 0, va);
       ring.read(stage, 1, vb);
     }
@@ -278,14 +278,16 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
     for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
     const float total = head_sum(sum.x + sum.y, group);
     if (h >= count) continue;
-    // (0 where there is nothing: with eps = 0 it would be infinite)
-    const float rstd = live ? rsqrtf(total * inv + a.eps) : 0.0f;
+    if (used) {                              // (else zeros, whatever epsilon and the weights are)
+      const float rstd = rsqrtf(total * inv + a.eps);
 #pragma unroll
-    for (int j = 0; j < V / 2; ++j) {
-      p[j] = mul2(p[j], make_float2(rstd, rstd));
-      q[j] = mul2(q[j], make_float2(rstd, rstd));
+      for (int j = 0; j < V / 2; ++j) {
+        p[j] = mul2(p[j], make_float2(rstd, rstd));
+        q[j] = mul2(q[j], make_float2(rstd, rstd));
+      }
+      turn.apply(p, q);
     }
-    turn.apply(p, q);
+    if (!mine) continue;
     pack_store<T, V>(p, y + at.x);
     pack_store<T, V>(q, y + at.y);
     y += y_step;
@@ -328,13 +330,13 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
     const bool some = item < items;
     const uint32_t local = some ? cdg_divide(item, a.parts[key]) : 0, share = item - local * a.parts[key].d;
     const uint32_t tok = blockIdx.y * tokens + local, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-    const int count = some && mine ? (z.heads - (int)share + parts - 1) / parts : 0;
-    const bool live = some && mine && (!a.lens || (int)t < a.lens[b]);
+    const int count = some ? (z.heads - (int)share + parts - 1) / parts : 0;
+    const bool used = some && (!a.lens || (int)t < a.lens[b]);
     const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
     const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + share * z.dys[2];
     T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
     auto request = [&](int h, int stage) {
-      if (live && h < count) {
+      if (used && mine && h < count) {
         ring.copy(stage, 0, x + at.x);
         ring.copy(stage, 1, x + at.y);
         ring.copy(stage, 2, dy + at.x);
@@ -354,7 +356,7 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
       float2 p[V / 2], q[V / 2], g[V / 2], e[V / 2], sum = make_float2(0.0f, 0.0f);
       CdgVec<T, V> va, vb, da, db;
       va.zero(); vb.zero(); da.zero(); db.zero();
-      if (live && h < count) {
+      if (used && mine && h < count) {
         ring.read(stage, 0, va);
         ring.read(stage, 1, vb);
         ring.read(stage, 2, da);
@@ -383,21 +385,22 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
         }
       }
       const float2 both = head_sums(make_float2(sum.x + sum.y, along.x + along.y), group);
-      // (0 where there is nothing: with eps = 0 it would be infinite)
-      const float rstd = live && h < count ? rsqrtf(both.x * inv + a.eps) : 0.0f;
-      const float off = -(both.y * inv * rstd * rstd) * rstd;
+      if (h >= count) continue;
+      if (used) {
+        const float rstd = rsqrtf(both.x * inv + a.eps);
+        const float off = -(both.y * inv * rstd * rstd) * rstd;
 #pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        wa[j] = fma2(ga[j], make_float2(rstd, rstd), wa[j]);
-        wb[j] = fma2(gb[j], make_float2(rstd, rstd), wb[j]);
-        p[j] = fma2(p[j], make_float2(off, off), mul2(g[j], make_float2(rstd, rstd)));
-        q[j] = fma2(q[j], make_float2(off, off), mul2(e[j], make_float2(rstd, rstd)));
-      }
-      if (h < count) {
-        pack_store<T, V>(p, y + at.x);
-        pack_store<T, V>(q, y + at.y);
-        y += y_step;
-      }
+        for (int j = 0; j < V / 2; ++j) {
+          wa[j] = fma2(ga[j], make_float2(rstd, rstd), wa[j]);
+          wb[j] = fma2(gb[j], make_float2(rstd, rstd), wb[j]);
+          p[j] = fma2(p[j], make_float2(off, off), mul2(g[j], make_float2(rstd, rstd)));
+          q[j] = fma2(q[j], make_float2(off, off), mul2(e[j], make_float2(rstd, rstd)));
+        }
+      }                                      // (else p and q are zeros, as there was nothing to read)
+      if (!mine) continue;
+      pack_store<T, V>(p, y + at.x);
+      pack_store<T, V>(q, y + at.y);
+      y += y_step;
     }
   }
   if (!out.w[0] && !out.w[1]) return;
