@@ -608,6 +608,8 @@ typedef struct {
  *                outputs there are zero.
  *   q_out, k_out may be q and k themselves, with the same strides
  * A NaN or an infinity in a head in use spoils that head, in the backward pass the worker's sums for the weight as well.
+ * Finite heads of any size do not, where the results are finite: those whose squares, or whose products with a gradient,
+ * leave 32 bits are brought into range first (and take longer, with their neighbours).
  */
 int cdgrab_rotary_forward(const cdgrab_rotary_shape *shape, const void *q_dev, const void *k_dev,
                           const float *q_weight_dev, const float *k_weight_dev, const void *positions_dev,

@@ -14,8 +14,9 @@
 namespace {
 
 constexpr int kForward = 128, kBackward = 256;           // threads to a block
+constexpr int kForwardResident = 7;        // blocks of the forward pass to an SM: 72 registers a thread (78 leave six blocks: 18.2 us for 15.6)
 constexpr int kWarps = kBackward / 32;
-constexpr int kResident = 2;               // blocks of the backward pass to an SM: 124 registers a thread
+constexpr int kResident = 2;               // blocks of the backward pass to an SM: 125 registers a thread
 constexpr int kMaxDim = 256, kMaxPairs = kMaxDim / 2;
 constexpr int kAhead = 4;                  // heads on their way
 
@@ -218,16 +219,111 @@ __device__ __forceinline__ float2 head_sums(float2 v, int group) {
   return v;
 }
 
+// A head on its way through the backward pass: a lane's values, their gradients turned back, times the weight.
+template <int V>
+struct Head {
+  float2 p[V / 2], q[V / 2], g[V / 2], e[V / 2], ga[V / 2], gb[V / 2];
+  // sum x^2 and sum h x: with x = n / rstd, both sums before rstd is known
+  template <typename T, bool NEAR>
+  __device__ __forceinline__ float2 sums(const CdgVec<T, V> &va, const CdgVec<T, V> &vb, const CdgVec<T, V> &da, const CdgVec<T, V> &db,
+                                         const TurnBack<V, NEAR> &turn, const float *weight_a, const float *weight_b, int step, int group) {
+    unpack(va, p); unpack(vb, q);
+    unpack(da, g); unpack(db, e);
+    turn.apply(g, e);
+    float2 sum = make_float2(0.0f, 0.0f), along = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+      ga[j] = mul2(g[j], p[j]);
+      gb[j] = mul2(e[j], q[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const float4 u = *reinterpret_cast<const float4 *>(weight_a + j * step), v = *reinterpret_cast<const float4 *>(weight_b + j * step);
+      const float2 w[4] = {make_float2(u.x, u.y), make_float2(u.z, u.w), make_float2(v.x, v.y), make_float2(v.z, v.w)};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        along = fma2(ga[2 * j + i], w[i], fma2(gb[2 * j + i], w[2 + i], along));
+        g[2 * j + i] = mul2(g[2 * j + i], w[i]);
+        e[2 * j + i] = mul2(e[2 * j + i], w[2 + i]);
+      }
+    }
+    return head_sums(make_float2(sum.x + sum.y, along.x + along.y), group);
+  }
+  // p, q: their gradients; the weights' sums with them
+  __device__ __forceinline__ void finish(float square, float along, float inv, float2 (&wa)[V / 2], float2 (&wb)[V / 2]) {
+    const float rstd = rsqrtf(square);
+    const float off = -(along * inv * rstd * rstd) * rstd;
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      wa[j] = fma2(ga[j], make_float2(rstd, rstd), wa[j]);
+      wb[j] = fma2(gb[j], make_float2(rstd, rstd), wb[j]);
+      p[j] = fma2(p[j], make_float2(off, off), mul2(g[j], make_float2(rstd, rstd)));
+      q[j] = fma2(q[j], make_float2(off, off), mul2(e[j], make_float2(rstd, rstd)));
+    }
+  }
+};
+
+// A head whose squares, or whose products with its gradient, may leave 32 bits although the results do not is brought to a size near
+// one first: by a power of two, which changes no digit, taken from its largest value (or epsilon's root, so that epsilon stays in
+// range with it).  n = x scale rstd,  1 / sqrt(sum x^2 / D + eps) = scale rstd.  Only the group's lanes take part.
+// The loops over heads stop where a group of the warp has such a head, and the warp goes on in a loop of its own, so that the first one
+// pays for the question alone: 2 % of the large backward pass (4 x 4096, 16 + 4 heads of 128: 50.2 us in a graph, 49.1 without), where a
+// branch for each head took 4 to 6 %.
+__device__ __forceinline__ unsigned group_lanes(int group) { return (0xffffffffu >> (32 - group)) << (threadIdx.x & 31 & ~(group - 1)); }
+template <int V>
+__device__ __forceinline__ float2 careful_norm(float2 (&p)[V / 2], float2 (&q)[V / 2], const Args &a) {
+  const unsigned lanes = group_lanes(a.group);
+  float most = sqrtf(a.eps);
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j)
+    most = fmaxf(most, fmaxf(fmaxf(fabsf(p[j].x), fabsf(p[j].y)), fmaxf(fabsf(q[j].x), fabsf(q[j].y))));
+  for (int o = 1; o < a.group; o <<= 1) most = fmaxf(most, __shfl_xor_sync(lanes, most, o));
+  const uint32_t exponent = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+  const float scale = __uint_as_float((254 - exponent) << 23);
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) {
+    p[j] = mul2(p[j], make_float2(scale, scale));
+    q[j] = mul2(q[j], make_float2(scale, scale));
+    sum += p[j].x * p[j].x + p[j].y * p[j].y + (q[j].x * q[j].x + q[j].y * q[j].y);
+  }
+  for (int o = 1; o < a.group; o <<= 1) sum += __shfl_xor_sync(lanes, sum, o);
+  const float rstd = rsqrtf(sum / (float)a.dim + a.eps * scale * scale);
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) {
+    p[j] = mul2(p[j], make_float2(rstd, rstd));
+    q[j] = mul2(q[j], make_float2(rstd, rstd));
+  }
+  return make_float2(scale, rstd);
+}
+// The mean squares (epsilon included) between which the squares of a head lose nothing that counts.
+constexpr float kForwardLow = 0x1p-60f, kForwardHigh = 0x1p120f;
+// Backward, x takes the place of n until the norm is known, and its third power comes in.  With |x| up to sqrt(D) 2^12 and 1 / rstd
+// from 2^-12 on, what products with the gradient lose below 2^-149 stays below 2^-122 times the weight in the results, and a sum up
+// to kMostSum leaves room for the powers of rstd.
+constexpr float kBackwardLow = 0x1p-24f, kBackwardHigh = 0x1p24f, kMostSum = 0x1p80f;
+
 __device__ __forceinline__ long long position(const Args &a, uint32_t b, uint32_t t) {
   if (!a.pos) return t;
   const long long at = b * a.pos_stride + t;
   return a.pos_bits == 64 ? static_cast<const long long *>(a.pos)[at] : static_cast<const int *>(a.pos)[at];
 }
 
+// what is not in use: zeros, whatever epsilon and the weights are
+template <typename T, int V>
+__device__ __forceinline__ void store_zeros(T *y, long long step, int heads, int2 at) {
+  const float2 none[V / 2] = {};
+  for (int h = 0; h < heads; ++h, y += step) {
+    pack_store<T, V>(none, y + at.x);
+    pack_store<T, V>(none, y + at.y);
+  }
+}
+
 // the first q_blocks blocks take queries, the others keys
 template <typename T, int V, bool NEAR>
-__global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t tokens, uint32_t q_blocks, const __grid_constant__ Args a,
-                                                                  const __grid_constant__ Frequencies f) {
+__global__ void __launch_bounds__(kForward, kForwardResident) rotary_forward_kernel(uint32_t tokens, uint32_t q_blocks, const __grid_constant__ Args a,
+                                                                                    const __grid_constant__ Frequencies f) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ __align__(16) Shared s;
   cdg_grid_dep_wait();
@@ -241,14 +337,16 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
   const uint32_t item = (blockIdx.x - (key ? q_blocks : 0)) * (kForward / group) + threadIdx.x / group;
   const bool some = item < tokens * a.parts[key].d;
   const uint32_t tok = some ? cdg_divide(item, a.parts[key]) : 0, share = item - tok * a.parts[key].d, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, count = some ? (z.heads - (int)share + parts - 1) / parts : 0;
+  const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts, heads = some ? (z.heads - (int)share + parts - 1) / parts : 0;
   const bool used = some && (!a.lens || (int)t < a.lens[b]);
+  const int count = used && mine ? heads : 0;
   const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
   T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
   const long long x_step = parts * z.xs[2], y_step = parts * z.ys[2];
+  if (!used && mine) store_zeros<T, V>(y, y_step, heads, at);
   Ring<T, V, 2, kAhead, kForward> ring(dyn);
   auto request = [&](int h, int stage) {
-    if (used && mine && h < count) {
+    if (h < count) {
       ring.copy(stage, 0, x + at.x);
       ring.copy(stage, 1, x + at.y);
     }
@@ -261,13 +359,14 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
   __syncthreads();
   Turn<V, NEAR> turn;
   turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0, s.weight[key][0] + (mine ? lane * 4 : 0), s.weight[key][1] + (mine ? lane * 4 : 0));
+  int done = -1;                             // heads that are done where one needs care
   for (int h = 0, stage = 0; h < per; ++h, stage = stage + 1 == kAhead ? 0 : stage + 1) {      // (as often for every group)
     request(h + kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
     ring.wait();
     CdgVec<T, V> va, vb;
     va.zero();
     vb.zero();
-    if (used && mine && h < count) {
+    if (h < count) {
       ring.read(stage, 0, va);
       ring.read(stage, 1, vb);
     }
@@ -277,20 +376,56 @@ __global__ void __launch_bounds__(kForward) rotary_forward_kernel(uint32_t token
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
     const float total = head_sum(sum.x + sum.y, group);
+    const float square = total * inv + a.eps, rstd = rsqrtf(square);
+    if (__any_sync(0xffffffffu, h < count && !(square >= kForwardLow && square <= kForwardHigh))) {
+      done = h;
+      break;
+    }
     if (h >= count) continue;
-    if (used) {                              // (else zeros, whatever epsilon and the weights are)
-      const float rstd = rsqrtf(total * inv + a.eps);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      p[j] = mul2(p[j], make_float2(rstd, rstd));
+      q[j] = mul2(q[j], make_float2(rstd, rstd));
+    }
+    turn.apply(p, q);
+    pack_store<T, V>(p, y + at.x);
+    pack_store<T, V>(q, y + at.y);
+    y += y_step;
+  }
+  if (__builtin_expect(done < 0, 1)) return;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
+  y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
+  for (int h = done; h < per; ++h) {
+    const bool on = used && h < heads;
+    CdgVec<T, V> va, vb;
+    va.zero();
+    vb.zero();
+    if (on && mine) {
+      va.load(x + h * x_step + at.x);
+      vb.load(x + h * x_step + at.y);
+    }
+    float2 p[V / 2], q[V / 2], sum = make_float2(0.0f, 0.0f);
+    unpack(va, p);
+    unpack(vb, q);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
+    const float square = head_sum(sum.x + sum.y, group) * inv + a.eps, rstd = rsqrtf(square);
+    if (!on) continue;
+    if (square >= kForwardLow && square <= kForwardHigh) {
 #pragma unroll
       for (int j = 0; j < V / 2; ++j) {
         p[j] = mul2(p[j], make_float2(rstd, rstd));
         q[j] = mul2(q[j], make_float2(rstd, rstd));
       }
-      turn.apply(p, q);
+    } else {
+      careful_norm<V>(p, q, a);
     }
-    if (!mine) continue;
-    pack_store<T, V>(p, y + at.x);
-    pack_store<T, V>(q, y + at.y);
-    y += y_step;
+    turn.apply(p, q);
+    if (mine) {
+      pack_store<T, V>(p, y + h * y_step + at.x);
+      pack_store<T, V>(q, y + h * y_step + at.y);
+    }
   }
 }
 
@@ -325,18 +460,22 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
   load_shared<V, NEAR>(a, f, s);
   __syncthreads();
   const float *weight_a = s.weight[key][0] + (mine ? lane * 4 : 0), *weight_b = s.weight[key][1] + (mine ? lane * 4 : 0);
-  for (uint32_t r = r0; r < r1; ++r) {
+  uint32_t r = r0;
+  int done = -1;                             // heads of the last item that are done where one needs care
+  for (; r < r1; ++r) {
     const uint32_t item = r * groups + threadIdx.x / group;
     const bool some = item < items;
     const uint32_t local = some ? cdg_divide(item, a.parts[key]) : 0, share = item - local * a.parts[key].d;
     const uint32_t tok = blockIdx.y * tokens + local, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
-    const int count = some ? (z.heads - (int)share + parts - 1) / parts : 0;
+    const int heads = some ? (z.heads - (int)share + parts - 1) / parts : 0;
     const bool used = some && (!a.lens || (int)t < a.lens[b]);
+    const int count = used && mine ? heads : 0;
     const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
     const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + share * z.dys[2];
     T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
+    if (!used && mine) store_zeros<T, V>(y, y_step, heads, at);
     auto request = [&](int h, int stage) {
-      if (used && mine && h < count) {
+      if (h < count) {
         ring.copy(stage, 0, x + at.x);
         ring.copy(stage, 1, x + at.y);
         ring.copy(stage, 2, dy + at.x);
@@ -353,54 +492,95 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
     for (int h = 0, stage = 0; h < per; ++h, stage = stage + 1 == kAhead ? 0 : stage + 1) {
       request(h + kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
       ring.wait();
-      float2 p[V / 2], q[V / 2], g[V / 2], e[V / 2], sum = make_float2(0.0f, 0.0f);
       CdgVec<T, V> va, vb, da, db;
       va.zero(); vb.zero(); da.zero(); db.zero();
-      if (used && mine && h < count) {
+      if (h < count) {
         ring.read(stage, 0, va);
         ring.read(stage, 1, vb);
         ring.read(stage, 2, da);
         ring.read(stage, 3, db);
       }
-      unpack(va, p); unpack(vb, q);
-      unpack(da, g); unpack(db, e);
-      // with x = n / rstd: both sums before rstd is known
-      turn.apply(g, e);
-      float2 along = make_float2(0.0f, 0.0f), ga[V / 2], gb[V / 2];
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        sum = fma2(p[j], p[j], fma2(q[j], q[j], sum));
-        ga[j] = mul2(g[j], p[j]);
-        gb[j] = mul2(e[j], q[j]);
+      Head<V> head;
+      const float2 both = head.sums(va, vb, da, db, turn, weight_a, weight_b, a.lanes * 4, group);
+      const float square = both.x * inv + a.eps;
+      const bool fits = square >= kBackwardLow && square <= kBackwardHigh && fabsf(both.y) <= kMostSum;
+      if (__any_sync(0xffffffffu, h < count && !fits)) {
+        done = h;
+        break;
       }
-#pragma unroll
-      for (int j = 0; j < V / 4; ++j) {
-        const float4 u = *reinterpret_cast<const float4 *>(weight_a + j * a.lanes * 4), v = *reinterpret_cast<const float4 *>(weight_b + j * a.lanes * 4);
-        const float2 w[4] = {make_float2(u.x, u.y), make_float2(u.z, u.w), make_float2(v.x, v.y), make_float2(v.z, v.w)};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          along = fma2(ga[2 * j + i], w[i], fma2(gb[2 * j + i], w[2 + i], along));
-          g[2 * j + i] = mul2(g[2 * j + i], w[i]);
-          e[2 * j + i] = mul2(e[2 * j + i], w[2 + i]);
-        }
-      }
-      const float2 both = head_sums(make_float2(sum.x + sum.y, along.x + along.y), group);
       if (h >= count) continue;
-      if (used) {
-        const float rstd = rsqrtf(both.x * inv + a.eps);
-        const float off = -(both.y * inv * rstd * rstd) * rstd;
-#pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-          wa[j] = fma2(ga[j], make_float2(rstd, rstd), wa[j]);
-          wb[j] = fma2(gb[j], make_float2(rstd, rstd), wb[j]);
-          p[j] = fma2(p[j], make_float2(off, off), mul2(g[j], make_float2(rstd, rstd)));
-          q[j] = fma2(q[j], make_float2(off, off), mul2(e[j], make_float2(rstd, rstd)));
-        }
-      }                                      // (else p and q are zeros, as there was nothing to read)
-      if (!mine) continue;
-      pack_store<T, V>(p, y + at.x);
-      pack_store<T, V>(q, y + at.y);
+      head.finish(square, both.y, inv, wa, wb);
+      pack_store<T, V>(head.p, y + at.x);
+      pack_store<T, V>(head.q, y + at.y);
       y += y_step;
+    }
+    if (done >= 0) break;
+  }
+  // From the first head on that needs care in any of a warp's groups, the warp goes on here.
+  if (__builtin_expect(done >= 0, 0)) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (; r < r1; ++r, done = 0) {
+      const uint32_t item = r * groups + threadIdx.x / group;
+      const bool some = item < items;
+      const uint32_t local = some ? cdg_divide(item, a.parts[key]) : 0, share = item - local * a.parts[key].d;
+      const uint32_t tok = blockIdx.y * tokens + local, b = cdg_divide(tok, a.len), t = tok - b * a.len.d;
+      const int heads = some ? (z.heads - (int)share + parts - 1) / parts : 0;
+      const bool used = some && (!a.lens || (int)t < a.lens[b]);
+      const T *x = static_cast<const T *>(z.x) + b * z.xs[0] + t * z.xs[1] + share * z.xs[2];
+      const T *dy = static_cast<const T *>(z.dy) + b * z.dys[0] + t * z.dys[1] + share * z.dys[2];
+      T *y = static_cast<T *>(z.y) + b * z.ys[0] + t * z.ys[1] + share * z.ys[2];
+      if (!used && mine && done == 0) store_zeros<T, V>(y, y_step, heads, at);
+      TurnBack<V, NEAR> turn;
+      turn.set(a, s, some ? position(a, b, t) : 0, mine ? lane : 0);
+      for (int h = done; h < per; ++h) {
+        const bool on = used && h < heads;
+        CdgVec<T, V> va, vb, da, db;
+        va.zero(); vb.zero(); da.zero(); db.zero();
+        if (on && mine) {
+          va.load(x + h * x_step + at.x);
+          vb.load(x + h * x_step + at.y);
+          da.load(dy + h * dy_step + at.x);
+          db.load(dy + h * dy_step + at.y);
+        }
+        Head<V> head;
+        const float2 both = head.sums(va, vb, da, db, turn, weight_a, weight_b, a.lanes * 4, group);
+        const float square = both.x * inv + a.eps;
+        if (!on) continue;
+        if (square >= kBackwardLow && square <= kBackwardHigh && fabsf(both.y) <= kMostSum) {
+          head.finish(square, both.y, inv, wa, wb);
+        } else {
+          // in the formula's own order: the norm, then the products with n
+          const float2 norm = careful_norm<V>(head.p, head.q, a);
+          // (the gradient is read again: kept, it would take registers from the loop above)
+          CdgVec<T, V> dc, dd;
+          dc.zero(); dd.zero();
+          if (mine) {
+            dc.load(dy + h * dy_step + at.x);
+            dd.load(dy + h * dy_step + at.y);
+          }
+          float2 g[V / 2], e[V / 2];
+          unpack(dc, g); unpack(dd, e);
+          turn.apply(g, e);
+          float sum = 0.0f;
+#pragma unroll
+          for (int j = 0; j < V / 2; ++j) {
+            wa[j] = fma2(g[j], head.p[j], wa[j]);
+            wb[j] = fma2(e[j], head.q[j], wb[j]);
+            sum += head.g[j].x * head.p[j].x + head.g[j].y * head.p[j].y + (head.e[j].x * head.q[j].x + head.e[j].y * head.q[j].y);
+          }
+          for (int o = 1; o < group; o <<= 1) sum += __shfl_xor_sync(group_lanes(group), sum, o);
+          const float2 mean = make_float2(-sum * inv, -sum * inv), scale = make_float2(norm.x, norm.x), rstd = make_float2(norm.y, norm.y);
+#pragma unroll
+          for (int j = 0; j < V / 2; ++j) {
+            head.p[j] = mul2(mul2(fma2(head.p[j], mean, head.g[j]), rstd), scale);
+            head.q[j] = mul2(mul2(fma2(head.q[j], mean, head.e[j]), rstd), scale);
+          }
+        }
+        if (mine) {
+          pack_store<T, V>(head.p, y + h * y_step + at.x);
+          pack_store<T, V>(head.q, y + h * y_step + at.y);
+        }
+      }
     }
   }
   if (!out.w[0] && !out.w[1]) return;
