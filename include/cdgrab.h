@@ -655,8 +655,8 @@ int cdgrab_call(int call, const void *record);
 /* What the training operators' kernels reported on the current device since the last call of this
  * function: CDGRAB_OK, CDGRAB_ERR_TIMEOUT when a bounded device-side wait expired (the outputs of
  * the calls since then are not valid), or CDGRAB_ERR_INVALID when an embedding call met a token outside its
- * vocabulary.  Synchronises the device and clears the word; not to be called
- * while a stream capture is open. */
+ * vocabulary.  Where both happened the time-out is returned, and the other by the next call.  Synchronises the
+ * device and clears what it returns; not to be called while a stream capture is open. */
 int cdgrab_operators_status(void);
 
 /* How long a device-side wait of the calls that follow (of every thread) may last, in SM clock cycles up to

@@ -937,7 +937,8 @@ def rotary_backward(dq, dk, q, k, q_weight=None, k_weight=None, positions=None, 
 
 
 def operators_status() -> int:
-    """cdgrab_operators_status: what the training operators' kernels reported so far (read and cleared)."""
+    """cdgrab_operators_status: what the training operators' kernels reported so far, an expired wait first (read and
+    cleared, one report a call)."""
     return int(lib().cdgrab_operators_status())
 
 

@@ -52,8 +52,14 @@ extern "C" int cdgrab_operators_status(void) {
   if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
   int st = 0;
   if (cudaMemcpy(&st, d->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
-  if (st != 0 && cudaMemset(d->status, 0, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return CDGRAB_ERR_CUDA; }
-  return st & CDG_ST_TIMEOUT ? CDGRAB_ERR_TIMEOUT : st & CDG_ST_INDEX ? CDGRAB_ERR_INVALID : CDGRAB_OK;
+  // one report a call: what else the word holds stays for the next (written before this returns: a later launch may report on a stream
+  // that does not wait for the copy)
+  const int said = st & CDG_ST_TIMEOUT ? CDG_ST_TIMEOUT : st, rest = st & ~said;
+  if (st != 0 && (cudaMemcpy(d->status, &rest, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)) {
+    cudaGetLastError();
+    return CDGRAB_ERR_CUDA;
+  }
+  return said & CDG_ST_TIMEOUT ? CDGRAB_ERR_TIMEOUT : said & CDG_ST_INDEX ? CDGRAB_ERR_INVALID : CDGRAB_OK;
 }
 
 namespace {
