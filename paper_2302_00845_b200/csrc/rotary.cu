@@ -450,7 +450,8 @@ __global__ void __launch_bounds__(kBackward, kResident) rotary_backward_kernel(u
   const bool mine = lane < a.lanes;
   const int2 at = places<V>(a, lane);
   const float inv = 1.0f / (float)a.dim;
-  const uint32_t items = tokens * a.parts[key].d, rounds = (items + groups - 1) / groups;           // each group an item
+  // each group an item; a side that is not there has none: its block only writes the zeros of its weight's gradient
+  const uint32_t items = z.heads > 0 ? tokens * a.parts[key].d : 0, rounds = (items + groups - 1) / groups;
   const uint32_t r0 = (uint32_t)((unsigned long long)rounds * chunk / chunks), r1 = (uint32_t)((unsigned long long)rounds * (chunk + 1) / chunks);
   const int parts = a.parts[key].d, per = (z.heads + parts - 1) / parts;
   const long long x_step = parts * z.xs[2], dy_step = parts * z.dys[2], y_step = parts * z.ys[2];
