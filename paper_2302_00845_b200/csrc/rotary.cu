@@ -738,17 +738,24 @@ void fill(const cdgrab_rotary_shape *s, Args &a, Frequencies &f) {
   a.lanes = lanes_of(s);
   a.group = group_of(s);
   a.dim = s->head_dim; a.rot = s->rotary_dim; a.eps = s->eps;
-  // (a power for each pair costs more than the launch: each thread keeps its last table)
-  static thread_local struct { double base; int rot; Frequencies f; } last = {};
-  if (last.base != s->base || last.rot != s->rotary_dim) {
+  // (a table of powers costs twice the rest of a small call: each thread keeps the last ones, replaced in turn)
+  struct Kept { double base; int rot; Frequencies f; };
+  static thread_local Kept kept[8] = {};
+  static thread_local unsigned next = 0;
+  const Kept *found = nullptr;
+  for (const Kept &k : kept)
+    if (k.base == s->base && k.rot == s->rotary_dim) found = &k;
+  if (!found) {
+    Kept &k = kept[next++ % 8];
     for (int i = 0; i < kMaxPairs; ++i) {
       long double whole, turns = 2 * i < s->rotary_dim ? std::pow((long double)s->base, -2.0L * i / s->rotary_dim) / (2.0L * kPi) : 0.0L;
-      last.f.turns[i] = (unsigned long long)(std::modf(turns, &whole) * 0x1p64L);
+      k.f.turns[i] = (unsigned long long)(std::modf(turns, &whole) * 0x1p64L);
     }
-    last.base = s->base;
-    last.rot = s->rotary_dim;
+    k.base = s->base;
+    k.rot = s->rotary_dim;
+    found = &k;
   }
-  f = last.f;
+  f = found->f;
 }
 
 // f(T(), V, NEAR) for a shape's kernel
