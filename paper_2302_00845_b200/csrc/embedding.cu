@@ -656,13 +656,15 @@ extern "C" int cdgrab_embedding_backward(int m, long long groups, long long leng
     auto go = [&](auto *kernel) {
       return cdg_launch_rc(cdg_ops_launch(kernel, dim3((unsigned)((all + kSumThreads / 32 - 1) / (kSumThreads / 32)), slabs(32 * vec * nv)), kSumThreads, 0, st, a, all));
     };
+    if constexpr (sizeof(T) == 2) {          // (of fp32 they would be 32 bytes to a lane)
+      if (vec == 4 && nv == 2) return go(run_sums_kernel<T, G, 4, 2>);
+      if (vec == 2 && nv == 4) return go(run_sums_kernel<T, G, 2, 4>);
+    }
     switch (vec * 10 + nv) {
       case 81: return go(run_sums_kernel<T, G, 8, 1>);
       case 41: return go(run_sums_kernel<T, G, 4, 1>);
-      case 42: return go(run_sums_kernel<T, G, 4, 2>);
       case 21: return go(run_sums_kernel<T, G, 2, 1>);
       case 22: return go(run_sums_kernel<T, G, 2, 2>);
-      case 24: return go(run_sums_kernel<T, G, 2, 4>);
       case 11: return go(run_sums_kernel<T, G, 1, 1>);
       case 12: return go(run_sums_kernel<T, G, 1, 2>);
       default: return go(run_sums_kernel<T, G, 1, 4>);
