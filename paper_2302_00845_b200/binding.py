@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import operator
 import os
 import struct
 
@@ -742,7 +743,12 @@ def embedding_backward(dy, tokens, dtable, scale: float = 1.0, padding: int | No
 
 
 def _dropout(x, residual, out, dtype, name, p, seed, call, step, stream):
-    steps = None if isinstance(step, int) else step
+    steps = None
+    if not isinstance(step, int):
+        if hasattr(step, "get_device"):
+            steps = step
+        else:
+            step = operator.index(step)
     handle, other = _place(stream, x, residual, out, steps)
     if x.dim() != 2:
         raise ValueError(f"[rows][cols], not {tuple(x.shape)}")
