@@ -529,8 +529,8 @@ int cdgrab_embedding_forward(long long groups, long long length, int cols, int v
  *   dtable[i][v] = scale * sum of dy over worker i's tokens that are v
  * every row of every worker's table written, zero where no token names it: that worker's part of the gather
  * buffer.  With accumulate = 1 the sums are added to what dtable holds (the gradient of a product that shares
- * the matrix) and the other rows are left as they are.  The sums run over the tokens in the order of their
- * positions, whatever the grid: results are the same bits every time.
+ * the matrix) and the other rows are left as they are.  The order of the sums depends on the tokens alone,
+ * whatever the grid: results are the same bits every time.
  *   dy           of `dtype`, a row for every token, dy_stride (>= cols) apart; rows of padding are not used.  Neither
  *                dy nor the tokens may overlap dtable.
  *   dtable       of grad_dtype: worker i's row v starts at i * worker_stride + v * row_stride;
@@ -578,7 +578,8 @@ int cdgrab_dropout_backward(long long rows, long long cols, int dtype, const voi
  *   n = x * rstd,  rstd = 1 / sqrt(sum x^2 / head_dim + eps),  g = n * weight,
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = position * base^(-2 i / rotary_dim)
  * over the pairs i of the first rotary_dim values of g: (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with
- * interleaved = 1.  Angles are reduced in 64 bits: positions of millions keep their digits.
+ * interleaved = 1.  Angles are reduced in 64 bits: positions of millions keep their digits.  (With a base below 1,
+ * where they are many turns a position, an angle t is within 2^-62 t.)
  *
  * Shape (HOST struct): strides in elements for batch, token and head; the head's values are contiguous.
  *   batch, len, heads, kv_heads   >= 0 (nothing to do where batch or len is 0, or both head counts); heads up to

@@ -6,8 +6,9 @@
 // every worker's table, most of them zero, and reads dy once.  It runs in three launches:
 //   1. each worker's tokens are sorted by value, stably, by a cluster of its own, while the other blocks clear the tables;
 //   2. runs of equal tokens are summed in the order of their positions, a warp to 16 sorted positions and up to 256 columns;
-//   3. runs that go on over more than two such windows, which step 2 leaves as a sum for each window, are joined in order.
-// No sum depends on the order in which blocks run, and nothing is added to memory by atomics.
+//   3. runs that go on over more than two such windows, which step 2 leaves as a sum for each window, are joined: eight warps take
+//      every eighth window each, and their sums are added in order.
+// The order of a sum depends on the tokens alone, not on the order in which blocks run, and nothing is added to memory by atomics.
 #include <cmath>
 
 #include "rows.cuh"

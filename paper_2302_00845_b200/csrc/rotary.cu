@@ -20,8 +20,9 @@ constexpr int kResident = 2;               // blocks of the backward pass to an 
 constexpr int kMaxDim = 256, kMaxPairs = kMaxDim / 2;
 constexpr int kAhead = 4;                  // heads on their way
 
-// Turns per position of each pair, base^(-2 i / rotary_dim) / (2 pi), less whole turns, in units of 2^-64: a position, which is whole,
-// times that is the angle modulo a turn, exactly but for the unit's half, in integer arithmetic that wraps.
+// Turns per position of each pair, base^(-2 i / rotary_dim) / (2 pi), less whole turns, in units of 2^-64, cut off: a position, which is
+// whole, times that is the angle modulo a turn, to two units a position, in integer arithmetic that wraps.  (With a base below 1 the
+// turns are many, and 64 bits hold less of their fraction.)
 struct Frequencies { unsigned long long turns[kMaxPairs]; };
 
 constexpr long double kPi = 3.14159265358979323846264338327950288L;
@@ -268,7 +269,7 @@ struct Head {
 // one first: by a power of two, which changes no digit, taken from its largest value (or epsilon's root, so that epsilon stays in
 // range with it).  n = x scale rstd,  1 / sqrt(sum x^2 / D + eps) = scale rstd.  Only the group's lanes take part.
 // The loops over heads stop where a group of the warp has such a head, and the warp goes on in a loop of its own, so that the first one
-// pays for the question alone: 2 % of the large backward pass (4 x 4096, 16 + 4 heads of 128: 50.2 us in a graph, 49.1 without), where a
+// pays for the question alone: 2 to 3 % of the large backward pass (4 x 4096, 16 + 4 heads of 128: 50.2 us in a graph, 49.1 without), where a
 // branch for each head took 4 to 6 %.
 __device__ __forceinline__ unsigned group_lanes(int group) { return (0xffffffffu >> (32 - group)) << (threadIdx.x & 31 & ~(group - 1)); }
 template <int V>
